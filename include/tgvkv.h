@@ -355,6 +355,128 @@ int tgvkv_decode(const tgvkv_desc* desc, const uint16_t* q, const uint16_t* k_ro
 /* Kernels one tgvkv_decode call launches (2).  -1 on bad arguments. */
 int tgvkv_decode_launches(const tgvkv_desc* desc);
 
+/* ---- the paged cache ---------------------------------------------------
+ *
+ * A growing cache for what follows the eviction: the next question's tokens,
+ * decode steps, drafted tokens.  After an eviction every (layer, KV head) holds
+ * a set of its own size, so the unit here is the set s = b * H_kv + g of
+ * sequence b (a request of a batch, or a layer of one request) and KV head g.
+ * Set s owns the pages page_table[s][0..max_pages) of a shared pool; its slot j
+ * is pool row page_table[s][j / page_size] * page_size + j % page_size, in the K
+ * pool and in the V pool alike.  Pages of one set may lie anywhere in the pool;
+ * a page may appear in several sets (a shared prefix) as long as nothing writes
+ * it.  Entries past a set's length are never used.
+ *
+ * Formats (desc->format).  A pool is [n_pages][page_size] rows:
+ *   TGVKV_CACHE_BF16  d bf16 values, bit copies of what was written;
+ *   TGVKV_CACHE_INT8  d codes of 8 bits, two's complement;
+ *   TGVKV_CACHE_INT4  d / 2 bytes, code + 8 in 4 bits, the even element in the
+ *                     low half of a byte.
+ * The integer formats have a scale pool [n_pages][page_size][d / 32] of bytes,
+ * one per 32 consecutive values: E = e + 127 for the scale 2^e, the smallest
+ * power of two (e >= -126) with max |x| <= Q * 2^e, Q = 127 (8 bits) or 7 (4 bits;
+ * there e <= 120, larger magnitudes saturate at 7 * 2^120).  Codes are x / 2^e
+ * rounded to nearest, ties to even.  A group that holds an infinity or a NaN
+ * has E = 255 and codes of 0 and reads back as NaN.  code * 2^e is exact in
+ * bf16: the only rounding of the integer formats is the quantisation itself.
+ *
+ * Faults found on the device set TGVKV_STATUS_INDEX and touch nothing out of
+ * range: a length outside [0, max_pages * page_size], token or row offsets that
+ * do not start at 0, decrease or exceed their tensors, a set that would grow past
+ * its pages, a page number outside [0, n_pages) that is needed. */
+#define TGVKV_CACHE_BF16 0
+#define TGVKV_CACHE_INT8 1
+#define TGVKV_CACHE_INT4 2
+
+typedef struct tgvkv_cache_desc {
+    int32_t B;              /* sequences */
+    int32_t H_q;            /* query heads */
+    int32_t H_kv;           /* KV heads; H_q % H_kv == 0, at most 128 query heads each */
+    int32_t d;              /* head dimension: 64 or 128 */
+    int32_t page_size;      /* slots per page: 16, 32, 64, 128 or 256 */
+    int32_t n_pages;        /* pages of the pool */
+    int32_t max_pages;      /* page-table entries of a set */
+    int32_t format;         /* TGVKV_CACHE_* */
+    float   softmax_scale;  /* logits = softmax_scale * <q, k>; <= 0 means 1/sqrt(d) */
+} tgvkv_cache_desc;
+/* Limits (TGVKV_ERR_UNSUPPORTED above them): B * H_kv <= 65535; n_pages *
+ * page_size < 2^31; max_pages * page_size <= 2^30; B * H_kv * max_pages *
+ * page_size < 2^35. */
+
+/* The pools of a cache, device memory, 16-byte aligned; the scales are NULL for
+ * TGVKV_CACHE_BF16. */
+typedef struct tgvkv_cache_pools {
+    void* k;
+    void* v;
+    uint8_t* k_scale;
+    uint8_t* v_scale;
+} tgvkv_cache_pools;
+
+/* Bytes of workspace the calls below need (0 when the descriptor is rejected).
+ * Its first word is the status word that tgvkv_status reads; zero that word (or
+ * call tgvkv_cache_workspace_init) once before the first call.  Calls that may
+ * overlap on the GPU must not share a workspace. */
+size_t tgvkv_cache_workspace_size(const tgvkv_cache_desc* desc);
+int tgvkv_cache_workspace_init(const tgvkv_cache_desc* desc, void* workspace, void* stream);
+
+/* Append new tokens.  Sequence b's new tokens are rows tok_offsets[b] ..
+ * tok_offsets[b+1] of k_new and v_new; row t of KV head g goes to slot
+ * lens[s] + (t - tok_offsets[b]) of set s = b * H_kv + g, and lens_out[s] =
+ * lens[s] + tok_offsets[b+1] - tok_offsets[b].
+ * k_new, v_new: bf16, element (t, g, c) at t * tok_stride + g * head_stride + c
+ *   (each tensor with its own strides, in elements, multiples of 8; slices of a
+ *   fused projection need no copy), 16-byte aligned, holding n_tokens rows;
+ * tok_offsets: int32 [B + 1]; page_table: int32 [B * H_kv][max_pages];
+ * lens, lens_out: int32 [B * H_kv], which must not overlap. */
+int tgvkv_cache_write(const tgvkv_cache_desc* desc, const tgvkv_cache_pools* pools,
+                      const int32_t* page_table, const int32_t* lens, const uint16_t* k_new,
+                      int64_t k_tok_stride, int64_t k_head_stride, const uint16_t* v_new,
+                      int64_t v_tok_stride, int64_t v_head_stride, int64_t n_tokens,
+                      const int32_t* tok_offsets, int32_t* lens_out, void* workspace,
+                      void* stream);
+
+/* Append the rows of a CSR cache (k_out, v_out and offsets of tgvkv_evict, with
+ * B = L): rows offsets[s] .. offsets[s+1] of k_rows and v_rows (bf16 [n_rows][d])
+ * go to the slots lens[s] on of set s.  Other arguments as in
+ * tgvkv_cache_write; offsets: int64 [B * H_kv + 1]. */
+int tgvkv_cache_write_rows(const tgvkv_cache_desc* desc, const tgvkv_cache_pools* pools,
+                           const int32_t* page_table, const int32_t* lens, const uint16_t* k_rows,
+                           const uint16_t* v_rows, int64_t n_rows, const int64_t* offsets,
+                           int32_t* lens_out, void* workspace, void* stream);
+
+/* Read rows back as bf16: rows offsets[s] .. offsets[s+1] of k_out and v_out
+ * (bf16 [n_rows][d]) become the slots first[s] on of set s (first NULL: from slot
+ * 0), code * 2^e exactly.  A contiguous cache for another tgvkv_evict, or one to
+ * keep elsewhere.  Rows whose slot has no page are left alone (and reported);
+ * n_rows: rows the outputs hold. */
+int tgvkv_cache_read(const tgvkv_cache_desc* desc, const tgvkv_cache_pools* pools,
+                     const int32_t* page_table, const int32_t* first, const int64_t* offsets,
+                     uint16_t* k_out, uint16_t* v_out, int64_t n_rows, void* workspace,
+                     void* stream);
+
+/* Attention of a chunk of new tokens over the cache, their own K and V already
+ * written: the n = tok_offsets[b+1] - tok_offsets[b] new tokens of sequence b are
+ * the last n of the lens[s] slots of each of its sets, and token i of them, row
+ * t = tok_offsets[b] + i, attends to the slots before and including its own:
+ *   out[t][h] = sum_{j <= lens[s] - n + i} softmax_j(softmax_scale <q[t][h], k_j>) v_j
+ * with s = b * H_kv + h / G.  One token per sequence is a decode step; lengths and
+ * chunk sizes may differ by sequence, and n may be 0.  A token that sees no slot
+ * (lens[s] < n) gives 0.
+ * q: bf16, element (t, h, c) at t * q_tok_stride + h * q_head_stride + c (strides
+ *   in elements, multiples of 8), 16-byte aligned, n_tokens rows;
+ * max_q: an upper bound of the new tokens of a sequence (a larger chunk sets
+ *   TGVKV_STATUS_INDEX and its tokens past max_q are not computed);
+ * out: bf16 [n_tokens][H_q][d], 16-byte aligned.
+ * bf16 products with fp32 accumulation and softmax; the attention weights enter
+ * the value product rounded to bf16, and out is rounded to bf16.  The slots of
+ * a set must hold finite values up to its length; what lies in its pages past
+ * the length does not matter, whatever it is. */
+int tgvkv_chunk_attention(const tgvkv_cache_desc* desc, const tgvkv_cache_pools* pools,
+                          const int32_t* page_table, const int32_t* lens, const uint16_t* q,
+                          int64_t q_tok_stride, int64_t q_head_stride, int64_t n_tokens,
+                          const int32_t* tok_offsets, int32_t max_q, uint16_t* out,
+                          void* workspace, void* stream);
+
 /* Zero `workspace` (asynchronously on `stream`).  Needed once after the
  * workspace is allocated: the calls leave their completion counters at zero
  * for the next call.  Zero it again after a call whose tgvkv_status reported

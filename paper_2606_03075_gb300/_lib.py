@@ -24,12 +24,27 @@ class Desc(ctypes.Structure):
                 ("head_budgets", c_int32)]
 
 
+class CacheDesc(ctypes.Structure):
+    """Mirror of ``tgvkv_cache_desc`` (include/tgvkv.h)."""
+    _fields_ = [("B", c_int32), ("H_q", c_int32), ("H_kv", c_int32), ("d", c_int32),
+                ("page_size", c_int32), ("n_pages", c_int32), ("max_pages", c_int32),
+                ("format", c_int32), ("softmax_scale", c_float)]
+
+
+class CachePools(ctypes.Structure):
+    """Mirror of ``tgvkv_cache_pools`` (include/tgvkv.h)."""
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("k_scale", c_void_p), ("v_scale", c_void_p)]
+
+
+CACHE_BF16, CACHE_INT8, CACHE_INT4 = 0, 1, 2
 BASIS_VISION, BASIS_ALL = 0, 1
 WEIGHTS_GIVEN, WEIGHTS_EQ7 = 0, 1
 STAT_TV, STAT_TT, STAT_UNIFORM = 0, 1, 2
 
 
 _P = ctypes.POINTER(Desc)
+_C = ctypes.POINTER(CacheDesc)
+_POOLS = ctypes.POINTER(CachePools)
 
 # name -> (restype, argtypes); the exported C ABI, one entry per declaration
 SIGNATURES = {
@@ -72,6 +87,17 @@ SIGNATURES = {
     "tgvkv_score_noalloc": (c_int, [_P, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                                     c_void_p, c_void_p, c_void_p]),
     "tgvkv_noalloc_status": (c_int, [c_void_p]),
+    "tgvkv_cache_workspace_size": (c_size_t, [_C]),
+    "tgvkv_cache_workspace_init": (c_int, [_C, c_void_p, c_void_p]),
+    "tgvkv_cache_write": (c_int, [_C, _POOLS, c_void_p, c_void_p, c_void_p, c_int64, c_int64,
+                                  c_void_p, c_int64, c_int64, c_int64, c_void_p, c_void_p,
+                                  c_void_p, c_void_p]),
+    "tgvkv_cache_write_rows": (c_int, [_C, _POOLS, c_void_p, c_void_p, c_void_p, c_void_p, c_int64,
+                                       c_void_p, c_void_p, c_void_p, c_void_p]),
+    "tgvkv_cache_read": (c_int, [_C, _POOLS, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                 c_int64, c_void_p, c_void_p]),
+    "tgvkv_chunk_attention": (c_int, [_C, _POOLS, c_void_p, c_void_p, c_void_p, c_int64, c_int64,
+                                      c_int64, c_void_p, c_int32, c_void_p, c_void_p, c_void_p]),
 }
 
 _lib = None

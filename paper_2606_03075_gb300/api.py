@@ -375,5 +375,171 @@ def tgvkv_evict_launches(desc: Desc) -> int:
     return int(n)
 
 
+# ---- the paged cache ---------------------------------------------------------
+
+CacheDesc = _lib.CacheDesc
+CACHE_FORMAT = {"bf16": _lib.CACHE_BF16, "int8": _lib.CACHE_INT8, "int4": _lib.CACHE_INT4}
+CACHE_GROUP = 32   # values that share a scale
+
+# format -> (dtypes a pool may have, pool elements per row of d values)
+_POOL = {_lib.CACHE_BF16: (_BF16_LIKE, lambda d: d),
+         _lib.CACHE_INT8: ((torch.int8, torch.uint8), lambda d: d),
+         _lib.CACHE_INT4: ((torch.uint8,), lambda d: d // 2)}
+
+
+def make_cache_desc(B, H_q, H_kv, d, page_size, n_pages, max_pages, format="bf16",
+                    softmax_scale=0.0) -> CacheDesc:
+    """A paged cache's descriptor (include/tgvkv.h).
+
+    B: sequences (the requests of a batch, or the layers of one); page_size:
+    slots per page (16 to 256, a power of two); n_pages: pages of the pool;
+    max_pages: page-table entries of a set; format: "bf16", "int8" or "int4"."""
+    return CacheDesc(B=B, H_q=H_q, H_kv=H_kv, d=d, page_size=page_size, n_pages=n_pages,
+                     max_pages=max_pages, format=CACHE_FORMAT[format],
+                     softmax_scale=float(softmax_scale))
+
+
+@dataclass
+class PagedCache:
+    k: torch.Tensor                      # [n_pages, page_size, d] (int4: d / 2)
+    v: torch.Tensor
+    k_scale: torch.Tensor | None = None  # uint8 [n_pages, page_size, d / 32]; None for bf16
+    v_scale: torch.Tensor | None = None
+
+
+def alloc_cache(desc: CacheDesc, device=None) -> PagedCache:
+    """Pools of this descriptor's geometry and format (uninitialised)."""
+    dev = device or "cuda"
+    dtypes, row = _POOL[desc.format]
+    pool = (desc.n_pages, desc.page_size, row(desc.d))
+    scale = (desc.n_pages, desc.page_size, desc.d // CACHE_GROUP)
+    quantised = desc.format != _lib.CACHE_BF16
+    new = [torch.empty(pool, dtype=dtypes[0], device=dev) for _ in range(2)]
+    new += [torch.empty(scale, dtype=torch.uint8, device=dev) if quantised else None
+            for _ in range(2)]
+    return PagedCache(*new)
+
+
+def tgvkv_cache_workspace_size(desc: CacheDesc) -> int:
+    n = _lib.load().tgvkv_cache_workspace_size(ctypes.byref(desc))
+    if n == 0:
+        raise TgvkvError(-1, "tgvkv_cache_workspace_size")
+    return int(n)
+
+
+def tgvkv_cache_workspace_init(desc: CacheDesc, ws: torch.Tensor, stream=None):
+    p = _ptr(ws, (torch.uint8,), tgvkv_cache_workspace_size(desc), "workspace")
+    _check(_lib.load().tgvkv_cache_workspace_init(ctypes.byref(desc), p, _stream(stream)),
+           "tgvkv_cache_workspace_init")
+
+
+def new_cache_workspace(desc: CacheDesc, device=None) -> torch.Tensor:
+    """A workspace tensor (uint8) for the paged-cache calls, its status clear."""
+    ws = torch.empty(tgvkv_cache_workspace_size(desc), dtype=torch.uint8, device=device or "cuda")
+    tgvkv_cache_workspace_init(desc, ws)
+    return ws
+
+
+def _pools(desc, cache: PagedCache):
+    dtypes, row = _POOL[desc.format]
+    slots = desc.n_pages * desc.page_size
+    quantised = desc.format != _lib.CACHE_BF16
+    if quantised and (cache.k_scale is None or cache.v_scale is None):
+        raise ValueError("an integer cache needs k_scale and v_scale")
+    scale = slots * (desc.d // CACHE_GROUP)
+    return ctypes.byref(_lib.CachePools(
+        _ptr(cache.k, dtypes, slots * row(desc.d), "cache.k"),
+        _ptr(cache.v, dtypes, slots * row(desc.d), "cache.v"),
+        _ptr(cache.k_scale, (torch.uint8,), scale, "cache.k_scale") if quantised else None,
+        _ptr(cache.v_scale, (torch.uint8,), scale, "cache.v_scale") if quantised else None))
+
+
+def _tokens(t, heads, d, name):
+    """Pointer and (token, head) strides of a token-major tensor [T, heads, d]."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.dtype not in _BF16_LIKE:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected one of {_BF16_LIKE}")
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected (tokens, {heads}, {d})")
+    if t.numel() and t.stride(2) != 1:
+        raise ValueError(f"{name}'s last dimension must be contiguous")
+    # the stride of a dimension with one entry never matters
+    tok = t.stride(0) if t.shape[0] > 1 else heads * d
+    head = t.stride(1) if heads > 1 and t.numel() else d
+    return ctypes.c_void_p(t.data_ptr()), tok, head
+
+
+def _page_table(desc, page_table):
+    return _ptr(page_table, (torch.int32,), desc.B * desc.H_kv * desc.max_pages, "page_table")
+
+
+def _sets(desc, t, name):
+    return _ptr(t, (torch.int32,), desc.B * desc.H_kv, name)
+
+
+def _cache_ws(desc, ws):
+    return _ptr(ws, (torch.uint8,), tgvkv_cache_workspace_size(desc), "workspace")
+
+
+def tgvkv_cache_write(desc, cache: PagedCache, page_table, lens, k_new, v_new, tok_offsets,
+                      lens_out, ws, stream=None):
+    """Append new tokens, k_new and v_new bf16 [T, H_kv, d] (any token and head
+    strides), to the cache, quantised to its format; lens_out receives the new
+    lengths (see include/tgvkv.h)."""
+    kp, kt, kh = _tokens(k_new, desc.H_kv, desc.d, "k_new")
+    vp, vt, vh = _tokens(v_new, desc.H_kv, desc.d, "v_new")
+    if k_new.shape[0] != v_new.shape[0]:
+        raise ValueError(f"k_new has {k_new.shape[0]} tokens, v_new {v_new.shape[0]}")
+    _check(_lib.load().tgvkv_cache_write(
+        ctypes.byref(desc), _pools(desc, cache), _page_table(desc, page_table),
+        _sets(desc, lens, "lens"), kp, kt, kh, vp, vt, vh, k_new.shape[0],
+        _ptr(tok_offsets, (torch.int32,), desc.B + 1, "tok_offsets"),
+        _sets(desc, lens_out, "lens_out"), _cache_ws(desc, ws), _stream(stream)),
+        "tgvkv_cache_write")
+
+
+def tgvkv_cache_write_rows(desc, cache: PagedCache, page_table, lens, k_rows, v_rows, offsets,
+                           lens_out, ws, stream=None):
+    """Append the rows of a CSR cache (tgvkv_evict's k_out, v_out and offsets)."""
+    rows = min(k_rows.numel(), v_rows.numel()) // desc.d
+    _check(_lib.load().tgvkv_cache_write_rows(
+        ctypes.byref(desc), _pools(desc, cache), _page_table(desc, page_table),
+        _sets(desc, lens, "lens"), _ptr(k_rows, _BF16_LIKE, 0, "k_rows"),
+        _ptr(v_rows, _BF16_LIKE, 0, "v_rows"), rows,
+        _ptr(offsets, (torch.int64,), desc.B * desc.H_kv + 1, "offsets"),
+        _sets(desc, lens_out, "lens_out"), _cache_ws(desc, ws), _stream(stream)),
+        "tgvkv_cache_write_rows")
+
+
+def tgvkv_cache_read(desc, cache: PagedCache, page_table, first, offsets, k_out, v_out, ws,
+                     stream=None):
+    """Read rows offsets[s] .. offsets[s+1] of k_out and v_out (bf16) back from
+    the slots first[s] on of every set s (first None: from slot 0)."""
+    rows = min(k_out.numel(), v_out.numel()) // desc.d
+    _check(_lib.load().tgvkv_cache_read(
+        ctypes.byref(desc), _pools(desc, cache), _page_table(desc, page_table),
+        _sets(desc, first, "first"),
+        _ptr(offsets, (torch.int64,), desc.B * desc.H_kv + 1, "offsets"),
+        _ptr(k_out, _BF16_LIKE, 0, "k_out"), _ptr(v_out, _BF16_LIKE, 0, "v_out"), rows,
+        _cache_ws(desc, ws), _stream(stream)), "tgvkv_cache_read")
+
+
+def tgvkv_chunk_attention(desc, cache: PagedCache, page_table, lens, q, tok_offsets, max_q, out, ws,
+                          stream=None):
+    """Attention of each sequence's new tokens (the last of lens slots) over the
+    paged cache: q bf16 [T, H_q, d] (any token and head strides), out bf16
+    [T, H_q, d] contiguous (see include/tgvkv.h)."""
+    qp, qt, qh = _tokens(q, desc.H_q, desc.d, "q")
+    _check(_lib.load().tgvkv_chunk_attention(
+        ctypes.byref(desc), _pools(desc, cache), _page_table(desc, page_table),
+        _sets(desc, lens, "lens"), qp, qt, qh, q.shape[0],
+        _ptr(tok_offsets, (torch.int32,), desc.B + 1, "tok_offsets"), int(max_q),
+        _ptr(out, _BF16_LIKE, q.shape[0] * desc.H_q * desc.d, "out"), _cache_ws(desc, ws),
+        _stream(stream)), "tgvkv_chunk_attention")
+
+
 def default_scale(d: int) -> float:
     return 1.0 / math.sqrt(d)

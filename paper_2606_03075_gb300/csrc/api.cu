@@ -7,6 +7,7 @@
 
 #include <algorithm>
 
+#include "cache_launch.h"
 #include "common.cuh"
 #include "launch.h"
 #include "tgvkv.h"
@@ -319,6 +320,128 @@ int evict_impl(const tgvkv_desc* desc, const uint16_t* q_text, const uint16_t* k
     return ok();
 }
 
+// ---- the paged cache ---------------------------------------------------------
+
+int make_cache_problem(const tgvkv_cache_desc* d, CacheProblem* p) {
+    if (!d) return fail(TGVKV_ERR_INVALID_ARG, "desc is NULL");
+    if (d->B < 1 || d->H_q < 1 || d->H_kv < 1 || d->n_pages < 1 || d->max_pages < 1)
+        return fail(TGVKV_ERR_INVALID_ARG, "bad sizes: B=%d H_q=%d H_kv=%d n_pages=%d max_pages=%d",
+                    d->B, d->H_q, d->H_kv, d->n_pages, d->max_pages);
+    if (d->H_q % d->H_kv != 0)
+        return fail(TGVKV_ERR_INVALID_ARG, "H_q=%d is not a multiple of H_kv=%d", d->H_q, d->H_kv);
+    if (d->d != 64 && d->d != 128)
+        return fail(TGVKV_ERR_UNSUPPORTED, "head dim %d unsupported (64 or 128)", d->d);
+    if (d->H_q / d->H_kv > kMaxGroupHeads)
+        return fail(TGVKV_ERR_UNSUPPORTED, "%d query heads per KV head above %d", d->H_q / d->H_kv,
+                    kMaxGroupHeads);
+    if (d->page_size < kMinPage || d->page_size > kMaxPage || (d->page_size & (d->page_size - 1)))
+        return fail(TGVKV_ERR_UNSUPPORTED, "page_size=%d unsupported (16, 32, 64, 128 or 256)",
+                    d->page_size);
+    if (d->format != TGVKV_CACHE_BF16 && d->format != TGVKV_CACHE_INT8 &&
+        d->format != TGVKV_CACHE_INT4)
+        return fail(TGVKV_ERR_INVALID_ARG, "format=%d unknown", d->format);
+    if (!(d->softmax_scale == d->softmax_scale) || isinf(d->softmax_scale))
+        return fail(TGVKV_ERR_INVALID_ARG, "softmax_scale is not finite");
+    const long long sets = (long long)d->B * d->H_kv;
+    const long long slots = (long long)d->max_pages * d->page_size;
+    if (sets > 65535) return fail(TGVKV_ERR_UNSUPPORTED, "B * H_kv = %lld above 65535", sets);
+    if ((long long)d->n_pages * d->page_size >= (1LL << 31))
+        return fail(TGVKV_ERR_UNSUPPORTED, "the pool holds 2^31 rows or more");
+    if (slots > (1LL << 30))
+        return fail(TGVKV_ERR_UNSUPPORTED, "max_pages * page_size = %lld above 2^30", slots);
+    if (sets * slots >= (1LL << 35))
+        return fail(TGVKV_ERR_UNSUPPORTED, "B * H_kv * max_pages * page_size is 2^35 or more");
+    p->B = d->B;
+    p->H_q = d->H_q;
+    p->H_kv = d->H_kv;
+    p->G = d->H_q / d->H_kv;
+    p->d = d->d;
+    p->S = (int)sets;
+    p->page = d->page_size;
+    p->page_shift = 0;
+    while ((1 << p->page_shift) < d->page_size) ++p->page_shift;
+    p->n_pages = d->n_pages;
+    p->max_pages = d->max_pages;
+    p->cap = (int)slots;
+    p->format = d->format;
+    const double scale = d->softmax_scale > 0.f ? (double)d->softmax_scale : 1.0 / sqrt((double)d->d);
+    p->scale_log2 = (float)(scale * 1.4426950408889634);  // log2(e)
+    return TGVKV_OK;
+}
+
+// Workspace of the paged-cache calls: the status word, the attention's plan
+// (the first unit of work of every set) and the partial results of split sets.
+struct CacheLayout {
+    size_t plan, part, total;
+};
+
+CacheLayout cache_layout(const CacheProblem& p) {
+    CacheLayout w;
+    size_t o = round_up(sizeof(uint32_t));
+    w.plan = o;
+    o += round_up(sizeof(int) * ((size_t)p.S + 1));
+    w.part = o;
+    o += round_up(sizeof(float) * 2 * kStreamMax * (size_t)chunk_record_floats(kStreamRows, p.d));
+    w.total = o;
+    return w;
+}
+
+int check_pools(const CacheProblem& p, const tgvkv_cache_pools* pools, CachePools* out) {
+    if (!pools) return fail(TGVKV_ERR_INVALID_ARG, "pools is NULL");
+    REQUIRE_PTR(pools->k, "the K pool", true);
+    REQUIRE_PTR(pools->v, "the V pool", true);
+    if (p.format != TGVKV_CACHE_BF16) {
+        REQUIRE_PTR(pools->k_scale, "the K scales", true);
+        REQUIRE_PTR(pools->v_scale, "the V scales", true);
+    }
+    *out = CachePools{static_cast<uint8_t*>(pools->k), static_cast<uint8_t*>(pools->v),
+                      pools->k_scale, pools->v_scale};
+    return TGVKV_OK;
+}
+
+// A token-major tensor [n_tokens][heads][d] with strides.
+int check_tokens(const CacheProblem& p, const char* name, const uint16_t* ptr, int64_t tok_stride,
+                 int64_t head_stride, int64_t n_tokens, int heads) {
+    if (n_tokens < 0 || n_tokens >= (1LL << 31) || n_tokens * heads >= (1LL << 31))
+        return fail(n_tokens < 0 ? TGVKV_ERR_INVALID_ARG : TGVKV_ERR_UNSUPPORTED,
+                    "%s: %lld tokens of %d heads", name, (long long)n_tokens, heads);
+    if (n_tokens > 0) REQUIRE_PTR(ptr, name, true);
+    // the TMA maps' strides are below 2^40 bytes
+    if (tok_stride < 0 || head_stride < 0 || tok_stride % 8 || head_stride % 8 ||
+        tok_stride >= (1LL << 38) || head_stride >= (1LL << 38) || (heads > 1 && head_stride < p.d))
+        return fail(TGVKV_ERR_INVALID_ARG,
+                    "%s: strides %lld (token) and %lld (head) must be multiples of 8 below 2^38, "
+                    "the heads' rows apart", name, (long long)tok_stride, (long long)head_stride);
+    return TGVKV_OK;
+}
+
+int check_rows(const void* k, const char* k_name, const void* v, const char* v_name, int64_t n_rows,
+               const int64_t* offsets) {
+    if (n_rows < 0) return fail(TGVKV_ERR_INVALID_ARG, "n_rows=%lld < 0", (long long)n_rows);
+    if (n_rows >= (1LL << 31)) return fail(TGVKV_ERR_UNSUPPORTED, "2^31 rows or more");
+    if (n_rows > 0) {
+        REQUIRE_PTR(k, k_name, true);
+        REQUIRE_PTR(v, v_name, true);
+    }
+    REQUIRE_PTR(offsets, "offsets", false);
+    if ((reinterpret_cast<uintptr_t>(offsets) & 7u) != 0)
+        return fail(TGVKV_ERR_INVALID_ARG, "offsets is not 8-byte aligned");
+    return TGVKV_OK;
+}
+
+int check_write(const CacheProblem& p, const int32_t* page_table, const int32_t* lens,
+                const int32_t* lens_out, const void* workspace) {
+    REQUIRE_PTR(page_table, "page_table", false);
+    REQUIRE_PTR(lens, "lens", false);
+    REQUIRE_PTR(lens_out, "lens_out", false);
+    const uintptr_t a = reinterpret_cast<uintptr_t>(lens), b = reinterpret_cast<uintptr_t>(lens_out);
+    const uintptr_t bytes = sizeof(int32_t) * (uintptr_t)p.S;
+    if (a < b + bytes && b < a + bytes)
+        return fail(TGVKV_ERR_INVALID_ARG, "lens and lens_out overlap");
+    REQUIRE_PTR(workspace, "workspace", true);
+    return TGVKV_OK;
+}
+
 }  // namespace
 }  // namespace tgvkv
 
@@ -607,6 +730,119 @@ int tgvkv_status(void* workspace, void* stream) {
 }
 
 const char* tgvkv_last_error(void) { return g_last_error; }
+
+// ---- the paged cache ---------------------------------------------------------
+
+size_t tgvkv_cache_workspace_size(const tgvkv_cache_desc* desc) {
+    CacheProblem p{};
+    if (make_cache_problem(desc, &p) != TGVKV_OK) return 0;
+    return cache_layout(p).total;
+}
+
+int tgvkv_cache_workspace_init(const tgvkv_cache_desc* desc, void* workspace, void* stream) {
+    CacheProblem p{};
+    int rc = make_cache_problem(desc, &p);
+    if (rc) return rc;
+    REQUIRE_PTR(workspace, "workspace", true);
+    cudaError_t e = cudaMemsetAsync(workspace, 0, sizeof(uint32_t), static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? ok() : cuda_fail(e, "workspace memset");
+}
+
+int tgvkv_cache_write(const tgvkv_cache_desc* desc, const tgvkv_cache_pools* pools,
+                      const int32_t* page_table, const int32_t* lens, const uint16_t* k_new,
+                      int64_t k_tok_stride, int64_t k_head_stride, const uint16_t* v_new,
+                      int64_t v_tok_stride, int64_t v_head_stride, int64_t n_tokens,
+                      const int32_t* tok_offsets, int32_t* lens_out, void* workspace,
+                      void* stream) {
+    CacheProblem p{};
+    CachePools pl{};
+    int rc = make_cache_problem(desc, &p);
+    if (rc || (rc = check_pools(p, pools, &pl))) return rc;
+    if ((rc = check_tokens(p, "k_new", k_new, k_tok_stride, k_head_stride, n_tokens, p.H_kv)) ||
+        (rc = check_tokens(p, "v_new", v_new, v_tok_stride, v_head_stride, n_tokens, p.H_kv)) ||
+        (rc = check_write(p, page_table, lens, lens_out, workspace)))
+        return rc;
+    REQUIRE_PTR(tok_offsets, "tok_offsets", false);
+    const long long strides[4] = {(long long)k_tok_stride, (long long)k_head_stride,
+                                  (long long)v_tok_stride, (long long)v_head_stride};
+    cudaError_t e = launch_cache_write(p, pl, k_new, v_new, strides, (long long)n_tokens * p.H_kv,
+                                       nullptr, tok_offsets, page_table, lens, lens_out,
+                                       static_cast<uint32_t*>(workspace),
+                                       static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? ok() : cuda_fail(e, "cache write launch");
+}
+
+int tgvkv_cache_write_rows(const tgvkv_cache_desc* desc, const tgvkv_cache_pools* pools,
+                           const int32_t* page_table, const int32_t* lens, const uint16_t* k_rows,
+                           const uint16_t* v_rows, int64_t n_rows, const int64_t* offsets,
+                           int32_t* lens_out, void* workspace, void* stream) {
+    CacheProblem p{};
+    CachePools pl{};
+    int rc = make_cache_problem(desc, &p);
+    if (rc || (rc = check_pools(p, pools, &pl))) return rc;
+    if ((rc = check_rows(k_rows, "k_rows", v_rows, "v_rows", n_rows, offsets)) ||
+        (rc = check_write(p, page_table, lens, lens_out, workspace)))
+        return rc;
+    const long long strides[4] = {0, 0, 0, 0};
+    cudaError_t e = launch_cache_write(p, pl, k_rows, v_rows, strides, (long long)n_rows, offsets,
+                                       nullptr, page_table, lens, lens_out,
+                                       static_cast<uint32_t*>(workspace),
+                                       static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? ok() : cuda_fail(e, "cache write launch");
+}
+
+int tgvkv_cache_read(const tgvkv_cache_desc* desc, const tgvkv_cache_pools* pools,
+                     const int32_t* page_table, const int32_t* first, const int64_t* offsets,
+                     uint16_t* k_out, uint16_t* v_out, int64_t n_rows, void* workspace,
+                     void* stream) {
+    CacheProblem p{};
+    CachePools pl{};
+    int rc = make_cache_problem(desc, &p);
+    if (rc || (rc = check_pools(p, pools, &pl))) return rc;
+    if ((rc = check_rows(k_out, "k_out", v_out, "v_out", n_rows, offsets))) return rc;
+    REQUIRE_PTR(page_table, "page_table", false);
+    REQUIRE_PTR(workspace, "workspace", true);
+    cudaError_t e = launch_cache_read(p, pl, page_table, first, offsets, k_out, v_out,
+                                      (long long)n_rows, static_cast<uint32_t*>(workspace),
+                                      static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? ok() : cuda_fail(e, "cache read launch");
+}
+
+int tgvkv_chunk_attention(const tgvkv_cache_desc* desc, const tgvkv_cache_pools* pools,
+                          const int32_t* page_table, const int32_t* lens, const uint16_t* q,
+                          int64_t q_tok_stride, int64_t q_head_stride, int64_t n_tokens,
+                          const int32_t* tok_offsets, int32_t max_q, uint16_t* out,
+                          void* workspace, void* stream) {
+    CacheProblem p{};
+    CachePools pl{};
+    int rc = make_cache_problem(desc, &p);
+    if (rc || (rc = check_pools(p, pools, &pl))) return rc;
+    if ((rc = check_tokens(p, "q", q, q_tok_stride, q_head_stride, n_tokens, p.H_q))) return rc;
+    if (max_q < 0) return fail(TGVKV_ERR_INVALID_ARG, "max_q=%d < 0", max_q);
+    REQUIRE_PTR(page_table, "page_table", false);
+    REQUIRE_PTR(lens, "lens", false);
+    REQUIRE_PTR(tok_offsets, "tok_offsets", false);
+    if (n_tokens > 0) REQUIRE_PTR(out, "out", true);
+    REQUIRE_PTR(workspace, "workspace", true);
+    if (n_tokens == 0 || max_q == 0) return ok();   // no token to compute
+    ChunkArgs a{};
+    a.q = q;
+    a.q_tok = q_tok_stride;
+    a.q_head = q_head_stride;
+    a.tok_offsets = tok_offsets;
+    a.T = (int)n_tokens;
+    a.max_q = max_q < a.T ? max_q : a.T;
+    a.page_table = page_table;
+    a.lens = lens;
+    a.out = out;
+    const CacheLayout lay = cache_layout(p);
+    char* ws = static_cast<char*>(workspace);
+    cudaError_t e = launch_chunk_stream(p, pl, a, reinterpret_cast<float*>(ws + lay.part),
+                                        reinterpret_cast<int*>(ws + lay.plan),
+                                        static_cast<uint32_t*>(workspace),
+                                        static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? ok() : cuda_fail(e, "chunk attention launch");
+}
 
 }  // extern "C"
 

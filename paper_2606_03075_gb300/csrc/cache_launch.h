@@ -1,0 +1,29 @@
+// Host-side launchers of the paged cache's kernels.  All of them are asynchronous
+// on `stream` and assume the arguments were validated by the C-ABI layer.
+#pragma once
+
+#include "cache.cuh"
+#include "chunk.cuh"
+
+namespace tgvkv {
+
+// cache_rows.cu: quantising writes and reads of whole rows.
+// Exactly one of row_offsets (CSR rows: [S + 1]) and tok_offsets (tokens x
+// heads: [B + 1], element strides k token, k head, v token, v head) is given;
+// rows: rows that k and v hold.
+cudaError_t launch_cache_write(const CacheProblem& p, const CachePools& pool, const uint16_t* k,
+                               const uint16_t* v, const long long (&strides)[4], long long rows,
+                               const int64_t* row_offsets, const int32_t* tok_offsets,
+                               const int32_t* page_table, const int32_t* lens, int32_t* lens_out,
+                               uint32_t* status, cudaStream_t stream);
+cudaError_t launch_cache_read(const CacheProblem& p, const CachePools& pool,
+                              const int32_t* page_table, const int32_t* first,
+                              const int64_t* offsets, uint16_t* k_out, uint16_t* v_out,
+                              long long rows, uint32_t* status, cudaStream_t stream);
+
+// Attention of a chunk of new tokens over the paged cache: the row-stream
+// kernel (chunk_stream.cu, query rows in tiles of 16).
+cudaError_t launch_chunk_stream(const CacheProblem& p, const CachePools& pool, const ChunkArgs& a,
+                                float* part, int* plan, uint32_t* status, cudaStream_t stream);
+
+}  // namespace tgvkv

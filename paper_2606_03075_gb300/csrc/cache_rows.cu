@@ -1,0 +1,371 @@
+// Writing rows into the paged cache, quantising on the way, and reading them
+// back as bf16 (cache.cuh has the layout and the formats).
+//
+//   write:  slot lens[s] + i of set s  <-  quantised row i of the set's new rows
+//           lens_out[s] = lens[s] + rows of s
+//   read:   out row offsets[s] + i     <-  slot first[s] + i of set s, exactly
+//
+// Both move each row once and are bound by HBM: 2 d bytes of bf16 plus the
+// stored row per row of K and of V.  A CTA takes kRowsPerCta consecutive rows;
+// one thread per row finds its set (a search over the offsets) and its pool
+// row while the row data's loads, whose addresses do not depend on it, are
+// already in flight.  A row is spread over d / 8 lanes of 8 values (16 bytes
+// of bf16), so a scale's 32 values sit in 4 neighbouring lanes.
+#include "cache_launch.h"
+
+namespace tgvkv {
+namespace {
+
+constexpr int kRowThreads = 256;
+constexpr int kRowUnroll = 4;          // rows of K and of V a thread has in flight
+
+template <int D>
+struct RowGeom {
+    static constexpr int LPR = D / 8;                          // lanes a row
+    static constexpr int RPI = kRowThreads / LPR;              // rows at a time
+    static constexpr int ROWS = RPI * kRowUnroll;              // rows a CTA
+};
+
+// The largest i in [lo, hi] with off[i] <= x, given off[lo] <= x.
+template <typename T>
+__device__ __forceinline__ int find_last(const T* off, int lo, int hi, long long x) {
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if ((long long)off[mid] <= x) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+
+// Pool row of (set, slot), or -1 (with the status bit) when there is none.
+__device__ __forceinline__ long long pool_row(const CacheProblem& p, const int32_t* page_table,
+                                              int s, long long slot, uint32_t* status) {
+    if (slot < 0 || slot >= p.cap) {
+        raise_status(status, TGVKV_STATUS_INDEX);
+        return -1;
+    }
+    const int page = __ldg(page_table + (size_t)s * p.max_pages + (int)(slot >> p.page_shift));
+    if (page < 0 || page >= p.n_pages) {
+        raise_status(status, TGVKV_STATUS_INDEX);
+        return -1;
+    }
+    return (long long)page * p.page + (slot & (p.page - 1));
+}
+
+// ---- 8 values to and from their stored form ----------------------------------
+__device__ __forceinline__ float2 unpack2(uint32_t w) {
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+}
+
+// The scale byte of a group from the largest magnitude among its values, as
+// bf16 bits (15 bits).  With bits = 2^X' (1 + f / 128): Q = 127 needs
+// e = X' - 6, one more when f > 126 (the value is above 127 * 2^(X' - 6));
+// Q = 7 needs e = X' - 2, one more when f > 96.
+template <int FMT>
+__device__ __forceinline__ int group_byte(uint32_t bits) {
+    const int x = (int)(bits >> 7), f = (int)(bits & 127u);
+    if (x == 255) return 255;
+    if (FMT == TGVKV_CACHE_INT8) return max(x - 6 + (f > 126 ? 1 : 0), 1);
+    return min(max(x - 2 + (f > 96 ? 1 : 0), 1), 247);
+}
+
+// Quantise this lane's 8 values (the group's other 24 are in the 3
+// neighbouring lanes; the whole warp takes part) and, where `on`, store them
+// with the group's scale byte.
+template <int FMT>
+__device__ __forceinline__ void store_row(uint4 w, uint8_t* row, uint8_t* scales, int unit,
+                                          bool on) {
+    // magnitudes as bf16 bits order like the values; NaN sorts above infinity
+    const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = __vmaxu2(top, words[i] & 0x7FFF7FFFu);
+    top = max(top & 0xFFFFu, top >> 16);
+    top = max(top, __shfl_xor_sync(~0u, top, 1));
+    top = max(top, __shfl_xor_sync(~0u, top, 2));
+    const int byte = group_byte<FMT>(top);
+    // 2^-e = 2^(127 - byte): an ordinary fp32 power of two for byte 1 .. 253
+    const float inv = byte == 255 ? 0.f : __uint_as_float((uint32_t)(254 - byte) << 23);
+    constexpr float Q = FMT == TGVKV_CACHE_INT8 ? 127.f : 7.f;
+    if (!on) return;
+    int q[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 x = unpack2(words[i]);
+        q[2 * i] = byte == 255 ? 0 : __float2int_rn(fminf(fmaxf(x.x * inv, -Q), Q));
+        q[2 * i + 1] = byte == 255 ? 0 : __float2int_rn(fminf(fmaxf(x.y * inv, -Q), Q));
+    }
+    if (FMT == TGVKV_CACHE_INT8) {
+        uint32_t lo = 0, hi = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            lo |= (uint32_t)(q[i] & 255) << (8 * i);
+            hi |= (uint32_t)(q[4 + i] & 255) << (8 * i);
+        }
+        reinterpret_cast<uint2*>(row)[unit] = make_uint2(lo, hi);
+    } else {
+        uint32_t c = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c |= (uint32_t)(q[i] + 8) << (4 * i);
+        reinterpret_cast<uint32_t*>(row)[unit] = c;
+    }
+    if ((unit & 3) == 0) scales[unit >> 2] = (uint8_t)byte;
+}
+
+// This lane's 8 stored values as bf16: raw holds 8 int8 or 8 int4 codes.
+template <int FMT>
+__device__ __forceinline__ uint4 load_values(uint2 raw, uint32_t byte) {
+    uint32_t r[4];
+    if (FMT == TGVKV_CACHE_INT8) {
+        const uint32_t sc = both(scale_bf16(byte));
+        const uint32_t words[2] = {raw.x, raw.y};
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            r[2 * i] = bf16x2_mul(int8x2_to_bf16(__byte_perm(words[i], 0, 0x4140)), sc);
+            r[2 * i + 1] = bf16x2_mul(int8x2_to_bf16(__byte_perm(words[i], 0, 0x4342)), sc);
+        }
+    } else {
+        const uint32_t base = both(int4_base(byte));
+        uint32_t t[4];   // (element j, element j + 4)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) t[j] = int4x2_to_bf16(raw.x >> (4 * j), base);
+        r[0] = __byte_perm(t[0], t[1], 0x5410);
+        r[1] = __byte_perm(t[2], t[3], 0x5410);
+        r[2] = __byte_perm(t[0], t[1], 0x7632);
+        r[3] = __byte_perm(t[2], t[3], 0x7632);
+    }
+    return make_uint4(r[0], r[1], r[2], r[3]);
+}
+
+// ---- write -------------------------------------------------------------------
+// The rows to write: of the CSR form, row u of [0, offsets[S]) belongs to the
+// set its offsets say; of the token form, row u = token * H_kv + head.
+struct WriteSource {
+    const uint16_t* k;
+    const uint16_t* v;
+    long long k_tok, k_head, v_tok, v_head;   // element strides (token form)
+    const int64_t* row_offsets;               // CSR form: [S + 1]
+    const int32_t* tok_offsets;               // token form: [B + 1]
+    long long rows;                           // rows the tensors hold (< 2^31)
+};
+
+template <int D, int FMT, bool TOKENS>
+__global__ void __launch_bounds__(kRowThreads)
+cache_write_kernel(const CacheProblem p, const WriteSource src, const CachePools pool,
+                   const int32_t* __restrict__ page_table, const int32_t* __restrict__ lens,
+                   int32_t* __restrict__ lens_out, uint32_t* __restrict__ status) {
+    using Gm = RowGeom<D>;
+    __shared__ long long dst[Gm::ROWS];
+    const int tid = threadIdx.x;
+    const long long u0 = (long long)blockIdx.x * Gm::ROWS;
+    const int unit = tid % Gm::LPR, sub = tid / Gm::LPR;
+
+    // the lengths after the write, and the check of the offsets
+    for (int s = blockIdx.x * kRowThreads + tid; s < p.S; s += gridDim.x * kRowThreads) {
+        long long lo, hi, most;
+        if (TOKENS) {
+            const int b = s / p.H_kv;
+            lo = src.tok_offsets[b];
+            hi = src.tok_offsets[b + 1];
+            most = src.rows / p.H_kv;
+            if (b == 0 && lo != 0) raise_status(status, TGVKV_STATUS_INDEX);
+        } else {
+            lo = src.row_offsets[s];
+            hi = src.row_offsets[s + 1];
+            most = src.rows;
+            if (s == 0 && lo != 0) raise_status(status, TGVKV_STATUS_INDEX);
+        }
+        const int len = lens[s];
+        if (lo < 0 || hi < lo || hi > most || len < 0 || len > p.cap || hi - lo > p.cap - len) {
+            raise_status(status, TGVKV_STATUS_INDEX);
+            const long long n = max(min(hi, most) - max(lo, 0ll), 0ll);
+            lens_out[s] = (int)min((long long)clamp_len(len, p.cap) + n, (long long)p.cap);
+        } else {
+            lens_out[s] = len + (int)(hi - lo);
+        }
+    }
+
+    // the rows' data, in flight while their places are looked up
+    uint4 kw[kRowUnroll], vw[kRowUnroll];
+#pragma unroll
+    for (int i = 0; i < kRowUnroll; ++i) {
+        const long long u = u0 + i * Gm::RPI + sub;
+        if (u < src.rows) {
+            long long ko, vo;
+            if (TOKENS) {
+                const unsigned t = (unsigned)u / (unsigned)p.H_kv, g = (unsigned)u - t * p.H_kv;
+                ko = t * src.k_tok + g * src.k_head;
+                vo = t * src.v_tok + g * src.v_head;
+            } else {
+                ko = vo = u * D;
+            }
+            kw[i] = __ldcs(reinterpret_cast<const uint4*>(src.k + ko) + unit);
+            vw[i] = __ldcs(reinterpret_cast<const uint4*>(src.v + vo) + unit);
+        }
+    }
+    if (tid < Gm::ROWS) {
+        const long long u = u0 + tid;
+        long long row = -1;
+        if (u < src.rows) {
+            int s = -1;
+            long long at = 0;
+            if (TOKENS) {
+                const long long t = (unsigned)u / (unsigned)p.H_kv;
+                if (t >= src.tok_offsets[0] && t < src.tok_offsets[p.B]) {
+                    const int b = find_last(src.tok_offsets, 0, p.B - 1, t);
+                    s = b * p.H_kv + (int)(u - t * p.H_kv);
+                    at = t - src.tok_offsets[b];
+                }
+            } else if (u >= src.row_offsets[0] && u < src.row_offsets[p.S]) {
+                s = find_last(src.row_offsets, 0, p.S - 1, u);
+                at = u - src.row_offsets[s];
+            }
+            if (s >= 0 && at >= 0)
+                row = pool_row(p, page_table, s, clamp_len(lens[s], p.cap) + at, status);
+        }
+        dst[tid] = row;
+    }
+    __syncthreads();
+    constexpr int RB = FMT == TGVKV_CACHE_BF16 ? 2 * D : FMT == TGVKV_CACHE_INT8 ? D : D / 2;
+#pragma unroll
+    for (int i = 0; i < kRowUnroll; ++i) {
+        const long long row = dst[i * Gm::RPI + sub];
+        // the lanes of a group of 4 share a row: all of them store or none
+        if (FMT == TGVKV_CACHE_BF16) {
+            if (row >= 0) {
+                reinterpret_cast<uint4*>(pool.k + row * RB)[unit] = kw[i];
+                reinterpret_cast<uint4*>(pool.v + row * RB)[unit] = vw[i];
+            }
+        } else {
+            const bool on = row >= 0;
+            if (!__any_sync(~0u, on)) continue;
+            // lanes without a row quantise zeros and store nothing
+            const uint4 z = make_uint4(0u, 0u, 0u, 0u);
+            store_row<FMT>(on ? kw[i] : z, pool.k + (on ? row : 0) * RB,
+                           pool.ks + (on ? row : 0) * (D / kGroup), unit, on);
+            store_row<FMT>(on ? vw[i] : z, pool.v + (on ? row : 0) * RB,
+                           pool.vs + (on ? row : 0) * (D / kGroup), unit, on);
+        }
+    }
+}
+
+// ---- read --------------------------------------------------------------------
+template <int D, int FMT>
+__global__ void __launch_bounds__(kRowThreads)
+cache_read_kernel(const CacheProblem p, const CachePools pool,
+                  const int32_t* __restrict__ page_table, const int32_t* __restrict__ first,
+                  const int64_t* __restrict__ offsets, uint16_t* __restrict__ k_out,
+                  uint16_t* __restrict__ v_out, long long rows, uint32_t* __restrict__ status) {
+    using Gm = RowGeom<D>;
+    __shared__ long long from[Gm::ROWS];
+    const int tid = threadIdx.x;
+    const long long u0 = (long long)blockIdx.x * Gm::ROWS;
+    const int unit = tid % Gm::LPR, sub = tid / Gm::LPR;
+    for (int s = blockIdx.x * kRowThreads + tid; s < p.S; s += gridDim.x * kRowThreads) {
+        const long long lo = offsets[s], hi = offsets[s + 1];
+        if (lo < 0 || hi < lo || hi > rows || (s == 0 && lo != 0))
+            raise_status(status, TGVKV_STATUS_INDEX);
+    }
+    if (tid < Gm::ROWS) {
+        const long long u = u0 + tid;
+        long long row = -1;
+        if (u < rows && u >= offsets[0] && u < offsets[p.S]) {
+            const int s = find_last(offsets, 0, p.S - 1, u);
+            const long long at = u - offsets[s];
+            if (at >= 0)
+                row = pool_row(p, page_table, s, at + (first ? (long long)first[s] : 0ll), status);
+        }
+        from[tid] = row;
+    }
+    __syncthreads();
+    uint4 kw[kRowUnroll], vw[kRowUnroll];
+    uint32_t kb[kRowUnroll], vb[kRowUnroll];
+#pragma unroll
+    for (int i = 0; i < kRowUnroll; ++i) {
+        const long long row = from[i * Gm::RPI + sub];
+        kw[i] = vw[i] = make_uint4(0u, 0u, 0u, 0u);
+        kb[i] = vb[i] = 0u;
+        if (row < 0) continue;
+        if (FMT == TGVKV_CACHE_BF16) {
+            kw[i] = __ldg(reinterpret_cast<const uint4*>(pool.k + row * (2 * D)) + unit);
+            vw[i] = __ldg(reinterpret_cast<const uint4*>(pool.v + row * (2 * D)) + unit);
+        } else {
+            if (FMT == TGVKV_CACHE_INT8) {
+                const uint2 a = __ldg(reinterpret_cast<const uint2*>(pool.k + row * D) + unit);
+                const uint2 b = __ldg(reinterpret_cast<const uint2*>(pool.v + row * D) + unit);
+                kw[i].x = a.x, kw[i].y = a.y, vw[i].x = b.x, vw[i].y = b.y;
+            } else {
+                kw[i].x = __ldg(reinterpret_cast<const uint32_t*>(pool.k + row * (D / 2)) + unit);
+                vw[i].x = __ldg(reinterpret_cast<const uint32_t*>(pool.v + row * (D / 2)) + unit);
+            }
+            kb[i] = __ldg(pool.ks + row * (D / kGroup) + (unit >> 2));
+            vb[i] = __ldg(pool.vs + row * (D / kGroup) + (unit >> 2));
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kRowUnroll; ++i) {
+        if (from[i * Gm::RPI + sub] < 0) continue;
+        const long long u = u0 + i * Gm::RPI + sub;
+        if (FMT != TGVKV_CACHE_BF16) {
+            kw[i] = load_values<FMT>(make_uint2(kw[i].x, kw[i].y), kb[i]);
+            vw[i] = load_values<FMT>(make_uint2(vw[i].x, vw[i].y), vb[i]);
+        }
+        __stcs(reinterpret_cast<uint4*>(k_out + u * D) + unit, kw[i]);
+        __stcs(reinterpret_cast<uint4*>(v_out + u * D) + unit, vw[i]);
+    }
+}
+
+// Calls f with the head dimension and the format as compile-time constants.
+template <int N>
+struct Int {
+    static constexpr int value = N;
+};
+template <typename F>
+cudaError_t by_shape(const CacheProblem& p, F&& f) {
+    auto fmt = [&](auto d) {
+        if (p.format == TGVKV_CACHE_BF16) return f(d, Int<TGVKV_CACHE_BF16>());
+        if (p.format == TGVKV_CACHE_INT8) return f(d, Int<TGVKV_CACHE_INT8>());
+        return f(d, Int<TGVKV_CACHE_INT4>());
+    };
+    return p.d == 64 ? fmt(Int<64>()) : fmt(Int<128>());
+}
+
+unsigned row_blocks(long long rows, int per) {
+    return rows <= 0 ? 1u : (unsigned)((rows + per - 1) / per);
+}
+
+}  // namespace
+
+cudaError_t launch_cache_write(const CacheProblem& p, const CachePools& pool, const uint16_t* k,
+                               const uint16_t* v, const long long (&strides)[4], long long rows,
+                               const int64_t* row_offsets, const int32_t* tok_offsets,
+                               const int32_t* page_table, const int32_t* lens, int32_t* lens_out,
+                               uint32_t* status, cudaStream_t stream) {
+    const WriteSource src{k, v, strides[0], strides[1], strides[2], strides[3], row_offsets,
+                          tok_offsets, rows};
+    return by_shape(p, [&](auto d, auto fmt) {
+        constexpr int D = decltype(d)::value, FMT = decltype(fmt)::value;
+        const unsigned blocks = row_blocks(rows, RowGeom<D>::ROWS);
+        if (tok_offsets)
+            cache_write_kernel<D, FMT, true><<<blocks, kRowThreads, 0, stream>>>(
+                p, src, pool, page_table, lens, lens_out, status);
+        else
+            cache_write_kernel<D, FMT, false><<<blocks, kRowThreads, 0, stream>>>(
+                p, src, pool, page_table, lens, lens_out, status);
+        return cudaGetLastError();
+    });
+}
+
+cudaError_t launch_cache_read(const CacheProblem& p, const CachePools& pool,
+                              const int32_t* page_table, const int32_t* first,
+                              const int64_t* offsets, uint16_t* k_out, uint16_t* v_out,
+                              long long rows, uint32_t* status, cudaStream_t stream) {
+    return by_shape(p, [&](auto d, auto fmt) {
+        constexpr int D = decltype(d)::value, FMT = decltype(fmt)::value;
+        cache_read_kernel<D, FMT><<<row_blocks(rows, RowGeom<D>::ROWS), kRowThreads, 0, stream>>>(
+            p, pool, page_table, first, offsets, k_out, v_out, rows, status);
+        return cudaGetLastError();
+    });
+}
+
+}  // namespace tgvkv
