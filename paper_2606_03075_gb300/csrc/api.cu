@@ -379,9 +379,12 @@ CacheLayout cache_layout(const CacheProblem& p) {
     CacheLayout w;
     size_t o = round_up(sizeof(uint32_t));
     w.plan = o;
-    o += round_up(sizeof(int) * ((size_t)p.S + 1));
+    o += round_up(sizeof(long long) * ((size_t)p.S + 1));
     w.part = o;
-    o += round_up(sizeof(float) * 2 * kStreamMax * (size_t)chunk_record_floats(kStreamRows, p.d));
+    // two records per stream, or per CTA and row tile of a pair
+    const size_t stream = 2 * (size_t)kStreamMax * chunk_record_floats(kStreamRows, p.d);
+    const size_t tile = 4 * (size_t)kTileMaxCtas * chunk_record_floats(TM, p.d);
+    o += round_up(sizeof(float) * std::max(stream, tile));
     w.total = o;
     return w;
 }
@@ -408,10 +411,11 @@ int check_tokens(const CacheProblem& p, const char* name, const uint16_t* ptr, i
     if (n_tokens > 0) REQUIRE_PTR(ptr, name, true);
     // the TMA maps' strides are below 2^40 bytes
     if (tok_stride < 0 || head_stride < 0 || tok_stride % 8 || head_stride % 8 ||
-        tok_stride >= (1LL << 38) || head_stride >= (1LL << 38) || (heads > 1 && head_stride < p.d))
+        tok_stride >= (1LL << 38) || head_stride >= (1LL << 38) || (heads > 1 && head_stride < p.d) ||
+        (n_tokens > 1 && tok_stride < p.d))
         return fail(TGVKV_ERR_INVALID_ARG,
                     "%s: strides %lld (token) and %lld (head) must be multiples of 8 below 2^38, "
-                    "the heads' rows apart", name, (long long)tok_stride, (long long)head_stride);
+                    "rows apart", name, (long long)tok_stride, (long long)head_stride);
     return TGVKV_OK;
 }
 
@@ -837,10 +841,19 @@ int tgvkv_chunk_attention(const tgvkv_cache_desc* desc, const tgvkv_cache_pools*
     a.out = out;
     const CacheLayout lay = cache_layout(p);
     char* ws = static_cast<char*>(workspace);
-    cudaError_t e = launch_chunk_stream(p, pl, a, reinterpret_cast<float*>(ws + lay.part),
-                                        reinterpret_cast<int*>(ws + lay.plan),
-                                        static_cast<uint32_t*>(workspace),
-                                        static_cast<cudaStream_t>(stream));
+    float* part = reinterpret_cast<float*>(ws + lay.part);
+    long long* plan = reinterpret_cast<long long*>(ws + lay.plan);
+    uint32_t* status = static_cast<uint32_t*>(workspace);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    cudaError_t e;
+    if ((long long)a.max_q * p.G <= kStreamRows) {
+        e = launch_chunk_stream(p, pl, a, part, plan, status, st);
+    } else {
+        const bool pair = a.max_q > TM / p.G;   // some chunk has more than one row tile
+        e = p.format == TGVKV_CACHE_BF16   ? launch_tile_bf16(p, pl, a, part, plan, pair, status, st)
+            : p.format == TGVKV_CACHE_INT8 ? launch_tile_int8(p, pl, a, part, plan, pair, status, st)
+                                           : launch_tile_int4(p, pl, a, part, plan, pair, status, st);
+    }
     return e == cudaSuccess ? ok() : cuda_fail(e, "chunk attention launch");
 }
 

@@ -89,4 +89,29 @@ __device__ __forceinline__ uint32_t int4_base(uint32_t byte) { return min(byte +
 
 __device__ __forceinline__ uint32_t both(uint32_t half) { return half | (half << 16); }
 
+// Eight consecutive stored codes (int4: in raw.x) of a group as bf16, in order.
+template <int FMT>
+__device__ __forceinline__ uint4 codes_to_bf16(uint2 raw, uint32_t byte) {
+    uint32_t r[4];
+    if (FMT == TGVKV_CACHE_INT8) {
+        const uint32_t sc = both(scale_bf16(byte));
+        const uint32_t words[2] = {raw.x, raw.y};
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            r[2 * i] = bf16x2_mul(int8x2_to_bf16(__byte_perm(words[i], 0, 0x4140)), sc);
+            r[2 * i + 1] = bf16x2_mul(int8x2_to_bf16(__byte_perm(words[i], 0, 0x4342)), sc);
+        }
+    } else {
+        const uint32_t base = both(int4_base(byte));
+        uint32_t t[4];   // (element j, element j + 4)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) t[j] = int4x2_to_bf16(raw.x >> (4 * j), base);
+        r[0] = __byte_perm(t[0], t[1], 0x5410);
+        r[1] = __byte_perm(t[2], t[3], 0x5410);
+        r[2] = __byte_perm(t[0], t[1], 0x7632);
+        r[3] = __byte_perm(t[2], t[3], 0x7632);
+    }
+    return make_uint4(r[0], r[1], r[2], r[3]);
+}
+
 }  // namespace tgvkv

@@ -21,9 +21,23 @@ cudaError_t launch_cache_read(const CacheProblem& p, const CachePools& pool,
                               const int64_t* offsets, uint16_t* k_out, uint16_t* v_out,
                               long long rows, uint32_t* status, cudaStream_t stream);
 
-// Attention of a chunk of new tokens over the paged cache: the row-stream
-// kernel (chunk_stream.cu, query rows in tiles of 16).
+// Attention of a chunk of new tokens: the row-stream kernel, for sets of at most
+// kStreamRows query rows (max_q * G; chunk_stream.cu), and the tile kernel for
+// larger ones, `pair`: two row tiles an item (chunk_tile.cuh), with its merge
+// (chunk_merge.cu).  plan: S + 1 entries; part: the split sets' records.
 cudaError_t launch_chunk_stream(const CacheProblem& p, const CachePools& pool, const ChunkArgs& a,
-                                float* part, int* plan, uint32_t* status, cudaStream_t stream);
+                                float* part, long long* plan, uint32_t* status,
+                                cudaStream_t stream);
+cudaError_t launch_tile_bf16(const CacheProblem& p, const CachePools& pool, const ChunkArgs& a,
+                             float* part, long long* plan, bool pair, uint32_t* status,
+                             cudaStream_t stream);
+cudaError_t launch_tile_int8(const CacheProblem& p, const CachePools& pool, const ChunkArgs& a,
+                             float* part, long long* plan, bool pair, uint32_t* status,
+                             cudaStream_t stream);
+cudaError_t launch_tile_int4(const CacheProblem& p, const CachePools& pool, const ChunkArgs& a,
+                             float* part, long long* plan, bool pair, uint32_t* status,
+                             cudaStream_t stream);
+cudaError_t launch_tile_merge(const CacheProblem& p, const ChunkArgs& a, const TilePlan& pl, int ctas,
+                              const float* part, const long long* plan, cudaStream_t stream);
 
 }  // namespace tgvkv

@@ -112,31 +112,6 @@ __device__ __forceinline__ void store_row(uint4 w, uint8_t* row, uint8_t* scales
     if ((unit & 3) == 0) scales[unit >> 2] = (uint8_t)byte;
 }
 
-// This lane's 8 stored values as bf16: raw holds 8 int8 or 8 int4 codes.
-template <int FMT>
-__device__ __forceinline__ uint4 load_values(uint2 raw, uint32_t byte) {
-    uint32_t r[4];
-    if (FMT == TGVKV_CACHE_INT8) {
-        const uint32_t sc = both(scale_bf16(byte));
-        const uint32_t words[2] = {raw.x, raw.y};
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            r[2 * i] = bf16x2_mul(int8x2_to_bf16(__byte_perm(words[i], 0, 0x4140)), sc);
-            r[2 * i + 1] = bf16x2_mul(int8x2_to_bf16(__byte_perm(words[i], 0, 0x4342)), sc);
-        }
-    } else {
-        const uint32_t base = both(int4_base(byte));
-        uint32_t t[4];   // (element j, element j + 4)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) t[j] = int4x2_to_bf16(raw.x >> (4 * j), base);
-        r[0] = __byte_perm(t[0], t[1], 0x5410);
-        r[1] = __byte_perm(t[2], t[3], 0x5410);
-        r[2] = __byte_perm(t[0], t[1], 0x7632);
-        r[3] = __byte_perm(t[2], t[3], 0x7632);
-    }
-    return make_uint4(r[0], r[1], r[2], r[3]);
-}
-
 // ---- write -------------------------------------------------------------------
 // The rows to write: of the CSR form, row u of [0, offsets[S]) belongs to the
 // set its offsets say; of the token form, row u = token * H_kv + head.
@@ -307,8 +282,8 @@ cache_read_kernel(const CacheProblem p, const CachePools pool,
         if (from[i * Gm::RPI + sub] < 0) continue;
         const long long u = u0 + i * Gm::RPI + sub;
         if (FMT != TGVKV_CACHE_BF16) {
-            kw[i] = load_values<FMT>(make_uint2(kw[i].x, kw[i].y), kb[i]);
-            vw[i] = load_values<FMT>(make_uint2(vw[i].x, vw[i].y), vb[i]);
+            kw[i] = codes_to_bf16<FMT>(make_uint2(kw[i].x, kw[i].y), kb[i]);
+            vw[i] = codes_to_bf16<FMT>(make_uint2(vw[i].x, vw[i].y), vb[i]);
         }
         __stcs(reinterpret_cast<uint4*>(k_out + u * D) + unit, kw[i]);
         __stcs(reinterpret_cast<uint4*>(v_out + u * D) + unit, vw[i]);

@@ -55,6 +55,94 @@ __host__ __device__ inline int chunk_record_floats(int rows, int d) {
 
 constexpr int kStreamMax = 2048;       // streams of the row-stream kernel
 constexpr int kStreamRows = 16;        // query rows it takes a set
+constexpr int kTileMaxCtas = 160;      // CTAs of the tile kernel
+constexpr int TM = 128;                // query rows of its row tiles
+constexpr int TN = 128;                // slots of its key tiles
+
+// The tile kernel's work.
+struct TilePlan {
+    int tpt;                           // tokens of a row tile
+    int tpi;                           // tokens of an item: one row tile, or two
+    int rows;                          // query rows of a record: tpt * G at most
+};
+
+// Key tiles that the tokens of set `sp` below `tok_end` see.
+__device__ __forceinline__ int tiles_seen(const SetSpan& sp, int tok_end) {
+    const int vis = min(sp.len - sp.n + min(sp.n, tok_end), sp.len);
+    return vis <= 0 ? 0 : (vis + TN - 1) / TN;
+}
+
+// Units of a set: the key tiles of all its items.
+__device__ __forceinline__ long long set_units(const SetSpan& sp, const TilePlan& pl) {
+    long long sum = 0;
+    for (int t = 0; t < sp.n; t += pl.tpi) sum += tiles_seen(sp, t + pl.tpi);
+    return sum;
+}
+
+
+// Joins the records of one query row, in order: record i is at rec(i), the row
+// is row r of its rec_rows.  A whole warp; lane t gets dims [t D / 32, (t + 1) D /
+// 32) of the normalised result in acc.
+template <int D, typename Rec>
+__device__ __forceinline__ void merge_records(int count, int rec_rows, int r, Rec&& rec,
+                                              float (&acc)[D / 32]) {
+    constexpr int DPL = D / 32;
+    const int lane = threadIdx.x & 31;
+    float M = -INFINITY, L = 0.f;
+#pragma unroll
+    for (int c = 0; c < DPL; ++c) acc[c] = 0.f;
+    for (int b = 0; b < count; b += 32) {
+        const int cnt = min(count - b, 32);
+        float mw = -INFINITY, lw = 0.f;
+        if (lane < cnt) {
+            const float* pp = rec(b + lane) + rec_rows * D + r;
+            mw = __ldcg(pp);
+            lw = __ldcg(pp + rec_rows);
+        }
+        float Mb = mw;
+#pragma unroll
+        for (int k = 16; k > 0; k >>= 1) Mb = fmaxf(Mb, __shfl_xor_sync(~0u, Mb, k));
+        const float Mn = fmaxf(M, Mb);
+        const float ref = Mn == -INFINITY ? 0.f : Mn;        // no mass yet: all factors 0
+        const float fa = fast_exp2(M - ref), f = fast_exp2(mw - ref);
+        float lf = lw * f;
+#pragma unroll
+        for (int k = 16; k > 0; k >>= 1) lf += __shfl_xor_sync(~0u, lf, k);
+        L = L * fa + lf;
+#pragma unroll
+        for (int c = 0; c < DPL; ++c) acc[c] *= fa;
+        M = Mn;
+        for (int j0 = 0; j0 < cnt; j0 += 8) {                // 8 records' loads in flight
+            float ov[8][DPL];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+#pragma unroll
+                for (int c = 0; c < DPL; ++c) ov[u][c] = 0.f;
+                if (j0 + u < cnt) {
+                    const float* ow = rec(b + j0 + u) + r * D + DPL * lane;
+                    if (DPL == 4) {
+                        const float4 x = __ldcg(reinterpret_cast<const float4*>(ow));
+                        ov[u][0] = x.x, ov[u][1 % DPL] = x.y, ov[u][2 % DPL] = x.z,
+                        ov[u][3 % DPL] = x.w;
+                    } else {
+                        const float2 x = __ldcg(reinterpret_cast<const float2*>(ow));
+                        ov[u][0] = x.x, ov[u][1 % DPL] = x.y;
+                    }
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const float fj = __shfl_sync(~0u, f, (j0 + u) & 31);
+#pragma unroll
+                for (int c = 0; c < DPL; ++c)
+                    if (j0 + u < cnt) acc[c] += ov[u][c] * fj;
+            }
+        }
+    }
+    const float inv = L > 0.f ? 1.f / L : (L == L ? 0.f : L);
+#pragma unroll
+    for (int c = 0; c < DPL; ++c) acc[c] *= inv;
+}
 
 // Two floats as bf16x2, `lo` in the low half.
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {

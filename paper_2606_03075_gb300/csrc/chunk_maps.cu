@@ -42,7 +42,9 @@ bool make_query_map(CUtensorMap* map, const CacheProblem& p, const ChunkArgs& a,
     auto fn = encode_fn();
     if (!fn) return false;
     const cuuint64_t dims[3] = {(cuuint64_t)p.d, (cuuint64_t)p.H_q, (cuuint64_t)(a.T > 0 ? a.T : 1)};
-    const cuuint64_t strides[2] = {(cuuint64_t)a.q_head * 2, (cuuint64_t)a.q_tok * 2};
+    // a dimension of one entry has no stride that matters, but a map needs one
+    const cuuint64_t strides[2] = {(cuuint64_t)(p.H_q > 1 ? a.q_head : p.d) * 2,
+                                   (cuuint64_t)(a.T > 1 ? a.q_tok : p.d) * 2};
     const cuuint32_t box[3] = {64, box_heads, box_tokens};
     const cuuint32_t estr[3] = {1, 1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<uint16_t*>(a.q), dims, strides,

@@ -129,31 +129,24 @@ __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_
         : "memory");
 }
 
-// Chunks of set s for the row tile that starts at query row `row0`: the slots
-// its last row sees.
+// Chunks of a set: its last new token sees every slot.
 template <int CH>
-__device__ __forceinline__ int set_chunks(const CacheProblem& p, const SetSpan& sp, int row0) {
-    const int rows = sp.n * p.G;
-    if (rows <= row0) return 0;
-    const int last = min(rows, row0 + kStreamRows) - 1;          // its last query row
-    const int seen = sp.len - sp.n + last / p.G + 1;
-    return seen <= 0 ? 0 : (min(seen, sp.len) + CH - 1) / CH;
+__device__ __forceinline__ int set_chunks(const SetSpan& sp) {
+    return sp.n > 0 ? (sp.len + CH - 1) / CH : 0;
 }
 
 // A stream's walk over its chunks [c, c1) of the sequence.
 template <int CH>
 struct Walk {
-    int s, at, left, chunks, row0;     // set, next chunk in it, chunks left of the share
+    int s, at, left, chunks;           // set, next chunk in it, chunks left of the share
     SetSpan sp;
 
     __device__ __forceinline__ void load(const CacheProblem& p, const ChunkArgs& a) {
         sp = set_span(p, a, s);
-        chunks = set_chunks<CH>(p, sp, row0);
+        chunks = set_chunks<CH>(sp);
     }
     __device__ __forceinline__ void init(const CacheProblem& p, const ChunkArgs& a,
-                                         const int* pref, int entries, int run, int row0_, int c,
-                                         int c1) {
-        row0 = row0_;
+                                         const int* pref, int entries, int run, int c, int c1) {
         left = c1 - c;
         int lo = 0, hi = entries - 1;  // the last entry that starts at or before c
         while (lo < hi) {
@@ -182,11 +175,9 @@ struct Walk {
             load(p, a);
             fresh = true;
         }
-        const int last = min((min(sp.n * p.G, row0 + kStreamRows) - 1) / p.G + 1 + sp.len - sp.n,
-                             sp.len);
         c.s = s;
         c.key0 = at * CH;
-        c.n = min(last - c.key0, CH);
+        c.n = min(sp.len - c.key0, CH);
         c.first = fresh;
         c.last = at + 1 == chunks || left == 1;
         c.len = sp.len;
@@ -205,16 +196,16 @@ template <int D, int FMT>
 __device__ __forceinline__ void issue(unsigned char* stage, uint64_t* bar, const Chunk& c, int page,
                                       int box, const CUtensorMap* mk, const CUtensorMap* mv,
                                       const CacheProblem& p, const CachePools& pool,
-                                      const ChunkArgs& a, int row0, int lane) {
+                                      const ChunkArgs& a, int lane) {
     using Gm = StreamGeom<D, FMT>;
     const int nb = (c.n + box - 1) / box;
-    const int rows = min(c.nq * p.G - row0, kStreamRows);
+    const int rows = c.nq * p.G;
     const uint32_t per_box = (uint32_t)box * (2 * Gm::ROWB + 2 * Gm::SCB);
     if (lane == 0)
         tc::mbar_arrive_expect_tx(bar, nb * per_box + (c.first ? (uint32_t)rows * 2 * D : 0u));
     __syncwarp();
     if (c.first && lane < rows) {
-        const int r = row0 + lane, i = r / p.G, h = r - i * p.G;
+        const int i = lane / p.G, h = lane - i * p.G;
         const uint16_t* src = a.q + (long long)(c.tok0 + i) * a.q_tok +
                               (long long)((c.s % p.H_kv) * p.G + h) * a.q_head;
         bulk_copy(smem_u32(stage + Gm::kQ) + lane * 2 * D, src, 2 * D, bar);
@@ -265,9 +256,9 @@ constexpr int out_step() {
 template <int D, int FMT>
 __global__ void __launch_bounds__(kW * 32, 1)
 chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
-                    const CacheProblem p, const CachePools pool, const ChunkArgs a, int row0,
-                    int box, int min_chunks, int rec_rows, float* __restrict__ part,
-                    int* __restrict__ plan, uint32_t* __restrict__ status) {
+                    const CacheProblem p, const CachePools pool, const ChunkArgs a, int box,
+                    int min_chunks, int rec_rows, float* __restrict__ part,
+                    long long* __restrict__ plan, uint32_t* __restrict__ status) {
     using Gm = StreamGeom<D, FMT>;
     constexpr int CH = Gm::CH;
     constexpr int KS = D / 16, ND = D / 8, NT = CH / 8, KK = CH / 16;
@@ -286,7 +277,7 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
         for (int st = 0; st < kStages; ++st) tc::mbar_init(&tl.full[warp][st], 1);
         tc::fence_mbar_init();
     }
-    if (blockIdx.x == 0 && row0 == 0) check_spans(p, a, tid, kW * 32, status);
+    if (blockIdx.x == 0) check_spans(p, a, tid, kW * 32, status);
 
     // ---- the plan: the first chunk of every entry (`run` consecutive sets)
     const int run = (p.S + kPlanSets - 1) / kPlanSets;
@@ -299,7 +290,7 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
         cnt[u] = 0;
         if (e < entries)
             for (int s = e * run; s < min((e + 1) * run, p.S); ++s)
-                cnt[u] += set_chunks<CH>(p, set_span(p, a, s), row0);
+                cnt[u] += set_chunks<CH>(set_span(p, a, s));
         sum += cnt[u];
     }
     int incl = sum;
@@ -323,7 +314,7 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
             int at = base;
             for (int s = e * run; s < min((e + 1) * run, p.S); ++s) {
                 plan[s] = at;
-                at += run == 1 ? cnt[u] : set_chunks<CH>(p, set_span(p, a, s), row0);
+                at += run == 1 ? cnt[u] : set_chunks<CH>(set_span(p, a, s));
             }
         }
         base += cnt[u];
@@ -341,7 +332,7 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
     unsigned char* wring = ring + warp * kStages * Gm::kStage;
     Walk<CH> walk;
     bool fresh = true;
-    walk.init(p, a, tl.pref, entries, run, row0, c0, c1);
+    walk.init(p, a, tl.pref, entries, run, c0, c1);
     Chunk nxt;
     bool more = walk.next(p, a, nxt, fresh);
     int nxt_page = more ? chunk_page(p, a, nxt, box, lane) : 0;
@@ -350,7 +341,7 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
         const int st = issued % kStages;
         if (lane == 0) tl.chunk[warp][st] = nxt;
         issue<D, FMT>(wring + st * Gm::kStage, &tl.full[warp][st], nxt,
-                      valid_page(p, nxt_page, status), box, &mk, &mv, p, pool, a, row0, lane);
+                      valid_page(p, nxt_page, status), box, &mk, &mv, p, pool, a, lane);
         ++issued;
         more = walk.next(p, a, nxt, fresh);
         if (more) nxt_page = chunk_page(p, a, nxt, box, lane);
@@ -375,7 +366,7 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
             seg_chunk = c0 + i;
             // Q fragments: pairs of dims in the order the K fragments have; 0 in
             // rows the tile does not have
-            const int rows = min(c.nq * p.G - row0, kStreamRows);
+            const int rows = c.nq * p.G;
             const uint32_t q0 = sb + Gm::kQ + g * 2 * D, q1 = q0 + 8 * 2 * D;
             if (FMT == TGVKV_CACHE_BF16) {
 #pragma unroll
@@ -494,7 +485,7 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
         if (c.n < CH || c.key0 + CH > c.len - c.nq + 1) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int lim = min(c.len - c.nq + (row0 + g + 8 * h) / p.G + 1 - c.key0, c.n);
+                const int lim = min(c.len - c.nq + (g + 8 * h) / p.G + 1 - c.key0, c.n);
 #pragma unroll
                 for (int j = 0; j < NT; ++j)
 #pragma unroll
@@ -618,10 +609,8 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
             l[h] += __shfl_xor_sync(~0u, l[h], 1);
             l[h] += __shfl_xor_sync(~0u, l[h], 2);
         }
-        const int rows = min(c.nq * p.G - row0, kStreamRows);
-        const int set_last = min((min(c.nq * p.G, row0 + kStreamRows) - 1) / p.G + 1 + c.len - c.nq,
-                                 c.len);
-        const bool whole = seg_chunk == c0 + i - c.key0 / CH && c.key0 + CH >= set_last;
+        const int rows = c.nq * p.G;
+        const bool whole = seg_chunk == c0 + i - c.key0 / CH && c.key0 + CH >= c.len;
         const int gk = c.s % p.H_kv;
         float* pp = part + ((size_t)si * 2 + (seg_chunk == c0 ? 0 : 1)) *
                                (size_t)chunk_record_floats(rec_rows, D);
@@ -631,7 +620,7 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
             if (r >= rows) continue;
             if (whole) {               // the whole set: written out
                 const float inv = l[h] > 0.f ? 1.f / l[h] : (l[h] == l[h] ? 0.f : l[h]);
-                const int t = (row0 + r) / p.G, hh = row0 + r - t * p.G;
+                const int t = r / p.G, hh = r - t * p.G;
                 uint16_t* op = a.out + ((size_t)(c.tok0 + t) * p.H_q + gk * p.G + hh) * D;
                 if (FMT == TGVKV_CACHE_BF16) {
 #pragma unroll
@@ -676,12 +665,13 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
 }
 
 // The split sets' merge and the rows that see nothing: one warp per (set, query
-// row of the tile), a programmatic dependent of the stream kernel.  A set's
-// partials are combined in stream order.
-template <int D, int CH>
+// row), a programmatic dependent of the stream kernel.  A set's partials are
+// combined in stream order.
+template <int D>
 __global__ void __launch_bounds__(128)
-chunk_stream_merge(const CacheProblem p, const ChunkArgs a, int row0, int n_streams, int min_chunks,
-                   int rec_rows, const float* __restrict__ part, const int* __restrict__ plan) {
+chunk_stream_merge(const CacheProblem p, const ChunkArgs a, int n_streams, int min_chunks,
+                   int rec_rows, const float* __restrict__ part,
+                   const long long* __restrict__ plan) {
     constexpr int DPL = D / 32;
     const int lane = threadIdx.x & 31;
     const long long gw = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
@@ -689,79 +679,28 @@ chunk_stream_merge(const CacheProblem p, const ChunkArgs a, int row0, int n_stre
     SetSpan sp{0, 0, 0};
     if (s < p.S) sp = set_span(p, a, s);
     griddep_wait();
-    if (s >= p.S || row0 + r >= sp.n * p.G) return;
-    const int c0 = __ldcg(plan + s), c1 = __ldcg(plan + s + 1), total = __ldcg(plan + p.S);
-    const int t = (row0 + r) / p.G, hh = row0 + r - t * p.G;
-    uint16_t* out = a.out + ((size_t)(sp.tok0 + t) * p.H_q + (s % p.H_kv) * p.G + hh) * D + DPL * lane;
+    if (s >= p.S || r >= sp.n * p.G) return;
+    const int c0 = (int)__ldcg(plan + s), c1 = (int)__ldcg(plan + s + 1);
+    const int total = (int)__ldcg(plan + p.S);
     float acc[DPL];
 #pragma unroll
     for (int c = 0; c < DPL; ++c) acc[c] = 0.f;
-    float inv = 0.f;
     if (c1 > c0) {
         const int per = max((total + n_streams - 1) / n_streams, min_chunks);
         const int w0 = c0 / per, w1 = (c1 - 1) / per;
         if (w0 == w1) return;          // inside one stream: written by it
-        const int rec = chunk_record_floats(rec_rows, D);
-        float M = -INFINITY, L = 0.f;
-        for (int b = w0; b <= w1; b += 32) {
-            const int cnt = min(w1 - b + 1, 32);
-            // the segment starts its stream's share, but for a set that begins inside it
-            const int w = b + lane;
-            const float* pp = part + ((size_t)w * 2 + (w == w0 && c0 != w0 * per ? 1 : 0)) * rec;
-            float mw = -INFINITY, lw = 0.f;
-            if (lane < cnt) {
-                mw = __ldcg(pp + rec_rows * D + r);
-                lw = __ldcg(pp + rec_rows * D + rec_rows + r);
-            }
-            float Mb = mw;
-#pragma unroll
-            for (int k = 16; k > 0; k >>= 1) Mb = fmaxf(Mb, __shfl_xor_sync(~0u, Mb, k));
-            const float Mn = fmaxf(M, Mb);
-            const float ref = Mn == -INFINITY ? 0.f : Mn;
-            const float fa = fast_exp2(M - ref);
-            const float f = fast_exp2(mw - ref);
-            float lf = lane < cnt ? lw * f : 0.f;
-#pragma unroll
-            for (int k = 16; k > 0; k >>= 1) lf += __shfl_xor_sync(~0u, lf, k);
-            L = L * fa + lf;
-#pragma unroll
-            for (int c = 0; c < DPL; ++c) acc[c] *= fa;
-            M = Mn;
-            for (int j0 = 0; j0 < cnt; j0 += 8) {
-                float ov[8][DPL];
-#pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    const int w2 = b + j0 + u;
-                    const float* ow =
-                        part + ((size_t)w2 * 2 + (w2 == w0 && c0 != w0 * per ? 1 : 0)) * rec + r * D +
-                        DPL * lane;
-#pragma unroll
-                    for (int c = 0; c < DPL; ++c) ov[u][c] = 0.f;
-                    if (j0 + u < cnt) {
-                        if (DPL == 4) {
-                            const float4 x = __ldcg(reinterpret_cast<const float4*>(ow));
-                            ov[u][0] = x.x, ov[u][1 % DPL] = x.y, ov[u][2 % DPL] = x.z,
-                            ov[u][3 % DPL] = x.w;
-                        } else {
-                            const float2 x = __ldcg(reinterpret_cast<const float2*>(ow));
-                            ov[u][0] = x.x, ov[u][1 % DPL] = x.y;
-                        }
-                    }
-                }
-#pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    const float fj = __shfl_sync(~0u, f, (j0 + u) & 31);
-#pragma unroll
-                    for (int c = 0; c < DPL; ++c)
-                        if (j0 + u < cnt) acc[c] += ov[u][c] * fj;
-                }
-            }
-        }
-        inv = L > 0.f ? 1.f / L : (L == L ? 0.f : L);
+        // a segment starts its stream's share, but for a set that begins inside it
+        const int first = c0 != w0 * per ? 1 : 0;
+        const size_t rec = chunk_record_floats(rec_rows, D);
+        merge_records<D>(w1 - w0 + 1, rec_rows, r, [&](int i) {
+            return part + ((size_t)(w0 + i) * 2 + (i == 0 ? first : 0)) * rec;
+        }, acc);
     }
+    const int t = r / p.G, hh = r - t * p.G;
+    uint16_t* out = a.out + ((size_t)(sp.tok0 + t) * p.H_q + (s % p.H_kv) * p.G + hh) * D + DPL * lane;
 #pragma unroll
     for (int c = 0; c < DPL; c += 2)
-        *reinterpret_cast<uint32_t*>(out + c) = pack_bf16x2(acc[c] * inv, acc[(c + 1) % DPL] * inv);
+        *reinterpret_cast<uint32_t*>(out + c) = pack_bf16x2(acc[c], acc[(c + 1) % DPL]);
 }
 
 // Chunks a stream takes at least: below this, splitting costs more than it saves.
@@ -769,7 +708,7 @@ constexpr int kMinChunks = 2;
 
 template <int D, int FMT>
 cudaError_t launch_stream(const CacheProblem& p, const CachePools& pool, const ChunkArgs& a,
-                          float* part, int* plan, uint32_t* status, cudaStream_t stream) {
+                          float* part, long long* plan, uint32_t* status, cudaStream_t stream) {
     using Gm = StreamGeom<D, FMT>;
     const int box = p.page < Gm::CH ? p.page : Gm::CH;
     alignas(64) CUtensorMap mk, mv;
@@ -786,26 +725,20 @@ cudaError_t launch_stream(const CacheProblem& p, const CachePools& pool, const C
     const int sms = device_sm_count();
     if (sms <= 0) return cudaErrorInvalidDevice;
     const int ctas = sms < kStreamMax / kW ? sms : kStreamMax / kW;
-    const long long all_rows = (long long)a.max_q * p.G;
-    for (long long row0 = 0; row0 < all_rows; row0 += kStreamRows) {
-        const int rec_rows = (int)(all_rows - row0 < kStreamRows ? all_rows - row0 : kStreamRows);
-        chunk_stream_kernel<D, FMT><<<ctas, kW * 32, smem, stream>>>(
-            mk, mv, p, pool, a, (int)row0, box, kMinChunks, rec_rows, part, plan, status);
-        if ((e = cudaGetLastError()) != cudaSuccess) return e;
-        const long long warps = (long long)p.S * rec_rows;
-        e = launch_dependent(chunk_stream_merge<D, Gm::CH>, dim3((unsigned)((warps + 3) / 4)),
-                             dim3(128), 0, stream, p, a, (int)row0, ctas * kW, (int)kMinChunks,
-                             rec_rows, static_cast<const float*>(part),
-                             static_cast<const int*>(plan));
-        if (e != cudaSuccess) return e;
-    }
-    return cudaSuccess;
+    const int rec_rows = a.max_q * p.G;
+    chunk_stream_kernel<D, FMT><<<ctas, kW * 32, smem, stream>>>(mk, mv, p, pool, a, box, kMinChunks,
+                                                                 rec_rows, part, plan, status);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    const long long warps = (long long)p.S * rec_rows;
+    return launch_dependent(chunk_stream_merge<D>, dim3((unsigned)((warps + 3) / 4)), dim3(128), 0,
+                            stream, p, a, ctas * kW, (int)kMinChunks, rec_rows,
+                            static_cast<const float*>(part), static_cast<const long long*>(plan));
 }
 
 }  // namespace
 
 cudaError_t launch_chunk_stream(const CacheProblem& p, const CachePools& pool, const ChunkArgs& a,
-                                float* part, int* plan, uint32_t* status, cudaStream_t stream) {
+                                float* part, long long* plan, uint32_t* status, cudaStream_t stream) {
     if (p.d == 64) {
         if (p.format == TGVKV_CACHE_BF16)
             return launch_stream<64, TGVKV_CACHE_BF16>(p, pool, a, part, plan, status, stream);

@@ -1,0 +1,842 @@
+// Attention of a chunk of new tokens over the paged cache on the 5th-generation
+// tensor cores (tcgen05), for sets with more than 16 query rows.
+//
+//   o[t][h] = sum_{j <= len - n + i} softmax_j(scale <q[t][h], k_j>) v_j
+//
+// A row tile is 128 query rows of a set: tpt = floor(128 / G) whole tokens times
+// the G query heads of the KV head, so every row of a tile reads the same K
+// and V.  Two groups of four softmax warps (thread = row) work in ping-pong, so
+// that the tensor cores have one group's products while the other does its
+// exponentials.  Their two streams are, by the call's longest chunk,
+//   PAIR   two consecutive row tiles over the same key tiles (each K / V tile is
+//          loaded once for 256 rows), when a chunk spans several row tiles;
+//   SPLIT  alternate key tiles of one row tile, joined at the segment's end
+//          (each group reading half of both O accumulators from TMEM).
+// A unit of work is one 128-slot key tile of an item (a row tile, or a pair);
+// each persistent CTA takes one contiguous share of the units of all items, so
+// ragged chunks, ragged lengths and single long caches all split evenly.  An item
+// that spans several CTAs leaves one partial (m, l, O) per CTA and row tile,
+// merged by a second kernel in CTA order.
+//
+// Tensor memory: S0, S1 (128 columns each), O0, O1 (D columns each).  P
+// (bf16) overwrites the first 64 columns of its S and is the A operand of P V
+// from there; K is the K-major and V the MN-major B operand from shared memory.
+// MMA order of one group: ... P V (j), Q K^T (j + 1) ..., the commit after Q K^T
+// covers both, so a softmax group that sees S (j + 1) knows that O holds j.
+//
+// Integer caches: TMA brings the codes of a key tile, eight converter warps
+// write them as bf16 in the swizzled layout (exact: scales are powers of two),
+// and the rest is the bf16 kernel.
+//
+// Roles: warp 0 TMA, warp 1 MMA issue (and TMEM), warps 4-11 softmax, warps
+// 12-19 converters (integer caches).  Every wait is bounded; a timeout sets
+// TGVKV_STATUS_TIMEOUT and the CTA unwinds after its copies and MMAs finished.
+#pragma once
+
+#include "cache_launch.h"
+#include "launch.h"
+#include "tc05.cuh"
+
+namespace tgvkv {
+
+constexpr int kSoftWarp = 4;           // first softmax warp
+constexpr int kConvWarp = 12;          // first converter warp
+constexpr int kConvWarps = 8;
+constexpr uint32_t kOCol = 256;        // first O column; S at 0 and 128
+constexpr float kRescale = 8.f;        // a stale maximum may trail by 2^8
+
+// D[tmem] (+)= A[tmem] * B[smem], issued by one thread.
+__device__ __forceinline__ void mma_bf16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t b,
+                                            uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_tmem), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+// Store 16 consecutive 32-bit columns of this thread's TMEM lane (warp-wide).
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+        "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
+        "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+        : "memory");
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
+// Untiled copy of `bytes` (a multiple of 16, both sides 16-byte aligned).
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+            smem_u32(dst)),
+        "l"(__cvta_generic_to_global(src)), "r"(bytes), "r"(smem_u32(bar))
+        : "memory");
+}
+
+template <int D, int FMT, bool PAIR>
+struct TileGeom {
+    static constexpr bool QUANT = FMT != TGVKV_CACHE_BF16;
+    static constexpr int TILE = D * 2 * TN;                       // bytes of a bf16 K or V tile
+    static constexpr int HALF = TN * 128;                         // bytes of its 64-dim half
+    static constexpr int NST = D == 64 ? 6 : QUANT ? 3 : PAIR ? 5 : 4;   // ring slots
+    static constexpr int ROWB = FMT == TGVKV_CACHE_INT8 ? D : D / 2;   // stored bytes a row
+    static constexpr int RAW = TN * ROWB, SC = TN * (D / kGroup); // raw tile, its scale bytes
+    static constexpr int NRAW = QUANT ? (FMT == TGVKV_CACHE_INT8 ? 3 : 6) : 0;
+    static constexpr int NQ = PAIR ? 1 : 2;                       // Q slots
+    static constexpr int QT = PAIR ? 2 : 1;                       // row tiles a slot
+    static constexpr int THREADS = 32 * (QUANT ? kConvWarp + kConvWarps : kConvWarp);
+};
+
+template <int D, int FMT, bool PAIR>
+struct TileSmem {
+    using Gm = TileGeom<D, FMT, PAIR>;
+    unsigned char q[Gm::NQ * Gm::QT][D * 2 * TM];     // 64 dims each, 128-byte swizzled rows
+    unsigned char kv[Gm::NST][Gm::TILE];              // the ring, in MMA order
+    unsigned char raw[Gm::QUANT ? Gm::NRAW : 1][Gm::QUANT ? Gm::RAW : 16];
+    unsigned char sc[Gm::QUANT ? Gm::NRAW : 1][Gm::QUANT ? Gm::SC : 16];
+    uint64_t full[Gm::NST], empty[Gm::NST];
+    uint64_t raw_full[Gm::QUANT ? Gm::NRAW : 1], raw_empty[Gm::QUANT ? Gm::NRAW : 1];
+    uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_done[2];
+    uint64_t join_in, join_out, mma_done;
+    float2 ml[PAIR ? 1 : 2][PAIR ? 1 : TM];           // SPLIT: the groups' (m, l)
+    uint32_t tmem_base;
+    int abort_flag, never;
+    long long warp_sum[Gm::THREADS / 32];
+    int start_s, start_u, start_j;
+};
+
+// ---- the work ----------------------------------------------------------------
+// A segment: key tiles [j0, j1) of item u of set s.
+struct Seg {
+    SetSpan sp;
+    int s, u, j0, j1, nk;              // nk: key tiles of the item
+    int tok0;                          // the item's first token within the chunk
+    bool starts;                       // begins the CTA's share
+};
+
+struct TileWalk {
+    SetSpan sp;
+    int s, u, j, left;
+    bool first;
+
+    __device__ __forceinline__ void init(const CacheProblem& p, const ChunkArgs& a, int s_, int u_,
+                                         int j_, int units) {
+        s = s_;
+        u = u_;
+        j = j_;
+        left = units;
+        first = true;
+        if (left > 0) sp = set_span(p, a, s);
+    }
+    __device__ __forceinline__ bool next(const CacheProblem& p, const ChunkArgs& a,
+                                         const TilePlan& pl, Seg& g) {
+        if (left <= 0) return false;
+        int nk = tiles_seen(sp, (u + 1) * pl.tpi);
+        while (u * pl.tpi >= sp.n || j >= nk) {
+            j = 0;
+            if (u * pl.tpi >= sp.n || ++u * pl.tpi >= sp.n) {
+                u = 0;
+                if (++s >= p.S) return false;
+                sp = set_span(p, a, s);
+            }
+            nk = tiles_seen(sp, (u + 1) * pl.tpi);
+        }
+        g.sp = sp;
+        g.s = s;
+        g.u = u;
+        g.j0 = j;
+        g.j1 = min(nk, j + left);
+        g.nk = nk;
+        g.tok0 = u * pl.tpi;
+        g.starts = first;
+        first = false;
+        left -= g.j1 - g.j0;
+        j = g.j1;
+        return true;
+    }
+};
+
+// Row tile w of a segment's item (PAIR), or its one row tile: its key tiles.
+template <bool PAIR>
+__device__ __forceinline__ int group_tiles(const Seg& g, const TilePlan& pl, int w) {
+    if (!PAIR) return g.nk;
+    const int t = g.tok0 + w * pl.tpt;
+    return t < g.sp.n ? tiles_seen(g.sp, t + pl.tpt) : 0;
+}
+
+// Place of key tile x (counted from the segment's first, of n) of K and of V in
+// the order of the ring.  PAIR: K0 V0 K1 V1 ...; SPLIT: K0 K1 V0 K2 V1 ...
+template <bool PAIR>
+__device__ __forceinline__ int k_place(int x) {
+    return PAIR ? 2 * x : (x == 0 ? 0 : 2 * x - 1);
+}
+template <bool PAIR>
+__device__ __forceinline__ int v_place(int x, int n) {
+    return PAIR ? 2 * x + 1 : min(2 * x + 2, 2 * n - 1);
+}
+
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort) {
+    return __all_sync(~0u, tc::mbar_wait(bar, parity, abort));
+}
+
+template <int D, int FMT, bool PAIR>
+__global__ void __launch_bounds__(TileGeom<D, FMT, PAIR>::THREADS, 1)
+chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
+                  const __grid_constant__ CUtensorMap mv, const CacheProblem p,
+                  const CachePools pool, const ChunkArgs a, const TilePlan pl,
+                  float* __restrict__ part, long long* __restrict__ plan,
+                  uint32_t* __restrict__ status) {
+    using Gm = TileGeom<D, FMT, PAIR>;
+    constexpr bool QUANT = Gm::QUANT;
+    constexpr int NST = Gm::NST, NRAW = QUANT ? Gm::NRAW : 1;
+    griddep_launch_dependents();
+    extern __shared__ unsigned char smem_raw[];
+    const uint32_t raw_addr = smem_u32(smem_raw);
+    TileSmem<D, FMT, PAIR>& sm = *reinterpret_cast<TileSmem<D, FMT, PAIR>*>(
+        smem_raw + (((raw_addr + 1023u) & ~1023u) - raw_addr));
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    if (tid == 0) {
+        sm.abort_flag = 0;
+        sm.never = 0;
+        for (int i = 0; i < NST; ++i) {
+            tc::mbar_init(&sm.full[i], QUANT ? kConvWarps : 1);
+            tc::mbar_init(&sm.empty[i], 1);
+        }
+        for (int i = 0; i < NRAW; ++i) {
+            tc::mbar_init(&sm.raw_full[i], 1);
+            tc::mbar_init(&sm.raw_empty[i], kConvWarps);
+        }
+        for (int i = 0; i < 2; ++i) {
+            tc::mbar_init(&sm.q_full[i], 1);
+            tc::mbar_init(&sm.q_empty[i], 1);
+            tc::mbar_init(&sm.s_full[i], 1);
+            tc::mbar_init(&sm.p_full[i], 4);
+            tc::mbar_init(&sm.o_done[i], 1);
+        }
+        tc::mbar_init(&sm.join_in, 8);
+        tc::mbar_init(&sm.join_out, 8);
+        tc::mbar_init(&sm.mma_done, 1);
+        tc::fence_mbar_init();
+        tc::tma_prefetch_desc(&mq);
+        if (!QUANT) {
+            tc::tma_prefetch_desc(&mk);
+            tc::tma_prefetch_desc(&mv);
+        }
+    }
+    if (warp == 1) {
+        tc::tmem_alloc(&sm.tmem_base, 512);
+        tc::tmem_relinquish();
+    }
+    if (blockIdx.x == 0) check_spans(p, a, tid, Gm::THREADS, status);
+
+    // ---- this CTA's share: units [c0, c0 + count) of all
+    const int run = (p.S + Gm::THREADS - 1) / Gm::THREADS;    // sets a thread sums
+    const int s_lo = min(tid * run, p.S), s_hi = min(s_lo + run, p.S);
+    long long sum = 0;
+    for (int s = s_lo; s < s_hi; ++s) sum += set_units(set_span(p, a, s), pl);
+    long long incl = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long y = __shfl_up_sync(~0u, incl, o);
+        if (lane >= o) incl += y;
+    }
+    if (lane == 31) sm.warp_sum[warp] = incl;
+    __syncthreads();
+    long long base = incl - sum, total = 0;
+#pragma unroll
+    for (int w = 0; w < Gm::THREADS / 32; ++w) {
+        if (w < warp) base += sm.warp_sum[w];
+        total += sm.warp_sum[w];
+    }
+    const long long per = (total + gridDim.x - 1) / gridDim.x;
+    const long long c0 = blockIdx.x * per;
+    const int count = (int)max(min(total - c0, per), 0ll);
+    if (count > 0 && c0 >= base && c0 < base + sum) {   // the first unit is in my sets
+        long long at = c0 - base;
+        for (int s = s_lo; s < s_hi; ++s) {
+            const SetSpan sp = set_span(p, a, s);
+            for (int u = 0; u * pl.tpi < sp.n; ++u) {
+                const int nk = tiles_seen(sp, (u + 1) * pl.tpi);
+                if (at >= 0 && at < nk) {
+                    sm.start_s = s;
+                    sm.start_u = u;
+                    sm.start_j = (int)at;
+                }
+                at -= nk;
+            }
+        }
+    }
+    if (blockIdx.x == 0) {             // the plan, for the merge kernel
+        long long at = base;
+        for (int s = s_lo; s < s_hi; ++s) {
+            plan[s] = at;
+            at += set_units(set_span(p, a, s), pl);
+        }
+        if (tid == 0) plan[p.S] = total;
+    }
+    tc::fence_before_sync();
+    __syncthreads();
+    tc::fence_after_sync();
+    const uint32_t tmem = sm.tmem_base;
+    volatile int* abort_flag = &sm.abort_flag;
+    TileWalk walk;
+    walk.init(p, a, count > 0 ? sm.start_s : 0, count > 0 ? sm.start_u : 0,
+              count > 0 ? sm.start_j : 0, count);
+    Seg g;
+
+    // ------------------------------------------------------------ producer
+    if (warp == 0) {
+        const int box = min(p.page, TN), boxes = TN / box;       // page slices of a key tile
+        const uint32_t q_bytes = (uint32_t)(D / 64) * 128u * (uint32_t)(pl.tpt * p.G);
+        int it = 0, ns = 0, nq[2] = {0, 0};
+        bool ok = true;
+        for (; ok && walk.next(p, a, pl, g); ++ns) {
+            const int slot = ns % Gm::NQ;
+            const int gk = g.s % p.H_kv, n = g.j1 - g.j0;
+            const int32_t* table = a.page_table + (size_t)g.s * p.max_pages;
+            if (!warp_wait(&sm.q_empty[slot], ((ns / Gm::NQ) & 1) ^ 1, abort_flag)) {
+                ok = false;
+                break;
+            }
+            if (lane == 0) {
+                const int tiles = PAIR && g.tok0 + pl.tpt < g.sp.n ? 2 : 1;
+                tc::mbar_arrive_expect_tx(&sm.q_full[slot], tiles * q_bytes);
+                for (int t = 0; t < tiles; ++t)
+                    for (int h = 0; h < D / 64; ++h)
+                        asm volatile(
+                            "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes"
+                            " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+                                smem_u32(&sm.q[slot * Gm::QT + t][h * TM * 128])),
+                            "l"(reinterpret_cast<uint64_t>(&mq)), "r"(64 * h), "r"(gk * p.G),
+                            "r"(g.sp.tok0 + g.tok0 + t * pl.tpt), "r"(smem_u32(&sm.q_full[slot]))
+                            : "memory");
+            }
+            ++nq[slot];
+            // lane b (and 16 + b): page slice b of the tile.  The order of the ring:
+            // place i holds V of tile x when i is v_place(x), else the next K.
+            const int b = lane & 15;
+            int kx = 0, vx = 0;
+            auto page_of = [&](int x) {
+                const int slot0 = (g.j0 + x) * TN + b * box;
+                return b < boxes && x < n && slot0 < g.sp.len ? __ldg(table + (slot0 >> p.page_shift))
+                                                              : 0;
+            };
+            int k_page = page_of(0), v_page = k_page;
+            for (int i = 0; ok && i < 2 * n; ++i) {
+                const bool is_v = vx < kx && i == v_place<PAIR>(vx, n);
+                const int x = is_v ? vx : kx;
+                int page = is_v ? v_page : k_page;
+                if (page < 0 || page >= p.n_pages) {
+                    raise_status(status, TGVKV_STATUS_INDEX);
+                    page = 0;
+                }
+                const int st = QUANT ? it % NRAW : it % NST;
+                const int ph = QUANT ? (it / NRAW) & 1 : (it / NST) & 1;
+                if (!warp_wait(QUANT ? &sm.raw_empty[st] : &sm.empty[st], ph ^ 1, abort_flag)) {
+                    ok = false;
+                    break;
+                }
+                const int valid = min(g.sp.len - (g.j0 + x) * TN, TN);
+                const int nb = (valid + box - 1) / box;
+                const int row = page * p.page + ((b * box) & (p.page - 1)) +
+                                (p.page > TN ? ((g.j0 + x) * TN & (p.page - 1)) : 0);
+                if (QUANT) {
+                    if (lane == 0)
+                        tc::mbar_arrive_expect_tx(&sm.raw_full[st],
+                                                  (uint32_t)(nb * box) * (Gm::ROWB + D / kGroup));
+                    __syncwarp();
+                    if (lane < nb) {
+                        const uint8_t* src = (is_v ? pool.v : pool.k) + (size_t)row * Gm::ROWB;
+                        bulk_load(&sm.raw[st][b * box * Gm::ROWB], src, box * Gm::ROWB, &sm.raw_full[st]);
+                    } else if (lane >= 16 && b < nb) {
+                        const uint8_t* src = (is_v ? pool.vs : pool.ks) + (size_t)row * (D / kGroup);
+                        bulk_load(&sm.sc[st][b * box * (D / kGroup)], src, box * (D / kGroup),
+                                  &sm.raw_full[st]);
+                    }
+                } else {
+                    if (lane == 0)
+                        tc::mbar_arrive_expect_tx(&sm.full[st], (uint32_t)(nb * box) * 2 * D);
+                    __syncwarp();
+                    const int h = lane >> 4;
+                    if (b < nb && h < D / 64)
+                        tc::tma_load_2d(&sm.kv[st][h * Gm::HALF + b * box * 128], is_v ? &mv : &mk,
+                                        128 * h, row, &sm.full[st]);
+                }
+                ++it;
+                // the next page numbers, a load ahead of their use
+                if (is_v) v_page = page_of(++vx);
+                else k_page = page_of(++kx);
+            }
+        }
+        if (!ok && lane == 0) {
+            sm.abort_flag = 1;
+            raise_status(status, TGVKV_STATUS_TIMEOUT);
+        }
+        __syncwarp();
+        // every copy this CTA issued has landed before it may exit
+        for (int slot = 0; slot < Gm::NQ; ++slot)
+            if (nq[slot] > 0) warp_wait(&sm.q_full[slot], (nq[slot] - 1) & 1, &sm.never);
+        constexpr int N = QUANT ? NRAW : NST;
+        for (int i = it > N ? it - N : 0; i < it; ++i)
+            warp_wait(QUANT ? &sm.raw_full[i % N] : &sm.full[i % N], (i / N) & 1, &sm.never);
+    }
+
+    // ------------------------------------------------------------ MMA issuer
+    if (warp == 1 && lane == 0) {
+        const uint64_t qd0 = tc::sdesc_k_sw128(smem_u32(&sm.q[0][0]));
+        const uint64_t kd0 = tc::sdesc_k_sw128(smem_u32(&sm.kv[0][0]));
+        const uint64_t vd0 = tc::sdesc_mn_sw128(smem_u32(&sm.kv[0][0]), Gm::HALF);
+        constexpr uint32_t QTILE = D * 2 * TM / 16, SLOT = Gm::TILE / 16, HALF16 = Gm::HALF / 16;
+        constexpr uint32_t IDESC_QK = tc::idesc_bf16(TM, TN), IDESC_PV = tc::idesc_bf16_bmn(TM, D);
+        int base_it = 0, ns = 0, np[2] = {0, 0};
+        bool ok = true;
+        auto wait = [&](uint64_t* bar, uint32_t parity) {
+            if (ok && !tc::mbar_wait(bar, parity, abort_flag)) ok = false;
+            if (ok) tc::fence_after_sync();
+            return ok;
+        };
+        // S_w = Q_w K^T with the K tile at ring place i
+        auto qk = [&](int w, int slot, int i) {
+            const uint64_t qd = qd0 + (uint64_t)((slot * Gm::QT + (PAIR ? w : 0)) * QTILE);
+            const uint64_t kd = kd0 + (uint64_t)((i % NST) * SLOT);
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) {
+                const uint64_t off = (uint64_t)((kk >> 2) * HALF16 + (kk & 3) * 2);
+                tc::mma_bf16(tmem + (uint32_t)(w * TN), qd + off, kd + off, IDESC_QK, kk > 0 ? 1u : 0u);
+            }
+            tc::mma_commit(&sm.s_full[w]);
+        };
+        // O_w (+)= P_w V with the V tile at ring place i
+        auto pv = [&](int w, int i, bool accumulate) {
+            const uint64_t vd = vd0 + (uint64_t)((i % NST) * SLOT);
+#pragma unroll
+            for (int kk = 0; kk < TN / 16; ++kk)
+                mma_bf16_ta(tmem + kOCol + (uint32_t)(w * D), tmem + (uint32_t)(w * TN + kk * 8),
+                            vd + (uint64_t)(kk * (16 * 128 / 16)), IDESC_PV,
+                            (accumulate || kk > 0) ? 1u : 0u);
+        };
+        for (; ok && walk.next(p, a, pl, g); ++ns) {
+            const int slot = ns % Gm::NQ, n = g.j1 - g.j0;
+            // tiles of each group in this segment
+            int hi[2];
+            for (int w = 0; w < 2; ++w)
+                hi[w] = PAIR ? min(group_tiles<PAIR>(g, pl, w), g.j1) - g.j0 : n;
+            if (!wait(&sm.q_full[slot], (ns / Gm::NQ) & 1)) break;
+            auto full = [&](int i) { return wait(&sm.full[i % NST], (i / NST) & 1); };
+            if (PAIR) {
+                if (!full(base_it + k_place<PAIR>(0))) break;
+                for (int w = 0; w < 2; ++w)
+                    if (0 < hi[w]) qk(w, slot, base_it);
+                tc::mma_commit(&sm.empty[base_it % NST]);
+                if (n == 1) tc::mma_commit(&sm.q_empty[slot]);
+                for (int x = 0; ok && x < n; ++x) {
+                    const int vi = base_it + v_place<PAIR>(x, n), ki = base_it + k_place<PAIR>(x + 1);
+                    bool v_in = false, k_in = false;
+                    for (int w = 0; ok && w < 2; ++w) {
+                        if (x >= hi[w]) continue;
+                        if (!wait(&sm.p_full[w], np[w]++ & 1)) break;
+                        if (!v_in && !full(vi)) break;
+                        v_in = true;
+                        pv(w, vi, x > 0);
+                        if (x + 1 < hi[w]) {
+                            if (!k_in && !full(ki)) break;
+                            k_in = true;
+                            qk(w, slot, ki);
+                        } else {
+                            tc::mma_commit(&sm.o_done[w]);
+                        }
+                    }
+                    if (!ok) break;
+                    // a tile that neither group uses is still waited for: its slot is reused
+                    if (!v_in && !full(vi)) break;
+                    tc::mma_commit(&sm.empty[vi % NST]);
+                    if (x + 1 < n) {
+                        if (!k_in && !full(ki)) break;
+                        tc::mma_commit(&sm.empty[ki % NST]);
+                        if (x + 2 == n) tc::mma_commit(&sm.q_empty[slot]);
+                    }
+                }
+            } else {
+                for (int x = 0; ok && x < min(n, 2); ++x) {
+                    const int ki = base_it + k_place<PAIR>(x);
+                    if (!full(ki)) break;
+                    qk(x, slot, ki);
+                    tc::mma_commit(&sm.empty[ki % NST]);
+                    if (x + 1 == n) tc::mma_commit(&sm.q_empty[slot]);
+                }
+                for (int x = 0; ok && x < n; ++x) {
+                    const int w = x & 1, vi = base_it + v_place<PAIR>(x, n);
+                    if (!wait(&sm.p_full[w], np[w]++ & 1) || !full(vi)) break;
+                    pv(w, vi, x > 1);
+                    tc::mma_commit(&sm.empty[vi % NST]);
+                    if (x + 2 < n) {
+                        const int ki = base_it + k_place<PAIR>(x + 2);
+                        if (!full(ki)) break;
+                        qk(w, slot, ki);
+                        tc::mma_commit(&sm.empty[ki % NST]);
+                        if (x + 3 == n) tc::mma_commit(&sm.q_empty[slot]);
+                    }
+                }
+                if (!ok) break;
+                tc::mma_commit(&sm.o_done[0]);
+                tc::mma_commit(&sm.o_done[1]);
+            }
+            base_it += 2 * n;
+        }
+        if (!ok) {
+            sm.abort_flag = 1;
+            raise_status(status, TGVKV_STATUS_TIMEOUT);
+        }
+        // every MMA this CTA issued has finished before TMEM is released
+        tc::mma_commit(&sm.mma_done);
+        tc::mbar_wait(&sm.mma_done, 0, &sm.never);
+    }
+
+    // ------------------------------------------------------------ softmax
+    if (warp >= kSoftWarp && warp < kConvWarp) {
+        const int w = (warp - kSoftWarp) >> 2;               // group
+        const int quarter = warp & 3;                        // TMEM lanes of this warp
+        const int r = quarter * 32 + lane;                   // row of the tile
+        const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
+        const uint32_t ts = lanes + (uint32_t)(w * TN), to = lanes + kOCol + (uint32_t)(w * D);
+        const float sl2 = p.scale_log2;
+        const int ri = r / p.G, rh = r - ri * p.G;           // token within the tile, head
+        constexpr int CB = 64;                               // S columns held at a time
+        int ns = 0, nso = 0, npart = 0, base_it = 0;
+        bool ok = true;
+        for (; ok && walk.next(p, a, pl, g); ++npart) {
+            const int n = g.j1 - g.j0;
+            const int tok = g.tok0 + (PAIR ? w * pl.tpt : 0);        // the tile's first token
+            const int hi = PAIR ? min(group_tiles<PAIR>(g, pl, w), g.j1) - g.j0 : n;
+            const int toks = min(g.sp.n - tok, pl.tpt);              // its tokens (<= 0: none)
+            const bool valid = ri < toks;
+            const bool warp_on = quarter * 32 < toks * p.G;          // some row of the warp is real
+            // slots that this row sees: its own and those before
+            const int lim = min(g.sp.len - g.sp.n + min(tok + ri, g.sp.n - 1) + 1, g.sp.len);
+            float m = -INFINITY, l = 0.f;
+            for (int x = PAIR ? 0 : w; x < hi; x += PAIR ? 1 : 2) {
+                if (!warp_wait(&sm.s_full[w], ns & 1, abort_flag)) {
+                    ok = false;
+                    break;
+                }
+                ++ns;
+                tc::fence_after_sync();
+                const int j = g.j0 + x;
+                const int seen = lim - j * TN;               // columns seen of this tile
+                const bool masked = __any_sync(~0u, seen < TN);
+                if (warp_on) {
+                    float y[CB];
+                    float mx = -INFINITY;
+                    auto load = [&](int c0) {
+#pragma unroll
+                        for (int c = 0; c < CB / 32; ++c) {
+                            float t[32];
+                            tc::tmem_ld32(ts + (uint32_t)(c0 + 32 * c), t);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) y[32 * c + e] = t[e];
+                        }
+                        tc::tmem_wait_ld();
+                        if (masked) {
+#pragma unroll
+                            for (int e = 0; e < CB; ++e)
+                                if (c0 + e >= seen) y[e] = -INFINITY;
+                        }
+                    };
+#pragma unroll
+                    for (int c0 = 0; c0 < TN; c0 += CB) {
+                        load(c0);
+                        float ma = -INFINITY, mb = -INFINITY;
+#pragma unroll
+                        for (int e = 0; e < CB; e += 4) {
+                            ma = max3(ma, y[e], y[e + 1]);
+                            mb = max3(mb, y[e + 2], y[e + 3]);
+                        }
+                        mx = max3(mx, ma, mb);
+                    }
+                    const float mt = mx * sl2;
+                    float alpha = 1.f;
+                    if (mt > m + kRescale) {                 // also the first tile with something seen
+                        alpha = fast_exp2(m - mt);
+                        m = mt;
+                        l *= alpha;
+                    }
+                    const float ref = m == -INFINITY ? 0.f : m;
+                    // O holds the tiles before this one (the commit of S covers P V before it)
+                    if (x > (PAIR ? 0 : 1) && __any_sync(~0u, alpha != 1.f)) {
+#pragma unroll
+                        for (int c = 0; c < D / 32; ++c) {
+                            float t[32];
+                            tc::tmem_ld32(to + (uint32_t)(32 * c), t);
+                            tc::tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) t[e] *= alpha;
+                            tc::tmem_st32(to + (uint32_t)(32 * c), t);
+                        }
+                    }
+                    const float2 s2 = make_float2(sl2, sl2), n2 = make_float2(-ref, -ref);
+                    float2 za = make_float2(0.f, 0.f), zb = za;
+#pragma unroll
+                    for (int c0 = 0; c0 < TN; c0 += CB) {
+                        if (CB < TN) load(c0);
+#pragma unroll
+                        for (int c = 0; c < CB; c += 32) {
+                            uint32_t pk[16];
+#pragma unroll
+                            for (int e = 0; e < 32; e += 4) {
+                                const float2 t0 = fma2(make_float2(y[c + e], y[c + e + 1]), s2, n2);
+                                const float2 t1 = fma2(make_float2(y[c + e + 2], y[c + e + 3]), s2, n2);
+                                const float2 e0 = make_float2(fast_exp2(t0.x), fast_exp2(t0.y));
+                                const float2 e1 = make_float2(fast_exp2(t1.x), fast_exp2(t1.y));
+                                za = add2(za, e0);
+                                zb = add2(zb, e1);
+                                pk[e / 2] = pack_bf16x2(e0.x, e0.y);
+                                pk[e / 2 + 1] = pack_bf16x2(e1.x, e1.y);
+                            }
+                            tmem_st16(ts + (uint32_t)((c0 + c) / 2), pk);
+                        }
+                    }
+                    l += (za.x + za.y) + (zb.x + zb.y);
+                    tc::tmem_wait_st();
+                }
+                // bf16 caches: the pool's rows past the set's end may hold anything, and
+                // 0 x NaN is not 0, so V's rows there are cleared (the converters do it
+                // for integer caches)
+                const int live = g.sp.len - j * TN;
+                if (!QUANT && live < TN) {
+                    const int vi = base_it + v_place<PAIR>(x, n);
+                    if (!warp_wait(&sm.full[vi % NST], (vi / NST) & 1, abort_flag)) {
+                        ok = false;
+                        break;
+                    }
+                    for (int e = quarter * 32 + lane; e < (TN - live) * (D / 8); e += TM) {
+                        const int row = live + e / (D / 8), u = e % (D / 8);
+                        *reinterpret_cast<uint4*>(&sm.kv[vi % NST][(u >> 3) * Gm::HALF + row * 128 +
+                                                                  (u & 7) * 16]) =
+                            make_uint4(0u, 0u, 0u, 0u);
+                    }
+                    tc::fence_proxy_async_smem();
+                }
+                tc::fence_before_sync();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(&sm.p_full[w]);
+            }
+            if (!ok) break;
+            base_it += 2 * n;
+
+            // ---- the segment's end: a whole item is written out, a part kept for the merge
+            const bool whole = g.j0 == 0 && g.j1 == g.nk;
+            const size_t rec = (size_t)((blockIdx.x * 2 + (g.starts ? 0 : 1)) * (PAIR ? 2 : 1) + (PAIR ? w : 0));
+            float* pp = part + rec * chunk_record_floats(pl.rows, D);
+            uint16_t* op = a.out + ((size_t)(g.sp.tok0 + (valid ? tok + ri : 0)) * p.H_q +
+                                    (g.s % p.H_kv) * p.G + rh) * D;
+            if (PAIR) {
+                if (hi > 0) {
+                    if (!warp_wait(&sm.o_done[w], nso & 1, abort_flag)) {
+                        ok = false;
+                        break;
+                    }
+                    ++nso;
+                    tc::fence_after_sync();
+                }
+                const float inv = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) {
+                    float t[32];
+                    if (hi > 0 && warp_on) {
+                        tc::tmem_ld32(to + (uint32_t)(32 * c), t);
+                        tc::tmem_wait_ld();
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) t[e] = 0.f;
+                    }
+                    if (valid && whole) {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 8)
+                            *reinterpret_cast<uint4*>(op + 32 * c + e) = make_uint4(
+                                pack_bf16x2(t[e] * inv, t[e + 1] * inv),
+                                pack_bf16x2(t[e + 2] * inv, t[e + 3] * inv),
+                                pack_bf16x2(t[e + 4] * inv, t[e + 5] * inv),
+                                pack_bf16x2(t[e + 6] * inv, t[e + 7] * inv));
+                    } else if (valid) {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4)
+                            *reinterpret_cast<float4*>(pp + r * D + 32 * c + e) =
+                                make_float4(t[e], t[e + 1], t[e + 2], t[e + 3]);
+                    }
+                    __syncwarp();
+                }
+                tc::fence_before_sync();
+                if (valid && !whole) {
+                    pp[pl.rows * D + r] = m;
+                    pp[pl.rows * D + pl.rows + r] = l;
+                }
+            } else {
+                // join the groups' halves: each takes half of the dims of both O
+                sm.ml[w][r] = make_float2(m, l);
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(&sm.join_in);
+                if (!warp_wait(&sm.o_done[0], npart & 1, abort_flag) ||
+                    !warp_wait(&sm.o_done[1], npart & 1, abort_flag) ||
+                    !warp_wait(&sm.join_in, npart & 1, abort_flag)) {
+                    ok = false;
+                    break;
+                }
+                tc::fence_after_sync();
+                const float2 a0 = sm.ml[0][r], a1 = sm.ml[PAIR ? 0 : 1][r];
+                const float M = fmaxf(a0.x, a1.x), ref = M == -INFINITY ? 0.f : M;
+                const float f0 = fast_exp2(a0.x - ref), f1 = fast_exp2(a1.x - ref);
+                const float L = a0.y * f0 + a1.y * f1;
+                const float inv = L > 0.f ? 1.f / L : (L == L ? 0.f : L);
+                // (a group that had no tile left its O as it was: its factor is 0)
+                const bool one = n == 1;
+                constexpr int HD = D / 2;
+                if (warp_on) {
+#pragma unroll
+                    for (int c = 0; c < HD / 32; ++c) {
+                        const int col = w * HD + 32 * c;
+                        float t[32];
+                        tc::tmem_ld32(lanes + kOCol + (uint32_t)col, t);
+                        tc::tmem_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) t[e] *= f0;
+                        if (!one) {
+                            float t1[32];
+                            tc::tmem_ld32(lanes + kOCol + (uint32_t)(D + col), t1);
+                            tc::tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) t[e] += t1[e] * f1;
+                        }
+                        if (valid && whole) {
+#pragma unroll
+                            for (int e = 0; e < 32; e += 8)
+                                *reinterpret_cast<uint4*>(op + col + e) = make_uint4(
+                                    pack_bf16x2(t[e] * inv, t[e + 1] * inv),
+                                    pack_bf16x2(t[e + 2] * inv, t[e + 3] * inv),
+                                    pack_bf16x2(t[e + 4] * inv, t[e + 5] * inv),
+                                    pack_bf16x2(t[e + 6] * inv, t[e + 7] * inv));
+                        } else if (valid) {
+#pragma unroll
+                            for (int e = 0; e < 32; e += 4)
+                                *reinterpret_cast<float4*>(pp + r * D + col + e) =
+                                    make_float4(t[e], t[e + 1], t[e + 2], t[e + 3]);
+                        }
+                        __syncwarp();
+                    }
+                    if (valid && !whole && w == 0) {
+                        pp[pl.rows * D + r] = M;
+                        pp[pl.rows * D + pl.rows + r] = L;
+                    }
+                }
+                tc::fence_before_sync();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(&sm.join_out);
+                // both O and (m, l) are free again
+                if (!warp_wait(&sm.join_out, npart & 1, abort_flag)) {
+                    ok = false;
+                    break;
+                }
+                tc::fence_after_sync();
+            }
+        }
+        if (!ok) {
+            sm.abort_flag = 1;
+            if (lane == 0) raise_status(status, TGVKV_STATUS_TIMEOUT);
+        }
+    }
+
+    // ------------------------------------------------------------ converters
+    if (QUANT && warp >= kConvWarp) {
+        const int ct = tid - kConvWarp * 32;
+        int it = 0;
+        bool ok = true;
+        while (ok && walk.next(p, a, pl, g)) {
+            const int n = g.j1 - g.j0;
+            int kx = 0, vx = 0;
+            for (int i = 0; ok && i < 2 * n; ++i, ++it) {
+                const bool is_v = vx < kx && i == v_place<PAIR>(vx, n);
+                const int x = is_v ? vx++ : kx++;
+                const int live = min(g.sp.len - (g.j0 + x) * TN, TN);
+                const int rs = it % NRAW, st = it % NST;
+                if (!warp_wait(&sm.raw_full[rs], (it / NRAW) & 1, abort_flag) ||
+                    !warp_wait(&sm.empty[st], ((it / NST) & 1) ^ 1, abort_flag)) {
+                    ok = false;
+                    break;
+                }
+                constexpr int UNITS = TN * (D / 8);          // 8 values each
+                const unsigned char* raw = sm.raw[rs];
+                unsigned char* dst = sm.kv[st];
+#pragma unroll 4
+                for (int e = ct; e < UNITS; e += kConvWarps * 32) {
+                    const int row = e / (D / 8), u = e % (D / 8);
+                    uint2 c = make_uint2(0u, 0u);
+                    if (FMT == TGVKV_CACHE_INT8) c = reinterpret_cast<const uint2*>(raw)[e];
+                    else c.x = reinterpret_cast<const uint32_t*>(raw)[e];
+                    uint4 v = codes_to_bf16<FMT>(c, sm.sc[rs][row * (D / kGroup) + (u >> 2)]);
+                    if (row >= live) v = make_uint4(0u, 0u, 0u, 0u);   // past the set's end
+                    *reinterpret_cast<uint4*>(dst + (u >> 3) * Gm::HALF + row * 128 +
+                                              (((u & 7) ^ (row & 7)) << 4)) = v;
+                }
+                tc::fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    tc::mbar_arrive(&sm.full[st]);
+                    tc::mbar_arrive(&sm.raw_empty[rs]);
+                }
+            }
+        }
+        if (!ok) {
+            sm.abort_flag = 1;
+            if (lane == 0) raise_status(status, TGVKV_STATUS_TIMEOUT);
+        }
+    }
+
+    // ------------------------------------------------------------ teardown
+    __syncwarp();
+    tc::fence_before_sync();
+    __syncthreads();
+    if (warp == 1) {
+        tc::fence_after_sync();
+        tc::tmem_dealloc(tmem, 512);
+    }
+}
+
+template <int D, int FMT, bool PAIR>
+cudaError_t launch_tile(const CacheProblem& p, const CachePools& pool, const ChunkArgs& a,
+                        float* part, long long* plan, uint32_t* status, cudaStream_t stream) {
+    using Sm = TileSmem<D, FMT, PAIR>;
+    static_assert(sizeof(Sm) + 1024 <= 227 * 1024, "shared memory of one CTA");
+    TilePlan pl;
+    pl.tpt = TM / p.G;
+    pl.tpi = PAIR ? 2 * pl.tpt : pl.tpt;
+    pl.rows = pl.tpt * p.G;
+    alignas(64) CUtensorMap mq, mk, mv;
+    if (!make_query_map(&mq, p, a, p.G, pl.tpt)) return cudaErrorInvalidValue;
+    mk = mv = mq;                      // not used by integer caches
+    const uint64_t rows = (uint64_t)p.n_pages * p.page;
+    if (FMT == TGVKV_CACHE_BF16 &&
+        (!make_pool_map(&mk, pool.k, rows, 2 * D, 128, p.page < TN ? p.page : TN) ||
+         !make_pool_map(&mv, pool.v, rows, 2 * D, 128, p.page < TN ? p.page : TN)))
+        return cudaErrorInvalidValue;
+    const size_t smem = sizeof(Sm) + 1024;
+    cudaError_t e = cudaFuncSetAttribute(chunk_tile_kernel<D, FMT, PAIR>,
+                                         cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    const int sms = device_sm_count();
+    if (sms <= 0) return cudaErrorInvalidDevice;
+    const int ctas = sms < kTileMaxCtas ? sms : kTileMaxCtas;
+    chunk_tile_kernel<D, FMT, PAIR><<<ctas, TileGeom<D, FMT, PAIR>::THREADS, smem, stream>>>(
+        mq, mk, mv, p, pool, a, pl, part, plan, status);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    return launch_tile_merge(p, a, pl, ctas, part, plan, stream);
+}
+
+}  // namespace tgvkv

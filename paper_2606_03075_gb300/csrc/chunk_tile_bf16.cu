@@ -1,0 +1,17 @@
+// The tile kernel of chunk_tile.cuh over bf16 caches.
+#include "chunk_tile.cuh"
+
+namespace tgvkv {
+
+cudaError_t launch_tile_bf16(const CacheProblem& p, const CachePools& pool, const ChunkArgs& a,
+                             float* part, long long* plan, bool pair, uint32_t* status,
+                             cudaStream_t stream) {
+    constexpr int F = TGVKV_CACHE_BF16;
+    if (p.d == 64)
+        return pair ? launch_tile<64, F, true>(p, pool, a, part, plan, status, stream)
+                    : launch_tile<64, F, false>(p, pool, a, part, plan, status, stream);
+    return pair ? launch_tile<128, F, true>(p, pool, a, part, plan, status, stream)
+                : launch_tile<128, F, false>(p, pool, a, part, plan, status, stream);
+}
+
+}  // namespace tgvkv
