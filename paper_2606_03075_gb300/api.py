@@ -9,6 +9,7 @@ provides device memory and streams.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 from dataclasses import dataclass
 
@@ -64,10 +65,11 @@ def desc_for_workload(wl, softmax_scale=0.0, **options) -> Desc:
 
 def _stream(stream):
     if stream is None:
-        return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+        # the current stream's handle, without a Stream object around it (5 us a call)
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     if isinstance(stream, torch.cuda.Stream):
-        return ctypes.c_void_p(stream.cuda_stream)
-    return ctypes.c_void_p(int(stream))
+        return stream.cuda_stream
+    return int(stream)
 
 
 def _ptr(t, dtypes, numel, name):
@@ -83,7 +85,7 @@ def _ptr(t, dtypes, numel, name):
         raise ValueError(f"{name} must be contiguous")
     if t.numel() < numel:
         raise ValueError(f"{name} holds {t.numel()} elements, needs {numel}")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def _check(code, fn):
@@ -420,11 +422,19 @@ def alloc_cache(desc: CacheDesc, device=None) -> PagedCache:
     return PagedCache(*new)
 
 
+@functools.lru_cache(maxsize=256)
+def _cache_ws_bytes(fields: bytes) -> int:
+    return int(_lib.load().tgvkv_cache_workspace_size(
+        ctypes.byref(CacheDesc.from_buffer_copy(fields))))
+
+
 def tgvkv_cache_workspace_size(desc: CacheDesc) -> int:
-    n = _lib.load().tgvkv_cache_workspace_size(ctypes.byref(desc))
+    n = _cache_ws_bytes(bytes(desc))
     if n == 0:
+        # not from the cache: the library's message is this call's
+        _lib.load().tgvkv_cache_workspace_size(ctypes.byref(desc))
         raise TgvkvError(-1, "tgvkv_cache_workspace_size")
-    return int(n)
+    return n
 
 
 def tgvkv_cache_workspace_init(desc: CacheDesc, ws: torch.Tensor, stream=None):
@@ -469,7 +479,7 @@ def _tokens(t, heads, d, name):
     # the stride of a dimension with one entry never matters
     tok = t.stride(0) if t.shape[0] > 1 else heads * d
     head = t.stride(1) if heads > 1 and t.numel() else d
-    return ctypes.c_void_p(t.data_ptr()), tok, head
+    return t.data_ptr(), tok, head
 
 
 def _page_table(desc, page_table):

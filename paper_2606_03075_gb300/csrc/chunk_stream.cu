@@ -16,15 +16,19 @@
 // chunk's page numbers are fetched one chunk ahead.
 //
 // Arithmetic per chunk on the tensor cores (mma.sync m16n8k16: bf16 operands,
-// fp32 accumulation), which can take operands converted in registers:
-//   S = Q K^T    integer K: a lane holds D / 4 consecutive values of a key
-//                (whole scale groups), Q's fragments follow the same order;
-//   O += P V     integer V: ldmatrix transposes pairs of slots; the values
-//                they hold spread over neighbouring column tiles of O.
-// Online softmax in base 2 (fp32); P is rounded to bf16 for the product, the
-// normaliser sums the unrounded P.  A set inside one stream is written out at
-// once; a split one leaves a partial (m, l, O) per stream, merged by a second
-// kernel in stream order, so results do not depend on timing.
+// fp32 accumulation), whose operands can be converted in registers, with the
+// cache's rows on the long side so that 8 query rows fill an instruction:
+//   S^T = K Q^T   16 slots x 8 rows; integer K: a lane holds D / 4 consecutive
+//                 values of a slot (whole scale groups), Q follows that order;
+//   O^T += V^T P^T  16 dims x 8 rows; P^T is S^T's fragment transposed
+//                 (movmatrix); integer V: ldmatrix transposes pairs of slots,
+//                 the 2 or 4 values of its 16-bit elements are rows apart.
+// Online softmax in base 2 (fp32), lane-local: a row's reference maximum moves
+// (and O is rescaled) only when some logit exceeds it by 2^8, which one vote per
+// chunk finds.  P is rounded to bf16 for the product, the normaliser sums the
+// unrounded P.  A set inside one stream is written out at once; a split one
+// leaves a partial (m, l, O) per stream, merged by a second kernel in stream
+// order, so results do not depend on timing.
 #include "cache_launch.h"
 #include "launch.h"
 #include "tc05.cuh"
@@ -35,8 +39,9 @@ namespace {
 constexpr int kW = 8;                  // streams (warps) per CTA
 constexpr int kStages = 2;
 constexpr int kPlanSets = 2048;        // plan entries kept in shared memory
+constexpr float kStale = 8.f;          // a reference maximum may trail by 2^8
 
-template <int D, int FMT>
+template <int D, int FMT, int NB>
 struct StreamGeom {
     static constexpr int ROWB = FMT == TGVKV_CACHE_BF16 ? 2 * D : FMT == TGVKV_CACHE_INT8 ? D : D / 2;
     // slots per chunk: 4 KB of K and of V, at most 64
@@ -50,19 +55,12 @@ struct StreamGeom {
     static constexpr int kKS = 2 * KT * kTile;
     static constexpr int kVS = kKS + CH * SCB;
     static constexpr int kQ = kVS + CH * SCB;
-    static constexpr int kStage = (kQ + kStreamRows * 2 * D + 1023) & ~1023;
+    static constexpr int kStage = (kQ + NB * 8 * 2 * D + 1023) & ~1023;   // NB * 8 query rows
     static constexpr int kRing = kW * kStages * kStage;
-};
-
-// A chunk: slots [key0, key0 + n) of set s.
-struct Chunk {
-    int s, key0, n, first, last;
-    int len, nq, tok0;
 };
 
 struct StreamTail {
     uint64_t full[kW][kStages];
-    Chunk chunk[kW][kStages];
     int warp_sum[kW];
     int never;
     int pref[kPlanSets + 1];           // first chunk of entry e (a run of `run` sets)
@@ -98,6 +96,13 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr) {
     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
                  : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w)
                  : "r"(addr));
+    return r;
+}
+
+// The 8 x 8 transpose of a fragment of 16-bit elements.
+__device__ __forceinline__ uint32_t movm_trans(uint32_t x) {
+    uint32_t r;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
     return r;
 }
 
@@ -138,8 +143,9 @@ __device__ __forceinline__ int set_chunks(const SetSpan& sp) {
 // A stream's walk over its chunks [c, c1) of the sequence.
 template <int CH>
 struct Walk {
-    int s, at, left, chunks;           // set, next chunk in it, chunks left of the share
     SetSpan sp;
+    int s, at, chunks, left;           // set, the chunk in it, its chunks, chunks left of the share
+    bool fresh;                        // the chunk starts a segment
 
     __device__ __forceinline__ void load(const CacheProblem& p, const ChunkArgs& a) {
         sp = set_span(p, a, s);
@@ -148,6 +154,7 @@ struct Walk {
     __device__ __forceinline__ void init(const CacheProblem& p, const ChunkArgs& a,
                                          const int* pref, int entries, int run, int c, int c1) {
         left = c1 - c;
+        fresh = true;
         int lo = 0, hi = entries - 1;  // the last entry that starts at or before c
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
@@ -166,52 +173,43 @@ struct Walk {
             load(p, a);
         }
     }
-    __device__ __forceinline__ bool next(const CacheProblem& p, const ChunkArgs& a, Chunk& c,
-                                         bool& fresh) {
-        if (left <= 0) return false;
-        while (at >= chunks) {
-            at = 0;
-            if (++s >= p.S) return false;
-            load(p, a);
-            fresh = true;
-        }
-        c.s = s;
-        c.key0 = at * CH;
-        c.n = min(sp.len - c.key0, CH);
-        c.first = fresh;
-        c.last = at + 1 == chunks || left == 1;
-        c.len = sp.len;
-        c.nq = sp.n;
-        c.tok0 = sp.tok0;
+    // the chunk: slots [key0(), key0() + n()) of set s
+    __device__ __forceinline__ int key0() const { return at * CH; }
+    __device__ __forceinline__ int n() const { return min(sp.len - at * CH, CH); }
+    __device__ __forceinline__ bool ends() const { return at + 1 == chunks || left == 1; }
+    __device__ __forceinline__ void step(const CacheProblem& p, const ChunkArgs& a) {
         fresh = false;
-        ++at;
-        --left;
-        return true;
+        if (--left <= 0) return;
+        if (++at < chunks) return;
+        fresh = true;
+        at = 0;
+        do {
+            if (++s >= p.S) {
+                left = 0;
+                return;
+            }
+            load(p, a);
+        } while (chunks == 0);
     }
 };
 
-// The copies of chunk c into one stage, spread over the warp's lanes.  Lane
-// b < boxes holds the page number of the chunk's b-th page slice.
-template <int D, int FMT>
-__device__ __forceinline__ void issue(unsigned char* stage, uint64_t* bar, const Chunk& c, int page,
-                                      int box, const CUtensorMap* mk, const CUtensorMap* mv,
+// The copies of the walk's chunk into one stage, spread over the warp's lanes.
+// Lane b < boxes holds the page number of the chunk's b-th page slice.
+template <int D, int FMT, int NB>
+__device__ __forceinline__ void issue(unsigned char* stage, uint64_t* bar,
+                                      const Walk<StreamGeom<D, FMT, NB>::CH>& w, int page, int box,
+                                      int box_shift, const CUtensorMap* mk, const CUtensorMap* mv,
                                       const CacheProblem& p, const CachePools& pool,
                                       const ChunkArgs& a, int lane) {
-    using Gm = StreamGeom<D, FMT>;
-    const int nb = (c.n + box - 1) / box;
-    const int rows = c.nq * p.G;
+    using Gm = StreamGeom<D, FMT, NB>;
+    const int nb = (w.n() + box - 1) >> box_shift;
     const uint32_t per_box = (uint32_t)box * (2 * Gm::ROWB + 2 * Gm::SCB);
-    if (lane == 0)
-        tc::mbar_arrive_expect_tx(bar, nb * per_box + (c.first ? (uint32_t)rows * 2 * D : 0u));
+    uint32_t bytes = nb * per_box;
+    if (w.fresh) bytes += (uint32_t)(w.sp.n * p.G) * 2 * D;
+    if (lane == 0) tc::mbar_arrive_expect_tx(bar, bytes);
     __syncwarp();
-    if (c.first && lane < rows) {
-        const int i = lane / p.G, h = lane - i * p.G;
-        const uint16_t* src = a.q + (long long)(c.tok0 + i) * a.q_tok +
-                              (long long)((c.s % p.H_kv) * p.G + h) * a.q_head;
-        bulk_copy(smem_u32(stage + Gm::kQ) + lane * 2 * D, src, 2 * D, bar);
-    }
     if (lane < nb) {
-        const int row = page * p.page + ((c.key0 + lane * box) & (p.page - 1));
+        const int row = page * p.page + ((w.key0() + lane * box) & (p.page - 1));
         const uint32_t at = (uint32_t)(lane * box);
 #pragma unroll
         for (int kt = 0; kt < Gm::KT; ++kt) {
@@ -224,44 +222,38 @@ __device__ __forceinline__ void issue(unsigned char* stage, uint64_t* bar, const
             bulk_copy(smem_u32(stage + Gm::kVS) + at * Gm::SCB, pool.vs + off, box * Gm::SCB, bar);
         }
     }
+    if (w.fresh && lane < w.sp.n * p.G) {
+        const int i = lane / p.G, h = lane - i * p.G;
+        const uint16_t* src = a.q + (long long)(w.sp.tok0 + i) * a.q_tok +
+                              (long long)((w.s % p.H_kv) * p.G + h) * a.q_head;
+        bulk_copy(smem_u32(stage + Gm::kQ) + lane * 2 * D, src, 2 * D, bar);
+    }
 }
 
-// The page number of lane b's slice of chunk c (0 and the status bit where the
-// table holds none).
-__device__ __forceinline__ int chunk_page(const CacheProblem& p, const ChunkArgs& a, const Chunk& c,
-                                          int box, int lane) {
-    const int nb = (c.n + box - 1) / box;
-    if (lane >= nb) return 0;
-    return __ldg(a.page_table + (size_t)c.s * p.max_pages + ((c.key0 + lane * box) >> p.page_shift));
-}
 __device__ __forceinline__ int valid_page(const CacheProblem& p, int page, uint32_t* status) {
     if (page >= 0 && page < p.n_pages) return page;
     raise_status(status, TGVKV_STATUS_INDEX);
     return 0;
 }
 
-// The first of the two columns (dims) whose results a lane's c0 and c1 (rows g)
-// hold in column tile t: dim of c0 is out_dim(t, tq), of c1 out_dim + step.
-template <int D, int FMT>
-__device__ __forceinline__ int out_dim(int t, int tq) {
-    if (FMT == TGVKV_CACHE_BF16) return 8 * t + 2 * tq;
-    if (FMT == TGVKV_CACHE_INT8) return 16 * (t >> 1) + 4 * tq + (t & 1);
-    return 32 * (t >> 2) + 8 * tq + (t & 3);
-}
+// The dims of a lane's results in the 16-dim row tile mt of O^T: its row g is
+// dim out_dim(mt, g), its row g + 8 the dim out_step later.
 template <int FMT>
-constexpr int out_step() {
-    return FMT == TGVKV_CACHE_BF16 ? 1 : FMT == TGVKV_CACHE_INT8 ? 2 : 4;
+__device__ __forceinline__ int out_dim(int mt, int g) {
+    if (FMT == TGVKV_CACHE_BF16) return 16 * mt + g;
+    if (FMT == TGVKV_CACHE_INT8) return 16 * mt + 2 * g;
+    return 32 * (mt >> 1) + 4 * g + 2 * (mt & 1);
 }
 
-template <int D, int FMT>
+template <int D, int FMT, int NB>
 __global__ void __launch_bounds__(kW * 32, 1)
 chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                     const CacheProblem p, const CachePools pool, const ChunkArgs a, int box,
-                    int min_chunks, int rec_rows, float* __restrict__ part,
+                    int box_shift, int min_chunks, int rec_rows, float* __restrict__ part,
                     long long* __restrict__ plan, uint32_t* __restrict__ status) {
-    using Gm = StreamGeom<D, FMT>;
+    using Gm = StreamGeom<D, FMT, NB>;
     constexpr int CH = Gm::CH;
-    constexpr int KS = D / 16, ND = D / 8, NT = CH / 8, KK = CH / 16;
+    constexpr int KS = D / 16, MT = D / 16, KB = CH / 16;
     griddep_launch_dependents();
     if (threadIdx.x == 0) {
         tc::tma_prefetch_desc(&mk);
@@ -330,227 +322,257 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
     const int c0 = (int)c_lo, c1 = min(c0 + per, total);
 
     unsigned char* wring = ring + warp * kStages * Gm::kStage;
-    Walk<CH> walk;
-    bool fresh = true;
-    walk.init(p, a, tl.pref, entries, run, c0, c1);
-    Chunk nxt;
-    bool more = walk.next(p, a, nxt, fresh);
-    int nxt_page = more ? chunk_page(p, a, nxt, box, lane) : 0;
+    Walk<CH> ahead;                    // the next chunk to fetch
+    ahead.init(p, a, tl.pref, entries, run, c0, c1);
+    Walk<CH> w = ahead;                // the next chunk to work on
+    const int32_t* table = a.page_table + (size_t)ahead.s * p.max_pages;
+    auto page_of = [&]() {             // lane b: page number of the chunk's slice b
+        const int slot = ahead.key0() + (lane << box_shift);
+        return (lane << box_shift) < ahead.n() ? __ldg(table + (slot >> p.page_shift)) : 0;
+    };
+    int page = ahead.left > 0 ? page_of() : 0;
     int issued = 0;
     auto refill = [&]() {              // the next chunk into the stage just read
         const int st = issued % kStages;
-        if (lane == 0) tl.chunk[warp][st] = nxt;
-        issue<D, FMT>(wring + st * Gm::kStage, &tl.full[warp][st], nxt,
-                      valid_page(p, nxt_page, status), box, &mk, &mv, p, pool, a, lane);
+        issue<D, FMT, NB>(wring + st * Gm::kStage, &tl.full[warp][st], ahead,
+                          valid_page(p, page, status), box, box_shift, &mk, &mv, p, pool, a, lane);
         ++issued;
-        more = walk.next(p, a, nxt, fresh);
-        if (more) nxt_page = chunk_page(p, a, nxt, box, lane);
+        ahead.step(p, a);
+        if (ahead.left > 0) {          // its page numbers, a chunk ahead of their use
+            if (ahead.fresh) table = a.page_table + (size_t)ahead.s * p.max_pages;
+            page = page_of();
+        }
     };
-    for (int st = 0; st < kStages && more; ++st) refill();
+    for (int st = 0; st < kStages && ahead.left > 0; ++st) refill();
     __syncwarp();
 
     const int g = lane >> 2, tq = lane & 3;
-    uint32_t qa[KS][4];
-    float o[ND][4];
-    float m[2], l[2];
-    int seg_chunk = c0;                // chunk index at which the current segment began
+    uint32_t qb[KS][NB][2];
+    float o[MT][NB][4];
+    float m[NB][2], l[NB][2];          // of rows 8 nb + 2 tq and the next
+    bool seg_starts = true;            // the segment began at its set's first chunk
+    bool share_starts = true;          // ... is the first of this stream
     int i = 0;
-    for (; i < issued; ++i) {
+    for (; w.left > 0; ++i) {
         const int st = i % kStages;
         const bool got = tc::mbar_wait(&tl.full[warp][st], (i / kStages) & 1, &tl.never);
         if (!__all_sync(~0u, got)) break;
-        const Chunk c = tl.chunk[warp][st];
         unsigned char* stage = wring + st * Gm::kStage;
         const uint32_t sb = smem_u32(stage);
-        if (c.first) {
-            seg_chunk = c0 + i;
-            // Q fragments: pairs of dims in the order the K fragments have; 0 in
-            // rows the tile does not have
-            const int rows = c.nq * p.G;
-            const uint32_t q0 = sb + Gm::kQ + g * 2 * D, q1 = q0 + 8 * 2 * D;
+        const int key0 = w.key0(), n = w.n();
+        if (w.fresh) {
+            seg_starts = w.at == 0;
+            share_starts = i == 0;
+            // Q^T fragments: pairs of dims in the order the K fragments have; 0 in
+            // rows the set does not have
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                const uint32_t q0 = sb + Gm::kQ + (8 * nb + g) * 2 * D;
+                if (FMT == TGVKV_CACHE_BF16) {
+#pragma unroll
+                    for (int s = 0; s < KS; ++s) {
+                        qb[s][nb][0] = lds32(q0 + 32 * s + 4 * tq);
+                        qb[s][nb][1] = lds32(q0 + 32 * s + 16 + 4 * tq);
+                    }
+                } else if (FMT == TGVKV_CACHE_INT8) {
+#pragma unroll
+                    for (int s = 0; s < KS; ++s) {   // 4 values: (0, 2) and (1, 3)
+                        const uint2 x = lds64(q0 + tq * (D / 2) + 8 * s);
+                        qb[s][nb][0] = __byte_perm(x.x, x.y, 0x5410);
+                        qb[s][nb][1] = __byte_perm(x.x, x.y, 0x7632);
+                    }
+                } else {
+#pragma unroll
+                    for (int s = 0; s < KS / 2; ++s) {   // 8: (0, 4) (1, 5), (2, 6) (3, 7)
+                        const uint4 x = lds128(q0 + tq * (D / 2) + 16 * s);
+                        qb[2 * s][nb][0] = __byte_perm(x.x, x.z, 0x5410);
+                        qb[2 * s][nb][1] = __byte_perm(x.x, x.z, 0x7632);
+                        qb[2 * s + 1][nb][0] = __byte_perm(x.y, x.w, 0x5410);
+                        qb[2 * s + 1][nb][1] = __byte_perm(x.y, x.w, 0x7632);
+                    }
+                }
+                if (8 * nb + g >= w.sp.n * p.G) {
+#pragma unroll
+                    for (int s = 0; s < KS; ++s) qb[s][nb][0] = qb[s][nb][1] = 0u;
+                }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) m[nb][e] = -INFINITY, l[nb][e] = 0.f;
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[t][nb][e] = 0.f;
+            }
+        }
+        // ---- S^T = K Q^T; tile kb holds slots 16 kb + g and 16 kb + g + 8
+        float sc[KB][NB][4];
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            float acc[2][NB][4];       // two halves of the dims: independent chains
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[y][nb][e] = 0.f;
             if (FMT == TGVKV_CACHE_BF16) {
 #pragma unroll
                 for (int s = 0; s < KS; ++s) {
-                    qa[s][0] = lds32(q0 + 32 * s + 4 * tq);
-                    qa[s][1] = lds32(q1 + 32 * s + 4 * tq);
-                    qa[s][2] = lds32(q0 + 32 * s + 16 + 4 * tq);
-                    qa[s][3] = lds32(q1 + 32 * s + 16 + 4 * tq);
-                }
-            } else if (FMT == TGVKV_CACHE_INT8) {
+                    const int unit = 2 * s + (lane >> 4);
+                    uint32_t r[4];
+                    ldsm_x4(sb + Gm::kK + (unit >> 3) * Gm::kTile +
+                                swz<128>(16 * kb + (lane & 15), unit & 7),
+                            r);
 #pragma unroll
-                for (int s = 0; s < KS; ++s) {       // 4 values: (0, 2) and (1, 3)
-                    const uint2 x = lds64(q0 + tq * (D / 2) + 8 * s);
-                    const uint2 y = lds64(q1 + tq * (D / 2) + 8 * s);
-                    qa[s][0] = __byte_perm(x.x, x.y, 0x5410);
-                    qa[s][1] = __byte_perm(y.x, y.y, 0x5410);
-                    qa[s][2] = __byte_perm(x.x, x.y, 0x7632);
-                    qa[s][3] = __byte_perm(y.x, y.y, 0x7632);
-                }
-            } else {
-#pragma unroll
-                for (int w = 0; w < KS / 2; ++w) {   // 8 values: (0, 4) (1, 5), (2, 6) (3, 7)
-                    const uint4 x = lds128(q0 + tq * (D / 2) + 16 * w);
-                    const uint4 y = lds128(q1 + tq * (D / 2) + 16 * w);
-                    qa[2 * w][0] = __byte_perm(x.x, x.z, 0x5410);
-                    qa[2 * w][1] = __byte_perm(y.x, y.z, 0x5410);
-                    qa[2 * w][2] = __byte_perm(x.x, x.z, 0x7632);
-                    qa[2 * w][3] = __byte_perm(y.x, y.z, 0x7632);
-                    qa[2 * w + 1][0] = __byte_perm(x.y, x.w, 0x5410);
-                    qa[2 * w + 1][1] = __byte_perm(y.y, y.w, 0x5410);
-                    qa[2 * w + 1][2] = __byte_perm(x.y, x.w, 0x7632);
-                    qa[2 * w + 1][3] = __byte_perm(y.y, y.w, 0x7632);
-                }
-            }
-#pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                if (g >= rows) qa[s][0] = qa[s][2] = 0u;
-                if (g + 8 >= rows) qa[s][1] = qa[s][3] = 0u;
-            }
-#pragma unroll
-            for (int e = 0; e < 2; ++e) m[e] = -INFINITY, l[e] = 0.f;
-#pragma unroll
-            for (int t = 0; t < ND; ++t)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[t][e] = 0.f;
-        }
-        // ---- S = Q K^T; column tile j holds slots 8j .. 8j + 7
-        float sc[NT][4];
-#pragma unroll
-        for (int j = 0; j < NT; j += 2) {
-            // two tiles x two halves of the dims: four independent chains
-            float acc[2][2][4];
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int y = 0; y < 2; ++y)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[x][y][e] = 0.f;
-            if (FMT == TGVKV_CACHE_BF16) {
-#pragma unroll
-                for (int u = 0; u < KS / 2; ++u) {
-                    const int unit = 4 * u + (lane >> 3);
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        uint32_t r[4];
-                        ldsm_x4(sb + Gm::kK + (unit >> 3) * Gm::kTile +
-                                    swz<128>(8 * (j + x) + (lane & 7), unit & 7),
-                                r);
-                        mma(acc[x][u & 1], qa[2 * u], r[0], r[1]);
-                        mma(acc[x][u & 1], qa[2 * u + 1], r[2], r[3]);
-                    }
+                    for (int nb = 0; nb < NB; ++nb)
+                        mma(acc[s & 1][nb], r, qb[s][nb][0], qb[s][nb][1]);
                 }
             } else {
                 constexpr int NW = Gm::ROWB / 16;    // words of codes a lane holds of a row
-                uint32_t w[2][NW], kb[2];
+                uint32_t wd[2][NW], kb_s[2];
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    const int row = 8 * (j + x) + g;
+                    const int row = 16 * kb + 8 * x + g;
                     if (NW == 2) {
                         const uint2 t = lds64(sb + Gm::kK + swz<Gm::TROW>(row, tq >> 1) + (tq & 1) * 8);
-                        w[x][0] = t.x, w[x][1 % NW] = t.y;
+                        wd[x][0] = t.x, wd[x][1 % NW] = t.y;
                     } else {
 #pragma unroll
                         for (int b = 0; b < NW / 4; ++b) {
                             const uint4 t =
                                 lds128(sb + Gm::kK + swz<Gm::TROW>(row, tq * (NW / 4) + b));
-                            w[x][(4 * b) % NW] = t.x, w[x][(4 * b + 1) % NW] = t.y;
-                            w[x][(4 * b + 2) % NW] = t.z, w[x][(4 * b + 3) % NW] = t.w;
+                            wd[x][(4 * b) % NW] = t.x, wd[x][(4 * b + 1) % NW] = t.y;
+                            wd[x][(4 * b + 2) % NW] = t.z, wd[x][(4 * b + 3) % NW] = t.w;
                         }
                     }
-                    kb[x] = lds8(sb + Gm::kKS + row * Gm::SCB + (D == 128 ? tq : tq >> 1));
-                    kb[x] = both(FMT == TGVKV_CACHE_INT8 ? scale_bf16(kb[x]) : int4_base(kb[x]));
+                    const uint32_t byte =
+                        lds8(sb + Gm::kKS + row * Gm::SCB + (D == 128 ? tq : tq >> 1));
+                    kb_s[x] = both(FMT == TGVKV_CACHE_INT8 ? scale_bf16(byte) : int4_base(byte));
                 }
 #pragma unroll
-                for (int s = 0; s < KS; ++s)
+                for (int s = 0; s < KS; ++s) {
+                    uint32_t r[4];
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        uint32_t b0, b1;
                         if (FMT == TGVKV_CACHE_INT8) {
-                            b0 = bf16x2_mul(int8x2_to_bf16(w[x][s % NW]), kb[x]);
-                            b1 = bf16x2_mul(int8x2_to_bf16(w[x][s % NW] >> 8), kb[x]);
+                            const uint32_t c = wd[x][s % NW];
+                            r[x] = bf16x2_mul(int8x2_to_bf16(c), kb_s[x]);
+                            r[2 + x] = bf16x2_mul(int8x2_to_bf16(c >> 8), kb_s[x]);
                         } else {
-                            b0 = int4x2_to_bf16(w[x][(s / 2) % NW] >> (8 * (s & 1)), kb[x]);
-                            b1 = int4x2_to_bf16(w[x][(s / 2) % NW] >> (8 * (s & 1) + 4), kb[x]);
+                            const uint32_t c = wd[x][(s / 2) % NW];
+                            r[x] = int4x2_to_bf16(c >> (8 * (s & 1)), kb_s[x]);
+                            r[2 + x] = int4x2_to_bf16(c >> (8 * (s & 1) + 4), kb_s[x]);
                         }
-                        mma(acc[x][s & 1], qa[s], b0, b1);
                     }
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+                        mma(acc[s & 1][nb], r, qb[s][nb][0], qb[s][nb][1]);
+                }
             }
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
+            for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    sc[j + x][e] = (acc[x][0][e] + acc[x][1][e]) * p.scale_log2;
+                    sc[kb][nb][e] = (acc[0][nb][e] + acc[1][nb][e]) * p.scale_log2;
         }
         // ---- hide what a row must not see: slots from its token's on
-        if (c.n < CH || c.key0 + CH > c.len - c.nq + 1) {
+        if (n < CH || key0 + CH > w.sp.len - w.sp.n + 1) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int lim = min(c.len - c.nq + (g + 8 * h) / p.G + 1 - c.key0, c.n);
-#pragma unroll
-                for (int j = 0; j < NT; ++j)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        if (8 * j + 2 * tq + e >= lim) sc[j][2 * h + e] = -INFINITY;
-            }
-        }
-        // ---- online softmax of rows g and g + 8 (the 4 lanes of a row share it)
-        float alpha[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float cm = fmaxf(sc[0][2 * h], sc[0][2 * h + 1]);
-#pragma unroll
-            for (int j = 1; j < NT; ++j) cm = fmaxf(cm, fmaxf(sc[j][2 * h], sc[j][2 * h + 1]));
-            cm = fmaxf(cm, __shfl_xor_sync(~0u, cm, 1));
-            cm = fmaxf(cm, __shfl_xor_sync(~0u, cm, 2));
-            const float mn = fmaxf(m[h], cm);
-            const float ref = mn == -INFINITY ? 0.f : mn;   // nothing seen yet: all weights 0
-            alpha[h] = fast_exp2(m[h] - ref);
-            float ps = 0.f;
-#pragma unroll
-            for (int j = 0; j < NT; ++j)
+            for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    sc[j][2 * h + e] = fast_exp2(sc[j][2 * h + e] - ref);
-                    ps += sc[j][2 * h + e];
-                }
-            l[h] = l[h] * alpha[h] + ps;
-            m[h] = mn;
-        }
-        if (__any_sync(~0u, alpha[0] != 1.f || alpha[1] != 1.f)) {
+                    const int lim =
+                        min(w.sp.len - w.sp.n + (8 * nb + 2 * tq + e) / p.G + 1 - key0, n);
 #pragma unroll
-            for (int t = 0; t < ND; ++t) {
-                o[t][0] *= alpha[0], o[t][1] *= alpha[0];
-                o[t][2] *= alpha[1], o[t][3] *= alpha[1];
-            }
+                    for (int kb = 0; kb < KB; ++kb) {
+                        if (16 * kb + g >= lim) sc[kb][nb][e] = -INFINITY;
+                        if (16 * kb + 8 + g >= lim) sc[kb][nb][2 + e] = -INFINITY;
+                    }
+                }
         }
+        // ---- online softmax; a row's 8 lanes share m
+        bool move = false;
+        float cm[NB][2];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                cm[nb][e] = fmaxf(sc[0][nb][e], sc[0][nb][2 + e]);
+#pragma unroll
+                for (int kb = 1; kb < KB; ++kb)
+                    cm[nb][e] = fmaxf(cm[nb][e], fmaxf(sc[kb][nb][e], sc[kb][nb][2 + e]));
+                move |= cm[nb][e] > m[nb][e] + kStale;
+            }
+        if (__any_sync(~0u, move)) {   // also a segment's first chunk
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float c = cm[nb][e];
+                    c = fmaxf(c, __shfl_xor_sync(~0u, c, 4));
+                    c = fmaxf(c, __shfl_xor_sync(~0u, c, 8));
+                    c = fmaxf(c, __shfl_xor_sync(~0u, c, 16));
+                    const float mn = fmaxf(m[nb][e], c);
+                    const float alpha = mn == -INFINITY ? 1.f : fast_exp2(m[nb][e] - mn);
+                    m[nb][e] = mn;
+                    l[nb][e] *= alpha;
+#pragma unroll
+                    for (int t = 0; t < MT; ++t) o[t][nb][e] *= alpha, o[t][nb][2 + e] *= alpha;
+                }
+        }
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float ref = m[nb][e] == -INFINITY ? 0.f : m[nb][e];   // nothing seen: weights 0
+                float ps = 0.f;
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) {
+                    sc[kb][nb][e] = fast_exp2(sc[kb][nb][e] - ref);
+                    sc[kb][nb][2 + e] = fast_exp2(sc[kb][nb][2 + e] - ref);
+                    ps += sc[kb][nb][e] + sc[kb][nb][2 + e];
+                }
+                l[nb][e] += ps;
+            }
         // ---- slots past the set's end hold what the pool holds there: their
         // weights are 0, and 0 x NaN is not, so V must be 0 (integer V: scale 0)
-        if (FMT == TGVKV_CACHE_BF16 && c.n < CH) {
-            const int end = (c.n + 15) & ~15;
-            for (int x = lane; x < (end - c.n) * 8 * Gm::KT; x += 32) {
-                const int r = c.n + x / (8 * Gm::KT), u = x % (8 * Gm::KT);
+        if (FMT == TGVKV_CACHE_BF16 && n < CH) {
+            const int end = (n + 15) & ~15;
+            for (int x = lane; x < (end - n) * 8 * Gm::KT; x += 32) {
+                const int r = n + x / (8 * Gm::KT), u = x % (8 * Gm::KT);
                 *reinterpret_cast<uint4*>(stage + Gm::kV + (u >> 3) * Gm::kTile + r * 128 + (u & 7) * 16) =
                     make_uint4(0u, 0u, 0u, 0u);
             }
             tc::fence_proxy_async_smem();   // before TMA writes the stage again
             __syncwarp();
         }
-        // ---- O += P V over 16 slots at a time
+        // ---- O^T += V^T P^T over 16 slots at a time
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) {
-            if (16 * kk >= c.n) break;
-            const uint32_t pa[4] = {pack_bf16x2(sc[2 * kk][0], sc[2 * kk][1]),
-                                    pack_bf16x2(sc[2 * kk][2], sc[2 * kk][3]),
-                                    pack_bf16x2(sc[2 * kk + 1][0], sc[2 * kk + 1][1]),
-                                    pack_bf16x2(sc[2 * kk + 1][2], sc[2 * kk + 1][3])};
-            const int row = 16 * kk + (lane & 7) + ((lane >> 3) & 1) * 8;
-            // scales of this lane's slot pairs (2 tq, + 1) and (2 tq + 8, + 9), by group
-            constexpr int NG = D / kGroup;
-            uint32_t vs[2][NG];
-            if (FMT != TGVKV_CACHE_BF16) {
+        for (int kb = 0; kb < KB; ++kb) {
+            if (16 * kb >= n) break;
+            uint32_t pb[NB][2];
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                pb[nb][0] = movm_trans(pack_bf16x2(sc[kb][nb][0], sc[kb][nb][1]));
+                pb[nb][1] = movm_trans(pack_bf16x2(sc[kb][nb][2], sc[kb][nb][3]));
+            }
+            if (FMT == TGVKV_CACHE_BF16) {
+#pragma unroll
+                for (int t = 0; t < MT; ++t) {
+                    const int unit = 2 * t + ((lane >> 3) & 1);
+                    uint32_t r[4];
+                    ldsm_x4_trans(sb + Gm::kV + (unit >> 3) * Gm::kTile +
+                                      swz<128>(16 * kb + (lane & 7) + (lane >> 4) * 8, unit & 7),
+                                  r);
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) mma(o[t][nb], r, pb[nb][0], pb[nb][1]);
+                }
+            } else {
+                // scales of this lane's slot pairs (2 tq, + 1) and (2 tq + 8, + 9), by group
+                constexpr int NG = D / kGroup;
+                uint32_t vs[2][NG];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int k0 = 16 * kk + 2 * tq + 8 * h;
+                    const int k0 = 16 * kb + 2 * tq + 8 * h;
                     uint32_t w0, w1;
                     if (D == 128) {
                         const uint2 t = lds64(sb + Gm::kVS + k0 * 4);
@@ -559,102 +581,111 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
                         const uint32_t t = lds32(sb + Gm::kVS + k0 * 2);
                         w0 = t & 0xFFFFu, w1 = t >> 16;
                     }
-                    if (k0 >= c.n) w0 = 0u;
-                    if (k0 + 1 >= c.n) w1 = 0u;
+                    if (k0 >= n) w0 = 0u;
+                    if (k0 + 1 >= n) w1 = 0u;
 #pragma unroll
                     for (int x = 0; x < NG; ++x) {
                         const uint32_t both_e =
-                            __byte_perm(w0, w1, (x << 4) | ((4 + x) << 12)) >> 1 & 0x7F807F80u;
+                            (__byte_perm(w0, w1, (x << 4) | ((4 + x) << 12)) >> 1) & 0x7F807F80u;
                         vs[h][x] = FMT == TGVKV_CACHE_INT8
                                        ? both_e
                                        : __vminu2(both_e + 0x03800380u, 0x7F807F80u);
                     }
                 }
-            }
 #pragma unroll
-            for (int u2 = 0; u2 < Gm::ROWB / 32; ++u2) {
-                const int unit = 2 * u2 + (lane >> 4);
-                uint32_t r[4];
-                ldsm_x4_trans(sb + Gm::kV + (unit / (Gm::TROW / 16)) * Gm::kTile +
-                                  swz<Gm::TROW>(row, unit % (Gm::TROW / 16)),
-                              r);
+                for (int u2 = 0; u2 < Gm::ROWB / 32; ++u2) {
+                    uint32_t r[4];
+                    ldsm_x4_trans(sb + Gm::kV + swz<Gm::TROW>(16 * kb + (lane & 15), 2 * u2 + (lane >> 4)),
+                                  r);
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const int u = 2 * u2 + x;        // 16-byte unit of the row
-                    const uint32_t r0 = r[2 * x], r1 = r[2 * x + 1];
-                    if (FMT == TGVKV_CACHE_BF16) {
-                        mma(o[u], pa, r0, r1);
-                    } else if (FMT == TGVKV_CACHE_INT8) {
-                        const uint32_t s0 = vs[0][(u / 2) % NG], s1 = vs[1][(u / 2) % NG];
+                    for (int x = 0; x < 2; ++x) {
+                        const int u = 2 * u2 + x;    // 16-byte unit of the row
+                        const uint32_t r0 = r[2 * x], r1 = r[2 * x + 1];
+                        if (FMT == TGVKV_CACHE_INT8) {
+                            const uint32_t s0 = vs[0][(u / 2) % NG], s1 = vs[1][(u / 2) % NG];
+                            const uint32_t v[4] = {bf16x2_mul(int8x2_to_bf16(r0), s0),
+                                                   bf16x2_mul(int8x2_to_bf16(r0 >> 8), s0),
+                                                   bf16x2_mul(int8x2_to_bf16(r1), s1),
+                                                   bf16x2_mul(int8x2_to_bf16(r1 >> 8), s1)};
 #pragma unroll
-                        for (int y = 0; y < 2; ++y)
-                            mma(o[(2 * u + y) % ND], pa, bf16x2_mul(int8x2_to_bf16(r0 >> (8 * y)), s0),
-                                bf16x2_mul(int8x2_to_bf16(r1 >> (8 * y)), s1));
-                    } else {
-                        const uint32_t s0 = vs[0][u % NG], s1 = vs[1][u % NG];
+                            for (int nb = 0; nb < NB; ++nb) mma(o[u % MT][nb], v, pb[nb][0], pb[nb][1]);
+                        } else {
+                            const uint32_t s0 = vs[0][u % NG], s1 = vs[1][u % NG];
 #pragma unroll
-                        for (int y = 0; y < 4; ++y)
-                            mma(o[(4 * u + y) % ND], pa, int4x2_to_bf16(r0 >> (4 * y), s0),
-                                int4x2_to_bf16(r1 >> (4 * y), s1));
+                            for (int y = 0; y < 2; ++y) {
+                                const uint32_t v[4] = {int4x2_to_bf16(r0 >> (8 * y), s0),
+                                                       int4x2_to_bf16(r0 >> (8 * y + 4), s0),
+                                                       int4x2_to_bf16(r1 >> (8 * y), s1),
+                                                       int4x2_to_bf16(r1 >> (8 * y + 4), s1)};
+#pragma unroll
+                                for (int nb = 0; nb < NB; ++nb)
+                                    mma(o[(2 * u + y) % MT][nb], v, pb[nb][0], pb[nb][1]);
+                            }
+                        }
                     }
                 }
             }
         }
         __syncwarp();                  // the stage is read: refill it
-        if (more) refill();
-        if (!c.last) continue;
-        // ---- the segment of set c.s is complete
+        if (ahead.left > 0) refill();
+        const bool ends = w.ends();
+        if (ends) {
+            // ---- the segment of set w.s is complete
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            l[h] += __shfl_xor_sync(~0u, l[h], 1);
-            l[h] += __shfl_xor_sync(~0u, l[h], 2);
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    l[nb][e] += __shfl_xor_sync(~0u, l[nb][e], 4);
+                    l[nb][e] += __shfl_xor_sync(~0u, l[nb][e], 8);
+                    l[nb][e] += __shfl_xor_sync(~0u, l[nb][e], 16);
+                }
+            const bool whole = seg_starts && w.at + 1 == w.chunks;
+            float* pp = part + ((size_t)si * 2 + (share_starts ? 0 : 1)) *
+                                   (size_t)chunk_record_floats(rec_rows, D);
+            constexpr int STEP = FMT == TGVKV_CACHE_BF16 ? 8 : 1;   // dims between rows g and g + 8
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int r = 8 * nb + 2 * tq + e;
+                    if (r >= w.sp.n * p.G) continue;
+                    if (whole) {       // the whole set: written out
+                        const float ls = l[nb][e];
+                        const float inv = ls > 0.f ? 1.f / ls : (ls == ls ? 0.f : ls);
+                        const int t = r / p.G, hh = r - t * p.G;
+                        uint16_t* op = a.out +
+                                       ((size_t)(w.sp.tok0 + t) * p.H_q + (w.s % p.H_kv) * p.G + hh) * D;
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt) {
+                            const uint32_t two =
+                                pack_bf16x2(o[mt][nb][e] * inv, o[mt][nb][2 + e] * inv);
+                            uint16_t* od = op + out_dim<FMT>(mt, g);
+                            if (STEP == 1) {
+                                *reinterpret_cast<uint32_t*>(od) = two;
+                            } else {
+                                od[0] = (uint16_t)two;
+                                od[STEP] = (uint16_t)(two >> 16);
+                            }
+                        }
+                    } else {
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt) {
+                            float* od = pp + r * D + out_dim<FMT>(mt, g);
+                            if (STEP == 1) {
+                                *reinterpret_cast<float2*>(od) = make_float2(o[mt][nb][e], o[mt][nb][2 + e]);
+                            } else {
+                                od[0] = o[mt][nb][e];
+                                od[STEP] = o[mt][nb][2 + e];
+                            }
+                        }
+                        if (g == 0) {
+                            pp[rec_rows * D + r] = m[nb][e];
+                            pp[rec_rows * D + rec_rows + r] = l[nb][e];
+                        }
+                    }
+                }
         }
-        const int rows = c.nq * p.G;
-        const bool whole = seg_chunk == c0 + i - c.key0 / CH && c.key0 + CH >= c.len;
-        const int gk = c.s % p.H_kv;
-        float* pp = part + ((size_t)si * 2 + (seg_chunk == c0 ? 0 : 1)) *
-                               (size_t)chunk_record_floats(rec_rows, D);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int r = g + 8 * h;
-            if (r >= rows) continue;
-            if (whole) {               // the whole set: written out
-                const float inv = l[h] > 0.f ? 1.f / l[h] : (l[h] == l[h] ? 0.f : l[h]);
-                const int t = r / p.G, hh = r - t * p.G;
-                uint16_t* op = a.out + ((size_t)(c.tok0 + t) * p.H_q + gk * p.G + hh) * D;
-                if (FMT == TGVKV_CACHE_BF16) {
-#pragma unroll
-                    for (int t8 = 0; t8 < ND; ++t8)
-                        *reinterpret_cast<uint32_t*>(op + 8 * t8 + 2 * tq) =
-                            pack_bf16x2(o[t8][2 * h] * inv, o[t8][2 * h + 1] * inv);
-                } else if (FMT == TGVKV_CACHE_INT8) {
-#pragma unroll
-                    for (int u = 0; u < ND / 2; ++u)
-                        *reinterpret_cast<uint2*>(op + 16 * u + 4 * tq) = make_uint2(
-                            pack_bf16x2(o[2 * u][2 * h] * inv, o[2 * u + 1][2 * h] * inv),
-                            pack_bf16x2(o[2 * u][2 * h + 1] * inv, o[2 * u + 1][2 * h + 1] * inv));
-                } else {
-#pragma unroll
-                    for (int u = 0; u < ND / 4; ++u)
-                        *reinterpret_cast<uint4*>(op + 32 * u + 8 * tq) = make_uint4(
-                            pack_bf16x2(o[4 * u][2 * h] * inv, o[4 * u + 1][2 * h] * inv),
-                            pack_bf16x2(o[4 * u + 2][2 * h] * inv, o[4 * u + 3][2 * h] * inv),
-                            pack_bf16x2(o[4 * u][2 * h + 1] * inv, o[4 * u + 1][2 * h + 1] * inv),
-                            pack_bf16x2(o[4 * u + 2][2 * h + 1] * inv, o[4 * u + 3][2 * h + 1] * inv));
-                }
-            } else {
-                float* op = pp + r * D;
-#pragma unroll
-                for (int t8 = 0; t8 < ND; ++t8) {
-                    op[out_dim<D, FMT>(t8, tq)] = o[t8][2 * h];
-                    op[out_dim<D, FMT>(t8, tq) + out_step<FMT>()] = o[t8][2 * h + 1];
-                }
-                if (tq == 0) {
-                    pp[rec_rows * D + r] = m[h];
-                    pp[rec_rows * D + rec_rows + r] = l[h];
-                }
-            }
-        }
+        w.step(p, a);
     }
     if (i < issued) {
         // a wait gave up: report it and let the copies in flight land
@@ -706,11 +737,13 @@ chunk_stream_merge(const CacheProblem p, const ChunkArgs a, int n_streams, int m
 // Chunks a stream takes at least: below this, splitting costs more than it saves.
 constexpr int kMinChunks = 2;
 
-template <int D, int FMT>
+template <int D, int FMT, int NB>
 cudaError_t launch_stream(const CacheProblem& p, const CachePools& pool, const ChunkArgs& a,
                           float* part, long long* plan, uint32_t* status, cudaStream_t stream) {
-    using Gm = StreamGeom<D, FMT>;
+    using Gm = StreamGeom<D, FMT, NB>;
     const int box = p.page < Gm::CH ? p.page : Gm::CH;
+    int box_shift = 0;
+    while ((1 << box_shift) < box) ++box_shift;
     alignas(64) CUtensorMap mk, mv;
     const uint64_t rows = (uint64_t)p.n_pages * p.page;
     const int box_bytes = FMT == TGVKV_CACHE_BF16 ? 128 : Gm::ROWB;
@@ -719,20 +752,27 @@ cudaError_t launch_stream(const CacheProblem& p, const CachePools& pool, const C
         return cudaErrorInvalidValue;
     const size_t smem = 1024 + Gm::kRing + sizeof(StreamTail);
     static_assert(1024 + Gm::kRing + sizeof(StreamTail) <= 227 * 1024, "shared memory of one CTA");
-    cudaError_t e = cudaFuncSetAttribute(chunk_stream_kernel<D, FMT>,
+    cudaError_t e = cudaFuncSetAttribute(chunk_stream_kernel<D, FMT, NB>,
                                          cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     const int sms = device_sm_count();
     if (sms <= 0) return cudaErrorInvalidDevice;
     const int ctas = sms < kStreamMax / kW ? sms : kStreamMax / kW;
     const int rec_rows = a.max_q * p.G;
-    chunk_stream_kernel<D, FMT><<<ctas, kW * 32, smem, stream>>>(mk, mv, p, pool, a, box, kMinChunks,
-                                                                 rec_rows, part, plan, status);
+    chunk_stream_kernel<D, FMT, NB><<<ctas, kW * 32, smem, stream>>>(
+        mk, mv, p, pool, a, box, box_shift, kMinChunks, rec_rows, part, plan, status);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     const long long warps = (long long)p.S * rec_rows;
     return launch_dependent(chunk_stream_merge<D>, dim3((unsigned)((warps + 3) / 4)), dim3(128), 0,
                             stream, p, a, ctas * kW, (int)kMinChunks, rec_rows,
                             static_cast<const float*>(part), static_cast<const long long*>(plan));
+}
+
+template <int D, int FMT>
+cudaError_t launch_rows(const CacheProblem& p, const CachePools& pool, const ChunkArgs& a,
+                        float* part, long long* plan, uint32_t* status, cudaStream_t stream) {
+    return a.max_q * p.G <= 8 ? launch_stream<D, FMT, 1>(p, pool, a, part, plan, status, stream)
+                              : launch_stream<D, FMT, 2>(p, pool, a, part, plan, status, stream);
 }
 
 }  // namespace
@@ -741,16 +781,16 @@ cudaError_t launch_chunk_stream(const CacheProblem& p, const CachePools& pool, c
                                 float* part, long long* plan, uint32_t* status, cudaStream_t stream) {
     if (p.d == 64) {
         if (p.format == TGVKV_CACHE_BF16)
-            return launch_stream<64, TGVKV_CACHE_BF16>(p, pool, a, part, plan, status, stream);
+            return launch_rows<64, TGVKV_CACHE_BF16>(p, pool, a, part, plan, status, stream);
         if (p.format == TGVKV_CACHE_INT8)
-            return launch_stream<64, TGVKV_CACHE_INT8>(p, pool, a, part, plan, status, stream);
-        return launch_stream<64, TGVKV_CACHE_INT4>(p, pool, a, part, plan, status, stream);
+            return launch_rows<64, TGVKV_CACHE_INT8>(p, pool, a, part, plan, status, stream);
+        return launch_rows<64, TGVKV_CACHE_INT4>(p, pool, a, part, plan, status, stream);
     }
     if (p.format == TGVKV_CACHE_BF16)
-        return launch_stream<128, TGVKV_CACHE_BF16>(p, pool, a, part, plan, status, stream);
+        return launch_rows<128, TGVKV_CACHE_BF16>(p, pool, a, part, plan, status, stream);
     if (p.format == TGVKV_CACHE_INT8)
-        return launch_stream<128, TGVKV_CACHE_INT8>(p, pool, a, part, plan, status, stream);
-    return launch_stream<128, TGVKV_CACHE_INT4>(p, pool, a, part, plan, status, stream);
+        return launch_rows<128, TGVKV_CACHE_INT8>(p, pool, a, part, plan, status, stream);
+    return launch_rows<128, TGVKV_CACHE_INT4>(p, pool, a, part, plan, status, stream);
 }
 
 }  // namespace tgvkv
