@@ -364,6 +364,7 @@ int make_cache_problem(const tgvkv_cache_desc* d, CacheProblem* p) {
     p->max_pages = d->max_pages;
     p->cap = (int)slots;
     p->format = d->format;
+    p->magic = 0x43004300u;
     const double scale = d->softmax_scale > 0.f ? (double)d->softmax_scale : 1.0 / sqrt((double)d->d);
     p->scale_log2 = (float)(scale * 1.4426950408889634);  // log2(e)
     return TGVKV_OK;

@@ -37,6 +37,9 @@ struct CacheProblem {
     int cap;                 // slots of a set: max_pages * page
     int format;              // TGVKV_CACHE_*
     float scale_log2;        // softmax_scale * log2(e)
+    uint32_t magic;          // 0x43004300, the int8 conversions' offset: as a parameter it
+                             // stays in a register, so that and-or is one instruction (it
+                             // is two with two immediates)
 };
 
 __host__ __device__ inline int cache_row_bytes(int d, int format) {
@@ -72,8 +75,8 @@ __device__ __forceinline__ uint32_t bf16x2_mul(uint32_t a, uint32_t b) {
 // Two int8 codes in the low bytes of x's halves (the high bytes are ignored):
 // bits 0-6 give 128 + low, bit 7 is the exponent's lowest bit, so or-ing it in
 // gives 128 or 256; the difference is the two's complement value.
-__device__ __forceinline__ uint32_t int8x2_to_bf16(uint32_t x) {
-    return bf16x2_sub((x & 0x007F007Fu) | 0x43004300u, (x & 0x00800080u) | 0x43004300u);
+__device__ __forceinline__ uint32_t int8x2_to_bf16(uint32_t x, uint32_t magic) {
+    return bf16x2_sub((x & 0x007F007Fu) | magic, (x & 0x00800080u) | magic);
 }
 
 // Two int4 codes (q + 8) in the low 4 bits of x's halves, times the scales
@@ -91,15 +94,15 @@ __device__ __forceinline__ uint32_t both(uint32_t half) { return half | (half <<
 
 // Eight consecutive stored codes (int4: in raw.x) of a group as bf16, in order.
 template <int FMT>
-__device__ __forceinline__ uint4 codes_to_bf16(uint2 raw, uint32_t byte) {
+__device__ __forceinline__ uint4 codes_to_bf16(uint2 raw, uint32_t byte, uint32_t magic) {
     uint32_t r[4];
     if (FMT == TGVKV_CACHE_INT8) {
         const uint32_t sc = both(scale_bf16(byte));
         const uint32_t words[2] = {raw.x, raw.y};
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            r[2 * i] = bf16x2_mul(int8x2_to_bf16(__byte_perm(words[i], 0, 0x4140)), sc);
-            r[2 * i + 1] = bf16x2_mul(int8x2_to_bf16(__byte_perm(words[i], 0, 0x4342)), sc);
+            r[2 * i] = bf16x2_mul(int8x2_to_bf16(__byte_perm(words[i], 0, 0x4140), magic), sc);
+            r[2 * i + 1] = bf16x2_mul(int8x2_to_bf16(__byte_perm(words[i], 0, 0x4342), magic), sc);
         }
     } else {
         const uint32_t base = both(int4_base(byte));

@@ -282,8 +282,8 @@ cache_read_kernel(const CacheProblem p, const CachePools pool,
         if (from[i * Gm::RPI + sub] < 0) continue;
         const long long u = u0 + i * Gm::RPI + sub;
         if (FMT != TGVKV_CACHE_BF16) {
-            kw[i] = codes_to_bf16<FMT>(make_uint2(kw[i].x, kw[i].y), kb[i]);
-            vw[i] = codes_to_bf16<FMT>(make_uint2(vw[i].x, vw[i].y), vb[i]);
+            kw[i] = codes_to_bf16<FMT>(make_uint2(kw[i].x, kw[i].y), kb[i], p.magic);
+            vw[i] = codes_to_bf16<FMT>(make_uint2(vw[i].x, vw[i].y), vb[i], p.magic);
         }
         __stcs(reinterpret_cast<uint4*>(k_out + u * D) + unit, kw[i]);
         __stcs(reinterpret_cast<uint4*>(v_out + u * D) + unit, vw[i]);

@@ -53,7 +53,7 @@ __host__ __device__ inline int chunk_record_floats(int rows, int d) {
     return rows * d + ((2 * rows + 3) & ~3);
 }
 
-constexpr int kStreamMax = 2048;       // streams of the row-stream kernel
+constexpr int kStreamMax = 2560;       // streams of the row-stream kernel
 constexpr int kStreamRows = 16;        // query rows it takes a set
 constexpr int kTileMaxCtas = 160;      // CTAs of the tile kernel
 constexpr int TM = 128;                // query rows of its row tiles
@@ -80,63 +80,86 @@ __device__ __forceinline__ long long set_units(const SetSpan& sp, const TilePlan
 }
 
 
-// Joins the records of one query row, in order: record i is at rec(i), the row
-// is row r of its rec_rows.  A whole warp; lane t gets dims [t D / 32, (t + 1) D /
-// 32) of the normalised result in acc.
-template <int D, typename Rec>
+// Joins the records of one query row (record i at rec(i), the row is row r of its
+// rec_rows), by WPR warps: warp wr takes every WPR-th batch of 8 and the warps'
+// sums are joined in warp order through `shared` (WPR > 1: floats [WPR][D + 2]).
+// Which record goes where depends on the count alone, so the result does not
+// depend on timing.  Lane t of warp 0 gets dims [t D / 32, (t + 1) D / 32) of the
+// normalised result in acc.
+template <int D, int WPR, typename Rec>
 __device__ __forceinline__ void merge_records(int count, int rec_rows, int r, Rec&& rec,
-                                              float (&acc)[D / 32]) {
+                                              float (&acc)[D / 32], float* shared, int wr) {
     constexpr int DPL = D / 32;
     const int lane = threadIdx.x & 31;
     float M = -INFINITY, L = 0.f;
 #pragma unroll
     for (int c = 0; c < DPL; ++c) acc[c] = 0.f;
-    for (int b = 0; b < count; b += 32) {
-        const int cnt = min(count - b, 32);
+    for (int b = 8 * wr; b < count; b += 8 * WPR) {
+        const int cnt = min(count - b, 8);
         float mw = -INFINITY, lw = 0.f;
         if (lane < cnt) {
             const float* pp = rec(b + lane) + rec_rows * D + r;
             mw = __ldcg(pp);
             lw = __ldcg(pp + rec_rows);
         }
+        float ov[8][DPL];                                    // 8 records' loads in flight
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+#pragma unroll
+            for (int c = 0; c < DPL; ++c) ov[u][c] = 0.f;
+            if (u < cnt) {
+                const float* ow = rec(b + u) + r * D + DPL * lane;
+                if (DPL == 4) {
+                    const float4 x = __ldcg(reinterpret_cast<const float4*>(ow));
+                    ov[u][0] = x.x, ov[u][1 % DPL] = x.y, ov[u][2 % DPL] = x.z, ov[u][3 % DPL] = x.w;
+                } else {
+                    const float2 x = __ldcg(reinterpret_cast<const float2*>(ow));
+                    ov[u][0] = x.x, ov[u][1 % DPL] = x.y;
+                }
+            }
+        }
         float Mb = mw;
 #pragma unroll
-        for (int k = 16; k > 0; k >>= 1) Mb = fmaxf(Mb, __shfl_xor_sync(~0u, Mb, k));
+        for (int k = 4; k > 0; k >>= 1) Mb = fmaxf(Mb, __shfl_xor_sync(~0u, Mb, k));
+        Mb = __shfl_sync(~0u, Mb, 0);
         const float Mn = fmaxf(M, Mb);
         const float ref = Mn == -INFINITY ? 0.f : Mn;        // no mass yet: all factors 0
         const float fa = fast_exp2(M - ref), f = fast_exp2(mw - ref);
-        float lf = lw * f;
-#pragma unroll
-        for (int k = 16; k > 0; k >>= 1) lf += __shfl_xor_sync(~0u, lf, k);
-        L = L * fa + lf;
+        L *= fa;
 #pragma unroll
         for (int c = 0; c < DPL; ++c) acc[c] *= fa;
         M = Mn;
-        for (int j0 = 0; j0 < cnt; j0 += 8) {                // 8 records' loads in flight
-            float ov[8][DPL];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
+        for (int u = 0; u < 8; ++u) {
+            const float fj = __shfl_sync(~0u, f, u), lj = __shfl_sync(~0u, lw, u);
+            if (u < cnt) {
+                L += lj * fj;
 #pragma unroll
-                for (int c = 0; c < DPL; ++c) ov[u][c] = 0.f;
-                if (j0 + u < cnt) {
-                    const float* ow = rec(b + j0 + u) + r * D + DPL * lane;
-                    if (DPL == 4) {
-                        const float4 x = __ldcg(reinterpret_cast<const float4*>(ow));
-                        ov[u][0] = x.x, ov[u][1 % DPL] = x.y, ov[u][2 % DPL] = x.z,
-                        ov[u][3 % DPL] = x.w;
-                    } else {
-                        const float2 x = __ldcg(reinterpret_cast<const float2*>(ow));
-                        ov[u][0] = x.x, ov[u][1 % DPL] = x.y;
-                    }
-                }
+                for (int c = 0; c < DPL; ++c) acc[c] += ov[u][c] * fj;
             }
+        }
+    }
+    if (WPR > 1) {
+        float* mine = shared + wr * (D + 2);
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const float fj = __shfl_sync(~0u, f, (j0 + u) & 31);
+        for (int c = 0; c < DPL; ++c) mine[DPL * lane + c] = acc[c];
+        if (lane == 0) mine[D] = M, mine[D + 1] = L;
+        __syncthreads();
+        if (wr != 0) return;
+        M = -INFINITY;
 #pragma unroll
-                for (int c = 0; c < DPL; ++c)
-                    if (j0 + u < cnt) acc[c] += ov[u][c] * fj;
-            }
+        for (int x = 0; x < WPR; ++x) M = fmaxf(M, shared[x * (D + 2) + D]);
+        const float ref = M == -INFINITY ? 0.f : M;
+        L = 0.f;
+#pragma unroll
+        for (int c = 0; c < DPL; ++c) acc[c] = 0.f;
+#pragma unroll
+        for (int x = 0; x < WPR; ++x) {
+            const float* o = shared + x * (D + 2);
+            const float f = fast_exp2(o[D] - ref);
+            L += o[D + 1] * f;
+#pragma unroll
+            for (int c = 0; c < DPL; ++c) acc[c] += o[DPL * lane + c] * f;
         }
     }
     const float inv = L > 0.f ? 1.f / L : (L == L ? 0.f : L);

@@ -48,9 +48,9 @@ chunk_tile_merge(const CacheProblem p, const ChunkArgs a, const TilePlan pl, int
         const int tiles = pl.tpi / pl.tpt, w = (i - u * pl.tpi) / pl.tpt;
         const int r = (i - u * pl.tpi - w * pl.tpt) * p.G + head % p.G;
         const size_t rec = chunk_record_floats(pl.rows, D);
-        merge_records<D>(w1 - w0 + 1, pl.rows, r, [&](int x) {
+        merge_records<D, 1>(w1 - w0 + 1, pl.rows, r, [&](int x) {
             return part + ((size_t)((w0 + x) * 2 + (x == 0 ? first : 0)) * tiles + w) * rec;
-        }, acc);
+        }, acc, nullptr, 0);
     }
     uint16_t* out = a.out + row * D + DPL * lane;
 #pragma unroll

@@ -36,34 +36,38 @@
 namespace tgvkv {
 namespace {
 
-constexpr int kW = 8;                  // streams (warps) per CTA
 constexpr int kStages = 2;
-constexpr int kPlanSets = 2048;        // plan entries kept in shared memory
 constexpr float kStale = 8.f;          // a reference maximum may trail by 2^8
 
 template <int D, int FMT, int NB>
 struct StreamGeom {
+    static constexpr bool QUANT = FMT != TGVKV_CACHE_BF16;
     static constexpr int ROWB = FMT == TGVKV_CACHE_BF16 ? 2 * D : FMT == TGVKV_CACHE_INT8 ? D : D / 2;
-    // slots per chunk: 4 KB of K and of V, at most 64
-    static constexpr int CH = 4096 / ROWB > 64 ? 64 : 4096 / ROWB;
-    static constexpr int KT = FMT == TGVKV_CACHE_BF16 ? D / 64 : 1;   // tiles of a row
-    static constexpr int TROW = ROWB / KT;                            // bytes of a tile's row
+    static constexpr int W = QUANT ? (NB == 1 ? 8 : 8) : (NB == 1 ? 8 : 8);                  // streams (warps) per CTA
+    static constexpr int TB = QUANT ? 4096 : 4096;
+    static constexpr int CH = TB / ROWB > 64 ? 64 : TB / ROWB < 16 ? 16 : TB / ROWB;                // slots per chunk
+    static constexpr int KT = QUANT ? 1 : D / 64; // tiles of a row
+    static constexpr int TROW = ROWB / KT;        // bytes of a tile's row
     static constexpr int kTile = CH * TROW;
-    static constexpr int SCB = FMT == TGVKV_CACHE_BF16 ? 0 : D / kGroup;   // scale bytes a row
+    static constexpr int SCB = QUANT ? D / kGroup : 0;   // scale bytes a row
+    // a stage: K, V; aside from the swizzled tiles: K's scales, V's, NB * 8 query rows
     static constexpr int kK = 0;
     static constexpr int kV = KT * kTile;
-    static constexpr int kKS = 2 * KT * kTile;
-    static constexpr int kVS = kKS + CH * SCB;
-    static constexpr int kQ = kVS + CH * SCB;
-    static constexpr int kStage = (kQ + NB * 8 * 2 * D + 1023) & ~1023;   // NB * 8 query rows
-    static constexpr int kRing = kW * kStages * kStage;
+    static constexpr int kStage = 2 * KT * kTile;
+    static constexpr int kKS = 0;
+    static constexpr int kVS = CH * SCB;
+    static constexpr int kQ = 2 * CH * SCB;
+    static constexpr int kSide = kQ + NB * 8 * 2 * D;
+    static constexpr int kRing = W * kStages * (kStage + kSide);
+    static_assert(kStage % 1024 == 0 && kTile % 256 == 0, "swizzled tiles");
 };
 
+template <int W>
 struct StreamTail {
-    uint64_t full[kW][kStages];
-    int warp_sum[kW];
+    uint64_t full[W][kStages];
+    int2 start[W];                     // each stream's first set, and chunk in it
+    int warp_sum[W];
     int never;
-    int pref[kPlanSets + 1];           // first chunk of entry e (a run of `run` sets)
 };
 
 __device__ __forceinline__ void ldsm_x4(uint32_t addr, uint32_t (&r)[4]) {
@@ -151,27 +155,13 @@ struct Walk {
         sp = set_span(p, a, s);
         chunks = set_chunks<CH>(sp);
     }
-    __device__ __forceinline__ void init(const CacheProblem& p, const ChunkArgs& a,
-                                         const int* pref, int entries, int run, int c, int c1) {
-        left = c1 - c;
+    __device__ __forceinline__ void init(const CacheProblem& p, const ChunkArgs& a, int2 start,
+                                         int count) {
+        left = count;
         fresh = true;
-        int lo = 0, hi = entries - 1;  // the last entry that starts at or before c
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (pref[mid] <= c) lo = mid;
-            else hi = mid - 1;
-        }
-        s = lo * run;
-        at = c - pref[lo];
+        s = start.x;
+        at = start.y;
         load(p, a);
-        while (at >= chunks) {         // c is below the total: a set holds it
-            at -= chunks;
-            if (++s >= p.S) {
-                left = 0;
-                return;
-            }
-            load(p, a);
-        }
     }
     // the chunk: slots [key0(), key0() + n()) of set s
     __device__ __forceinline__ int key0() const { return at * CH; }
@@ -196,7 +186,7 @@ struct Walk {
 // The copies of the walk's chunk into one stage, spread over the warp's lanes.
 // Lane b < boxes holds the page number of the chunk's b-th page slice.
 template <int D, int FMT, int NB>
-__device__ __forceinline__ void issue(unsigned char* stage, uint64_t* bar,
+__device__ __forceinline__ void issue(unsigned char* stage, unsigned char* side, uint64_t* bar,
                                       const Walk<StreamGeom<D, FMT, NB>::CH>& w, int page, int box,
                                       int box_shift, const CUtensorMap* mk, const CUtensorMap* mv,
                                       const CacheProblem& p, const CachePools& pool,
@@ -218,15 +208,15 @@ __device__ __forceinline__ void issue(unsigned char* stage, uint64_t* bar,
         }
         if (FMT != TGVKV_CACHE_BF16) {
             const size_t off = (size_t)row * Gm::SCB;
-            bulk_copy(smem_u32(stage + Gm::kKS) + at * Gm::SCB, pool.ks + off, box * Gm::SCB, bar);
-            bulk_copy(smem_u32(stage + Gm::kVS) + at * Gm::SCB, pool.vs + off, box * Gm::SCB, bar);
+            bulk_copy(smem_u32(side + Gm::kKS) + at * Gm::SCB, pool.ks + off, box * Gm::SCB, bar);
+            bulk_copy(smem_u32(side + Gm::kVS) + at * Gm::SCB, pool.vs + off, box * Gm::SCB, bar);
         }
     }
     if (w.fresh && lane < w.sp.n * p.G) {
         const int i = lane / p.G, h = lane - i * p.G;
         const uint16_t* src = a.q + (long long)(w.sp.tok0 + i) * a.q_tok +
                               (long long)((w.s % p.H_kv) * p.G + h) * a.q_head;
-        bulk_copy(smem_u32(stage + Gm::kQ) + lane * 2 * D, src, 2 * D, bar);
+        bulk_copy(smem_u32(side + Gm::kQ) + lane * 2 * D, src, 2 * D, bar);
     }
 }
 
@@ -246,13 +236,13 @@ __device__ __forceinline__ int out_dim(int mt, int g) {
 }
 
 template <int D, int FMT, int NB>
-__global__ void __launch_bounds__(kW * 32, 1)
+__global__ void __launch_bounds__(StreamGeom<D, FMT, NB>::W * 32, 1)
 chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                     const CacheProblem p, const CachePools pool, const ChunkArgs a, int box,
                     int box_shift, int min_chunks, int rec_rows, float* __restrict__ part,
                     long long* __restrict__ plan, uint32_t* __restrict__ status) {
     using Gm = StreamGeom<D, FMT, NB>;
-    constexpr int CH = Gm::CH;
+    constexpr int CH = Gm::CH, W = Gm::W;
     constexpr int KS = D / 16, MT = D / 16, KB = CH / 16;
     griddep_launch_dependents();
     if (threadIdx.x == 0) {
@@ -262,29 +252,20 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
     extern __shared__ unsigned char smem_raw[];
     unsigned char* ring = reinterpret_cast<unsigned char*>(
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    StreamTail& tl = *reinterpret_cast<StreamTail*>(ring + Gm::kRing);
+    StreamTail<W>& tl = *reinterpret_cast<StreamTail<W>*>(ring + Gm::kRing);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) tl.never = 0;
     if (lane == 0) {
         for (int st = 0; st < kStages; ++st) tc::mbar_init(&tl.full[warp][st], 1);
         tc::fence_mbar_init();
     }
-    if (blockIdx.x == 0) check_spans(p, a, tid, kW * 32, status);
+    if (blockIdx.x == 0) check_spans(p, a, tid, W * 32, status);
 
-    // ---- the plan: the first chunk of every entry (`run` consecutive sets)
-    const int run = (p.S + kPlanSets - 1) / kPlanSets;
-    const int entries = (p.S + run - 1) / run;
-    constexpr int PER = kPlanSets / (kW * 32);       // entries a thread sums
-    int cnt[PER], sum = 0;
-#pragma unroll
-    for (int u = 0; u < PER; ++u) {
-        const int e = tid * PER + u;
-        cnt[u] = 0;
-        if (e < entries)
-            for (int s = e * run; s < min((e + 1) * run, p.S); ++s)
-                cnt[u] += set_chunks<CH>(set_span(p, a, s));
-        sum += cnt[u];
-    }
+    // ---- the plan: thread t counts the chunks of sets [t * run, (t + 1) * run)
+    const int run = (p.S + W * 32 - 1) / (W * 32);
+    const int s_lo = min(tid * run, p.S), s_hi = min(s_lo + run, p.S);
+    int sum = 0;
+    for (int s = s_lo; s < s_hi; ++s) sum += set_chunks<CH>(set_span(p, a, s));
     int incl = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -294,36 +275,39 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
     if (lane == 31) tl.warp_sum[warp] = incl;
     __syncthreads();
     int base = incl - sum, total = 0;
-    for (int w = 0; w < kW; ++w) {
-        if (w < warp) base += tl.warp_sum[w];
-        total += tl.warp_sum[w];
-    }
 #pragma unroll
-    for (int u = 0; u < PER; ++u) {
-        const int e = tid * PER + u;
-        if (e < entries) tl.pref[e] = base;
-        if (blockIdx.x == 0 && e < entries) {        // the plan, for the merge kernel
+    for (int x = 0; x < W; ++x) {
+        if (x < warp) base += tl.warp_sum[x];
+        total += tl.warp_sum[x];
+    }
+    const int n_streams = gridDim.x * W;
+    const int per = max((total + n_streams - 1) / n_streams, min_chunks);
+    // the starts of this CTA's streams that lie in my sets; CTA 0 also writes the plan
+    {
+        const long long first = (long long)blockIdx.x * W * per;
+        if (blockIdx.x == 0 || (first < (long long)base + sum && first + (long long)W * per > base)) {
             int at = base;
-            for (int s = e * run; s < min((e + 1) * run, p.S); ++s) {
-                plan[s] = at;
-                at += run == 1 ? cnt[u] : set_chunks<CH>(set_span(p, a, s));
+            for (int s = s_lo; s < s_hi; ++s) {
+                const int n = set_chunks<CH>(set_span(p, a, s));
+                if (blockIdx.x == 0) plan[s] = at;
+                for (int x = 0; x < W; ++x) {
+                    const long long c = first + (long long)x * per;
+                    if (c >= at && c < (long long)at + n) tl.start[x] = make_int2(s, (int)c - at);
+                }
+                at += n;
             }
         }
-        base += cnt[u];
+        if (blockIdx.x == 0 && tid == 0) plan[p.S] = total;
     }
-    if (blockIdx.x == 0 && tid == 0) plan[p.S] = total;
     __syncthreads();
-
-    const int n_streams = gridDim.x * kW;
-    const int per = max((total + n_streams - 1) / n_streams, min_chunks);
-    const int si = blockIdx.x * kW + warp;
+    const int si = blockIdx.x * W + warp;
     const long long c_lo = (long long)si * per;
     if (c_lo >= total) return;
-    const int c0 = (int)c_lo, c1 = min(c0 + per, total);
 
     unsigned char* wring = ring + warp * kStages * Gm::kStage;
+    unsigned char* wside = ring + W * kStages * Gm::kStage + warp * kStages * Gm::kSide;
     Walk<CH> ahead;                    // the next chunk to fetch
-    ahead.init(p, a, tl.pref, entries, run, c0, c1);
+    ahead.init(p, a, tl.start[warp], (int)min((long long)per, total - c_lo));
     Walk<CH> w = ahead;                // the next chunk to work on
     const int32_t* table = a.page_table + (size_t)ahead.s * p.max_pages;
     auto page_of = [&]() {             // lane b: page number of the chunk's slice b
@@ -334,7 +318,7 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
     int issued = 0;
     auto refill = [&]() {              // the next chunk into the stage just read
         const int st = issued % kStages;
-        issue<D, FMT, NB>(wring + st * Gm::kStage, &tl.full[warp][st], ahead,
+        issue<D, FMT, NB>(wring + st * Gm::kStage, wside + st * Gm::kSide, &tl.full[warp][st], ahead,
                           valid_page(p, page, status), box, box_shift, &mk, &mv, p, pool, a, lane);
         ++issued;
         ahead.step(p, a);
@@ -358,7 +342,7 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
         const bool got = tc::mbar_wait(&tl.full[warp][st], (i / kStages) & 1, &tl.never);
         if (!__all_sync(~0u, got)) break;
         unsigned char* stage = wring + st * Gm::kStage;
-        const uint32_t sb = smem_u32(stage);
+        const uint32_t sb = smem_u32(stage), sd = smem_u32(wside + st * Gm::kSide);
         const int key0 = w.key0(), n = w.n();
         if (w.fresh) {
             seg_starts = w.at == 0;
@@ -367,7 +351,7 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
             // rows the set does not have
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
-                const uint32_t q0 = sb + Gm::kQ + (8 * nb + g) * 2 * D;
+                const uint32_t q0 = sd + Gm::kQ + (8 * nb + g) * 2 * D;
                 if (FMT == TGVKV_CACHE_BF16) {
 #pragma unroll
                     for (int s = 0; s < KS; ++s) {
@@ -445,7 +429,7 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
                         }
                     }
                     const uint32_t byte =
-                        lds8(sb + Gm::kKS + row * Gm::SCB + (D == 128 ? tq : tq >> 1));
+                        lds8(sd + Gm::kKS + row * Gm::SCB + (D == 128 ? tq : tq >> 1));
                     kb_s[x] = both(FMT == TGVKV_CACHE_INT8 ? scale_bf16(byte) : int4_base(byte));
                 }
 #pragma unroll
@@ -455,8 +439,8 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
                     for (int x = 0; x < 2; ++x) {
                         if (FMT == TGVKV_CACHE_INT8) {
                             const uint32_t c = wd[x][s % NW];
-                            r[x] = bf16x2_mul(int8x2_to_bf16(c), kb_s[x]);
-                            r[2 + x] = bf16x2_mul(int8x2_to_bf16(c >> 8), kb_s[x]);
+                            r[x] = bf16x2_mul(int8x2_to_bf16(c, p.magic), kb_s[x]);
+                            r[2 + x] = bf16x2_mul(int8x2_to_bf16(c >> 8, p.magic), kb_s[x]);
                         } else {
                             const uint32_t c = wd[x][(s / 2) % NW];
                             r[x] = int4x2_to_bf16(c >> (8 * (s & 1)), kb_s[x]);
@@ -575,10 +559,10 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
                     const int k0 = 16 * kb + 2 * tq + 8 * h;
                     uint32_t w0, w1;
                     if (D == 128) {
-                        const uint2 t = lds64(sb + Gm::kVS + k0 * 4);
+                        const uint2 t = lds64(sd + Gm::kVS + k0 * 4);
                         w0 = t.x, w1 = t.y;
                     } else {
-                        const uint32_t t = lds32(sb + Gm::kVS + k0 * 2);
+                        const uint32_t t = lds32(sd + Gm::kVS + k0 * 2);
                         w0 = t & 0xFFFFu, w1 = t >> 16;
                     }
                     if (k0 >= n) w0 = 0u;
@@ -603,10 +587,10 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
                         const uint32_t r0 = r[2 * x], r1 = r[2 * x + 1];
                         if (FMT == TGVKV_CACHE_INT8) {
                             const uint32_t s0 = vs[0][(u / 2) % NG], s1 = vs[1][(u / 2) % NG];
-                            const uint32_t v[4] = {bf16x2_mul(int8x2_to_bf16(r0), s0),
-                                                   bf16x2_mul(int8x2_to_bf16(r0 >> 8), s0),
-                                                   bf16x2_mul(int8x2_to_bf16(r1), s1),
-                                                   bf16x2_mul(int8x2_to_bf16(r1 >> 8), s1)};
+                            const uint32_t v[4] = {bf16x2_mul(int8x2_to_bf16(r0, p.magic), s0),
+                                                   bf16x2_mul(int8x2_to_bf16(r0 >> 8, p.magic), s0),
+                                                   bf16x2_mul(int8x2_to_bf16(r1, p.magic), s1),
+                                                   bf16x2_mul(int8x2_to_bf16(r1 >> 8, p.magic), s1)};
 #pragma unroll
                             for (int nb = 0; nb < NB; ++nb) mma(o[u % MT][nb], v, pb[nb][0], pb[nb][1]);
                         } else {
@@ -695,17 +679,18 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
     }
 }
 
-// The split sets' merge and the rows that see nothing: one warp per (set, query
+// The split sets' merge and the rows that see nothing: WPR warps per (set, query
 // row), a programmatic dependent of the stream kernel.  A set's partials are
 // combined in stream order.
-template <int D>
-__global__ void __launch_bounds__(128)
+template <int D, int WPR>
+__global__ void __launch_bounds__(WPR == 1 ? 128 : WPR * 32)
 chunk_stream_merge(const CacheProblem p, const ChunkArgs a, int n_streams, int min_chunks,
                    int rec_rows, const float* __restrict__ part,
                    const long long* __restrict__ plan) {
     constexpr int DPL = D / 32;
-    const int lane = threadIdx.x & 31;
-    const long long gw = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
+    __shared__ float shared[WPR == 1 ? 1 : WPR * (D + 2)];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const long long gw = WPR == 1 ? (long long)blockIdx.x * 4 + warp : (long long)blockIdx.x;
     const int s = (int)(gw / rec_rows), r = (int)(gw % rec_rows);
     SetSpan sp{0, 0, 0};
     if (s < p.S) sp = set_span(p, a, s);
@@ -723,10 +708,11 @@ chunk_stream_merge(const CacheProblem p, const ChunkArgs a, int n_streams, int m
         // a segment starts its stream's share, but for a set that begins inside it
         const int first = c0 != w0 * per ? 1 : 0;
         const size_t rec = chunk_record_floats(rec_rows, D);
-        merge_records<D>(w1 - w0 + 1, rec_rows, r, [&](int i) {
+        merge_records<D, WPR>(w1 - w0 + 1, rec_rows, r, [&](int i) {
             return part + ((size_t)(w0 + i) * 2 + (i == 0 ? first : 0)) * rec;
-        }, acc);
+        }, acc, shared, WPR == 1 ? 0 : warp);
     }
+    if (WPR > 1 && warp != 0) return;
     const int t = r / p.G, hh = r - t * p.G;
     uint16_t* out = a.out + ((size_t)(sp.tok0 + t) * p.H_q + (s % p.H_kv) * p.G + hh) * D + DPL * lane;
 #pragma unroll
@@ -735,7 +721,7 @@ chunk_stream_merge(const CacheProblem p, const ChunkArgs a, int n_streams, int m
 }
 
 // Chunks a stream takes at least: below this, splitting costs more than it saves.
-constexpr int kMinChunks = 2;
+constexpr int kMinChunks = 4;
 
 template <int D, int FMT, int NB>
 cudaError_t launch_stream(const CacheProblem& p, const CachePools& pool, const ChunkArgs& a,
@@ -750,22 +736,27 @@ cudaError_t launch_stream(const CacheProblem& p, const CachePools& pool, const C
     if (!make_pool_map(&mk, pool.k, rows, Gm::ROWB, box_bytes, box) ||
         !make_pool_map(&mv, pool.v, rows, Gm::ROWB, box_bytes, box))
         return cudaErrorInvalidValue;
-    const size_t smem = 1024 + Gm::kRing + sizeof(StreamTail);
-    static_assert(1024 + Gm::kRing + sizeof(StreamTail) <= 227 * 1024, "shared memory of one CTA");
+    const size_t smem = 1024 + Gm::kRing + sizeof(StreamTail<Gm::W>);
+    static_assert(1024 + Gm::kRing + sizeof(StreamTail<Gm::W>) <= 227 * 1024, "shared memory of one CTA");
     cudaError_t e = cudaFuncSetAttribute(chunk_stream_kernel<D, FMT, NB>,
                                          cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     const int sms = device_sm_count();
     if (sms <= 0) return cudaErrorInvalidDevice;
-    const int ctas = sms < kStreamMax / kW ? sms : kStreamMax / kW;
+    const int ctas = sms < kStreamMax / Gm::W ? sms : kStreamMax / Gm::W;
     const int rec_rows = a.max_q * p.G;
-    chunk_stream_kernel<D, FMT, NB><<<ctas, kW * 32, smem, stream>>>(
+    chunk_stream_kernel<D, FMT, NB><<<ctas, Gm::W * 32, smem, stream>>>(
         mk, mv, p, pool, a, box, box_shift, kMinChunks, rec_rows, part, plan, status);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    const long long warps = (long long)p.S * rec_rows;
-    return launch_dependent(chunk_stream_merge<D>, dim3((unsigned)((warps + 3) / 4)), dim3(128), 0,
-                            stream, p, a, ctas * kW, (int)kMinChunks, rec_rows,
-                            static_cast<const float*>(part), static_cast<const long long*>(plan));
+    // a set has about n_streams / S records: from 16 on, 8 warps join a row
+    const long long rows_out = (long long)p.S * rec_rows;
+    const float* parts = part;
+    const long long* plans = plan;
+    if ((long long)p.S * 16 <= ctas * Gm::W)
+        return launch_dependent(chunk_stream_merge<D, 8>, dim3((unsigned)rows_out), dim3(256), 0, stream,
+                                p, a, ctas * Gm::W, (int)kMinChunks, rec_rows, parts, plans);
+    return launch_dependent(chunk_stream_merge<D, 1>, dim3((unsigned)((rows_out + 3) / 4)), dim3(128),
+                            0, stream, p, a, ctas * Gm::W, (int)kMinChunks, rec_rows, parts, plans);
 }
 
 template <int D, int FMT>

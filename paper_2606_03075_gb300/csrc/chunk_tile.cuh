@@ -780,7 +780,8 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
                     uint2 c = make_uint2(0u, 0u);
                     if (FMT == TGVKV_CACHE_INT8) c = reinterpret_cast<const uint2*>(raw)[e];
                     else c.x = reinterpret_cast<const uint32_t*>(raw)[e];
-                    uint4 v = codes_to_bf16<FMT>(c, sm.sc[rs][row * (D / kGroup) + (u >> 2)]);
+                    uint4 v = codes_to_bf16<FMT>(c, sm.sc[rs][row * (D / kGroup) + (u >> 2)],
+                                                 p.magic);
                     if (row >= live) v = make_uint4(0u, 0u, 0u, 0u);   // past the set's end
                     *reinterpret_cast<uint4*>(dst + (u >> 3) * Gm::HALF + row * 128 +
                                               (((u & 7) ^ (row & 7)) << 4)) = v;
