@@ -371,9 +371,10 @@ int make_cache_problem(const tgvkv_cache_desc* d, CacheProblem* p) {
 }
 
 // Workspace of the paged-cache calls: the status word, the attention's plan
-// (the first unit of work of every set) and the partial results of split sets.
+// (the first unit of work of every set; the items split over CTAs) and the
+// partial results of split sets.
 struct CacheLayout {
-    size_t plan, part, total;
+    size_t plan, split, part, total;
 };
 
 CacheLayout cache_layout(const CacheProblem& p) {
@@ -381,6 +382,8 @@ CacheLayout cache_layout(const CacheProblem& p) {
     size_t o = round_up(sizeof(uint32_t));
     w.plan = o;
     o += round_up(sizeof(long long) * ((size_t)p.S + 1));
+    w.split = o;
+    o += round_up(sizeof(SplitItem) * kTileMaxCtas);
     w.part = o;
     // two records per stream, or per CTA and row tile of a pair
     const size_t stream = 2 * (size_t)kStreamMax * chunk_record_floats(kStreamRows, p.d);
@@ -844,6 +847,7 @@ int tgvkv_chunk_attention(const tgvkv_cache_desc* desc, const tgvkv_cache_pools*
     char* ws = static_cast<char*>(workspace);
     float* part = reinterpret_cast<float*>(ws + lay.part);
     long long* plan = reinterpret_cast<long long*>(ws + lay.plan);
+    SplitItem* split = reinterpret_cast<SplitItem*>(ws + lay.split);
     uint32_t* status = static_cast<uint32_t*>(workspace);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     cudaError_t e;
@@ -851,9 +855,9 @@ int tgvkv_chunk_attention(const tgvkv_cache_desc* desc, const tgvkv_cache_pools*
         e = launch_chunk_stream(p, pl, a, part, plan, status, st);
     } else {
         const bool pair = a.max_q > TM / p.G;   // some chunk has more than one row tile
-        e = p.format == TGVKV_CACHE_BF16   ? launch_tile_bf16(p, pl, a, part, plan, pair, status, st)
-            : p.format == TGVKV_CACHE_INT8 ? launch_tile_int8(p, pl, a, part, plan, pair, status, st)
-                                           : launch_tile_int4(p, pl, a, part, plan, pair, status, st);
+        e = p.format == TGVKV_CACHE_BF16   ? launch_tile_bf16(p, pl, a, part, split, pair, status, st)
+            : p.format == TGVKV_CACHE_INT8 ? launch_tile_int8(p, pl, a, part, split, pair, status, st)
+                                           : launch_tile_int4(p, pl, a, part, split, pair, status, st);
     }
     return e == cudaSuccess ? ok() : cuda_fail(e, "chunk attention launch");
 }

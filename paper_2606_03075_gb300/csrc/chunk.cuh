@@ -66,6 +66,13 @@ struct TilePlan {
     int rows;                          // query rows of a record: tpt * G at most
 };
 
+// What a CTA of the tile kernel leaves for the merge: the item that begins in it
+// and ends in a later CTA (set -1: none), the CTAs it spans, and which of this
+// CTA's two records is its first.
+struct SplitItem {
+    int s, u, ctas, slot;
+};
+
 // Key tiles that the tokens of set `sp` below `tok_end` see.
 __device__ __forceinline__ int tiles_seen(const SetSpan& sp, int tok_end) {
     const int vis = min(sp.len - sp.n + min(sp.n, tok_end), sp.len);

@@ -1,74 +1,67 @@
 // Joins the partial results that the tile kernel (chunk_tile.cuh) leaves for items
-// that span several CTAs, in CTA order (so results do not depend on timing),
-// and writes 0 for the rows that see no slot.  One warp per output row; most
-// rows of a large call were written by the tile kernel and return at once.  A
-// programmatic dependent of that kernel: the search for a row's item reads
-// inputs only and overlaps it.
+// that span several CTAs, in CTA order (so results do not depend on timing).  Each
+// CTA of that kernel names the one item that begins in it and goes on in the
+// next; the merge's CTA (x, y) takes rows 8 x .. 8 x + 7 of CTA y's item, a warp
+// each, or all 8 warps row after row when an item has many records.  A
+// programmatic dependent of the tile kernel.
 #include "cache_launch.h"
 #include "launch.h"
 
 namespace tgvkv {
 namespace {
 
+constexpr int kMergeRows = 8;
+constexpr int kManyRecords = 32;       // from here on, 8 warps a row
+
 template <int D>
-__global__ void __launch_bounds__(128)
-chunk_tile_merge(const CacheProblem p, const ChunkArgs a, const TilePlan pl, int ctas,
-                 const float* __restrict__ part, const long long* __restrict__ plan) {
+__global__ void __launch_bounds__(256)
+chunk_tile_merge(const CacheProblem p, const ChunkArgs a, const TilePlan pl,
+                 const float* __restrict__ part, const SplitItem* __restrict__ split) {
     constexpr int DPL = D / 32;
-    const int lane = threadIdx.x & 31;
-    const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
-    const int t = (int)(row / p.H_q), head = (int)(row - (long long)t * p.H_q);
-    int lo = 0, hi = p.B - 1;          // the last sequence that starts at or before t
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (__ldg(a.tok_offsets + mid) <= t) lo = mid;
-        else hi = mid - 1;
-    }
-    const int s = lo * p.H_kv + head / p.G;
-    const SetSpan sp = set_span(p, a, s);
-    const int i = t - sp.tok0;
-    const bool mine = t < a.T && i >= 0 && i < sp.n;
-    const int u = mine ? i / pl.tpi : 0;
-    const int nk = mine ? tiles_seen(sp, (u + 1) * pl.tpi) : 0;
-    long long before = 0;              // units of the set's earlier items
-    for (int x = lane; x < u; x += 32) before += tiles_seen(sp, (x + 1) * pl.tpi);
-#pragma unroll
-    for (int k = 16; k > 0; k >>= 1) before += __shfl_xor_sync(~0u, before, k);
+    __shared__ float shared[8 * (D + 2)];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     griddep_wait();
-    if (!mine) return;
-    float acc[DPL];
+    const int4 raw = __ldcg(reinterpret_cast<const int4*>(split) + blockIdx.y);
+    const SplitItem it{raw.x, raw.y, raw.z, raw.w};
+    if (it.s < 0) return;
+    const SetSpan sp = set_span(p, a, it.s);
+    const int tok0 = it.u * pl.tpi;    // the item's first token within its chunk
+    const int rows = min(pl.tpi, sp.n - tok0) * p.G;
+    const int tiles = pl.tpi / pl.tpt;
+    const size_t rec = chunk_record_floats(pl.rows, D);
+    const bool many = it.ctas >= kManyRecords;
+    for (int k = many ? 0 : warp; k < kMergeRows; k += many ? 1 : 8) {
+        const int row = blockIdx.x * kMergeRows + k;         // row of the item
+        if (row >= rows) break;
+        const int w = row / pl.rows, r = row - w * pl.rows;  // its tile, and row there
+        const int t = tok0 + row / p.G, head = (it.s % p.H_kv) * p.G + row % p.G;
+        float acc[DPL];
+        auto record = [&](int x) {
+            return part + (((size_t)blockIdx.y + x) * 2 * tiles + (x == 0 ? it.slot : 0) * tiles + w) * rec;
+        };
+        if (many) {
+            merge_records<D, 8>(it.ctas, pl.rows, r, record, acc, shared, warp);
+            __syncthreads();           // shared is free for the next row
+            if (warp != 0) continue;
+        } else {
+            merge_records<D, 1>(it.ctas, pl.rows, r, record, acc, nullptr, 0);
+        }
+        uint16_t* out = a.out + ((size_t)(sp.tok0 + t) * p.H_q + head) * D + DPL * lane;
 #pragma unroll
-    for (int c = 0; c < DPL; ++c) acc[c] = 0.f;
-    if (nk > 0) {
-        const long long total = __ldcg(plan + p.S), c0 = __ldcg(plan + s) + before;
-        const long long per = (total + ctas - 1) / ctas;
-        const int w0 = (int)(c0 / per), w1 = (int)((c0 + nk - 1) / per);
-        if (w0 == w1) return;          // inside one CTA: written by it
-        const int first = c0 != w0 * per ? 1 : 0;
-        const int tiles = pl.tpi / pl.tpt, w = (i - u * pl.tpi) / pl.tpt;
-        const int r = (i - u * pl.tpi - w * pl.tpt) * p.G + head % p.G;
-        const size_t rec = chunk_record_floats(pl.rows, D);
-        merge_records<D, 1>(w1 - w0 + 1, pl.rows, r, [&](int x) {
-            return part + ((size_t)((w0 + x) * 2 + (x == 0 ? first : 0)) * tiles + w) * rec;
-        }, acc, nullptr, 0);
+        for (int c = 0; c < DPL; c += 2)
+            *reinterpret_cast<uint32_t*>(out + c) = pack_bf16x2(acc[c], acc[(c + 1) % DPL]);
     }
-    uint16_t* out = a.out + row * D + DPL * lane;
-#pragma unroll
-    for (int c = 0; c < DPL; c += 2)
-        *reinterpret_cast<uint32_t*>(out + c) = pack_bf16x2(acc[c], acc[(c + 1) % DPL]);
 }
 
 }  // namespace
 
 cudaError_t launch_tile_merge(const CacheProblem& p, const ChunkArgs& a, const TilePlan& pl, int ctas,
-                              const float* part, const long long* plan, cudaStream_t stream) {
-    const long long rows = (long long)a.T * p.H_q;
-    const dim3 grid((unsigned)((rows + 3) / 4));
+                              const float* part, const SplitItem* split, cudaStream_t stream) {
+    const int tokens = a.max_q < pl.tpi ? a.max_q : pl.tpi;      // of an item, at most
+    const dim3 grid((unsigned)((tokens * p.G + kMergeRows - 1) / kMergeRows), (unsigned)ctas);
     if (p.d == 64)
-        return launch_dependent(chunk_tile_merge<64>, grid, dim3(128), 0, stream, p, a, pl, ctas, part,
-                                plan);
-    return launch_dependent(chunk_tile_merge<128>, grid, dim3(128), 0, stream, p, a, pl, ctas, part,
-                            plan);
+        return launch_dependent(chunk_tile_merge<64>, grid, dim3(256), 0, stream, p, a, pl, part, split);
+    return launch_dependent(chunk_tile_merge<128>, grid, dim3(256), 0, stream, p, a, pl, part, split);
 }
 
 }  // namespace tgvkv

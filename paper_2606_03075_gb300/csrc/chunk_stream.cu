@@ -721,7 +721,7 @@ chunk_stream_merge(const CacheProblem p, const ChunkArgs a, int n_streams, int m
 }
 
 // Chunks a stream takes at least: below this, splitting costs more than it saves.
-constexpr int kMinChunks = 4;
+constexpr int kMinChunks = 1;
 
 template <int D, int FMT, int NB>
 cudaError_t launch_stream(const CacheProblem& p, const CachePools& pool, const ChunkArgs& a,

@@ -28,8 +28,10 @@
 // write them as bf16 in the swizzled layout (exact: scales are powers of two),
 // and the rest is the bf16 kernel.
 //
-// Roles: warp 0 TMA, warp 1 MMA issue (and TMEM), warps 4-11 softmax, warps
-// 12-19 converters (integer caches).  Every wait is bounded; a timeout sets
+// Roles: warp 0 TMA, warps 1 and 2 MMA issue, one per group (1 also owns the
+// TMEM), warp 3 rows without work, warps 4-11 softmax, warps 12
+// on converters (integer caches).  Registers are split by role (setmaxnreg), so
+// that a softmax thread holds a whole row of S.  Every wait is bounded; a timeout sets
 // TGVKV_STATUS_TIMEOUT and the CTA unwinds after its copies and MMAs finished.
 #pragma once
 
@@ -41,18 +43,41 @@ namespace tgvkv {
 
 constexpr int kSoftWarp = 4;           // first softmax warp
 constexpr int kConvWarp = 12;          // first converter warp
-constexpr int kConvWarps = 8;
 constexpr uint32_t kOCol = 256;        // first O column; S at 0 and 128
 constexpr float kRescale = 8.f;        // a stale maximum may trail by 2^8
 
-// D[tmem] (+)= A[tmem] * B[smem], issued by one thread.
-__device__ __forceinline__ void mma_bf16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t b,
-                                            uint32_t idesc, uint32_t accumulate) {
+// The issuing warps run as a whole, so that addresses stay in uniform registers;
+// one elected lane issues.
+__device__ __forceinline__ uint32_t elect_one() {
+    uint32_t r;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
-        "r"(a_tmem), "l"(b), "r"(idesc), "r"(accumulate)
+        "elect.sync _|p, 0xFFFFFFFF;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(r));
+    return r;
+}
+// D[tmem] (+)= A[smem] * B[smem]^T.  Of a descriptor only the low word (the address)
+// changes between the instructions of a tile: an add and no carry.
+__device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t a_hi,
+                                       uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "mov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %4};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %5, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_lo), "r"(b_lo), "r"(a_hi), "r"(b_hi), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// D[tmem] (+)= A[tmem] * B[smem]
+__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t b_hi,
+                                       uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "mov.b64 b, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_tmem), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
         : "memory");
 }
 
@@ -63,6 +88,18 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16
         "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
         "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
         "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+        : "memory");
+}
+
+// 16 consecutive 32-bit columns of this thread's TMEM lane (warp-wide).
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]),
+          "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]),
+          "=r"(v[14]), "=r"(v[15])
+        : "r"(taddr)
         : "memory");
 }
 
@@ -92,26 +129,29 @@ struct TileGeom {
     static constexpr int NRAW = QUANT ? (FMT == TGVKV_CACHE_INT8 ? 3 : 6) : 0;
     static constexpr int NQ = PAIR ? 1 : 2;                       // Q slots
     static constexpr int QT = PAIR ? 2 : 1;                       // row tiles a slot
-    static constexpr int THREADS = 32 * (QUANT ? kConvWarp + kConvWarps : kConvWarp);
+    // converters: SPLIT calls wait for memory and softmax has few rows, PAIR calls
+    // need the registers for softmax
+    static constexpr int CW = !QUANT ? 0 : PAIR ? 4 : 8;
+    static constexpr int THREADS = 32 * (kConvWarp + CW);
+    // registers a thread: at launch (the most that the thread count allows), then by
+    // role.  The roles' sum is at most the launch's: what setmaxnreg raises one by has
+    // to come from the others.
+    static constexpr int LAUNCH_REGS = CW == 0 ? 168 : CW == 4 ? 128 : 96;
+    static constexpr int FEW_REGS = 72, CONV_REGS = CW == 4 ? 80 : 64;
+    static constexpr int SOFT_REGS = CW == 0 ? 208 : CW == 4 ? 176 : 136;
+    static constexpr int S_COLS = CW == 8 ? 64 : 128;   // S columns a thread holds at a time
+    static_assert(128 * FEW_REGS + 256 * SOFT_REGS + 32 * CW * CONV_REGS <= THREADS * LAUNCH_REGS,
+                  "register split");
 };
 
-template <int D, int FMT, bool PAIR>
-struct TileSmem {
-    using Gm = TileGeom<D, FMT, PAIR>;
-    unsigned char q[Gm::NQ * Gm::QT][D * 2 * TM];     // 64 dims each, 128-byte swizzled rows
-    unsigned char kv[Gm::NST][Gm::TILE];              // the ring, in MMA order
-    unsigned char raw[Gm::QUANT ? Gm::NRAW : 1][Gm::QUANT ? Gm::RAW : 16];
-    unsigned char sc[Gm::QUANT ? Gm::NRAW : 1][Gm::QUANT ? Gm::SC : 16];
-    uint64_t full[Gm::NST], empty[Gm::NST];
-    uint64_t raw_full[Gm::QUANT ? Gm::NRAW : 1], raw_empty[Gm::QUANT ? Gm::NRAW : 1];
-    uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_done[2];
-    uint64_t join_in, join_out, mma_done;
-    float2 ml[PAIR ? 1 : 2][PAIR ? 1 : TM];           // SPLIT: the groups' (m, l)
-    uint32_t tmem_base;
-    int abort_flag, never;
-    long long warp_sum[Gm::THREADS / 32];
-    int start_s, start_u, start_j;
-};
+template <int N>
+__device__ __forceinline__ void regs_down() {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void regs_up() {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
 
 // ---- the work ----------------------------------------------------------------
 // A segment: key tiles [j0, j1) of item u of set s.
@@ -164,6 +204,28 @@ struct TileWalk {
     }
 };
 
+template <int D, int FMT, bool PAIR>
+struct TileSmem {
+    using Gm = TileGeom<D, FMT, PAIR>;
+    unsigned char q[Gm::NQ * Gm::QT][D * 2 * TM];     // 64 dims each, 128-byte swizzled rows
+    unsigned char kv[Gm::NST][Gm::TILE];              // the ring, in MMA order
+    unsigned char raw[Gm::QUANT ? Gm::NRAW : 1][Gm::QUANT ? Gm::RAW : 16];
+    unsigned char sc[Gm::QUANT ? Gm::NRAW : 1][Gm::QUANT ? Gm::SC : 16];
+    uint64_t full[Gm::NST], empty[Gm::NST];
+    uint64_t raw_full[Gm::QUANT ? Gm::NRAW : 1], raw_empty[Gm::QUANT ? Gm::NRAW : 1];
+    uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_done[2];
+    uint64_t join_in, join_out, mma_done;
+    float2 ml[PAIR ? 1 : 2][PAIR ? 1 : TM];           // SPLIT: the groups' (m, l)
+    struct {                                          // a softmax warp's place in the work:
+        TileWalk walk;                                // here, as its registers hold S
+        Seg g;
+    } at[8];
+    uint32_t tmem_base;
+    int abort_flag, never, turn;
+    long long warp_sum[Gm::THREADS / 32];
+    int start_s, start_u, start_j;
+};
+
 // Row tile w of a segment's item (PAIR), or its one row tile: its key tiles.
 template <bool PAIR>
 __device__ __forceinline__ int group_tiles(const Seg& g, const TilePlan& pl, int w) {
@@ -172,12 +234,9 @@ __device__ __forceinline__ int group_tiles(const Seg& g, const TilePlan& pl, int
     return t < g.sp.n ? tiles_seen(g.sp, t + pl.tpt) : 0;
 }
 
-// Place of key tile x (counted from the segment's first, of n) of K and of V in
-// the order of the ring.  PAIR: K0 V0 K1 V1 ...; SPLIT: K0 K1 V0 K2 V1 ...
-template <bool PAIR>
-__device__ __forceinline__ int k_place(int x) {
-    return PAIR ? 2 * x : (x == 0 ? 0 : 2 * x - 1);
-}
+// Place of V of key tile x (counted from the segment's first, of n) in the order
+// of the ring, K's taking the other places.  PAIR: K0 V0 K1 V1 ...; SPLIT: K0 K1
+// V0 K2 V1 ...
 template <bool PAIR>
 __device__ __forceinline__ int v_place(int x, int n) {
     return PAIR ? 2 * x + 1 : min(2 * x + 2, 2 * n - 1);
@@ -187,12 +246,27 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volati
     return __all_sync(~0u, tc::mbar_wait(bar, parity, abort));
 }
 
+// A turn of issuing, for two warps; the wait is bounded like those on mbarriers.
+__device__ __forceinline__ bool take_turn(int* turn, int lane, volatile int* abort) {
+    int got = 1;
+    if (lane == 0) {
+        const long long c0 = clock64();
+        while ((got = atomicExch(turn, 1) == 0) == 0)
+            if (*abort || clock64() - c0 > tc::kWaitLimitCycles) break;
+    }
+    return __shfl_sync(~0u, got, 0) != 0;
+}
+__device__ __forceinline__ void end_turn(int* turn, int lane) {
+    __syncwarp();
+    if (lane == 0) atomicExch(turn, 0);
+}
+
 template <int D, int FMT, bool PAIR>
 __global__ void __launch_bounds__(TileGeom<D, FMT, PAIR>::THREADS, 1)
 chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                   const __grid_constant__ CUtensorMap mv, const CacheProblem p,
                   const CachePools pool, const ChunkArgs a, const TilePlan pl,
-                  float* __restrict__ part, long long* __restrict__ plan,
+                  float* __restrict__ part, SplitItem* __restrict__ split,
                   uint32_t* __restrict__ status) {
     using Gm = TileGeom<D, FMT, PAIR>;
     constexpr bool QUANT = Gm::QUANT;
@@ -207,24 +281,25 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
     if (tid == 0) {
         sm.abort_flag = 0;
         sm.never = 0;
+        sm.turn = 0;
         for (int i = 0; i < NST; ++i) {
-            tc::mbar_init(&sm.full[i], QUANT ? kConvWarps : 1);
-            tc::mbar_init(&sm.empty[i], 1);
+            tc::mbar_init(&sm.full[i], QUANT ? Gm::CW : 1);
+            tc::mbar_init(&sm.empty[i], 2);               // both issuers
         }
         for (int i = 0; i < NRAW; ++i) {
             tc::mbar_init(&sm.raw_full[i], 1);
-            tc::mbar_init(&sm.raw_empty[i], kConvWarps);
+            tc::mbar_init(&sm.raw_empty[i], QUANT ? Gm::CW : 1);
         }
         for (int i = 0; i < 2; ++i) {
             tc::mbar_init(&sm.q_full[i], 1);
-            tc::mbar_init(&sm.q_empty[i], 1);
+            tc::mbar_init(&sm.q_empty[i], 2);
             tc::mbar_init(&sm.s_full[i], 1);
             tc::mbar_init(&sm.p_full[i], 4);
             tc::mbar_init(&sm.o_done[i], 1);
         }
         tc::mbar_init(&sm.join_in, 8);
         tc::mbar_init(&sm.join_out, 8);
-        tc::mbar_init(&sm.mma_done, 1);
+        tc::mbar_init(&sm.mma_done, 2);
         tc::fence_mbar_init();
         tc::tma_prefetch_desc(&mq);
         if (!QUANT) {
@@ -275,23 +350,18 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
             }
         }
     }
-    if (blockIdx.x == 0) {             // the plan, for the merge kernel
-        long long at = base;
-        for (int s = s_lo; s < s_hi; ++s) {
-            plan[s] = at;
-            at += set_units(set_span(p, a, s), pl);
-        }
-        if (tid == 0) plan[p.S] = total;
-    }
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
     const uint32_t tmem = sm.tmem_base;
     volatile int* abort_flag = &sm.abort_flag;
-    TileWalk walk;
-    walk.init(p, a, count > 0 ? sm.start_s : 0, count > 0 ? sm.start_u : 0,
-              count > 0 ? sm.start_j : 0, count);
-    Seg g;
+    auto begin = [&](TileWalk& walk) {
+        walk.init(p, a, count > 0 ? sm.start_s : 0, count > 0 ? sm.start_u : 0,
+                  count > 0 ? sm.start_j : 0, count);
+    };
+
+    if (warp < kSoftWarp) {
+    regs_down<Gm::FEW_REGS>();
 
     // ------------------------------------------------------------ producer
     if (warp == 0) {
@@ -299,6 +369,9 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
         const uint32_t q_bytes = (uint32_t)(D / 64) * 128u * (uint32_t)(pl.tpt * p.G);
         int it = 0, ns = 0, nq[2] = {0, 0};
         bool ok = true;
+        TileWalk walk;
+        Seg g;
+        begin(walk);
         for (; ok && walk.next(p, a, pl, g); ++ns) {
             const int slot = ns % Gm::NQ;
             const int gk = g.s % p.H_kv, n = g.j1 - g.j0;
@@ -390,119 +463,143 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
             warp_wait(QUANT ? &sm.raw_full[i % N] : &sm.full[i % N], (i / N) & 1, &sm.never);
     }
 
-    // ------------------------------------------------------------ MMA issuer
-    if (warp == 1 && lane == 0) {
+    // ------------------------------------------------------------ rows that see nothing
+    // (the items without a key tile, which no CTA's share contains)
+    if (warp == 3) {
+        for (int s = blockIdx.x; s < p.S; s += gridDim.x) {
+            const SetSpan sp = set_span(p, a, s);
+            int none = 0;              // tokens of such items
+            if (sp.len < sp.n)
+                while (none < sp.n && tiles_seen(sp, none + pl.tpi) == 0) none += pl.tpi;
+            none = min(none, sp.n);
+            constexpr int U = D / 8;
+            for (long long e = lane; e < (long long)none * p.G * U; e += 32) {
+                const int row = (int)(e / U), t = row / p.G;
+                uint16_t* op = a.out + ((size_t)(sp.tok0 + t) * p.H_q + (s % p.H_kv) * p.G +
+                                        (row - t * p.G)) * D;
+                reinterpret_cast<uint4*>(op)[e % U] = make_uint4(0u, 0u, 0u, 0u);
+            }
+        }
+    }
+
+    // ------------------------------------------------------------ MMA issuers
+    // One warp per group: a single one is busy for longer than the products of
+    // both groups take.
+    if (warp == 1 || warp == 2) {
+        const int w = __shfl_sync(~0u, warp - 1, 0);
+        const uint32_t leader = elect_one();
+        const uint32_t tm = __shfl_sync(~0u, tmem, 0);
         const uint64_t qd0 = tc::sdesc_k_sw128(smem_u32(&sm.q[0][0]));
         const uint64_t kd0 = tc::sdesc_k_sw128(smem_u32(&sm.kv[0][0]));
         const uint64_t vd0 = tc::sdesc_mn_sw128(smem_u32(&sm.kv[0][0]), Gm::HALF);
+        const uint32_t q_lo = (uint32_t)qd0, k_lo = (uint32_t)kd0, v_lo = (uint32_t)vd0;
+        const uint32_t q_hi = (uint32_t)(qd0 >> 32), k_hi = (uint32_t)(kd0 >> 32),
+                       v_hi = (uint32_t)(vd0 >> 32);
         constexpr uint32_t QTILE = D * 2 * TM / 16, SLOT = Gm::TILE / 16, HALF16 = Gm::HALF / 16;
         constexpr uint32_t IDESC_QK = tc::idesc_bf16(TM, TN), IDESC_PV = tc::idesc_bf16_bmn(TM, D);
-        int base_it = 0, ns = 0, np[2] = {0, 0};
+        const uint32_t ts = tm + (uint32_t)(w * TN), to = tm + kOCol + (uint32_t)(w * D);
+        int st = 0, ph = 0, ns = 0, np = 0;      // ring slot and its phase
         bool ok = true;
         auto wait = [&](uint64_t* bar, uint32_t parity) {
-            if (ok && !tc::mbar_wait(bar, parity, abort_flag)) ok = false;
+            if (ok && !warp_wait(bar, parity, abort_flag)) ok = false;
             if (ok) tc::fence_after_sync();
             return ok;
         };
-        // S_w = Q_w K^T with the K tile at ring place i
-        auto qk = [&](int w, int slot, int i) {
-            const uint64_t qd = qd0 + (uint64_t)((slot * Gm::QT + (PAIR ? w : 0)) * QTILE);
-            const uint64_t kd = kd0 + (uint64_t)((i % NST) * SLOT);
+        // S = Q K^T with the K tile in ring slot st; then the slot is free, and so is Q
+        // after its last tile
+        auto qk = [&](int slot, bool last) {
+            const uint32_t qa = q_lo + (uint32_t)(slot * Gm::QT + (PAIR ? w : 0)) * QTILE;
+            const uint32_t ka = k_lo + (uint32_t)st * SLOT;
+            if (leader) {
 #pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) {
-                const uint64_t off = (uint64_t)((kk >> 2) * HALF16 + (kk & 3) * 2);
-                tc::mma_bf16(tmem + (uint32_t)(w * TN), qd + off, kd + off, IDESC_QK, kk > 0 ? 1u : 0u);
+                for (int kk = 0; kk < D / 16; ++kk) {
+                    const uint32_t off = (kk >> 2) * HALF16 + (kk & 3) * 2;
+                    mma_ss(ts, qa + off, ka + off, q_hi, k_hi, IDESC_QK, kk > 0 ? 1u : 0u);
+                }
+                tc::mma_commit(&sm.s_full[w]);
+                tc::mma_commit(&sm.empty[st]);
+                if (last) tc::mma_commit(&sm.q_empty[slot]);
             }
-            tc::mma_commit(&sm.s_full[w]);
+            __syncwarp();
         };
-        // O_w (+)= P_w V with the V tile at ring place i
-        auto pv = [&](int w, int i, bool accumulate) {
-            const uint64_t vd = vd0 + (uint64_t)((i % NST) * SLOT);
+        // O (+)= P V with the V tile in ring slot st
+        auto pv = [&](bool accumulate, bool last) {
+            const uint32_t va = v_lo + (uint32_t)st * SLOT;
+            if (leader) {
+                mma_ts(to, ts, va, v_hi, IDESC_PV, accumulate ? 1u : 0u);
 #pragma unroll
-            for (int kk = 0; kk < TN / 16; ++kk)
-                mma_bf16_ta(tmem + kOCol + (uint32_t)(w * D), tmem + (uint32_t)(w * TN + kk * 8),
-                            vd + (uint64_t)(kk * (16 * 128 / 16)), IDESC_PV,
-                            (accumulate || kk > 0) ? 1u : 0u);
+                for (int kk = 1; kk < TN / 16; ++kk)
+                    mma_ts(to, ts + (uint32_t)(kk * 8), va + (uint32_t)(kk * (16 * 128 / 16)), v_hi,
+                           IDESC_PV, 1u);
+                tc::mma_commit(&sm.empty[st]);
+                if (last) tc::mma_commit(&sm.o_done[w]);
+            }
+            __syncwarp();
         };
-        for (; ok && walk.next(p, a, pl, g); ++ns) {
-            const int slot = ns % Gm::NQ, n = g.j1 - g.j0;
-            // tiles of each group in this segment
-            int hi[2];
-            for (int w = 0; w < 2; ++w)
-                hi[w] = PAIR ? min(group_tiles<PAIR>(g, pl, w), g.j1) - g.j0 : n;
+        TileWalk walk;
+        Seg g;
+        begin(walk);
+        for (; ok; ++ns) {
+            const int more = walk.next(p, a, pl, g);
+            if (!__shfl_sync(~0u, more, 0)) break;
+            const int slot = ns % Gm::NQ, n = __shfl_sync(~0u, g.j1 - g.j0, 0);
+            // the group's tiles: x < hi (PAIR), or every second one from w on
+            const int hi = __shfl_sync(
+                ~0u, PAIR ? min(group_tiles<PAIR>(g, pl, w), g.j1) - g.j0 : n, 0);
+            const int x0 = PAIR ? 0 : w, step = PAIR ? 1 : 2;        // its tiles: x0, x0 + step ..
             if (!wait(&sm.q_full[slot], (ns / Gm::NQ) & 1)) break;
-            auto full = [&](int i) { return wait(&sm.full[i % NST], (i / NST) & 1); };
-            if (PAIR) {
-                if (!full(base_it + k_place<PAIR>(0))) break;
-                for (int w = 0; w < 2; ++w)
-                    if (0 < hi[w]) qk(w, slot, base_it);
-                tc::mma_commit(&sm.empty[base_it % NST]);
-                if (n == 1) tc::mma_commit(&sm.q_empty[slot]);
-                for (int x = 0; ok && x < n; ++x) {
-                    const int vi = base_it + v_place<PAIR>(x, n), ki = base_it + k_place<PAIR>(x + 1);
-                    bool v_in = false, k_in = false;
-                    for (int w = 0; ok && w < 2; ++w) {
-                        if (x >= hi[w]) continue;
-                        if (!wait(&sm.p_full[w], np[w]++ & 1)) break;
-                        if (!v_in && !full(vi)) break;
-                        v_in = true;
-                        pv(w, vi, x > 0);
-                        if (x + 1 < hi[w]) {
-                            if (!k_in && !full(ki)) break;
-                            k_in = true;
-                            qk(w, slot, ki);
-                        } else {
-                            tc::mma_commit(&sm.o_done[w]);
-                        }
-                    }
-                    if (!ok) break;
-                    // a tile that neither group uses is still waited for: its slot is reused
-                    if (!v_in && !full(vi)) break;
-                    tc::mma_commit(&sm.empty[vi % NST]);
-                    if (x + 1 < n) {
-                        if (!k_in && !full(ki)) break;
-                        tc::mma_commit(&sm.empty[ki % NST]);
-                        if (x + 2 == n) tc::mma_commit(&sm.q_empty[slot]);
-                    }
-                }
-            } else {
-                for (int x = 0; ok && x < min(n, 2); ++x) {
-                    const int ki = base_it + k_place<PAIR>(x);
-                    if (!full(ki)) break;
-                    qk(x, slot, ki);
-                    tc::mma_commit(&sm.empty[ki % NST]);
-                    if (x + 1 == n) tc::mma_commit(&sm.q_empty[slot]);
-                }
-                for (int x = 0; ok && x < n; ++x) {
-                    const int w = x & 1, vi = base_it + v_place<PAIR>(x, n);
-                    if (!wait(&sm.p_full[w], np[w]++ & 1) || !full(vi)) break;
-                    pv(w, vi, x > 1);
-                    tc::mma_commit(&sm.empty[vi % NST]);
-                    if (x + 2 < n) {
-                        const int ki = base_it + k_place<PAIR>(x + 2);
-                        if (!full(ki)) break;
-                        qk(w, slot, ki);
-                        tc::mma_commit(&sm.empty[ki % NST]);
-                        if (x + 3 == n) tc::mma_commit(&sm.q_empty[slot]);
-                    }
-                }
-                if (!ok) break;
-                tc::mma_commit(&sm.o_done[0]);
-                tc::mma_commit(&sm.o_done[1]);
+            if (x0 >= hi && leader) tc::mma_commit(&sm.q_empty[slot]);   // no use of Q
+            __syncwarp();
+            // Both issuers take every slot of the ring in its order and release it, their
+            // own tiles' or not: one that skipped slots could come to wait for a fill two
+            // ahead of the last, which a parity cannot tell from the one before.
+            auto k_slot = [&](int x) {
+                if (x < hi && (PAIR || (x & 1) == w)) qk(slot, x + step >= hi);
+                else if (leader) tc::mma_commit(&sm.empty[st]);
+                if (++st == NST) st = 0, ph ^= 1;
+            };
+            const int pre = PAIR ? 1 : min(n, 2);                    // K tiles before the first V
+            for (int x = 0; x < pre; ++x) {
+                if (!wait(&sm.full[st], ph)) break;
+                k_slot(x);
             }
-            base_it += 2 * n;
+            // then V of tile x, and K of the same group's next tile
+            for (int x = 0; ok && x < n; ++x) {
+                const int kx = x + step;
+                const bool own = x < hi && (PAIR || (x & 1) == w);
+                if (own && !wait(&sm.p_full[w], np++ & 1)) break;
+                if (!wait(&sm.full[st], ph)) break;
+                const int kst = st + 1 == NST ? 0 : st + 1;
+                if (own && kx < hi && !wait(&sm.full[kst], kst ? ph : ph ^ 1)) break;
+                // P V and the next Q K^T go in one run: were the two groups' products to
+                // alternate, both would end late, and the groups fall into step instead of
+                // using the tensor cores in turn
+                if (own && !(ok = take_turn(&sm.turn, lane, abort_flag))) break;
+                if (own) pv(x > x0, kx >= hi);
+                else if (leader) tc::mma_commit(&sm.empty[st]);
+                if (++st == NST) st = 0, ph ^= 1;
+                if (kx < n && !(own && kx < hi) && !wait(&sm.full[st], ph)) {
+                    if (own) end_turn(&sm.turn, lane);
+                    break;
+                }
+                if (kx < n) k_slot(kx);
+                if (own) end_turn(&sm.turn, lane);
+            }
         }
-        if (!ok) {
+        if (!ok && lane == 0) {
             sm.abort_flag = 1;
             raise_status(status, TGVKV_STATUS_TIMEOUT);
         }
+        __syncwarp();
         // every MMA this CTA issued has finished before TMEM is released
-        tc::mma_commit(&sm.mma_done);
-        tc::mbar_wait(&sm.mma_done, 0, &sm.never);
+        if (leader) tc::mma_commit(&sm.mma_done);
+        __syncwarp();
+        warp_wait(&sm.mma_done, 0, &sm.never);
     }
 
-    // ------------------------------------------------------------ softmax
-    if (warp >= kSoftWarp && warp < kConvWarp) {
+    } else if (warp < kConvWarp) {
+        // -------------------------------------------------------- softmax
+        regs_up<Gm::SOFT_REGS>();
         const int w = (warp - kSoftWarp) >> 2;               // group
         const int quarter = warp & 3;                        // TMEM lanes of this warp
         const int r = quarter * 32 + lane;                   // row of the tile
@@ -510,18 +607,28 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
         const uint32_t ts = lanes + (uint32_t)(w * TN), to = lanes + kOCol + (uint32_t)(w * D);
         const float sl2 = p.scale_log2;
         const int ri = r / p.G, rh = r - ri * p.G;           // token within the tile, head
-        constexpr int CB = 64;                               // S columns held at a time
+        constexpr int CB = Gm::S_COLS;
         int ns = 0, nso = 0, npart = 0, base_it = 0;
         bool ok = true;
-        for (; ok && walk.next(p, a, pl, g); ++npart) {
-            const int n = g.j1 - g.j0;
-            const int tok = g.tok0 + (PAIR ? w * pl.tpt : 0);        // the tile's first token
-            const int hi = PAIR ? min(group_tiles<PAIR>(g, pl, w), g.j1) - g.j0 : n;
-            const int toks = min(g.sp.n - tok, pl.tpt);              // its tokens (<= 0: none)
+        if (warp == kSoftWarp && lane == 0) split[blockIdx.x] = SplitItem{-1, 0, 0, 0};
+        auto& at = sm.at[warp - kSoftWarp];
+        const volatile Seg& g = at.g;
+        if (lane == 0) begin(at.walk);
+        for (; ok; ++npart) {
+            __syncwarp();
+            int more = 0;
+            if (lane == 0) more = at.walk.next(p, a, pl, at.g);
+            if (!__shfl_sync(~0u, more, 0)) break;
+            const int n = g.j1 - g.j0, j0 = g.j0, len = g.sp.len;
+            const int nt = g.sp.n, tok = g.tok0 + (PAIR ? w * pl.tpt : 0);   // the tile's first token
+            const SetSpan span{len, nt, 0};
+            const int seen_tiles = !PAIR ? 0 : tok < nt ? tiles_seen(span, tok + pl.tpt) : 0;
+            const int hi = PAIR ? min(seen_tiles, j0 + n) - j0 : n;
+            const int toks = min(nt - tok, pl.tpt);                  // its tokens (<= 0: none)
             const bool valid = ri < toks;
             const bool warp_on = quarter * 32 < toks * p.G;          // some row of the warp is real
             // slots that this row sees: its own and those before
-            const int lim = min(g.sp.len - g.sp.n + min(tok + ri, g.sp.n - 1) + 1, g.sp.len);
+            const int lim = min(len - nt + min(tok + ri, nt - 1) + 1, len);
             float m = -INFINITY, l = 0.f;
             for (int x = PAIR ? 0 : w; x < hi; x += PAIR ? 1 : 2) {
                 if (!warp_wait(&sm.s_full[w], ns & 1, abort_flag)) {
@@ -530,7 +637,7 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
                 }
                 ++ns;
                 tc::fence_after_sync();
-                const int j = g.j0 + x;
+                const int j = j0 + x;
                 const int seen = lim - j * TN;               // columns seen of this tile
                 const bool masked = __any_sync(~0u, seen < TN);
                 if (warp_on) {
@@ -573,13 +680,14 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
                     // O holds the tiles before this one (the commit of S covers P V before it)
                     if (x > (PAIR ? 0 : 1) && __any_sync(~0u, alpha != 1.f)) {
 #pragma unroll
-                        for (int c = 0; c < D / 32; ++c) {
-                            float t[32];
-                            tc::tmem_ld32(to + (uint32_t)(32 * c), t);
+                        for (int c = 0; c < D / 16; ++c) {   // in pieces: S is in registers
+                            uint32_t t[16];
+                            tmem_ld16(to + (uint32_t)(16 * c), t);
                             tc::tmem_wait_ld();
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) t[e] *= alpha;
-                            tc::tmem_st32(to + (uint32_t)(32 * c), t);
+                            for (int e = 0; e < 16; ++e)
+                                t[e] = __float_as_uint(__uint_as_float(t[e]) * alpha);
+                            tmem_st16(to + (uint32_t)(16 * c), t);
                         }
                     }
                     const float2 s2 = make_float2(sl2, sl2), n2 = make_float2(-ref, -ref);
@@ -610,7 +718,7 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
                 // bf16 caches: the pool's rows past the set's end may hold anything, and
                 // 0 x NaN is not 0, so V's rows there are cleared (the converters do it
                 // for integer caches)
-                const int live = g.sp.len - j * TN;
+                const int live = len - j * TN;
                 if (!QUANT && live < TN) {
                     const int vi = base_it + v_place<PAIR>(x, n);
                     if (!warp_wait(&sm.full[vi % NST], (vi / NST) & 1, abort_flag)) {
@@ -634,6 +742,11 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
 
             // ---- the segment's end: a whole item is written out, a part kept for the merge
             const bool whole = g.j0 == 0 && g.j1 == g.nk;
+            if (warp == kSoftWarp && lane == 0 && g.j0 == 0 && !whole) {
+                // an item that begins here and goes on in the next CTAs
+                const int rest = g.nk - g.j1;
+                split[blockIdx.x] = SplitItem{g.s, g.u, 2 + (int)((rest - 1) / per), g.starts ? 0 : 1};
+            }
             const size_t rec = (size_t)((blockIdx.x * 2 + (g.starts ? 0 : 1)) * (PAIR ? 2 : 1) + (PAIR ? w : 0));
             float* pp = part + rec * chunk_record_floats(pl.rows, D);
             uint16_t* op = a.out + ((size_t)(g.sp.tok0 + (valid ? tok + ri : 0)) * p.H_q +
@@ -684,12 +797,14 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
                 sm.ml[w][r] = make_float2(m, l);
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(&sm.join_in);
+                // (group 1 has no tile, and no O, in a segment of one)
                 if (!warp_wait(&sm.o_done[0], npart & 1, abort_flag) ||
-                    !warp_wait(&sm.o_done[1], npart & 1, abort_flag) ||
+                    (n > 1 && !warp_wait(&sm.o_done[1], nso & 1, abort_flag)) ||
                     !warp_wait(&sm.join_in, npart & 1, abort_flag)) {
                     ok = false;
                     break;
                 }
+                if (n > 1) ++nso;
                 tc::fence_after_sync();
                 const float2 a0 = sm.ml[0][r], a1 = sm.ml[PAIR ? 0 : 1][r];
                 const float M = fmaxf(a0.x, a1.x), ref = M == -INFINITY ? 0.f : M;
@@ -751,13 +866,15 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
             sm.abort_flag = 1;
             if (lane == 0) raise_status(status, TGVKV_STATUS_TIMEOUT);
         }
-    }
-
-    // ------------------------------------------------------------ converters
-    if (QUANT && warp >= kConvWarp) {
+    } else if (QUANT) {
+        // -------------------------------------------------------- converters
+        regs_down<Gm::CONV_REGS>();
         const int ct = tid - kConvWarp * 32;
         int it = 0;
         bool ok = true;
+        TileWalk walk;
+        Seg g;
+        begin(walk);
         while (ok && walk.next(p, a, pl, g)) {
             const int n = g.j1 - g.j0;
             int kx = 0, vx = 0;
@@ -775,7 +892,7 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
                 const unsigned char* raw = sm.raw[rs];
                 unsigned char* dst = sm.kv[st];
 #pragma unroll 4
-                for (int e = ct; e < UNITS; e += kConvWarps * 32) {
+                for (int e = ct; e < UNITS; e += Gm::CW * 32) {
                     const int row = e / (D / 8), u = e % (D / 8);
                     uint2 c = make_uint2(0u, 0u);
                     if (FMT == TGVKV_CACHE_INT8) c = reinterpret_cast<const uint2*>(raw)[e];
@@ -812,7 +929,7 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
 
 template <int D, int FMT, bool PAIR>
 cudaError_t launch_tile(const CacheProblem& p, const CachePools& pool, const ChunkArgs& a,
-                        float* part, long long* plan, uint32_t* status, cudaStream_t stream) {
+                        float* part, SplitItem* split, uint32_t* status, cudaStream_t stream) {
     using Sm = TileSmem<D, FMT, PAIR>;
     static_assert(sizeof(Sm) + 1024 <= 227 * 1024, "shared memory of one CTA");
     TilePlan pl;
@@ -831,13 +948,17 @@ cudaError_t launch_tile(const CacheProblem& p, const CachePools& pool, const Chu
     cudaError_t e = cudaFuncSetAttribute(chunk_tile_kernel<D, FMT, PAIR>,
                                          cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
+    // the register split needs what the launch bounds ask the compiler for
+    cudaFuncAttributes at;
+    if ((e = cudaFuncGetAttributes(&at, chunk_tile_kernel<D, FMT, PAIR>)) != cudaSuccess) return e;
+    if (at.numRegs < TileGeom<D, FMT, PAIR>::LAUNCH_REGS) return cudaErrorInvalidConfiguration;
     const int sms = device_sm_count();
     if (sms <= 0) return cudaErrorInvalidDevice;
     const int ctas = sms < kTileMaxCtas ? sms : kTileMaxCtas;
     chunk_tile_kernel<D, FMT, PAIR><<<ctas, TileGeom<D, FMT, PAIR>::THREADS, smem, stream>>>(
-        mq, mk, mv, p, pool, a, pl, part, plan, status);
+        mq, mk, mv, p, pool, a, pl, part, split, status);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    return launch_tile_merge(p, a, pl, ctas, part, plan, stream);
+    return launch_tile_merge(p, a, pl, ctas, part, split, stream);
 }
 
 }  // namespace tgvkv

@@ -4,14 +4,14 @@
 namespace tgvkv {
 
 cudaError_t launch_tile_bf16(const CacheProblem& p, const CachePools& pool, const ChunkArgs& a,
-                             float* part, long long* plan, bool pair, uint32_t* status,
+                             float* part, SplitItem* split, bool pair, uint32_t* status,
                              cudaStream_t stream) {
     constexpr int F = TGVKV_CACHE_BF16;
     if (p.d == 64)
-        return pair ? launch_tile<64, F, true>(p, pool, a, part, plan, status, stream)
-                    : launch_tile<64, F, false>(p, pool, a, part, plan, status, stream);
-    return pair ? launch_tile<128, F, true>(p, pool, a, part, plan, status, stream)
-                : launch_tile<128, F, false>(p, pool, a, part, plan, status, stream);
+        return pair ? launch_tile<64, F, true>(p, pool, a, part, split, status, stream)
+                    : launch_tile<64, F, false>(p, pool, a, part, split, status, stream);
+    return pair ? launch_tile<128, F, true>(p, pool, a, part, split, status, stream)
+                : launch_tile<128, F, false>(p, pool, a, part, split, status, stream);
 }
 
 }  // namespace tgvkv

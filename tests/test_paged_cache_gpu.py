@@ -324,6 +324,23 @@ def test_chunks(api, fmt, d, H_q, H_kv, page):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,longest", [(2, 300), (6, 1500)])
+def test_one_row_tile_per_set(api, fmt, d, B, longest):
+    """Chunks of one row tile (more than 16 query rows): a few key tiles in all, so
+    that a CTA gets one or none, then shares of several sets, parts of sets and
+    single tiles in one CTA."""
+    H = 16
+    box = Box(api, B, H, H, d, 64, fmt, longest)
+    lens = [1 + (s * 7919) % longest for s in range(B * H)]
+    box.fill(lens)
+    news = [(96, 17, 128, 1, 40, 0)[b % 6] for b in range(B)]
+    for _ in range(3):                           # back to back, no wait in between
+        q, got = box.attend(news)
+    box.check(news, q, got)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
 def test_long_sets_split_over_the_whole_gpu(api, fmt):
     """Few sets, long caches: every set is split over many streams and joined."""
     box = Box(api, 1, 4, 2, 128, 64, fmt, 9001)
