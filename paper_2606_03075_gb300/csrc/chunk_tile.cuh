@@ -866,10 +866,17 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
             sm.abort_flag = 1;
             if (lane == 0) raise_status(status, TGVKV_STATUS_TIMEOUT);
         }
-    } else if (QUANT) {
+    } else if constexpr (QUANT) {
         // -------------------------------------------------------- converters
         regs_down<Gm::CONV_REGS>();
-        const int ct = tid - kConvWarp * 32;
+        // A thread converts 8 consecutive values of every RSTEP-th row; RSTEP is a
+        // multiple of 8, so the swizzle is the same in all of them.
+        constexpr int T = Gm::CW * 32, UPR = D / 8, RSTEP = T / UPR, PER = TN / RSTEP;
+        constexpr int BATCH = PER < 8 ? PER : 8;
+        static_assert(RSTEP % 8 == 0 && PER % BATCH == 0, "converter threads");
+        const int ct = tid - kConvWarp * 32, u = ct % UPR, r0 = ct / UPR;
+        const int src = ct * (FMT == TGVKV_CACHE_INT8 ? 8 : 4), sc0 = r0 * (D / kGroup) + (u >> 2);
+        const int dst0 = (u >> 3) * Gm::HALF + r0 * 128 + (((u & 7) ^ (r0 & 7)) << 4);
         int it = 0;
         bool ok = true;
         TileWalk walk;
@@ -888,20 +895,31 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
                     ok = false;
                     break;
                 }
-                constexpr int UNITS = TN * (D / 8);          // 8 values each
-                const unsigned char* raw = sm.raw[rs];
-                unsigned char* dst = sm.kv[st];
-#pragma unroll 4
-                for (int e = ct; e < UNITS; e += Gm::CW * 32) {
-                    const int row = e / (D / 8), u = e % (D / 8);
-                    uint2 c = make_uint2(0u, 0u);
-                    if (FMT == TGVKV_CACHE_INT8) c = reinterpret_cast<const uint2*>(raw)[e];
-                    else c.x = reinterpret_cast<const uint32_t*>(raw)[e];
-                    uint4 v = codes_to_bf16<FMT>(c, sm.sc[rs][row * (D / kGroup) + (u >> 2)],
-                                                 p.magic);
-                    if (row >= live) v = make_uint4(0u, 0u, 0u, 0u);   // past the set's end
-                    *reinterpret_cast<uint4*>(dst + (u >> 3) * Gm::HALF + row * 128 +
-                                              (((u & 7) ^ (row & 7)) << 4)) = v;
+                const unsigned char* raw = sm.raw[rs] + src;
+                const unsigned char* sc = sm.sc[rs] + sc0;
+                unsigned char* dst = sm.kv[st] + dst0;
+#pragma unroll
+                for (int b0 = 0; b0 < PER; b0 += BATCH) {
+                    // a batch's loads before its stores: they cannot pass one another
+                    uint2 c[BATCH];
+                    uint32_t byte[BATCH];
+#pragma unroll
+                    for (int b = 0; b < BATCH; ++b) {
+                        const int e = b0 + b;
+                        c[b] = make_uint2(0u, 0u);
+                        if (FMT == TGVKV_CACHE_INT8)
+                            c[b] = *reinterpret_cast<const uint2*>(raw + e * T * 8);
+                        else
+                            c[b].x = *reinterpret_cast<const uint32_t*>(raw + e * T * 4);
+                        byte[b] = sc[e * RSTEP * (D / kGroup)];
+                    }
+#pragma unroll
+                    for (int b = 0; b < BATCH; ++b) {
+                        uint4 v = codes_to_bf16<FMT>(c[b], byte[b], p.magic);
+                        // past the set's end
+                        if (live < TN && r0 + (b0 + b) * RSTEP >= live) v = make_uint4(0u, 0u, 0u, 0u);
+                        *reinterpret_cast<uint4*>(dst + (b0 + b) * RSTEP * 128) = v;
+                    }
                 }
                 tc::fence_proxy_async_smem();
                 __syncwarp();
