@@ -18,19 +18,22 @@
 // that spans several CTAs leaves one partial (m, l, O) per CTA and row tile,
 // merged by a second kernel in CTA order.
 //
-// Tensor memory: S0, S1 (128 columns each), O0, O1 (D columns each).  P
-// (bf16) overwrites the first 64 columns of its S and is the A operand of P V
-// from there; K is the K-major and V the MN-major B operand from shared memory.
-// MMA order of one group: ... P V (j), Q K^T (j + 1) ..., the commit after Q K^T
-// covers both, so a softmax group that sees S (j + 1) knows that O holds j.
+// Tensor memory: one S (128 columns), P0, P1 (64 columns each: 128 bf16), O0, O1
+// (D columns each).  A softmax thread takes its row of S into registers and frees
+// the columns at once, so the groups share S: the tensor cores run P V of one
+// group while the other reads, and Q K^T never waits for an exponential.  The
+// products are issued in one order,
+//   ... P0 V (j), Q0 K (j + 1), P1 V (j), Q1 K (j + 1) ...
+// so that a group's S (j + 1) tells that its O holds tile j.  P is the A operand
+// from tensor memory; K is the K-major and V the MN-major B operand from shared
+// memory.
 //
-// Integer caches: TMA brings the codes of a key tile, eight converter warps
+// Integer caches: TMA brings the codes of a key tile, four converter warps
 // write them as bf16 in the swizzled layout (exact: scales are powers of two),
 // and the rest is the bf16 kernel.
 //
-// Roles: warp 0 TMA, warps 1 and 2 MMA issue, one per group (1 also owns the
-// TMEM), warp 3 rows without work, warps 4-11 softmax, warps 12
-// on converters (integer caches).  Registers are split by role (setmaxnreg), so
+// Roles: warp 0 TMA, warp 1 MMA issue (and TMEM), warp 3 rows without work,
+// warps 4-11 softmax, warps 12-15 converters (integer caches).  Registers are split by role (setmaxnreg), so
 // that a softmax thread holds a whole row of S.  Every wait is bounded; a timeout sets
 // TGVKV_STATUS_TIMEOUT and the CTA unwinds after its copies and MMAs finished.
 #pragma once
@@ -43,7 +46,7 @@ namespace tgvkv {
 
 constexpr int kSoftWarp = 4;           // first softmax warp
 constexpr int kConvWarp = 12;          // first converter warp
-constexpr uint32_t kOCol = 256;        // first O column; S at 0 and 128
+constexpr uint32_t kPCol = 128, kOCol = 256;   // first P and O columns; S at 0
 constexpr float kRescale = 8.f;        // a stale maximum may trail by 2^8
 
 // The issuing warps run as a whole, so that addresses stay in uniform registers;
@@ -129,17 +132,13 @@ struct TileGeom {
     static constexpr int NRAW = QUANT ? (FMT == TGVKV_CACHE_INT8 ? 3 : 6) : 0;
     static constexpr int NQ = PAIR ? 1 : 2;                       // Q slots
     static constexpr int QT = PAIR ? 2 : 1;                       // row tiles a slot
-    // converters: SPLIT calls wait for memory and softmax has few rows, PAIR calls
-    // need the registers for softmax
-    static constexpr int CW = !QUANT ? 0 : PAIR ? 4 : 8;
+    static constexpr int CW = QUANT ? 4 : 0;                      // converter warps
     static constexpr int THREADS = 32 * (kConvWarp + CW);
     // registers a thread: at launch (the most that the thread count allows), then by
     // role.  The roles' sum is at most the launch's: what setmaxnreg raises one by has
     // to come from the others.
-    static constexpr int LAUNCH_REGS = CW == 0 ? 168 : CW == 4 ? 128 : 96;
-    static constexpr int FEW_REGS = 72, CONV_REGS = CW == 4 ? 80 : 64;
-    static constexpr int SOFT_REGS = CW == 0 ? 208 : CW == 4 ? 176 : 136;
-    static constexpr int S_COLS = CW == 8 ? 64 : 128;   // S columns a thread holds at a time
+    static constexpr int LAUNCH_REGS = QUANT ? 128 : 168;
+    static constexpr int FEW_REGS = 72, CONV_REGS = 80, SOFT_REGS = QUANT ? 176 : 208;
     static_assert(128 * FEW_REGS + 256 * SOFT_REGS + 32 * CW * CONV_REGS <= THREADS * LAUNCH_REGS,
                   "register split");
 };
@@ -213,7 +212,7 @@ struct TileSmem {
     unsigned char sc[Gm::QUANT ? Gm::NRAW : 1][Gm::QUANT ? Gm::SC : 16];
     uint64_t full[Gm::NST], empty[Gm::NST];
     uint64_t raw_full[Gm::QUANT ? Gm::NRAW : 1], raw_empty[Gm::QUANT ? Gm::NRAW : 1];
-    uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_done[2];
+    uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_done[2], s_free;
     uint64_t join_in, join_out, mma_done;
     float2 ml[PAIR ? 1 : 2][PAIR ? 1 : TM];           // SPLIT: the groups' (m, l)
     struct {                                          // a softmax warp's place in the work:
@@ -221,7 +220,7 @@ struct TileSmem {
         Seg g;
     } at[8];
     uint32_t tmem_base;
-    int abort_flag, never, turn;
+    int abort_flag, never;
     long long warp_sum[Gm::THREADS / 32];
     int start_s, start_u, start_j;
 };
@@ -246,21 +245,6 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volati
     return __all_sync(~0u, tc::mbar_wait(bar, parity, abort));
 }
 
-// A turn of issuing, for two warps; the wait is bounded like those on mbarriers.
-__device__ __forceinline__ bool take_turn(int* turn, int lane, volatile int* abort) {
-    int got = 1;
-    if (lane == 0) {
-        const long long c0 = clock64();
-        while ((got = atomicExch(turn, 1) == 0) == 0)
-            if (*abort || clock64() - c0 > tc::kWaitLimitCycles) break;
-    }
-    return __shfl_sync(~0u, got, 0) != 0;
-}
-__device__ __forceinline__ void end_turn(int* turn, int lane) {
-    __syncwarp();
-    if (lane == 0) atomicExch(turn, 0);
-}
-
 template <int D, int FMT, bool PAIR>
 __global__ void __launch_bounds__(TileGeom<D, FMT, PAIR>::THREADS, 1)
 chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
@@ -281,10 +265,9 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
     if (tid == 0) {
         sm.abort_flag = 0;
         sm.never = 0;
-        sm.turn = 0;
         for (int i = 0; i < NST; ++i) {
             tc::mbar_init(&sm.full[i], QUANT ? Gm::CW : 1);
-            tc::mbar_init(&sm.empty[i], 2);               // both issuers
+            tc::mbar_init(&sm.empty[i], 1);
         }
         for (int i = 0; i < NRAW; ++i) {
             tc::mbar_init(&sm.raw_full[i], 1);
@@ -292,14 +275,15 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
         }
         for (int i = 0; i < 2; ++i) {
             tc::mbar_init(&sm.q_full[i], 1);
-            tc::mbar_init(&sm.q_empty[i], 2);
+            tc::mbar_init(&sm.q_empty[i], 1);
             tc::mbar_init(&sm.s_full[i], 1);
             tc::mbar_init(&sm.p_full[i], 4);
             tc::mbar_init(&sm.o_done[i], 1);
         }
         tc::mbar_init(&sm.join_in, 8);
         tc::mbar_init(&sm.join_out, 8);
-        tc::mbar_init(&sm.mma_done, 2);
+        tc::mbar_init(&sm.s_free, 4);
+        tc::mbar_init(&sm.mma_done, 1);
         tc::fence_mbar_init();
         tc::tma_prefetch_desc(&mq);
         if (!QUANT) {
@@ -482,11 +466,8 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
         }
     }
 
-    // ------------------------------------------------------------ MMA issuers
-    // One warp per group: a single one is busy for longer than the products of
-    // both groups take.
-    if (warp == 1 || warp == 2) {
-        const int w = __shfl_sync(~0u, warp - 1, 0);
+    // ------------------------------------------------------------ MMA issuer
+    if (warp == 1) {
         const uint32_t leader = elect_one();
         const uint32_t tm = __shfl_sync(~0u, tmem, 0);
         const uint64_t qd0 = tc::sdesc_k_sw128(smem_u32(&sm.q[0][0]));
@@ -497,43 +478,48 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
                        v_hi = (uint32_t)(vd0 >> 32);
         constexpr uint32_t QTILE = D * 2 * TM / 16, SLOT = Gm::TILE / 16, HALF16 = Gm::HALF / 16;
         constexpr uint32_t IDESC_QK = tc::idesc_bf16(TM, TN), IDESC_PV = tc::idesc_bf16_bmn(TM, D);
-        const uint32_t ts = tm + (uint32_t)(w * TN), to = tm + kOCol + (uint32_t)(w * D);
-        int st = 0, ph = 0, ns = 0, np = 0;      // ring slot and its phase
+        int st = 0, ph = 0;                      // next slot of the ring, and its phase
+        int ns = 0, nqk = 0, np[2] = {0, 0};
         bool ok = true;
         auto wait = [&](uint64_t* bar, uint32_t parity) {
             if (ok && !warp_wait(bar, parity, abort_flag)) ok = false;
             if (ok) tc::fence_after_sync();
             return ok;
         };
-        // S = Q K^T with the K tile in ring slot st; then the slot is free, and so is Q
-        // after its last tile
-        auto qk = [&](int slot, bool last) {
-            const uint32_t qa = q_lo + (uint32_t)(slot * Gm::QT + (PAIR ? w : 0)) * QTILE;
-            const uint32_t ka = k_lo + (uint32_t)st * SLOT;
+        auto slot_after = [&](int x) { return x + 1 == NST ? 0 : x + 1; };
+        // S = Q_w K^T with the K tile in slot k, once S has been read
+        auto qk = [&](int w, int qslot, int k) {
+            if (nqk > 0 && !wait(&sm.s_free, (nqk - 1) & 1)) return;
+            ++nqk;
+            const uint32_t qa = q_lo + (uint32_t)(qslot * Gm::QT + (PAIR ? w : 0)) * QTILE;
+            const uint32_t ka = k_lo + (uint32_t)k * SLOT;
             if (leader) {
 #pragma unroll
                 for (int kk = 0; kk < D / 16; ++kk) {
                     const uint32_t off = (kk >> 2) * HALF16 + (kk & 3) * 2;
-                    mma_ss(ts, qa + off, ka + off, q_hi, k_hi, IDESC_QK, kk > 0 ? 1u : 0u);
+                    mma_ss(tm, qa + off, ka + off, q_hi, k_hi, IDESC_QK, kk > 0 ? 1u : 0u);
                 }
                 tc::mma_commit(&sm.s_full[w]);
-                tc::mma_commit(&sm.empty[st]);
-                if (last) tc::mma_commit(&sm.q_empty[slot]);
             }
             __syncwarp();
         };
-        // O (+)= P V with the V tile in ring slot st
-        auto pv = [&](bool accumulate, bool last) {
-            const uint32_t va = v_lo + (uint32_t)st * SLOT;
+        // O_w (+)= P_w V with the V tile in slot v, once P_w is there
+        auto pv = [&](int w, int v, bool accumulate, bool last) {
+            if (!wait(&sm.p_full[w], np[w]++ & 1)) return;
+            const uint32_t va = v_lo + (uint32_t)v * SLOT;
+            const uint32_t to = tm + kOCol + (uint32_t)(w * D), tp = tm + kPCol + (uint32_t)(w * 64);
             if (leader) {
-                mma_ts(to, ts, va, v_hi, IDESC_PV, accumulate ? 1u : 0u);
+                mma_ts(to, tp, va, v_hi, IDESC_PV, accumulate ? 1u : 0u);
 #pragma unroll
                 for (int kk = 1; kk < TN / 16; ++kk)
-                    mma_ts(to, ts + (uint32_t)(kk * 8), va + (uint32_t)(kk * (16 * 128 / 16)), v_hi,
+                    mma_ts(to, tp + (uint32_t)(kk * 8), va + (uint32_t)(kk * (16 * 128 / 16)), v_hi,
                            IDESC_PV, 1u);
-                tc::mma_commit(&sm.empty[st]);
                 if (last) tc::mma_commit(&sm.o_done[w]);
             }
+            __syncwarp();
+        };
+        auto release = [&](uint64_t* bar) {
+            if (leader) tc::mma_commit(bar);
             __syncwarp();
         };
         TileWalk walk;
@@ -542,48 +528,62 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
         for (; ok; ++ns) {
             const int more = walk.next(p, a, pl, g);
             if (!__shfl_sync(~0u, more, 0)) break;
-            const int slot = ns % Gm::NQ, n = __shfl_sync(~0u, g.j1 - g.j0, 0);
-            // the group's tiles: x < hi (PAIR), or every second one from w on
-            const int hi = __shfl_sync(
-                ~0u, PAIR ? min(group_tiles<PAIR>(g, pl, w), g.j1) - g.j0 : n, 0);
-            const int x0 = PAIR ? 0 : w, step = PAIR ? 1 : 2;        // its tiles: x0, x0 + step ..
-            if (!wait(&sm.q_full[slot], (ns / Gm::NQ) & 1)) break;
-            if (x0 >= hi && leader) tc::mma_commit(&sm.q_empty[slot]);   // no use of Q
-            __syncwarp();
-            // Both issuers take every slot of the ring in its order and release it, their
-            // own tiles' or not: one that skipped slots could come to wait for a fill two
-            // ahead of the last, which a parity cannot tell from the one before.
-            auto k_slot = [&](int x) {
-                if (x < hi && (PAIR || (x & 1) == w)) qk(slot, x + step >= hi);
-                else if (leader) tc::mma_commit(&sm.empty[st]);
-                if (++st == NST) st = 0, ph ^= 1;
-            };
-            const int pre = PAIR ? 1 : min(n, 2);                    // K tiles before the first V
-            for (int x = 0; x < pre; ++x) {
+            const int qs = ns % Gm::NQ, n = __shfl_sync(~0u, g.j1 - g.j0, 0);
+            if (!wait(&sm.q_full[qs], (ns / Gm::NQ) & 1)) break;
+            if (PAIR) {
+                // group w's tiles are x < hi[w]
+                const int hi0 = __shfl_sync(~0u, min(group_tiles<PAIR>(g, pl, 0), g.j1) - g.j0, 0);
+                const int hi1 = __shfl_sync(~0u, min(group_tiles<PAIR>(g, pl, 1), g.j1) - g.j0, 0);
                 if (!wait(&sm.full[st], ph)) break;
-                k_slot(x);
-            }
-            // then V of tile x, and K of the same group's next tile
-            for (int x = 0; ok && x < n; ++x) {
-                const int kx = x + step;
-                const bool own = x < hi && (PAIR || (x & 1) == w);
-                if (own && !wait(&sm.p_full[w], np++ & 1)) break;
-                if (!wait(&sm.full[st], ph)) break;
-                const int kst = st + 1 == NST ? 0 : st + 1;
-                if (own && kx < hi && !wait(&sm.full[kst], kst ? ph : ph ^ 1)) break;
-                // P V and the next Q K^T go in one run: were the two groups' products to
-                // alternate, both would end late, and the groups fall into step instead of
-                // using the tensor cores in turn
-                if (own && !(ok = take_turn(&sm.turn, lane, abort_flag))) break;
-                if (own) pv(x > x0, kx >= hi);
-                else if (leader) tc::mma_commit(&sm.empty[st]);
-                if (++st == NST) st = 0, ph ^= 1;
-                if (kx < n && !(own && kx < hi) && !wait(&sm.full[st], ph)) {
-                    if (own) end_turn(&sm.turn, lane);
-                    break;
+                if (0 < hi0) qk(0, qs, st);
+                if (ok && 0 < hi1) qk(1, qs, st);
+                if (!ok) break;
+                release(&sm.empty[st]);
+                if (n == 1) release(&sm.q_empty[qs]);
+                st = slot_after(st), ph ^= st == 0;
+                for (int x = 0; ok && x < n; ++x) {
+                    const int v = st, k = slot_after(st);
+                    const int kph = ph ^ (k == 0);
+                    if (!wait(&sm.full[v], ph)) break;
+                    if (x < hi0) pv(0, v, x > 0, x + 1 == hi0);
+                    if (ok && x + 1 < n) wait(&sm.full[k], kph);
+                    if (ok && x + 1 < hi0) qk(0, qs, k);
+                    if (ok && x < hi1) pv(1, v, x > 0, x + 1 == hi1);
+                    if (!ok) break;
+                    release(&sm.empty[v]);
+                    st = k, ph = kph;
+                    if (x + 1 < n) {
+                        if (x + 1 < hi1) qk(1, qs, k);
+                        if (!ok) break;
+                        release(&sm.empty[k]);
+                        if (x + 2 == n) release(&sm.q_empty[qs]);
+                        st = slot_after(k), ph = kph ^ (st == 0);
+                    }
                 }
-                if (kx < n) k_slot(kx);
-                if (own) end_turn(&sm.turn, lane);
+            } else {
+                for (int x = 0; x < min(n, 2); ++x) {
+                    if (!wait(&sm.full[st], ph)) break;
+                    qk(x, qs, st);
+                    if (!ok) break;
+                    release(&sm.empty[st]);
+                    if (x + 1 == n) release(&sm.q_empty[qs]);
+                    st = slot_after(st), ph ^= st == 0;
+                }
+                for (int x = 0; ok && x < n; ++x) {
+                    if (!wait(&sm.full[st], ph)) break;
+                    pv(x & 1, st, x > 1, x + 2 >= n);
+                    if (!ok) break;
+                    release(&sm.empty[st]);
+                    st = slot_after(st), ph ^= st == 0;
+                    if (x + 2 < n) {
+                        if (!wait(&sm.full[st], ph)) break;
+                        qk(x & 1, qs, st);
+                        if (!ok) break;
+                        release(&sm.empty[st]);
+                        if (x + 3 == n) release(&sm.q_empty[qs]);
+                        st = slot_after(st), ph ^= st == 0;
+                    }
+                }
             }
         }
         if (!ok && lane == 0) {
@@ -592,8 +592,7 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
         }
         __syncwarp();
         // every MMA this CTA issued has finished before TMEM is released
-        if (leader) tc::mma_commit(&sm.mma_done);
-        __syncwarp();
+        release(&sm.mma_done);
         warp_wait(&sm.mma_done, 0, &sm.never);
     }
 
@@ -604,10 +603,9 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
         const int quarter = warp & 3;                        // TMEM lanes of this warp
         const int r = quarter * 32 + lane;                   // row of the tile
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
-        const uint32_t ts = lanes + (uint32_t)(w * TN), to = lanes + kOCol + (uint32_t)(w * D);
+        const uint32_t tp = lanes + kPCol + (uint32_t)(w * 64), to = lanes + kOCol + (uint32_t)(w * D);
         const float sl2 = p.scale_log2;
         const int ri = r / p.G, rh = r - ri * p.G;           // token within the tile, head
-        constexpr int CB = Gm::S_COLS;
         int ns = 0, nso = 0, npart = 0, base_it = 0;
         bool ok = true;
         if (warp == kSoftWarp && lane == 0) split[blockIdx.x] = SplitItem{-1, 0, 0, 0};
@@ -640,35 +638,33 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
                 const int j = j0 + x;
                 const int seen = lim - j * TN;               // columns seen of this tile
                 const bool masked = __any_sync(~0u, seen < TN);
+                float y[TN];
                 if (warp_on) {
-                    float y[CB];
-                    float mx = -INFINITY;
-                    auto load = [&](int c0) {
 #pragma unroll
-                        for (int c = 0; c < CB / 32; ++c) {
-                            float t[32];
-                            tc::tmem_ld32(ts + (uint32_t)(c0 + 32 * c), t);
+                    for (int c = 0; c < TN / 32; ++c) {
+                        float t[32];
+                        tc::tmem_ld32(lanes + (uint32_t)(32 * c), t);
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) y[32 * c + e] = t[e];
-                        }
-                        tc::tmem_wait_ld();
-                        if (masked) {
-#pragma unroll
-                            for (int e = 0; e < CB; ++e)
-                                if (c0 + e >= seen) y[e] = -INFINITY;
-                        }
-                    };
-#pragma unroll
-                    for (int c0 = 0; c0 < TN; c0 += CB) {
-                        load(c0);
-                        float ma = -INFINITY, mb = -INFINITY;
-#pragma unroll
-                        for (int e = 0; e < CB; e += 4) {
-                            ma = max3(ma, y[e], y[e + 1]);
-                            mb = max3(mb, y[e + 2], y[e + 3]);
-                        }
-                        mx = max3(mx, ma, mb);
+                        for (int e = 0; e < 32; ++e) y[32 * c + e] = t[e];
                     }
+                    tc::tmem_wait_ld();
+                }
+                tc::fence_before_sync();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(&sm.s_free);
+                if (warp_on) {
+                    if (masked) {
+#pragma unroll
+                        for (int e = 0; e < TN; ++e)
+                            if (e >= seen) y[e] = -INFINITY;
+                    }
+                    float ma = -INFINITY, mb = -INFINITY;
+#pragma unroll
+                    for (int e = 0; e < TN; e += 4) {
+                        ma = max3(ma, y[e], y[e + 1]);
+                        mb = max3(mb, y[e + 2], y[e + 3]);
+                    }
+                    const float mx = fmaxf(ma, mb);
                     const float mt = mx * sl2;
                     float alpha = 1.f;
                     if (mt > m + kRescale) {                 // also the first tile with something seen
@@ -693,24 +689,20 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
                     const float2 s2 = make_float2(sl2, sl2), n2 = make_float2(-ref, -ref);
                     float2 za = make_float2(0.f, 0.f), zb = za;
 #pragma unroll
-                    for (int c0 = 0; c0 < TN; c0 += CB) {
-                        if (CB < TN) load(c0);
+                    for (int c = 0; c < TN; c += 32) {
+                        uint32_t pk[16];
 #pragma unroll
-                        for (int c = 0; c < CB; c += 32) {
-                            uint32_t pk[16];
-#pragma unroll
-                            for (int e = 0; e < 32; e += 4) {
-                                const float2 t0 = fma2(make_float2(y[c + e], y[c + e + 1]), s2, n2);
-                                const float2 t1 = fma2(make_float2(y[c + e + 2], y[c + e + 3]), s2, n2);
-                                const float2 e0 = make_float2(fast_exp2(t0.x), fast_exp2(t0.y));
-                                const float2 e1 = make_float2(fast_exp2(t1.x), fast_exp2(t1.y));
-                                za = add2(za, e0);
-                                zb = add2(zb, e1);
-                                pk[e / 2] = pack_bf16x2(e0.x, e0.y);
-                                pk[e / 2 + 1] = pack_bf16x2(e1.x, e1.y);
-                            }
-                            tmem_st16(ts + (uint32_t)((c0 + c) / 2), pk);
+                        for (int e = 0; e < 32; e += 4) {
+                            const float2 t0 = fma2(make_float2(y[c + e], y[c + e + 1]), s2, n2);
+                            const float2 t1 = fma2(make_float2(y[c + e + 2], y[c + e + 3]), s2, n2);
+                            const float2 e0 = make_float2(fast_exp2(t0.x), fast_exp2(t0.y));
+                            const float2 e1 = make_float2(fast_exp2(t1.x), fast_exp2(t1.y));
+                            za = add2(za, e0);
+                            zb = add2(zb, e1);
+                            pk[e / 2] = pack_bf16x2(e0.x, e0.y);
+                            pk[e / 2 + 1] = pack_bf16x2(e1.x, e1.y);
                         }
+                        tmem_st16(tp + (uint32_t)(c / 2), pk);
                     }
                     l += (za.x + za.y) + (zb.x + zb.y);
                     tc::tmem_wait_st();
