@@ -413,9 +413,11 @@ typedef struct tgvkv_cache_pools {
 } tgvkv_cache_pools;
 
 /* Bytes of workspace the calls below need (0 when the descriptor is rejected).
- * Its first word is the status word that tgvkv_status reads; zero that word (or
- * call tgvkv_cache_workspace_init) once before the first call.  Calls that may
- * overlap on the GPU must not share a workspace. */
+ * Its first word is the status word that tgvkv_status reads.  Call
+ * tgvkv_cache_workspace_init once before the first call (the calls leave their
+ * counters and flags at zero for the next one), and again after a call whose
+ * tgvkv_status reported TGVKV_STATUS_TIMEOUT.  Calls that may overlap on the GPU
+ * must not share a workspace. */
 size_t tgvkv_cache_workspace_size(const tgvkv_cache_desc* desc);
 int tgvkv_cache_workspace_init(const tgvkv_cache_desc* desc, void* workspace, void* stream);
 

@@ -370,16 +370,19 @@ int make_cache_problem(const tgvkv_cache_desc* d, CacheProblem* p) {
     return TGVKV_OK;
 }
 
-// Workspace of the paged-cache calls: the status word, the attention's plan
+// Workspace of the paged-cache calls: the status word, the attention's tickets
+// and flags, its plan
 // (the first unit of work of every set; the items split over CTAs) and the
 // partial results of split sets.
 struct CacheLayout {
-    size_t plan, split, part, total;
+    size_t sync, plan, split, part, total;
 };
 
 CacheLayout cache_layout(const CacheProblem& p) {
     CacheLayout w;
     size_t o = round_up(sizeof(uint32_t));
+    w.sync = o;                        // tickets and flags: zero between calls
+    o += round_up(sizeof(uint32_t) * kTileSync);
     w.plan = o;
     o += round_up(sizeof(long long) * ((size_t)p.S + 1));
     w.split = o;
@@ -752,7 +755,8 @@ int tgvkv_cache_workspace_init(const tgvkv_cache_desc* desc, void* workspace, vo
     int rc = make_cache_problem(desc, &p);
     if (rc) return rc;
     REQUIRE_PTR(workspace, "workspace", true);
-    cudaError_t e = cudaMemsetAsync(workspace, 0, sizeof(uint32_t), static_cast<cudaStream_t>(stream));
+    // the status word, the tickets and the flags
+    cudaError_t e = cudaMemsetAsync(workspace, 0, cache_layout(p).plan, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? ok() : cuda_fail(e, "workspace memset");
 }
 
@@ -848,6 +852,7 @@ int tgvkv_chunk_attention(const tgvkv_cache_desc* desc, const tgvkv_cache_pools*
     float* part = reinterpret_cast<float*>(ws + lay.part);
     long long* plan = reinterpret_cast<long long*>(ws + lay.plan);
     SplitItem* split = reinterpret_cast<SplitItem*>(ws + lay.split);
+    uint32_t* sync = reinterpret_cast<uint32_t*>(ws + lay.sync);
     uint32_t* status = static_cast<uint32_t*>(workspace);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     cudaError_t e;
@@ -855,9 +860,9 @@ int tgvkv_chunk_attention(const tgvkv_cache_desc* desc, const tgvkv_cache_pools*
         e = launch_chunk_stream(p, pl, a, part, plan, status, st);
     } else {
         const bool pair = a.max_q > TM / p.G;   // some chunk has more than one row tile
-        e = p.format == TGVKV_CACHE_BF16   ? launch_tile_bf16(p, pl, a, part, split, pair, status, st)
-            : p.format == TGVKV_CACHE_INT8 ? launch_tile_int8(p, pl, a, part, split, pair, status, st)
-                                           : launch_tile_int4(p, pl, a, part, split, pair, status, st);
+        e = p.format == TGVKV_CACHE_BF16   ? launch_tile_bf16(p, pl, a, part, split, sync, pair, status, st)
+            : p.format == TGVKV_CACHE_INT8 ? launch_tile_int8(p, pl, a, part, split, sync, pair, status, st)
+                                           : launch_tile_int4(p, pl, a, part, split, sync, pair, status, st);
     }
     return e == cudaSuccess ? ok() : cuda_fail(e, "chunk attention launch");
 }

@@ -24,20 +24,20 @@ cudaError_t launch_cache_read(const CacheProblem& p, const CachePools& pool,
 // Attention of a chunk of new tokens: the row-stream kernel, for sets of at most
 // kStreamRows query rows (max_q * G; chunk_stream.cu), and the tile kernel for
 // larger ones, `pair`: two row tiles an item (chunk_tile.cuh), with its merge
-// (chunk_merge.cu).  plan: S + 1 entries; split: one per CTA; part: the split sets'
-// records.
+// (chunk_merge.cu).  plan: S + 1 entries; split: one per CTA; sync: kTileSync words,
+// zero at the start and left zero; part: the split sets' records.
 cudaError_t launch_chunk_stream(const CacheProblem& p, const CachePools& pool, const ChunkArgs& a,
                                 float* part, long long* plan, uint32_t* status,
                                 cudaStream_t stream);
 cudaError_t launch_tile_bf16(const CacheProblem& p, const CachePools& pool, const ChunkArgs& a,
-                             float* part, SplitItem* split, bool pair, uint32_t* status,
-                             cudaStream_t stream);
+                             float* part, SplitItem* split, uint32_t* sync, bool pair,
+                             uint32_t* status, cudaStream_t stream);
 cudaError_t launch_tile_int8(const CacheProblem& p, const CachePools& pool, const ChunkArgs& a,
-                             float* part, SplitItem* split, bool pair, uint32_t* status,
-                             cudaStream_t stream);
+                             float* part, SplitItem* split, uint32_t* sync, bool pair,
+                             uint32_t* status, cudaStream_t stream);
 cudaError_t launch_tile_int4(const CacheProblem& p, const CachePools& pool, const ChunkArgs& a,
-                             float* part, SplitItem* split, bool pair, uint32_t* status,
-                             cudaStream_t stream);
+                             float* part, SplitItem* split, uint32_t* sync, bool pair,
+                             uint32_t* status, cudaStream_t stream);
 cudaError_t launch_tile_merge(const CacheProblem& p, const ChunkArgs& a, const TilePlan& pl, int ctas,
                               const float* part, const SplitItem* split, cudaStream_t stream);
 

@@ -66,9 +66,14 @@ struct TilePlan {
     int rows;                          // query rows of a record: tpt * G at most
 };
 
+constexpr int kJoin = 3;               // later parts that the CTA of an item's start joins
+// words of the tile kernel's tickets and flags: two tickets, then 8 flags per CTA
+constexpr int kTileFlags = 8;
+constexpr int kTileSync = kTileFlags + 8 * kTileMaxCtas;
+
 // What a CTA of the tile kernel leaves for the merge: the item that begins in it
-// and ends in a later CTA (set -1: none), the CTAs it spans, and which of this
-// CTA's two records is its first.
+// and spans more than kJoin + 1 CTAs (set -1: none), the CTAs it spans, and which
+// of this CTA's two records is its first.
 struct SplitItem {
     int s, u, ctas, slot;
 };

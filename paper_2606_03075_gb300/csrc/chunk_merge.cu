@@ -1,9 +1,9 @@
 // Joins the partial results that the tile kernel (chunk_tile.cuh) leaves for items
-// that span several CTAs, in CTA order (so results do not depend on timing).  Each
-// CTA of that kernel names the one item that begins in it and goes on in the
-// next; the merge's CTA (x, y) takes rows 8 x .. 8 x + 7 of CTA y's item, a warp
-// each, or all 8 warps row after row when an item has many records.  A
-// programmatic dependent of the tile kernel.
+// that span many CTAs, in CTA order (so results do not depend on timing).  The CTA
+// of that kernel in which such an item begins names it; the merge's CTA (x, y)
+// takes rows 8 x .. 8 x + 7 of the y-th item named, a warp each, or all 8 warps
+// row after row when it has many records.  A programmatic dependent of the tile
+// kernel.
 #include "cache_launch.h"
 #include "launch.h"
 
@@ -15,15 +15,28 @@ constexpr int kManyRecords = 32;       // from here on, 8 warps a row
 
 template <int D>
 __global__ void __launch_bounds__(256)
-chunk_tile_merge(const CacheProblem p, const ChunkArgs a, const TilePlan pl,
+chunk_tile_merge(const CacheProblem p, const ChunkArgs a, const TilePlan pl, int ctas,
                  const float* __restrict__ part, const SplitItem* __restrict__ split) {
     constexpr int DPL = D / 32;
     __shared__ float shared[8 * (D + 2)];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    __shared__ int found[4], count[8];
     griddep_wait();
-    const int4 raw = __ldcg(reinterpret_cast<const int4*>(split) + blockIdx.y);
-    const SplitItem it{raw.x, raw.y, raw.z, raw.w};
-    if (it.s < 0) return;
+    // the y-th of the items named: threads 0 .. ctas - 1 hold one CTA's word each
+    int4 raw = make_int4(-1, 0, 0, 0);
+    if (threadIdx.x < ctas) raw = __ldcg(reinterpret_cast<const int4*>(split) + threadIdx.x);
+    const uint32_t named = __ballot_sync(~0u, raw.x >= 0);
+    if (lane == 0) count[warp] = __popc(named);
+    if (threadIdx.x == 0) found[0] = -1;
+    __syncthreads();
+    int rank = __popc(named & ((1u << lane) - 1u));
+    for (int x = 0; x < warp; ++x) rank += count[x];
+    if (raw.x >= 0 && rank == blockIdx.y)
+        found[0] = threadIdx.x, found[1] = raw.x, found[2] = raw.y, found[3] = raw.z | (raw.w << 16);
+    __syncthreads();
+    const int start = found[0];        // the CTA in which it begins
+    if (start < 0) return;
+    const SplitItem it{found[1], found[2], found[3] & 0xFFFF, found[3] >> 16};
     const SetSpan sp = set_span(p, a, it.s);
     const int tok0 = it.u * pl.tpi;    // the item's first token within its chunk
     const int rows = min(pl.tpi, sp.n - tok0) * p.G;
@@ -37,7 +50,7 @@ chunk_tile_merge(const CacheProblem p, const ChunkArgs a, const TilePlan pl,
         const int t = tok0 + row / p.G, head = (it.s % p.H_kv) * p.G + row % p.G;
         float acc[DPL];
         auto record = [&](int x) {
-            return part + (((size_t)blockIdx.y + x) * 2 * tiles + (x == 0 ? it.slot : 0) * tiles + w) * rec;
+            return part + (((size_t)start + x) * 2 * tiles + (x == 0 ? it.slot : 0) * tiles + w) * rec;
         };
         if (many) {
             merge_records<D, 8>(it.ctas, pl.rows, r, record, acc, shared, warp);
@@ -58,10 +71,14 @@ chunk_tile_merge(const CacheProblem p, const ChunkArgs a, const TilePlan pl,
 cudaError_t launch_tile_merge(const CacheProblem& p, const ChunkArgs& a, const TilePlan& pl, int ctas,
                               const float* part, const SplitItem* split, cudaStream_t stream) {
     const int tokens = a.max_q < pl.tpi ? a.max_q : pl.tpi;      // of an item, at most
-    const dim3 grid((unsigned)((tokens * p.G + kMergeRows - 1) / kMergeRows), (unsigned)ctas);
+    // such items begin at least kJoin + 1 CTAs apart
+    const dim3 grid((unsigned)((tokens * p.G + kMergeRows - 1) / kMergeRows),
+                    (unsigned)(ctas / (kJoin + 1) + 1));
     if (p.d == 64)
-        return launch_dependent(chunk_tile_merge<64>, grid, dim3(256), 0, stream, p, a, pl, part, split);
-    return launch_dependent(chunk_tile_merge<128>, grid, dim3(256), 0, stream, p, a, pl, part, split);
+        return launch_dependent(chunk_tile_merge<64>, grid, dim3(256), 0, stream, p, a, pl, ctas,
+                                part, split);
+    return launch_dependent(chunk_tile_merge<128>, grid, dim3(256), 0, stream, p, a, pl, ctas,
+                                part, split);
 }
 
 }  // namespace tgvkv

@@ -15,8 +15,12 @@
 // A unit of work is one 128-slot key tile of an item (a row tile, or a pair);
 // each persistent CTA takes one contiguous share of the units of all items, so
 // ragged chunks, ragged lengths and single long caches all split evenly.  An item
-// that spans several CTAs leaves one partial (m, l, O) per CTA and row tile,
-// merged by a second kernel in CTA order.
+// that spans a few CTAs is joined by the one that begins it: that is the last
+// segment of its share, and the first of the others', whose partial (m, l, O) is
+// there by then (a flag per warp; shares are handed out by a ticket in descending
+// order, so that a CTA only ever waits for CTAs that started before it).  An item
+// that spans many leaves all its partials to a second kernel.  Both join in CTA
+// order.
 //
 // Tensor memory: one S (128 columns), P0, P1 (64 columns each: 128 bf16), O0, O1
 // (D columns each).  A softmax thread takes its row of S into registers and frees
@@ -222,7 +226,7 @@ struct TileSmem {
     uint32_t tmem_base;
     int abort_flag, never;
     long long warp_sum[Gm::THREADS / 32];
-    int start_s, start_u, start_j;
+    int start_s, start_u, start_j, share;
 };
 
 // Row tile w of a segment's item (PAIR), or its one row tile: its key tiles.
@@ -245,13 +249,31 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volati
     return __all_sync(~0u, tc::mbar_wait(bar, parity, abort));
 }
 
+// A warp's part of a record is written / is awaited and taken (the flag is down
+// again for the next call).  The wait is bounded like those on mbarriers.
+__device__ __forceinline__ void give_flag(uint32_t* flag, int lane) {
+    __threadfence();
+    __syncwarp();
+    if (lane == 0) atomicExch(flag, 1u);
+}
+__device__ __forceinline__ bool take_flag(uint32_t* flag, int lane, volatile int* abort) {
+    int got = 1;
+    if (lane == 0) {
+        const long long t0 = clock64();
+        while ((got = atomicExch(flag, 0u) == 1u) == 0)
+            if (*abort || clock64() - t0 > tc::kWaitLimitCycles) break;
+        __threadfence();
+    }
+    return __shfl_sync(~0u, got, 0) != 0;
+}
+
 template <int D, int FMT, bool PAIR>
 __global__ void __launch_bounds__(TileGeom<D, FMT, PAIR>::THREADS, 1)
 chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                   const __grid_constant__ CUtensorMap mv, const CacheProblem p,
                   const CachePools pool, const ChunkArgs a, const TilePlan pl,
                   float* __restrict__ part, SplitItem* __restrict__ split,
-                  uint32_t* __restrict__ status) {
+                  uint32_t* __restrict__ sync, uint32_t* __restrict__ status) {
     using Gm = TileGeom<D, FMT, PAIR>;
     constexpr bool QUANT = Gm::QUANT;
     constexpr int NST = Gm::NST, NRAW = QUANT ? Gm::NRAW : 1;
@@ -265,6 +287,7 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
     if (tid == 0) {
         sm.abort_flag = 0;
         sm.never = 0;
+        sm.share = (int)gridDim.x - 1 - (int)atomicAdd(sync, 1u);
         for (int i = 0; i < NST; ++i) {
             tc::mbar_init(&sm.full[i], QUANT ? Gm::CW : 1);
             tc::mbar_init(&sm.empty[i], 1);
@@ -317,7 +340,8 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
         total += sm.warp_sum[w];
     }
     const long long per = (total + gridDim.x - 1) / gridDim.x;
-    const long long c0 = blockIdx.x * per;
+    const int share = sm.share;        // written before the barrier above
+    const long long c0 = share * per;
     const int count = (int)max(min(total - c0, per), 0ll);
     if (count > 0 && c0 >= base && c0 < base + sum) {   // the first unit is in my sets
         long long at = c0 - base;
@@ -608,7 +632,7 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
         const int ri = r / p.G, rh = r - ri * p.G;           // token within the tile, head
         int ns = 0, nso = 0, npart = 0, base_it = 0;
         bool ok = true;
-        if (warp == kSoftWarp && lane == 0) split[blockIdx.x] = SplitItem{-1, 0, 0, 0};
+        if (warp == kSoftWarp && lane == 0) split[share] = SplitItem{-1, 0, 0, 0};
         auto& at = sm.at[warp - kSoftWarp];
         const volatile Seg& g = at.g;
         if (lane == 0) begin(at.walk);
@@ -639,16 +663,14 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
                 const int seen = lim - j * TN;               // columns seen of this tile
                 const bool masked = __any_sync(~0u, seen < TN);
                 float y[TN];
-                if (warp_on) {
 #pragma unroll
-                    for (int c = 0; c < TN / 32; ++c) {
-                        float t[32];
-                        tc::tmem_ld32(lanes + (uint32_t)(32 * c), t);
+                for (int c = 0; c < TN / 32; ++c) {
+                    float t[32];
+                    tc::tmem_ld32(lanes + (uint32_t)(32 * c), t);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) y[32 * c + e] = t[e];
-                    }
-                    tc::tmem_wait_ld();
+                    for (int e = 0; e < 32; ++e) y[32 * c + e] = t[e];
                 }
+                tc::tmem_wait_ld();
                 tc::fence_before_sync();
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(&sm.s_free);
@@ -732,17 +754,26 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
             if (!ok) break;
             base_it += 2 * n;
 
-            // ---- the segment's end: a whole item is written out, a part kept for the merge
-            const bool whole = g.j0 == 0 && g.j1 == g.nk;
-            if (warp == kSoftWarp && lane == 0 && g.j0 == 0 && !whole) {
-                // an item that begins here and goes on in the next CTAs
-                const int rest = g.nk - g.j1;
-                split[blockIdx.x] = SplitItem{g.s, g.u, 2 + (int)((rest - 1) / per), g.starts ? 0 : 1};
-            }
-            const size_t rec = (size_t)((blockIdx.x * 2 + (g.starts ? 0 : 1)) * (PAIR ? 2 : 1) + (PAIR ? w : 0));
-            float* pp = part + rec * chunk_record_floats(pl.rows, D);
+            // ---- the segment's end
+            const int wi = warp - kSoftWarp;
+            const bool begins = g.j0 == 0, ends = g.j1 == g.nk;
+            // CTAs that hold earlier and later parts of the item
+            const int before = begins ? 0 : (int)((g.j0 + per - 1) / per);
+            const int after = ends ? 0 : (int)((g.nk - g.j1 + per - 1) / per);
+            const bool few = before + after <= kJoin;
+            const bool writes = begins && few;                   // joins the others' parts, if any
+            const size_t rec_floats = chunk_record_floats(pl.rows, D);
+            auto record = [&](int cta, int slot) {
+                return part + (size_t)((cta * 2 + slot) * (PAIR ? 2 : 1) + (PAIR ? w : 0)) * rec_floats;
+            };
+            float* pp = record(share, g.starts ? 0 : 1);
             uint16_t* op = a.out + ((size_t)(g.sp.tok0 + (valid ? tok + ri : 0)) * p.H_q +
                                     (g.s % p.H_kv) * p.G + rh) * D;
+            if (begins && !few && wi == 0 && lane == 0)
+                split[share] = SplitItem{g.s, g.u, 1 + after, g.starts ? 0 : 1};
+
+            // this CTA's result: O = f0 O0 + f1 O1 (SPLIT), its maximum M and mass L
+            float M = m, L = l, f0 = 1.f, f1 = 0.f;
             if (PAIR) {
                 if (hi > 0) {
                     if (!warp_wait(&sm.o_done[w], nso & 1, abort_flag)) {
@@ -750,39 +781,6 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
                         break;
                     }
                     ++nso;
-                    tc::fence_after_sync();
-                }
-                const float inv = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
-#pragma unroll
-                for (int c = 0; c < D / 32; ++c) {
-                    float t[32];
-                    if (hi > 0 && warp_on) {
-                        tc::tmem_ld32(to + (uint32_t)(32 * c), t);
-                        tc::tmem_wait_ld();
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) t[e] = 0.f;
-                    }
-                    if (valid && whole) {
-#pragma unroll
-                        for (int e = 0; e < 32; e += 8)
-                            *reinterpret_cast<uint4*>(op + 32 * c + e) = make_uint4(
-                                pack_bf16x2(t[e] * inv, t[e + 1] * inv),
-                                pack_bf16x2(t[e + 2] * inv, t[e + 3] * inv),
-                                pack_bf16x2(t[e + 4] * inv, t[e + 5] * inv),
-                                pack_bf16x2(t[e + 6] * inv, t[e + 7] * inv));
-                    } else if (valid) {
-#pragma unroll
-                        for (int e = 0; e < 32; e += 4)
-                            *reinterpret_cast<float4*>(pp + r * D + 32 * c + e) =
-                                make_float4(t[e], t[e + 1], t[e + 2], t[e + 3]);
-                    }
-                    __syncwarp();
-                }
-                tc::fence_before_sync();
-                if (valid && !whole) {
-                    pp[pl.rows * D + r] = m;
-                    pp[pl.rows * D + pl.rows + r] = l;
                 }
             } else {
                 // join the groups' halves: each takes half of the dims of both O
@@ -797,56 +795,90 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
                     break;
                 }
                 if (n > 1) ++nso;
-                tc::fence_after_sync();
                 const float2 a0 = sm.ml[0][r], a1 = sm.ml[PAIR ? 0 : 1][r];
-                const float M = fmaxf(a0.x, a1.x), ref = M == -INFINITY ? 0.f : M;
-                const float f0 = fast_exp2(a0.x - ref), f1 = fast_exp2(a1.x - ref);
-                const float L = a0.y * f0 + a1.y * f1;
-                const float inv = L > 0.f ? 1.f / L : (L == L ? 0.f : L);
-                // (a group that had no tile left its O as it was: its factor is 0)
-                const bool one = n == 1;
-                constexpr int HD = D / 2;
-                if (warp_on) {
+                M = fmaxf(a0.x, a1.x);
+                const float ref = M == -INFINITY ? 0.f : M;
+                f0 = fast_exp2(a0.x - ref);
+                f1 = fast_exp2(a1.x - ref);
+                L = a0.y * f0 + a1.y * f1;
+            }
+            tc::fence_after_sync();
+            // the other parts of an item that this CTA writes
+            float ref = 0.f;
+            const float* others = record(share + 1, 0) + (valid ? r : 0) * D;
+            const size_t next = (size_t)(PAIR ? 4 : 2) * rec_floats;
+            const int ml_at = pl.rows * D + (valid ? r : 0) * (1 - D);   // from O's row to m's
+            if (writes && after > 0) {
+                for (int x = 1; ok && x <= after; ++x)
+                    ok = take_flag(sync + kTileFlags + (share + x) * 8 + wi, lane, abort_flag);
+                if (!ok) break;
+                float Mn = M;
+                for (int x = 0; x < after; ++x) Mn = fmaxf(Mn, __ldcg(others + x * next + ml_at));
+                ref = Mn == -INFINITY ? 0.f : Mn;
+                const float f = fast_exp2(M - ref);
+                f0 *= f, f1 *= f, L *= f;
+                for (int x = 0; x < after; ++x)
+                    L += __ldcg(others + x * next + ml_at + pl.rows) *
+                         fast_exp2(__ldcg(others + x * next + ml_at) - ref);
+            }
+            const float inv = L > 0.f ? 1.f / L : (L == L ? 0.f : L);
+            constexpr int COLS = PAIR ? D : D / 2;               // dims this thread writes
+            const int col0 = PAIR ? 0 : w * COLS;
+            // (a group without a tile left its O as it was)
+            const bool has0 = PAIR ? hi > 0 : true, has1 = n > 1;
+#pragma unroll 1
+            for (int c = 0; c < COLS; c += 16) {
+                uint32_t u[16];
+                float t[16];
+                tmem_ld16(lanes + kOCol + (uint32_t)((PAIR ? w * D : 0) + col0 + c), u);
+                tc::tmem_wait_ld();
 #pragma unroll
-                    for (int c = 0; c < HD / 32; ++c) {
-                        const int col = w * HD + 32 * c;
-                        float t[32];
-                        tc::tmem_ld32(lanes + kOCol + (uint32_t)col, t);
-                        tc::tmem_wait_ld();
+                for (int e = 0; e < 16; ++e) t[e] = has0 ? __uint_as_float(u[e]) * f0 : 0.f;
+                if (!PAIR) {
+                    tmem_ld16(lanes + kOCol + (uint32_t)(D + col0 + c), u);
+                    tc::tmem_wait_ld();
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) t[e] *= f0;
-                        if (!one) {
-                            float t1[32];
-                            tc::tmem_ld32(lanes + kOCol + (uint32_t)(D + col), t1);
-                            tc::tmem_wait_ld();
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) t[e] += t1[e] * f1;
-                        }
-                        if (valid && whole) {
-#pragma unroll
-                            for (int e = 0; e < 32; e += 8)
-                                *reinterpret_cast<uint4*>(op + col + e) = make_uint4(
-                                    pack_bf16x2(t[e] * inv, t[e + 1] * inv),
-                                    pack_bf16x2(t[e + 2] * inv, t[e + 3] * inv),
-                                    pack_bf16x2(t[e + 4] * inv, t[e + 5] * inv),
-                                    pack_bf16x2(t[e + 6] * inv, t[e + 7] * inv));
-                        } else if (valid) {
-#pragma unroll
-                            for (int e = 0; e < 32; e += 4)
-                                *reinterpret_cast<float4*>(pp + r * D + col + e) =
-                                    make_float4(t[e], t[e + 1], t[e + 2], t[e + 3]);
-                        }
-                        __syncwarp();
-                    }
-                    if (valid && !whole && w == 0) {
-                        pp[pl.rows * D + r] = M;
-                        pp[pl.rows * D + pl.rows + r] = L;
-                    }
+                    for (int e = 0; e < 16; ++e) t[e] += has1 ? __uint_as_float(u[e]) * f1 : 0.f;
                 }
-                tc::fence_before_sync();
+                if (valid && writes) {
+#pragma unroll 1
+                    for (int x = 0; x < after; ++x) {
+                        const float f = fast_exp2(__ldcg(others + x * next + ml_at) - ref);
+                        const float4* pj = reinterpret_cast<const float4*>(others + x * next + col0 + c);
+#pragma unroll
+                        for (int e = 0; e < 16; e += 4) {
+                            const float4 o4 = __ldcg(pj + e / 4);
+                            t[e] += o4.x * f, t[e + 1] += o4.y * f;
+                            t[e + 2] += o4.z * f, t[e + 3] += o4.w * f;
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; e += 8)
+                        *reinterpret_cast<uint4*>(op + col0 + c + e) = make_uint4(
+                            pack_bf16x2(t[e] * inv, t[e + 1] * inv),
+                            pack_bf16x2(t[e + 2] * inv, t[e + 3] * inv),
+                            pack_bf16x2(t[e + 4] * inv, t[e + 5] * inv),
+                            pack_bf16x2(t[e + 6] * inv, t[e + 7] * inv));
+                } else if (valid) {
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4)
+                        *reinterpret_cast<float4*>(pp + r * D + col0 + c + e) =
+                            make_float4(t[e], t[e + 1], t[e + 2], t[e + 3]);
+                }
+                __syncwarp();
+            }
+            tc::fence_before_sync();
+            if (!writes) {
+                if (valid) {           // (SPLIT: both groups write the same)
+                    pp[pl.rows * D + r] = M;
+                    pp[pl.rows * D + pl.rows + r] = L;
+                }
+                if (few) give_flag(sync + kTileFlags + share * 8 + wi, lane);
+            }
+            if (!PAIR) {
+                // both O and (m, l) are free again
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(&sm.join_out);
-                // both O and (m, l) are free again
                 if (!warp_wait(&sm.join_out, npart & 1, abort_flag)) {
                     ok = false;
                     break;
@@ -935,11 +967,17 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
         tc::fence_after_sync();
         tc::tmem_dealloc(tmem, 512);
     }
+    // the last CTA leaves the tickets at zero for the next call
+    if (tid == 0 && atomicAdd(sync + 1, 1u) == gridDim.x - 1) {
+        atomicExch(sync, 0u);
+        atomicExch(sync + 1, 0u);
+    }
 }
 
 template <int D, int FMT, bool PAIR>
 cudaError_t launch_tile(const CacheProblem& p, const CachePools& pool, const ChunkArgs& a,
-                        float* part, SplitItem* split, uint32_t* status, cudaStream_t stream) {
+                        float* part, SplitItem* split, uint32_t* sync, uint32_t* status,
+                        cudaStream_t stream) {
     using Sm = TileSmem<D, FMT, PAIR>;
     static_assert(sizeof(Sm) + 1024 <= 227 * 1024, "shared memory of one CTA");
     TilePlan pl;
@@ -966,7 +1004,7 @@ cudaError_t launch_tile(const CacheProblem& p, const CachePools& pool, const Chu
     if (sms <= 0) return cudaErrorInvalidDevice;
     const int ctas = sms < kTileMaxCtas ? sms : kTileMaxCtas;
     chunk_tile_kernel<D, FMT, PAIR><<<ctas, TileGeom<D, FMT, PAIR>::THREADS, smem, stream>>>(
-        mq, mk, mv, p, pool, a, pl, part, split, status);
+        mq, mk, mv, p, pool, a, pl, part, split, sync, status);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     return launch_tile_merge(p, a, pl, ctas, part, split, stream);
 }
