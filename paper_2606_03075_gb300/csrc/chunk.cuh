@@ -98,11 +98,15 @@ __device__ __forceinline__ long long set_units(const SetSpan& sp, const TilePlan
 // Which record goes where depends on the count alone, so the result does not
 // depend on timing.  Lane t of warp 0 gets dims [t D / 32, (t + 1) D / 32) of the
 // normalised result in acc.
-template <int D, int WPR, typename Rec>
+// INTERLEAVED: a record's dims 4 k .. 4 k + 3 of row r are float4 k * rows + r (as the
+// tile kernel, thread = row, writes them); else O is [rows][D].
+template <int D, int WPR, bool INTERLEAVED, typename Rec>
 __device__ __forceinline__ void merge_records(int count, int rec_rows, int r, Rec&& rec,
                                               float (&acc)[D / 32], float* shared, int wr) {
     constexpr int DPL = D / 32;
     const int lane = threadIdx.x & 31;
+    const int at = INTERLEAVED ? ((DPL * lane / 4) * rec_rows + r) * 4 + DPL * lane % 4
+                               : r * D + DPL * lane;
     float M = -INFINITY, L = 0.f;
 #pragma unroll
     for (int c = 0; c < DPL; ++c) acc[c] = 0.f;
@@ -120,7 +124,7 @@ __device__ __forceinline__ void merge_records(int count, int rec_rows, int r, Re
 #pragma unroll
             for (int c = 0; c < DPL; ++c) ov[u][c] = 0.f;
             if (u < cnt) {
-                const float* ow = rec(b + u) + r * D + DPL * lane;
+                const float* ow = rec(b + u) + at;
                 if (DPL == 4) {
                     const float4 x = __ldcg(reinterpret_cast<const float4*>(ow));
                     ov[u][0] = x.x, ov[u][1 % DPL] = x.y, ov[u][2 % DPL] = x.z, ov[u][3 % DPL] = x.w;

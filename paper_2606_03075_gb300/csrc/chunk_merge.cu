@@ -53,11 +53,11 @@ chunk_tile_merge(const CacheProblem p, const ChunkArgs a, const TilePlan pl, int
             return part + (((size_t)start + x) * 2 * tiles + (x == 0 ? it.slot : 0) * tiles + w) * rec;
         };
         if (many) {
-            merge_records<D, 8>(it.ctas, pl.rows, r, record, acc, shared, warp);
+            merge_records<D, 8, true>(it.ctas, pl.rows, r, record, acc, shared, warp);
             __syncthreads();           // shared is free for the next row
             if (warp != 0) continue;
         } else {
-            merge_records<D, 1>(it.ctas, pl.rows, r, record, acc, nullptr, 0);
+            merge_records<D, 1, true>(it.ctas, pl.rows, r, record, acc, nullptr, 0);
         }
         uint16_t* out = a.out + ((size_t)(sp.tok0 + t) * p.H_q + head) * D + DPL * lane;
 #pragma unroll

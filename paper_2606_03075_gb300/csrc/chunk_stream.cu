@@ -708,7 +708,7 @@ chunk_stream_merge(const CacheProblem p, const ChunkArgs a, int n_streams, int m
         // a segment starts its stream's share, but for a set that begins inside it
         const int first = c0 != w0 * per ? 1 : 0;
         const size_t rec = chunk_record_floats(rec_rows, D);
-        merge_records<D, WPR>(w1 - w0 + 1, rec_rows, r, [&](int i) {
+        merge_records<D, WPR, false>(w1 - w0 + 1, rec_rows, r, [&](int i) {
             return part + ((size_t)(w0 + i) * 2 + (i == 0 ? first : 0)) * rec;
         }, acc, shared, WPR == 1 ? 0 : warp);
     }

@@ -804,66 +804,77 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
             }
             tc::fence_after_sync();
             // the other parts of an item that this CTA writes
+            // (a record's dims 4 k .. 4 k + 3 of row r are float4 k * rows + r: a warp's rows
+            // lie side by side)
             float ref = 0.f;
-            const float* others = record(share + 1, 0) + (valid ? r : 0) * D;
+            const float* others = record(share + 1, 0);
             const size_t next = (size_t)(PAIR ? 4 : 2) * rec_floats;
-            const int ml_at = pl.rows * D + (valid ? r : 0) * (1 - D);   // from O's row to m's
+            const int row = valid ? r : 0, m_at = pl.rows * D + row, l_at = m_at + pl.rows;
             if (writes && after > 0) {
                 for (int x = 1; ok && x <= after; ++x)
                     ok = take_flag(sync + kTileFlags + (share + x) * 8 + wi, lane, abort_flag);
                 if (!ok) break;
                 float Mn = M;
-                for (int x = 0; x < after; ++x) Mn = fmaxf(Mn, __ldcg(others + x * next + ml_at));
+                for (int x = 0; x < after; ++x) Mn = fmaxf(Mn, __ldcg(others + x * next + m_at));
                 ref = Mn == -INFINITY ? 0.f : Mn;
                 const float f = fast_exp2(M - ref);
                 f0 *= f, f1 *= f, L *= f;
                 for (int x = 0; x < after; ++x)
-                    L += __ldcg(others + x * next + ml_at + pl.rows) *
-                         fast_exp2(__ldcg(others + x * next + ml_at) - ref);
+                    L += __ldcg(others + x * next + l_at) *
+                         fast_exp2(__ldcg(others + x * next + m_at) - ref);
             }
             const float inv = L > 0.f ? 1.f / L : (L == L ? 0.f : L);
             constexpr int COLS = PAIR ? D : D / 2;               // dims this thread writes
             const int col0 = PAIR ? 0 : w * COLS;
             // (a group without a tile left its O as it was)
             const bool has0 = PAIR ? hi > 0 : true, has1 = n > 1;
+            constexpr int CC = COLS < 64 ? COLS : 64;            // columns at a time
 #pragma unroll 1
-            for (int c = 0; c < COLS; c += 16) {
-                uint32_t u[16];
-                float t[16];
-                tmem_ld16(lanes + kOCol + (uint32_t)((PAIR ? w * D : 0) + col0 + c), u);
-                tc::tmem_wait_ld();
+            for (int c = 0; c < COLS; c += CC) {
+                float t[CC];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) t[e] = has0 ? __uint_as_float(u[e]) * f0 : 0.f;
-                if (!PAIR) {
-                    tmem_ld16(lanes + kOCol + (uint32_t)(D + col0 + c), u);
+                for (int cc = 0; cc < CC; cc += 16) {
+                    uint32_t u[16];
+                    tmem_ld16(lanes + kOCol + (uint32_t)((PAIR ? w * D : 0) + col0 + c + cc), u);
                     tc::tmem_wait_ld();
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) t[e] += has1 ? __uint_as_float(u[e]) * f1 : 0.f;
+                    for (int e = 0; e < 16; ++e) t[cc + e] = has0 ? __uint_as_float(u[e]) * f0 : 0.f;
+                    if (!PAIR) {
+                        tmem_ld16(lanes + kOCol + (uint32_t)(D + col0 + c + cc), u);
+                        tc::tmem_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            t[cc + e] += has1 ? __uint_as_float(u[e]) * f1 : 0.f;
+                    }
                 }
+                const int k0 = (col0 + c) / 4;
                 if (valid && writes) {
 #pragma unroll 1
                     for (int x = 0; x < after; ++x) {
-                        const float f = fast_exp2(__ldcg(others + x * next + ml_at) - ref);
-                        const float4* pj = reinterpret_cast<const float4*>(others + x * next + col0 + c);
+                        const float f = fast_exp2(__ldcg(others + x * next + m_at) - ref);
+                        const float4* pj =
+                            reinterpret_cast<const float4*>(others + x * next) + (size_t)k0 * pl.rows + r;
+                        float4 o4[CC / 4];
 #pragma unroll
-                        for (int e = 0; e < 16; e += 4) {
-                            const float4 o4 = __ldcg(pj + e / 4);
-                            t[e] += o4.x * f, t[e + 1] += o4.y * f;
-                            t[e + 2] += o4.z * f, t[e + 3] += o4.w * f;
+                        for (int e = 0; e < CC / 4; ++e) o4[e] = __ldcg(pj + e * pl.rows);
+#pragma unroll
+                        for (int e = 0; e < CC / 4; ++e) {
+                            t[4 * e] += o4[e].x * f, t[4 * e + 1] += o4[e].y * f;
+                            t[4 * e + 2] += o4[e].z * f, t[4 * e + 3] += o4[e].w * f;
                         }
                     }
 #pragma unroll
-                    for (int e = 0; e < 16; e += 8)
+                    for (int e = 0; e < CC; e += 8)
                         *reinterpret_cast<uint4*>(op + col0 + c + e) = make_uint4(
                             pack_bf16x2(t[e] * inv, t[e + 1] * inv),
                             pack_bf16x2(t[e + 2] * inv, t[e + 3] * inv),
                             pack_bf16x2(t[e + 4] * inv, t[e + 5] * inv),
                             pack_bf16x2(t[e + 6] * inv, t[e + 7] * inv));
                 } else if (valid) {
+                    float4* pj = reinterpret_cast<float4*>(pp) + (size_t)k0 * pl.rows + r;
 #pragma unroll
-                    for (int e = 0; e < 16; e += 4)
-                        *reinterpret_cast<float4*>(pp + r * D + col0 + c + e) =
-                            make_float4(t[e], t[e + 1], t[e + 2], t[e + 3]);
+                    for (int e = 0; e < CC / 4; ++e)
+                        pj[e * pl.rows] = make_float4(t[4 * e], t[4 * e + 1], t[4 * e + 2], t[4 * e + 3]);
                 }
                 __syncwarp();
             }
