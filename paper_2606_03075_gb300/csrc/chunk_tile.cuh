@@ -36,7 +36,8 @@
 // write them as bf16 in the swizzled layout (exact: scales are powers of two),
 // and the rest is the bf16 kernel.
 //
-// Roles: warp 0 TMA, warp 1 MMA issue (and TMEM), warp 3 rows without work,
+// Roles: warps 0 and 2 TMA (Q and K; V), warp 1 MMA issue (and TMEM), warp 3 rows
+// without work,
 // warps 4-11 softmax, warps 12-15 converters (integer caches).  Registers are split by role (setmaxnreg), so
 // that a softmax thread holds a whole row of S.  Every wait is bounded; a timeout sets
 // TGVKV_STATUS_TIMEOUT and the CTA unwinds after its copies and MMAs finished.
@@ -225,6 +226,7 @@ struct TileSmem {
     } at[8];
     uint32_t tmem_base;
     int abort_flag, never;
+    int filled[Gm::QUANT ? Gm::NRAW : Gm::NST];       // the last copy into each slot (-1: none)
     long long warp_sum[Gm::THREADS / 32];
     int start_s, start_u, start_j, share;
 };
@@ -237,9 +239,13 @@ __device__ __forceinline__ int group_tiles(const Seg& g, const TilePlan& pl, int
     return t < g.sp.n ? tiles_seen(g.sp, t + pl.tpt) : 0;
 }
 
-// Place of V of key tile x (counted from the segment's first, of n) in the order
-// of the ring, K's taking the other places.  PAIR: K0 V0 K1 V1 ...; SPLIT: K0 K1
+// Places of K and V of key tile x (counted from the segment's first, of n) in the
+// order of the ring.  PAIR: K0 V0 K1 V1 ...; SPLIT: K0 K1
 // V0 K2 V1 ...
+template <bool PAIR>
+__device__ __forceinline__ int k_place(int x) {
+    return PAIR ? 2 * x : max(2 * x - 1, 0);
+}
 template <bool PAIR>
 __device__ __forceinline__ int v_place(int x, int n) {
     return PAIR ? 2 * x + 1 : min(2 * x + 2, 2 * n - 1);
@@ -288,6 +294,7 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
         sm.abort_flag = 0;
         sm.never = 0;
         sm.share = (int)gridDim.x - 1 - (int)atomicAdd(sync, 1u);
+        for (int i = 0; i < (QUANT ? NRAW : NST); ++i) sm.filled[i] = -1;
         for (int i = 0; i < NST; ++i) {
             tc::mbar_init(&sm.full[i], QUANT ? Gm::CW : 1);
             tc::mbar_init(&sm.empty[i], 1);
@@ -371,104 +378,114 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
     if (warp < kSoftWarp) {
     regs_down<Gm::FEW_REGS>();
 
-    // ------------------------------------------------------------ producer
-    if (warp == 0) {
-        const int box = min(p.page, TN), boxes = TN / box;       // page slices of a key tile
+    // ------------------------------------------------------------ producers
+    // Warp 0 brings Q and K, warp 2 brings V: a single one takes longer to issue a key
+    // tile's copies than the tile's products take.
+    if (warp == 0 || warp == 2) {
+        const bool is_v = warp == 2;
+        const int box = min(p.page, TN);         // slots of a page slice of a key tile
         const uint32_t q_bytes = (uint32_t)(D / 64) * 128u * (uint32_t)(pl.tpt * p.G);
-        int it = 0, ns = 0, nq[2] = {0, 0};
+        const uint8_t* codes = is_v ? pool.v : pool.k;
+        const uint8_t* scales = is_v ? pool.vs : pool.ks;
+        const CUtensorMap* map = is_v ? &mv : &mk;
+        constexpr int N = QUANT ? NRAW : NST;
+        // lane b (and 16 + b): page slice b of the tile
+        const int b = lane & 15;
+        int base_it = 0, ns = 0, nq[2] = {0, 0};
         bool ok = true;
         TileWalk walk;
         Seg g;
         begin(walk);
         for (; ok && walk.next(p, a, pl, g); ++ns) {
-            const int slot = ns % Gm::NQ;
             const int gk = g.s % p.H_kv, n = g.j1 - g.j0;
             const int32_t* table = a.page_table + (size_t)g.s * p.max_pages;
-            if (!warp_wait(&sm.q_empty[slot], ((ns / Gm::NQ) & 1) ^ 1, abort_flag)) {
-                ok = false;
-                break;
+            if (!is_v) {
+                const int slot = ns % Gm::NQ;
+                if (!warp_wait(&sm.q_empty[slot], ((ns / Gm::NQ) & 1) ^ 1, abort_flag)) {
+                    ok = false;
+                    break;
+                }
+                if (lane == 0) {
+                    const int tiles = PAIR && g.tok0 + pl.tpt < g.sp.n ? 2 : 1;
+                    tc::mbar_arrive_expect_tx(&sm.q_full[slot], tiles * q_bytes);
+                    for (int t = 0; t < tiles; ++t)
+                        for (int h = 0; h < D / 64; ++h)
+                            asm volatile(
+                                "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes"
+                                " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+                                    smem_u32(&sm.q[slot * Gm::QT + t][h * TM * 128])),
+                                "l"(reinterpret_cast<uint64_t>(&mq)), "r"(64 * h), "r"(gk * p.G),
+                                "r"(g.sp.tok0 + g.tok0 + t * pl.tpt), "r"(smem_u32(&sm.q_full[slot]))
+                                : "memory");
+                }
+                ++nq[slot];
             }
-            if (lane == 0) {
-                const int tiles = PAIR && g.tok0 + pl.tpt < g.sp.n ? 2 : 1;
-                tc::mbar_arrive_expect_tx(&sm.q_full[slot], tiles * q_bytes);
-                for (int t = 0; t < tiles; ++t)
-                    for (int h = 0; h < D / 64; ++h)
-                        asm volatile(
-                            "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes"
-                            " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
-                                smem_u32(&sm.q[slot * Gm::QT + t][h * TM * 128])),
-                            "l"(reinterpret_cast<uint64_t>(&mq)), "r"(64 * h), "r"(gk * p.G),
-                            "r"(g.sp.tok0 + g.tok0 + t * pl.tpt), "r"(smem_u32(&sm.q_full[slot]))
-                            : "memory");
-            }
-            ++nq[slot];
-            // lane b (and 16 + b): page slice b of the tile.  The order of the ring:
-            // place i holds V of tile x when i is v_place(x), else the next K.
-            const int b = lane & 15;
-            int kx = 0, vx = 0;
-            auto page_of = [&](int x) {
-                const int slot0 = (g.j0 + x) * TN + b * box;
-                return b < boxes && x < n && slot0 < g.sp.len ? __ldg(table + (slot0 >> p.page_shift))
-                                                              : 0;
+            // The set's page numbers, a window of 32 to a register (a lane each): the
+            // tile's, and the next, whose load has a window's time to arrive.
+            const int last_page = (g.sp.len - 1) >> p.page_shift;
+            auto window = [&](int i) {
+                const int at = 32 * i + lane;
+                return at <= last_page ? __ldg(table + at) : 0;
             };
-            int k_page = page_of(0), v_page = k_page;
-            for (int i = 0; ok && i < 2 * n; ++i) {
-                const bool is_v = vx < kx && i == v_place<PAIR>(vx, n);
-                const int x = is_v ? vx : kx;
-                int page = is_v ? v_page : k_page;
+            int wk = (g.j0 * TN >> p.page_shift) >> 5;
+            int pages = window(wk), pages_next = window(wk + 1);
+            for (int x = 0; x < n; ++x) {
+                const int slot0 = (g.j0 + x) * TN;               // the tile's first slot
+                if ((slot0 >> p.page_shift) >> 5 > wk) {
+                    pages = pages_next;
+                    pages_next = window(++wk + 1);
+                }
+                const int at = (slot0 + b * box) >> p.page_shift;
+                // (a tile's pages lie in one window: 32 is a multiple of their number)
+                int page = __shfl_sync(~0u, pages, at & 31);
+                const int nb = (min(g.sp.len - slot0, TN) + box - 1) / box;
+                if (b >= nb) page = 0;
                 if (page < 0 || page >= p.n_pages) {
                     raise_status(status, TGVKV_STATUS_INDEX);
                     page = 0;
                 }
-                const int st = QUANT ? it % NRAW : it % NST;
-                const int ph = QUANT ? (it / NRAW) & 1 : (it / NST) & 1;
+                const int row = page * p.page + ((slot0 + b * box) & (p.page - 1));
+                const int it = base_it + (is_v ? v_place<PAIR>(x, n) : k_place<PAIR>(x));
+                const int st = it % N, ph = (it / N) & 1;
                 if (!warp_wait(QUANT ? &sm.raw_empty[st] : &sm.empty[st], ph ^ 1, abort_flag)) {
                     ok = false;
                     break;
                 }
-                const int valid = min(g.sp.len - (g.j0 + x) * TN, TN);
-                const int nb = (valid + box - 1) / box;
-                const int row = page * p.page + ((b * box) & (p.page - 1)) +
-                                (p.page > TN ? ((g.j0 + x) * TN & (p.page - 1)) : 0);
                 if (QUANT) {
-                    if (lane == 0)
+                    if (lane == 0) {
+                        sm.filled[st] = it;
                         tc::mbar_arrive_expect_tx(&sm.raw_full[st],
                                                   (uint32_t)(nb * box) * (Gm::ROWB + D / kGroup));
-                    __syncwarp();
-                    if (lane < nb) {
-                        const uint8_t* src = (is_v ? pool.v : pool.k) + (size_t)row * Gm::ROWB;
-                        bulk_load(&sm.raw[st][b * box * Gm::ROWB], src, box * Gm::ROWB, &sm.raw_full[st]);
-                    } else if (lane >= 16 && b < nb) {
-                        const uint8_t* src = (is_v ? pool.vs : pool.ks) + (size_t)row * (D / kGroup);
-                        bulk_load(&sm.sc[st][b * box * (D / kGroup)], src, box * (D / kGroup),
-                                  &sm.raw_full[st]);
                     }
+                    __syncwarp();
+                    if (lane < nb)
+                        bulk_load(&sm.raw[st][b * box * Gm::ROWB], codes + (size_t)row * Gm::ROWB,
+                                  box * Gm::ROWB, &sm.raw_full[st]);
+                    else if (lane >= 16 && b < nb)
+                        bulk_load(&sm.sc[st][b * box * (D / kGroup)], scales + (size_t)row * (D / kGroup),
+                                  box * (D / kGroup), &sm.raw_full[st]);
                 } else {
-                    if (lane == 0)
+                    if (lane == 0) {
+                        sm.filled[st] = it;
                         tc::mbar_arrive_expect_tx(&sm.full[st], (uint32_t)(nb * box) * 2 * D);
+                    }
                     __syncwarp();
                     const int h = lane >> 4;
                     if (b < nb && h < D / 64)
-                        tc::tma_load_2d(&sm.kv[st][h * Gm::HALF + b * box * 128], is_v ? &mv : &mk,
-                                        128 * h, row, &sm.full[st]);
+                        tc::tma_load_2d(&sm.kv[st][h * Gm::HALF + b * box * 128], map, 128 * h, row,
+                                        &sm.full[st]);
                 }
-                ++it;
-                // the next page numbers, a load ahead of their use
-                if (is_v) v_page = page_of(++vx);
-                else k_page = page_of(++kx);
             }
+            base_it += 2 * n;
         }
         if (!ok && lane == 0) {
             sm.abort_flag = 1;
             raise_status(status, TGVKV_STATUS_TIMEOUT);
         }
         __syncwarp();
-        // every copy this CTA issued has landed before it may exit
+        // every Q copy has landed before the CTA may exit (K and V: at the teardown)
         for (int slot = 0; slot < Gm::NQ; ++slot)
             if (nq[slot] > 0) warp_wait(&sm.q_full[slot], (nq[slot] - 1) & 1, &sm.never);
-        constexpr int N = QUANT ? NRAW : NST;
-        for (int i = it > N ? it - N : 0; i < it; ++i)
-            warp_wait(QUANT ? &sm.raw_full[i % N] : &sm.full[i % N], (i / N) & 1, &sm.never);
     }
 
     // ------------------------------------------------------------ rows that see nothing
@@ -974,6 +991,14 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
     __syncwarp();
     tc::fence_before_sync();
     __syncthreads();
+    // every K and V copy this CTA issued has landed before it may exit (no producer
+    // is at work any more: the slots' last copies are the ones to wait for)
+    if (warp == 0) {
+        constexpr int N = QUANT ? NRAW : NST;
+        for (int st = 0; st < N; ++st)
+            if (sm.filled[st] >= 0)
+                warp_wait(QUANT ? &sm.raw_full[st] : &sm.full[st], (sm.filled[st] / N) & 1, &sm.never);
+    }
     if (warp == 1) {
         tc::fence_after_sync();
         tc::tmem_dealloc(tmem, 512);
