@@ -66,26 +66,38 @@ __device__ __forceinline__ uint32_t elect_one() {
     return r;
 }
 // D[tmem] (+)= A[smem] * B[smem]^T.  Of a descriptor only the low word (the address)
-// changes between the instructions of a tile: an add and no carry.
-__device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t a_hi,
-                                       uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
+// changes between the instructions of a tile: an add and no carry.  `leader`: a
+// predicate and no branch, so that the warp's operands stay uniform.
+template <int ACC>
+__device__ __forceinline__ void mma_ss(uint32_t leader, uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo,
+                                       uint32_t a_hi, uint32_t b_hi, uint32_t idesc) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
-        "setp.ne.b32 p, %6, 0;\n\t"
+        "{\n\t.reg .pred p, q;\n\t.reg .b64 a, b;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\tsetp.ne.b32 q, %7, 0;\n\t"
         "mov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %4};\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %5, p;\n\t}" ::"r"(d_tmem),
-        "r"(a_lo), "r"(b_lo), "r"(a_hi), "r"(b_hi), "r"(idesc), "r"(accumulate)
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %5, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_lo), "r"(b_lo), "r"(a_hi), "r"(b_hi), "r"(idesc), "n"(ACC), "r"(leader)
         : "memory");
 }
 // D[tmem] (+)= A[tmem] * B[smem]
-__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t b_hi,
-                                       uint32_t idesc, uint32_t accumulate) {
+__device__ __forceinline__ void mma_ts(uint32_t leader, uint32_t d_tmem, uint32_t a_tmem,
+                                       uint32_t b_lo, uint32_t b_hi, uint32_t idesc,
+                                       uint32_t accumulate) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\t"
-        "setp.ne.b32 p, %5, 0;\n\t"
+        "{\n\t.reg .pred p, q;\n\t.reg .b64 b;\n\t"
+        "setp.ne.b32 p, %5, 0;\n\tsetp.ne.b32 q, %6, 0;\n\t"
         "mov.b64 b, {%2, %3};\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t}" ::"r"(d_tmem),
-        "r"(a_tmem), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_tmem), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate), "r"(leader)
+        : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t leader, uint64_t* bar) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "setp.ne.b32 q, %1, 0;\n\t"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(
+            smem_u32(bar)),
+        "r"(leader)
         : "memory");
 }
 
@@ -534,35 +546,27 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
             ++nqk;
             const uint32_t qa = q_lo + (uint32_t)(qslot * Gm::QT + (PAIR ? w : 0)) * QTILE;
             const uint32_t ka = k_lo + (uint32_t)k * SLOT;
-            if (leader) {
+            mma_ss<0>(leader, tm, qa, ka, q_hi, k_hi, IDESC_QK);
 #pragma unroll
-                for (int kk = 0; kk < D / 16; ++kk) {
-                    const uint32_t off = (kk >> 2) * HALF16 + (kk & 3) * 2;
-                    mma_ss(tm, qa + off, ka + off, q_hi, k_hi, IDESC_QK, kk > 0 ? 1u : 0u);
-                }
-                tc::mma_commit(&sm.s_full[w]);
+            for (int kk = 1; kk < D / 16; ++kk) {
+                const uint32_t off = (kk >> 2) * HALF16 + (kk & 3) * 2;
+                mma_ss<1>(leader, tm, qa + off, ka + off, q_hi, k_hi, IDESC_QK);
             }
-            __syncwarp();
+            commit(leader, &sm.s_full[w]);
         };
         // O_w (+)= P_w V with the V tile in slot v, once P_w is there
         auto pv = [&](int w, int v, bool accumulate, bool last) {
             if (!wait(&sm.p_full[w], np[w]++ & 1)) return;
             const uint32_t va = v_lo + (uint32_t)v * SLOT;
             const uint32_t to = tm + kOCol + (uint32_t)(w * D), tp = tm + kPCol + (uint32_t)(w * 64);
-            if (leader) {
-                mma_ts(to, tp, va, v_hi, IDESC_PV, accumulate ? 1u : 0u);
+            mma_ts(leader, to, tp, va, v_hi, IDESC_PV, accumulate ? 1u : 0u);
 #pragma unroll
-                for (int kk = 1; kk < TN / 16; ++kk)
-                    mma_ts(to, tp + (uint32_t)(kk * 8), va + (uint32_t)(kk * (16 * 128 / 16)), v_hi,
-                           IDESC_PV, 1u);
-                if (last) tc::mma_commit(&sm.o_done[w]);
-            }
-            __syncwarp();
+            for (int kk = 1; kk < TN / 16; ++kk)
+                mma_ts(leader, to, tp + (uint32_t)(kk * 8), va + (uint32_t)(kk * (16 * 128 / 16)), v_hi,
+                       IDESC_PV, 1u);
+            if (last) commit(leader, &sm.o_done[w]);
         };
-        auto release = [&](uint64_t* bar) {
-            if (leader) tc::mma_commit(bar);
-            __syncwarp();
-        };
+        auto release = [&](uint64_t* bar) { commit(leader, bar); };
         TileWalk walk;
         Seg g;
         begin(walk);
