@@ -423,18 +423,29 @@ def alloc_cache(desc: CacheDesc, device=None) -> PagedCache:
 
 
 @functools.lru_cache(maxsize=256)
-def _cache_ws_bytes(fields: bytes) -> int:
-    return int(_lib.load().tgvkv_cache_workspace_size(
-        ctypes.byref(CacheDesc.from_buffer_copy(fields))))
+def _cache_geometry(fields: bytes):
+    """Of a descriptor (its bytes): workspace bytes (0: rejected), sets, page-table
+    entries, elements of a pool and of a scale pool (0: none)."""
+    d = CacheDesc.from_buffer_copy(fields)
+    ws = int(_lib.load().tgvkv_cache_workspace_size(ctypes.byref(d)))
+    if ws == 0:
+        return 0, 0, 0, 0, 0
+    slots, sets = d.n_pages * d.page_size, d.B * d.H_kv
+    scale = 0 if d.format == _lib.CACHE_BF16 else slots * (d.d // CACHE_GROUP)
+    return ws, sets, sets * d.max_pages, slots * _POOL[d.format][1](d.d), scale
+
+
+def _geometry(desc, fn):
+    geo = _cache_geometry(bytes(desc))
+    if geo[0] == 0:
+        # asked again, as the library's message is that of its last call
+        _lib.load().tgvkv_cache_workspace_size(ctypes.byref(desc))
+        raise TgvkvError(-1, fn)
+    return geo
 
 
 def tgvkv_cache_workspace_size(desc: CacheDesc) -> int:
-    n = _cache_ws_bytes(bytes(desc))
-    if n == 0:
-        # not from the cache: the library's message is this call's
-        _lib.load().tgvkv_cache_workspace_size(ctypes.byref(desc))
-        raise TgvkvError(-1, "tgvkv_cache_workspace_size")
-    return n
+    return _geometry(desc, "tgvkv_cache_workspace_size")[0]
 
 
 def tgvkv_cache_workspace_init(desc: CacheDesc, ws: torch.Tensor, stream=None):
@@ -450,48 +461,46 @@ def new_cache_workspace(desc: CacheDesc, device=None) -> torch.Tensor:
     return ws
 
 
-def _pools(desc, cache: PagedCache):
-    dtypes, row = _POOL[desc.format]
-    slots = desc.n_pages * desc.page_size
-    quantised = desc.format != _lib.CACHE_BF16
-    if quantised and (cache.k_scale is None or cache.v_scale is None):
+def _dev(t, dtype, numel, name):
+    """_ptr for one dtype; these calls are short, so the checks are one expression."""
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.is_contiguous()
+            and t.numel() >= numel):
+        return t.data_ptr()
+    if t is None:
+        raise TypeError(f"{name} must be a torch.Tensor")
+    return _ptr(t, (dtype,), numel, name)
+
+
+def _pools(desc, cache: PagedCache, geo):
+    dtypes = _POOL[desc.format][0]
+    k, v = _ptr(cache.k, dtypes, geo[3], "cache.k"), _ptr(cache.v, dtypes, geo[3], "cache.v")
+    if not geo[4]:
+        return ctypes.byref(_lib.CachePools(k, v))
+    if cache.k_scale is None or cache.v_scale is None:
         raise ValueError("an integer cache needs k_scale and v_scale")
-    scale = slots * (desc.d // CACHE_GROUP)
-    return ctypes.byref(_lib.CachePools(
-        _ptr(cache.k, dtypes, slots * row(desc.d), "cache.k"),
-        _ptr(cache.v, dtypes, slots * row(desc.d), "cache.v"),
-        _ptr(cache.k_scale, (torch.uint8,), scale, "cache.k_scale") if quantised else None,
-        _ptr(cache.v_scale, (torch.uint8,), scale, "cache.v_scale") if quantised else None))
+    return ctypes.byref(_lib.CachePools(k, v, _dev(cache.k_scale, torch.uint8, geo[4], "cache.k_scale"),
+                                        _dev(cache.v_scale, torch.uint8, geo[4], "cache.v_scale")))
 
 
 def _tokens(t, heads, d, name):
-    """Pointer and (token, head) strides of a token-major tensor [T, heads, d]."""
+    """Pointer, (token, head) strides and tokens of a token-major tensor [T, heads, d]."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
     if t.dtype not in _BF16_LIKE:
         raise TypeError(f"{name} has dtype {t.dtype}, expected one of {_BF16_LIKE}")
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected (tokens, {heads}, {d})")
-    if t.numel() and t.stride(2) != 1:
+    shape = t.shape
+    if len(shape) != 3 or shape[1] != heads or shape[2] != d:
+        raise ValueError(f"{name} has shape {tuple(shape)}, expected (tokens, {heads}, {d})")
+    n = shape[0]
+    if n == 0:
+        return t.data_ptr(), heads * d, d, 0
+    tok, head, last = t.stride()
+    if last != 1:
         raise ValueError(f"{name}'s last dimension must be contiguous")
     # the stride of a dimension with one entry never matters
-    tok = t.stride(0) if t.shape[0] > 1 else heads * d
-    head = t.stride(1) if heads > 1 and t.numel() else d
-    return t.data_ptr(), tok, head
-
-
-def _page_table(desc, page_table):
-    return _ptr(page_table, (torch.int32,), desc.B * desc.H_kv * desc.max_pages, "page_table")
-
-
-def _sets(desc, t, name):
-    return _ptr(t, (torch.int32,), desc.B * desc.H_kv, name)
-
-
-def _cache_ws(desc, ws):
-    return _ptr(ws, (torch.uint8,), tgvkv_cache_workspace_size(desc), "workspace")
+    return t.data_ptr(), tok if n > 1 else heads * d, head if heads > 1 else d, n
 
 
 def tgvkv_cache_write(desc, cache: PagedCache, page_table, lens, k_new, v_new, tok_offsets,
@@ -499,42 +508,49 @@ def tgvkv_cache_write(desc, cache: PagedCache, page_table, lens, k_new, v_new, t
     """Append new tokens, k_new and v_new bf16 [T, H_kv, d] (any token and head
     strides), to the cache, quantised to its format; lens_out receives the new
     lengths (see include/tgvkv.h)."""
-    kp, kt, kh = _tokens(k_new, desc.H_kv, desc.d, "k_new")
-    vp, vt, vh = _tokens(v_new, desc.H_kv, desc.d, "v_new")
-    if k_new.shape[0] != v_new.shape[0]:
-        raise ValueError(f"k_new has {k_new.shape[0]} tokens, v_new {v_new.shape[0]}")
+    geo = _geometry(desc, "tgvkv_cache_write")
+    heads, d, sets = desc.H_kv, desc.d, geo[1]
+    kp, kt, kh, n = _tokens(k_new, heads, d, "k_new")
+    vp, vt, vh, nv = _tokens(v_new, heads, d, "v_new")
+    if n != nv:
+        raise ValueError(f"k_new has {n} tokens, v_new {nv}")
     _check(_lib.load().tgvkv_cache_write(
-        ctypes.byref(desc), _pools(desc, cache), _page_table(desc, page_table),
-        _sets(desc, lens, "lens"), kp, kt, kh, vp, vt, vh, k_new.shape[0],
-        _ptr(tok_offsets, (torch.int32,), desc.B + 1, "tok_offsets"),
-        _sets(desc, lens_out, "lens_out"), _cache_ws(desc, ws), _stream(stream)),
-        "tgvkv_cache_write")
+        ctypes.byref(desc), _pools(desc, cache, geo),
+        _dev(page_table, torch.int32, geo[2], "page_table"), _dev(lens, torch.int32, sets, "lens"),
+        kp, kt, kh, vp, vt, vh, n, _dev(tok_offsets, torch.int32, desc.B + 1, "tok_offsets"),
+        _dev(lens_out, torch.int32, sets, "lens_out"), _dev(ws, torch.uint8, geo[0], "workspace"),
+        _stream(stream)), "tgvkv_cache_write")
 
 
 def tgvkv_cache_write_rows(desc, cache: PagedCache, page_table, lens, k_rows, v_rows, offsets,
                            lens_out, ws, stream=None):
     """Append the rows of a CSR cache (tgvkv_evict's k_out, v_out and offsets)."""
-    rows = min(k_rows.numel(), v_rows.numel()) // desc.d
+    geo = _geometry(desc, "tgvkv_cache_write_rows")
+    sets = geo[1]
+    kp, vp = _ptr(k_rows, _BF16_LIKE, 0, "k_rows"), _ptr(v_rows, _BF16_LIKE, 0, "v_rows")
+    rows = min(k_rows.numel(), v_rows.numel()) // desc.d if kp is not None and vp is not None else 0
     _check(_lib.load().tgvkv_cache_write_rows(
-        ctypes.byref(desc), _pools(desc, cache), _page_table(desc, page_table),
-        _sets(desc, lens, "lens"), _ptr(k_rows, _BF16_LIKE, 0, "k_rows"),
-        _ptr(v_rows, _BF16_LIKE, 0, "v_rows"), rows,
-        _ptr(offsets, (torch.int64,), desc.B * desc.H_kv + 1, "offsets"),
-        _sets(desc, lens_out, "lens_out"), _cache_ws(desc, ws), _stream(stream)),
-        "tgvkv_cache_write_rows")
+        ctypes.byref(desc), _pools(desc, cache, geo),
+        _dev(page_table, torch.int32, geo[2], "page_table"), _dev(lens, torch.int32, sets, "lens"),
+        kp, vp, rows, _dev(offsets, torch.int64, sets + 1, "offsets"),
+        _dev(lens_out, torch.int32, sets, "lens_out"), _dev(ws, torch.uint8, geo[0], "workspace"),
+        _stream(stream)), "tgvkv_cache_write_rows")
 
 
 def tgvkv_cache_read(desc, cache: PagedCache, page_table, first, offsets, k_out, v_out, ws,
                      stream=None):
     """Read rows offsets[s] .. offsets[s+1] of k_out and v_out (bf16) back from
     the slots first[s] on of every set s (first None: from slot 0)."""
-    rows = min(k_out.numel(), v_out.numel()) // desc.d
+    geo = _geometry(desc, "tgvkv_cache_read")
+    sets = geo[1]
+    kp, vp = _ptr(k_out, _BF16_LIKE, 0, "k_out"), _ptr(v_out, _BF16_LIKE, 0, "v_out")
+    rows = min(k_out.numel(), v_out.numel()) // desc.d if kp is not None and vp is not None else 0
     _check(_lib.load().tgvkv_cache_read(
-        ctypes.byref(desc), _pools(desc, cache), _page_table(desc, page_table),
-        _sets(desc, first, "first"),
-        _ptr(offsets, (torch.int64,), desc.B * desc.H_kv + 1, "offsets"),
-        _ptr(k_out, _BF16_LIKE, 0, "k_out"), _ptr(v_out, _BF16_LIKE, 0, "v_out"), rows,
-        _cache_ws(desc, ws), _stream(stream)), "tgvkv_cache_read")
+        ctypes.byref(desc), _pools(desc, cache, geo),
+        _dev(page_table, torch.int32, geo[2], "page_table"),
+        None if first is None else _dev(first, torch.int32, sets, "first"),
+        _dev(offsets, torch.int64, sets + 1, "offsets"), kp, vp, rows,
+        _dev(ws, torch.uint8, geo[0], "workspace"), _stream(stream)), "tgvkv_cache_read")
 
 
 def tgvkv_chunk_attention(desc, cache: PagedCache, page_table, lens, q, tok_offsets, max_q, out, ws,
@@ -542,12 +558,14 @@ def tgvkv_chunk_attention(desc, cache: PagedCache, page_table, lens, q, tok_offs
     """Attention of each sequence's new tokens (the last of lens slots) over the
     paged cache: q bf16 [T, H_q, d] (any token and head strides), out bf16
     [T, H_q, d] contiguous (see include/tgvkv.h)."""
-    qp, qt, qh = _tokens(q, desc.H_q, desc.d, "q")
+    geo = _geometry(desc, "tgvkv_chunk_attention")
+    heads, d = desc.H_q, desc.d
+    qp, qt, qh, n = _tokens(q, heads, d, "q")
     _check(_lib.load().tgvkv_chunk_attention(
-        ctypes.byref(desc), _pools(desc, cache), _page_table(desc, page_table),
-        _sets(desc, lens, "lens"), qp, qt, qh, q.shape[0],
-        _ptr(tok_offsets, (torch.int32,), desc.B + 1, "tok_offsets"), int(max_q),
-        _ptr(out, _BF16_LIKE, q.shape[0] * desc.H_q * desc.d, "out"), _cache_ws(desc, ws),
+        ctypes.byref(desc), _pools(desc, cache, geo),
+        _dev(page_table, torch.int32, geo[2], "page_table"), _dev(lens, torch.int32, geo[1], "lens"),
+        qp, qt, qh, n, _dev(tok_offsets, torch.int32, desc.B + 1, "tok_offsets"), max_q,
+        _ptr(out, _BF16_LIKE, n * heads * d, "out"), _dev(ws, torch.uint8, geo[0], "workspace"),
         _stream(stream)), "tgvkv_chunk_attention")
 
 
