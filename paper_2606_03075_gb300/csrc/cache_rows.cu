@@ -37,6 +37,33 @@ __device__ __forceinline__ int find_last(const T* off, int lo, int hi, long long
     return lo;
 }
 
+// The same by a whole warp, 32 probes at a time: two loads in a row for 1024
+// entries where a binary search has ten.
+template <typename T>
+__device__ __forceinline__ int find_last_warp(const T* off, int hi, long long x, int lane) {
+    int lo = 0;
+    while (lo < hi) {
+        const int step = (hi - lo + 32) / 32;    // candidates lo, lo + step, ..: the span is hi - lo + 1
+        const int at = lo + lane * step;
+        const bool le = at <= hi && (long long)off[at] <= x;
+        const uint32_t m = __ballot_sync(~0u, le);
+        lo += max(__popc(m) - 1, 0) * step;      // offsets ascend: the lanes that hold come first
+        hi = min(hi, lo + step - 1);
+    }
+    return lo;
+}
+
+// The first and last set (or sequence) of a CTA's rows, by two of its warps.
+template <typename T>
+__device__ __forceinline__ void find_span(const T* off, int last, long long x0, long long x1,
+                                          int (&span)[2]) {
+    const int warp = threadIdx.x >> 5;
+    if (warp < 2) {
+        const int i = find_last_warp(off, last, warp ? x1 : x0, threadIdx.x & 31);
+        if ((threadIdx.x & 31) == 0) span[warp] = i;
+    }
+}
+
 // Pool row of (set, slot), or -1 (with the status bit) when there is none.
 __device__ __forceinline__ long long pool_row(const CacheProblem& p, const int32_t* page_table,
                                               int s, long long slot, uint32_t* status) {
@@ -52,11 +79,7 @@ __device__ __forceinline__ long long pool_row(const CacheProblem& p, const int32
     return (long long)page * p.page + (slot & (p.page - 1));
 }
 
-// ---- 8 values to and from their stored form ----------------------------------
-__device__ __forceinline__ float2 unpack2(uint32_t w) {
-    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
-}
-
+// ---- 8 values to their stored form -------------------------------------------
 // The scale byte of a group from the largest magnitude among its values, as
 // bf16 bits (15 bits).  With bits = 2^X' (1 + f / 128): Q = 127 needs
 // e = X' - 6, one more when f > 126 (the value is above 127 * 2^(X' - 6));
@@ -84,30 +107,44 @@ __device__ __forceinline__ void store_row(uint4 w, uint8_t* row, uint8_t* scales
     top = max(top, __shfl_xor_sync(~0u, top, 1));
     top = max(top, __shfl_xor_sync(~0u, top, 2));
     const int byte = group_byte<FMT>(top);
-    // 2^-e = 2^(127 - byte): an ordinary fp32 power of two for byte 1 .. 253
-    const float inv = byte == 255 ? 0.f : __uint_as_float((uint32_t)(254 - byte) << 23);
-    constexpr float Q = FMT == TGVKV_CACHE_INT8 ? 127.f : 7.f;
     if (!on) return;
-    int q[8];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 x = unpack2(words[i]);
-        q[2 * i] = byte == 255 ? 0 : __float2int_rn(fminf(fmaxf(x.x * inv, -Q), Q));
-        q[2 * i + 1] = byte == 255 ? 0 : __float2int_rn(fminf(fmaxf(x.y * inv, -Q), Q));
-    }
     if (FMT == TGVKV_CACHE_INT8) {
-        uint32_t lo = 0, hi = 0;
+        // x 2^-e + 1.5 * 2^23 rounds x 2^-e to an integer (ties to even) and leaves it, in two's
+        // complement, in the low bits; |x 2^-e| <= 127 by the choice of e
+        const float inv = __uint_as_float((uint32_t)(254 - min(byte, 253)) << 23);
+        uint32_t q[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            lo |= (uint32_t)(q[i] & 255) << (8 * i);
-            hi |= (uint32_t)(q[4 + i] & 255) << (8 * i);
+            q[2 * i] = __float_as_uint(fmaf(__uint_as_float(words[i] << 16), inv, 12582912.f));
+            q[2 * i + 1] = __float_as_uint(fmaf(__uint_as_float(words[i] & 0xFFFF0000u), inv, 12582912.f));
         }
-        reinterpret_cast<uint2*>(row)[unit] = make_uint2(lo, hi);
-    } else {
-        uint32_t c = 0;
+        uint32_t c[2];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) c |= (uint32_t)(q[i] + 8) << (4 * i);
-        reinterpret_cast<uint32_t*>(row)[unit] = c;
+        for (int i = 0; i < 2; ++i) {
+            c[i] = __byte_perm(__byte_perm(q[4 * i], q[4 * i + 1], 0x0040),
+                               __byte_perm(q[4 * i + 2], q[4 * i + 3], 0x0040), 0x5410);
+            if (byte == 255) c[i] = 0u;
+        }
+        reinterpret_cast<uint2*>(row)[unit] = make_uint2(c[0], c[1]);
+    } else {
+        // in bf16, whose step is 1 from 128 to 256: x 2^-e + 136 rounds to 128 + (q + 8)
+        const uint32_t inv = both((uint32_t)(254 - min(byte, 253)) << 7);
+        uint32_t q[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (byte == 247) {         // e at its cap: the values may be beyond 7 * 2^e
+                const uint32_t v = bf16x2_min(bf16x2_max(bf16x2_mul(words[i], inv), 0xC0E0C0E0u), 0x40E040E0u);
+                q[i] = bf16x2_fma(v, 0x3F803F80u, 0x43084308u);
+            } else {
+                q[i] = bf16x2_fma(words[i], inv, 0x43084308u);
+            }
+        }
+        // the nibbles: elements 0, 2, 1, 3 (and 4, 6, 5, 7) a byte apart, then the odd ones
+        // beside the even ones
+        const uint32_t a = (q[0] & 0x000F000Fu) | ((q[1] & 0x000F000Fu) << 8);
+        const uint32_t b = (q[2] & 0x000F000Fu) | ((q[3] & 0x000F000Fu) << 8);
+        const uint32_t c = __byte_perm(a, b, 0x5410) | (__byte_perm(a, b, 0x7632) << 4);
+        reinterpret_cast<uint32_t*>(row)[unit] = byte == 255 ? 0x88888888u : c;
     }
     if ((unit & 3) == 0) scales[unit >> 2] = (uint8_t)byte;
 }
@@ -131,6 +168,7 @@ cache_write_kernel(const CacheProblem p, const WriteSource src, const CachePools
                    int32_t* __restrict__ lens_out, uint32_t* __restrict__ status) {
     using Gm = RowGeom<D>;
     __shared__ long long dst[Gm::ROWS];
+    __shared__ int span[2];
     const int tid = threadIdx.x;
     const long long u0 = (long long)blockIdx.x * Gm::ROWS;
     const int unit = tid % Gm::LPR, sub = tid / Gm::LPR;
@@ -178,6 +216,13 @@ cache_write_kernel(const CacheProblem p, const WriteSource src, const CachePools
             vw[i] = __ldcs(reinterpret_cast<const uint4*>(src.v + vo) + unit);
         }
     }
+    const long long u_last = min(u0 + Gm::ROWS, src.rows) - 1;
+    if (TOKENS)
+        find_span(src.tok_offsets, p.B - 1, (unsigned)u0 / (unsigned)p.H_kv,
+                  (unsigned)max(u_last, 0ll) / (unsigned)p.H_kv, span);
+    else
+        find_span(src.row_offsets, p.S - 1, u0, u_last, span);
+    __syncthreads();
     if (tid < Gm::ROWS) {
         const long long u = u0 + tid;
         long long row = -1;
@@ -187,12 +232,12 @@ cache_write_kernel(const CacheProblem p, const WriteSource src, const CachePools
             if (TOKENS) {
                 const long long t = (unsigned)u / (unsigned)p.H_kv;
                 if (t >= src.tok_offsets[0] && t < src.tok_offsets[p.B]) {
-                    const int b = find_last(src.tok_offsets, 0, p.B - 1, t);
+                    const int b = find_last(src.tok_offsets, span[0], span[1], t);
                     s = b * p.H_kv + (int)(u - t * p.H_kv);
                     at = t - src.tok_offsets[b];
                 }
             } else if (u >= src.row_offsets[0] && u < src.row_offsets[p.S]) {
-                s = find_last(src.row_offsets, 0, p.S - 1, u);
+                s = find_last(src.row_offsets, span[0], span[1], u);
                 at = u - src.row_offsets[s];
             }
             if (s >= 0 && at >= 0)
@@ -233,6 +278,7 @@ cache_read_kernel(const CacheProblem p, const CachePools pool,
                   uint16_t* __restrict__ v_out, long long rows, uint32_t* __restrict__ status) {
     using Gm = RowGeom<D>;
     __shared__ long long from[Gm::ROWS];
+    __shared__ int span[2];
     const int tid = threadIdx.x;
     const long long u0 = (long long)blockIdx.x * Gm::ROWS;
     const int unit = tid % Gm::LPR, sub = tid / Gm::LPR;
@@ -241,11 +287,13 @@ cache_read_kernel(const CacheProblem p, const CachePools pool,
         if (lo < 0 || hi < lo || hi > rows || (s == 0 && lo != 0))
             raise_status(status, TGVKV_STATUS_INDEX);
     }
+    find_span(offsets, p.S - 1, u0, min(u0 + Gm::ROWS, rows) - 1, span);
+    __syncthreads();
     if (tid < Gm::ROWS) {
         const long long u = u0 + tid;
         long long row = -1;
         if (u < rows && u >= offsets[0] && u < offsets[p.S]) {
-            const int s = find_last(offsets, 0, p.S - 1, u);
+            const int s = find_last(offsets, span[0], span[1], u);
             const long long at = u - offsets[s];
             if (at >= 0)
                 row = pool_row(p, page_table, s, at + (first ? (long long)first[s] : 0ll), status);
