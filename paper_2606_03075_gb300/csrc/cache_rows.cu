@@ -65,7 +65,7 @@ __device__ __forceinline__ void find_span(const T* off, int last, long long x0, 
 }
 
 // Pool row of (set, slot), or -1 (with the status bit) when there is none.
-__device__ __forceinline__ long long pool_row(const CacheProblem& p, const int32_t* page_table,
+__device__ __forceinline__ int pool_row(const CacheProblem& p, const int32_t* page_table,
                                               int s, long long slot, uint32_t* status) {
     if (slot < 0 || slot >= p.cap) {
         raise_status(status, TGVKV_STATUS_INDEX);
@@ -76,7 +76,7 @@ __device__ __forceinline__ long long pool_row(const CacheProblem& p, const int32
         raise_status(status, TGVKV_STATUS_INDEX);
         return -1;
     }
-    return (long long)page * p.page + (slot & (p.page - 1));
+    return page * p.page + ((int)slot & (p.page - 1));
 }
 
 // ---- 8 values to their stored form -------------------------------------------
@@ -162,15 +162,15 @@ struct WriteSource {
 };
 
 template <int D, int FMT, bool TOKENS>
-__global__ void __launch_bounds__(kRowThreads)
+__global__ void __launch_bounds__(kRowThreads, 5)
 cache_write_kernel(const CacheProblem p, const WriteSource src, const CachePools pool,
                    const int32_t* __restrict__ page_table, const int32_t* __restrict__ lens,
                    int32_t* __restrict__ lens_out, uint32_t* __restrict__ status) {
     using Gm = RowGeom<D>;
-    __shared__ long long dst[Gm::ROWS];
+    __shared__ int dst[Gm::ROWS];
     __shared__ int span[2];
     const int tid = threadIdx.x;
-    const long long u0 = (long long)blockIdx.x * Gm::ROWS;
+    const unsigned u0 = blockIdx.x * (unsigned)Gm::ROWS;
     const int unit = tid % Gm::LPR, sub = tid / Gm::LPR;
 
     // the lengths after the write, and the check of the offsets
@@ -199,41 +199,41 @@ cache_write_kernel(const CacheProblem p, const WriteSource src, const CachePools
     }
 
     // the rows' data, in flight while their places are looked up
+    const unsigned n_rows = (unsigned)src.rows;
     uint4 kw[kRowUnroll], vw[kRowUnroll];
 #pragma unroll
     for (int i = 0; i < kRowUnroll; ++i) {
-        const long long u = u0 + i * Gm::RPI + sub;
-        if (u < src.rows) {
-            long long ko, vo;
-            if (TOKENS) {
-                const unsigned t = (unsigned)u / (unsigned)p.H_kv, g = (unsigned)u - t * p.H_kv;
-                ko = t * src.k_tok + g * src.k_head;
-                vo = t * src.v_tok + g * src.v_head;
-            } else {
-                ko = vo = u * D;
-            }
-            kw[i] = __ldcs(reinterpret_cast<const uint4*>(src.k + ko) + unit);
-            vw[i] = __ldcs(reinterpret_cast<const uint4*>(src.v + vo) + unit);
+        const unsigned u = u0 + i * Gm::RPI + sub;
+        kw[i] = vw[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (u >= n_rows) continue;
+        size_t ko, vo;
+        if (TOKENS) {
+            const unsigned t = u / (unsigned)p.H_kv, g = u - t * p.H_kv;
+            ko = t * src.k_tok + g * src.k_head;
+            vo = t * src.v_tok + g * src.v_head;
+        } else {
+            ko = vo = (size_t)u * D;
         }
+        kw[i] = __ldcs(reinterpret_cast<const uint4*>(src.k + ko) + unit);
+        vw[i] = __ldcs(reinterpret_cast<const uint4*>(src.v + vo) + unit);
     }
-    const long long u_last = min(u0 + Gm::ROWS, src.rows) - 1;
+    const unsigned u_last = max(min(u0 + Gm::ROWS, n_rows), 1u) - 1u;
     if (TOKENS)
-        find_span(src.tok_offsets, p.B - 1, (unsigned)u0 / (unsigned)p.H_kv,
-                  (unsigned)max(u_last, 0ll) / (unsigned)p.H_kv, span);
+        find_span(src.tok_offsets, p.B - 1, u0 / (unsigned)p.H_kv, u_last / (unsigned)p.H_kv, span);
     else
         find_span(src.row_offsets, p.S - 1, u0, u_last, span);
     __syncthreads();
     if (tid < Gm::ROWS) {
-        const long long u = u0 + tid;
-        long long row = -1;
-        if (u < src.rows) {
+        const unsigned u = u0 + tid;
+        int row = -1;
+        if (u < n_rows) {
             int s = -1;
             long long at = 0;
             if (TOKENS) {
-                const long long t = (unsigned)u / (unsigned)p.H_kv;
+                const int t = (int)(u / (unsigned)p.H_kv);
                 if (t >= src.tok_offsets[0] && t < src.tok_offsets[p.B]) {
                     const int b = find_last(src.tok_offsets, span[0], span[1], t);
-                    s = b * p.H_kv + (int)(u - t * p.H_kv);
+                    s = b * p.H_kv + (int)(u - (unsigned)t * p.H_kv);
                     at = t - src.tok_offsets[b];
                 }
             } else if (u >= src.row_offsets[0] && u < src.row_offsets[p.S]) {
@@ -249,50 +249,46 @@ cache_write_kernel(const CacheProblem p, const WriteSource src, const CachePools
     constexpr int RB = FMT == TGVKV_CACHE_BF16 ? 2 * D : FMT == TGVKV_CACHE_INT8 ? D : D / 2;
 #pragma unroll
     for (int i = 0; i < kRowUnroll; ++i) {
-        const long long row = dst[i * Gm::RPI + sub];
-        // the lanes of a group of 4 share a row: all of them store or none
+        const int row = dst[i * Gm::RPI + sub];
+        const bool on = row >= 0;
+        const size_t at = on ? row : 0;
         if (FMT == TGVKV_CACHE_BF16) {
-            if (row >= 0) {
-                reinterpret_cast<uint4*>(pool.k + row * RB)[unit] = kw[i];
-                reinterpret_cast<uint4*>(pool.v + row * RB)[unit] = vw[i];
-            }
+            if (!on) continue;
+            reinterpret_cast<uint4*>(pool.k + at * RB)[unit] = kw[i];
+            reinterpret_cast<uint4*>(pool.v + at * RB)[unit] = vw[i];
         } else {
-            const bool on = row >= 0;
-            if (!__any_sync(~0u, on)) continue;
-            // lanes without a row quantise zeros and store nothing
-            const uint4 z = make_uint4(0u, 0u, 0u, 0u);
-            store_row<FMT>(on ? kw[i] : z, pool.k + (on ? row : 0) * RB,
-                           pool.ks + (on ? row : 0) * (D / kGroup), unit, on);
-            store_row<FMT>(on ? vw[i] : z, pool.v + (on ? row : 0) * RB,
-                           pool.vs + (on ? row : 0) * (D / kGroup), unit, on);
+            // lanes without a row take part in the group's maximum and store nothing
+            store_row<FMT>(kw[i], pool.k + at * RB, pool.ks + at * (D / kGroup), unit, on);
+            store_row<FMT>(vw[i], pool.v + at * RB, pool.vs + at * (D / kGroup), unit, on);
         }
     }
 }
 
 // ---- read --------------------------------------------------------------------
 template <int D, int FMT>
-__global__ void __launch_bounds__(kRowThreads)
+__global__ void __launch_bounds__(kRowThreads, 5)
 cache_read_kernel(const CacheProblem p, const CachePools pool,
                   const int32_t* __restrict__ page_table, const int32_t* __restrict__ first,
                   const int64_t* __restrict__ offsets, uint16_t* __restrict__ k_out,
                   uint16_t* __restrict__ v_out, long long rows, uint32_t* __restrict__ status) {
     using Gm = RowGeom<D>;
-    __shared__ long long from[Gm::ROWS];
+    __shared__ int from[Gm::ROWS];
     __shared__ int span[2];
     const int tid = threadIdx.x;
-    const long long u0 = (long long)blockIdx.x * Gm::ROWS;
+    const unsigned u0 = blockIdx.x * (unsigned)Gm::ROWS;
     const int unit = tid % Gm::LPR, sub = tid / Gm::LPR;
     for (int s = blockIdx.x * kRowThreads + tid; s < p.S; s += gridDim.x * kRowThreads) {
         const long long lo = offsets[s], hi = offsets[s + 1];
         if (lo < 0 || hi < lo || hi > rows || (s == 0 && lo != 0))
             raise_status(status, TGVKV_STATUS_INDEX);
     }
-    find_span(offsets, p.S - 1, u0, min(u0 + Gm::ROWS, rows) - 1, span);
+    const unsigned n_rows = (unsigned)rows;
+    find_span(offsets, p.S - 1, u0, (long long)min(u0 + Gm::ROWS, n_rows) - 1, span);
     __syncthreads();
     if (tid < Gm::ROWS) {
-        const long long u = u0 + tid;
-        long long row = -1;
-        if (u < rows && u >= offsets[0] && u < offsets[p.S]) {
+        const unsigned u = u0 + tid;
+        int row = -1;
+        if (u < n_rows && u >= offsets[0] && u < offsets[p.S]) {
             const int s = find_last(offsets, span[0], span[1], u);
             const long long at = u - offsets[s];
             if (at >= 0)
@@ -305,30 +301,31 @@ cache_read_kernel(const CacheProblem p, const CachePools pool,
     uint32_t kb[kRowUnroll], vb[kRowUnroll];
 #pragma unroll
     for (int i = 0; i < kRowUnroll; ++i) {
-        const long long row = from[i * Gm::RPI + sub];
+        const int row = from[sub + i * Gm::RPI];
         kw[i] = vw[i] = make_uint4(0u, 0u, 0u, 0u);
         kb[i] = vb[i] = 0u;
         if (row < 0) continue;
+        const size_t at = row;
         if (FMT == TGVKV_CACHE_BF16) {
-            kw[i] = __ldg(reinterpret_cast<const uint4*>(pool.k + row * (2 * D)) + unit);
-            vw[i] = __ldg(reinterpret_cast<const uint4*>(pool.v + row * (2 * D)) + unit);
+            kw[i] = __ldcs(reinterpret_cast<const uint4*>(pool.k + at * (2 * D)) + unit);
+            vw[i] = __ldcs(reinterpret_cast<const uint4*>(pool.v + at * (2 * D)) + unit);
         } else {
             if (FMT == TGVKV_CACHE_INT8) {
-                const uint2 a = __ldg(reinterpret_cast<const uint2*>(pool.k + row * D) + unit);
-                const uint2 b = __ldg(reinterpret_cast<const uint2*>(pool.v + row * D) + unit);
+                const uint2 a = __ldcs(reinterpret_cast<const uint2*>(pool.k + at * D) + unit);
+                const uint2 b = __ldcs(reinterpret_cast<const uint2*>(pool.v + at * D) + unit);
                 kw[i].x = a.x, kw[i].y = a.y, vw[i].x = b.x, vw[i].y = b.y;
             } else {
-                kw[i].x = __ldg(reinterpret_cast<const uint32_t*>(pool.k + row * (D / 2)) + unit);
-                vw[i].x = __ldg(reinterpret_cast<const uint32_t*>(pool.v + row * (D / 2)) + unit);
+                kw[i].x = __ldcs(reinterpret_cast<const uint32_t*>(pool.k + at * (D / 2)) + unit);
+                vw[i].x = __ldcs(reinterpret_cast<const uint32_t*>(pool.v + at * (D / 2)) + unit);
             }
-            kb[i] = __ldg(pool.ks + row * (D / kGroup) + (unit >> 2));
-            vb[i] = __ldg(pool.vs + row * (D / kGroup) + (unit >> 2));
+            kb[i] = __ldg(pool.ks + at * (D / kGroup) + (unit >> 2));
+            vb[i] = __ldg(pool.vs + at * (D / kGroup) + (unit >> 2));
         }
     }
 #pragma unroll
     for (int i = 0; i < kRowUnroll; ++i) {
-        if (from[i * Gm::RPI + sub] < 0) continue;
-        const long long u = u0 + i * Gm::RPI + sub;
+        if (from[sub + i * Gm::RPI] < 0) continue;
+        const size_t u = u0 + sub + i * Gm::RPI;
         if (FMT != TGVKV_CACHE_BF16) {
             kw[i] = codes_to_bf16<FMT>(make_uint2(kw[i].x, kw[i].y), kb[i], p.magic);
             vw[i] = codes_to_bf16<FMT>(make_uint2(vw[i].x, vw[i].y), vb[i], p.magic);
