@@ -71,6 +71,15 @@ constexpr int kJoin = 3;               // later parts that the CTA of an item's 
 constexpr int kTileFlags = 8;
 constexpr int kTileSync = kTileFlags + 8 * kTileMaxCtas;
 
+// The CTA's share of the work, the last for the first CTA that starts.  A workspace
+// that was not at zero gives shares that do not exist: none is taken then.
+__device__ __forceinline__ int take_share(uint32_t* ticket, uint32_t* status) {
+    const uint32_t t = atomicAdd(ticket, 1u);
+    if (t < gridDim.x) return (int)(gridDim.x - 1 - t);
+    raise_status(status, TGVKV_STATUS_TIMEOUT);
+    return (int)gridDim.x;
+}
+
 // What a CTA of the tile kernel leaves for the merge: the item that begins in it
 // and spans more than kJoin + 1 CTAs (set -1: none), the CTAs it spans, and which
 // of this CTA's two records is its first.

@@ -25,6 +25,10 @@ chunk_tile_merge(const CacheProblem p, const ChunkArgs a, const TilePlan pl, int
     // the y-th of the items named: threads 0 .. ctas - 1 hold one CTA's word each
     int4 raw = make_int4(-1, 0, 0, 0);
     if (threadIdx.x < ctas) raw = __ldcg(reinterpret_cast<const int4*>(split) + threadIdx.x);
+    // a CTA without a share leaves its word as it was: nothing out of range is taken
+    if (raw.x >= p.S || raw.y < 0 || (long long)raw.y * pl.tpi > a.max_q || raw.z < 1 ||
+        raw.z > ctas - (int)threadIdx.x || (raw.w & ~1))
+        raw.x = -1;
     const uint32_t named = __ballot_sync(~0u, raw.x >= 0);
     if (lane == 0) count[warp] = __popc(named);
     if (threadIdx.x == 0) found[0] = -1;

@@ -305,7 +305,7 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
     if (tid == 0) {
         sm.abort_flag = 0;
         sm.never = 0;
-        sm.share = (int)gridDim.x - 1 - (int)atomicAdd(sync, 1u);
+        sm.share = take_share(sync, status);
         for (int i = 0; i < (QUANT ? NRAW : NST); ++i) sm.filled[i] = -1;
         for (int i = 0; i < NST; ++i) {
             tc::mbar_init(&sm.full[i], QUANT ? Gm::CW : 1);
@@ -388,258 +388,258 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
     };
 
     if (warp < kSoftWarp) {
-    regs_down<Gm::FEW_REGS>();
+        regs_down<Gm::FEW_REGS>();
 
-    // ------------------------------------------------------------ producers
-    // Warp 0 brings Q and K, warp 2 brings V: a single one takes longer to issue a key
-    // tile's copies than the tile's products take.
-    if (warp == 0 || warp == 2) {
-        const bool is_v = warp == 2;
-        const int box = min(p.page, TN);         // slots of a page slice of a key tile
-        const uint32_t q_bytes = (uint32_t)(D / 64) * 128u * (uint32_t)(pl.tpt * p.G);
-        const uint8_t* codes = is_v ? pool.v : pool.k;
-        const uint8_t* scales = is_v ? pool.vs : pool.ks;
-        const CUtensorMap* map = is_v ? &mv : &mk;
-        constexpr int N = QUANT ? NRAW : NST;
-        // lane b (and 16 + b): page slice b of the tile
-        const int b = lane & 15;
-        int base_it = 0, ns = 0, nq[2] = {0, 0};
-        bool ok = true;
-        TileWalk walk;
-        Seg g;
-        begin(walk);
-        for (; ok && walk.next(p, a, pl, g); ++ns) {
-            const int gk = g.s % p.H_kv, n = g.j1 - g.j0;
-            const int32_t* table = a.page_table + (size_t)g.s * p.max_pages;
-            if (!is_v) {
-                const int slot = ns % Gm::NQ;
-                if (!warp_wait(&sm.q_empty[slot], ((ns / Gm::NQ) & 1) ^ 1, abort_flag)) {
-                    ok = false;
-                    break;
+        // ------------------------------------------------------------ producers
+        // Warp 0 brings Q and K, warp 2 brings V: a single one takes longer to issue a key
+        // tile's copies than the tile's products take.
+        if (warp == 0 || warp == 2) {
+            const bool is_v = warp == 2;
+            const int box = min(p.page, TN);         // slots of a page slice of a key tile
+            const uint32_t q_bytes = (uint32_t)(D / 64) * 128u * (uint32_t)(pl.tpt * p.G);
+            const uint8_t* codes = is_v ? pool.v : pool.k;
+            const uint8_t* scales = is_v ? pool.vs : pool.ks;
+            const CUtensorMap* map = is_v ? &mv : &mk;
+            constexpr int N = QUANT ? NRAW : NST;
+            // lane b (and 16 + b): page slice b of the tile
+            const int b = lane & 15;
+            int base_it = 0, ns = 0, nq[2] = {0, 0};
+            bool ok = true;
+            TileWalk walk;
+            Seg g;
+            begin(walk);
+            for (; ok && walk.next(p, a, pl, g); ++ns) {
+                const int gk = g.s % p.H_kv, n = g.j1 - g.j0;
+                const int32_t* table = a.page_table + (size_t)g.s * p.max_pages;
+                if (!is_v) {
+                    const int slot = ns % Gm::NQ;
+                    if (!warp_wait(&sm.q_empty[slot], ((ns / Gm::NQ) & 1) ^ 1, abort_flag)) {
+                        ok = false;
+                        break;
+                    }
+                    if (lane == 0) {
+                        const int tiles = PAIR && g.tok0 + pl.tpt < g.sp.n ? 2 : 1;
+                        tc::mbar_arrive_expect_tx(&sm.q_full[slot], tiles * q_bytes);
+                        for (int t = 0; t < tiles; ++t)
+                            for (int h = 0; h < D / 64; ++h)
+                                asm volatile(
+                                    "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes"
+                                    " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+                                        smem_u32(&sm.q[slot * Gm::QT + t][h * TM * 128])),
+                                    "l"(reinterpret_cast<uint64_t>(&mq)), "r"(64 * h), "r"(gk * p.G),
+                                    "r"(g.sp.tok0 + g.tok0 + t * pl.tpt), "r"(smem_u32(&sm.q_full[slot]))
+                                    : "memory");
+                    }
+                    ++nq[slot];
                 }
-                if (lane == 0) {
-                    const int tiles = PAIR && g.tok0 + pl.tpt < g.sp.n ? 2 : 1;
-                    tc::mbar_arrive_expect_tx(&sm.q_full[slot], tiles * q_bytes);
-                    for (int t = 0; t < tiles; ++t)
-                        for (int h = 0; h < D / 64; ++h)
-                            asm volatile(
-                                "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes"
-                                " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
-                                    smem_u32(&sm.q[slot * Gm::QT + t][h * TM * 128])),
-                                "l"(reinterpret_cast<uint64_t>(&mq)), "r"(64 * h), "r"(gk * p.G),
-                                "r"(g.sp.tok0 + g.tok0 + t * pl.tpt), "r"(smem_u32(&sm.q_full[slot]))
-                                : "memory");
+                // The set's page numbers, a window of 32 to a register (a lane each): the
+                // tile's, and the next, whose load has a window's time to arrive.
+                const int last_page = (g.sp.len - 1) >> p.page_shift;
+                auto window = [&](int i) {
+                    const int at = 32 * i + lane;
+                    return at <= last_page ? __ldg(table + at) : 0;
+                };
+                int wk = (g.j0 * TN >> p.page_shift) >> 5;
+                int pages = window(wk), pages_next = window(wk + 1);
+                for (int x = 0; x < n; ++x) {
+                    const int slot0 = (g.j0 + x) * TN;               // the tile's first slot
+                    if ((slot0 >> p.page_shift) >> 5 > wk) {
+                        pages = pages_next;
+                        pages_next = window(++wk + 1);
+                    }
+                    const int at = (slot0 + b * box) >> p.page_shift;
+                    // (a tile's pages lie in one window: 32 is a multiple of their number)
+                    int page = __shfl_sync(~0u, pages, at & 31);
+                    const int nb = (min(g.sp.len - slot0, TN) + box - 1) / box;
+                    if (b >= nb) page = 0;
+                    if (page < 0 || page >= p.n_pages) {
+                        raise_status(status, TGVKV_STATUS_INDEX);
+                        page = 0;
+                    }
+                    const int row = page * p.page + ((slot0 + b * box) & (p.page - 1));
+                    const int it = base_it + (is_v ? v_place<PAIR>(x, n) : k_place<PAIR>(x));
+                    const int st = it % N, ph = (it / N) & 1;
+                    if (!warp_wait(QUANT ? &sm.raw_empty[st] : &sm.empty[st], ph ^ 1, abort_flag)) {
+                        ok = false;
+                        break;
+                    }
+                    if (QUANT) {
+                        if (lane == 0) {
+                            sm.filled[st] = it;
+                            tc::mbar_arrive_expect_tx(&sm.raw_full[st],
+                                                      (uint32_t)(nb * box) * (Gm::ROWB + D / kGroup));
+                        }
+                        __syncwarp();
+                        if (lane < nb)
+                            bulk_load(&sm.raw[st][b * box * Gm::ROWB], codes + (size_t)row * Gm::ROWB,
+                                      box * Gm::ROWB, &sm.raw_full[st]);
+                        else if (lane >= 16 && b < nb)
+                            bulk_load(&sm.sc[st][b * box * (D / kGroup)], scales + (size_t)row * (D / kGroup),
+                                      box * (D / kGroup), &sm.raw_full[st]);
+                    } else {
+                        if (lane == 0) {
+                            sm.filled[st] = it;
+                            tc::mbar_arrive_expect_tx(&sm.full[st], (uint32_t)(nb * box) * 2 * D);
+                        }
+                        __syncwarp();
+                        const int h = lane >> 4;
+                        if (b < nb && h < D / 64)
+                            tc::tma_load_2d(&sm.kv[st][h * Gm::HALF + b * box * 128], map, 128 * h, row,
+                                            &sm.full[st]);
+                    }
                 }
-                ++nq[slot];
+                base_it += 2 * n;
             }
-            // The set's page numbers, a window of 32 to a register (a lane each): the
-            // tile's, and the next, whose load has a window's time to arrive.
-            const int last_page = (g.sp.len - 1) >> p.page_shift;
-            auto window = [&](int i) {
-                const int at = 32 * i + lane;
-                return at <= last_page ? __ldg(table + at) : 0;
+            if (!ok && lane == 0) {
+                sm.abort_flag = 1;
+                raise_status(status, TGVKV_STATUS_TIMEOUT);
+            }
+            __syncwarp();
+            // every Q copy has landed before the CTA may exit (K and V: at the teardown)
+            for (int slot = 0; slot < Gm::NQ; ++slot)
+                if (nq[slot] > 0) warp_wait(&sm.q_full[slot], (nq[slot] - 1) & 1, &sm.never);
+        }
+
+        // ------------------------------------------------------------ rows that see nothing
+        // (the items without a key tile, which no CTA's share contains)
+        if (warp == 3) {
+            for (int s = blockIdx.x; s < p.S; s += gridDim.x) {
+                const SetSpan sp = set_span(p, a, s);
+                int none = 0;              // tokens of such items
+                if (sp.len < sp.n)
+                    while (none < sp.n && tiles_seen(sp, none + pl.tpi) == 0) none += pl.tpi;
+                none = min(none, sp.n);
+                constexpr int U = D / 8;
+                for (long long e = lane; e < (long long)none * p.G * U; e += 32) {
+                    const int row = (int)(e / U), t = row / p.G;
+                    uint16_t* op = a.out + ((size_t)(sp.tok0 + t) * p.H_q + (s % p.H_kv) * p.G +
+                                            (row - t * p.G)) * D;
+                    reinterpret_cast<uint4*>(op)[e % U] = make_uint4(0u, 0u, 0u, 0u);
+                }
+            }
+        }
+
+        // ------------------------------------------------------------ MMA issuer
+        if (warp == 1) {
+            const uint32_t leader = elect_one();
+            const uint32_t tm = __shfl_sync(~0u, tmem, 0);
+            const uint64_t qd0 = tc::sdesc_k_sw128(smem_u32(&sm.q[0][0]));
+            const uint64_t kd0 = tc::sdesc_k_sw128(smem_u32(&sm.kv[0][0]));
+            const uint64_t vd0 = tc::sdesc_mn_sw128(smem_u32(&sm.kv[0][0]), Gm::HALF);
+            const uint32_t q_lo = (uint32_t)qd0, k_lo = (uint32_t)kd0, v_lo = (uint32_t)vd0;
+            const uint32_t q_hi = (uint32_t)(qd0 >> 32), k_hi = (uint32_t)(kd0 >> 32),
+                           v_hi = (uint32_t)(vd0 >> 32);
+            constexpr uint32_t QTILE = D * 2 * TM / 16, SLOT = Gm::TILE / 16, HALF16 = Gm::HALF / 16;
+            constexpr uint32_t IDESC_QK = tc::idesc_bf16(TM, TN), IDESC_PV = tc::idesc_bf16_bmn(TM, D);
+            int st = 0, ph = 0;                      // next slot of the ring, and its phase
+            int ns = 0, nqk = 0, np[2] = {0, 0};
+            bool ok = true;
+            auto wait = [&](uint64_t* bar, uint32_t parity) {
+                if (ok && !warp_wait(bar, parity, abort_flag)) ok = false;
+                if (ok) tc::fence_after_sync();
+                return ok;
             };
-            int wk = (g.j0 * TN >> p.page_shift) >> 5;
-            int pages = window(wk), pages_next = window(wk + 1);
-            for (int x = 0; x < n; ++x) {
-                const int slot0 = (g.j0 + x) * TN;               // the tile's first slot
-                if ((slot0 >> p.page_shift) >> 5 > wk) {
-                    pages = pages_next;
-                    pages_next = window(++wk + 1);
-                }
-                const int at = (slot0 + b * box) >> p.page_shift;
-                // (a tile's pages lie in one window: 32 is a multiple of their number)
-                int page = __shfl_sync(~0u, pages, at & 31);
-                const int nb = (min(g.sp.len - slot0, TN) + box - 1) / box;
-                if (b >= nb) page = 0;
-                if (page < 0 || page >= p.n_pages) {
-                    raise_status(status, TGVKV_STATUS_INDEX);
-                    page = 0;
-                }
-                const int row = page * p.page + ((slot0 + b * box) & (p.page - 1));
-                const int it = base_it + (is_v ? v_place<PAIR>(x, n) : k_place<PAIR>(x));
-                const int st = it % N, ph = (it / N) & 1;
-                if (!warp_wait(QUANT ? &sm.raw_empty[st] : &sm.empty[st], ph ^ 1, abort_flag)) {
-                    ok = false;
-                    break;
-                }
-                if (QUANT) {
-                    if (lane == 0) {
-                        sm.filled[st] = it;
-                        tc::mbar_arrive_expect_tx(&sm.raw_full[st],
-                                                  (uint32_t)(nb * box) * (Gm::ROWB + D / kGroup));
-                    }
-                    __syncwarp();
-                    if (lane < nb)
-                        bulk_load(&sm.raw[st][b * box * Gm::ROWB], codes + (size_t)row * Gm::ROWB,
-                                  box * Gm::ROWB, &sm.raw_full[st]);
-                    else if (lane >= 16 && b < nb)
-                        bulk_load(&sm.sc[st][b * box * (D / kGroup)], scales + (size_t)row * (D / kGroup),
-                                  box * (D / kGroup), &sm.raw_full[st]);
-                } else {
-                    if (lane == 0) {
-                        sm.filled[st] = it;
-                        tc::mbar_arrive_expect_tx(&sm.full[st], (uint32_t)(nb * box) * 2 * D);
-                    }
-                    __syncwarp();
-                    const int h = lane >> 4;
-                    if (b < nb && h < D / 64)
-                        tc::tma_load_2d(&sm.kv[st][h * Gm::HALF + b * box * 128], map, 128 * h, row,
-                                        &sm.full[st]);
-                }
-            }
-            base_it += 2 * n;
-        }
-        if (!ok && lane == 0) {
-            sm.abort_flag = 1;
-            raise_status(status, TGVKV_STATUS_TIMEOUT);
-        }
-        __syncwarp();
-        // every Q copy has landed before the CTA may exit (K and V: at the teardown)
-        for (int slot = 0; slot < Gm::NQ; ++slot)
-            if (nq[slot] > 0) warp_wait(&sm.q_full[slot], (nq[slot] - 1) & 1, &sm.never);
-    }
-
-    // ------------------------------------------------------------ rows that see nothing
-    // (the items without a key tile, which no CTA's share contains)
-    if (warp == 3) {
-        for (int s = blockIdx.x; s < p.S; s += gridDim.x) {
-            const SetSpan sp = set_span(p, a, s);
-            int none = 0;              // tokens of such items
-            if (sp.len < sp.n)
-                while (none < sp.n && tiles_seen(sp, none + pl.tpi) == 0) none += pl.tpi;
-            none = min(none, sp.n);
-            constexpr int U = D / 8;
-            for (long long e = lane; e < (long long)none * p.G * U; e += 32) {
-                const int row = (int)(e / U), t = row / p.G;
-                uint16_t* op = a.out + ((size_t)(sp.tok0 + t) * p.H_q + (s % p.H_kv) * p.G +
-                                        (row - t * p.G)) * D;
-                reinterpret_cast<uint4*>(op)[e % U] = make_uint4(0u, 0u, 0u, 0u);
-            }
-        }
-    }
-
-    // ------------------------------------------------------------ MMA issuer
-    if (warp == 1) {
-        const uint32_t leader = elect_one();
-        const uint32_t tm = __shfl_sync(~0u, tmem, 0);
-        const uint64_t qd0 = tc::sdesc_k_sw128(smem_u32(&sm.q[0][0]));
-        const uint64_t kd0 = tc::sdesc_k_sw128(smem_u32(&sm.kv[0][0]));
-        const uint64_t vd0 = tc::sdesc_mn_sw128(smem_u32(&sm.kv[0][0]), Gm::HALF);
-        const uint32_t q_lo = (uint32_t)qd0, k_lo = (uint32_t)kd0, v_lo = (uint32_t)vd0;
-        const uint32_t q_hi = (uint32_t)(qd0 >> 32), k_hi = (uint32_t)(kd0 >> 32),
-                       v_hi = (uint32_t)(vd0 >> 32);
-        constexpr uint32_t QTILE = D * 2 * TM / 16, SLOT = Gm::TILE / 16, HALF16 = Gm::HALF / 16;
-        constexpr uint32_t IDESC_QK = tc::idesc_bf16(TM, TN), IDESC_PV = tc::idesc_bf16_bmn(TM, D);
-        int st = 0, ph = 0;                      // next slot of the ring, and its phase
-        int ns = 0, nqk = 0, np[2] = {0, 0};
-        bool ok = true;
-        auto wait = [&](uint64_t* bar, uint32_t parity) {
-            if (ok && !warp_wait(bar, parity, abort_flag)) ok = false;
-            if (ok) tc::fence_after_sync();
-            return ok;
-        };
-        auto slot_after = [&](int x) { return x + 1 == NST ? 0 : x + 1; };
-        // S = Q_w K^T with the K tile in slot k, once S has been read
-        auto qk = [&](int w, int qslot, int k) {
-            if (nqk > 0 && !wait(&sm.s_free, (nqk - 1) & 1)) return;
-            ++nqk;
-            const uint32_t qa = q_lo + (uint32_t)(qslot * Gm::QT + (PAIR ? w : 0)) * QTILE;
-            const uint32_t ka = k_lo + (uint32_t)k * SLOT;
-            mma_ss<0>(leader, tm, qa, ka, q_hi, k_hi, IDESC_QK);
+            auto slot_after = [&](int x) { return x + 1 == NST ? 0 : x + 1; };
+            // S = Q_w K^T with the K tile in slot k, once S has been read
+            auto qk = [&](int w, int qslot, int k) {
+                if (nqk > 0 && !wait(&sm.s_free, (nqk - 1) & 1)) return;
+                ++nqk;
+                const uint32_t qa = q_lo + (uint32_t)(qslot * Gm::QT + (PAIR ? w : 0)) * QTILE;
+                const uint32_t ka = k_lo + (uint32_t)k * SLOT;
+                mma_ss<0>(leader, tm, qa, ka, q_hi, k_hi, IDESC_QK);
 #pragma unroll
-            for (int kk = 1; kk < D / 16; ++kk) {
-                const uint32_t off = (kk >> 2) * HALF16 + (kk & 3) * 2;
-                mma_ss<1>(leader, tm, qa + off, ka + off, q_hi, k_hi, IDESC_QK);
-            }
-            commit(leader, &sm.s_full[w]);
-        };
-        // O_w (+)= P_w V with the V tile in slot v, once P_w is there
-        auto pv = [&](int w, int v, bool accumulate, bool last) {
-            if (!wait(&sm.p_full[w], np[w]++ & 1)) return;
-            const uint32_t va = v_lo + (uint32_t)v * SLOT;
-            const uint32_t to = tm + kOCol + (uint32_t)(w * D), tp = tm + kPCol + (uint32_t)(w * 64);
-            mma_ts(leader, to, tp, va, v_hi, IDESC_PV, accumulate ? 1u : 0u);
+                for (int kk = 1; kk < D / 16; ++kk) {
+                    const uint32_t off = (kk >> 2) * HALF16 + (kk & 3) * 2;
+                    mma_ss<1>(leader, tm, qa + off, ka + off, q_hi, k_hi, IDESC_QK);
+                }
+                commit(leader, &sm.s_full[w]);
+            };
+            // O_w (+)= P_w V with the V tile in slot v, once P_w is there
+            auto pv = [&](int w, int v, bool accumulate, bool last) {
+                if (!wait(&sm.p_full[w], np[w]++ & 1)) return;
+                const uint32_t va = v_lo + (uint32_t)v * SLOT;
+                const uint32_t to = tm + kOCol + (uint32_t)(w * D), tp = tm + kPCol + (uint32_t)(w * 64);
+                mma_ts(leader, to, tp, va, v_hi, IDESC_PV, accumulate ? 1u : 0u);
 #pragma unroll
-            for (int kk = 1; kk < TN / 16; ++kk)
-                mma_ts(leader, to, tp + (uint32_t)(kk * 8), va + (uint32_t)(kk * (16 * 128 / 16)), v_hi,
-                       IDESC_PV, 1u);
-            if (last) commit(leader, &sm.o_done[w]);
-        };
-        auto release = [&](uint64_t* bar) { commit(leader, bar); };
-        TileWalk walk;
-        Seg g;
-        begin(walk);
-        for (; ok; ++ns) {
-            const int more = walk.next(p, a, pl, g);
-            if (!__shfl_sync(~0u, more, 0)) break;
-            const int qs = ns % Gm::NQ, n = __shfl_sync(~0u, g.j1 - g.j0, 0);
-            if (!wait(&sm.q_full[qs], (ns / Gm::NQ) & 1)) break;
-            if (PAIR) {
-                // group w's tiles are x < hi[w]
-                const int hi0 = __shfl_sync(~0u, min(group_tiles<PAIR>(g, pl, 0), g.j1) - g.j0, 0);
-                const int hi1 = __shfl_sync(~0u, min(group_tiles<PAIR>(g, pl, 1), g.j1) - g.j0, 0);
-                if (!wait(&sm.full[st], ph)) break;
-                if (0 < hi0) qk(0, qs, st);
-                if (ok && 0 < hi1) qk(1, qs, st);
-                if (!ok) break;
-                release(&sm.empty[st]);
-                if (n == 1) release(&sm.q_empty[qs]);
-                st = slot_after(st), ph ^= st == 0;
-                for (int x = 0; ok && x < n; ++x) {
-                    const int v = st, k = slot_after(st);
-                    const int kph = ph ^ (k == 0);
-                    if (!wait(&sm.full[v], ph)) break;
-                    if (x < hi0) pv(0, v, x > 0, x + 1 == hi0);
-                    if (ok && x + 1 < n) wait(&sm.full[k], kph);
-                    if (ok && x + 1 < hi0) qk(0, qs, k);
-                    if (ok && x < hi1) pv(1, v, x > 0, x + 1 == hi1);
+                for (int kk = 1; kk < TN / 16; ++kk)
+                    mma_ts(leader, to, tp + (uint32_t)(kk * 8), va + (uint32_t)(kk * (16 * 128 / 16)), v_hi,
+                           IDESC_PV, 1u);
+                if (last) commit(leader, &sm.o_done[w]);
+            };
+            auto release = [&](uint64_t* bar) { commit(leader, bar); };
+            TileWalk walk;
+            Seg g;
+            begin(walk);
+            for (; ok; ++ns) {
+                const int more = walk.next(p, a, pl, g);
+                if (!__shfl_sync(~0u, more, 0)) break;
+                const int qs = ns % Gm::NQ, n = __shfl_sync(~0u, g.j1 - g.j0, 0);
+                if (!wait(&sm.q_full[qs], (ns / Gm::NQ) & 1)) break;
+                if (PAIR) {
+                    // group w's tiles are x < hi[w]
+                    const int hi0 = __shfl_sync(~0u, min(group_tiles<PAIR>(g, pl, 0), g.j1) - g.j0, 0);
+                    const int hi1 = __shfl_sync(~0u, min(group_tiles<PAIR>(g, pl, 1), g.j1) - g.j0, 0);
+                    if (!wait(&sm.full[st], ph)) break;
+                    if (0 < hi0) qk(0, qs, st);
+                    if (ok && 0 < hi1) qk(1, qs, st);
                     if (!ok) break;
-                    release(&sm.empty[v]);
-                    st = k, ph = kph;
-                    if (x + 1 < n) {
-                        if (x + 1 < hi1) qk(1, qs, k);
+                    release(&sm.empty[st]);
+                    if (n == 1) release(&sm.q_empty[qs]);
+                    st = slot_after(st), ph ^= st == 0;
+                    for (int x = 0; ok && x < n; ++x) {
+                        const int v = st, k = slot_after(st);
+                        const int kph = ph ^ (k == 0);
+                        if (!wait(&sm.full[v], ph)) break;
+                        if (x < hi0) pv(0, v, x > 0, x + 1 == hi0);
+                        if (ok && x + 1 < n) wait(&sm.full[k], kph);
+                        if (ok && x + 1 < hi0) qk(0, qs, k);
+                        if (ok && x < hi1) pv(1, v, x > 0, x + 1 == hi1);
                         if (!ok) break;
-                        release(&sm.empty[k]);
-                        if (x + 2 == n) release(&sm.q_empty[qs]);
-                        st = slot_after(k), ph = kph ^ (st == 0);
+                        release(&sm.empty[v]);
+                        st = k, ph = kph;
+                        if (x + 1 < n) {
+                            if (x + 1 < hi1) qk(1, qs, k);
+                            if (!ok) break;
+                            release(&sm.empty[k]);
+                            if (x + 2 == n) release(&sm.q_empty[qs]);
+                            st = slot_after(k), ph = kph ^ (st == 0);
+                        }
                     }
-                }
-            } else {
-                for (int x = 0; x < min(n, 2); ++x) {
-                    if (!wait(&sm.full[st], ph)) break;
-                    qk(x, qs, st);
-                    if (!ok) break;
-                    release(&sm.empty[st]);
-                    if (x + 1 == n) release(&sm.q_empty[qs]);
-                    st = slot_after(st), ph ^= st == 0;
-                }
-                for (int x = 0; ok && x < n; ++x) {
-                    if (!wait(&sm.full[st], ph)) break;
-                    pv(x & 1, st, x > 1, x + 2 >= n);
-                    if (!ok) break;
-                    release(&sm.empty[st]);
-                    st = slot_after(st), ph ^= st == 0;
-                    if (x + 2 < n) {
+                } else {
+                    for (int x = 0; x < min(n, 2); ++x) {
                         if (!wait(&sm.full[st], ph)) break;
-                        qk(x & 1, qs, st);
+                        qk(x, qs, st);
                         if (!ok) break;
                         release(&sm.empty[st]);
-                        if (x + 3 == n) release(&sm.q_empty[qs]);
+                        if (x + 1 == n) release(&sm.q_empty[qs]);
                         st = slot_after(st), ph ^= st == 0;
+                    }
+                    for (int x = 0; ok && x < n; ++x) {
+                        if (!wait(&sm.full[st], ph)) break;
+                        pv(x & 1, st, x > 1, x + 2 >= n);
+                        if (!ok) break;
+                        release(&sm.empty[st]);
+                        st = slot_after(st), ph ^= st == 0;
+                        if (x + 2 < n) {
+                            if (!wait(&sm.full[st], ph)) break;
+                            qk(x & 1, qs, st);
+                            if (!ok) break;
+                            release(&sm.empty[st]);
+                            if (x + 3 == n) release(&sm.q_empty[qs]);
+                            st = slot_after(st), ph ^= st == 0;
+                        }
                     }
                 }
             }
+            if (!ok && lane == 0) {
+                sm.abort_flag = 1;
+                raise_status(status, TGVKV_STATUS_TIMEOUT);
+            }
+            __syncwarp();
+            // every MMA this CTA issued has finished before TMEM is released
+            release(&sm.mma_done);
+            warp_wait(&sm.mma_done, 0, &sm.never);
         }
-        if (!ok && lane == 0) {
-            sm.abort_flag = 1;
-            raise_status(status, TGVKV_STATUS_TIMEOUT);
-        }
-        __syncwarp();
-        // every MMA this CTA issued has finished before TMEM is released
-        release(&sm.mma_done);
-        warp_wait(&sm.mma_done, 0, &sm.never);
-    }
 
     } else if (warp < kConvWarp) {
         // -------------------------------------------------------- softmax
@@ -653,7 +653,7 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
         const int ri = r / p.G, rh = r - ri * p.G;           // token within the tile, head
         int ns = 0, nso = 0, npart = 0, base_it = 0;
         bool ok = true;
-        if (warp == kSoftWarp && lane == 0) split[share] = SplitItem{-1, 0, 0, 0};
+        if (warp == kSoftWarp && lane == 0 && share < (int)gridDim.x) split[share] = SplitItem{-1, 0, 0, 0};
         auto& at = sm.at[warp - kSoftWarp];
         const volatile Seg& g = at.g;
         if (lane == 0) begin(at.walk);

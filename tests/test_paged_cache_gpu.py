@@ -117,6 +117,7 @@ class Box:
 
 
 FORMATS = ["bf16", "int8", "int4"]
+TIMEOUT = 0x20
 
 
 # ---- writing and reading -------------------------------------------------------
@@ -494,3 +495,44 @@ def test_another_stream_and_graph_replay(api):
         box.k[s] = np.concatenate([box.k[s], R.round_trip(kv[0][b:b + 1, g], "int8")])
         box.v[s] = np.concatenate([box.v[s], R.round_trip(kv[1][b:b + 1, g], "int8")])
     box.check([1] * B, q, R.bf16_values(host_bits(out)).reshape(B, H_q, d))
+
+
+def test_a_workspace_that_was_not_initialised_is_reported(api):
+    """Counters that are not at zero give no CTA a share: nothing is read or written out
+    of range, the status says so, and an initialisation makes the workspace good."""
+    box = Box(api, 3, 8, 2, 128, 32, "int8", 400)
+    box.fill([300, 250, 400, 90, 200, 333])
+    news = [40, 40, 40]
+    q = torch.randn(120, 8, 128, device="cuda").bfloat16()
+    off = torch.tensor([0, 40, 80, 120], dtype=torch.int32, device="cuda")
+    out = torch.zeros(120, 8, 128, dtype=torch.bfloat16, device="cuda")
+    box.ws.fill_(0x7F)
+    box.ws[:4] = 0
+    api.tgvkv_chunk_attention(box.desc, box.cache, box.table, box.lens_t(box.lens), q, off, 40, out,
+                              box.ws)
+    assert api.tgvkv_status(box.ws) == TIMEOUT
+    assert (out == 0).all()
+    api.tgvkv_cache_workspace_init(box.desc, box.ws)
+    q, got = box.attend(news)
+    box.check(news, q, got)
+
+
+@pytest.mark.parametrize("fmt,page_bytes", [("bf16", 65536), ("int8", 32768), ("int4", 16384)])
+def test_pools_past_32_bits(api, fmt, page_bytes):
+    """Pages on either side of byte 2^32 (and element 2^31) of a pool."""
+    d, page = 128, 256
+    edge = 2 ** 32 // page_bytes
+    box = Box(api, 2, 16, 2, d, page, fmt, 700, spare=edge + 16)
+    far = np.arange(box.S * box.max_pages).reshape(box.S, -1)
+    box.table_np = np.where(far % 3 == 0, far, edge + far).astype(np.int32)
+    box.table = torch.from_numpy(box.table_np).cuda()
+    box.fill([700, 300, 513, 256])
+    for news in ([1, 1], [2, 0], [30, 41]):
+        q, got = box.attend(news)
+        box.check(news, q, got)
+    off = torch.tensor([0, 700, 1000, 1513, 1769], dtype=torch.int64, device="cuda")
+    k, v = (torch.empty(1769, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    api.tgvkv_cache_read(box.desc, box.cache, box.table, None, off, k, v, box.ws)
+    assert api.tgvkv_status(box.ws) == 0
+    assert np.array_equal(R.bf16_values(host_bits(k)), np.concatenate(box.k).astype(np.float32))
+    assert np.array_equal(R.bf16_values(host_bits(v)), np.concatenate(box.v).astype(np.float32))
