@@ -149,13 +149,13 @@ struct TileGeom {
     static constexpr int NRAW = QUANT ? (FMT == TGVKV_CACHE_INT8 ? 3 : 6) : 0;
     static constexpr int NQ = PAIR ? 1 : 2;                       // Q slots
     static constexpr int QT = PAIR ? 2 : 1;                       // row tiles a slot
-    static constexpr int CW = QUANT ? 4 : 0;                      // converter warps
+    static constexpr int CW = QUANT ? 8 : 0;                      // converter warps
     static constexpr int THREADS = 32 * (kConvWarp + CW);
     // registers a thread: at launch (the most that the thread count allows), then by
     // role.  The roles' sum is at most the launch's: what setmaxnreg raises one by has
     // to come from the others.
-    static constexpr int LAUNCH_REGS = QUANT ? 128 : 168;
-    static constexpr int FEW_REGS = 72, CONV_REGS = 80, SOFT_REGS = QUANT ? 176 : 208;
+    static constexpr int LAUNCH_REGS = QUANT ? 96 : 168;
+    static constexpr int FEW_REGS = QUANT ? 64 : 72, CONV_REGS = 40, SOFT_REGS = QUANT ? 168 : 208;
     static_assert(128 * FEW_REGS + 256 * SOFT_REGS + 32 * CW * CONV_REGS <= THREADS * LAUNCH_REGS,
                   "register split");
 };
@@ -239,6 +239,7 @@ struct TileSmem {
     uint32_t tmem_base;
     int abort_flag, never;
     int filled[Gm::QUANT ? Gm::NRAW : Gm::NST];       // the last copy into each slot (-1: none)
+    int live[Gm::QUANT ? Gm::NRAW : 1];               // and the slots of the set in it
     long long warp_sum[Gm::THREADS / 32];
     int start_s, start_u, start_j, share;
 };
@@ -265,6 +266,19 @@ __device__ __forceinline__ int v_place(int x, int n) {
 
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort) {
     return __all_sync(~0u, tc::mbar_wait(bar, parity, abort));
+}
+
+// Whether the phase with the given parity is complete: no wait.
+__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+    return ok != 0;
 }
 
 // A warp's part of a record is written / is awaited and taken (the flag is down
@@ -466,6 +480,7 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
                     if (QUANT) {
                         if (lane == 0) {
                             sm.filled[st] = it;
+                            sm.live[st] = min(g.sp.len - slot0, TN);
                             tc::mbar_arrive_expect_tx(&sm.raw_full[st],
                                                       (uint32_t)(nb * box) * (Gm::ROWB + D / kGroup));
                         }
@@ -927,62 +942,51 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
         regs_down<Gm::CONV_REGS>();
         // A thread converts 8 consecutive values of every RSTEP-th row; RSTEP is a
         // multiple of 8, so the swizzle is the same in all of them.
-        constexpr int T = Gm::CW * 32, UPR = D / 8, RSTEP = T / UPR, PER = TN / RSTEP;
-        constexpr int BATCH = PER < 8 ? PER : 8;
-        static_assert(RSTEP % 8 == 0 && PER % BATCH == 0, "converter threads");
+        constexpr int T = Gm::CW * 32, UPR = D / 8, RSTEP = T / UPR, PER = TN / RSTEP, BATCH = PER / 2;
+        static_assert(RSTEP % 8 == 0 && TN % RSTEP == 0 && PER % BATCH == 0, "converter threads");
         const int ct = tid - kConvWarp * 32, u = ct % UPR, r0 = ct / UPR;
         const int src = ct * (FMT == TGVKV_CACHE_INT8 ? 8 : 4), sc0 = r0 * (D / kGroup) + (u >> 2);
         const int dst0 = (u >> 3) * Gm::HALF + r0 * 128 + (((u & 7) ^ (r0 & 7)) << 4);
-        int it = 0;
         bool ok = true;
-        TileWalk walk;
-        Seg g;
-        begin(walk);
-        while (ok && walk.next(p, a, pl, g)) {
-            const int n = g.j1 - g.j0;
-            int kx = 0, vx = 0;
-            for (int i = 0; ok && i < 2 * n; ++i, ++it) {
-                const bool is_v = vx < kx && i == v_place<PAIR>(vx, n);
-                const int x = is_v ? vx++ : kx++;
-                const int live = min(g.sp.len - (g.j0 + x) * TN, TN);
-                const int rs = it % NRAW, st = it % NST;
-                if (!warp_wait(&sm.raw_full[rs], (it / NRAW) & 1, abort_flag) ||
-                    !warp_wait(&sm.empty[st], ((it / NST) & 1) ^ 1, abort_flag)) {
-                    ok = false;
-                    break;
-                }
-                const unsigned char* raw = sm.raw[rs] + src;
-                const unsigned char* sc = sm.sc[rs] + sc0;
-                unsigned char* dst = sm.kv[st] + dst0;
+        for (int it = 0; it < 2 * count; ++it) {         // K and V tiles in the ring's order
+            const int rs = it % NRAW, st = it % NST;
+            if (!warp_wait(&sm.raw_full[rs], (it / NRAW) & 1, abort_flag) ||
+                !warp_wait(&sm.empty[st], ((it / NST) & 1) ^ 1, abort_flag)) {
+                ok = false;
+                break;
+            }
+            const unsigned char* raw = sm.raw[rs] + src;
+            const unsigned char* sc = sm.sc[rs] + sc0;
+            unsigned char* dst = sm.kv[st] + dst0;
+            const int live = sm.live[rs];
 #pragma unroll
-                for (int b0 = 0; b0 < PER; b0 += BATCH) {
-                    // a batch's loads before its stores: they cannot pass one another
-                    uint2 c[BATCH];
-                    uint32_t byte[BATCH];
+            for (int b0 = 0; b0 < PER; b0 += BATCH) {
+                // a batch's loads before its stores: they cannot pass one another
+                uint2 c[BATCH];
+                uint32_t byte[BATCH];
 #pragma unroll
-                    for (int b = 0; b < BATCH; ++b) {
-                        const int e = b0 + b;
-                        c[b] = make_uint2(0u, 0u);
-                        if (FMT == TGVKV_CACHE_INT8)
-                            c[b] = *reinterpret_cast<const uint2*>(raw + e * T * 8);
-                        else
-                            c[b].x = *reinterpret_cast<const uint32_t*>(raw + e * T * 4);
-                        byte[b] = sc[e * RSTEP * (D / kGroup)];
-                    }
+                for (int b = 0; b < BATCH; ++b) {
+                    const int e = b0 + b;
+                    c[b] = make_uint2(0u, 0u);
+                    if (FMT == TGVKV_CACHE_INT8)
+                        c[b] = *reinterpret_cast<const uint2*>(raw + e * T * 8);
+                    else
+                        c[b].x = *reinterpret_cast<const uint32_t*>(raw + e * T * 4);
+                    byte[b] = sc[e * RSTEP * (D / kGroup)];
+                }
 #pragma unroll
-                    for (int b = 0; b < BATCH; ++b) {
-                        uint4 v = codes_to_bf16<FMT>(c[b], byte[b], p.magic);
-                        // past the set's end
-                        if (live < TN && r0 + (b0 + b) * RSTEP >= live) v = make_uint4(0u, 0u, 0u, 0u);
-                        *reinterpret_cast<uint4*>(dst + (b0 + b) * RSTEP * 128) = v;
-                    }
+                for (int b = 0; b < BATCH; ++b) {
+                    uint4 v = codes_to_bf16<FMT>(c[b], byte[b], p.magic);
+                    // past the set's end
+                    if (live < TN && r0 + (b0 + b) * RSTEP >= live) v = make_uint4(0u, 0u, 0u, 0u);
+                    *reinterpret_cast<uint4*>(dst + (b0 + b) * RSTEP * 128) = v;
                 }
-                tc::fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) {
-                    tc::mbar_arrive(&sm.full[st]);
-                    tc::mbar_arrive(&sm.raw_empty[rs]);
-                }
+            }
+            tc::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                tc::mbar_arrive(&sm.full[st]);
+                tc::mbar_arrive(&sm.raw_empty[rs]);
             }
         }
         if (!ok) {
