@@ -93,13 +93,17 @@ __device__ __forceinline__ int tiles_seen(const SetSpan& sp, int tok_end) {
     return vis <= 0 ? 0 : (vis + TN - 1) / TN;
 }
 
-// Units of a set: the key tiles of all its items.
-__device__ __forceinline__ long long set_units(const SetSpan& sp, const TilePlan& pl) {
-    long long sum = 0;
-    for (int t = 0; t < sp.n; t += pl.tpi) sum += tiles_seen(sp, t + pl.tpi);
-    return sum;
+// An item's units of work: its key tiles, and `start` for what its start and end cost.
+__device__ __forceinline__ int item_units(int tiles, int start) {
+    return tiles > 0 ? tiles + start : 0;
 }
 
+// Units of a set, of all its items.
+__device__ __forceinline__ long long set_units(const SetSpan& sp, const TilePlan& pl, int start) {
+    long long sum = 0;
+    for (int t = 0; t < sp.n; t += pl.tpi) sum += item_units(tiles_seen(sp, t + pl.tpi), start);
+    return sum;
+}
 
 // Joins the records of one query row (record i at rec(i), the row is row r of its
 // rec_rows), by WPR warps: warp wr takes every WPR-th batch of 8 and the warps'

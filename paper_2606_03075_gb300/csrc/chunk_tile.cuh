@@ -149,6 +149,11 @@ struct TileGeom {
     static constexpr int NRAW = QUANT ? (FMT == TGVKV_CACHE_INT8 ? 3 : 6) : 0;
     static constexpr int NQ = PAIR ? 1 : 2;                       // Q slots
     static constexpr int QT = PAIR ? 2 : 1;                       // row tiles a slot
+    // What an item's start and end cost, in key tiles: the shares are of equal cost.  SPLIT
+    // (the groups' join besides): 256 sets of 96 tokens over 0 .. 3104 slots take (int8, us)
+    // 68.6 at 0, 67.6 at 2, 64.5 at 3, 66.6 at 4; at d = 64 54.3, 53.1, 49.2, 52.2 and 48.2 at 6.
+    // PAIR: 16 sequences' 500-token chunks over 2000 slots 125 at 0, 114 at 2, 112 at 3.
+    static constexpr int START = PAIR || D == 128 ? 3 : 6;
     static constexpr int CW = QUANT ? 8 : 0;                      // converter warps
     static constexpr int THREADS = 32 * (kConvWarp + CW);
     // registers a thread: at launch (the most that the thread count allows), then by
@@ -178,6 +183,7 @@ struct Seg {
     bool starts;                       // begins the CTA's share
 };
 
+template <int START>
 struct TileWalk {
     SetSpan sp;
     int s, u, j, left;
@@ -194,29 +200,33 @@ struct TileWalk {
     }
     __device__ __forceinline__ bool next(const CacheProblem& p, const ChunkArgs& a,
                                          const TilePlan& pl, Seg& g) {
-        if (left <= 0) return false;
-        int nk = tiles_seen(sp, (u + 1) * pl.tpi);
-        while (u * pl.tpi >= sp.n || j >= nk) {
-            j = 0;
-            if (u * pl.tpi >= sp.n || ++u * pl.tpi >= sp.n) {
-                u = 0;
-                if (++s >= p.S) return false;
-                sp = set_span(p, a, s);
+        while (left > 0) {
+            int nk = tiles_seen(sp, (u + 1) * pl.tpi);
+            while (u * pl.tpi >= sp.n || j >= item_units(nk, START)) {
+                j = 0;
+                if (u * pl.tpi >= sp.n || ++u * pl.tpi >= sp.n) {
+                    u = 0;
+                    if (++s >= p.S) return false;
+                    sp = set_span(p, a, s);
+                }
+                nk = tiles_seen(sp, (u + 1) * pl.tpi);
             }
-            nk = tiles_seen(sp, (u + 1) * pl.tpi);
+            const int j1 = min(item_units(nk, START), j + left);
+            g.j0 = max(j - START, 0);
+            g.j1 = j1 - START;
+            left -= j1 - j;
+            j = j1;
+            if (g.j1 <= g.j0) continue;
+            g.sp = sp;
+            g.s = s;
+            g.u = u;
+            g.nk = nk;
+            g.tok0 = u * pl.tpi;
+            g.starts = first;
+            first = false;
+            return true;
         }
-        g.sp = sp;
-        g.s = s;
-        g.u = u;
-        g.j0 = j;
-        g.j1 = min(nk, j + left);
-        g.nk = nk;
-        g.tok0 = u * pl.tpi;
-        g.starts = first;
-        first = false;
-        left -= g.j1 - g.j0;
-        j = g.j1;
-        return true;
+        return false;
     }
 };
 
@@ -233,7 +243,7 @@ struct TileSmem {
     uint64_t join_in, join_out, mma_done;
     float2 ml[PAIR ? 1 : 2][PAIR ? 1 : TM];           // SPLIT: the groups' (m, l)
     struct {                                          // a softmax warp's place in the work:
-        TileWalk walk;                                // here, as its registers hold S
+        TileWalk<Gm::START> walk;                     // here, as its registers hold S
         Seg g;
     } at[8];
     uint32_t tmem_base;
@@ -241,7 +251,7 @@ struct TileSmem {
     int filled[Gm::QUANT ? Gm::NRAW : Gm::NST];       // the last copy into each slot (-1: none)
     int live[Gm::QUANT ? Gm::NRAW : 1];               // and the slots of the set in it
     long long warp_sum[Gm::THREADS / 32];
-    int start_s, start_u, start_j, share;
+    int start_s, start_u, start_j, share, tiles;
 };
 
 // Row tile w of a segment's item (PAIR), or its one row tile: its key tiles.
@@ -308,7 +318,7 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
                   uint32_t* __restrict__ sync, uint32_t* __restrict__ status) {
     using Gm = TileGeom<D, FMT, PAIR>;
     constexpr bool QUANT = Gm::QUANT;
-    constexpr int NST = Gm::NST, NRAW = QUANT ? Gm::NRAW : 1;
+    constexpr int NST = Gm::NST, NRAW = QUANT ? Gm::NRAW : 1, START = Gm::START;
     griddep_launch_dependents();
     extern __shared__ unsigned char smem_raw[];
     const uint32_t raw_addr = smem_u32(smem_raw);
@@ -319,6 +329,7 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
     if (tid == 0) {
         sm.abort_flag = 0;
         sm.never = 0;
+        sm.tiles = 0;
         sm.share = take_share(sync, status);
         for (int i = 0; i < (QUANT ? NRAW : NST); ++i) sm.filled[i] = -1;
         for (int i = 0; i < NST; ++i) {
@@ -357,7 +368,7 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
     const int run = (p.S + Gm::THREADS - 1) / Gm::THREADS;    // sets a thread sums
     const int s_lo = min(tid * run, p.S), s_hi = min(s_lo + run, p.S);
     long long sum = 0;
-    for (int s = s_lo; s < s_hi; ++s) sum += set_units(set_span(p, a, s), pl);
+    for (int s = s_lo; s < s_hi; ++s) sum += set_units(set_span(p, a, s), pl, START);
     long long incl = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -376,27 +387,33 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
     const int share = sm.share;        // written before the barrier above
     const long long c0 = share * per;
     const int count = (int)max(min(total - c0, per), 0ll);
-    if (count > 0 && c0 >= base && c0 < base + sum) {   // the first unit is in my sets
-        long long at = c0 - base;
+    if (c0 < base + sum && c0 + count > base) {          // my sets hold some of them
+        int tiles = 0;
+        long long at = base - c0;      // the item's first unit, counted from the share's
         for (int s = s_lo; s < s_hi; ++s) {
             const SetSpan sp = set_span(p, a, s);
             for (int u = 0; u * pl.tpi < sp.n; ++u) {
-                const int nk = tiles_seen(sp, (u + 1) * pl.tpi);
-                if (at >= 0 && at < nk) {
-                    sm.start_s = s;
-                    sm.start_u = u;
-                    sm.start_j = (int)at;
+                const int n = item_units(tiles_seen(sp, (u + 1) * pl.tpi), START);
+                const long long lo = max(at, 0ll), hi = min(at + n, (long long)count);
+                if (lo < hi) {
+                    tiles += (int)(max(hi - at - START, 0ll) - max(lo - at - START, 0ll));
+                    if (lo == 0) {
+                        sm.start_s = s;
+                        sm.start_u = u;
+                        sm.start_j = (int)-at;
+                    }
                 }
-                at -= nk;
+                at += n;
             }
         }
+        if (tiles > 0) atomicAdd(&sm.tiles, tiles);
     }
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
     const uint32_t tmem = sm.tmem_base;
     volatile int* abort_flag = &sm.abort_flag;
-    auto begin = [&](TileWalk& walk) {
+    auto begin = [&](TileWalk<START>& walk) {
         walk.init(p, a, count > 0 ? sm.start_s : 0, count > 0 ? sm.start_u : 0,
                   count > 0 ? sm.start_j : 0, count);
     };
@@ -419,7 +436,7 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
             const int b = lane & 15;
             int base_it = 0, ns = 0, nq[2] = {0, 0};
             bool ok = true;
-            TileWalk walk;
+            TileWalk<START> walk;
             Seg g;
             begin(walk);
             for (; ok && walk.next(p, a, pl, g); ++ns) {
@@ -582,7 +599,7 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
                 if (last) commit(leader, &sm.o_done[w]);
             };
             auto release = [&](uint64_t* bar) { commit(leader, bar); };
-            TileWalk walk;
+            TileWalk<START> walk;
             Seg g;
             begin(walk);
             for (; ok; ++ns) {
@@ -869,18 +886,15 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
             for (int c = 0; c < COLS; c += CC) {
                 float t[CC];
 #pragma unroll
-                for (int cc = 0; cc < CC; cc += 16) {
-                    uint32_t u[16];
-                    tmem_ld16(lanes + kOCol + (uint32_t)((PAIR ? w * D : 0) + col0 + c + cc), u);
+                for (int cc = 0; cc < CC; cc += 32) {
+                    float o0[32], o1[32];
+                    tc::tmem_ld32(lanes + kOCol + (uint32_t)((PAIR ? w * D : 0) + col0 + c + cc), o0);
+                    if (!PAIR) tc::tmem_ld32(lanes + kOCol + (uint32_t)(D + col0 + c + cc), o1);
                     tc::tmem_wait_ld();
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) t[cc + e] = has0 ? __uint_as_float(u[e]) * f0 : 0.f;
-                    if (!PAIR) {
-                        tmem_ld16(lanes + kOCol + (uint32_t)(D + col0 + c + cc), u);
-                        tc::tmem_wait_ld();
-#pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            t[cc + e] += has1 ? __uint_as_float(u[e]) * f1 : 0.f;
+                    for (int e = 0; e < 32; ++e) {
+                        t[cc + e] = has0 ? o0[e] * f0 : 0.f;
+                        if (!PAIR) t[cc + e] += has1 ? o1[e] * f1 : 0.f;
                     }
                 }
                 const int k0 = (col0 + c) / 4;
@@ -948,7 +962,8 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
         const int src = ct * (FMT == TGVKV_CACHE_INT8 ? 8 : 4), sc0 = r0 * (D / kGroup) + (u >> 2);
         const int dst0 = (u >> 3) * Gm::HALF + r0 * 128 + (((u & 7) ^ (r0 & 7)) << 4);
         bool ok = true;
-        for (int it = 0; it < 2 * count; ++it) {         // K and V tiles in the ring's order
+        const int tiles = 2 * sm.tiles;
+        for (int it = 0; it < tiles; ++it) {             // K and V tiles in the ring's order
             const int rs = it % NRAW, st = it % NST;
             if (!warp_wait(&sm.raw_full[rs], (it / NRAW) & 1, abort_flag) ||
                 !warp_wait(&sm.empty[st], ((it / NST) & 1) ^ 1, abort_flag)) {
