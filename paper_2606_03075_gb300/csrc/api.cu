@@ -389,7 +389,7 @@ CacheLayout cache_layout(const CacheProblem& p) {
     o += round_up(sizeof(SplitItem) * kTileMaxCtas);
     w.part = o;
     // two records per stream, or per CTA and row tile of a pair
-    const size_t stream = 2 * (size_t)kStreamMax * chunk_record_floats(kStreamRows, p.d);
+    const size_t stream = 2 * (size_t)kStreamMaxCtas * 8 * chunk_record_floats(kStreamRows, p.d);
     const size_t tile = 4 * (size_t)kTileMaxCtas * chunk_record_floats(TM, p.d);
     o += round_up(sizeof(float) * std::max(stream, tile));
     w.total = o;
@@ -856,7 +856,7 @@ int tgvkv_chunk_attention(const tgvkv_cache_desc* desc, const tgvkv_cache_pools*
     uint32_t* status = static_cast<uint32_t*>(workspace);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     cudaError_t e;
-    if ((long long)a.max_q * p.G <= kStreamRows) {
+    if ((long long)a.max_q * p.G <= stream_rows(p.d, p.format)) {
         e = launch_chunk_stream(p, pl, a, part, plan, status, st);
     } else {
         const bool pair = a.max_q > TM / p.G;   // some chunk has more than one row tile

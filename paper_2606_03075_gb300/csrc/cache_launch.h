@@ -22,7 +22,7 @@ cudaError_t launch_cache_read(const CacheProblem& p, const CachePools& pool,
                               long long rows, uint32_t* status, cudaStream_t stream);
 
 // Attention of a chunk of new tokens: the row-stream kernel, for sets of at most
-// kStreamRows query rows (max_q * G; chunk_stream.cu), and the tile kernel for
+// stream_rows() query rows (max_q * G; chunk_stream.cu), and the tile kernel for
 // larger ones, `pair`: two row tiles an item (chunk_tile.cuh), with its merge
 // (chunk_merge.cu).  plan: S + 1 entries; split: one per CTA; sync: kTileSync words,
 // zero at the start and left zero; part: the split sets' records.

@@ -53,8 +53,17 @@ __host__ __device__ inline int chunk_record_floats(int rows, int d) {
     return rows * d + ((2 * rows + 3) & ~3);
 }
 
-constexpr int kStreamMax = 2560;       // streams of the row-stream kernel
-constexpr int kStreamRows = 16;        // query rows it takes a set
+constexpr int kStreamMaxCtas = 160;    // CTAs of the row-stream kernel
+constexpr int kStreamRows = 32;        // query rows a set that it takes at most
+
+// Query rows a set up to which the row-stream kernel takes a call.  Where it still has
+// the registers it does without the tile kernel's 128-row tiles and the bf16 copy of
+// integer codes: 256 sets of 20 rows over 0 .. 4101 slots, tile kernel against it
+// (us): d = 64 bf16 50 / 45, int8 62 / 45, int4 62 / 42 (32 rows 50 / 49, 62 / 54,
+// 61 / 50); d = 128 bf16 75 / 78, int8 80 / 78, int4 82 / 60.
+__host__ __device__ constexpr int stream_rows(int d, int format) {
+    return d == 64 ? kStreamRows : format == TGVKV_CACHE_BF16 ? 16 : 24;
+}
 constexpr int kTileMaxCtas = 160;      // CTAs of the tile kernel
 constexpr int TM = 128;                // query rows of its row tiles
 constexpr int TN = 128;                // slots of its key tiles

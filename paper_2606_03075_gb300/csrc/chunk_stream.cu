@@ -1,14 +1,14 @@
 // Attention of a few new tokens over the paged cache (a decode step, drafted
-// tokens): the query rows of a set, n tokens x G heads, fit one 16-row tile.
+// tokens): up to 32 query rows a set, n tokens x G heads (stream_rows()).
 //
 //   o[t][h] = sum_{j <= len - n + i} softmax_j(scale <q[t][h], k_j>) v_j
 //
 // for token i of the n new tokens of its sequence (t = its row of q), over the
 // slots j of set (b, h / G).  A row that sees no slot gives 0.
 //
-// HBM-bound: each slot's K and V row is read once, for up to 16 query rows (4
-// d * 16 flops against 4 d bytes at most, far below the 278 flops a byte where
-// the tensor cores would bound).  The sets' slots form one sequence of chunks
+// Each slot's K and V row is read once, for all query rows of its set (4 d * 32
+// flops against 4 d bytes at most, far below the 278 flops a byte where the
+// tensor cores would bound): what is left is to keep the reads in flight.  The sets' slots form one sequence of chunks
 // (CH slots, never across a set); each warp of a persistent CTA takes one
 // contiguous share of it, so ragged lengths and long caches split evenly.  A
 // chunk moves as whole page slices by TMA into the warp's own two-stage ring,
@@ -46,11 +46,12 @@ struct StreamGeom {
     // Streams (warps) per CTA and bytes of a chunk's K.  8 streams of 4 KB, but for integer
     // caches of 64 dims and up to 8 query rows, whose loop has the registers for 16
     // streams of 2 KB: 32 layers x 32 heads x 2257 slots of int4 take 55 us instead of 62.
-    // (128 dims: 16 streams of 2 KB 92 us, 8 of 4 KB 86 us.)
+    // (128 dims: 16 streams of 2 KB 92 us, 8 of 4 KB 86 us.)  24 rows of 128 dims leave
+    // the integer caches room for 2 KB only.
     static constexpr bool MANY = QUANT && NB == 1 && D == 64;
     static constexpr int W = MANY ? 16 : 8;
-    static constexpr int TB = MANY ? 2048 : 4096;
-    static constexpr int CH = TB / ROWB > 64 ? 64 : TB / ROWB < 16 ? 16 : TB / ROWB;                // slots per chunk
+    static constexpr int TB = MANY || (QUANT && NB > 2 && D == 128) ? 2048 : 4096;
+    static constexpr int CH = TB / ROWB > 64 ? 64 : TB / ROWB < 16 ? 16 : TB / ROWB;   // slots a chunk
     static constexpr int KT = QUANT ? 1 : D / 64; // tiles of a row
     static constexpr int TROW = ROWB / KT;        // bytes of a tile's row
     static constexpr int kTile = CH * TROW;
@@ -744,7 +745,7 @@ cudaError_t launch_stream(const CacheProblem& p, const CachePools& pool, const C
     if (e != cudaSuccess) return e;
     const int sms = device_sm_count();
     if (sms <= 0) return cudaErrorInvalidDevice;
-    const int ctas = sms < kStreamMax / Gm::W ? sms : kStreamMax / Gm::W;
+    const int ctas = sms < kStreamMaxCtas ? sms : kStreamMaxCtas;
     const int rec_rows = a.max_q * p.G;
     chunk_stream_kernel<D, FMT, NB><<<ctas, Gm::W * 32, smem, stream>>>(
         mk, mv, p, pool, a, box, box_shift, kMinChunks, rec_rows, part, plan, status);
@@ -763,8 +764,14 @@ cudaError_t launch_stream(const CacheProblem& p, const CachePools& pool, const C
 template <int D, int FMT>
 cudaError_t launch_rows(const CacheProblem& p, const CachePools& pool, const ChunkArgs& a,
                         float* part, long long* plan, uint32_t* status, cudaStream_t stream) {
-    return a.max_q * p.G <= 8 ? launch_stream<D, FMT, 1>(p, pool, a, part, plan, status, stream)
-                              : launch_stream<D, FMT, 2>(p, pool, a, part, plan, status, stream);
+    const int rows = a.max_q * p.G;    // at most stream_rows(D, FMT)
+    constexpr int most = stream_rows(D, FMT);
+    if (rows <= 8) return launch_stream<D, FMT, 1>(p, pool, a, part, plan, status, stream);
+    if (rows <= 16) return launch_stream<D, FMT, 2>(p, pool, a, part, plan, status, stream);
+    if constexpr (most > 24)
+        if (rows > 24) return launch_stream<D, FMT, 4>(p, pool, a, part, plan, status, stream);
+    if constexpr (most > 16) return launch_stream<D, FMT, 3>(p, pool, a, part, plan, status, stream);
+    return cudaErrorInvalidValue;
 }
 
 }  // namespace

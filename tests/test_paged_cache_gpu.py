@@ -536,3 +536,20 @@ def test_pools_past_32_bits(api, fmt, page_bytes):
     assert api.tgvkv_status(box.ws) == 0
     assert np.array_equal(R.bf16_values(host_bits(k)), np.concatenate(box.k).astype(np.float32))
     assert np.array_equal(R.bf16_values(host_bits(v)), np.concatenate(box.v).astype(np.float32))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("H_q,H_kv,most", [(8, 2, 6), (8, 2, 8), (7, 1, 3), (2, 2, 17), (2, 2, 25), (2, 2, 33),
+                                           (16, 1, 2), (12, 1, 2)])
+def test_a_few_tokens_of_17_to_33_rows(api, fmt, d, H_q, H_kv, most):
+    """Around the largest calls of the kernel for few rows: ragged tokens, idle
+    sequences, sets shorter than their tokens, and sets split over many streams."""
+    news = [most, 0, 1, most - 1, most, 2]
+    box = Box(api, 6, H_q, H_kv, d, 16, fmt, 3000)
+    lens = [1700, most - 1, 1, 65, most // 2, 3000, 90, 0, 128, 400, most, 2][:6 * H_kv]
+    box.fill(lens)
+    q, got = box.attend(news)
+    box.check(news, q, got)
+    q2, again = box.attend(news, q=q)
+    assert np.array_equal(got, again)
