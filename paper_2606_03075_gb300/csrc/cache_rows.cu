@@ -12,6 +12,7 @@
 // already in flight.  A row is spread over d / 8 lanes of 8 values (16 bytes
 // of bf16), so a scale's 32 values sit in 4 neighbouring lanes.
 #include "cache_launch.h"
+#include "launch.h"
 
 namespace tgvkv {
 namespace {
@@ -71,7 +72,7 @@ __device__ __forceinline__ int pool_row(const CacheProblem& p, const int32_t* pa
         raise_status(status, TGVKV_STATUS_INDEX);
         return -1;
     }
-    const int page = __ldg(page_table + (size_t)s * p.max_pages + (int)(slot >> p.page_shift));
+    const int page = page_table[(size_t)s * p.max_pages + (int)(slot >> p.page_shift)];
     if (page < 0 || page >= p.n_pages) {
         raise_status(status, TGVKV_STATUS_INDEX);
         return -1;
@@ -164,7 +165,7 @@ struct WriteSource {
 template <int D, int FMT, bool TOKENS>
 __global__ void __launch_bounds__(kRowThreads, 5)
 cache_write_kernel(const CacheProblem p, const WriteSource src, const CachePools pool,
-                   const int32_t* __restrict__ page_table, const int32_t* __restrict__ lens,
+                   const int32_t* page_table, const int32_t* lens,
                    int32_t* __restrict__ lens_out, uint32_t* __restrict__ status) {
     using Gm = RowGeom<D>;
     __shared__ int dst[Gm::ROWS];
@@ -173,6 +174,8 @@ cache_write_kernel(const CacheProblem p, const WriteSource src, const CachePools
     const unsigned u0 = blockIdx.x * (unsigned)Gm::ROWS;
     const int unit = tid % Gm::LPR, sub = tid / Gm::LPR;
 
+    griddep_launch_dependents();       // the next call's set-up may overlap this one's end
+    griddep_wait();
     // the lengths after the write, and the check of the offsets
     for (int s = blockIdx.x * kRowThreads + tid; s < p.S; s += gridDim.x * kRowThreads) {
         long long lo, hi, most;
@@ -268,8 +271,8 @@ cache_write_kernel(const CacheProblem p, const WriteSource src, const CachePools
 template <int D, int FMT>
 __global__ void __launch_bounds__(kRowThreads, 5)
 cache_read_kernel(const CacheProblem p, const CachePools pool,
-                  const int32_t* __restrict__ page_table, const int32_t* __restrict__ first,
-                  const int64_t* __restrict__ offsets, uint16_t* __restrict__ k_out,
+                  const int32_t* page_table, const int32_t* first,
+                  const int64_t* offsets, uint16_t* __restrict__ k_out,
                   uint16_t* __restrict__ v_out, long long rows, uint32_t* __restrict__ status) {
     using Gm = RowGeom<D>;
     __shared__ int from[Gm::ROWS];
@@ -277,6 +280,8 @@ cache_read_kernel(const CacheProblem p, const CachePools pool,
     const int tid = threadIdx.x;
     const unsigned u0 = blockIdx.x * (unsigned)Gm::ROWS;
     const int unit = tid % Gm::LPR, sub = tid / Gm::LPR;
+    griddep_launch_dependents();
+    griddep_wait();
     for (int s = blockIdx.x * kRowThreads + tid; s < p.S; s += gridDim.x * kRowThreads) {
         const long long lo = offsets[s], hi = offsets[s + 1];
         if (lo < 0 || hi < lo || hi > rows || (s == 0 && lo != 0))
@@ -318,8 +323,8 @@ cache_read_kernel(const CacheProblem p, const CachePools pool,
                 kw[i].x = __ldcs(reinterpret_cast<const uint32_t*>(pool.k + at * (D / 2)) + unit);
                 vw[i].x = __ldcs(reinterpret_cast<const uint32_t*>(pool.v + at * (D / 2)) + unit);
             }
-            kb[i] = __ldg(pool.ks + at * (D / kGroup) + (unit >> 2));
-            vb[i] = __ldg(pool.vs + at * (D / kGroup) + (unit >> 2));
+            kb[i] = pool.ks[at * (D / kGroup) + (unit >> 2)];
+            vb[i] = pool.vs[at * (D / kGroup) + (unit >> 2)];
         }
     }
 #pragma unroll
@@ -366,13 +371,9 @@ cudaError_t launch_cache_write(const CacheProblem& p, const CachePools& pool, co
     return by_shape(p, [&](auto d, auto fmt) {
         constexpr int D = decltype(d)::value, FMT = decltype(fmt)::value;
         const unsigned blocks = row_blocks(rows, RowGeom<D>::ROWS);
-        if (tok_offsets)
-            cache_write_kernel<D, FMT, true><<<blocks, kRowThreads, 0, stream>>>(
-                p, src, pool, page_table, lens, lens_out, status);
-        else
-            cache_write_kernel<D, FMT, false><<<blocks, kRowThreads, 0, stream>>>(
-                p, src, pool, page_table, lens, lens_out, status);
-        return cudaGetLastError();
+        return launch_dependent(tok_offsets ? cache_write_kernel<D, FMT, true> : cache_write_kernel<D, FMT, false>,
+                                dim3(blocks), dim3(kRowThreads), 0, stream, p, src, pool, page_table, lens,
+                                lens_out, status);
     });
 }
 
@@ -382,9 +383,9 @@ cudaError_t launch_cache_read(const CacheProblem& p, const CachePools& pool,
                               long long rows, uint32_t* status, cudaStream_t stream) {
     return by_shape(p, [&](auto d, auto fmt) {
         constexpr int D = decltype(d)::value, FMT = decltype(fmt)::value;
-        cache_read_kernel<D, FMT><<<row_blocks(rows, RowGeom<D>::ROWS), kRowThreads, 0, stream>>>(
-            p, pool, page_table, first, offsets, k_out, v_out, rows, status);
-        return cudaGetLastError();
+        return launch_dependent(cache_read_kernel<D, FMT>, dim3(row_blocks(rows, RowGeom<D>::ROWS)),
+                                dim3(kRowThreads), 0, stream, p, pool, page_table, first, offsets, k_out,
+                                v_out, rows, status);
     });
 }
 

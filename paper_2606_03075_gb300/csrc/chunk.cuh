@@ -27,8 +27,8 @@ struct SetSpan {
 __device__ __forceinline__ SetSpan set_span(const CacheProblem& p, const ChunkArgs& a, int s) {
     SetSpan r;
     const int b = s / p.H_kv;
-    const int lo = __ldg(a.tok_offsets + b), hi = __ldg(a.tok_offsets + b + 1);
-    r.len = clamp_len(__ldg(a.lens + s), p.cap);
+    const int lo = a.tok_offsets[b], hi = a.tok_offsets[b + 1];
+    r.len = clamp_len(a.lens[s], p.cap);
     r.tok0 = min(max(lo, 0), a.T);
     r.n = min(min(max(hi, r.tok0), a.T) - r.tok0, a.max_q);
     return r;

@@ -21,6 +21,7 @@ chunk_tile_merge(const CacheProblem p, const ChunkArgs a, const TilePlan pl, int
     __shared__ float shared[8 * (D + 2)];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     __shared__ int found[4], count[8];
+    griddep_launch_dependents();       // the next call's set-up may overlap
     griddep_wait();
     // the y-th of the items named: threads 0 .. ctas - 1 hold one CTA's word each
     int4 raw = make_int4(-1, 0, 0, 0);

@@ -72,7 +72,7 @@ template <int W>
 struct StreamTail {
     uint64_t full[W][kStages];
     int2 start[W];                     // each stream's first set, and chunk in it
-    int warp_sum[W];
+    long long warp_sum[W];
     int never;
 };
 
@@ -245,12 +245,11 @@ template <int D, int FMT, int NB>
 __global__ void __launch_bounds__(StreamGeom<D, FMT, NB>::W * 32, 1)
 chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                     const CacheProblem p, const CachePools pool, const ChunkArgs a, int box,
-                    int box_shift, int min_chunks, int rec_rows, float* __restrict__ part,
+                    int box_shift, int rec_rows, float* __restrict__ part,
                     long long* __restrict__ plan, uint32_t* __restrict__ status) {
     using Gm = StreamGeom<D, FMT, NB>;
     constexpr int CH = Gm::CH, W = Gm::W;
     constexpr int KS = D / 16, MT = D / 16, KB = CH / 16;
-    griddep_launch_dependents();
     if (threadIdx.x == 0) {
         tc::tma_prefetch_desc(&mk);
         tc::tma_prefetch_desc(&mv);
@@ -265,40 +264,44 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
         for (int st = 0; st < kStages; ++st) tc::mbar_init(&tl.full[warp][st], 1);
         tc::fence_mbar_init();
     }
+    // The kernel before has finished; the merge, which may start from now on, reads this
+    // call's inputs before it waits in turn.
+    griddep_wait();
+    griddep_launch_dependents();
     if (blockIdx.x == 0) check_spans(p, a, tid, W * 32, status);
 
     // ---- the plan: thread t counts the chunks of sets [t * run, (t + 1) * run)
     const int run = (p.S + W * 32 - 1) / (W * 32);
     const int s_lo = min(tid * run, p.S), s_hi = min(s_lo + run, p.S);
-    int sum = 0;
+    long long sum = 0;
     for (int s = s_lo; s < s_hi; ++s) sum += set_chunks<CH>(set_span(p, a, s));
-    int incl = sum;
+    long long incl = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(~0u, incl, o);
+        const long long y = __shfl_up_sync(~0u, incl, o);
         if (lane >= o) incl += y;
     }
     if (lane == 31) tl.warp_sum[warp] = incl;
     __syncthreads();
-    int base = incl - sum, total = 0;
+    long long base = incl - sum, total = 0;
 #pragma unroll
     for (int x = 0; x < W; ++x) {
         if (x < warp) base += tl.warp_sum[x];
         total += tl.warp_sum[x];
     }
     const int n_streams = gridDim.x * W;
-    const int per = max((total + n_streams - 1) / n_streams, min_chunks);
+    const int per = max((int)((total + n_streams - 1) / n_streams), 1);      // chunks a stream
     // the starts of this CTA's streams that lie in my sets; CTA 0 also writes the plan
     {
         const long long first = (long long)blockIdx.x * W * per;
-        if (blockIdx.x == 0 || (first < (long long)base + sum && first + (long long)W * per > base)) {
-            int at = base;
+        if (blockIdx.x == 0 || (first < base + sum && first + (long long)W * per > base)) {
+            long long at = base;
             for (int s = s_lo; s < s_hi; ++s) {
                 const int n = set_chunks<CH>(set_span(p, a, s));
                 if (blockIdx.x == 0) plan[s] = at;
                 for (int x = 0; x < W; ++x) {
                     const long long c = first + (long long)x * per;
-                    if (c >= at && c < (long long)at + n) tl.start[x] = make_int2(s, (int)c - at);
+                    if (c >= at && c < at + n) tl.start[x] = make_int2(s, (int)(c - at));
                 }
                 at += n;
             }
@@ -318,7 +321,7 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
     const int32_t* table = a.page_table + (size_t)ahead.s * p.max_pages;
     auto page_of = [&]() {             // lane b: page number of the chunk's slice b
         const int slot = ahead.key0() + (lane << box_shift);
-        return (lane << box_shift) < ahead.n() ? __ldg(table + (slot >> p.page_shift)) : 0;
+        return (lane << box_shift) < ahead.n() ? table[slot >> p.page_shift] : 0;
     };
     int page = ahead.left > 0 ? page_of() : 0;
     int issued = 0;
@@ -686,29 +689,29 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
 // combined in stream order.
 template <int D, int WPR>
 __global__ void __launch_bounds__(WPR == 1 ? 128 : WPR * 32)
-chunk_stream_merge(const CacheProblem p, const ChunkArgs a, int n_streams, int min_chunks,
-                   int rec_rows, const float* __restrict__ part,
+chunk_stream_merge(const CacheProblem p, const ChunkArgs a, int n_streams, int rec_rows,
+                   const float* __restrict__ part,
                    const long long* __restrict__ plan) {
     constexpr int DPL = D / 32;
     __shared__ float shared[WPR == 1 ? 1 : WPR * (D + 2)];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const long long gw = WPR == 1 ? (long long)blockIdx.x * 4 + warp : (long long)blockIdx.x;
     const int s = (int)(gw / rec_rows), r = (int)(gw % rec_rows);
+    griddep_launch_dependents();       // the next call's set-up may overlap
     SetSpan sp{0, 0, 0};
     if (s < p.S) sp = set_span(p, a, s);
     griddep_wait();
     if (s >= p.S || r >= sp.n * p.G) return;
-    const int c0 = (int)__ldcg(plan + s), c1 = (int)__ldcg(plan + s + 1);
-    const int total = (int)__ldcg(plan + p.S);
+    const long long c0 = __ldcg(plan + s), c1 = __ldcg(plan + s + 1), total = __ldcg(plan + p.S);
     float acc[DPL];
 #pragma unroll
     for (int c = 0; c < DPL; ++c) acc[c] = 0.f;
     if (c1 > c0) {
-        const int per = max((total + n_streams - 1) / n_streams, min_chunks);
-        const int w0 = c0 / per, w1 = (c1 - 1) / per;
+        const int per = max((int)((total + n_streams - 1) / n_streams), 1);
+        const int w0 = (int)(c0 / per), w1 = (int)((c1 - 1) / per);
         if (w0 == w1) return;          // inside one stream: written by it
         // a segment starts its stream's share, but for a set that begins inside it
-        const int first = c0 != w0 * per ? 1 : 0;
+        const int first = c0 != (long long)w0 * per ? 1 : 0;
         const size_t rec = chunk_record_floats(rec_rows, D);
         merge_records<D, WPR, false>(w1 - w0 + 1, rec_rows, r, [&](int i) {
             return part + ((size_t)(w0 + i) * 2 + (i == 0 ? first : 0)) * rec;
@@ -721,9 +724,6 @@ chunk_stream_merge(const CacheProblem p, const ChunkArgs a, int n_streams, int m
     for (int c = 0; c < DPL; c += 2)
         *reinterpret_cast<uint32_t*>(out + c) = pack_bf16x2(acc[c], acc[(c + 1) % DPL]);
 }
-
-// Chunks a stream takes at least: below this, splitting costs more than it saves.
-constexpr int kMinChunks = 1;
 
 template <int D, int FMT, int NB>
 cudaError_t launch_stream(const CacheProblem& p, const CachePools& pool, const ChunkArgs& a,
@@ -747,18 +747,18 @@ cudaError_t launch_stream(const CacheProblem& p, const CachePools& pool, const C
     if (sms <= 0) return cudaErrorInvalidDevice;
     const int ctas = sms < kStreamMaxCtas ? sms : kStreamMaxCtas;
     const int rec_rows = a.max_q * p.G;
-    chunk_stream_kernel<D, FMT, NB><<<ctas, Gm::W * 32, smem, stream>>>(
-        mk, mv, p, pool, a, box, box_shift, kMinChunks, rec_rows, part, plan, status);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    e = launch_dependent(chunk_stream_kernel<D, FMT, NB>, dim3((unsigned)ctas), dim3(Gm::W * 32), smem,
+                         stream, mk, mv, p, pool, a, box, box_shift, rec_rows, part, plan, status);
+    if (e != cudaSuccess) return e;
     // a set has about n_streams / S records: from 16 on, 8 warps join a row
     const long long rows_out = (long long)p.S * rec_rows;
     const float* parts = part;
     const long long* plans = plan;
     if ((long long)p.S * 16 <= ctas * Gm::W)
         return launch_dependent(chunk_stream_merge<D, 8>, dim3((unsigned)rows_out), dim3(256), 0, stream,
-                                p, a, ctas * Gm::W, (int)kMinChunks, rec_rows, parts, plans);
+                                p, a, ctas * Gm::W, rec_rows, parts, plans);
     return launch_dependent(chunk_stream_merge<D, 1>, dim3((unsigned)((rows_out + 3) / 4)), dim3(128),
-                            0, stream, p, a, ctas * Gm::W, (int)kMinChunks, rec_rows, parts, plans);
+                            0, stream, p, a, ctas * Gm::W, rec_rows, parts, plans);
 }
 
 template <int D, int FMT>

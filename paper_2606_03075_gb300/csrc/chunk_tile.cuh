@@ -319,7 +319,6 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
     using Gm = TileGeom<D, FMT, PAIR>;
     constexpr bool QUANT = Gm::QUANT;
     constexpr int NST = Gm::NST, NRAW = QUANT ? Gm::NRAW : 1, START = Gm::START;
-    griddep_launch_dependents();
     extern __shared__ unsigned char smem_raw[];
     const uint32_t raw_addr = smem_u32(smem_raw);
     TileSmem<D, FMT, PAIR>& sm = *reinterpret_cast<TileSmem<D, FMT, PAIR>*>(
@@ -330,7 +329,6 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
         sm.abort_flag = 0;
         sm.never = 0;
         sm.tiles = 0;
-        sm.share = take_share(sync, status);
         for (int i = 0; i < (QUANT ? NRAW : NST); ++i) sm.filled[i] = -1;
         for (int i = 0; i < NST; ++i) {
             tc::mbar_init(&sm.full[i], QUANT ? Gm::CW : 1);
@@ -362,6 +360,11 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
         tc::tmem_alloc(&sm.tmem_base, 512);
         tc::tmem_relinquish();
     }
+    // The kernel before has finished; the merge, which may start from now on, reads this
+    // call's inputs before it waits in turn.
+    griddep_wait();
+    griddep_launch_dependents();
+    if (tid == 0) sm.share = take_share(sync, status);
     if (blockIdx.x == 0) check_spans(p, a, tid, Gm::THREADS, status);
 
     // ---- this CTA's share: units [c0, c0 + count) of all
@@ -468,7 +471,7 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
                 const int last_page = (g.sp.len - 1) >> p.page_shift;
                 auto window = [&](int i) {
                     const int at = 32 * i + lane;
-                    return at <= last_page ? __ldg(table + at) : 0;
+                    return at <= last_page ? table[at] : 0;
                 };
                 int wk = (g.j0 * TN >> p.page_shift) >> 5;
                 int pages = window(wk), pages_next = window(wk + 1);
@@ -1062,9 +1065,10 @@ cudaError_t launch_tile(const CacheProblem& p, const CachePools& pool, const Chu
     const int sms = device_sm_count();
     if (sms <= 0) return cudaErrorInvalidDevice;
     const int ctas = sms < kTileMaxCtas ? sms : kTileMaxCtas;
-    chunk_tile_kernel<D, FMT, PAIR><<<ctas, TileGeom<D, FMT, PAIR>::THREADS, smem, stream>>>(
-        mq, mk, mv, p, pool, a, pl, part, split, sync, status);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    e = launch_dependent(chunk_tile_kernel<D, FMT, PAIR>, dim3((unsigned)ctas),
+                         dim3(TileGeom<D, FMT, PAIR>::THREADS), smem, stream, mq, mk, mv, p, pool, a, pl,
+                         part, split, sync, status);
+    if (e != cudaSuccess) return e;
     return launch_tile_merge(p, a, pl, ctas, part, split, stream);
 }
 

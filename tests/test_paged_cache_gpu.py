@@ -553,3 +553,37 @@ def test_a_few_tokens_of_17_to_33_rows(api, fmt, d, H_q, H_kv, most):
     box.check(news, q, got)
     q2, again = box.attend(news, q=q)
     assert np.array_equal(got, again)
+
+
+@pytest.mark.parametrize("fmt,n", [("bf16", 1), ("int8", 1), ("int4", 9), ("int8", 40)])
+def test_steps_in_a_row_see_what_the_step_before_wrote(api, fmt, n):
+    """Writes, attention and reads queued without a pause: the kernels may start
+    before the ones ahead of them have finished, and wait for what they read."""
+    B, H_q, H_kv, d, steps = 4, 8, 2, 64, 24
+    box = Box(api, B, H_q, H_kv, d, 16, fmt, 40 + n * steps)
+    box.fill([5, 17, 0, 33, 40, 12, 1, 8])
+    off = torch.arange(0, B * n + 1, n, dtype=torch.int32, device="cuda")
+    lens, grown = box.lens_t(box.lens), box.lens_t(box.lens)
+    kv = [[box.values(B * n * H_kv, keys=i == 0).reshape(B * n, H_kv, d) for i in (0, 1)]
+          for _ in range(steps)]
+    qs = [R.bf16_values(R.bf16_bits(box.rng.standard_normal((B * n, H_q, d)))) for _ in range(steps)]
+    kv_t = [[dev_bf16(R.bf16_bits(x)).view(B * n, H_kv, d) for x in pair] for pair in kv]
+    qs_t = [dev_bf16(R.bf16_bits(q)).view(B * n, H_q, d) for q in qs]
+    outs = [torch.empty(B * n, H_q, d, dtype=torch.bfloat16, device="cuda") for _ in range(steps)]
+    back = [torch.empty(B * H_kv, d, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    rows = torch.arange(B * H_kv + 1, dtype=torch.int64, device="cuda")
+    torch.cuda.synchronize()
+    for i in range(steps):
+        api.tgvkv_cache_write(box.desc, box.cache, box.table, lens, *kv_t[i], off, grown, box.ws)
+        api.tgvkv_chunk_attention(box.desc, box.cache, box.table, grown, qs_t[i], off, n, outs[i], box.ws)
+        lens, grown = grown, lens
+    api.tgvkv_cache_read(box.desc, box.cache, box.table, lens - 1, rows, *back, box.ws)
+    assert api.tgvkv_status(box.ws) == 0
+    for i in range(steps):
+        for s in range(B * H_kv):
+            b, g = divmod(s, H_kv)
+            new = [R.round_trip(x[b * n:(b + 1) * n, g], fmt) for x in kv[i]]
+            box.k[s], box.v[s] = np.concatenate([box.k[s], new[0]]), np.concatenate([box.v[s], new[1]])
+        box.check([n] * B, qs[i], R.bf16_values(host_bits(outs[i])).reshape(B * n, H_q, d))
+    for t, held in zip(back, (box.k, box.v)):
+        assert np.array_equal(R.bf16_values(host_bits(t)), np.stack([x[-1] for x in held]).astype(np.float32))
