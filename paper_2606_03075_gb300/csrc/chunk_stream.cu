@@ -241,7 +241,10 @@ __device__ __forceinline__ int out_dim(int mt, int g) {
     return 32 * (mt >> 1) + 4 * g + 2 * (mt & 1);
 }
 
-template <int D, int FMT, int NB>
+// SHORT: CTA b has set b, its warps one stretch of it each, joined through shared
+// memory; else the warps of all CTAs share all sets, and split sets are left to
+// chunk_stream_merge.
+template <int D, int FMT, int NB, bool SHORT>
 __global__ void __launch_bounds__(StreamGeom<D, FMT, NB>::W * 32, 1)
 chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                     const CacheProblem p, const CachePools pool, const ChunkArgs a, int box,
@@ -270,53 +273,63 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
     griddep_launch_dependents();
     if (blockIdx.x == 0) check_spans(p, a, tid, W * 32, status);
 
-    // ---- the plan: thread t counts the chunks of sets [t * run, (t + 1) * run)
-    const int run = (p.S + W * 32 - 1) / (W * 32);
-    const int s_lo = min(tid * run, p.S), s_hi = min(s_lo + run, p.S);
-    long long sum = 0;
-    for (int s = s_lo; s < s_hi; ++s) sum += set_chunks<CH>(set_span(p, a, s));
-    long long incl = sum;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long y = __shfl_up_sync(~0u, incl, o);
-        if (lane >= o) incl += y;
-    }
-    if (lane == 31) tl.warp_sum[warp] = incl;
-    __syncthreads();
-    long long base = incl - sum, total = 0;
-#pragma unroll
-    for (int x = 0; x < W; ++x) {
-        if (x < warp) base += tl.warp_sum[x];
-        total += tl.warp_sum[x];
-    }
-    const int n_streams = gridDim.x * W;
-    const int per = max((int)((total + n_streams - 1) / n_streams), 1);      // chunks a stream
-    // the starts of this CTA's streams that lie in my sets; CTA 0 also writes the plan
-    {
-        const long long first = (long long)blockIdx.x * W * per;
-        if (blockIdx.x == 0 || (first < base + sum && first + (long long)W * per > base)) {
-            long long at = base;
-            for (int s = s_lo; s < s_hi; ++s) {
-                const int n = set_chunks<CH>(set_span(p, a, s));
-                if (blockIdx.x == 0) plan[s] = at;
-                for (int x = 0; x < W; ++x) {
-                    const long long c = first + (long long)x * per;
-                    if (c >= at && c < at + n) tl.start[x] = make_int2(s, (int)(c - at));
-                }
-                at += n;
-            }
-        }
-        if (blockIdx.x == 0 && tid == 0) plan[p.S] = total;
-    }
-    __syncthreads();
     const int si = blockIdx.x * W + warp;
-    const long long c_lo = (long long)si * per;
-    if (c_lo >= total) return;
+    int per;                           // chunks a stream
+    long long total = 0, c_lo;         // chunks of all (SHORT: of the set), this stream's first
+    if constexpr (SHORT) {
+        total = set_chunks<CH>(set_span(p, a, blockIdx.x));
+        per = max((int)((total + W - 1) / W), 1);
+        c_lo = (long long)warp * per;
+        if (lane == 0) tl.start[warp] = make_int2(blockIdx.x, (int)c_lo);
+        __syncthreads();
+    } else {
+        // ---- the plan: thread t counts the chunks of sets [t * run, (t + 1) * run)
+        const int run = (p.S + W * 32 - 1) / (W * 32);
+        const int s_lo = min(tid * run, p.S), s_hi = min(s_lo + run, p.S);
+        long long sum = 0;
+        for (int s = s_lo; s < s_hi; ++s) sum += set_chunks<CH>(set_span(p, a, s));
+        long long incl = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long y = __shfl_up_sync(~0u, incl, o);
+            if (lane >= o) incl += y;
+        }
+        if (lane == 31) tl.warp_sum[warp] = incl;
+        __syncthreads();
+        long long base = incl - sum;
+#pragma unroll
+        for (int x = 0; x < W; ++x) {
+            if (x < warp) base += tl.warp_sum[x];
+            total += tl.warp_sum[x];
+        }
+        const int n_streams = gridDim.x * W;
+        per = max((int)((total + n_streams - 1) / n_streams), 1);      // chunks a stream
+        // the starts of this CTA's streams that lie in my sets; CTA 0 also writes the plan
+        {
+            const long long first = (long long)blockIdx.x * W * per;
+            if (blockIdx.x == 0 || (first < base + sum && first + (long long)W * per > base)) {
+                long long at = base;
+                for (int s = s_lo; s < s_hi; ++s) {
+                    const int n = set_chunks<CH>(set_span(p, a, s));
+                    if (blockIdx.x == 0) plan[s] = at;
+                    for (int x = 0; x < W; ++x) {
+                        const long long c = first + (long long)x * per;
+                        if (c >= at && c < at + n) tl.start[x] = make_int2(s, (int)(c - at));
+                    }
+                    at += n;
+                }
+            }
+            if (blockIdx.x == 0 && tid == 0) plan[p.S] = total;
+        }
+        __syncthreads();
+        c_lo = (long long)si * per;
+        if (c_lo >= total) return;
+    }
 
     unsigned char* wring = ring + warp * kStages * Gm::kStage;
     unsigned char* wside = ring + W * kStages * Gm::kStage + warp * kStages * Gm::kSide;
     Walk<CH> ahead;                    // the next chunk to fetch
-    ahead.init(p, a, tl.start[warp], (int)min((long long)per, total - c_lo));
+    ahead.init(p, a, tl.start[warp], (int)max(min((long long)per, total - c_lo), 0ll));
     Walk<CH> w = ahead;                // the next chunk to work on
     const int32_t* table = a.page_table + (size_t)ahead.s * p.max_pages;
     auto page_of = [&]() {             // lane b: page number of the chunk's slice b
@@ -345,6 +358,12 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
     float m[NB][2], l[NB][2];          // of rows 8 nb + 2 tq and the next
     bool seg_starts = true;            // the segment began at its set's first chunk
     bool share_starts = true;          // ... is the first of this stream
+    if constexpr (SHORT) {             // a stretch without a chunk
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) m[nb][e] = -INFINITY, l[nb][e] = 0.f;
+    }
     int i = 0;
     for (; w.left > 0; ++i) {
         const int st = i % kStages;
@@ -628,51 +647,53 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
                     l[nb][e] += __shfl_xor_sync(~0u, l[nb][e], 8);
                     l[nb][e] += __shfl_xor_sync(~0u, l[nb][e], 16);
                 }
-            const bool whole = seg_starts && w.at + 1 == w.chunks;
-            float* pp = part + ((size_t)si * 2 + (share_starts ? 0 : 1)) *
-                                   (size_t)chunk_record_floats(rec_rows, D);
-            constexpr int STEP = FMT == TGVKV_CACHE_BF16 ? 8 : 1;   // dims between rows g and g + 8
+            if constexpr (!SHORT) {
+                const bool whole = seg_starts && w.at + 1 == w.chunks;
+                float* pp = part + ((size_t)si * 2 + (share_starts ? 0 : 1)) *
+                                       (size_t)chunk_record_floats(rec_rows, D);
+                constexpr int STEP = FMT == TGVKV_CACHE_BF16 ? 8 : 1;   // dims between rows g and g + 8
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
+                for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int r = 8 * nb + 2 * tq + e;
-                    if (r >= w.sp.n * p.G) continue;
-                    if (whole) {       // the whole set: written out
-                        const float ls = l[nb][e];
-                        const float inv = ls > 0.f ? 1.f / ls : (ls == ls ? 0.f : ls);
-                        const int t = r / p.G, hh = r - t * p.G;
-                        uint16_t* op = a.out +
-                                       ((size_t)(w.sp.tok0 + t) * p.H_q + (w.s % p.H_kv) * p.G + hh) * D;
+                    for (int e = 0; e < 2; ++e) {
+                        const int r = 8 * nb + 2 * tq + e;
+                        if (r >= w.sp.n * p.G) continue;
+                        if (whole) {       // the whole set: written out
+                            const float ls = l[nb][e];
+                            const float inv = ls > 0.f ? 1.f / ls : (ls == ls ? 0.f : ls);
+                            const int t = r / p.G, hh = r - t * p.G;
+                            uint16_t* op = a.out +
+                                           ((size_t)(w.sp.tok0 + t) * p.H_q + (w.s % p.H_kv) * p.G + hh) * D;
 #pragma unroll
-                        for (int mt = 0; mt < MT; ++mt) {
-                            const uint32_t two =
-                                pack_bf16x2(o[mt][nb][e] * inv, o[mt][nb][2 + e] * inv);
-                            uint16_t* od = op + out_dim<FMT>(mt, g);
-                            if (STEP == 1) {
-                                *reinterpret_cast<uint32_t*>(od) = two;
-                            } else {
-                                od[0] = (uint16_t)two;
-                                od[STEP] = (uint16_t)(two >> 16);
+                            for (int mt = 0; mt < MT; ++mt) {
+                                const uint32_t two =
+                                    pack_bf16x2(o[mt][nb][e] * inv, o[mt][nb][2 + e] * inv);
+                                uint16_t* od = op + out_dim<FMT>(mt, g);
+                                if (STEP == 1) {
+                                    *reinterpret_cast<uint32_t*>(od) = two;
+                                } else {
+                                    od[0] = (uint16_t)two;
+                                    od[STEP] = (uint16_t)(two >> 16);
+                                }
                             }
-                        }
-                    } else {
+                        } else {
 #pragma unroll
-                        for (int mt = 0; mt < MT; ++mt) {
-                            float* od = pp + r * D + out_dim<FMT>(mt, g);
-                            if (STEP == 1) {
-                                *reinterpret_cast<float2*>(od) = make_float2(o[mt][nb][e], o[mt][nb][2 + e]);
-                            } else {
-                                od[0] = o[mt][nb][e];
-                                od[STEP] = o[mt][nb][2 + e];
+                            for (int mt = 0; mt < MT; ++mt) {
+                                float* od = pp + r * D + out_dim<FMT>(mt, g);
+                                if (STEP == 1) {
+                                    *reinterpret_cast<float2*>(od) = make_float2(o[mt][nb][e], o[mt][nb][2 + e]);
+                                } else {
+                                    od[0] = o[mt][nb][e];
+                                    od[STEP] = o[mt][nb][2 + e];
+                                }
                             }
-                        }
-                        if (g == 0) {
-                            pp[rec_rows * D + r] = m[nb][e];
-                            pp[rec_rows * D + rec_rows + r] = l[nb][e];
+                            if (g == 0) {
+                                pp[rec_rows * D + r] = m[nb][e];
+                                pp[rec_rows * D + rec_rows + r] = l[nb][e];
+                            }
                         }
                     }
-                }
+            }
         }
         w.step(p, a);
     }
@@ -681,6 +702,58 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
         if (lane == 0) raise_status(status, TGVKV_STATUS_TIMEOUT);
         for (; i < issued; ++i)
             if (!tc::mbar_wait(&tl.full[warp][i % kStages], (i / kStages) & 1, &tl.never)) break;
+    }
+    if constexpr (SHORT) {
+        // the warps' partials, as their lanes hold them, in their rings (read by now):
+        // float4 x of lane t at 32 x + t; a warp joins every W-th float4
+        constexpr int X = MT * NB;
+        static_assert(16 * 32 * (X + NB) <= kStages * Gm::kStage, "a partial fits a ring");
+        const int used = (int)min((total + per - 1) / per, (long long)W);
+        float4* mine = reinterpret_cast<float4*>(wring) + lane;
+        if (warp < used) {
+#pragma unroll
+            for (int x = 0; x < X; ++x) {
+                const float(&c)[4] = o[x / NB][x % NB];
+                mine[32 * x] = make_float4(c[0], c[1], c[2], c[3]);
+            }
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+                mine[32 * (X + nb)] = make_float4(m[nb][0], m[nb][1], l[nb][0], l[nb][1]);
+        }
+        __syncthreads();
+        for (int x = warp; x < X; x += W) {
+            const int mt = x / NB, nb = x % NB;
+            const float4* recs = reinterpret_cast<const float4*>(ring) + lane;
+            constexpr int REC = kStages * Gm::kStage / 16;
+            float M[2] = {-INFINITY, -INFINITY}, L[2] = {0.f, 0.f}, c[4] = {0.f, 0.f, 0.f, 0.f};
+            for (int j = 0; j < used; ++j) {
+                const float4 ml = recs[j * REC + 32 * (X + nb)];
+                M[0] = fmaxf(M[0], ml.x), M[1] = fmaxf(M[1], ml.y);
+            }
+            const float r0 = M[0] == -INFINITY ? 0.f : M[0], r1 = M[1] == -INFINITY ? 0.f : M[1];
+            for (int j = 0; j < used; ++j) {
+                const float4 ml = recs[j * REC + 32 * (X + nb)], t = recs[j * REC + 32 * x];
+                const float f0 = fast_exp2(ml.x - r0), f1 = fast_exp2(ml.y - r1);
+                L[0] += ml.z * f0, L[1] += ml.w * f1;
+                c[0] += t.x * f0, c[1] += t.y * f1, c[2] += t.z * f0, c[3] += t.w * f1;
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int r = 8 * nb + 2 * tq + e;
+                if (r >= w.sp.n * p.G) continue;
+                const float inv = L[e] > 0.f ? 1.f / L[e] : (L[e] == L[e] ? 0.f : L[e]);
+                const int t = r / p.G, hh = r - t * p.G;
+                uint16_t* od = a.out + ((size_t)(w.sp.tok0 + t) * p.H_q + (w.s % p.H_kv) * p.G + hh) * D +
+                               out_dim<FMT>(mt, g);
+                const uint32_t two = pack_bf16x2(c[e] * inv, c[2 + e] * inv);
+                if (FMT == TGVKV_CACHE_BF16) {
+                    od[0] = (uint16_t)two;
+                    od[8] = (uint16_t)(two >> 16);
+                } else {
+                    *reinterpret_cast<uint32_t*>(od) = two;
+                }
+            }
+        }
     }
 }
 
@@ -725,6 +798,16 @@ chunk_stream_merge(const CacheProblem p, const ChunkArgs a, int n_streams, int r
         *reinterpret_cast<uint32_t*>(out + c) = pack_bf16x2(acc[c], acc[(c + 1) % DPL]);
 }
 
+// SHORT takes calls of up to 16 rows with a CTA for every set at once, whose page
+// tables hold at most this many chunks a warp.  One kernel and no records in global
+// memory against shares of equal size (one token, us): 8 sets of bf16, d = 64,
+// 113 slots 4.4 / 7.6, 1000 (4 chunks) 7.3 / 7.2, 2000 10.7 / 7.3; d = 128, 500 (4) 7.7 / 8.0,
+// 1000 10.8 / 8.6; int4, d = 128, 500 (1) 6.8 / 9.5, 1000 (2) 9.7 / 9.4, 2000 15.4 / 9.8.
+template <int FMT>
+constexpr int short_chunks() {
+    return FMT == TGVKV_CACHE_BF16 ? 4 : 2;
+}
+
 template <int D, int FMT, int NB>
 cudaError_t launch_stream(const CacheProblem& p, const CachePools& pool, const ChunkArgs& a,
                           float* part, long long* plan, uint32_t* status, cudaStream_t stream) {
@@ -740,15 +823,26 @@ cudaError_t launch_stream(const CacheProblem& p, const CachePools& pool, const C
         return cudaErrorInvalidValue;
     const size_t smem = 1024 + Gm::kRing + sizeof(StreamTail<Gm::W>);
     static_assert(1024 + Gm::kRing + sizeof(StreamTail<Gm::W>) <= 227 * 1024, "shared memory of one CTA");
-    cudaError_t e = cudaFuncSetAttribute(chunk_stream_kernel<D, FMT, NB>,
-                                         cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
+    auto prepare = [&](auto kernel) {
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    };
+    cudaError_t e;
     const int sms = device_sm_count();
     if (sms <= 0) return cudaErrorInvalidDevice;
+    if constexpr (NB <= 2) {
+        if (p.S <= sms && (p.cap + Gm::CH - 1) / Gm::CH <= short_chunks<FMT>() * Gm::W) {
+            const auto kernel = chunk_stream_kernel<D, FMT, NB, true>;
+            if ((e = prepare(kernel)) != cudaSuccess) return e;
+            return launch_dependent(kernel, dim3((unsigned)p.S), dim3(Gm::W * 32), smem, stream, mk, mv, p,
+                                    pool, a, box, box_shift, 0, part, plan, status);
+        }
+    }
+    const auto kernel = chunk_stream_kernel<D, FMT, NB, false>;
+    if ((e = prepare(kernel)) != cudaSuccess) return e;
     const int ctas = sms < kStreamMaxCtas ? sms : kStreamMaxCtas;
     const int rec_rows = a.max_q * p.G;
-    e = launch_dependent(chunk_stream_kernel<D, FMT, NB>, dim3((unsigned)ctas), dim3(Gm::W * 32), smem,
-                         stream, mk, mv, p, pool, a, box, box_shift, rec_rows, part, plan, status);
+    e = launch_dependent(kernel, dim3((unsigned)ctas), dim3(Gm::W * 32), smem, stream, mk, mv, p, pool, a,
+                         box, box_shift, rec_rows, part, plan, status);
     if (e != cudaSuccess) return e;
     // a set has about n_streams / S records: from 16 on, 8 warps join a row
     const long long rows_out = (long long)p.S * rec_rows;

@@ -587,3 +587,18 @@ def test_steps_in_a_row_see_what_the_step_before_wrote(api, fmt, n):
         box.check([n] * B, qs[i], R.bf16_values(host_bits(outs[i])).reshape(B * n, H_q, d))
     for t, held in zip(back, (box.k, box.v)):
         assert np.array_equal(R.bf16_values(host_bits(t)), np.stack([x[-1] for x in held]).astype(np.float32))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("cap", [200, 513, 1100, 2200, 9000])
+def test_few_rows_for_short_and_long_page_tables(api, fmt, d, cap):
+    """The same small sets under page tables of several sizes (short ones have a kernel
+    that takes a set a CTA), a full set, empty ones, and sets at chunk boundaries."""
+    box = Box(api, 8, 8, 2, d, 64, fmt, cap)
+    lens = [box.max_pages * box.page, 64, 65, 0, 1, 127, 128, 129, 16, 15, 0, 3, min(cap, 511), 200, 33, 2]
+    box.fill(lens)
+    for news in ([1] * 8, [2, 0, 1, 2, 1, 2, 1, 1], [4, 3, 0, 4, 1, 4, 2, 3]):
+        q, got = box.attend(news)
+        box.check(news, q, got)
+        assert np.array_equal(got, box.attend(news, q=q)[1])
