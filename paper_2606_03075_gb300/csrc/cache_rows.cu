@@ -6,11 +6,21 @@
 //   read:   out row offsets[s] + i     <-  slot first[s] + i of set s, exactly
 //
 // Both move each row once and are bound by HBM: 2 d bytes of bf16 plus the
-// stored row per row of K and of V.  A CTA takes kRowsPerCta consecutive rows;
-// one thread per row finds its set (a search over the offsets) and its pool
-// row while the row data's loads, whose addresses do not depend on it, are
-// already in flight.  A row is spread over d / 8 lanes of 8 values (16 bytes
-// of bf16), so a scale's 32 values sit in 4 neighbouring lanes.
+// stored row per row of K and of V.  A CTA takes RowGeom::ROWS consecutive rows;
+// one thread per row finds its set (a search over the offsets, by a warp first for
+// the CTA's span) and its pool row, for writes while the row data's loads, whose
+// addresses do not depend on it, are already in flight.  A row is spread over d / 8
+// lanes of 8 values (16 bytes of bf16), so a scale's 32 values sit in 4 neighbouring
+// lanes.  Five CTAs an SM: the searches and barriers of one run under the loads of
+// the others.
+//
+// Measured (of 6790 GB/s): the evicted rows of 32 x 32 sets into int8 pages and back
+// 43 us (88%), 28 layers' prompts of 8704 tokens into int4 pages and back 204 us (91%),
+// 32 x 32 sets of 0 .. 3009 slots read back from int4 pages 226 us (98%); one token of 28
+// layers 4 us on the GPU, which is the launch and three dependent reads.
+//
+// Loads are never of the read-only kind: a kernel may start while the one that writes
+// its inputs is still at work (griddep_wait).
 #include "cache_launch.h"
 #include "launch.h"
 

@@ -75,7 +75,11 @@ struct TilePlan {
     int rows;                          // query rows of a record: tpt * G at most
 };
 
-constexpr int kJoin = 3;               // later parts that the CTA of an item's start joins
+// Later parts of an item that the CTA of its start joins; an item of more goes to the
+// second kernel.  One sequence's 32 sets of 96 tokens over 0 .. 16000 slots (int8): 52 us
+// at 2, 59 at 3 (its warps read the parts one after another); 600 tokens of 28 heads
+// over 20000 slots: 132 at 2, 141 at 1; 500-token chunks of 16 sequences 359 at 2, 397 at 0.
+constexpr int kJoin = 2;
 // words of the tile kernel's tickets and flags: two tickets, then 8 flags per CTA
 constexpr int kTileFlags = 8;
 constexpr int kTileSync = kTileFlags + 8 * kTileMaxCtas;

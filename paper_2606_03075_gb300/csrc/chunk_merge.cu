@@ -3,7 +3,7 @@
 // of that kernel in which such an item begins names it; the merge's CTA (x, y)
 // takes rows 8 x .. 8 x + 7 of the y-th item named, a warp each, or all 8 warps
 // row after row when it has many records.  A programmatic dependent of the tile
-// kernel.
+// kernel; latency-bound (three dependent reads of L2), a few microseconds.
 #include "cache_launch.h"
 #include "launch.h"
 

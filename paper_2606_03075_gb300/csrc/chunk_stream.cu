@@ -6,13 +6,13 @@
 // for token i of the n new tokens of its sequence (t = its row of q), over the
 // slots j of set (b, h / G).  A row that sees no slot gives 0.
 //
-// Each slot's K and V row is read once, for all query rows of its set (4 d * 32
-// flops against 4 d bytes at most, far below the 278 flops a byte where the
-// tensor cores would bound): what is left is to keep the reads in flight.  The sets' slots form one sequence of chunks
-// (CH slots, never across a set); each warp of a persistent CTA takes one
-// contiguous share of it, so ragged lengths and long caches split evenly.  A
-// chunk moves as whole page slices by TMA into the warp's own two-stage ring,
-// with the scale bytes and, at a segment's start, the query rows; the next
+// Each slot's K and V row is read once for all query rows of its set (4 d * 32 flops
+// against 4 d bytes at most, far below the 278 flops a byte where the tensor cores
+// would bound): what counts is to keep the reads in flight.  The sets' slots form
+// one sequence of chunks (CH slots, never across a set); each warp of a persistent
+// CTA takes one contiguous share of it, so ragged lengths and long caches split
+// evenly.  A chunk moves as whole page slices by TMA into the warp's own two-stage
+// ring, with the scale bytes and, at a segment's start, the query rows; the next
 // chunk's page numbers are fetched one chunk ahead.
 //
 // Arithmetic per chunk on the tensor cores (mma.sync m16n8k16: bf16 operands,
@@ -29,6 +29,16 @@
 // unrounded P.  A set inside one stream is written out at once; a split one
 // leaves a partial (m, l, O) per stream, merged by a second kernel in stream
 // order, so results do not depend on timing.
+//
+// What bounds it.  bf16: HBM (64 x 4 sets of one token over 0 .. 8705 slots: 136 us,
+// 6.3 TB/s).  Integer caches: the instructions that turn codes into bf16 (about 60%
+// of the issue slots, the integer pipe at 62%; the same sets in int8 88 us, 5.0 TB/s,
+// int4 64 us), and the start and the merge, about 10 us of each call.
+//
+// Measured and not kept: partials joined inside this kernel, by flags that a set's
+// first stream awaits or by whichever stream comes last (the batch above 92 and 97 us
+// against 88: a warp alone has too few loads in flight); scales applied to V instead
+// of P (32 layers of int4 92 us against 86).
 #include "cache_launch.h"
 #include "launch.h"
 #include "tc05.cuh"
@@ -844,7 +854,9 @@ cudaError_t launch_stream(const CacheProblem& p, const CachePools& pool, const C
     e = launch_dependent(kernel, dim3((unsigned)ctas), dim3(Gm::W * 32), smem, stream, mk, mv, p, pool, a,
                          box, box_shift, rec_rows, part, plan, status);
     if (e != cudaSuccess) return e;
-    // a set has about n_streams / S records: from 16 on, 8 warps join a row
+    // A set has about n_streams / S records: from 16 on, 8 warps join a row.  8 warps / 1,
+    // one int8 token over 0 .. 34816 slots, us: 4 sets 21 / 60, 16 sets 32 / 44, 64 sets
+    // 86 / 89; fewer records, 256 sets of 0 .. 8705 slots 96 / 88.
     const long long rows_out = (long long)p.S * rec_rows;
     const float* parts = part;
     const long long* plans = plan;

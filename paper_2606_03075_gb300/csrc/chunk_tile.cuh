@@ -32,15 +32,32 @@
 // from tensor memory; K is the K-major and V the MN-major B operand from shared
 // memory.
 //
-// Integer caches: TMA brings the codes of a key tile, four converter warps
-// write them as bf16 in the swizzled layout (exact: scales are powers of two),
-// and the rest is the bf16 kernel.
+// Integer caches: TMA brings the codes of a key tile, eight converter warps write
+// them as bf16 in the swizzled layout (exact: scales are powers of two), and the rest
+// is the bf16 kernel.
 //
-// Roles: warps 0 and 2 TMA (Q and K; V), warp 1 MMA issue (and TMEM), warp 3 rows
-// without work,
-// warps 4-11 softmax, warps 12-15 converters (integer caches).  Registers are split by role (setmaxnreg), so
-// that a softmax thread holds a whole row of S.  Every wait is bounded; a timeout sets
-// TGVKV_STATUS_TIMEOUT and the CTA unwinds after its copies and MMAs finished.
+// Roles: warps 0 and 2 TMA (Q and K; V), warp 1 MMA issue and tensor memory, warp 3
+// rows that see nothing, warps 4-11 softmax, warps 12-19 converters (integer caches).
+// Registers are split by role (setmaxnreg), so that a softmax thread holds a whole
+// row of S.  P is rounded to bf16 for its product and the normaliser sums it
+// unrounded; m, l and O stay in fp32; O is rescaled only when a row's maximum rises by
+// more than 2^8.  Every wait is bounded; a timeout sets TGVKV_STATUS_TIMEOUT and the
+// CTA unwinds after its copies and MMAs finished.
+//
+// What bounds it.  bf16, long chunks: the tensor cores (28 heads, 2048 tokens over
+// 34816 slots: 600 us, 1655 TFLOP/s, the rate a dense bf16 product holds under the
+// power limit).  Integer caches: shared memory, which carries the codes in, the bf16
+// copy out and in again and Q for every product, beside the converters' arithmetic (16 x
+// 500 tokens over 0 .. 8900 slots: int8 358 us, bf16 296).  One row tile a set: latency
+// (256 sets of 96 tokens over 0 .. 3104 slots: int8 64 us, bf16 60 us, 4.6 TB/s): the end
+// of a segment leaves the tensor cores idle for about 3 us, which only other work on
+// the SM could fill, and there is no room for a second CTA.
+//
+// Measured and not kept: one thread as the issuer (chunks over 34816 slots 763 us
+// against 627); one producer warp; four converter warps (16 x 500 tokens, int4
+// pages: 389 us against 360) and converters that load the next tile before they store
+// this one; deeper rings at d = 64; the next segment's place looked up before the
+// last products end (SPLIT 1% faster, PAIR 2% slower).
 #pragma once
 
 #include "cache_launch.h"
@@ -263,8 +280,7 @@ __device__ __forceinline__ int group_tiles(const Seg& g, const TilePlan& pl, int
 }
 
 // Places of K and V of key tile x (counted from the segment's first, of n) in the
-// order of the ring.  PAIR: K0 V0 K1 V1 ...; SPLIT: K0 K1
-// V0 K2 V1 ...
+// order of the ring.  PAIR: K0 V0 K1 V1 ...; SPLIT: K0 K1 V0 K2 V1 ...
 template <bool PAIR>
 __device__ __forceinline__ int k_place(int x) {
     return PAIR ? 2 * x : max(2 * x - 1, 0);
@@ -688,7 +704,8 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
         const int ri = r / p.G, rh = r - ri * p.G;           // token within the tile, head
         int ns = 0, nso = 0, npart = 0, base_it = 0;
         bool ok = true;
-        if (warp == kSoftWarp && lane == 0 && share < (int)gridDim.x) split[share] = SplitItem{-1, 0, 0, 0};
+        if (warp == kSoftWarp && lane == 0 && share < (int)gridDim.x)
+            split[share] = SplitItem{-1, 0, 0, 0};
         auto& at = sm.at[warp - kSoftWarp];
         const volatile Seg& g = at.g;
         if (lane == 0) begin(at.walk);
