@@ -164,7 +164,7 @@ struct TileGeom {
     static constexpr int ROWB = FMT == TGVKV_CACHE_INT8 ? D : D / 2;   // stored bytes a row
     static constexpr int RAW = TN * ROWB, SC = TN * (D / kGroup); // raw tile, its scale bytes
     static constexpr int NRAW = QUANT ? (FMT == TGVKV_CACHE_INT8 ? 3 : 6) : 0;
-    static constexpr int NQ = PAIR ? 1 : 2;                       // Q slots
+    static constexpr int NQ = PAIR && D == 128 ? 1 : 2;           // Q slots (what there is room for)
     static constexpr int QT = PAIR ? 2 : 1;                       // row tiles a slot
     // What an item's start and end cost, in key tiles: the shares are of equal cost.  SPLIT
     // (the groups' join besides): 256 sets of 96 tokens over 0 .. 3104 slots take (int8, us)
