@@ -859,9 +859,9 @@ int tgvkv_chunk_attention(const tgvkv_cache_desc* desc, const tgvkv_cache_pools*
     if ((long long)a.max_q * p.G <= stream_rows(p.d, p.format)) {
         e = launch_chunk_stream(p, pl, a, part, plan, status, st);
     } else {
-        // PAIR where some chunk has more than one row tile.  PAIR / SPLIT, us: 160 tokens of
-        // 8 x 32 int8 sets 80 / 85, 16 sequences' 500 tokens 359 / 524, 2048 tokens over 34816
-        // slots (bf16) 595 / 702; with one row tile, 96 tokens, 77 / 65 (bf16 63 / 60).
+        // PAIR where some chunk has more than one row tile.  PAIR / SPLIT, us: 0 .. 160 tokens
+        // of 8 x 32 int8 sets 80 / 85, 0 .. 500 of 16 sequences 359 / 524, 2048 tokens over 34816
+        // slots (bf16) 595 / 702; with one row tile, 0 .. 96, 77 / 65 (bf16 63 / 60).
         const bool pair = a.max_q > TM / p.G;
         e = p.format == TGVKV_CACHE_BF16   ? launch_tile_bf16(p, pl, a, part, split, sync, pair, status, st)
             : p.format == TGVKV_CACHE_INT8 ? launch_tile_int8(p, pl, a, part, split, sync, pair, status, st)

@@ -16,7 +16,7 @@
 //
 // Measured (of 6790 GB/s): the evicted rows of 32 x 32 sets into int8 pages and back
 // 43 us (88%), 28 layers' prompts of 8704 tokens into int4 pages and back 204 us (91%),
-// 32 x 32 sets of 0 .. 3009 slots read back from int4 pages 226 us (98%); one token of 28
+// 32 x 32 sets of 1505 .. 3009 slots read back from int4 pages 226 us (98%); one token of 28
 // layers 4 us on the GPU, which is the launch and three dependent reads.
 //
 // Loads are never of the read-only kind: a kernel may start while the one that writes

@@ -58,7 +58,7 @@ constexpr int kStreamRows = 32;        // query rows a set that it takes at most
 
 // Query rows a set up to which the row-stream kernel takes a call.  Where it still has
 // the registers it does without the tile kernel's 128-row tiles and the bf16 copy of
-// integer codes: 256 sets of 20 rows over 0 .. 4101 slots, tile kernel against it
+// integer codes: 256 sets of 20 rows over 2051 .. 4101 slots, tile kernel against it
 // (us): d = 64 bf16 50 / 45, int8 62 / 45, int4 62 / 42 (32 rows 50 / 49, 62 / 54,
 // 61 / 50); d = 128 bf16 75 / 78, int8 80 / 78, int4 82 / 60.
 __host__ __device__ constexpr int stream_rows(int d, int format) {
@@ -76,9 +76,9 @@ struct TilePlan {
 };
 
 // Later parts of an item that the CTA of its start joins; an item of more goes to the
-// second kernel.  One sequence's 32 sets of 96 tokens over 0 .. 16000 slots (int8): 52 us
+// second kernel.  One sequence's 32 sets of 96 tokens over 8001 .. 16000 slots (int8): 52 us
 // at 2, 59 at 3 (its warps read the parts one after another); 600 tokens of 28 heads
-// over 20000 slots: 132 at 2, 141 at 1; 500-token chunks of 16 sequences 359 at 2, 397 at 0.
+// over 20000 slots: 132 at 2, 141 at 1; 0 .. 500 tokens of 16 sequences 359 at 2, 397 at 0.
 constexpr int kJoin = 2;
 // words of the tile kernel's tickets and flags: two tickets, then 8 flags per CTA
 constexpr int kTileFlags = 8;

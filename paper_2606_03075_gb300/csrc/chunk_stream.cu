@@ -30,7 +30,7 @@
 // leaves a partial (m, l, O) per stream, merged by a second kernel in stream
 // order, so results do not depend on timing.
 //
-// What bounds it.  bf16: HBM (64 x 4 sets of one token over 0 .. 8705 slots: 136 us,
+// What bounds it.  bf16: HBM (64 x 4 sets of one token over 4353 .. 8705 slots: 136 us,
 // 6.3 TB/s).  Integer caches: the instructions that turn codes into bf16 (about 60%
 // of the issue slots, the integer pipe at 62%; the same sets in int8 88 us, 5.0 TB/s,
 // int4 64 us), and the start and the merge, about 10 us of each call.
@@ -855,8 +855,8 @@ cudaError_t launch_stream(const CacheProblem& p, const CachePools& pool, const C
                          box, box_shift, rec_rows, part, plan, status);
     if (e != cudaSuccess) return e;
     // A set has about n_streams / S records: from 16 on, 8 warps join a row.  8 warps / 1,
-    // one int8 token over 0 .. 34816 slots, us: 4 sets 21 / 60, 16 sets 32 / 44, 64 sets
-    // 86 / 89; fewer records, 256 sets of 0 .. 8705 slots 96 / 88.
+    // one int8 token over 17409 .. 34816 slots, us: 4 sets 21 / 60, 16 sets 32 / 44, 64 sets
+    // 86 / 89; fewer records, 256 sets of 4353 .. 8705 slots 96 / 88.
     const long long rows_out = (long long)p.S * rec_rows;
     const float* parts = part;
     const long long* plans = plan;

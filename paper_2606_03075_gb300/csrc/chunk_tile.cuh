@@ -48,13 +48,13 @@
 // 34816 slots: 600 us, 1655 TFLOP/s, the rate a dense bf16 product holds under the
 // power limit).  Integer caches: shared memory, which carries the codes in, the bf16
 // copy out and in again and Q for every product, beside the converters' arithmetic (16 x
-// 500 tokens over 0 .. 8900 slots: int8 358 us, bf16 296).  One row tile a set: latency
-// (256 sets of 96 tokens over 0 .. 3104 slots: int8 64 us, bf16 60 us, 4.6 TB/s): the end
+// 0 .. 500 tokens over 4451 .. 8900 slots: int8 358 us, bf16 296).  One row tile a set: latency
+// (256 sets of 0 .. 96 tokens over 1553 .. 3104 slots: int8 64 us, bf16 60 us, 4.6 TB/s): the end
 // of a segment leaves the tensor cores idle for about 3 us, which only other work on
 // the SM could fill, and there is no room for a second CTA.
 //
 // Measured and not kept: one thread as the issuer (chunks over 34816 slots 763 us
-// against 627); one producer warp; four converter warps (16 x 500 tokens, int4
+// against 627); one producer warp; four converter warps (16 x 0 .. 500 tokens, int4
 // pages: 389 us against 360) and converters that load the next tile before they store
 // this one; deeper rings at d = 64; the next segment's place looked up before the
 // last products end (SPLIT 1% faster, PAIR 2% slower).
@@ -167,9 +167,9 @@ struct TileGeom {
     static constexpr int NQ = PAIR && D == 128 ? 1 : 2;           // Q slots (what there is room for)
     static constexpr int QT = PAIR ? 2 : 1;                       // row tiles a slot
     // What an item's start and end cost, in key tiles: the shares are of equal cost.  SPLIT
-    // (the groups' join besides): 256 sets of 96 tokens over 0 .. 3104 slots take (int8, us)
+    // (the groups' join besides): 256 sets of 0 .. 96 tokens over 1553 .. 3104 slots take (int8, us)
     // 68.6 at 0, 67.6 at 2, 64.5 at 3, 66.6 at 4; at d = 64 54.3, 53.1, 49.2, 52.2 and 48.2 at 6.
-    // PAIR: 16 sequences' 500-token chunks over 2000 slots 125 at 0, 114 at 2, 112 at 3.
+    // PAIR: 0 .. 500 tokens of 16 sequences over 1001 .. 2000 slots 125 at 0, 114 at 2, 112 at 3.
     static constexpr int START = PAIR || D == 128 ? 3 : 6;
     static constexpr int CW = QUANT ? 8 : 0;                      // converter warps
     static constexpr int THREADS = 32 * (kConvWarp + CW);
