@@ -602,3 +602,16 @@ def test_few_rows_for_short_and_long_page_tables(api, fmt, d, cap):
         q, got = box.attend(news)
         box.check(news, q, got)
         assert np.array_equal(got, box.attend(news, q=q)[1])
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("H_q,H_kv,most", [(8, 8, 96), (8, 8, 130), (16, 8, 40)])
+def test_many_sets_that_each_span_several_ctas(api, fmt, H_q, H_kv, most):
+    """Sets whose parts lie in four CTAs or more, with many rows in all: the second
+    kernel joins several rows a CTA."""
+    box = Box(api, 4, H_q, H_kv, 64, 64, fmt, 4100)
+    box.fill([4100 - 37 * s for s in range(4 * H_kv)])
+    for news in ([most] * 4, [most, 0, most - 1, 33]):
+        q, got = box.attend(news)
+        box.check(news, q, got)
+        assert np.array_equal(got, box.attend(news, q=q)[1])
