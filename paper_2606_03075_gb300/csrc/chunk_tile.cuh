@@ -372,14 +372,14 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
             tc::tma_prefetch_desc(&mv);
         }
     }
-    if (warp == 1) {
-        tc::tmem_alloc(&sm.tmem_base, 512);
-        tc::tmem_relinquish();
-    }
     // The kernel before has finished; the merge, which may start from now on, reads this
     // call's inputs before it waits in turn.
     griddep_wait();
     griddep_launch_dependents();
+    if (warp == 1) {                   // (not before: a kernel still at work may yet want its own)
+        tc::tmem_alloc(&sm.tmem_base, 512);
+        tc::tmem_relinquish();
+    }
     if (tid == 0) sm.share = take_share(sync, status);
     if (blockIdx.x == 0) check_spans(p, a, tid, Gm::THREADS, status);
 
