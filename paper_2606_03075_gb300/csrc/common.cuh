@@ -89,7 +89,7 @@ constexpr int kMaxL = 1024;      // layers handled by the budget kernel
 // stream runs; griddep_wait blocks until that kernel has completed (a no-op
 // for an ordinary launch).  What that kernel wrote must then be read through
 // L2 (__ldcg), not the read-only path: a dependent that started early can
-// otherwise read a recycled buffer's old contents.  A kernel that calls
+// otherwise read a recycled buffer's old contents (launch.h has the whole rule).  A kernel that calls
 // griddep_launch_dependents lets its dependent be scheduled from then on.
 __device__ __forceinline__ void griddep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void griddep_launch_dependents() {

@@ -13,7 +13,23 @@ namespace tgvkv {
 
 // Launch `kern` as a programmatic dependent of the kernel before it on
 // `stream` (see griddep_wait): its CTAs may be scheduled while that kernel
-// finishes, and must call griddep_wait before reading what it wrote.
+// finishes, and the kernels before that one too where it signals before it has
+// waited itself.  What such a kernel must keep, whatever ran before it:
+//   - before griddep_wait it reads only what no kernel of this library writes
+//     (modality, text positions, tensor maps) and its own kernel parameters; a
+//     second kernel of a call also the call's inputs, if the first one waited (or
+//     was an ordinary launch) before it signalled.  A caller's own kernels and
+//     copies signal nothing, so that they have always finished;
+//   - every role that reads or writes other memory waits for itself, the producer of
+//     TMA loads included (prefetches to L2 are no reads: what is written later
+//     reaches them);
+//   - what other kernels write is not read through the read-only path afterwards;
+//   - tensor memory is taken after the wait, unless the kernel cannot share an SM with
+//     one that has yet to take its own.
+// Dependents: score_tc_kernel (each role waits), tpr_select_kernel and
+// tpr_select_warp_kernel, decode_merge_kernel (its offsets are the call's inputs),
+// cache_write_kernel, cache_read_kernel, chunk_stream_kernel, chunk_stream_merge
+// (lengths and offsets: the call's inputs), chunk_tile_kernel, chunk_tile_merge.
 template <typename... KArgs, typename... Args>
 cudaError_t launch_dependent(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem,
                              cudaStream_t stream, Args&&... args) {

@@ -402,6 +402,26 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
     if (warp == 0 && lane == 0) {
         tc::tma_prefetch_desc(&tmap_q);
         tc::tma_prefetch_desc(&tmap_k);
+        // Q and K may be what the kernels before write (rows read back from a paged
+        // cache, the rows of an eviction whose sets have one length): nothing of them is
+        // used before those have finished.  Meanwhile the first item's tiles come to L2.
+        {
+            const Item itm = item_info(p, s, mode, (int)blockIdx.x, n_two);
+            const int nslot = mode == MODE_PAIR ? itm.nparts : 1;
+            for (int r = 0; r < nslot; ++r)
+                for (int qg = 0; qg < 4; ++qg)
+                    for (int h = 0; h < D / 64; ++h)
+                        tc::tma_prefetch_2d(&tmap_q, h * 64, q_box_row(itm, mode, r, qg));
+            int cur = 0, kt[2];
+            for (int x = 0; x < STAGES; ++x) {
+                if (!next_step(itm, mode, p.stats_given ? 1 : 0, cur, s.vis_before, kt, p.stats_given)) break;
+                for (int y = 0; y < 2 && kt[y] >= 0; ++y)
+                    for (int h = 0; h < D / 64; ++h)
+                        tc::tma_prefetch_2d(&tmap_k, h * 64,
+                                            itm.lh[mode == MODE_PACKED ? y : 0] * p.N + kt[y] * BN);
+            }
+        }
+        griddep_wait();
         int it = 0;
         int qn0 = 0, qn1 = 0;     // uses of each Q slot
         bool ok = true;
@@ -593,7 +613,7 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
         // The kernel before (the select + gather of the previous eviction, when it
         // is one) may still read the scores and budgets this kernel overwrites: the
         // softmax role, the only one writing global memory before the end, waits
-        // for it.  The loads and MMAs of the first items overlap its end.
+        // for it too.
         griddep_wait();
         const int sid = tid - 64;
         const int quarter = warp & 3;

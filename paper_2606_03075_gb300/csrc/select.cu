@@ -94,7 +94,8 @@ __device__ __forceinline__ void vision_span_block(const uint8_t* modality, int N
 
 // Copy `rows` consecutive K and V rows of head `head` starting at position
 // `src0` to output rows starting at `dst0`, with the threads [t0, t0 + nt)
-// (16-byte vectors, loads before stores).
+// (16-byte vectors, loads before stores).  K and V are read through L2, as a
+// kernel before may have written them.
 template <int VPR>
 __device__ __forceinline__ void copy_rows(const uint4* __restrict__ k, const uint4* __restrict__ v,
                                           uint4* __restrict__ k_out, uint4* __restrict__ v_out,
@@ -108,8 +109,8 @@ __device__ __forceinline__ void copy_rows(const uint4* __restrict__ k, const uin
         for (int u = 0; u < UNROLL; ++u) {
             const int i = i0 + u * nt;
             if (i < nvec) {
-                kr[u] = __ldg(k + (head + src0) * VPR + i);
-                vr[u] = __ldg(v + (head + src0) * VPR + i);
+                kr[u] = __ldcg(k + (head + src0) * VPR + i);
+                vr[u] = __ldcg(v + (head + src0) * VPR + i);
             }
         }
 #pragma unroll
@@ -150,8 +151,8 @@ tpr_select_kernel(Problem p, const float* __restrict__ scores, const int32_t* __
     __shared__ int s_kk;
     __shared__ int s_ties;
 
-    // a kernel after this one (the next eviction's score kernel) reads nothing
-    // this one writes: it may be scheduled once every CTA of this grid has begun
+    // a kernel after this one (the next eviction's score kernel) waits before it reads
+    // what this one writes: it may be scheduled once every CTA of this grid has begun
     if (COMPACT) griddep_launch_dependents();
     // fused form: CTA 2h selects head h and gathers its interior rows, CTA
     // 2h + 1 copies its edge rows
@@ -388,8 +389,8 @@ tpr_select_kernel(Problem p, const float* __restrict__ scores, const int32_t* __
             const int r = r0 + u * RPI + sub;
             if (r < n) {
                 const size_t src = (head + rows[r]) * VPR + vec;
-                kr[u] = __ldg(k + src);
-                vr[u] = __ldg(v + src);
+                kr[u] = __ldcg(k + src);
+                vr[u] = __ldcg(v + src);
             }
         }
 #pragma unroll
@@ -424,8 +425,8 @@ tpr_select_warp_kernel(Problem p, const float* __restrict__ scores,
     extern __shared__ __align__(16) unsigned char dyn_raw[];
     const int wid = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int nw = blockDim.x >> 5;
-    // a kernel after this one (the next eviction's score kernel) reads nothing
-    // this one writes: it may be scheduled once every CTA of this grid has begun
+    // a kernel after this one (the next eviction's score kernel) waits before it reads
+    // what this one writes: it may be scheduled once every CTA of this grid has begun
     griddep_launch_dependents();
     const size_t mod_bytes = ((size_t)p.N + 15) & ~size_t(15);
     uint8_t* modality = dyn_raw;
@@ -584,8 +585,8 @@ tpr_select_warp_kernel(Problem p, const float* __restrict__ scores,
             const int r = r0 + u * RPI + sub;
             if (r < n) {
                 const size_t src = (head + rows[r]) * VPR + vec;
-                kr[u] = __ldg(k + src);
-                vr[u] = __ldg(v + src);
+                kr[u] = __ldcg(k + src);
+                vr[u] = __ldcg(v + src);
             }
         }
 #pragma unroll
@@ -865,8 +866,8 @@ tpr_select_general_kernel(Problem p, const float* __restrict__ scores,
             const int r = r0 + u * RPI + sub;
             if (r < n) {
                 const size_t src = (head + rows[r]) * VPR + vec;
-                kr[u] = __ldg(k + src);
-                vr[u] = __ldg(v + src);
+                kr[u] = __ldcg(k + src);
+                vr[u] = __ldcg(v + src);
             }
         }
 #pragma unroll
