@@ -41,7 +41,8 @@ __device__ __forceinline__ void check_spans(const CacheProblem& p, const ChunkAr
     for (int s = tid; s < p.S; s += threads) {
         const int b = s / p.H_kv;
         const int lo = a.tok_offsets[b], hi = a.tok_offsets[b + 1], len = a.lens[s];
-        if (lo < 0 || hi < lo || hi > a.T || hi - lo > a.max_q || len < 0 || len > p.cap)
+        if ((s == 0 && lo != 0) || lo < 0 || hi < lo || hi > a.T || hi - lo > a.max_q || len < 0 ||
+            len > p.cap)
             raise_status(status, TGVKV_STATUS_INDEX);
     }
 }

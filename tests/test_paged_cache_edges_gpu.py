@@ -1,0 +1,75 @@
+"""GPU tests of the paged cache's attention at its edges: faults in the offsets.
+
+Tolerances.  The weights of one output, relative to the largest, are rounded to bf16
+for the value product (a relative error d_j of at most 2^-9 each) and summed unrounded;
+the output is rounded to bf16 (at most 2^-9).  So for every element
+    |error| <= 2^-9 sum_j A_j |v_j| + 2^-9 |o| <= 2^-8 sum_j A_j |v_j|,
+of which twice is allowed (the fp32 accumulation has its room in it), and for a whole
+output row, over values v_j whose signs are independent of the d_j,
+    E |error - output rounding|^2 = sum_j A_j^2 d_j^2 |v_j|^2 <= 2^-18 sum_j A_j^2 |v_j|^2,
+of whose root four times is allowed, plus 2^-8 |o| for the output's rounding and the
+accumulation.  A lost slot moves the row by A_j |v_j|, which is more up to thousands of
+slots of equal weight."""
+import numpy as np
+import pytest
+import torch
+
+import _cache_ref as R
+from test_paged_cache_gpu import FORMATS, Box, api, dev_bf16, host_bits  # noqa: F401 (api: the fixture)
+
+pytestmark = pytest.mark.gpu
+INDEX = 0x08
+
+
+def ints(x):
+    return torch.tensor(list(x), dtype=torch.int32, device="cuda")
+
+
+def weights(q, k, seen, scale):
+    """fp64 attention weights [G, seen] of one token's heads."""
+    x = scale * (q @ k[:seen].T)
+    p = np.exp(x - x.max(-1, keepdims=True))
+    return p / p.sum(-1, keepdims=True)
+
+
+def check_rows(box, news, q, got, t0=0):
+    """Both bounds of the module's comment, for every output row."""
+    G = box.H_q // box.H_kv
+    for b, n in enumerate(news):
+        for g in range(box.H_kv):
+            s = b * box.H_kv + g
+            for i in range(n):
+                o, seen = got[t0 + i, g * G:(g + 1) * G], box.lens[s] - n + i + 1
+                if seen <= 0:
+                    assert (o == 0).all()
+                    continue
+                a = weights(q[t0 + i, g * G:(g + 1) * G], box.k[s], seen, box.scale)
+                v = box.v[s][:seen]
+                ref = a @ v
+                err = o - ref
+                top = np.abs(v).max()
+                assert (np.abs(err) <= 2.0 ** -7 * (a @ np.abs(v)) + 1e-9 * top).all(), (b, g, i)
+                spread = np.sqrt((a * a) @ (v * v).sum(-1))
+                norm = np.linalg.norm(ref, axis=-1)
+                assert (np.linalg.norm(err, axis=-1) <= 2.0 ** -7 * spread + 2.0 ** -8 * norm).all(), (b, g, i)
+        t0 += n
+
+
+# ---------------------------------------------------------------- faults in the offsets
+@pytest.mark.parametrize("fmt", ["bf16", "int8"])
+@pytest.mark.parametrize("news", [[1, 2], [2, 1], [40, 17]])
+def test_offsets_that_do_not_start_at_zero_are_reported(api, fmt, news):
+    """The status says so, in both kernels; the tokens there are get their attention and
+    the rows before them stay as they were."""
+    box = Box(api, 2, 4, 2, 64, 16, fmt, 90)
+    box.fill([70, 90, 45, 66])
+    T, skip = sum(news) + 1, 1
+    q = R.bf16_values(R.bf16_bits(box.rng.standard_normal((T, 4, 64))))
+    out = torch.full((T, 4, 64), 3.0, dtype=torch.bfloat16, device="cuda")
+    off = ints([skip, skip + news[0], T])
+    api.tgvkv_chunk_attention(box.desc, box.cache, box.table, box.lens_t(box.lens),
+                              dev_bf16(R.bf16_bits(q)).view(T, 4, 64), off, max(news), out, box.ws)
+    assert api.tgvkv_status(box.ws) == INDEX
+    got = R.bf16_values(host_bits(out)).reshape(T, 4, 64)
+    assert (got[:skip] == 3).all()
+    check_rows(box, news, q[skip:], got[skip:])
