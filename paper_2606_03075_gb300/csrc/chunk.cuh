@@ -19,7 +19,9 @@ struct ChunkArgs {
     uint16_t* out;               // [T][H_q][d]
 };
 
-// Set s: its slots, its sequence's new tokens and the first of them.
+// Set s: its sequence's new tokens and the first of them, and the slots up to the
+// last of them.  Tokens past max_q or past q's end are left out, with the slots they
+// stand for, so that the others see what they would have seen.
 struct SetSpan {
     int len, n, tok0;
 };
@@ -28,9 +30,10 @@ __device__ __forceinline__ SetSpan set_span(const CacheProblem& p, const ChunkAr
     SetSpan r;
     const int b = s / p.H_kv;
     const int lo = a.tok_offsets[b], hi = a.tok_offsets[b + 1];
-    r.len = clamp_len(a.lens[s], p.cap);
     r.tok0 = min(max(lo, 0), a.T);
-    r.n = min(min(max(hi, r.tok0), a.T) - r.tok0, a.max_q);
+    const int all = max(hi, r.tok0) - r.tok0;
+    r.n = min(min(all, a.T - r.tok0), a.max_q);
+    r.len = max(clamp_len(a.lens[s], p.cap) - (all - r.n), 0);
     return r;
 }
 

@@ -1,4 +1,5 @@
-"""GPU tests of the paged cache's attention at its edges: faults in the offsets.
+"""GPU tests of the paged cache's attention at its edges: faults in the offsets, and
+chunks longer than the caller said.
 
 Tolerances.  The weights of one output, relative to the largest, are rounded to bf16
 for the value product (a relative error d_j of at most 2^-9 each) and summed unrounded;
@@ -73,3 +74,28 @@ def test_offsets_that_do_not_start_at_zero_are_reported(api, fmt, news):
     got = R.bf16_values(host_bits(out)).reshape(T, 4, 64)
     assert (got[:skip] == 3).all()
     check_rows(box, news, q[skip:], got[skip:])
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "int8", "int4"])
+@pytest.mark.parametrize("H_q,news,most", [(4, [5, 2], 3), (4, [2, 7], 2), (8, [70, 20], 33), (2, [200, 3], 150)])
+def test_a_chunk_longer_than_the_caller_said(api, fmt, H_q, news, most):
+    """The status says so; its first max_q tokens get their attention (each up to its own
+    slot, also where the set has fewer slots than the chunk has tokens), the rest no row."""
+    box = Box(api, 2, H_q, 2, 128, 16, fmt, 400)
+    box.fill([400, news[0] - 1, 333, 1])
+    T = sum(news)
+    q = R.bf16_values(R.bf16_bits(box.rng.standard_normal((T, H_q, 128))))
+    out = torch.full((T, H_q, 128), 3.0, dtype=torch.bfloat16, device="cuda")
+    api.tgvkv_chunk_attention(box.desc, box.cache, box.table, box.lens_t(box.lens),
+                              dev_bf16(R.bf16_bits(q)).view(T, H_q, 128), ints([0, news[0], T]), most, out, box.ws)
+    assert api.tgvkv_status(box.ws) == INDEX
+    got = R.bf16_values(host_bits(out)).reshape(T, H_q, 128)
+    lens, t0 = box.lens, 0
+    for b, n in enumerate(news):
+        done = min(n, most)
+        # the computed tokens are the last of the slots before the ones left out
+        box.lens = [x - (n - done) for x in lens]
+        alone = [done if x == b else 0 for x in range(2)]
+        check_rows(box, alone, q[t0:t0 + done], got[t0:t0 + done])
+        assert (got[t0 + done:t0 + n] == 3).all()
+        t0 += n
