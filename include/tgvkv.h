@@ -472,8 +472,12 @@ int tgvkv_cache_read(const tgvkv_cache_desc* desc, const tgvkv_cache_pools* pool
  * out: bf16 [n_tokens][H_q][d], 16-byte aligned.
  * bf16 products with fp32 accumulation and softmax; the attention weights enter
  * the value product rounded to bf16, and out is rounded to bf16.  The slots of
- * a set must hold finite values up to its length; what lies in its pages past
- * the length does not matter, whatever it is. */
+ * a set must hold finite values up to its length, also those that some tokens do
+ * not see; what lies in its pages past the length does not matter, whatever it is.
+ * Values V between 2^-100 and 2^100 in magnitude (and zeros) are exact to the
+ * roundings named: the weights are relative to a logit that may lie 8 (base 2)
+ * below the row's largest, so sums of larger values may overflow fp32, and bf16
+ * weights times the scales of smaller ones may fall below bf16's normal numbers. */
 int tgvkv_chunk_attention(const tgvkv_cache_desc* desc, const tgvkv_cache_pools* pools,
                           const int32_t* page_table, const int32_t* lens, const uint16_t* q,
                           int64_t q_tok_stride, int64_t q_head_stride, int64_t n_tokens,

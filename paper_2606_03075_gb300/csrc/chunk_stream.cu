@@ -589,9 +589,10 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
                     for (int nb = 0; nb < NB; ++nb) mma(o[t][nb], r, pb[nb][0], pb[nb][1]);
                 }
             } else {
-                // V's scales go to P instead (exactly: they are powers of two), 2 values a
-                // group where V has 32: the scales of this lane's slot pairs (2 tq, + 1) and
-                // (2 tq + 8, + 9)
+                // V's scales go to P instead, 2 values a group where V has 32 (exactly, as they are
+                // powers of two, while P 2^e, P at most 2^8, stays a normal bf16 number: not
+                // for P below 2^-126-e or e above 119): the scales of this lane's slot pairs
+                // (2 tq, + 1) and (2 tq + 8, + 9)
                 constexpr int NG = D / kGroup, UPG = Gm::ROWB / 16 / NG;   // units a group
                 uint32_t sw[2][2];     // scale bytes of slot pair h, one slot and the next
 #pragma unroll

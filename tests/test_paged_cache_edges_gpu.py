@@ -1,5 +1,5 @@
-"""GPU tests of the paged cache's attention at its edges: faults in the offsets, and
-chunks longer than the caller said.
+"""GPU tests of the paged cache's attention at its edges: faults in the offsets, chunks
+longer than the caller said, and the range of the values.
 
 Tolerances.  The weights of one output, relative to the largest, are rounded to bf16
 for the value product (a relative error d_j of at most 2^-9 each) and summed unrounded;
@@ -99,3 +99,27 @@ def test_a_chunk_longer_than_the_caller_said(api, fmt, H_q, news, most):
         check_rows(box, alone, q[t0:t0 + done], got[t0:t0 + done])
         assert (got[t0 + done:t0 + n] == 3).all()
         t0 += n
+
+
+# ---------------------------------------------------------------- the range of the values
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("exponent", [-100, -60, 60, 100])
+def test_values_of_any_magnitude(api, fmt, d, exponent):
+    """Values of magnitudes around 2^-100 to 2^100, beside logits that rise along the
+    cache (so that weights above the running reference occur), in both kernels."""
+    box = Box(api, 2, 8, 4, d, 32, fmt, 900)
+    box.fill([900 - 100 * s for s in range(8)])
+    v, off = [], np.concatenate([[0], np.cumsum(box.lens)]).astype(np.int64)
+    for s in range(8):
+        v.append(R.bf16_values(R.bf16_bits(box.values(box.lens[s]).astype(np.float32))) * 2.0 ** exponent)
+        box.k[s] = box.k[s] * np.linspace(0, 4, box.lens[s])[:, None]
+    k = R.bf16_values(R.bf16_bits(np.concatenate(box.k)))
+    api.tgvkv_cache_write_rows(box.desc, box.cache, box.table, ints([0] * 8), dev_bf16(R.bf16_bits(k)).view(-1, d),
+                               dev_bf16(R.bf16_bits(np.concatenate(v))).view(-1, d),
+                               torch.from_numpy(off).cuda(), ints([0] * 8), box.ws)
+    kk, vv = R.round_trip(k, fmt), R.round_trip(np.concatenate(v), fmt)
+    box.k, box.v = ([x[off[s]:off[s + 1]] for s in range(8)] for x in (kk, vv))
+    for news in ([1, 1], [2, 3], [40, 70]):
+        q, got = box.attend(news)
+        check_rows(box, news, q, got)
