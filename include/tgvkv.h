@@ -468,7 +468,8 @@ int tgvkv_cache_read(const tgvkv_cache_desc* desc, const tgvkv_cache_pools* pool
  *   in elements, multiples of 8), 16-byte aligned, n_tokens rows;
  * max_q: an upper bound of the new tokens of a sequence (a larger chunk sets
  *   TGVKV_STATUS_INDEX; its first max_q tokens are computed, each over the slots up
- *   to its own, and the others are not);
+ *   to its own, and the others are not).  0, or n_tokens = 0, is a call without work:
+ *   arguments are checked, nothing on the device is, nothing is launched;
  * out: bf16 [n_tokens][H_q][d], 16-byte aligned.
  * bf16 products with fp32 accumulation and softmax; the attention weights enter
  * the value product rounded to bf16, and out is rounded to bf16.  The slots of
