@@ -1,5 +1,6 @@
 """GPU tests of the paged cache's attention at its edges: faults in the offsets, chunks
-longer than the caller said, and the range of the values.
+longer than the caller said, every slot counted once, many query heads per KV head,
+and the range of the values.
 
 Tolerances.  The weights of one output, relative to the largest, are rounded to bf16
 for the value product (a relative error d_j of at most 2^-9 each) and summed unrounded;
@@ -99,6 +100,79 @@ def test_a_chunk_longer_than_the_caller_said(api, fmt, H_q, news, most):
         check_rows(box, alone, q[t0:t0 + done], got[t0:t0 + done])
         assert (got[t0 + done:t0 + n] == 3).all()
         t0 += n
+
+
+# ---------------------------------------------------------------- every slot, once
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,H_q,H_kv,page,longest,news", [
+    (1, 2, 2, 64, 9001, [1]), (1, 2, 1, 16, 9001, [8]), (1, 14, 2, 256, 8193, [1]), (2, 4, 4, 32, 4100, [5, 5]),
+    (1, 2, 2, 64, 9001, [70]), (2, 7, 1, 16, 5003, [90, 300]), (6, 16, 16, 64, 700, [96, 17, 128, 1, 40, 0]),
+    (40, 8, 8, 64, 900, [1] * 40), (8, 2, 2, 16, 500, [1, 2, 0, 4, 3, 1, 1, 2])])
+def test_every_slot_counts_once(api, fmt, d, B, H_q, H_kv, page, longest, news):
+    """Keys of zero weigh every visible slot alike, and slot j's value is 1 in dim j mod d
+    alone: output c is (slots seen of residue c) / (slots seen), a quotient of integers.
+    Sums of ones are exact and so is P; one slot more or less changes a count below 142
+    by more than 2^-7.2, and the output is rounded once (2^-9)."""
+    box = Box(api, B, H_q, H_kv, d, page, fmt, longest)
+    lens = [longest - (s * 7919) % (longest // 2) for s in range(box.S)]
+    off = np.concatenate([[0], np.cumsum(lens)]).astype(np.int64)
+    v = np.zeros((int(off[-1]), d))
+    at = np.concatenate([np.arange(n) for n in lens])
+    v[np.arange(len(at)), at % d] = 1
+    k_t, v_t = torch.zeros(len(at), d, dtype=torch.bfloat16, device="cuda"), dev_bf16(R.bf16_bits(v)).view(-1, d)
+    api.tgvkv_cache_write_rows(box.desc, box.cache, box.table, ints([0] * box.S), k_t, v_t,
+                               torch.from_numpy(off).cuda(), ints([0] * box.S), box.ws)
+    box.lens = lens
+    _, got = box.attend(news)
+    G, t0 = H_q // H_kv, 0
+    for b, n in enumerate(news):
+        for g in range(H_kv):
+            for i in range(n):
+                seen = lens[b * H_kv + g] - n + i + 1
+                want = np.bincount(np.arange(max(seen, 0)) % d, minlength=d) / max(seen, 1)
+                o = got[t0 + i, g * G:(g + 1) * G]
+                assert (np.abs(o - want) <= 2.0 ** -8 * want).all(), (b, g, i)
+        t0 += n
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("B,H_q,H_kv,d,longest,news", [
+    (1, 4, 2, 128, 9001, [1]), (1, 4, 2, 128, 9001, [4]), (1, 4, 2, 64, 9001, [20]), (4, 8, 8, 64, 2000, [3] * 4),
+    (4, 16, 8, 128, 600, [40, 1, 0, 33]), (1, 7, 1, 128, 3000, [150])])
+def test_rows_within_their_spread(api, fmt, B, H_q, H_kv, d, longest, news):
+    """Random values: every element, and every row as a whole."""
+    box = Box(api, B, H_q, H_kv, d, 64, fmt, longest)
+    box.fill([longest - (s * 911) % (longest // 3) for s in range(box.S)])
+    q, got = box.attend(news)
+    check_rows(box, news, q, got)
+
+
+# ---------------------------------------------------------------- many heads a KV head
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G", [32, 33, 65, 100, 128])
+@pytest.mark.parametrize("H_kv,page,lens,news", [
+    (1, 16, [300, 77, 1, 0], [1, 1, 1, 1]), (2, 64, [130, 129, 3, 128, 257, 60], [2, 0, 3]),
+    (1, 256, [1400, 20], [29, 30]), (2, 32, [6000, 5500], [1])])
+def test_many_query_heads(api, fmt, d, G, H_kv, page, lens, news):
+    """17 to 128 query heads a KV head: row tiles of one to four tokens, partly filled
+    warps, one token as a tile, items over several CTAs."""
+    box = Box(api, len(news), G * H_kv, H_kv, d, page, fmt, max(lens))
+    box.fill(lens)
+    q, got = box.attend(news)
+    check_rows(box, news, q, got)
+    assert np.array_equal(got, box.attend(news, q=q)[1])
+
+
+def test_thousands_of_sets_with_few_tokens(api):
+    """2050 sequences of which one has a token, then every third one or two."""
+    B = 2050
+    box = Box(api, B, 2, 2, 64, 16, "int8", 40)
+    box.fill([(s * 7) % 41 for s in range(2 * B)])
+    for news in ([int(b == 1371) for b in range(B)], [(b + 1) % 3 for b in range(B)]):
+        q, got = box.attend(news)
+        box.check(news, q, got)
 
 
 # ---------------------------------------------------------------- the range of the values
