@@ -383,7 +383,8 @@ int tgvkv_decode_launches(const tgvkv_desc* desc);
  * Faults found on the device set TGVKV_STATUS_INDEX and touch nothing out of
  * range: a length outside [0, max_pages * page_size], token or row offsets that
  * do not start at 0, decrease or exceed their tensors, a set that would grow past
- * its pages, a page number outside [0, n_pages) that is needed. */
+ * its pages, a page number outside [0, n_pages) that is needed.  Pointers to int32
+ * are 4-byte aligned, to int64 8-byte (TGVKV_ERR_INVALID_ARG otherwise). */
 #define TGVKV_CACHE_BF16 0
 #define TGVKV_CACHE_INT8 1
 #define TGVKV_CACHE_INT4 2

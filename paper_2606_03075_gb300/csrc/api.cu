@@ -426,6 +426,14 @@ int check_tokens(const CacheProblem& p, const char* name, const uint16_t* ptr, i
     return TGVKV_OK;
 }
 
+// An int32 array of the paged-cache calls.
+int check_ints(const int32_t* ptr, const char* name) {
+    REQUIRE_PTR(ptr, name, false);
+    if ((reinterpret_cast<uintptr_t>(ptr) & 3u) != 0)
+        return fail(TGVKV_ERR_INVALID_ARG, "%s is not 4-byte aligned", name);
+    return TGVKV_OK;
+}
+
 int check_rows(const void* k, const char* k_name, const void* v, const char* v_name, int64_t n_rows,
                const int64_t* offsets) {
     if (n_rows < 0) return fail(TGVKV_ERR_INVALID_ARG, "n_rows=%lld < 0", (long long)n_rows);
@@ -442,9 +450,10 @@ int check_rows(const void* k, const char* k_name, const void* v, const char* v_n
 
 int check_write(const CacheProblem& p, const int32_t* page_table, const int32_t* lens,
                 const int32_t* lens_out, const void* workspace) {
-    REQUIRE_PTR(page_table, "page_table", false);
-    REQUIRE_PTR(lens, "lens", false);
-    REQUIRE_PTR(lens_out, "lens_out", false);
+    int rc;
+    if ((rc = check_ints(page_table, "page_table")) || (rc = check_ints(lens, "lens")) ||
+        (rc = check_ints(lens_out, "lens_out")))
+        return rc;
     const uintptr_t a = reinterpret_cast<uintptr_t>(lens), b = reinterpret_cast<uintptr_t>(lens_out);
     const uintptr_t bytes = sizeof(int32_t) * (uintptr_t)p.S;
     if (a < b + bytes && b < a + bytes)
@@ -774,7 +783,7 @@ int tgvkv_cache_write(const tgvkv_cache_desc* desc, const tgvkv_cache_pools* poo
         (rc = check_tokens(p, "v_new", v_new, v_tok_stride, v_head_stride, n_tokens, p.H_kv)) ||
         (rc = check_write(p, page_table, lens, lens_out, workspace)))
         return rc;
-    REQUIRE_PTR(tok_offsets, "tok_offsets", false);
+    if ((rc = check_ints(tok_offsets, "tok_offsets"))) return rc;
     const long long strides[4] = {(long long)k_tok_stride, (long long)k_head_stride,
                                   (long long)v_tok_stride, (long long)v_head_stride};
     cudaError_t e = launch_cache_write(p, pl, k_new, v_new, strides, (long long)n_tokens * p.H_kv,
@@ -812,7 +821,7 @@ int tgvkv_cache_read(const tgvkv_cache_desc* desc, const tgvkv_cache_pools* pool
     int rc = make_cache_problem(desc, &p);
     if (rc || (rc = check_pools(p, pools, &pl))) return rc;
     if ((rc = check_rows(k_out, "k_out", v_out, "v_out", n_rows, offsets))) return rc;
-    REQUIRE_PTR(page_table, "page_table", false);
+    if ((rc = check_ints(page_table, "page_table")) || (first && (rc = check_ints(first, "first")))) return rc;
     REQUIRE_PTR(workspace, "workspace", true);
     cudaError_t e = launch_cache_read(p, pl, page_table, first, offsets, k_out, v_out,
                                       (long long)n_rows, static_cast<uint32_t*>(workspace),
@@ -831,9 +840,9 @@ int tgvkv_chunk_attention(const tgvkv_cache_desc* desc, const tgvkv_cache_pools*
     if (rc || (rc = check_pools(p, pools, &pl))) return rc;
     if ((rc = check_tokens(p, "q", q, q_tok_stride, q_head_stride, n_tokens, p.H_q))) return rc;
     if (max_q < 0) return fail(TGVKV_ERR_INVALID_ARG, "max_q=%d < 0", max_q);
-    REQUIRE_PTR(page_table, "page_table", false);
-    REQUIRE_PTR(lens, "lens", false);
-    REQUIRE_PTR(tok_offsets, "tok_offsets", false);
+    if ((rc = check_ints(page_table, "page_table")) || (rc = check_ints(lens, "lens")) ||
+        (rc = check_ints(tok_offsets, "tok_offsets")))
+        return rc;
     if (n_tokens > 0) REQUIRE_PTR(out, "out", true);
     REQUIRE_PTR(workspace, "workspace", true);
     if (n_tokens == 0 || max_q == 0) return ok();   // no token to compute
