@@ -471,6 +471,14 @@ def _dev(t, dtype, numel, name):
     return _ptr(t, (dtype,), numel, name)
 
 
+def _table(desc, t, geo):
+    """The page table: flat, or with max_pages as its last dimension (another width would
+    be read with the wrong row length)."""
+    if isinstance(t, torch.Tensor) and t.dim() > 1 and t.shape[-1] != desc.max_pages:
+        raise ValueError(f"page_table has shape {tuple(t.shape)}, expected max_pages = {desc.max_pages} columns")
+    return _dev(t, torch.int32, geo[2], "page_table")
+
+
 def _pools(desc, cache: PagedCache, geo):
     dtypes = _POOL[desc.format][0]
     k, v = _ptr(cache.k, dtypes, geo[3], "cache.k"), _ptr(cache.v, dtypes, geo[3], "cache.v")
@@ -516,7 +524,7 @@ def tgvkv_cache_write(desc, cache: PagedCache, page_table, lens, k_new, v_new, t
         raise ValueError(f"k_new has {n} tokens, v_new {nv}")
     _check(_lib.load().tgvkv_cache_write(
         ctypes.byref(desc), _pools(desc, cache, geo),
-        _dev(page_table, torch.int32, geo[2], "page_table"), _dev(lens, torch.int32, sets, "lens"),
+        _table(desc, page_table, geo), _dev(lens, torch.int32, sets, "lens"),
         kp, kt, kh, vp, vt, vh, n, _dev(tok_offsets, torch.int32, desc.B + 1, "tok_offsets"),
         _dev(lens_out, torch.int32, sets, "lens_out"), _dev(ws, torch.uint8, geo[0], "workspace"),
         _stream(stream)), "tgvkv_cache_write")
@@ -531,7 +539,7 @@ def tgvkv_cache_write_rows(desc, cache: PagedCache, page_table, lens, k_rows, v_
     rows = min(k_rows.numel(), v_rows.numel()) // desc.d if kp is not None and vp is not None else 0
     _check(_lib.load().tgvkv_cache_write_rows(
         ctypes.byref(desc), _pools(desc, cache, geo),
-        _dev(page_table, torch.int32, geo[2], "page_table"), _dev(lens, torch.int32, sets, "lens"),
+        _table(desc, page_table, geo), _dev(lens, torch.int32, sets, "lens"),
         kp, vp, rows, _dev(offsets, torch.int64, sets + 1, "offsets"),
         _dev(lens_out, torch.int32, sets, "lens_out"), _dev(ws, torch.uint8, geo[0], "workspace"),
         _stream(stream)), "tgvkv_cache_write_rows")
@@ -547,7 +555,7 @@ def tgvkv_cache_read(desc, cache: PagedCache, page_table, first, offsets, k_out,
     rows = min(k_out.numel(), v_out.numel()) // desc.d if kp is not None and vp is not None else 0
     _check(_lib.load().tgvkv_cache_read(
         ctypes.byref(desc), _pools(desc, cache, geo),
-        _dev(page_table, torch.int32, geo[2], "page_table"),
+        _table(desc, page_table, geo),
         None if first is None else _dev(first, torch.int32, sets, "first"),
         _dev(offsets, torch.int64, sets + 1, "offsets"), kp, vp, rows,
         _dev(ws, torch.uint8, geo[0], "workspace"), _stream(stream)), "tgvkv_cache_read")
@@ -563,7 +571,7 @@ def tgvkv_chunk_attention(desc, cache: PagedCache, page_table, lens, q, tok_offs
     qp, qt, qh, n = _tokens(q, heads, d, "q")
     _check(_lib.load().tgvkv_chunk_attention(
         ctypes.byref(desc), _pools(desc, cache, geo),
-        _dev(page_table, torch.int32, geo[2], "page_table"), _dev(lens, torch.int32, geo[1], "lens"),
+        _table(desc, page_table, geo), _dev(lens, torch.int32, geo[1], "lens"),
         qp, qt, qh, n, _dev(tok_offsets, torch.int32, desc.B + 1, "tok_offsets"), max_q,
         _ptr(out, _BF16_LIKE, n * heads * d, "out"), _dev(ws, torch.uint8, geo[0], "workspace"),
         _stream(stream)), "tgvkv_chunk_attention")
