@@ -63,10 +63,17 @@ def desc_for_workload(wl, softmax_scale=0.0, **options) -> Desc:
                      **options)
 
 
+# The current stream's handle without a Stream object around it (which costs 5 us a
+# call).  Not public names: where a torch lacks them, the public way is taken.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_raw_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
 def _stream(stream):
     if stream is None:
-        # the current stream's handle, without a Stream object around it (5 us a call)
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        if _raw_stream is None or _raw_device is None:
+            return torch.cuda.current_stream().cuda_stream
+        return _raw_stream(_raw_device())
     if isinstance(stream, torch.cuda.Stream):
         return stream.cuda_stream
     return int(stream)
