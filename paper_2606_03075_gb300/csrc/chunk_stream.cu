@@ -144,16 +144,6 @@ __device__ __forceinline__ uint32_t swz(int r, int u) {
     return (uint32_t)(r * TROW + ((u ^ ((r >> shift) & mask)) << 4));
 }
 
-// Plain (untiled) copy of `bytes` (a multiple of 16, both sides aligned).
-__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes,
-                                          uint64_t* bar) {
-    asm volatile(
-        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
-            dst),
-        "l"(__cvta_generic_to_global(src)), "r"(bytes), "r"(smem_u32(bar))
-        : "memory");
-}
-
 // Chunks of a set: its last new token sees every slot.
 template <int CH>
 __device__ __forceinline__ int set_chunks(const SetSpan& sp) {
@@ -224,15 +214,15 @@ __device__ __forceinline__ void issue(unsigned char* stage, unsigned char* side,
         }
         if (FMT != TGVKV_CACHE_BF16) {
             const size_t off = (size_t)row * Gm::SCB;
-            bulk_copy(smem_u32(side + Gm::kKS) + at * Gm::SCB, pool.ks + off, box * Gm::SCB, bar);
-            bulk_copy(smem_u32(side + Gm::kVS) + at * Gm::SCB, pool.vs + off, box * Gm::SCB, bar);
+            tc::bulk_load(smem_u32(side + Gm::kKS) + at * Gm::SCB, pool.ks + off, box * Gm::SCB, bar);
+            tc::bulk_load(smem_u32(side + Gm::kVS) + at * Gm::SCB, pool.vs + off, box * Gm::SCB, bar);
         }
     }
     if (w.fresh && lane < w.sp.n * p.G) {
         const int i = lane / p.G, h = lane - i * p.G;
         const uint16_t* src = a.q + (long long)(w.sp.tok0 + i) * a.q_tok +
                               (long long)((w.s % p.H_kv) * p.G + h) * a.q_head;
-        bulk_copy(smem_u32(side + Gm::kQ) + lane * 2 * D, src, 2 * D, bar);
+        tc::bulk_load(smem_u32(side + Gm::kQ) + lane * 2 * D, src, 2 * D, bar);
     }
 }
 

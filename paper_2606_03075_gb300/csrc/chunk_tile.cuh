@@ -146,15 +146,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return r;
 }
 
-// Untiled copy of `bytes` (a multiple of 16, both sides 16-byte aligned).
-__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
-    asm volatile(
-        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
-            smem_u32(dst)),
-        "l"(__cvta_generic_to_global(src)), "r"(bytes), "r"(smem_u32(bar))
-        : "memory");
-}
-
 template <int D, int FMT, bool PAIR>
 struct TileGeom {
     static constexpr bool QUANT = FMT != TGVKV_CACHE_BF16;
@@ -522,11 +513,13 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
                         }
                         __syncwarp();
                         if (lane < nb)
-                            bulk_load(&sm.raw[st][b * box * Gm::ROWB], codes + (size_t)row * Gm::ROWB,
-                                      box * Gm::ROWB, &sm.raw_full[st]);
+                            tc::bulk_load(smem_u32(&sm.raw[st][b * box * Gm::ROWB]),
+                                          codes + (size_t)row * Gm::ROWB, box * Gm::ROWB,
+                                          &sm.raw_full[st]);
                         else if (lane >= 16 && b < nb)
-                            bulk_load(&sm.sc[st][b * box * (D / kGroup)], scales + (size_t)row * (D / kGroup),
-                                      box * (D / kGroup), &sm.raw_full[st]);
+                            tc::bulk_load(smem_u32(&sm.sc[st][b * box * (D / kGroup)]),
+                                          scales + (size_t)row * (D / kGroup), box * (D / kGroup),
+                                          &sm.raw_full[st]);
                     } else {
                         if (lane == 0) {
                             sm.filled[st] = it;

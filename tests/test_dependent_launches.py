@@ -16,7 +16,7 @@ DEPENDENTS = {
     "chunk_stream_merge": "chunk_stream.cu", "chunk_tile_kernel": "chunk_tile.cuh",
     "chunk_tile_merge": "chunk_merge.cu"}
 # (issue() is the row streams' copies)
-EARLY = re.compile(r"\b(tma_load_\w+|bulk_copy|bulk_load|issue\s*<|refill\s*\(\)|cp\.async\.bulk\.tensor|"
+EARLY = re.compile(r"\b(tma_load_\w+|bulk_load|issue\s*<|refill\s*\(\)|cp\.async\.bulk\.tensor|"
                    r"take_share|atomicAdd\(work_counter|copy_rows|__ldcs|__ldcg)")
 
 
