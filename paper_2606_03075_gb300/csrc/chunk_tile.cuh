@@ -285,19 +285,6 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volati
     return __all_sync(~0u, tc::mbar_wait(bar, parity, abort));
 }
 
-// Whether the phase with the given parity is complete: no wait.
-__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity)
-        : "memory");
-    return ok != 0;
-}
-
 // A warp's part of a record is written / is awaited and taken (the flag is down
 // again for the next call).  The wait is bounded like those on mbarriers.
 __device__ __forceinline__ void give_flag(uint32_t* flag, int lane) {
