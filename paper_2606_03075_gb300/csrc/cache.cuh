@@ -1,5 +1,5 @@
 // The paged cache (cache_rows.cu writes and reads it, chunk_stream.cu and
-// chunk_tile.cu attend to it): its geometry, its integer formats and the
+// chunk_tile.cuh attend to it): its geometry, its integer formats and the
 // conversions back to bf16.
 //
 // Set s = b * H_kv + g (sequence b, KV head g) owns page_table[s][0..max_pages)

@@ -1,5 +1,6 @@
 // Attention of a chunk of new tokens over the paged cache on the 5th-generation
-// tensor cores (tcgen05), for sets with more than 16 query rows.
+// tensor cores (tcgen05), for sets with more query rows than the row streams take
+// (stream_rows()).
 //
 //   o[t][h] = sum_{j <= len - n + i} softmax_j(scale <q[t][h], k_j>) v_j
 //
@@ -350,8 +351,7 @@ chunk_tile_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant_
             tc::tma_prefetch_desc(&mv);
         }
     }
-    // The kernel before has finished; the merge, which may start from now on, reads this
-    // call's inputs before it waits in turn.
+    // The kernels before have finished; the merge may start from now on (and waits in turn).
     griddep_wait();
     griddep_launch_dependents();
     if (warp == 1) {                   // (not before: a kernel still at work may yet want its own)
