@@ -31,9 +31,11 @@
 // order, so results do not depend on timing.
 //
 // What bounds it.  bf16: HBM (64 x 4 sets of one token over 4353 .. 8705 slots: 136 us,
-// 6.3 TB/s).  Integer caches: the instructions that turn codes into bf16 (about 60%
-// of the issue slots, the integer pipe at 62%; the same sets in int8 88 us, 5.0 TB/s,
-// int4 64 us), and the start and the merge, about 10 us of each call.
+// 6.3 TB/s).  Integer caches (the same sets in int8 88 us, 5.0 TB/s, int4 64 us): the chain
+// of one chunk, from conversion over S and its maximum to P V, with two warps a
+// scheduler to hide it: the integer pipe, which does the conversion, is at 51 to 54%, half
+// the cycles issue, and most stalls wait for the instruction before; and the start
+// and the merge, about 10 us of each call.
 //
 // Measured and not kept: partials joined inside this kernel, by flags that a set's
 // first stream awaits or by whichever stream comes last (the batch above 92 and 97 us

@@ -45,17 +45,20 @@
 // more than 2^8.  Every wait is bounded; a timeout sets TGVKV_STATUS_TIMEOUT and the
 // CTA unwinds after its copies and MMAs finished.
 //
-// What bounds it.  bf16, long chunks: the tensor cores (28 heads, 2048 tokens over
-// 34816 slots: 600 us, 1655 TFLOP/s, the rate a dense bf16 product holds under the
-// power limit).  Integer caches: shared memory, which carries the codes in, the bf16
-// copy out and in again and Q for every product, beside the converters' arithmetic (16 x
-// 0 .. 500 tokens over 4451 .. 8900 slots: int8 358 us, bf16 296).  One row tile a set: latency
-// (256 sets of 0 .. 96 tokens over 1553 .. 3104 slots: int8 64 us, bf16 60 us, 4.6 TB/s): the end
-// of a segment leaves the tensor cores idle for about 3 us, which only other work on
-// the SM could fill, and there is no room for a second CTA.
+// What bounds it.  bf16, long chunks: the tensor cores under the power limit (28 heads,
+// 2048 tokens over 34816 slots: 651 us, 1525 TFLOP/s, call after call, where a dense
+// bf16 product holds 1685; 600 us in a burst of a dozen calls).  Integer caches: no unit
+// is full (6 x 0 .. 500 tokens over 2001 .. 4000 slots, int8: tensor pipe 36%, integer pipe
+// 43%, shared-memory wavefronts 30%, an instruction issued in half the cycles): a key
+// tile passes from the copy to the converters to the products, and every pair of row
+// tiles brings and converts its set's tiles again (16 x 0 .. 500 tokens over 4451 .. 8900 slots:
+// int8 365 us, bf16 296).  One row tile a set: latency (256 sets of 0 .. 96 tokens over 1553 ..
+// 3104 slots: int8 65 us, bf16 60 us, 4.6 TB/s): the end of a segment leaves the tensor cores
+// idle for about 3 us, which only other work on the SM could fill, and there is no room
+// for a second CTA.
 //
 // Measured and not kept: one thread as the issuer (chunks over 34816 slots 763 us
-// against 627); one producer warp; four converter warps (16 x 0 .. 500 tokens, int4
+// against 627, in a burst); one producer warp; four converter warps (16 x 0 .. 500 tokens, int4
 // pages: 389 us against 360) and converters that load the next tile before they store
 // this one; deeper rings at d = 64; the next segment's place looked up before the
 // last products end (SPLIT 1% faster, PAIR 2% slower).
