@@ -371,7 +371,10 @@ int tgvkv_decode_launches(const tgvkv_desc* desc);
  *   TGVKV_CACHE_BF16  d bf16 values, bit copies of what was written;
  *   TGVKV_CACHE_INT8  d codes of 8 bits, two's complement;
  *   TGVKV_CACHE_INT4  d / 2 bytes, code + 8 in 4 bits, the even element in the
- *                     low half of a byte.
+ *                     low half of a byte;
+ *   TGVKV_CACHE_FP4   d / 2 bytes of 4-bit floats (1 sign, 2 exponent, 1 mantissa
+ *                     bits: the values 0, 0.5, 1, 1.5, 2, 3, 4, 6 have the codes 0 .. 7,
+ *                     plus 8 below zero), packed like TGVKV_CACHE_INT4.
  * The integer formats have a scale pool [n_pages][page_size][d / 32] of bytes,
  * one per 32 consecutive values: E = e + 127 for the scale 2^e, the smallest
  * power of two (e >= -126) with max |x| <= Q * 2^e, Q = 127 (8 bits) or 7 (4 bits;
@@ -379,6 +382,11 @@ int tgvkv_decode_launches(const tgvkv_desc* desc);
  * rounded to nearest, ties to even.  A group that holds an infinity or a NaN
  * has E = 255 and codes of 0 and reads back as NaN.  code * 2^e is exact in
  * bf16: the only rounding of the integer formats is the quantisation itself.
+ * TGVKV_CACHE_FP4 has the same scale bytes with Q = 6 and -60 <= e <= 56 (larger
+ * magnitudes saturate at 6 * 2^56; the attention multiplies codes of these scales
+ * exactly): x / 2^e goes to the nearest of the values, ties to the even code, a zero
+ * keeps its sign.  Its steps are finer near zero than at the top, where int4's are
+ * equal: groups with a few large values, such as keys, lose less.
  *
  * Faults found on the device set TGVKV_STATUS_INDEX and touch nothing out of
  * range: a length outside [0, max_pages * page_size], token or row offsets that
@@ -388,6 +396,7 @@ int tgvkv_decode_launches(const tgvkv_desc* desc);
 #define TGVKV_CACHE_BF16 0
 #define TGVKV_CACHE_INT8 1
 #define TGVKV_CACHE_INT4 2
+#define TGVKV_CACHE_FP4  4
 
 typedef struct tgvkv_cache_desc {
     int32_t B;              /* sequences */

@@ -36,7 +36,7 @@ class CachePools(ctypes.Structure):
     _fields_ = [("k", c_void_p), ("v", c_void_p), ("k_scale", c_void_p), ("v_scale", c_void_p)]
 
 
-CACHE_BF16, CACHE_INT8, CACHE_INT4 = 0, 1, 2
+CACHE_BF16, CACHE_INT8, CACHE_INT4, CACHE_FP4 = 0, 1, 2, 4
 BASIS_VISION, BASIS_ALL = 0, 1
 WEIGHTS_GIVEN, WEIGHTS_EQ7 = 0, 1
 STAT_TV, STAT_TT, STAT_UNIFORM = 0, 1, 2

@@ -387,13 +387,15 @@ def tgvkv_evict_launches(desc: Desc) -> int:
 # ---- the paged cache ---------------------------------------------------------
 
 CacheDesc = _lib.CacheDesc
-CACHE_FORMAT = {"bf16": _lib.CACHE_BF16, "int8": _lib.CACHE_INT8, "int4": _lib.CACHE_INT4}
+CACHE_FORMAT = {"bf16": _lib.CACHE_BF16, "int8": _lib.CACHE_INT8, "int4": _lib.CACHE_INT4,
+                "fp4": _lib.CACHE_FP4}
 CACHE_GROUP = 32   # values that share a scale
 
 # format -> (dtypes a pool may have, pool elements per row of d values)
 _POOL = {_lib.CACHE_BF16: (_BF16_LIKE, lambda d: d),
          _lib.CACHE_INT8: ((torch.int8, torch.uint8), lambda d: d),
-         _lib.CACHE_INT4: ((torch.uint8,), lambda d: d // 2)}
+         _lib.CACHE_INT4: ((torch.uint8,), lambda d: d // 2),
+         _lib.CACHE_FP4: ((torch.uint8,), lambda d: d // 2)}
 
 
 def make_cache_desc(B, H_q, H_kv, d, page_size, n_pages, max_pages, format="bf16",
@@ -402,7 +404,8 @@ def make_cache_desc(B, H_q, H_kv, d, page_size, n_pages, max_pages, format="bf16
 
     B: sequences (the requests of a batch, or the layers of one); page_size:
     slots per page (16 to 256, a power of two); n_pages: pages of the pool;
-    max_pages: page-table entries of a set; format: "bf16", "int8" or "int4"."""
+    max_pages: page-table entries of a set; format: "bf16", "int8", "int4" or "fp4"
+    (4-bit floats)."""
     return CacheDesc(B=B, H_q=H_q, H_kv=H_kv, d=d, page_size=page_size, n_pages=n_pages,
                      max_pages=max_pages, format=CACHE_FORMAT[format],
                      softmax_scale=float(softmax_scale))
@@ -410,7 +413,7 @@ def make_cache_desc(B, H_q, H_kv, d, page_size, n_pages, max_pages, format="bf16
 
 @dataclass
 class PagedCache:
-    k: torch.Tensor                      # [n_pages, page_size, d] (int4: d / 2)
+    k: torch.Tensor                      # [n_pages, page_size, d] (int4, fp4: d / 2)
     v: torch.Tensor
     k_scale: torch.Tensor | None = None  # uint8 [n_pages, page_size, d / 32]; None for bf16
     v_scale: torch.Tensor | None = None
@@ -492,7 +495,7 @@ def _pools(desc, cache: PagedCache, geo):
     if not geo[4]:
         return ctypes.byref(_lib.CachePools(k, v))
     if cache.k_scale is None or cache.v_scale is None:
-        raise ValueError("an integer cache needs k_scale and v_scale")
+        raise ValueError("a quantised cache needs k_scale and v_scale")
     return ctypes.byref(_lib.CachePools(k, v, _dev(cache.k_scale, torch.uint8, geo[4], "cache.k_scale"),
                                         _dev(cache.v_scale, torch.uint8, geo[4], "cache.v_scale")))
 

@@ -338,7 +338,7 @@ int make_cache_problem(const tgvkv_cache_desc* d, CacheProblem* p) {
         return fail(TGVKV_ERR_UNSUPPORTED, "page_size=%d unsupported (16, 32, 64, 128 or 256)",
                     d->page_size);
     if (d->format != TGVKV_CACHE_BF16 && d->format != TGVKV_CACHE_INT8 &&
-        d->format != TGVKV_CACHE_INT4)
+        d->format != TGVKV_CACHE_INT4 && d->format != TGVKV_CACHE_FP4)
         return fail(TGVKV_ERR_INVALID_ARG, "format=%d unknown", d->format);
     if (!(d->softmax_scale == d->softmax_scale) || isinf(d->softmax_scale))
         return fail(TGVKV_ERR_INVALID_ARG, "softmax_scale is not finite");
@@ -874,7 +874,8 @@ int tgvkv_chunk_attention(const tgvkv_cache_desc* desc, const tgvkv_cache_pools*
         const bool pair = a.max_q > TM / p.G;
         e = p.format == TGVKV_CACHE_BF16   ? launch_tile_bf16(p, pl, a, part, split, sync, pair, status, st)
             : p.format == TGVKV_CACHE_INT8 ? launch_tile_int8(p, pl, a, part, split, sync, pair, status, st)
-                                           : launch_tile_int4(p, pl, a, part, split, sync, pair, status, st);
+            : p.format == TGVKV_CACHE_INT4 ? launch_tile_int4(p, pl, a, part, split, sync, pair, status, st)
+                                           : launch_tile_fp4(p, pl, a, part, split, sync, pair, status, st);
     }
     return e == cudaSuccess ? ok() : cuda_fail(e, "chunk attention launch");
 }

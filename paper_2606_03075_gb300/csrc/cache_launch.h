@@ -38,6 +38,9 @@ cudaError_t launch_tile_int8(const CacheProblem& p, const CachePools& pool, cons
 cudaError_t launch_tile_int4(const CacheProblem& p, const CachePools& pool, const ChunkArgs& a,
                              float* part, SplitItem* split, uint32_t* sync, bool pair,
                              uint32_t* status, cudaStream_t stream);
+cudaError_t launch_tile_fp4(const CacheProblem& p, const CachePools& pool, const ChunkArgs& a,
+                             float* part, SplitItem* split, uint32_t* sync, bool pair,
+                             uint32_t* status, cudaStream_t stream);
 cudaError_t launch_tile_merge(const CacheProblem& p, const ChunkArgs& a, const TilePlan& pl, int ctas,
                               const float* part, const SplitItem* split, cudaStream_t stream);
 

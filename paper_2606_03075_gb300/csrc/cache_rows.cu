@@ -90,76 +90,6 @@ __device__ __forceinline__ int pool_row(const CacheProblem& p, const int32_t* pa
     return page * p.page + ((int)slot & (p.page - 1));
 }
 
-// ---- 8 values to their stored form -------------------------------------------
-// The scale byte of a group from the largest magnitude among its values, as
-// bf16 bits (15 bits).  With bits = 2^X' (1 + f / 128): Q = 127 needs
-// e = X' - 6, one more when f > 126 (the value is above 127 * 2^(X' - 6));
-// Q = 7 needs e = X' - 2, one more when f > 96.
-template <int FMT>
-__device__ __forceinline__ int group_byte(uint32_t bits) {
-    const int x = (int)(bits >> 7), f = (int)(bits & 127u);
-    if (x == 255) return 255;
-    if (FMT == TGVKV_CACHE_INT8) return max(x - 6 + (f > 126 ? 1 : 0), 1);
-    return min(max(x - 2 + (f > 96 ? 1 : 0), 1), 247);
-}
-
-// Quantise this lane's 8 values (the group's other 24 are in the 3
-// neighbouring lanes; the whole warp takes part) and, where `on`, store them
-// with the group's scale byte.
-template <int FMT>
-__device__ __forceinline__ void store_row(uint4 w, uint8_t* row, uint8_t* scales, int unit,
-                                          bool on) {
-    // magnitudes as bf16 bits order like the values; NaN sorts above infinity
-    const uint32_t words[4] = {w.x, w.y, w.z, w.w};
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) top = __vmaxu2(top, words[i] & 0x7FFF7FFFu);
-    top = max(top & 0xFFFFu, top >> 16);
-    top = max(top, __shfl_xor_sync(~0u, top, 1));
-    top = max(top, __shfl_xor_sync(~0u, top, 2));
-    const int byte = group_byte<FMT>(top);
-    if (!on) return;
-    if (FMT == TGVKV_CACHE_INT8) {
-        // x 2^-e + 1.5 * 2^23 rounds x 2^-e to an integer (ties to even) and leaves it, in two's
-        // complement, in the low bits; |x 2^-e| <= 127 by the choice of e
-        const float inv = __uint_as_float((uint32_t)(254 - min(byte, 253)) << 23);
-        uint32_t q[8];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            q[2 * i] = __float_as_uint(fmaf(__uint_as_float(words[i] << 16), inv, 12582912.f));
-            q[2 * i + 1] = __float_as_uint(fmaf(__uint_as_float(words[i] & 0xFFFF0000u), inv, 12582912.f));
-        }
-        uint32_t c[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            c[i] = __byte_perm(__byte_perm(q[4 * i], q[4 * i + 1], 0x0040),
-                               __byte_perm(q[4 * i + 2], q[4 * i + 3], 0x0040), 0x5410);
-            if (byte == 255) c[i] = 0u;
-        }
-        reinterpret_cast<uint2*>(row)[unit] = make_uint2(c[0], c[1]);
-    } else {
-        // in bf16, whose step is 1 from 128 to 256: x 2^-e + 136 rounds to 128 + (q + 8)
-        const uint32_t inv = both((uint32_t)(254 - min(byte, 253)) << 7);
-        uint32_t q[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (byte == 247) {         // e at its cap: the values may be beyond 7 * 2^e
-                const uint32_t v = bf16x2_min(bf16x2_max(bf16x2_mul(words[i], inv), 0xC0E0C0E0u), 0x40E040E0u);
-                q[i] = bf16x2_fma(v, 0x3F803F80u, 0x43084308u);
-            } else {
-                q[i] = bf16x2_fma(words[i], inv, 0x43084308u);
-            }
-        }
-        // the nibbles: elements 0, 2, 1, 3 (and 4, 6, 5, 7) a byte apart, then the odd ones
-        // beside the even ones
-        const uint32_t a = (q[0] & 0x000F000Fu) | ((q[1] & 0x000F000Fu) << 8);
-        const uint32_t b = (q[2] & 0x000F000Fu) | ((q[3] & 0x000F000Fu) << 8);
-        const uint32_t c = __byte_perm(a, b, 0x5410) | (__byte_perm(a, b, 0x7632) << 4);
-        reinterpret_cast<uint32_t*>(row)[unit] = byte == 255 ? 0x88888888u : c;
-    }
-    if ((unit & 3) == 0) scales[unit >> 2] = (uint8_t)byte;
-}
-
 // ---- write -------------------------------------------------------------------
 // The rows to write: of the CSR form, row u of [0, offsets[S]) belongs to the
 // set its offsets say; of the token form, row u = token * H_kv + head.
@@ -360,7 +290,8 @@ cudaError_t by_shape(const CacheProblem& p, F&& f) {
     auto fmt = [&](auto d) {
         if (p.format == TGVKV_CACHE_BF16) return f(d, Int<TGVKV_CACHE_BF16>());
         if (p.format == TGVKV_CACHE_INT8) return f(d, Int<TGVKV_CACHE_INT8>());
-        return f(d, Int<TGVKV_CACHE_INT4>());
+        if (p.format == TGVKV_CACHE_INT4) return f(d, Int<TGVKV_CACHE_INT4>());
+        return f(d, Int<TGVKV_CACHE_FP4>());
     };
     return p.d == 64 ? fmt(Int<64>()) : fmt(Int<128>());
 }

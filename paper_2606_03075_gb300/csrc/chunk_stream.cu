@@ -137,6 +137,10 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// bf16 bits of 2^(62 + e): with fp4x2_small()'s 2^-126, a 4-bit float of scale 2^e times
+// 2^-64, exact for e in [-60, 56] (255: infinity, which times a code of 0 is NaN).
+__device__ __forceinline__ uint32_t fp4_scale(uint32_t byte) { return min(byte + 62u, 255u) << 7; }
+
 // Byte offset of 16-byte unit u of row r in a tile that TMA wrote with the
 // swizzle of its row length (128, 64 or 32 bytes).
 template <int TROW>
@@ -255,6 +259,9 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
     using Gm = StreamGeom<D, FMT, NB>;
     constexpr int CH = Gm::CH, W = Gm::W;
     constexpr int KS = D / 16, MT = D / 16, KB = CH / 16;
+    // 4-bit floats are multiplied as K 2^-64 and, P having taken V's scales, as P V 2^-64
+    // (fp4_scale): one factor of 2^64 on S and on O in the place of one on every K and V
+    constexpr float kUp = FMT == TGVKV_CACHE_FP4 ? 0x1p64f : 1.f;
     if (threadIdx.x == 0) {
         tc::tma_prefetch_desc(&mk);
         tc::tma_prefetch_desc(&mv);
@@ -460,7 +467,9 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
                     }
                     const uint32_t byte =
                         lds8(sd + Gm::kKS + row * Gm::SCB + (D == 128 ? tq : tq >> 1));
-                    kb_s[x] = both(FMT == TGVKV_CACHE_INT8 ? scale_bf16(byte) : int4_base(byte));
+                    kb_s[x] = both(FMT == TGVKV_CACHE_INT8   ? scale_bf16(byte)
+                                   : FMT == TGVKV_CACHE_INT4 ? int4_base(byte)
+                                                             : fp4_scale(byte));
                 }
 #pragma unroll
                 for (int s = 0; s < KS; ++s) {
@@ -471,10 +480,14 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
                             const uint32_t c = wd[x][s % NW];
                             r[x] = bf16x2_mul(int8x2_to_bf16(c, p.magic), kb_s[x]);
                             r[2 + x] = bf16x2_mul(int8x2_to_bf16(c >> 8, p.magic), kb_s[x]);
-                        } else {
+                        } else if (FMT == TGVKV_CACHE_INT4) {
                             const uint32_t c = wd[x][(s / 2) % NW];
                             r[x] = int4x2_to_bf16(c >> (8 * (s & 1)), kb_s[x]);
                             r[2 + x] = int4x2_to_bf16(c >> (8 * (s & 1) + 4), kb_s[x]);
+                        } else {
+                            const uint32_t c = wd[x][(s / 2) % NW];
+                            r[x] = bf16x2_mul(s & 1 ? fp4x2_small<8>(c) : fp4x2_small<0>(c), kb_s[x]);
+                            r[2 + x] = bf16x2_mul(s & 1 ? fp4x2_small<12>(c) : fp4x2_small<4>(c), kb_s[x]);
                         }
                     }
 #pragma unroll
@@ -486,7 +499,7 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    sc[kb][nb][e] = (acc[0][nb][e] + acc[1][nb][e]) * p.scale_log2;
+                    sc[kb][nb][e] = (acc[0][nb][e] + acc[1][nb][e]) * kUp * p.scale_log2;
         }
         // ---- hide what a row must not see: slots from its token's on
         if (n < CH || key0 + CH > w.sp.len - w.sp.n + 1) {
@@ -607,9 +620,10 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
                         const int x = u / UPG;
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            const uint32_t sc2 =
+                            uint32_t sc2 =
                                 (__byte_perm(sw[h][0], sw[h][1], (x << 4) | ((4 + x) << 12)) >> 1) &
                                 0x7F807F80u;
+                            if (FMT == TGVKV_CACHE_FP4) sc2 = __vminu2(sc2 + 0x1F001F00u, 0x7F807F80u);
 #pragma unroll
                             for (int nb = 0; nb < NB; ++nb) pg[nb][h] = bf16x2_mul(pb[nb][h], sc2);
                         }
@@ -622,6 +636,17 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
                                                int8x2_to_bf16(r1, p.magic), int8x2_to_bf16(r1 >> 8, p.magic)};
 #pragma unroll
                         for (int nb = 0; nb < NB; ++nb) mma(o[u % MT][nb], v, pg[nb][0], pg[nb][1]);
+                    } else if (FMT == TGVKV_CACHE_FP4) {
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            const uint32_t v[4] = {y ? fp4x2_small<8>(r0) : fp4x2_small<0>(r0),
+                                                   y ? fp4x2_small<12>(r0) : fp4x2_small<4>(r0),
+                                                   y ? fp4x2_small<8>(r1) : fp4x2_small<0>(r1),
+                                                   y ? fp4x2_small<12>(r1) : fp4x2_small<4>(r1)};
+#pragma unroll
+                            for (int nb = 0; nb < NB; ++nb)
+                                mma(o[(2 * u + y) % MT][nb], v, pg[nb][0], pg[nb][1]);
+                        }
                     } else {
 #pragma unroll
                         for (int y = 0; y < 2; ++y) {
@@ -642,6 +667,14 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
         const bool ends = w.ends();
         if (ends) {
             // ---- the segment of set w.s is complete
+            if (FMT == TGVKV_CACHE_FP4) {
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[t][nb][e] *= kUp;
+            }
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -877,18 +910,16 @@ cudaError_t launch_rows(const CacheProblem& p, const CachePools& pool, const Chu
 
 cudaError_t launch_chunk_stream(const CacheProblem& p, const CachePools& pool, const ChunkArgs& a,
                                 float* part, long long* plan, uint32_t* status, cudaStream_t stream) {
-    if (p.d == 64) {
-        if (p.format == TGVKV_CACHE_BF16)
-            return launch_rows<64, TGVKV_CACHE_BF16>(p, pool, a, part, plan, status, stream);
-        if (p.format == TGVKV_CACHE_INT8)
-            return launch_rows<64, TGVKV_CACHE_INT8>(p, pool, a, part, plan, status, stream);
-        return launch_rows<64, TGVKV_CACHE_INT4>(p, pool, a, part, plan, status, stream);
+    const auto by_dim = [&](auto kernels_of_64, auto kernels_of_128) {
+        return p.d == 64 ? kernels_of_64(p, pool, a, part, plan, status, stream)
+                         : kernels_of_128(p, pool, a, part, plan, status, stream);
+    };
+    switch (p.format) {
+        case TGVKV_CACHE_BF16: return by_dim(launch_rows<64, TGVKV_CACHE_BF16>, launch_rows<128, TGVKV_CACHE_BF16>);
+        case TGVKV_CACHE_INT8: return by_dim(launch_rows<64, TGVKV_CACHE_INT8>, launch_rows<128, TGVKV_CACHE_INT8>);
+        case TGVKV_CACHE_INT4: return by_dim(launch_rows<64, TGVKV_CACHE_INT4>, launch_rows<128, TGVKV_CACHE_INT4>);
+        default: return by_dim(launch_rows<64, TGVKV_CACHE_FP4>, launch_rows<128, TGVKV_CACHE_FP4>);
     }
-    if (p.format == TGVKV_CACHE_BF16)
-        return launch_rows<128, TGVKV_CACHE_BF16>(p, pool, a, part, plan, status, stream);
-    if (p.format == TGVKV_CACHE_INT8)
-        return launch_rows<128, TGVKV_CACHE_INT8>(p, pool, a, part, plan, status, stream);
-    return launch_rows<128, TGVKV_CACHE_INT4>(p, pool, a, part, plan, status, stream);
 }
 
 }  // namespace tgvkv
