@@ -97,6 +97,7 @@ extern "C" {
 #define TGVKV_STATUS_COUNT        0x10u /* a retained set did not hold N_t + b_l rows */
 #define TGVKV_STATUS_TIMEOUT      0x20u /* a bounded on-chip wait gave up, or a workspace was not at zero */
 #define TGVKV_STATUS_WEIGHT       0x40u /* a text weight is negative or not finite */
+#define TGVKV_STATUS_PAGES        0x80u /* fewer free pages than a call had to take: it took none */
 
 /* ---- modes ------------------------------------------------------------ */
 #define TGVKV_BASIS_VISION  0   /* r counts vision KV; all text KV kept (default) */
@@ -494,6 +495,169 @@ int tgvkv_chunk_attention(const tgvkv_cache_desc* desc, const tgvkv_cache_pools*
                           int64_t q_tok_stride, int64_t q_head_stride, int64_t n_tokens,
                           const int32_t* tok_offsets, int32_t max_q, uint16_t* out,
                           void* workspace, void* stream);
+
+/* ---- pages: tables and slots built on the device ------------------------
+ *
+ * A pool's pages handed out to the sets of a descriptor as their lengths grow, and
+ * taken back, without the host knowing a length.  A set of lens[s] slots holds the
+ * pages that the first ceil(lens[s] / page_size) entries of its table row name; the
+ * other entries are -1, which the calls above refuse (TGVKV_STATUS_INDEX) instead of
+ * using.  free_pages[0 .. n_free) is a stack of the pages that no set holds.
+ *
+ * The calls below are exact and the same on every run: sets take pages from the top
+ * of the stack in the order of s, each set in the order of its table's entries, and
+ * give them back in the opposite order, so that taking pages and giving the same ones
+ * back leaves the list as it was.  A page belongs to one set; a prefix shared by hand
+ * is safe as long as no call shortens a set to less than it.
+ *
+ * A call does all it is asked or nothing: with a length outside [0, max_pages *
+ * page_size], offsets that do not start at 0, decrease or exceed n_tokens, a set that
+ * would outgrow its table row, or n_free outside [0, n_pages], it sets
+ * TGVKV_STATUS_INDEX and changes no table, no list (lens_out = lens, every slot -1);
+ * likewise TGVKV_STATUS_PAGES where fewer pages are free than it would take.  An
+ * entry of the stack, or of a table that gives pages back, that names no page of the
+ * pool moves as -1 and sets TGVKV_STATUS_INDEX.
+ *
+ * page_table, free_pages, n_free: int32, 4-byte aligned, device memory.  Calls on one
+ * list must follow one another (one stream, or events). */
+typedef struct tgvkv_page_list {
+    int32_t* page_table;    /* [B * H_kv][max_pages] */
+    int32_t* free_pages;    /* [n_pages] */
+    int32_t* n_free;        /* [1] */
+} tgvkv_page_list;
+
+/* An empty table (every entry -1) and every page free, page 0 on top. */
+int tgvkv_pages_init(const tgvkv_cache_desc* desc, const tgvkv_page_list* pages, void* stream);
+
+/* Set s goes from lens[s] to lens_new[s] slots: grow takes the pages it lacks (sets
+ * that would shrink keep theirs), shrink gives back the ones past lens_new[s], their
+ * entries becoming -1 (sets that would grow stay as they are).  A finished sequence
+ * shrinks to 0.  lens, lens_new: int32 [B * H_kv]. */
+int tgvkv_pages_grow(const tgvkv_cache_desc* desc, const tgvkv_page_list* pages,
+                     const int32_t* lens, const int32_t* lens_new, void* workspace, void* stream);
+int tgvkv_pages_shrink(const tgvkv_cache_desc* desc, const tgvkv_page_list* pages,
+                       const int32_t* lens, const int32_t* lens_new, void* workspace,
+                       void* stream);
+
+/* Room for new tokens: every set of sequence b grows by tok_offsets[b+1] -
+ * tok_offsets[b] slots, as tgvkv_pages_grow would grow it, and
+ *   lens_out[s] = lens[s] + tok_offsets[b+1] - tok_offsets[b],
+ *   slots[t][g] = the pool row of token t of KV head g (slot lens[s] + t -
+ *                 tok_offsets[b] of set s = b * H_kv + g), which is what
+ *                 tgvkv_rope_write writes to, in every layer that shares the table;
+ *                 -1 for tokens past the last sequence's (padding).
+ * tok_offsets: int32 [B + 1]; slots: int32 [n_tokens][H_kv], or NULL; lens_out: int32
+ * [B * H_kv], which must not overlap lens. */
+int tgvkv_pages_append(const tgvkv_cache_desc* desc, const tgvkv_page_list* pages,
+                       const int32_t* lens, const int32_t* tok_offsets, int64_t n_tokens,
+                       int32_t* slots, int32_t* lens_out, void* workspace, void* stream);
+
+/* The slots of tgvkv_pages_append for sets that hold their pages already, of a table
+ * from wherever: page_table int32 [B * H_kv][max_pages].  A slot whose page is not in
+ * the pool, or past the table, is -1 (TGVKV_STATUS_INDEX). */
+int tgvkv_page_slots(const tgvkv_cache_desc* desc, const int32_t* page_table, const int32_t* lens,
+                     const int32_t* tok_offsets, int64_t n_tokens, int32_t* slots,
+                     void* workspace, void* stream);
+
+/* ---- rotary positions ----------------------------------------------------
+ *
+ * Rows of d values whose first rot_dim are turned by their token's position: pair i
+ * of rot_dim / 2, (x1, x2), becomes
+ *   (x1 c - x2 s, x2 c + x1 s) a,   c, s = cos, sin(p f_i),
+ * the other values are copied.  Pair i is values (i, i + rot_dim / 2)
+ * (TGVKV_ROPE_HALF) or (2 i, 2 i + 1) (TGVKV_ROPE_INTERLEAVED).  Several position axes
+ * (time, height, width of vision tokens): the first sections[0] pairs follow axis 0,
+ * the next sections[1] axis 1, and so on.
+ *
+ * f_i = base^(-2 i / rot_dim), scaled for contexts longer than those of the training
+ * (desc->scaling):
+ *   TGVKV_ROPE_LINEAR  f_i / factor;
+ *   TGVKV_ROPE_BASE    with base * factor^(rot_dim / (rot_dim - 2)) for base
+ *                      (rot_dim = 2, whose one pair has f = 1 at any base: as it is);
+ *   TGVKV_ROPE_PARTS   by the turns t_i = original * f_i / (2 pi) that a pair makes over the
+ *                      original context: f_i where t_i >= high, f_i / factor where
+ *                      t_i <= low, between them f_i (g + (1 - g) / factor),
+ *                      g = (t_i - low) / (high - low).
+ * attention is the factor a (0 stands for 1).  Pairs with other frequencies:
+ * desc->freqs, radians a position, which then stand in the place of all of this.
+ *
+ * Angles are right for every int32 position: a plan holds f_i / (2 pi), computed in
+ * double, as a 64-bit fraction, so that an integer product leaves p f_i mod 1, to 2^-32
+ * turns and 2^-51 of p f_i.  c, s and the products are fp32, the result is rounded to
+ * bf16 once. */
+#define TGVKV_ROPE_HALF        0
+#define TGVKV_ROPE_INTERLEAVED 1
+
+#define TGVKV_ROPE_NONE   0
+#define TGVKV_ROPE_LINEAR 1
+#define TGVKV_ROPE_BASE   2
+#define TGVKV_ROPE_PARTS  3
+
+#define TGVKV_ROPE_FORWARD  0   /* as above */
+#define TGVKV_ROPE_GRADIENT 1   /* the transposed map: of outputs' gradients, the inputs' */
+#define TGVKV_ROPE_MOVE     2   /* turned rows moved by differences of positions: a = 1 */
+
+#define TGVKV_ROPE_MAX_DIM  256
+#define TGVKV_ROPE_MAX_AXES 4
+
+typedef struct tgvkv_rope_desc {
+    int32_t d;              /* values of a row: a multiple of 8, at most 256 */
+    int32_t rot_dim;        /* how many of them turn: even, 2 .. d */
+    int32_t layout;         /* TGVKV_ROPE_HALF or TGVKV_ROPE_INTERLEAVED */
+    int32_t axes;           /* position axes, 1 .. 4 */
+    int32_t sections[TGVKV_ROPE_MAX_AXES];   /* pairs of every axis, in all rot_dim / 2 (axes = 1: not read) */
+    int32_t scaling;        /* TGVKV_ROPE_NONE ... */
+    int32_t original;       /* PARTS: the original context's positions, > 0 */
+    double  base;           /* > 0 */
+    double  factor;         /* LINEAR, BASE, PARTS: > 0 */
+    double  low, high;      /* PARTS: 0 <= low < high */
+    double  attention;      /* a; 0 stands for 1 */
+    const double* freqs;    /* NULL, or rot_dim / 2 frequencies (host memory, read by
+                               tgvkv_rope_init; each finite, below 2 pi 2^31 in size) */
+} tgvkv_rope_desc;
+
+/* What the calls take: plain host data, written by tgvkv_rope_init and only read
+ * afterwards (by value into each launch; it may be freed as soon as a call returns). */
+typedef struct tgvkv_rope_plan {
+    int32_t d, rot_dim, layout, axes;
+    float   attention;
+    int32_t ready;                                    /* set by tgvkv_rope_init */
+    uint8_t axis[TGVKV_ROPE_MAX_DIM / 2];             /* of every pair */
+    uint64_t turns[TGVKV_ROPE_MAX_DIM / 2];           /* f_i / (2 pi) mod 1, times 2^64 */
+} tgvkv_rope_plan;
+
+int tgvkv_rope_init(tgvkv_rope_plan* plan, const tgvkv_rope_desc* desc);
+
+/* Turns the rows of one or two tensors that share their tokens' positions, queries and
+ * keys: element (t, h, c) at t * tok_stride + h * head_stride + c, bf16, strides in
+ * elements, multiples of 8, each tensor with its own, 16-byte aligned.  An output may
+ * be its own input (the same pointer and strides); other overlaps are not allowed.
+ * k and k_out may be NULL with H_k = 0.  positions: int32, of axis a and token t at
+ * a * pos_stride + t (pos_stride 0: the axes share them).  mode: TGVKV_ROPE_FORWARD, GRADIENT or MOVE.  n_tokens = 0
+ * launches nothing.  No workspace: nothing is reported by the device. */
+int tgvkv_rope(const tgvkv_rope_plan* plan, int32_t mode, const int32_t* positions,
+               int64_t pos_stride, int64_t n_tokens, const uint16_t* q, int64_t q_tok_stride,
+               int64_t q_head_stride, int32_t H_q, uint16_t* q_out, int64_t q_out_tok_stride,
+               int64_t q_out_head_stride, const uint16_t* k, int64_t k_tok_stride,
+               int64_t k_head_stride, int32_t H_k, uint16_t* k_out, int64_t k_out_tok_stride,
+               int64_t k_out_head_stride, void* stream);
+
+/* A serving step's tokens into the paged cache in one pass: queries turned into q_out,
+ * keys turned, rounded to bf16 and stored in the cache's format, values stored, at the
+ * pool rows that slots names (int32 [n_tokens][H_kv], of tgvkv_pages_append).  The same,
+ * bit for bit, as tgvkv_rope (FORWARD) followed by tgvkv_cache_write.
+ * A negative slot has no row: the token's key and value go nowhere (padding).  One past the
+ * pool sets TGVKV_STATUS_INDEX and is skipped.  No row may be named twice.
+ * plan->d is desc->d.  q [n_tokens][H_q], k and v [n_tokens][H_kv] and q_out as in
+ * tgvkv_rope (q and q_out NULL: keys and values only; q_out may be q itself). */
+int tgvkv_rope_write(const tgvkv_cache_desc* desc, const tgvkv_cache_pools* pools,
+                     const tgvkv_rope_plan* plan, const int32_t* positions, int64_t pos_stride,
+                     const int32_t* slots, int64_t n_tokens, const uint16_t* q,
+                     int64_t q_tok_stride, int64_t q_head_stride, const uint16_t* k,
+                     int64_t k_tok_stride, int64_t k_head_stride, const uint16_t* v,
+                     int64_t v_tok_stride, int64_t v_head_stride, uint16_t* q_out,
+                     int64_t q_out_tok_stride, int64_t q_out_head_stride, void* workspace,
+                     void* stream);
 
 /* Zero `workspace` (asynchronously on `stream`).  Needed once after the
  * workspace is allocated: the calls leave their completion counters at zero

@@ -36,15 +36,41 @@ class CachePools(ctypes.Structure):
     _fields_ = [("k", c_void_p), ("v", c_void_p), ("k_scale", c_void_p), ("v_scale", c_void_p)]
 
 
+class PageListPointers(ctypes.Structure):
+    """Mirror of ``tgvkv_page_list`` (include/tgvkv.h)."""
+    _fields_ = [("page_table", c_void_p), ("free_pages", c_void_p), ("n_free", c_void_p)]
+
+
+class RopeDesc(ctypes.Structure):
+    """Mirror of ``tgvkv_rope_desc`` (include/tgvkv.h)."""
+    _fields_ = [("d", c_int32), ("rot_dim", c_int32), ("layout", c_int32), ("axes", c_int32),
+                ("sections", c_int32 * 4), ("scaling", c_int32), ("original", c_int32),
+                ("base", c_double), ("factor", c_double), ("low", c_double), ("high", c_double),
+                ("attention", c_double), ("freqs", ctypes.POINTER(c_double))]
+
+
+class RopePlan(ctypes.Structure):
+    """Mirror of ``tgvkv_rope_plan`` (include/tgvkv.h)."""
+    _fields_ = [("d", c_int32), ("rot_dim", c_int32), ("layout", c_int32), ("axes", c_int32),
+                ("attention", c_float), ("ready", c_int32), ("axis", ctypes.c_uint8 * 128),
+                ("turns", ctypes.c_uint64 * 128)]
+
+
 CACHE_BF16, CACHE_INT8, CACHE_INT4, CACHE_FP4 = 0, 1, 2, 4
 BASIS_VISION, BASIS_ALL = 0, 1
 WEIGHTS_GIVEN, WEIGHTS_EQ7 = 0, 1
 STAT_TV, STAT_TT, STAT_UNIFORM = 0, 1, 2
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_NONE, ROPE_LINEAR, ROPE_BASE, ROPE_PARTS = 0, 1, 2, 3
+ROPE_FORWARD, ROPE_GRADIENT, ROPE_MOVE = 0, 1, 2
 
 
 _P = ctypes.POINTER(Desc)
 _C = ctypes.POINTER(CacheDesc)
 _POOLS = ctypes.POINTER(CachePools)
+_PAGES = ctypes.POINTER(PageListPointers)
+_PLAN = ctypes.POINTER(RopePlan)
+_T = [c_void_p, c_int64, c_int64]      # a tensor of rows: pointer, token and head strides
 
 # name -> (restype, argtypes); the exported C ABI, one entry per declaration
 SIGNATURES = {
@@ -98,6 +124,18 @@ SIGNATURES = {
                                  c_int64, c_void_p, c_void_p]),
     "tgvkv_chunk_attention": (c_int, [_C, _POOLS, c_void_p, c_void_p, c_void_p, c_int64, c_int64,
                                       c_int64, c_void_p, c_int32, c_void_p, c_void_p, c_void_p]),
+    "tgvkv_pages_init": (c_int, [_C, _PAGES, c_void_p]),
+    "tgvkv_pages_grow": (c_int, [_C, _PAGES, c_void_p, c_void_p, c_void_p, c_void_p]),
+    "tgvkv_pages_shrink": (c_int, [_C, _PAGES, c_void_p, c_void_p, c_void_p, c_void_p]),
+    "tgvkv_pages_append": (c_int, [_C, _PAGES, c_void_p, c_void_p, c_int64, c_void_p, c_void_p,
+                                   c_void_p, c_void_p]),
+    "tgvkv_page_slots": (c_int, [_C, c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_void_p,
+                                 c_void_p]),
+    "tgvkv_rope_init": (c_int, [_PLAN, ctypes.POINTER(RopeDesc)]),
+    "tgvkv_rope": (c_int, [_PLAN, c_int32, c_void_p, c_int64, c_int64, *_T, c_int32, *_T, *_T,
+                           c_int32, *_T, c_void_p]),
+    "tgvkv_rope_write": (c_int, [_C, _POOLS, _PLAN, c_void_p, c_int64, c_void_p, c_int64, *_T, *_T,
+                                 *_T, *_T, c_void_p, c_void_p]),
 }
 
 _lib = None

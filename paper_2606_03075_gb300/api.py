@@ -587,5 +587,213 @@ def tgvkv_chunk_attention(desc, cache: PagedCache, page_table, lens, q, tok_offs
         _stream(stream)), "tgvkv_chunk_attention")
 
 
+# ---- pages of the cache, handed out on the GPU ---------------------------------
+
+@dataclass
+class PageList:
+    page_table: torch.Tensor   # int32 [B * H_kv, max_pages]; -1: no page
+    free: torch.Tensor         # int32 [n_pages]: a stack, of which n_free are left
+    n_free: torch.Tensor       # int32 [1]
+
+
+def alloc_pages(desc: CacheDesc, device=None) -> PageList:
+    """A descriptor's page list: an empty table, every page of the pool free."""
+    _geometry(desc, "alloc_pages")
+    new = dict(dtype=torch.int32, device=device or "cuda")
+    pages = PageList(torch.empty((desc.B * desc.H_kv, desc.max_pages), **new),
+                     torch.empty(desc.n_pages, **new), torch.empty(1, **new))
+    if pages.free.is_cuda:
+        tgvkv_pages_init(desc, pages)
+    return pages
+
+
+def _page_list(desc, pages: PageList, geo):
+    return ctypes.byref(_lib.PageListPointers(
+        _table(desc, pages.page_table, geo), _dev(pages.free, torch.int32, desc.n_pages, "pages.free"),
+        _dev(pages.n_free, torch.int32, 1, "pages.n_free")))
+
+
+def tgvkv_pages_init(desc, pages: PageList, stream=None):
+    """An empty table and every page free (see include/tgvkv.h)."""
+    geo = _geometry(desc, "tgvkv_pages_init")
+    _check(_lib.load().tgvkv_pages_init(ctypes.byref(desc), _page_list(desc, pages, geo),
+                                        _stream(stream)), "tgvkv_pages_init")
+
+
+def _resize(fn, desc, pages, lens, lens_new, ws, stream):
+    geo = _geometry(desc, fn)
+    sets = geo[1]
+    _check(getattr(_lib.load(), fn)(
+        ctypes.byref(desc), _page_list(desc, pages, geo), _dev(lens, torch.int32, sets, "lens"),
+        _dev(lens_new, torch.int32, sets, "lens_new"), _dev(ws, torch.uint8, geo[0], "workspace"),
+        _stream(stream)), fn)
+
+
+def tgvkv_pages_grow(desc, pages: PageList, lens, lens_new, ws, stream=None):
+    """Pages for sets that go from lens to lens_new slots (those that get longer)."""
+    _resize("tgvkv_pages_grow", desc, pages, lens, lens_new, ws, stream)
+
+
+def tgvkv_pages_shrink(desc, pages: PageList, lens, lens_new, ws, stream=None):
+    """Pages back from sets that go from lens to lens_new slots (those that get shorter)."""
+    _resize("tgvkv_pages_shrink", desc, pages, lens, lens_new, ws, stream)
+
+
+def _slot_map(desc, slots):
+    """Pointer and tokens of a slot map, int32 [T, H_kv]."""
+    if not isinstance(slots, torch.Tensor):
+        raise TypeError("slots must be a torch.Tensor")
+    if slots.dim() != 2 or slots.shape[1] != desc.H_kv:
+        raise ValueError(f"slots has shape {tuple(slots.shape)}, expected (tokens, {desc.H_kv})")
+    return _dev(slots, torch.int32, 0, "slots"), slots.shape[0]
+
+
+def tgvkv_pages_append(desc, pages: PageList, lens, tok_offsets, slots, lens_out, ws, n_tokens=None,
+                       stream=None):
+    """Room for new tokens: pages taken, slots int32 [T, H_kv] (the pool row of every token
+    and KV head) and the new lengths written.  slots None: no map, n_tokens says how many
+    tokens tok_offsets may count (see include/tgvkv.h)."""
+    geo = _geometry(desc, "tgvkv_pages_append")
+    sets = geo[1]
+    if slots is None:
+        if n_tokens is None:
+            raise TypeError("n_tokens is needed where slots is None")
+        sp, n = None, int(n_tokens)
+    else:
+        sp, n = _slot_map(desc, slots)
+        if n_tokens is not None and n_tokens != n:
+            raise ValueError(f"slots has {n} tokens, n_tokens is {n_tokens}")
+        sp = sp or None
+    _check(_lib.load().tgvkv_pages_append(
+        ctypes.byref(desc), _page_list(desc, pages, geo), _dev(lens, torch.int32, sets, "lens"),
+        _dev(tok_offsets, torch.int32, desc.B + 1, "tok_offsets"), n, sp,
+        _dev(lens_out, torch.int32, sets, "lens_out"), _dev(ws, torch.uint8, geo[0], "workspace"),
+        _stream(stream)), "tgvkv_pages_append")
+
+
+def tgvkv_page_slots(desc, page_table, lens, tok_offsets, slots, ws, stream=None):
+    """The slots of new tokens whose sets hold their pages already."""
+    geo = _geometry(desc, "tgvkv_page_slots")
+    sp, n = _slot_map(desc, slots)
+    _check(_lib.load().tgvkv_page_slots(
+        ctypes.byref(desc), _table(desc, page_table, geo), _dev(lens, torch.int32, geo[1], "lens"),
+        _dev(tok_offsets, torch.int32, desc.B + 1, "tok_offsets"), n, sp,
+        _dev(ws, torch.uint8, geo[0], "workspace"), _stream(stream)), "tgvkv_page_slots")
+
+
+# ---- rotary positions ----------------------------------------------------------
+
+RopePlan = _lib.RopePlan
+ROPE_LAYOUT = {"half": _lib.ROPE_HALF, "interleaved": _lib.ROPE_INTERLEAVED}
+ROPE_SCALING = {"none": _lib.ROPE_NONE, "linear": _lib.ROPE_LINEAR, "base": _lib.ROPE_BASE,
+                "parts": _lib.ROPE_PARTS}
+ROPE_MODE = {"forward": _lib.ROPE_FORWARD, "gradient": _lib.ROPE_GRADIENT, "move": _lib.ROPE_MOVE}
+
+
+def make_rope(d, rot_dim=None, base=10000.0, layout="half", sections=None, scaling="none",
+              factor=1.0, original=0, low=1.0, high=32.0, attention=1.0, freqs=None) -> RopePlan:
+    """A rotary plan (include/tgvkv.h): host data, made once for a model.
+
+    d: values of a row; rot_dim: how many turn (default: all); layout: "half" or
+    "interleaved"; sections: pairs of every position axis (default: one axis); scaling:
+    "none", "linear" (factor), "base" (factor) or "parts" (factor, original, low, high);
+    attention: the factor of turned values; freqs: rot_dim / 2 frequencies, radians a
+    position, in the place of base and scaling."""
+    rot_dim = d if rot_dim is None else rot_dim
+    sections = [rot_dim // 2] if sections is None else [int(n) for n in sections]
+    if not 1 <= len(sections) <= 4:
+        raise ValueError(f"{len(sections)} position axes, expected 1 to 4")
+    if len(sections) == 1 and sections[0] != rot_dim // 2:
+        raise ValueError(f"sections {sections} are not the {rot_dim // 2} pairs")
+    if attention == 0:
+        raise ValueError("attention is 0")
+    values = None
+    if freqs is not None:
+        values = [float(f) for f in freqs]
+        if len(values) != rot_dim // 2:
+            raise ValueError(f"{len(values)} frequencies, expected {rot_dim // 2}")
+        values = (ctypes.c_double * max(len(values), 1))(*values)
+    desc = _lib.RopeDesc(d=d, rot_dim=rot_dim, layout=ROPE_LAYOUT[layout], axes=len(sections),
+                         sections=(ctypes.c_int32 * 4)(*sections), scaling=ROPE_SCALING[scaling],
+                         original=original, base=base, factor=factor, low=low, high=high,
+                         attention=attention, freqs=values)
+    plan = RopePlan()
+    _check(_lib.load().tgvkv_rope_init(ctypes.byref(plan), ctypes.byref(desc)), "tgvkv_rope_init")
+    return plan
+
+
+def _positions(plan, t, n):
+    """Pointer and axis stride of positions, int32 [n] (one axis) or [axes, n]."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("positions must be a torch.Tensor")
+    if not t.is_cuda:
+        raise ValueError("positions must be a CUDA tensor")
+    if t.dtype is not torch.int32:
+        raise TypeError(f"positions has dtype {t.dtype}, expected torch.int32")
+    if not (t.shape == (plan.axes, n) or (plan.axes == 1 and t.shape == (n,))):
+        raise ValueError(f"positions has shape {tuple(t.shape)}, expected ({plan.axes}, {n})")
+    if n > 1 and t.stride(-1) != 1:
+        raise ValueError("positions' last dimension must be contiguous")
+    return t.data_ptr(), t.stride(0) if plan.axes > 1 else n
+
+
+def _rows(t, d, name):
+    """Pointer, (token, head) strides, heads and tokens of a tensor [T, heads, d]."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dim() != 3:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected (tokens, heads, {d})")
+    heads = t.shape[1]
+    p, tok, head, n = _tokens(t, heads, d, name)
+    return p, tok, head, heads, n
+
+
+def tgvkv_rope(plan, positions, q, q_out, k=None, k_out=None, mode="forward", stream=None):
+    """q_out (and k_out) receive the rows of q (and k), bf16 [T, heads, d] with any token
+    and head strides, turned by their tokens' positions, int32 [T] or [axes, T]; an output
+    may be its input.  mode: "forward", "gradient" (q, k: the gradients of turned rows) or
+    "move" (positions: differences) (see include/tgvkv.h)."""
+    qp, qt, qh, H_q, n = _rows(q, plan.d, "q")
+    op, ot, oh, H_o, n_o = _rows(q_out, plan.d, "q_out")
+    if (H_o, n_o) != (H_q, n):
+        raise ValueError(f"q_out has shape {tuple(q_out.shape)}, q {tuple(q.shape)}")
+    if (k is None) != (k_out is None):
+        raise TypeError("k and k_out go together")
+    ks = (None, 0, 0, 0, None, 0, 0)
+    if k is not None:
+        kp, kt, kh, H_k, n_k = _rows(k, plan.d, "k")
+        lp, lt, lh, H_l, n_l = _rows(k_out, plan.d, "k_out")
+        if n_k != n or (H_l, n_l) != (H_k, n_k):
+            raise ValueError(f"k has shape {tuple(k.shape)}, k_out {tuple(k_out.shape)}, q {tuple(q.shape)}")
+        ks = (kp, kt, kh, H_k, lp, lt, lh) if H_k else ks
+    pp, ps = _positions(plan, positions, n)
+    _check(_lib.load().tgvkv_rope(ctypes.byref(plan), ROPE_MODE[mode], pp, ps, n, qp, qt, qh, H_q, op,
+                                  ot, oh, *ks, _stream(stream)), "tgvkv_rope")
+
+
+def tgvkv_rope_write(desc, cache: PagedCache, plan, positions, slots, q, k_new, v_new, q_out, ws,
+                     stream=None):
+    """A serving step's tokens in one pass: q bf16 [T, H_q, d] turned into q_out, k_new turned
+    and v_new stored in the cache's format at the pool rows of slots, int32 [T, H_kv] (any
+    token and head strides; q and q_out None: keys and values only) (see include/tgvkv.h)."""
+    geo = _geometry(desc, "tgvkv_rope_write")
+    heads, d = desc.H_kv, desc.d
+    kp, kt, kh, n = _tokens(k_new, heads, d, "k_new")
+    vp, vt, vh, nv = _tokens(v_new, heads, d, "v_new")
+    sp, ns = _slot_map(desc, slots)
+    if (q is None) != (q_out is None):
+        raise TypeError("q and q_out go together")
+    qs = os = (None, 0, 0, n)
+    if q is not None:
+        qs, os = _tokens(q, desc.H_q, d, "q"), _tokens(q_out, desc.H_q, d, "q_out")
+    if not n == nv == ns == qs[3] == os[3]:
+        raise ValueError(f"tokens: k_new {n}, v_new {nv}, slots {ns}, q {qs[3]}, q_out {os[3]}")
+    pp, ps = _positions(plan, positions, n)
+    _check(_lib.load().tgvkv_rope_write(
+        ctypes.byref(desc), _pools(desc, cache, geo), ctypes.byref(plan), pp, ps, sp, n, *qs[:3],
+        kp, kt, kh, vp, vt, vh, *os[:3], _dev(ws, torch.uint8, geo[0], "workspace"),
+        _stream(stream)), "tgvkv_rope_write")
+
+
 def default_scale(d: int) -> float:
     return 1.0 / math.sqrt(d)

@@ -21,7 +21,7 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libtgvkv.so")
 
 SOURCES = ["api.cu", "score_tc.cu", "budget.cu", "select.cu", "compact.cu", "text.cu", "decode.cu",
-           "prefill.cu", "selftest.cu", "cache_rows.cu", "chunk_stream.cu",
+           "prefill.cu", "selftest.cu", "cache_rows.cu", "pages.cu", "rope.cu", "chunk_stream.cu",
            "chunk_tile_bf16.cu", "chunk_tile_int8.cu", "chunk_tile_int4.cu", "chunk_tile_fp4.cu",
            "chunk_merge.cu", "chunk_maps.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]

@@ -371,11 +371,11 @@ int make_cache_problem(const tgvkv_cache_desc* d, CacheProblem* p) {
 }
 
 // Workspace of the paged-cache calls: the status word, the attention's tickets
-// and flags, its plan
+// and flags, the page list's ticket, the attention's plan
 // (the first unit of work of every set; the items split over CTAs) and the
 // partial results of split sets.
 struct CacheLayout {
-    size_t sync, plan, split, part, total;
+    size_t sync, pages, plan, split, part, total;
 };
 
 CacheLayout cache_layout(const CacheProblem& p) {
@@ -383,6 +383,8 @@ CacheLayout cache_layout(const CacheProblem& p) {
     size_t o = round_up(sizeof(uint32_t));
     w.sync = o;                        // tickets and flags: zero between calls
     o += round_up(sizeof(uint32_t) * kTileSync);
+    w.pages = o;                       // likewise
+    o += round_up(sizeof(uint32_t));
     w.plan = o;
     o += round_up(sizeof(long long) * ((size_t)p.S + 1));
     w.split = o;
@@ -459,6 +461,83 @@ int check_write(const CacheProblem& p, const int32_t* page_table, const int32_t*
     if (a < b + bytes && b < a + bytes)
         return fail(TGVKV_ERR_INVALID_ARG, "lens and lens_out overlap");
     REQUIRE_PTR(workspace, "workspace", true);
+    return TGVKV_OK;
+}
+
+// ---- pages and rotary positions ------------------------------------------------
+
+int check_pages(const tgvkv_page_list* pages, PagesArgs* a) {
+    if (!pages) return fail(TGVKV_ERR_INVALID_ARG, "pages is NULL");
+    int rc;
+    if ((rc = check_ints(pages->page_table, "page_table")) ||
+        (rc = check_ints(pages->free_pages, "free_pages")) || (rc = check_ints(pages->n_free, "n_free")))
+        return rc;
+    a->table = pages->page_table;
+    a->free_pages = pages->free_pages;
+    a->n_free = pages->n_free;
+    return TGVKV_OK;
+}
+
+// New tokens of H_kv heads, as slots counts them.
+int check_token_count(const CacheProblem& p, int64_t n_tokens) {
+    if (n_tokens < 0) return fail(TGVKV_ERR_INVALID_ARG, "n_tokens=%lld < 0", (long long)n_tokens);
+    if (n_tokens >= (1LL << 31) || n_tokens * p.H_kv >= (1LL << 31))
+        return fail(TGVKV_ERR_UNSUPPORTED, "%lld tokens of %d heads", (long long)n_tokens, p.H_kv);
+    return TGVKV_OK;
+}
+
+int do_pages(int mode, const tgvkv_cache_desc* desc, const tgvkv_page_list* pages,
+             const int32_t* lens, const int32_t* lens_new, void* workspace, void* stream) {
+    CacheProblem p{};
+    PagesArgs a{};
+    int rc = make_cache_problem(desc, &p);
+    if (rc || (rc = check_pages(pages, &a)) || (rc = check_ints(lens, "lens")) ||
+        (rc = check_ints(lens_new, "lens_new")))
+        return rc;
+    REQUIRE_PTR(workspace, "workspace", true);
+    a.lens = lens;
+    a.lens_new = lens_new;
+    uint32_t* ticket = reinterpret_cast<uint32_t*>(static_cast<char*>(workspace) + cache_layout(p).pages);
+    cudaError_t e = launch_pages(p, mode, a, ticket, static_cast<uint32_t*>(workspace),
+                                 static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? ok() : cuda_fail(e, "pages launch");
+}
+
+int check_plan(const tgvkv_rope_plan* plan) {
+    if (!plan) return fail(TGVKV_ERR_INVALID_ARG, "plan is NULL");
+    if (plan->ready != kPlanReady)
+        return fail(TGVKV_ERR_INVALID_ARG, "plan was not made by tgvkv_rope_init");
+    return TGVKV_OK;
+}
+
+int check_positions(const tgvkv_rope_plan* plan, const int32_t* positions, int64_t pos_stride,
+                    int64_t n_tokens) {
+    if (n_tokens < 0) return fail(TGVKV_ERR_INVALID_ARG, "n_tokens=%lld < 0", (long long)n_tokens);
+    if (n_tokens >= (1LL << 31)) return fail(TGVKV_ERR_UNSUPPORTED, "2^31 tokens or more");
+    if (n_tokens == 0) return TGVKV_OK;
+    int rc = check_ints(positions, "positions");
+    if (rc) return rc;
+    if (plan->axes > 1 && (pos_stride < 0 || pos_stride >= (1LL << 38)))
+        return fail(TGVKV_ERR_INVALID_ARG, "pos_stride=%lld (0 .. 2^38)", (long long)pos_stride);
+    return TGVKV_OK;
+}
+
+// A tensor of a rotary call, its strides as check_tokens has them.
+int check_rows_of(int d, const char* name, const uint16_t* ptr, int64_t tok_stride,
+                  int64_t head_stride, int64_t n_tokens, int heads) {
+    CacheProblem p{};
+    p.d = d;
+    return check_tokens(p, name, ptr, tok_stride, head_stride, n_tokens, heads);
+}
+
+int check_turned(int d, const char* name, const char* out_name, const RopeTensor& x, int64_t n_tokens) {
+    int rc;
+    if ((rc = check_rows_of(d, name, x.x, x.x_tok, x.x_head, n_tokens, x.heads)) ||
+        (rc = check_rows_of(d, out_name, x.y, x.y_tok, x.y_head, n_tokens, x.heads)))
+        return rc;
+    if (n_tokens > 0 && x.x == x.y &&
+        ((n_tokens > 1 && x.x_tok != x.y_tok) || (x.heads > 1 && x.x_head != x.y_head)))
+        return fail(TGVKV_ERR_INVALID_ARG, "%s is %s with other strides", out_name, name);
     return TGVKV_OK;
 }
 
@@ -827,6 +906,196 @@ int tgvkv_cache_read(const tgvkv_cache_desc* desc, const tgvkv_cache_pools* pool
                                       (long long)n_rows, static_cast<uint32_t*>(workspace),
                                       static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? ok() : cuda_fail(e, "cache read launch");
+}
+
+int tgvkv_pages_init(const tgvkv_cache_desc* desc, const tgvkv_page_list* pages, void* stream) {
+    CacheProblem p{};
+    PagesArgs a{};
+    int rc = make_cache_problem(desc, &p);
+    if (rc || (rc = check_pages(pages, &a))) return rc;
+    cudaError_t e = launch_pages_init(p, a, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? ok() : cuda_fail(e, "pages launch");
+}
+
+int tgvkv_pages_grow(const tgvkv_cache_desc* desc, const tgvkv_page_list* pages,
+                     const int32_t* lens, const int32_t* lens_new, void* workspace, void* stream) {
+    return do_pages(kPagesGrow, desc, pages, lens, lens_new, workspace, stream);
+}
+
+int tgvkv_pages_shrink(const tgvkv_cache_desc* desc, const tgvkv_page_list* pages,
+                       const int32_t* lens, const int32_t* lens_new, void* workspace,
+                       void* stream) {
+    return do_pages(kPagesShrink, desc, pages, lens, lens_new, workspace, stream);
+}
+
+int tgvkv_pages_append(const tgvkv_cache_desc* desc, const tgvkv_page_list* pages,
+                       const int32_t* lens, const int32_t* tok_offsets, int64_t n_tokens,
+                       int32_t* slots, int32_t* lens_out, void* workspace, void* stream) {
+    CacheProblem p{};
+    PagesArgs a{};
+    int rc = make_cache_problem(desc, &p);
+    if (rc || (rc = check_pages(pages, &a)) || (rc = check_token_count(p, n_tokens)) ||
+        (rc = check_write(p, pages->page_table, lens, lens_out, workspace)) ||
+        (rc = check_ints(tok_offsets, "tok_offsets")) || (slots && (rc = check_ints(slots, "slots"))))
+        return rc;
+    a.lens = lens;
+    a.tok_offsets = tok_offsets;
+    a.T = (int)n_tokens;
+    a.slots = slots;
+    a.lens_out = lens_out;
+    uint32_t* ticket = reinterpret_cast<uint32_t*>(static_cast<char*>(workspace) + cache_layout(p).pages);
+    cudaError_t e = launch_pages(p, kPagesAppend, a, ticket, static_cast<uint32_t*>(workspace),
+                                 static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? ok() : cuda_fail(e, "pages launch");
+}
+
+int tgvkv_page_slots(const tgvkv_cache_desc* desc, const int32_t* page_table, const int32_t* lens,
+                     const int32_t* tok_offsets, int64_t n_tokens, int32_t* slots,
+                     void* workspace, void* stream) {
+    CacheProblem p{};
+    PagesArgs a{};
+    int rc = make_cache_problem(desc, &p);
+    if (rc || (rc = check_token_count(p, n_tokens)) || (rc = check_ints(page_table, "page_table")) ||
+        (rc = check_ints(lens, "lens")) || (rc = check_ints(tok_offsets, "tok_offsets")) ||
+        (n_tokens > 0 && (rc = check_ints(slots, "slots"))))
+        return rc;
+    REQUIRE_PTR(workspace, "workspace", true);
+    a.table = const_cast<int32_t*>(page_table);   // only read
+    a.lens = lens;
+    a.tok_offsets = tok_offsets;
+    a.T = (int)n_tokens;
+    a.slots = slots;
+    cudaError_t e = launch_page_slots(p, a, static_cast<uint32_t*>(workspace),
+                                      static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? ok() : cuda_fail(e, "page slots launch");
+}
+
+int tgvkv_rope_init(tgvkv_rope_plan* plan, const tgvkv_rope_desc* d) {
+    if (!plan || !d) return fail(TGVKV_ERR_INVALID_ARG, "%s is NULL", plan ? "desc" : "plan");
+    plan->ready = 0;
+    if (d->d < 8 || d->d % 8 != 0 || d->rot_dim < 2 || d->rot_dim % 2 != 0 || d->rot_dim > d->d)
+        return fail(TGVKV_ERR_INVALID_ARG, "bad sizes: d=%d (a multiple of 8), rot_dim=%d (even, up to d)",
+                    d->d, d->rot_dim);
+    if (d->d > TGVKV_ROPE_MAX_DIM)
+        return fail(TGVKV_ERR_UNSUPPORTED, "d=%d above %d", d->d, TGVKV_ROPE_MAX_DIM);
+    if (d->layout != TGVKV_ROPE_HALF && d->layout != TGVKV_ROPE_INTERLEAVED)
+        return fail(TGVKV_ERR_INVALID_ARG, "layout=%d unknown", d->layout);
+    if (d->axes < 1 || d->axes > TGVKV_ROPE_MAX_AXES)
+        return fail(TGVKV_ERR_INVALID_ARG, "axes=%d (1 .. %d)", d->axes, TGVKV_ROPE_MAX_AXES);
+    const int pairs = d->rot_dim / 2;
+    long long sum = 0;
+    for (int x = 0; x < d->axes; ++x) {
+        if (d->axes > 1 && d->sections[x] < 0) sum = -1;
+        if (d->axes > 1 && sum >= 0) sum += d->sections[x];
+    }
+    if (d->axes > 1 && sum != pairs)
+        return fail(TGVKV_ERR_INVALID_ARG, "the sections are not the %d pairs", pairs);
+    const double a = d->attention == 0.0 ? 1.0 : d->attention;
+    if (!(a > 0.0) || !(a < 1e30)) return fail(TGVKV_ERR_INVALID_ARG, "attention=%g", d->attention);
+    if (!d->freqs) {
+        if (d->scaling < TGVKV_ROPE_NONE || d->scaling > TGVKV_ROPE_PARTS)
+            return fail(TGVKV_ERR_INVALID_ARG, "scaling=%d unknown", d->scaling);
+        if (!(d->base > 0.0) || isinf(d->base)) return fail(TGVKV_ERR_INVALID_ARG, "base=%g", d->base);
+        if (d->scaling != TGVKV_ROPE_NONE && (!(d->factor > 0.0) || isinf(d->factor)))
+            return fail(TGVKV_ERR_INVALID_ARG, "factor=%g", d->factor);
+        if (d->scaling == TGVKV_ROPE_PARTS &&
+            (!(d->low >= 0.0) || !(d->high > d->low) || isinf(d->high) || d->original < 1))
+            return fail(TGVKV_ERR_INVALID_ARG, "low=%g, high=%g, original=%d", d->low, d->high, d->original);
+    }
+    const double two_pi = 6.283185307179586;
+    double base = d->base;
+    if (!d->freqs && d->scaling == TGVKV_ROPE_BASE && d->rot_dim > 2)
+        base *= pow(d->factor, (double)d->rot_dim / (d->rot_dim - 2));
+    int axis = 0, left = d->axes > 1 ? d->sections[0] : pairs;
+    for (int i = 0; i < pairs; ++i) {
+        double f;
+        if (d->freqs) {
+            f = d->freqs[i];
+        } else {
+            f = pow(base, -2.0 * i / d->rot_dim);
+            if (d->scaling == TGVKV_ROPE_LINEAR) f /= d->factor;
+            if (d->scaling == TGVKV_ROPE_PARTS) {
+                const double t = d->original * f / two_pi;
+                const double g = std::min(std::max((t - d->low) / (d->high - d->low), 0.0), 1.0);
+                f = f * g + f / d->factor * (1.0 - g);
+            }
+        }
+        const double turns = f / two_pi;
+        if (!(fabs(turns) < 2147483648.0))
+            return fail(TGVKV_ERR_INVALID_ARG, "frequency %d is %g radians a position", i, f);
+        const double size = fabs(turns);
+        const uint64_t part = (uint64_t)ldexp(size - floor(size), 64);   // exact but for bits below 2^-64
+        plan->turns[i] = turns < 0.0 ? 0u - part : part;
+        while (left == 0) left = d->sections[++axis];
+        plan->axis[i] = (uint8_t)axis;
+        --left;
+    }
+    plan->d = d->d;
+    plan->rot_dim = d->rot_dim;
+    plan->layout = d->layout;
+    plan->axes = d->axes;
+    plan->attention = (float)a;
+    plan->ready = kPlanReady;
+    return ok();
+}
+
+int tgvkv_rope(const tgvkv_rope_plan* plan, int32_t mode, const int32_t* positions,
+               int64_t pos_stride, int64_t n_tokens, const uint16_t* q, int64_t q_tok_stride,
+               int64_t q_head_stride, int32_t H_q, uint16_t* q_out, int64_t q_out_tok_stride,
+               int64_t q_out_head_stride, const uint16_t* k, int64_t k_tok_stride,
+               int64_t k_head_stride, int32_t H_k, uint16_t* k_out, int64_t k_out_tok_stride,
+               int64_t k_out_head_stride, void* stream) {
+    int rc = check_plan(plan);
+    if (rc || (rc = check_positions(plan, positions, pos_stride, n_tokens))) return rc;
+    if (mode < TGVKV_ROPE_FORWARD || mode > TGVKV_ROPE_MOVE)
+        return fail(TGVKV_ERR_INVALID_ARG, "mode=%d unknown", mode);
+    if (H_q < 1 || H_k < 0 || H_q > 65535 || H_k > 65535)
+        return fail(TGVKV_ERR_INVALID_ARG, "H_q=%d (1 .. 65535), H_k=%d (0 .. 65535)", H_q, H_k);
+    const RopeTensor tq{q, q_tok_stride, q_head_stride, q_out, q_out_tok_stride, q_out_head_stride, H_q};
+    const RopeTensor tk{k, k_tok_stride, k_head_stride, k_out, k_out_tok_stride, k_out_head_stride, H_k};
+    if ((rc = check_turned(plan->d, "q", "q_out", tq, n_tokens)) ||
+        (H_k > 0 && (rc = check_turned(plan->d, "k", "k_out", tk, n_tokens))))
+        return rc;
+    if (n_tokens == 0) return ok();
+    cudaError_t e = launch_rope(*plan, mode, positions, (long long)pos_stride, (int)n_tokens, tq, tk,
+                                static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? ok() : cuda_fail(e, "rope launch");
+}
+
+int tgvkv_rope_write(const tgvkv_cache_desc* desc, const tgvkv_cache_pools* pools,
+                     const tgvkv_rope_plan* plan, const int32_t* positions, int64_t pos_stride,
+                     const int32_t* slots, int64_t n_tokens, const uint16_t* q,
+                     int64_t q_tok_stride, int64_t q_head_stride, const uint16_t* k,
+                     int64_t k_tok_stride, int64_t k_head_stride, const uint16_t* v,
+                     int64_t v_tok_stride, int64_t v_head_stride, uint16_t* q_out,
+                     int64_t q_out_tok_stride, int64_t q_out_head_stride, void* workspace,
+                     void* stream) {
+    CacheProblem p{};
+    CachePools pl{};
+    int rc = make_cache_problem(desc, &p);
+    if (rc || (rc = check_pools(p, pools, &pl)) || (rc = check_plan(plan)) ||
+        (rc = check_positions(plan, positions, pos_stride, n_tokens)) ||
+        (rc = check_token_count(p, n_tokens)))
+        return rc;
+    if (plan->d != p.d)
+        return fail(TGVKV_ERR_INVALID_ARG, "the plan is for rows of %d values, the cache has %d", plan->d, p.d);
+    if ((q == nullptr) != (q_out == nullptr) && n_tokens > 0)
+        return fail(TGVKV_ERR_INVALID_ARG, "q and q_out go together");
+    const int heads = q ? p.H_q : 0;
+    const RopeTensor tq{q, q_tok_stride, q_head_stride, q_out, q_out_tok_stride, q_out_head_stride, heads};
+    if ((heads > 0 && (rc = check_turned(p.d, "q", "q_out", tq, n_tokens))) ||
+        (rc = check_rows_of(p.d, "k", k, k_tok_stride, k_head_stride, n_tokens, p.H_kv)) ||
+        (rc = check_rows_of(p.d, "v", v, v_tok_stride, v_head_stride, n_tokens, p.H_kv)) ||
+        (n_tokens > 0 && (rc = check_ints(slots, "slots"))))
+        return rc;
+    REQUIRE_PTR(workspace, "workspace", true);
+    if (n_tokens == 0) return ok();
+    const long long strides[4] = {(long long)k_tok_stride, (long long)k_head_stride,
+                                  (long long)v_tok_stride, (long long)v_head_stride};
+    cudaError_t e = launch_rope_write(p, pl, *plan, positions, (long long)pos_stride, slots, (int)n_tokens,
+                                      tq, k, v, strides, static_cast<uint32_t*>(workspace),
+                                      static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? ok() : cuda_fail(e, "rope write launch");
 }
 
 int tgvkv_chunk_attention(const tgvkv_cache_desc* desc, const tgvkv_cache_pools* pools,

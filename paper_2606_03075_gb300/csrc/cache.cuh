@@ -61,6 +61,59 @@ struct CachePools {
 
 __device__ __forceinline__ int clamp_len(int len, int cap) { return min(max(len, 0), cap); }
 
+// The largest i in [lo, hi] with off[i] <= x, given off[lo] <= x.
+template <typename T>
+__device__ __forceinline__ int find_last(const T* off, int lo, int hi, long long x) {
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if ((long long)off[mid] <= x) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+
+// The same by a whole warp, 32 probes at a time: two loads in a row for 1024
+// entries where a binary search has ten.
+template <typename T>
+__device__ __forceinline__ int find_last_warp(const T* off, int hi, long long x, int lane) {
+    int lo = 0;
+    while (lo < hi) {
+        const int step = (hi - lo + 32) / 32;    // candidates lo, lo + step, ..: the span is hi - lo + 1
+        const int at = lo + lane * step;
+        const bool le = at <= hi && (long long)off[at] <= x;
+        const uint32_t m = __ballot_sync(~0u, le);
+        lo += max(__popc(m) - 1, 0) * step;      // offsets ascend: the lanes that hold come first
+        hi = min(hi, lo + step - 1);
+    }
+    return lo;
+}
+
+// The first and last set (or sequence) of a CTA's rows, by two of its warps.
+template <typename T>
+__device__ __forceinline__ void find_span(const T* off, int last, long long x0, long long x1,
+                                          int (&span)[2]) {
+    const int warp = threadIdx.x >> 5;
+    if (warp < 2) {
+        const int i = find_last_warp(off, last, warp ? x1 : x0, threadIdx.x & 31);
+        if ((threadIdx.x & 31) == 0) span[warp] = i;
+    }
+}
+
+// Pool row of (set, slot), or -1 (with the status bit) when there is none.
+__device__ __forceinline__ int pool_row(const CacheProblem& p, const int32_t* page_table,
+                                              int s, long long slot, uint32_t* status) {
+    if (slot < 0 || slot >= p.cap) {
+        raise_status(status, TGVKV_STATUS_INDEX);
+        return -1;
+    }
+    const int page = page_table[(size_t)s * p.max_pages + (int)(slot >> p.page_shift)];
+    if (page < 0 || page >= p.n_pages) {
+        raise_status(status, TGVKV_STATUS_INDEX);
+        return -1;
+    }
+    return page * p.page + ((int)slot & (p.page - 1));
+}
+
 // ---- integer codes to bf16 ---------------------------------------------------
 // With 0x4300 = 128.0 and its mantissa step 1, a code's low bits or-ed into
 // the mantissa give 128 + bits exactly, and a subtraction takes the offset off

@@ -2,8 +2,11 @@
 // on `stream` and assume the arguments were validated by the C-ABI layer.
 #pragma once
 
+#include <algorithm>
+
 #include "cache.cuh"
 #include "chunk.cuh"
+#include "rope.cuh"
 
 namespace tgvkv {
 
@@ -20,6 +23,33 @@ cudaError_t launch_cache_read(const CacheProblem& p, const CachePools& pool,
                               const int32_t* page_table, const int32_t* first,
                               const int64_t* offsets, uint16_t* k_out, uint16_t* v_out,
                               long long rows, uint32_t* status, cudaStream_t stream);
+
+// pages.cu: a page list's takings and givings back (mode), with the slots of new tokens
+// (kPagesAppend), and the slots alone.  ticket: zero at the start and left zero.
+enum { kPagesGrow, kPagesShrink, kPagesAppend };
+struct PagesArgs {
+    int32_t *table, *free_pages, *n_free;
+    const int32_t *lens, *lens_new, *tok_offsets;
+    int T;
+    int32_t *slots, *lens_out;
+    int granule;                       // set by the launcher
+};
+cudaError_t launch_pages(const CacheProblem& p, int mode, const PagesArgs& a, uint32_t* ticket,
+                         uint32_t* status, cudaStream_t stream);
+cudaError_t launch_page_slots(const CacheProblem& p, const PagesArgs& a, uint32_t* status,
+                              cudaStream_t stream);
+cudaError_t launch_pages_init(const CacheProblem& p, const PagesArgs& a, cudaStream_t stream);
+
+// rope.cu: rows turned by their positions, and turned into the paged cache (strides: k
+// token, k head, v token, v head).
+cudaError_t launch_rope(const tgvkv_rope_plan& plan, int mode, const int32_t* positions,
+                        long long pos_stride, int T, const RopeTensor& q, const RopeTensor& k,
+                        cudaStream_t stream);
+cudaError_t launch_rope_write(const CacheProblem& p, const CachePools& pool,
+                              const tgvkv_rope_plan& plan, const int32_t* positions,
+                              long long pos_stride, const int32_t* slots, int T, const RopeTensor& q,
+                              const uint16_t* k, const uint16_t* v, const long long (&strides)[4],
+                              uint32_t* status, cudaStream_t stream);
 
 // Attention of a chunk of new tokens: the row-stream kernel, for sets of at most
 // stream_rows() query rows (max_q * G; chunk_stream.cu), and the tile kernel for

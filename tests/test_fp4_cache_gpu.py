@@ -3,9 +3,8 @@ through the C ABI, against the fp64 reference of _fp4_ref.py.
 
 Stored codes, scale bytes and rows read back are exact.  The attention's tolerance is that
 of the other formats, whose arithmetic it shares (products of bf16 operands, which the
-stored values are exactly): weights rounded to bf16 and an output rounded to bf16, 2^-9
-relative each, are off by at most 2^-8 sum_j A_ij |v_j|; twice that is tested, plus the
-fp32 accumulation's room."""
+stored values are exactly): weights rounded to bf16 and an output rounded to bf16, 2^-8
+relative each, are off by at most 2^-7 sum_j A_ij |v_j|, plus 1e-6 for the fp32 sums."""
 import numpy as np
 import pytest
 import torch
@@ -131,10 +130,10 @@ def test_every_code_of_every_scale_through_the_attention(api, d, n):
     assert np.array_equal(box.v[3], v[3 * n:4 * n])
     q, got = box.attend([n] * B)
     assert np.array_equal(got[::n, 0], v[::n])
-    # later tokens see several equal rows: a convex combination of equal values, weights
-    # rounded to bf16 (2^-9 of the sum at most) and the output too
+    # later tokens see several equal rows: a convex combination of equal values, whose
+    # weights are rounded to bf16 (their sum is off by 2^-8 at most), and the output too
     for b in range(B):
-        assert (np.abs(got[b * n:(b + 1) * n, 0] - v[b * n]) <= 2.0 ** -8 * np.abs(v[b * n])).all(), e[b]
+        assert (np.abs(got[b * n:(b + 1) * n, 0] - v[b * n]) <= 2.0 ** -7 * np.abs(v[b * n])).all(), e[b]
 
 
 @pytest.mark.parametrize("n", [1, 40])
