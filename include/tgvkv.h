@@ -582,7 +582,7 @@ int tgvkv_page_slots(const tgvkv_cache_desc* desc, const int32_t* page_table, co
  * desc->freqs, radians a position, which then stand in the place of all of this.
  *
  * Angles are right for every int32 position: a plan holds f_i / (2 pi), computed in
- * double, as a 64-bit fraction, so that an integer product leaves p f_i mod 1, to 2^-32
+ * double, as a 64-bit fraction, so that an integer product leaves p f_i mod 1, to 2^-31
  * turns and 2^-51 of p f_i.  c, s and the products are fp32, the result is rounded to
  * bf16 once. */
 #define TGVKV_ROPE_HALF        0
@@ -620,7 +620,7 @@ typedef struct tgvkv_rope_desc {
  * afterwards (by value into each launch; it may be freed as soon as a call returns). */
 typedef struct tgvkv_rope_plan {
     int32_t d, rot_dim, layout, axes;
-    float   attention;
+    double  attention;
     int32_t ready;                                    /* set by tgvkv_rope_init */
     uint8_t axis[TGVKV_ROPE_MAX_DIM / 2];             /* of every pair */
     uint64_t turns[TGVKV_ROPE_MAX_DIM / 2];           /* f_i / (2 pi) mod 1, times 2^64 */

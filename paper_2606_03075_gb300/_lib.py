@@ -52,7 +52,7 @@ class RopeDesc(ctypes.Structure):
 class RopePlan(ctypes.Structure):
     """Mirror of ``tgvkv_rope_plan`` (include/tgvkv.h)."""
     _fields_ = [("d", c_int32), ("rot_dim", c_int32), ("layout", c_int32), ("axes", c_int32),
-                ("attention", c_float), ("ready", c_int32), ("axis", ctypes.c_uint8 * 128),
+                ("attention", c_double), ("ready", c_int32), ("axis", ctypes.c_uint8 * 128),
                 ("turns", ctypes.c_uint64 * 128)]
 
 

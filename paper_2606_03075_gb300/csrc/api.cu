@@ -1034,7 +1034,7 @@ int tgvkv_rope_init(tgvkv_rope_plan* plan, const tgvkv_rope_desc* d) {
     plan->rot_dim = d->rot_dim;
     plan->layout = d->layout;
     plan->axes = d->axes;
-    plan->attention = (float)a;
+    plan->attention = a;
     plan->ready = kPlanReady;
     return ok();
 }

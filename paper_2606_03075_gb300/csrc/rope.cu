@@ -1,12 +1,16 @@
-// Rotary positions: rows turned by their tokens' positions (rope_kernel), and a serving
-// step's queries, keys and values in one pass, the keys turned and stored in the paged
-// cache's format (rope_write_kernel).
+// Rotary positions: rows turned by their tokens' positions (rope_kernel, and rope_one_kernel
+// for tensors of one row a token), and a serving step's queries, keys and values in one pass,
+// the keys turned and stored in the paged cache's format (rope_write_kernel).
 //
 //   (y1, y2) = a (x1 c - x2 s, x2 c + x1 s),   c, s = cos, sin(p f_i)
 //
-// Both move each row once and are bound by HBM for long prompts, by the launch for a few
-// tokens.  The rows of a token share their angles: a thread computes those of its pairs
-// once and goes through heads, as many as leave the GPU filled.
+// All move each row once and are bound by HBM for long prompts, by the launch for a few
+// tokens.  An angle's c and s take about 30 instructions, a pair itself 4, so the rows of a
+// token share them: a CTA goes through tiles of a tensor's tokens, starts a tile's first
+// loads, computes its angles into shared memory meanwhile, and turns the rows, kRopeRows in
+// flight a thread.  What a row needs beside its arithmetic counts, too (of some 60
+// instructions a 16-byte vector): a thread keeps to one tensor and to one row of its
+// tokens, so that addresses go on by constants.
 #include "cache_launch.h"
 #include "launch.h"
 #include "rope.cuh"
@@ -15,6 +19,10 @@ namespace tgvkv {
 namespace {
 
 constexpr int kRopeThreads = 256;
+constexpr int kRopeRows = 3;                  // rows a thread has in flight
+constexpr int kRopeResident = 4;              // CTAs of an SM
+constexpr int kOneResident = 3;               // likewise, of rope_one_kernel
+constexpr int kTableAngles = 2048;            // of a tile (32 KB for two tables)
 
 // W values of bf16 as they are loaded and stored.
 template <int W>
@@ -27,264 +35,567 @@ template <> struct Words<1> { using type = uint16_t; };
 template <int W>
 union Values {
     typename Words<W>::type w;
+    uint32_t two[W > 1 ? W / 2 : 1];
     uint16_t h[W];
 };
 
-__device__ __forceinline__ float bf16_value(uint16_t h) { return __uint_as_float((uint32_t)h << 16); }
-__device__ __forceinline__ uint16_t bf16_round(float x) {
-    return __bfloat16_as_ushort(__float2bfloat16_rn(x));
-}
+__device__ __forceinline__ float low_value(uint32_t two) { return __uint_as_float(two << 16); }
+__device__ __forceinline__ float high_value(uint32_t two) { return __uint_as_float(two & 0xFFFF0000u); }
+// y1 and y2 of a pair
+__device__ __forceinline__ float first_of(float x1, float x2, float c, float s) { return fmaf(x1, c, -(x2 * s)); }
+__device__ __forceinline__ float second_of(float x1, float x2, float c, float s) { return fmaf(x2, c, x1 * s); }
 
-// A row's units: of W pairs (values i and i + half of a turned part in halves), of W
-// values (W / 2 neighbouring pairs), and of W values that are copied.
-struct RopeShape {
-    int units;               // of a row
-    int turned;              // units that turn, the first ones
-    int chunks;              // slots (groups of `units` threads) that share a token's heads
-    int T;
-    int heads;               // of both tensors
-    bool copy_q, copy_k;     // copied values have somewhere else to go
+// What angles are made of.
+struct Angles {
+    const int32_t* positions;
+    long long pos_stride;
+    Factor attention;
+    int axes;
+    int pairs;                                // of a row
+    int T;                                    // tokens
+
+    __device__ __forceinline__ bool plain() const { return attention.hi == 1.f && attention.lo == 0.f; }
 };
 
-// Slot (token t, chunk c) takes heads c, c + chunks, ..: neighbouring slots are at
-// neighbouring rows at any moment.
-template <int LAYOUT, int W>
-__global__ void __launch_bounds__(kRopeThreads)
-rope_kernel(const __grid_constant__ tgvkv_rope_plan plan, const RopeShape sh, const float sign,
-            const int32_t* positions, const long long pos_stride, const RopeTensor q,
-            const RopeTensor k) {
-    constexpr bool HALF = LAYOUT == TGVKV_ROPE_HALF;
-    constexpr int P = HALF ? W : W / 2;              // pairs of a unit
-    constexpr int BATCH = 4;
-    const int per_block = kRopeThreads / sh.units;   // slots
-    const int sub = threadIdx.x / sh.units, unit = threadIdx.x - sub * sh.units;
-    const unsigned slot = blockIdx.x * (unsigned)per_block + sub;
-    const int t = (int)(slot / (unsigned)sh.chunks), c0 = (int)(slot - (unsigned)t * sh.chunks);
-    if (sub >= per_block || t >= sh.T) return;
-    const int half = plan.rot_dim >> 1;
-    const bool turns = unit < sh.turned;
-    // the unit's first value, and for pairs of two halves their second ones' distance
-    const int at = HALF && !turns ? plan.rot_dim + (unit - sh.turned) * W : unit * W;
-    float c[P], s[P];
-    if (turns) {
+// A plan's pairs in shared memory: lanes that read different ones of a parameter wait for one
+// another.
+struct PlanPairs {
+    uint64_t turns[TGVKV_ROPE_MAX_DIM / 2];
+    uint8_t axis[TGVKV_ROPE_MAX_DIM / 2];
+
+    __device__ __forceinline__ void take(const tgvkv_rope_plan& plan, int pairs) {
+        for (int i = threadIdx.x; i < pairs; i += kRopeThreads) turns[i] = plan.turns[i], axis[i] = plan.axis[i];
+        __syncthreads();
+    }
+};
+
+// Where pair i's (c, s) lies among a token's: the P pairs of a unit are read two at a time,
+// by neighbouring units from neighbouring places.
+template <int P>
+__device__ __forceinline__ int angle_place(int i, int pairs) {
+    if (P == 1) return i;
+    const int unit = i / P, j = i % P;
+    return ((j >> 1) * (pairs / P) + unit) * 2 + (j & 1);
+}
+
+// The angles of n tokens from t0 on into `table`, [token][pairs], by the CTA.
+template <int P>
+__device__ __forceinline__ void make_angles(const Angles& an, const PlanPairs& pp, int t0, int n, float2* table) {
+    int t = threadIdx.x / an.pairs, i = threadIdx.x - t * an.pairs;
+    const int dt = kRopeThreads / an.pairs, di = kRopeThreads - dt * an.pairs;
+    while (t < n) {
+        const int32_t* of_token = an.positions + t0 + t;
+        const int p = an.axes == 1 ? *of_token : of_token[pp.axis[i] * an.pos_stride];
+        float c, s;
+        cos_sin_of_turn(turn_of(p, pp.turns[i]), c, s);
+        if (!an.plain()) c = an.attention.times(c), s = an.attention.times(s);
+        table[t * an.pairs + angle_place<P>(i, an.pairs)] = make_float2(c, s);
+        t += dt, i += di;
+        if (i >= an.pairs) i -= an.pairs, ++t;
+    }
+}
+
+// The P pairs of unit `unit` of one token.
+template <int P>
+__device__ __forceinline__ void take_angles(const float2* of_token, int unit, int pairs, float (&c)[P], float (&s)[P]) {
+    if constexpr (P == 1) {
+        c[0] = of_token[unit].x, s[0] = of_token[unit].y;
+    } else {
 #pragma unroll
-        for (int i = 0; i < P; ++i) {
-            pair_at(plan, unit * P + i, positions, pos_stride, t, c[i], s[i]);
-            s[i] *= sign;
+        for (int j = 0; j < P; j += 2) {
+            const float4 two = reinterpret_cast<const float4*>(of_token)[(j >> 1) * (pairs / P) + unit];
+            c[j] = two.x, s[j] = two.y, c[j + 1] = two.z, s[j + 1] = two.w;
         }
     }
-    for (int h0 = c0; h0 < sh.heads; h0 += BATCH * sh.chunks) {
-        Values<W> a[BATCH], b[BATCH];
+}
+
+// A tensor's rows cut into tiles of `tokens` tokens: groups of threads take `rows` of a token's
+// rows at a time, `parts` times, of `side` tokens side by side, and of the `deep` tokens that
+// are `side` apart.
+struct Tiles {
+    int first, blocks;                        // CTAs
+    int count;                                // tiles, which the CTAs take in turn
+    int side, deep, tokens, rows, parts;
+    unsigned magic;                           // n / rows = n * magic >> 16 for n < 256
+};
+
+// Where a CTA is among its tiles and their parts.
+struct Step {
+    int tile, part;
+
+    __device__ __forceinline__ void next(const Tiles& ti) {
+        if (++part == ti.parts) part = 0, tile += ti.blocks;
+    }
+    // every token of the tile is there, kRopeRows deep
+    __device__ __forceinline__ bool full(const Tiles& ti, int T) const {
+        return ti.deep == kRopeRows && (long long)tile * ti.tokens + ti.tokens <= T;
+    }
+};
+
+// A group's place in every tile: row r of a part, token `of` of those side by side.
+struct Place {
+    int of, r;
+
+    __device__ __forceinline__ Place(const Tiles& ti, int group) {
+        of = (int)(group * ti.magic >> 16);
+        r = group - of * ti.rows;
+    }
+    // how many of the tokens of, of + side, .. it has rows of: the row u is u * side < left
+    __device__ __forceinline__ int left(const Tiles& ti, const Step& st, int heads, int T) const {
+        if (of >= ti.side || st.part * ti.rows + r >= heads || st.tile >= ti.count) return 0;
+        return min(T - st.tile * ti.tokens, ti.tokens) - of;
+    }
+};
+
+// A thread's address in a tensor, which goes on by constants: `side` to the next of its rows
+// in a tile, then on to the next part or tile.
+template <typename T>
+struct Walk {
+    T* at;
+    long long side, part, tile;
+
+    __device__ __forceinline__ Walk(const Tiles& ti, const Step& st, const Place& pl, T* base, long long tok,
+                                    long long head, int value) {
+        at = base + ((long long)st.tile * ti.tokens + pl.of) * tok + pl.r * head + value;
+        side = ti.side * tok;
+        part = ti.rows * head;
+        tile = (long long)ti.blocks * ti.tokens * tok - (ti.parts - 1) * part;
+    }
+    __device__ __forceinline__ void next(const Tiles& ti, const Step& st) {
+        at += st.part + 1 < ti.parts ? part : tile;
+    }
+};
+
+// Calls f(u, address) for the rows of a part that the thread has, without a test a row where
+// the tile is full.
+template <typename T, typename F>
+__device__ __forceinline__ void for_rows(const Tiles& ti, const Step& st, int left, int tokens,
+                                         const Walk<T>& walk, F&& f) {
+    T* at = walk.at;
+    if (st.full(ti, tokens)) {
+        if (left > 0) {
 #pragma unroll
-        for (int u = 0; u < BATCH; ++u) {
-            const int h = h0 + u * sh.chunks;
-            if (h >= sh.heads) break;
-            const RopeTensor& x = h < q.heads ? q : k;
-            const uint16_t* row = x.x + t * x.x_tok + (h < q.heads ? h : h - q.heads) * x.x_head + at;
-            a[u].w = *reinterpret_cast<const typename Words<W>::type*>(row);
-            if (HALF && turns) b[u].w = *reinterpret_cast<const typename Words<W>::type*>(row + half);
+            for (int u = 0; u < kRopeRows; ++u, at += walk.side) f(u, at);
         }
+    } else {
 #pragma unroll
-        for (int u = 0; u < BATCH; ++u) {
-            const int h = h0 + u * sh.chunks;
-            if (h >= sh.heads) break;
-            const bool is_q = h < q.heads;
-            const RopeTensor& x = is_q ? q : k;
-            uint16_t* row = x.y + t * x.y_tok + (is_q ? h : h - q.heads) * x.y_head + at;
+        for (int u = 0; u < kRopeRows; ++u, at += walk.side)
+            if (u * ti.side < left) f(u, at);
+    }
+}
+
+// Host: the tiles of the tokens' `heads` rows for CTAs of `groups` groups: kRopeRows tokens deep,
+// less where that would leave SMs without one, or where their angles would exceed
+// kTableAngles.
+Tiles make_tiles(const Angles& an, int heads, int groups, int sms) {
+    Tiles ti{};
+    if (heads == 0) return ti;
+    ti.parts = (heads + groups - 1) / groups;
+    ti.rows = (heads + ti.parts - 1) / ti.parts;
+    ti.side = groups / ti.rows;
+    ti.deep = std::min(std::min(an.T / (ti.side * sms), kTableAngles / (ti.side * an.pairs)), kRopeRows);
+    ti.deep = std::max(ti.deep, 1);
+    ti.tokens = ti.side * ti.deep;
+    ti.count = (int)(((long long)an.T + ti.tokens - 1) / ti.tokens);
+    ti.magic = (65536u + ti.rows - 1) / ti.rows;
+    return ti;
+}
+
+// Host: CTAs for tensors' tiles, as many as are resident at a time, shared out by their rows.
+template <int N>
+unsigned share_blocks(Tiles* (&ti)[N], const int (&heads)[N], int sms) {
+    int all = 0, first = 0;
+    for (int h : heads) all += h;
+    const long long most = (long long)sms * kRopeResident;
+    for (int i = 0; i < N; ++i) {
+        const long long share = (most * heads[i] + all / 2) / all;
+        ti[i]->first = first;
+        ti[i]->blocks = heads[i] > 0 ? (int)std::min<long long>(std::max<long long>(share, 1), ti[i]->count) : 0;
+        first += ti[i]->blocks;
+    }
+    return (unsigned)first;
+}
+
+// A unit of a row: W pairs (values i and i + half of a turned part in halves), W values (W / 2
+// neighbouring pairs), or W values that are copied.
+template <int LAYOUT, int W>
+struct Unit {
+    using Word = typename Words<W>::type;
+    static constexpr bool HALF = LAYOUT == TGVKV_ROPE_HALF;
+    static constexpr int P = HALF ? W : W / 2;
+    Values<W> x, y;                           // values; second halves
+
+    __device__ __forceinline__ void turn(const float (&c)[P], const float (&s)[P]) {
+        if constexpr (!HALF) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                const float x1 = low_value(x.two[i]), x2 = high_value(x.two[i]);
+                x.two[i] = pack_bf16x2(first_of(x1, x2, c[i], s[i]), second_of(x1, x2, c[i], s[i]));
+            }
+        } else if constexpr (W > 1) {
+#pragma unroll
+            for (int i = 0; i < P; i += 2) {
+                uint32_t &f = x.two[i / 2], &g = y.two[i / 2];
+                const float x1 = low_value(f), x2 = low_value(g), z1 = high_value(f), z2 = high_value(g);
+                f = pack_bf16x2(first_of(x1, x2, c[i], s[i]), first_of(z1, z2, c[i + 1], s[i + 1]));
+                g = pack_bf16x2(second_of(x1, x2, c[i], s[i]), second_of(z1, z2, c[i + 1], s[i + 1]));
+            }
+        } else {
+            const float x1 = low_value(x.h[0]), x2 = low_value(y.h[0]);
+            const uint32_t two = pack_bf16x2(first_of(x1, x2, c[0], s[0]), second_of(x1, x2, c[0], s[0]));
+            x.h[0] = (uint16_t)two;
+            y.h[0] = (uint16_t)(two >> 16);
+        }
+    }
+};
+
+// A call's rows.
+struct RopeCall {
+    RopeTensor q, k;
+    Tiles q_tiles, k_tiles;
+    int units, turned;                        // of a row, the turned ones first
+};
+
+template <int LAYOUT, int W>
+__global__ void __launch_bounds__(kRopeThreads, kRopeResident)
+rope_kernel(const __grid_constant__ tgvkv_rope_plan plan, const __grid_constant__ RopeCall a,
+            const __grid_constant__ Angles an) {
+    using U = Unit<LAYOUT, W>;
+    using Word = typename U::Word;
+    constexpr int P = U::P;
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ PlanPairs pp;
+    const bool is_k = blockIdx.x >= (unsigned)a.q_tiles.blocks;
+    const RopeTensor x = is_k ? a.k : a.q;
+    const Tiles ti = is_k ? a.k_tiles : a.q_tiles;
+    const int group = threadIdx.x / a.units, unit = threadIdx.x - group * a.units;
+    const int half = plan.rot_dim >> 1;
+    const bool turns = unit < a.turned, moves = x.x != x.y;
+    const int first = U::HALF && !turns ? plan.rot_dim + (unit - a.turned) * W : unit * W;
+    const Place place(ti, group);
+    Step st{(int)blockIdx.x - ti.first, 0};
+    Walk<const uint16_t> from(ti, st, place, x.x, x.x_tok, x.x_head, first);
+    Walk<uint16_t> to(ti, st, place, x.y, x.y_tok, x.y_head, first);
+    U v[kRopeRows];
+    auto load = [&](const Step& of) {
+        for_rows(ti, of, place.left(ti, of, x.heads, an.T), an.T, from, [&](int u, const uint16_t* row) {
+            v[u].x.w = *reinterpret_cast<const Word*>(row);
+            if (U::HALF && turns) v[u].y.w = *reinterpret_cast<const Word*>(row + half);
+        });
+    };
+    load(st);
+    pp.take(plan, an.pairs);
+    float2* table = reinterpret_cast<float2*>(smem);           // two, in turn
+    for (int flip = 0; st.tile < ti.count; flip ^= 1) {
+        float2* angles = table + flip * (ti.tokens * an.pairs);
+        const int t0 = st.tile * ti.tokens;
+        make_angles<P>(an, pp, t0, min(ti.tokens, an.T - t0), angles);
+        __syncthreads();           // (and all are done with the other table, the next tile's)
+        angles += place.of * an.pairs;
+        const int deeper = ti.side * an.pairs;
+        for (int part = 0; part < ti.parts; ++part) {
+            for_rows(ti, st, place.left(ti, st, x.heads, an.T), an.T, to, [&](int u, uint16_t* row) {
+                if (turns) {
+                    float c[P], s[P];
+                    take_angles<P>(angles + u * deeper, unit, an.pairs, c, s);
+                    v[u].turn(c, s);
+                    if (U::HALF) *reinterpret_cast<Word*>(row + half) = v[u].y.w;
+                }
+                if (turns || moves) *reinterpret_cast<Word*>(row) = v[u].x.w;
+            });
+            from.next(ti, st);
+            to.next(ti, st);
+            st.next(ti);
+            load(st);
+        }
+    }
+}
+
+// One row a token: there is nothing to share, every thread computes the angles of its rows.
+template <int LAYOUT, int W>
+__global__ void __launch_bounds__(kRopeThreads, kOneResident)
+rope_one_kernel(const __grid_constant__ tgvkv_rope_plan plan, const RopeTensor x, int units, int turned,
+                const __grid_constant__ Angles an) {
+    using U = Unit<LAYOUT, W>;
+    using Word = typename U::Word;
+    constexpr int P = U::P, N = 2;
+    const int groups = kRopeThreads / units, group = threadIdx.x / units, unit = threadIdx.x - group * units;
+    if (group >= groups) return;
+    const int half = plan.rot_dim >> 1;
+    const bool turns = unit < turned, moves = x.x != x.y;
+    const int first = U::HALF && !turns ? plan.rot_dim + (unit - turned) * W : unit * W;
+    uint64_t f[P];
+#pragma unroll
+    for (int i = 0; i < P; ++i) f[i] = plan.turns[turns ? unit * P + i : 0];
+    const long long step = (long long)gridDim.x * groups;
+    long long t = (long long)blockIdx.x * groups + group, loads = t;
+    const uint16_t* from = x.x + t * x.x_tok + first;
+    uint16_t* to = x.y + t * x.y_tok + first;
+    const long long from_step = step * x.x_tok, to_step = step * x.y_tok;
+    U v[N];
+    int p[N];
+    auto load = [&](int u) {
+        if (loads < an.T) {
+            v[u].x.w = *reinterpret_cast<const Word*>(from);
+            if (U::HALF && turns) v[u].y.w = *reinterpret_cast<const Word*>(from + half);
+            p[u] = an.positions[loads];
+        }
+        loads += step;
+        from += from_step;
+    };
+#pragma unroll
+    for (int u = 0; u < N; ++u) load(u);
+    while (t < an.T) {
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            if (t >= an.T) break;
             if (turns) {
+                float c[P], s[P];
 #pragma unroll
                 for (int i = 0; i < P; ++i) {
-                    uint16_t& h1 = a[u].h[HALF ? i : 2 * i];
-                    uint16_t& h2 = HALF ? b[u].h[i] : a[u].h[(2 * i + 1) % W];
-                    const float x1 = bf16_value(h1), x2 = bf16_value(h2);
-                    h1 = bf16_round(fmaf(x1, c[i], -(x2 * s[i])));
-                    h2 = bf16_round(fmaf(x2, c[i], x1 * s[i]));
+                    const int pi = an.axes == 1 ? p[u] : an.positions[plan.axis[unit * P + i] * an.pos_stride + t];
+                    cos_sin_of_turn(turn_of(pi, f[i]), c[i], s[i]);
                 }
-                if (HALF) *reinterpret_cast<typename Words<W>::type*>(row + half) = b[u].w;
-            } else if (!(is_q ? sh.copy_q : sh.copy_k)) {
-                continue;
+                if (!an.plain()) {
+#pragma unroll
+                    for (int i = 0; i < P; ++i) c[i] = an.attention.times(c[i]), s[i] = an.attention.times(s[i]);
+                }
+                v[u].turn(c, s);
+                if (U::HALF) *reinterpret_cast<Word*>(to + half) = v[u].y.w;
             }
-            *reinterpret_cast<typename Words<W>::type*>(row) = a[u].w;
+            if (turns || moves) *reinterpret_cast<Word*>(to) = v[u].x.w;
+            to += to_step;
+            t += step;
+            load(u);
         }
     }
 }
 
-// Slots that share a token's rows, so that few tokens fill the GPU (2048 threads an SM)
-// and many compute their angles once.
-int chunks_of(long long tokens, int threads_a_slot, int rows, int sms) {
-    const long long want = (long long)sms * 2048, have = tokens * threads_a_slot;
-    return (int)std::min<long long>(std::max<long long>((want + have - 1) / have, 1), rows);
-}
-
 template <int LAYOUT, int W>
-cudaError_t launch_rope_w(const tgvkv_rope_plan& plan, RopeShape sh, float sign,
-                          const int32_t* positions, long long pos_stride, const RopeTensor& q,
-                          const RopeTensor& k, cudaStream_t stream) {
-    const int rot = plan.rot_dim;
-    sh.turned = LAYOUT == TGVKV_ROPE_HALF ? rot / 2 / W : rot / W;
-    sh.units = sh.turned + (plan.d - rot) / W;
-    const int sms = device_sm_count();
+cudaError_t launch_rope_w(const tgvkv_rope_plan& plan, RopeCall a, const Angles& an, cudaStream_t stream) {
+    const int rot = plan.rot_dim, sms = device_sm_count();
     if (sms <= 0) return cudaErrorInvalidDevice;
-    sh.chunks = chunks_of(sh.T, sh.units, sh.heads, sms);
-    const long long slots = (long long)sh.T * sh.chunks;
-    const int per_block = kRopeThreads / sh.units;
-    rope_kernel<LAYOUT, W><<<(unsigned)((slots + per_block - 1) / per_block), kRopeThreads, 0, stream>>>(
-        plan, sh, sign, positions, pos_stride, q, k);
+    a.turned = LAYOUT == TGVKV_ROPE_HALF ? rot / 2 / W : rot / W;
+    a.units = a.turned + (plan.d - rot) / W;
+    const int groups = kRopeThreads / a.units;
+    for (RopeTensor* x : {&a.q, &a.k}) {
+        if (x->heads != 1) continue;
+        const unsigned blocks = (unsigned)std::min<long long>(((long long)an.T + groups - 1) / groups,
+                                                              (long long)sms * kOneResident);
+        rope_one_kernel<LAYOUT, W><<<blocks, kRopeThreads, 0, stream>>>(plan, *x, a.units, a.turned, an);
+        x->heads = 0;
+    }
+    if (a.q.heads + a.k.heads > 0) {
+        a.q_tiles = make_tiles(an, a.q.heads, groups, sms);
+        a.k_tiles = make_tiles(an, a.k.heads, groups, sms);
+        Tiles* tiles[2] = {&a.q_tiles, &a.k_tiles};
+        const unsigned blocks = share_blocks(tiles, {a.q.heads, a.k.heads}, sms);
+        const size_t smem = 2 * sizeof(float2) * std::max(a.q_tiles.tokens, a.k_tiles.tokens) * an.pairs;
+        rope_kernel<LAYOUT, W><<<blocks, kRopeThreads, smem, stream>>>(plan, a, an);
+    }
     return cudaGetLastError();
 }
 
 // ---- turned and stored -------------------------------------------------------------
 struct RopeWrite {
-    RopeTensor q;                             // y: q_out
-    const uint16_t *k, *v;
-    long long k_tok, k_head, v_tok, v_head;
+    RopeTensor q;                             // y: q_out; no heads where there are no queries
+    RopeTensor k, v;                          // y: none
+    Tiles q_tiles, k_tiles, v_tiles;
     const int32_t* slots;                     // [T][H_kv]
-    int T, rows;                              // rows of a token: H_q (0 without q) + 2 H_kv
-    int chunks;
 };
 
-// Lane `unit` of a slot has values 8 unit .. 8 unit + 7 of its rows (the groups of a scale
-// are then 4 neighbouring lanes, as in cache_write_kernel) and loads their partners beside
-// them.  EVEN: whole vectors turn, and partners are whole vectors too.
-template <int D, int FMT, int LAYOUT, bool EVEN>
-__global__ void __launch_bounds__(kRopeThreads)
-rope_write_kernel(const __grid_constant__ tgvkv_rope_plan plan, const CacheProblem p,
-                  const RopeWrite a, const CachePools pool, const int32_t* positions,
-                  const long long pos_stride, uint32_t* __restrict__ status) {
-    constexpr bool HALF = LAYOUT == TGVKV_ROPE_HALF;
-    constexpr int LPR = D / 8, BATCH = 2;
+// One vector of 8 values into row `row` of a pool (-1: none), `unit` being the vector's number
+// in its row; 4 neighbouring lanes have 4 neighbouring vectors.
+template <int D, int FMT>
+__device__ __forceinline__ void store_vector(uint4 w, uint8_t* rows, uint8_t* scales, int row, int unit) {
     constexpr int RB = FMT == TGVKV_CACHE_BF16 ? 2 * D : FMT == TGVKV_CACHE_INT8 ? D : D / 2;
-    const int unit = threadIdx.x % LPR;
-    const unsigned slot = blockIdx.x * (unsigned)(kRopeThreads / LPR) + threadIdx.x / LPR;
-    const int t = (int)(slot / (unsigned)a.chunks), c0 = (int)(slot - (unsigned)t * a.chunks);
-    const bool live = t < a.T;                // all lanes stay: the groups' maxima need them
-    const int half = plan.rot_dim >> 1, e0 = 8 * unit;
-    float c[8], s[8];                         // of each value; s with the sign its partner takes
-#pragma unroll
-    for (int j = 0; j < 8; ++j) c[j] = 1.f, s[j] = 0.f;
-    if (live && e0 < plan.rot_dim) {
-        if (HALF) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int e = e0 + j;
-                if (!EVEN && e >= plan.rot_dim) break;
-                pair_at(plan, e < half ? e : e - half, positions, pos_stride, t, c[j], s[j]);
-                if (e < half) s[j] = -s[j];
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; j += 2) {
-                if (!EVEN && e0 + j >= plan.rot_dim) break;
-                pair_at(plan, (e0 + j) >> 1, positions, pos_stride, t, c[j], s[j + 1]);
-                c[j + 1] = c[j];
-                s[j] = -s[j + 1];
-            }
-        }
+    const size_t at = row >= 0 ? row : 0;
+    if (FMT == TGVKV_CACHE_BF16) {
+        if (row >= 0) reinterpret_cast<uint4*>(rows + at * RB)[unit] = w;
+    } else {                           // lanes without a row take part in the maxima
+        store_row<FMT>(w, rows + at * RB, scales + at * (D / kGroup), unit, row >= 0);
     }
-    const long long pool_rows = (long long)p.n_pages * p.page;
-    const int n_q = a.q.heads;
-    for (int r0 = 0; r0 < a.rows; r0 += BATCH * a.chunks) {
-        Values<8> x[BATCH], y[BATCH];
+}
+
+// The lanes of a group hold a row's vectors of 8 values so that a scale's 4 vectors are in 4
+// neighbouring lanes.  TWO (whole heads in halves, and neighbouring pairs): lane i has vectors
+// i and i + D / 16, which are each other's partners in halves.  Else (part of a head in halves,
+// and parts that end inside a vector) lane i has vector i and loads the partners beside it.
+template <int D, int FMT, int LAYOUT, bool TWO>
+__global__ void __launch_bounds__(kRopeThreads, kRopeResident)
+rope_write_kernel(const __grid_constant__ tgvkv_rope_plan plan, const __grid_constant__ RopeWrite a,
+                  const __grid_constant__ Angles an, const CacheProblem p, const CachePools pool,
+                  uint32_t* __restrict__ status) {
+    constexpr bool HALF = LAYOUT == TGVKV_ROPE_HALF;
+    constexpr int LPR = TWO ? D / 16 : D / 8, P = HALF ? 8 : 4;
+    constexpr int PLACED = TWO ? P : 1;       // how the angles lie in their table
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ PlanPairs pp;
+    const bool is_v = blockIdx.x >= (unsigned)a.v_tiles.first;
+    const bool is_q = !is_v && blockIdx.x < (unsigned)a.q_tiles.blocks;
+    const RopeTensor x = is_q ? a.q : is_v ? a.v : a.k;
+    const Tiles ti = is_q ? a.q_tiles : is_v ? a.v_tiles : a.k_tiles;
+    const int unit = threadIdx.x % LPR, half = plan.rot_dim >> 1, e0 = 8 * unit;
+    const Place place(ti, threadIdx.x / LPR);
+    Step st{(int)blockIdx.x - ti.first, 0};
+    Walk<const uint16_t> from(ti, st, place, x.x, x.x_tok, x.x_head, e0);
+    Walk<uint16_t> to(ti, st, place, x.y, x.y_tok, x.y_head, e0);          // of queries
+    Values<8> v[kRopeRows], w[kRopeRows];     // the values; the other vector, or the partners
+    int row_of[kRopeRows];                    // pool rows
+    auto load = [&](const Step& of) {
+        const int left = place.left(ti, of, x.heads, an.T);
 #pragma unroll
-        for (int u = 0; u < BATCH; ++u) {
-            const int r = r0 + u * a.chunks + c0;
-            x[u].w = y[u].w = make_uint4(0u, 0u, 0u, 0u);
-            if (!live || r >= a.rows) continue;
-            const bool is_v = r >= n_q + p.H_kv;
-            const uint16_t* row = r < n_q ? a.q.x + t * a.q.x_tok + r * a.q.x_head
-                                  : is_v  ? a.v + t * a.v_tok + (r - n_q - p.H_kv) * a.v_head
-                                          : a.k + t * a.k_tok + (r - n_q) * a.k_head;
-            x[u].w = *reinterpret_cast<const uint4*>(row + e0);
-            if (HALF && !is_v && e0 < plan.rot_dim) {
-                if (EVEN) {
-                    y[u].w = *reinterpret_cast<const uint4*>(row + (e0 < half ? e0 + half : e0 - half));
-                } else {
+        for (int u = 0; u < kRopeRows; ++u) row_of[u] = -1;
+        if (!is_q) {
+            const int at = (of.tile * ti.tokens + place.of) * p.H_kv + of.part * ti.rows + place.r;   // below 2^31
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int e = e0 + j;
-                        if (e < plan.rot_dim) y[u].h[j] = row[e < half ? e + half : e - half];
-                    }
-                }
-            }
+            for (int u = 0; u < kRopeRows; ++u)
+                if (u * ti.side < left) row_of[u] = a.slots[at + u * ti.side * p.H_kv];
         }
-        __syncwarp();                          // q_out may be q: every partner is read by now
-#pragma unroll
-        for (int u = 0; u < BATCH; ++u) {
-            const int r = r0 + u * a.chunks + c0;
-            const bool mine = live && r < a.rows, is_q = r < n_q, is_v = r >= n_q + p.H_kv;
-            if (mine && !is_v && e0 < plan.rot_dim) {
-                Values<8> z;
+        for_rows(ti, of, left, an.T, from, [&](int u, const uint16_t* row) {
+            v[u].w = *reinterpret_cast<const uint4*>(row);
+            if (TWO) {
+                w[u].w = *reinterpret_cast<const uint4*>(row + D / 2);
+            } else if (HALF && !is_v) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const uint16_t other = HALF ? y[u].h[j] : x[u].h[j ^ 1];
-                    z.h[j] = bf16_round(fmaf(bf16_value(x[u].h[j]), c[j], bf16_value(other) * s[j]));
-                    if (!EVEN && e0 + j >= plan.rot_dim) z.h[j] = x[u].h[j];
-                }
-                x[u] = z;
-            }
-            if (mine && is_q)
-                reinterpret_cast<uint4*>(a.q.y + t * a.q.y_tok + r * a.q.y_head)[unit] = x[u].w;
-            const bool stores = mine && !is_q;
-            int at = -1;
-            if (stores) {
-                at = a.slots[(size_t)t * p.H_kv + (is_v ? r - n_q - p.H_kv : r - n_q)];
-                if (at >= pool_rows) {
-                    if (unit == 0) raise_status(status, TGVKV_STATUS_INDEX);
-                    at = -1;
+                    const int e = e0 + j;
+                    w[u].h[j] = e < plan.rot_dim ? row[e < half ? j + half : j - half] : 0;
                 }
             }
-            const bool on = at >= 0;
-            const size_t row = on ? at : 0;
-            uint8_t* to = is_v ? pool.v : pool.k;
-            if (FMT == TGVKV_CACHE_BF16) {
-                if (on) reinterpret_cast<uint4*>(to + row * RB)[unit] = x[u].w;
-            } else if (__any_sync(~0u, on)) {
-                store_row<FMT>(x[u].w, to + row * RB, (is_v ? pool.vs : pool.ks) + row * (D / kGroup), unit, on);
+        });
+    };
+#pragma unroll
+    for (int u = 0; u < kRopeRows; ++u) v[u].w = w[u].w = make_uint4(0u, 0u, 0u, 0u);
+    load(st);
+    pp.take(plan, an.pairs);
+    float2* table = reinterpret_cast<float2*>(smem);
+    const int pool_rows = p.n_pages * p.page;          // below 2^31
+    uint8_t* rows = is_v ? pool.v : pool.k;
+    uint8_t* scales = is_v ? pool.vs : pool.ks;
+    for (int flip = 0; st.tile < ti.count; flip ^= 1) {
+        float2* angles = table + flip * (ti.tokens * an.pairs);
+        if (!is_v) {
+            const int t0 = st.tile * ti.tokens;
+            make_angles<PLACED>(an, pp, t0, min(ti.tokens, an.T - t0), angles);
+            __syncthreads();       // (and all are done with the other table, the next tile's)
+        }
+        angles += place.of * an.pairs;
+        const int deeper = ti.side * an.pairs;
+        for (int part = 0; part < ti.parts; ++part) {
+            const int left = place.left(ti, st, x.heads, an.T);
+            if (!TWO) __syncwarp();            // q_out may be q: a group's rows have been loaded before one is stored
+            for_rows(ti, st, is_v ? 0 : left, an.T, to, [&](int u, uint16_t* row) {
+                const float2* of_token = angles + u * deeper;
+                float c[P], s[P];
+                if constexpr (TWO && HALF) {
+                    take_angles<P>(of_token, unit, an.pairs, c, s);
+                    Unit<LAYOUT, 8> both{v[u], w[u]};
+                    both.turn(c, s);
+                    v[u] = both.x, w[u] = both.y;
+                } else if constexpr (TWO) {
+                    Unit<LAYOUT, 8> one{v[u], v[u]}, two{w[u], w[u]};
+                    if (e0 < plan.rot_dim) {
+                        take_angles<P>(of_token, unit, an.pairs, c, s);
+                        one.turn(c, s);
+                    }
+                    if (e0 + D / 2 < plan.rot_dim) {
+                        take_angles<P>(of_token, unit + D / 16, an.pairs, c, s);
+                        two.turn(c, s);
+                    }
+                    v[u] = one.x, w[u] = two.x;
+                } else {
+#pragma unroll
+                    for (int j = 0; j < P; ++j) {
+                        const int e = HALF ? e0 + j : e0 + 2 * j;
+                        const float2 cs = of_token[e >= plan.rot_dim ? 0 : !HALF ? e >> 1 : e < half ? e : e - half];
+                        c[j] = cs.x, s[j] = cs.y;
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t own = v[u].two[j];
+                        uint32_t z;
+                        if constexpr (HALF) {
+                            // y1 takes the partner's product off, y2 adds it
+                            uint32_t other = w[u].two[j];
+                            if (e0 + 2 * j < half) other ^= 0x00008000u;
+                            if (e0 + 2 * j + 1 < half) other ^= 0x80000000u;
+                            z = pack_bf16x2(fmaf(low_value(own), c[2 * j], low_value(other) * s[2 * j]),
+                                            fmaf(high_value(own), c[(2 * j + 1) % P],
+                                                 high_value(other) * s[(2 * j + 1) % P]));
+                        } else {
+                            const float x1 = low_value(own), x2 = high_value(own);
+                            z = pack_bf16x2(first_of(x1, x2, c[j % P], s[j % P]), second_of(x1, x2, c[j % P], s[j % P]));
+                        }
+                        v[u].two[j] = e0 + 2 * j < plan.rot_dim ? z : own;
+                    }
+                }
+                if (is_q) {
+                    *reinterpret_cast<uint4*>(row) = v[u].w;
+                    if (TWO) *reinterpret_cast<uint4*>(row + D / 2) = w[u].w;
+                }
+            });
+            if (!is_q) {
+#pragma unroll
+                for (int u = 0; u < kRopeRows; ++u) {
+                    if (row_of[u] >= pool_rows) {
+                        if (unit == 0) raise_status(status, TGVKV_STATUS_INDEX);
+                        row_of[u] = -1;
+                    }
+                    store_vector<D, FMT>(v[u].w, rows, scales, row_of[u], unit);
+                    if (TWO) store_vector<D, FMT>(w[u].w, rows, scales, row_of[u], unit + D / 16);
+                }
             }
+            from.next(ti, st);
+            to.next(ti, st);
+            st.next(ti);
+            load(st);
         }
     }
 }
 
-template <int D, int FMT, int LAYOUT, bool EVEN>
+template <int D, int FMT, int LAYOUT, bool TWO>
 cudaError_t launch_write(const CacheProblem& p, const CachePools& pool, const tgvkv_rope_plan& plan,
-                         RopeWrite a, const int32_t* positions, long long pos_stride, uint32_t* status,
-                         cudaStream_t stream) {
+                         RopeWrite a, const Angles& an, uint32_t* status, cudaStream_t stream) {
     const int sms = device_sm_count();
     if (sms <= 0) return cudaErrorInvalidDevice;
-    a.chunks = chunks_of(a.T, D / 8, a.rows, sms);
-    constexpr int per_block = kRopeThreads / (D / 8);
-    const long long slots = (long long)a.T * a.chunks;
-    rope_write_kernel<D, FMT, LAYOUT, EVEN>
-        <<<(unsigned)((slots + per_block - 1) / per_block), kRopeThreads, 0, stream>>>(
-            plan, p, a, pool, positions, pos_stride, status);
+    constexpr int groups = kRopeThreads / (TWO ? D / 16 : D / 8);
+    a.q_tiles = make_tiles(an, a.q.heads, groups, sms);
+    a.k_tiles = a.v_tiles = make_tiles(an, p.H_kv, groups, sms);
+    Tiles* tiles[3] = {&a.q_tiles, &a.k_tiles, &a.v_tiles};
+    const unsigned blocks = share_blocks(tiles, {a.q.heads, p.H_kv, p.H_kv}, sms);
+    const size_t smem = 2 * sizeof(float2) * std::max(a.q_tiles.tokens, a.k_tiles.tokens) * an.pairs;
+    rope_write_kernel<D, FMT, LAYOUT, TWO><<<blocks, kRopeThreads, smem, stream>>>(plan, a, an, p, pool, status);
     return cudaGetLastError();
 }
 
 template <int D, int FMT>
-cudaError_t launch_write_by_layout(const CacheProblem& p, const CachePools& pool,
-                                   const tgvkv_rope_plan& plan, const RopeWrite& a,
-                                   const int32_t* positions, long long pos_stride, uint32_t* status,
-                                   cudaStream_t stream) {
+cudaError_t launch_write_by_layout(const CacheProblem& p, const CachePools& pool, const tgvkv_rope_plan& plan,
+                                   const RopeWrite& a, const Angles& an, uint32_t* status, cudaStream_t stream) {
     if (plan.layout == TGVKV_ROPE_HALF)
-        return plan.rot_dim % 16 == 0
-                   ? launch_write<D, FMT, TGVKV_ROPE_HALF, true>(p, pool, plan, a, positions, pos_stride, status, stream)
-                   : launch_write<D, FMT, TGVKV_ROPE_HALF, false>(p, pool, plan, a, positions, pos_stride, status, stream);
+        return plan.rot_dim == D
+                   ? launch_write<D, FMT, TGVKV_ROPE_HALF, true>(p, pool, plan, a, an, status, stream)
+                   : launch_write<D, FMT, TGVKV_ROPE_HALF, false>(p, pool, plan, a, an, status, stream);
     return plan.rot_dim % 8 == 0
-               ? launch_write<D, FMT, TGVKV_ROPE_INTERLEAVED, true>(p, pool, plan, a, positions, pos_stride, status, stream)
-               : launch_write<D, FMT, TGVKV_ROPE_INTERLEAVED, false>(p, pool, plan, a, positions, pos_stride, status, stream);
+               ? launch_write<D, FMT, TGVKV_ROPE_INTERLEAVED, true>(p, pool, plan, a, an, status, stream)
+               : launch_write<D, FMT, TGVKV_ROPE_INTERLEAVED, false>(p, pool, plan, a, an, status, stream);
 }
 
 template <int D>
-cudaError_t launch_write_by_format(const CacheProblem& p, const CachePools& pool,
-                                   const tgvkv_rope_plan& plan, const RopeWrite& a,
-                                   const int32_t* positions, long long pos_stride, uint32_t* status,
-                                   cudaStream_t stream) {
+cudaError_t launch_write_by_format(const CacheProblem& p, const CachePools& pool, const tgvkv_rope_plan& plan,
+                                   const RopeWrite& a, const Angles& an, uint32_t* status, cudaStream_t stream) {
     switch (p.format) {
-        case TGVKV_CACHE_BF16: return launch_write_by_layout<D, TGVKV_CACHE_BF16>(p, pool, plan, a, positions, pos_stride, status, stream);
-        case TGVKV_CACHE_INT8: return launch_write_by_layout<D, TGVKV_CACHE_INT8>(p, pool, plan, a, positions, pos_stride, status, stream);
-        case TGVKV_CACHE_INT4: return launch_write_by_layout<D, TGVKV_CACHE_INT4>(p, pool, plan, a, positions, pos_stride, status, stream);
-        default: return launch_write_by_layout<D, TGVKV_CACHE_FP4>(p, pool, plan, a, positions, pos_stride, status, stream);
+        case TGVKV_CACHE_BF16: return launch_write_by_layout<D, TGVKV_CACHE_BF16>(p, pool, plan, a, an, status, stream);
+        case TGVKV_CACHE_INT8: return launch_write_by_layout<D, TGVKV_CACHE_INT8>(p, pool, plan, a, an, status, stream);
+        case TGVKV_CACHE_INT4: return launch_write_by_layout<D, TGVKV_CACHE_INT4>(p, pool, plan, a, an, status, stream);
+        default: return launch_write_by_layout<D, TGVKV_CACHE_FP4>(p, pool, plan, a, an, status, stream);
     }
+}
+
+// A plan's angles; its attention factor is 1 for rows that are only moved.
+Angles angles_of(const tgvkv_rope_plan& plan, int mode, const int32_t* positions, long long pos_stride, int T) {
+    const double x = mode == TGVKV_ROPE_MOVE ? 1.0 : plan.attention;
+    return Angles{positions, pos_stride, Factor{(float)x, (float)(x - (float)x)}, plan.axes, plan.rot_dim / 2, T};
 }
 
 }  // namespace
@@ -292,25 +603,23 @@ cudaError_t launch_write_by_format(const CacheProblem& p, const CachePools& pool
 cudaError_t launch_rope(const tgvkv_rope_plan& plan, int mode, const int32_t* positions,
                         long long pos_stride, int T, const RopeTensor& q, const RopeTensor& k,
                         cudaStream_t stream) {
+    const Angles an = angles_of(plan, mode, positions, pos_stride, T);
+    RopeCall a{};
+    a.q = q;
+    a.k = k;
     tgvkv_rope_plan used = plan;
-    if (mode == TGVKV_ROPE_MOVE) used.attention = 1.f;
-    const float sign = mode == TGVKV_ROPE_GRADIENT ? -1.f : 1.f;
-    RopeShape sh{};
-    sh.T = T;
-    sh.heads = q.heads + k.heads;
-    sh.copy_q = q.x != q.y;
-    sh.copy_k = k.x != k.y;
+    if (mode == TGVKV_ROPE_GRADIENT)         // turned the other way
+        for (int i = 0; i < an.pairs; ++i) used.turns[i] = 0u - plan.turns[i];
     // the widest load that pairs and their partners allow (rows are 16-byte aligned)
-    const int step = plan.layout == TGVKV_ROPE_HALF ? plan.rot_dim / 2 : plan.rot_dim;
     if (plan.layout == TGVKV_ROPE_HALF) {
-        if (step % 8 == 0) return launch_rope_w<TGVKV_ROPE_HALF, 8>(used, sh, sign, positions, pos_stride, q, k, stream);
-        if (step % 4 == 0) return launch_rope_w<TGVKV_ROPE_HALF, 4>(used, sh, sign, positions, pos_stride, q, k, stream);
-        if (step % 2 == 0) return launch_rope_w<TGVKV_ROPE_HALF, 2>(used, sh, sign, positions, pos_stride, q, k, stream);
-        return launch_rope_w<TGVKV_ROPE_HALF, 1>(used, sh, sign, positions, pos_stride, q, k, stream);
+        if (an.pairs % 8 == 0) return launch_rope_w<TGVKV_ROPE_HALF, 8>(used, a, an, stream);
+        if (an.pairs % 4 == 0) return launch_rope_w<TGVKV_ROPE_HALF, 4>(used, a, an, stream);
+        if (an.pairs % 2 == 0) return launch_rope_w<TGVKV_ROPE_HALF, 2>(used, a, an, stream);
+        return launch_rope_w<TGVKV_ROPE_HALF, 1>(used, a, an, stream);
     }
-    if (step % 8 == 0) return launch_rope_w<TGVKV_ROPE_INTERLEAVED, 8>(used, sh, sign, positions, pos_stride, q, k, stream);
-    if (step % 4 == 0) return launch_rope_w<TGVKV_ROPE_INTERLEAVED, 4>(used, sh, sign, positions, pos_stride, q, k, stream);
-    return launch_rope_w<TGVKV_ROPE_INTERLEAVED, 2>(used, sh, sign, positions, pos_stride, q, k, stream);
+    if (plan.rot_dim % 8 == 0) return launch_rope_w<TGVKV_ROPE_INTERLEAVED, 8>(used, a, an, stream);
+    if (plan.rot_dim % 4 == 0) return launch_rope_w<TGVKV_ROPE_INTERLEAVED, 4>(used, a, an, stream);
+    return launch_rope_w<TGVKV_ROPE_INTERLEAVED, 2>(used, a, an, stream);
 }
 
 cudaError_t launch_rope_write(const CacheProblem& p, const CachePools& pool,
@@ -318,16 +627,14 @@ cudaError_t launch_rope_write(const CacheProblem& p, const CachePools& pool,
                               long long pos_stride, const int32_t* slots, int T, const RopeTensor& q,
                               const uint16_t* k, const uint16_t* v, const long long (&strides)[4],
                               uint32_t* status, cudaStream_t stream) {
+    const Angles an = angles_of(plan, TGVKV_ROPE_FORWARD, positions, pos_stride, T);
     RopeWrite a{};
     a.q = q;
-    a.k = k;
-    a.v = v;
-    a.k_tok = strides[0], a.k_head = strides[1], a.v_tok = strides[2], a.v_head = strides[3];
+    a.k = RopeTensor{k, strides[0], strides[1], nullptr, 0, 0, p.H_kv};
+    a.v = RopeTensor{v, strides[2], strides[3], nullptr, 0, 0, p.H_kv};
     a.slots = slots;
-    a.T = T;
-    a.rows = q.heads + 2 * p.H_kv;
-    return p.d == 64 ? launch_write_by_format<64>(p, pool, plan, a, positions, pos_stride, status, stream)
-                     : launch_write_by_format<128>(p, pool, plan, a, positions, pos_stride, status, stream);
+    return p.d == 64 ? launch_write_by_format<64>(p, pool, plan, a, an, status, stream)
+                     : launch_write_by_format<128>(p, pool, plan, a, an, status, stream);
 }
 
 }  // namespace tgvkv
