@@ -32,7 +32,7 @@ struct PagesArgs {
     const int32_t *lens, *lens_new, *tok_offsets;
     int T;
     int32_t *slots, *lens_out;
-    int granule;                       // set by the launcher
+    int granule_shift;                 // set by the launcher
 };
 cudaError_t launch_pages(const CacheProblem& p, int mode, const PagesArgs& a, uint32_t* ticket,
                          uint32_t* status, cudaStream_t stream);

@@ -11,8 +11,8 @@
 
 namespace tgvkv {
 
-// Launch `kern` as a programmatic dependent of the kernel before it on
-// `stream` (see griddep_wait): its CTAs may be scheduled while that kernel
+// Launch `kern` so that it may start early: as a programmatic dependent of the kernel before it
+// on `stream` (see griddep_wait): its CTAs may be scheduled while that kernel
 // finishes, and the kernels before that one too where it signals before it has
 // waited itself.  What such a kernel must keep, whatever ran before it:
 //   - before griddep_wait it reads only what no kernel of this library writes
@@ -29,10 +29,12 @@ namespace tgvkv {
 // Dependents: score_tc_kernel (each role waits), tpr_select_kernel and
 // tpr_select_warp_kernel, decode_merge_kernel (its offsets are the call's inputs),
 // cache_write_kernel, cache_read_kernel, chunk_stream_kernel, chunk_stream_merge
-// (lengths and offsets: the call's inputs), chunk_tile_kernel, chunk_tile_merge.
+// (lengths and offsets: the call's inputs), chunk_tile_kernel, chunk_tile_merge; and, by
+// launch_early itself, pages_kernel, page_slots_kernel, pages_init_kernel, rope_kernel,
+// rope_one_kernel, rope_write_kernel.
 template <typename... KArgs, typename... Args>
-cudaError_t launch_dependent(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem,
-                             cudaStream_t stream, Args&&... args) {
+cudaError_t launch_early(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem,
+                         cudaStream_t stream, Args&&... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = block;
@@ -44,6 +46,11 @@ cudaError_t launch_dependent(void (*kern)(KArgs...), dim3 grid, dim3 block, size
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, kern, static_cast<Args&&>(args)...);
+}
+template <typename... KArgs, typename... Args>
+cudaError_t launch_dependent(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem,
+                             cudaStream_t stream, Args&&... args) {
+    return launch_early(kern, grid, block, smem, stream, static_cast<Args&&>(args)...);
 }
 
 // TWR scores + TVB statistic (score_tc.cu).  The completion counters in the

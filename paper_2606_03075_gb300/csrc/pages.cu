@@ -9,8 +9,10 @@
 // for long prompts.  Every CTA makes the prefix sums of all sets for itself (8 bytes a set
 // from L2), so that none waits for another; the one that ends last writes n_free, which
 // all have read by then.  Prefixes are kept of granules of 1, 2, 4 or 8 sets, at most
-// kGranules of them (32 KB); entries and tokens are shared out flat, so that one long set
-// is spread as well as many short ones.
+// kGranules of them (32 KB).  Entries and tokens are shared out flat, so that one long set
+// is spread as well as many short ones; where sequences have few new tokens (a decode step) a
+// thread does all of its sets instead, without a search (BY_SET).
+// Followers are not let in early: with that, two calls for 64 prompts took 41 us against 25.
 #include "cache_launch.h"
 #include "launch.h"
 
@@ -19,8 +21,11 @@ namespace {
 
 constexpr int kPageThreads = 256;
 constexpr int kGranules = 8192;
-constexpr int kSlotUnroll = 4;
-constexpr int kSlotTile = kPageThreads * kSlotUnroll;    // slots a CTA makes at a time
+constexpr int kSlotUnroll = 4;                           // slots a thread has in flight
+constexpr int kSlotRun = 512;                            // slots in a row that a warp makes
+constexpr int kSlotTile = kPageThreads * kSlotUnroll;    // of page_slots_kernel
+constexpr int kHeldOffsets = 2048;                       // sequences whose offsets a CTA holds
+constexpr int kFewTokens = 4;                            // new tokens a sequence, on average, up to which BY_SET
 
 __device__ __forceinline__ int pages_of(const CacheProblem& p, int len) {
     return (int)(((long long)len + p.page - 1) >> p.page_shift);
@@ -55,16 +60,27 @@ __device__ __forceinline__ int set_need(const CacheProblem& p, const PagesArgs& 
     return max(MODE == kPagesShrink ? before - after : after - before, 0);
 }
 
-template <int MODE>
+// A page number of the list or of a table, or -1 (with the status bit) where it names none.
+__device__ __forceinline__ int valid_entry(const CacheProblem& p, int page, uint32_t* status) {
+    if (page >= 0 && page < p.n_pages) return page;
+    raise_status(status, TGVKV_STATUS_INDEX);
+    return -1;
+}
+
+template <int MODE, bool BY_SET>
 __global__ void __launch_bounds__(kPageThreads)
 pages_kernel(const CacheProblem p, const PagesArgs a, uint32_t* __restrict__ ticket,
              uint32_t* __restrict__ status) {
-    extern __shared__ int prefix[];                      // of every granule, then the total
+    extern __shared__ int prefix[];                      // of every granule
+    __shared__ int offsets[MODE == kPagesAppend && !BY_SET ? kHeldOffsets + 1 : 1];
     __shared__ int warp_sum[kPageThreads / 32];
-    __shared__ int span[2];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int size = a.granule, n_gran = (p.S + size - 1) / size;
+    const int shift = a.granule_shift, size = 1 << shift, n_gran = (p.S + size - 1) >> shift;
+    griddep_wait();
     const int free_now = *a.n_free;
+    const bool held_offsets = MODE == kPagesAppend && !BY_SET && p.B <= kHeldOffsets;
+    if (held_offsets)
+        for (int b = tid; b <= p.B; b += kPageThreads) offsets[b] = a.tok_offsets[b];
     // ---- what every set needs
     int carry = 0;
     bool bad = free_now < 0 || free_now > p.n_pages;
@@ -72,7 +88,7 @@ pages_kernel(const CacheProblem p, const PagesArgs a, uint32_t* __restrict__ tic
         const int g = g0 + tid;
         int sum = 0;
         if (g < n_gran)
-            for (int s = g * size; s < min((g + 1) * size, p.S); ++s) {
+            for (int s = g << shift; s < min((g + 1) << shift, p.S); ++s) {
                 int len, now, held;
                 bad |= !set_lengths<MODE>(p, a, s, len, now);
                 sum += set_need<MODE>(p, a, s, held);
@@ -92,7 +108,7 @@ pages_kernel(const CacheProblem p, const PagesArgs a, uint32_t* __restrict__ tic
             carry += warp_sum[w];
         }
         if (g < n_gran) prefix[g] = base + incl - sum;
-        __syncthreads();
+        if (g0 + kPageThreads < n_gran) __syncthreads();
     }
     bad = __syncthreads_or(bad);
     const int total = carry;
@@ -100,70 +116,98 @@ pages_kernel(const CacheProblem p, const PagesArgs a, uint32_t* __restrict__ tic
     const bool go = !bad && room;
     if (!go && blockIdx.x == 0 && tid == 0)
         raise_status(status, bad || MODE == kPagesShrink ? TGVKV_STATUS_INDEX : TGVKV_STATUS_PAGES);
+    const int threads = gridDim.x * kPageThreads, thread = blockIdx.x * kPageThreads + tid;
+    // the page that the list's i-th taking gets
+    const auto taken = [&](int i) { return a.free_pages[free_now - 1 - i]; };
+    // pages taken by the sets before s
+    const auto before = [&](int s) {
+        int i = prefix[s >> shift], h;
+        for (int e = s >> shift << shift; e < s; ++e) i += set_need<MODE>(p, a, e, h);
+        return i;
+    };
 
-    // ---- the entries that change
-    if (go) {
-        for (int i = blockIdx.x * kPageThreads + tid; i < total; i += gridDim.x * kPageThreads) {
+    if constexpr (BY_SET) {
+        for (int s = thread; s < p.S; s += threads) {
+            const int b = s / p.H_kv, g = s - b * p.H_kv;
+            const int len = a.lens[s], lo = a.tok_offsets[b], hi = a.tok_offsets[b + 1];
+            a.lens_out[s] = go ? len + hi - lo : len;
+            if (!go) continue;
+            int32_t* entries = a.table + (size_t)s * p.max_pages;
+            const int held = pages_of(p, len), i0 = before(s) - held;
+            int at = -1, page = -1;                      // the page of the token before
+            for (int t = lo; t < hi; ++t) {
+                const int j = len + t - lo;
+                if (j >> p.page_shift != at) {
+                    at = j >> p.page_shift;
+                    page = at < held ? entries[at] : taken(i0 + at);
+                    page = valid_entry(p, page, status);
+                    if (at >= held) entries[at] = page;
+                }
+                if (a.slots) a.slots[(size_t)t * p.H_kv + g] = page < 0 ? -1 : page * p.page + (j & (p.page - 1));
+            }
+        }
+        if (a.slots)                                     // tokens that are no sequence's, or all
+            for (long long u = (long long)(go ? a.tok_offsets[p.B] : 0) * p.H_kv + thread;
+                 u < (long long)a.T * p.H_kv; u += threads)
+                a.slots[u] = -1;
+    } else {
+        // ---- the entries that change
+        for (int i = thread; go && i < total; i += threads) {
             const int g = find_last(prefix, 0, n_gran - 1, i);
-            int s = g * size, at = i - prefix[g], held, need;
+            int s = g << shift, at = i - prefix[g], held, need;
             while ((need = set_need<MODE>(p, a, s, held)) <= at) at -= need, ++s;
             int32_t* entry = a.table + (size_t)s * p.max_pages + held + at;
-            int page;
             if (MODE == kPagesShrink) {
-                page = *entry;
+                a.free_pages[free_now + total - 1 - i] = valid_entry(p, *entry, status);
                 *entry = -1;
             } else {
-                page = a.free_pages[free_now - 1 - i];
+                *entry = valid_entry(p, taken(i), status);
             }
-            if (page < 0 || page >= p.n_pages) {
-                raise_status(status, TGVKV_STATUS_INDEX);
-                page = -1;
-            }
-            if (MODE == kPagesShrink) a.free_pages[free_now + total - 1 - i] = page;
-            else *entry = page;
         }
     }
-    if (MODE == kPagesAppend) {
-        for (int s = blockIdx.x * kPageThreads + tid; s < p.S; s += gridDim.x * kPageThreads) {
+    if constexpr (MODE == kPagesAppend && !BY_SET) {
+        for (int s = thread; s < p.S; s += threads) {
             int len, now;
             set_lengths<MODE>(p, a, s, len, now);
             a.lens_out[s] = go ? now : a.lens[s];
         }
-        // ---- the tokens' slots
-        const unsigned n_slots = a.slots ? (unsigned)a.T * p.H_kv : 0u;
-        for (unsigned u0 = blockIdx.x * kSlotTile; u0 < n_slots; u0 += gridDim.x * kSlotTile) {
-            const unsigned u1 = min(u0 + kSlotTile, n_slots) - 1;
-            __syncthreads();
-            if (go) find_span(a.tok_offsets, p.B - 1, u0 / (unsigned)p.H_kv, u1 / (unsigned)p.H_kv, span);
-            __syncthreads();
+        // ---- the tokens' slots: a warp takes kSlotRun in a row, which have few sequences
+        const unsigned n_slots = a.slots ? (unsigned)a.T * p.H_kv : 0u, H = p.H_kv;
+        const int end = go ? a.tok_offsets[p.B] : 0;
+        const int32_t* off = held_offsets ? offsets : a.tok_offsets;
+        for (unsigned u0 = (thread >> 5) * kSlotRun; u0 < n_slots; u0 += (threads >> 5) * kSlotRun) {
+            unsigned t = (u0 + lane) / H, g = u0 + lane - t * H;
+            const unsigned dt = 32u / H, dg = 32u - dt * H;
+            int b = (int)t < end ? find_last(off, 0, p.B - 1, t) : 0;
+#pragma unroll 2
+            for (unsigned u = u0 + lane; u < min(u0 + kSlotRun, n_slots); u += 32 * kSlotUnroll) {
+                int page[kSlotUnroll], in_page[kSlotUnroll];
 #pragma unroll
-            for (int x = 0; x < kSlotUnroll; ++x) {
-                const unsigned u = u0 + x * kPageThreads + tid;
-                if (u > u1) break;
-                int slot = -1;
-                const int t = (int)(u / (unsigned)p.H_kv);
-                if (go && t < a.tok_offsets[p.B]) {
-                    const int b = find_last(a.tok_offsets, span[0], span[1], t);
-                    const int s = b * p.H_kv + (int)(u - (unsigned)t * p.H_kv);
-                    const int len = a.lens[s], j = len + t - a.tok_offsets[b];
-                    const int at = j >> p.page_shift, held = pages_of(p, len);
-                    int page;
-                    if (at >= held) {                    // a page taken just now
-                        int i = prefix[s / size] + at - held, h;
-                        for (int e = s / size * size; e < s; ++e) i += set_need<MODE>(p, a, e, h);
-                        page = a.free_pages[free_now - 1 - i];
-                    } else {
-                        page = a.table[(size_t)s * p.max_pages + at];
+                for (int x = 0; x < kSlotUnroll; ++x) {
+                    page[x] = -1;
+                    in_page[x] = 0;
+                    if ((int)t < end && u + 32 * x < n_slots) {
+                        while ((int)t >= off[b + 1]) ++b;
+                        const int s = b * H + g, len = a.lens[s], j = len + (int)t - off[b];
+                        const int at = j >> p.page_shift, held = pages_of(p, len);
+                        in_page[x] = j & (p.page - 1);
+                        page[x] = at >= held ? taken(before(s) + at - held) : a.table[(size_t)s * p.max_pages + at];
+                        if (page[x] < 0 || page[x] >= p.n_pages) page[x] = -2;
                     }
-                    if (page >= 0 && page < p.n_pages) slot = page * p.page + (j & (p.page - 1));
-                    else raise_status(status, TGVKV_STATUS_INDEX);
+                    t += dt, g += dg;
+                    if (g >= H) g -= H, ++t;
                 }
-                a.slots[u] = slot;
+#pragma unroll
+                for (int x = 0; x < kSlotUnroll; ++x) {
+                    if (u + 32 * x >= n_slots) break;
+                    if (page[x] == -2) raise_status(status, TGVKV_STATUS_INDEX);
+                    a.slots[u + 32 * x] = page[x] < 0 ? -1 : page[x] * p.page + in_page[x];
+                }
             }
         }
     }
     // ---- the list's size, by the CTA that ends last
-    __syncthreads();
+    if (gridDim.x > 1) __syncthreads();
     if (tid == 0) {
         if (gridDim.x > 1) {
             __threadfence();
@@ -181,6 +225,7 @@ __global__ void __launch_bounds__(kPageThreads)
 page_slots_kernel(const CacheProblem p, const PagesArgs a, uint32_t* __restrict__ status) {
     __shared__ int span[2];
     const int tid = threadIdx.x;
+    griddep_wait();
     if (blockIdx.x == 0)
         for (int s = tid; s < p.S; s += kPageThreads) {
             int len, now;
@@ -212,49 +257,49 @@ pages_init_kernel(const CacheProblem p, const PagesArgs a) {
     const long long entries = (long long)p.S * p.max_pages;
     const long long step = (long long)gridDim.x * kPageThreads;
     const long long i0 = (long long)blockIdx.x * kPageThreads + threadIdx.x;
+    griddep_wait();
     for (long long i = i0; i < entries; i += step) a.table[i] = -1;
     for (long long i = i0; i < p.n_pages; i += step) a.free_pages[i] = p.n_pages - 1 - (int)i;
     if (i0 == 0) *a.n_free = p.n_pages;
 }
 
-template <int MODE>
-cudaError_t launch_mode(const CacheProblem& p, PagesArgs a, long long work, uint32_t* ticket,
+// `work`: entries or slots, of which a thread does `each`.
+template <int MODE, bool BY_SET>
+cudaError_t launch_mode(const CacheProblem& p, PagesArgs a, long long work, int each, uint32_t* ticket,
                         uint32_t* status, cudaStream_t stream) {
     const int sms = device_sm_count();
     if (sms <= 0) return cudaErrorInvalidDevice;
-    a.granule = 1;
-    while ((p.S + a.granule - 1) / a.granule > kGranules) a.granule *= 2;
-    const int granules = (p.S + a.granule - 1) / a.granule;
-    const long long blocks = std::min<long long>(std::max<long long>((work + kSlotTile - 1) / kSlotTile, 1), 2 * sms);
-    pages_kernel<MODE><<<(unsigned)blocks, kPageThreads, sizeof(int) * granules, stream>>>(p, a, ticket, status);
-    return cudaGetLastError();
+    a.granule_shift = 0;
+    while ((p.S - 1) >> a.granule_shift >= kGranules) ++a.granule_shift;
+    const int granules = ((p.S - 1) >> a.granule_shift) + 1, tile = kPageThreads * each;
+    const long long blocks = std::min<long long>(std::max<long long>((work + tile - 1) / tile, 1), 4 * sms);
+    return launch_early(pages_kernel<MODE, BY_SET>, dim3((unsigned)blocks), dim3(kPageThreads),
+                        sizeof(int) * granules, stream, p, a, ticket, status);
 }
 
 }  // namespace
 
 cudaError_t launch_pages(const CacheProblem& p, int mode, const PagesArgs& a, uint32_t* ticket,
                          uint32_t* status, cudaStream_t stream) {
-    const long long entries = (long long)p.S * p.max_pages;
-    if (mode == kPagesGrow) return launch_mode<kPagesGrow>(p, a, entries, ticket, status, stream);
-    if (mode == kPagesShrink) return launch_mode<kPagesShrink>(p, a, entries, ticket, status, stream);
-    // an entry for every `page` tokens and set at most, and one
-    return launch_mode<kPagesAppend>(p, a, std::max<long long>((long long)a.T * p.H_kv, p.S), ticket, status,
-                                     stream);
+    const long long entries = (long long)p.S * p.max_pages, slots = (long long)a.T * p.H_kv;
+    if (mode == kPagesGrow) return launch_mode<kPagesGrow, false>(p, a, entries, 1, ticket, status, stream);
+    if (mode == kPagesShrink) return launch_mode<kPagesShrink, false>(p, a, entries, 1, ticket, status, stream);
+    if (a.T <= (long long)kFewTokens * p.B)
+        return launch_mode<kPagesAppend, true>(p, a, p.S, 1, ticket, status, stream);
+    return launch_mode<kPagesAppend, false>(p, a, std::max<long long>(slots, p.S), kSlotRun / 32, ticket, status, stream);
 }
 
 cudaError_t launch_page_slots(const CacheProblem& p, const PagesArgs& a, uint32_t* status,
                               cudaStream_t stream) {
     const long long n = (long long)a.T * p.H_kv;
     const unsigned blocks = (unsigned)std::max<long long>((n + kSlotTile - 1) / kSlotTile, 1);
-    page_slots_kernel<<<blocks, kPageThreads, 0, stream>>>(p, a, status);
-    return cudaGetLastError();
+    return launch_early(page_slots_kernel, dim3(blocks), dim3(kPageThreads), 0, stream, p, a, status);
 }
 
 cudaError_t launch_pages_init(const CacheProblem& p, const PagesArgs& a, cudaStream_t stream) {
     const long long work = std::max<long long>((long long)p.S * p.max_pages, p.n_pages);
     const unsigned blocks = (unsigned)std::min<long long>((work + 1023) / 1024, 4096);
-    pages_init_kernel<<<blocks, kPageThreads, 0, stream>>>(p, a);
-    return cudaGetLastError();
+    return launch_early(pages_init_kernel, dim3(blocks), dim3(kPageThreads), 0, stream, p, a);
 }
 
 }  // namespace tgvkv

@@ -11,6 +11,8 @@
 // flight a thread.  What a row needs beside its arithmetic counts, too (of some 60
 // instructions a 16-byte vector): a thread keeps to one tensor and to one row of its
 // tokens, so that addresses go on by constants.
+#include <numeric>
+
 #include "cache_launch.h"
 #include "launch.h"
 #include "rope.cuh"
@@ -111,10 +113,11 @@ __device__ __forceinline__ void take_angles(const float2* of_token, int unit, in
 
 // A tensor's rows cut into tiles of `tokens` tokens: groups of threads take `rows` of a token's
 // rows at a time, `parts` times, of `side` tokens side by side, and of the `deep` tokens that
-// are `side` apart.
+// are `side` apart.  The tiles of a call's tensors, one tensor after another, go round the
+// CTAs, so that each has as many as any other.
 struct Tiles {
-    int first, blocks;                        // CTAs
-    int count;                                // tiles, which the CTAs take in turn
+    int before;                               // tiles of the tensors before
+    int count;
     int side, deep, tokens, rows, parts;
     unsigned magic;                           // n / rows = n * magic >> 16 for n < 256
 };
@@ -123,8 +126,11 @@ struct Tiles {
 struct Step {
     int tile, part;
 
+    __device__ __forceinline__ explicit Step(const Tiles& ti)
+        : tile((int)((blockIdx.x + gridDim.x - ti.before % gridDim.x) % gridDim.x)), part(0) {}
+
     __device__ __forceinline__ void next(const Tiles& ti) {
-        if (++part == ti.parts) part = 0, tile += ti.blocks;
+        if (++part == ti.parts) part = 0, tile += gridDim.x;
     }
     // every token of the tile is there, kRopeRows deep
     __device__ __forceinline__ bool full(const Tiles& ti, int T) const {
@@ -159,7 +165,7 @@ struct Walk {
         at = base + ((long long)st.tile * ti.tokens + pl.of) * tok + pl.r * head + value;
         side = ti.side * tok;
         part = ti.rows * head;
-        tile = (long long)ti.blocks * ti.tokens * tok - (ti.parts - 1) * part;
+        tile = (long long)gridDim.x * ti.tokens * tok - (ti.parts - 1) * part;
     }
     __device__ __forceinline__ void next(const Tiles& ti, const Step& st) {
         at += st.part + 1 < ti.parts ? part : tile;
@@ -201,19 +207,18 @@ Tiles make_tiles(const Angles& an, int heads, int groups, int sms) {
     return ti;
 }
 
-// Host: CTAs for tensors' tiles, as many as are resident at a time, shared out by their rows.
+// Host: CTAs for tensors' tiles, as many as are resident at a time; *table: angles of the
+// largest tile.
 template <int N>
-unsigned share_blocks(Tiles* (&ti)[N], const int (&heads)[N], int sms) {
-    int all = 0, first = 0;
-    for (int h : heads) all += h;
-    const long long most = (long long)sms * kRopeResident;
-    for (int i = 0; i < N; ++i) {
-        const long long share = (most * heads[i] + all / 2) / all;
-        ti[i]->first = first;
-        ti[i]->blocks = heads[i] > 0 ? (int)std::min<long long>(std::max<long long>(share, 1), ti[i]->count) : 0;
-        first += ti[i]->blocks;
+unsigned count_blocks(Tiles* (&ti)[N], int pairs, int sms, int* table) {
+    long long all = 0;
+    *table = 0;
+    for (Tiles* t : ti) {
+        t->before = (int)(all % ((long long)sms * kRopeResident));    // only its place among them counts
+        all += t->count;
+        *table = std::max(*table, t->tokens * pairs);
     }
-    return (unsigned)first;
+    return (unsigned)std::min<long long>(all, (long long)sms * kRopeResident);
 }
 
 // A unit of a row: W pairs (values i and i + half of a turned part in halves), W values (W / 2
@@ -253,6 +258,7 @@ struct Unit {
 struct RopeCall {
     RopeTensor q, k;
     Tiles q_tiles, k_tiles;
+    int table;                                // angles of the largest tile
     int units, turned;                        // of a row, the turned ones first
 };
 
@@ -265,48 +271,54 @@ rope_kernel(const __grid_constant__ tgvkv_rope_plan plan, const __grid_constant_
     constexpr int P = U::P;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ PlanPairs pp;
-    const bool is_k = blockIdx.x >= (unsigned)a.q_tiles.blocks;
-    const RopeTensor x = is_k ? a.k : a.q;
-    const Tiles ti = is_k ? a.k_tiles : a.q_tiles;
     const int group = threadIdx.x / a.units, unit = threadIdx.x - group * a.units;
     const int half = plan.rot_dim >> 1;
-    const bool turns = unit < a.turned, moves = x.x != x.y;
+    const bool turns = unit < a.turned;
     const int first = U::HALF && !turns ? plan.rot_dim + (unit - a.turned) * W : unit * W;
-    const Place place(ti, group);
-    Step st{(int)blockIdx.x - ti.first, 0};
-    Walk<const uint16_t> from(ti, st, place, x.x, x.x_tok, x.x_head, first);
-    Walk<uint16_t> to(ti, st, place, x.y, x.y_tok, x.y_head, first);
-    U v[kRopeRows];
-    auto load = [&](const Step& of) {
-        for_rows(ti, of, place.left(ti, of, x.heads, an.T), an.T, from, [&](int u, const uint16_t* row) {
-            v[u].x.w = *reinterpret_cast<const Word*>(row);
-            if (U::HALF && turns) v[u].y.w = *reinterpret_cast<const Word*>(row + half);
-        });
-    };
-    load(st);
     pp.take(plan, an.pairs);
+    griddep_launch_dependents();       // the next call's set-up may overlap this one
+    griddep_wait();
     float2* table = reinterpret_cast<float2*>(smem);           // two, in turn
-    for (int flip = 0; st.tile < ti.count; flip ^= 1) {
-        float2* angles = table + flip * (ti.tokens * an.pairs);
-        const int t0 = st.tile * ti.tokens;
-        make_angles<P>(an, pp, t0, min(ti.tokens, an.T - t0), angles);
-        __syncthreads();           // (and all are done with the other table, the next tile's)
-        angles += place.of * an.pairs;
-        const int deeper = ti.side * an.pairs;
-        for (int part = 0; part < ti.parts; ++part) {
-            for_rows(ti, st, place.left(ti, st, x.heads, an.T), an.T, to, [&](int u, uint16_t* row) {
-                if (turns) {
-                    float c[P], s[P];
-                    take_angles<P>(angles + u * deeper, unit, an.pairs, c, s);
-                    v[u].turn(c, s);
-                    if (U::HALF) *reinterpret_cast<Word*>(row + half) = v[u].y.w;
-                }
-                if (turns || moves) *reinterpret_cast<Word*>(row) = v[u].x.w;
+    int flip = 0;
+    for (int tensor = 0; tensor < 2; ++tensor) {
+        const RopeTensor x = tensor ? a.k : a.q;
+        const Tiles ti = tensor ? a.k_tiles : a.q_tiles;
+        Step st(ti);
+        if (st.tile >= ti.count) continue;
+        const bool moves = x.x != x.y;
+        const Place place(ti, group);
+        Walk<const uint16_t> from(ti, st, place, x.x, x.x_tok, x.x_head, first);
+        Walk<uint16_t> to(ti, st, place, x.y, x.y_tok, x.y_head, first);
+        U v[kRopeRows];
+        auto load = [&](const Step& of) {
+            for_rows(ti, of, place.left(ti, of, x.heads, an.T), an.T, from, [&](int u, const uint16_t* row) {
+                v[u].x.w = *reinterpret_cast<const Word*>(row);
+                if (U::HALF && turns) v[u].y.w = *reinterpret_cast<const Word*>(row + half);
             });
-            from.next(ti, st);
-            to.next(ti, st);
-            st.next(ti);
-            load(st);
+        };
+        load(st);
+        for (; st.tile < ti.count; flip ^= 1) {
+            float2* angles = table + flip * a.table;
+            const int t0 = st.tile * ti.tokens;
+            make_angles<P>(an, pp, t0, min(ti.tokens, an.T - t0), angles);
+            __syncthreads();       // (and all are done with the other table, the next tile's)
+            angles += place.of * an.pairs;
+            const int deeper = ti.side * an.pairs;
+            for (int part = 0; part < ti.parts; ++part) {
+                for_rows(ti, st, place.left(ti, st, x.heads, an.T), an.T, to, [&](int u, uint16_t* row) {
+                    if (turns) {
+                        float c[P], s[P];
+                        take_angles<P>(angles + u * deeper, unit, an.pairs, c, s);
+                        v[u].turn(c, s);
+                        if (U::HALF) *reinterpret_cast<Word*>(row + half) = v[u].y.w;
+                    }
+                    if (turns || moves) *reinterpret_cast<Word*>(row) = v[u].x.w;
+                });
+                from.next(ti, st);
+                to.next(ti, st);
+                st.next(ti);
+                load(st);
+            }
         }
     }
 }
@@ -343,6 +355,8 @@ rope_one_kernel(const __grid_constant__ tgvkv_rope_plan plan, const RopeTensor x
         loads += step;
         from += from_step;
     };
+    griddep_launch_dependents();
+    griddep_wait();
 #pragma unroll
     for (int u = 0; u < N; ++u) load(u);
     while (t < an.T) {
@@ -382,18 +396,18 @@ cudaError_t launch_rope_w(const tgvkv_rope_plan& plan, RopeCall a, const Angles&
         if (x->heads != 1) continue;
         const unsigned blocks = (unsigned)std::min<long long>(((long long)an.T + groups - 1) / groups,
                                                               (long long)sms * kOneResident);
-        rope_one_kernel<LAYOUT, W><<<blocks, kRopeThreads, 0, stream>>>(plan, *x, a.units, a.turned, an);
+        const cudaError_t e = launch_early(rope_one_kernel<LAYOUT, W>, dim3(blocks), dim3(kRopeThreads), 0, stream,
+                                           plan, *x, a.units, a.turned, an);
+        if (e != cudaSuccess) return e;
         x->heads = 0;
     }
-    if (a.q.heads + a.k.heads > 0) {
-        a.q_tiles = make_tiles(an, a.q.heads, groups, sms);
-        a.k_tiles = make_tiles(an, a.k.heads, groups, sms);
-        Tiles* tiles[2] = {&a.q_tiles, &a.k_tiles};
-        const unsigned blocks = share_blocks(tiles, {a.q.heads, a.k.heads}, sms);
-        const size_t smem = 2 * sizeof(float2) * std::max(a.q_tiles.tokens, a.k_tiles.tokens) * an.pairs;
-        rope_kernel<LAYOUT, W><<<blocks, kRopeThreads, smem, stream>>>(plan, a, an);
-    }
-    return cudaGetLastError();
+    if (a.q.heads + a.k.heads == 0) return cudaSuccess;
+    a.q_tiles = make_tiles(an, a.q.heads, groups, sms);
+    a.k_tiles = make_tiles(an, a.k.heads, groups, sms);
+    Tiles* tiles[2] = {&a.q_tiles, &a.k_tiles};
+    const unsigned blocks = count_blocks(tiles, an.pairs, sms, &a.table);
+    const size_t smem = 2 * sizeof(float2) * a.table;
+    return launch_early(rope_kernel<LAYOUT, W>, dim3(blocks), dim3(kRopeThreads), smem, stream, plan, a, an);
 }
 
 // ---- turned and stored -------------------------------------------------------------
@@ -401,7 +415,9 @@ struct RopeWrite {
     RopeTensor q;                             // y: q_out; no heads where there are no queries
     RopeTensor k, v;                          // y: none
     Tiles q_tiles, k_tiles, v_tiles;
+    int table;                                // angles of the largest tile
     const int32_t* slots;                     // [T][H_kv]
+    bool early;                               // lets the next call's set-up overlap
 };
 
 // One vector of 8 values into row `row` of a pool (-1: none), `unit` being the vector's number
@@ -431,125 +447,133 @@ rope_write_kernel(const __grid_constant__ tgvkv_rope_plan plan, const __grid_con
     constexpr int PLACED = TWO ? P : 1;       // how the angles lie in their table
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ PlanPairs pp;
-    const bool is_v = blockIdx.x >= (unsigned)a.v_tiles.first;
-    const bool is_q = !is_v && blockIdx.x < (unsigned)a.q_tiles.blocks;
-    const RopeTensor x = is_q ? a.q : is_v ? a.v : a.k;
-    const Tiles ti = is_q ? a.q_tiles : is_v ? a.v_tiles : a.k_tiles;
     const int unit = threadIdx.x % LPR, half = plan.rot_dim >> 1, e0 = 8 * unit;
-    const Place place(ti, threadIdx.x / LPR);
-    Step st{(int)blockIdx.x - ti.first, 0};
-    Walk<const uint16_t> from(ti, st, place, x.x, x.x_tok, x.x_head, e0);
-    Walk<uint16_t> to(ti, st, place, x.y, x.y_tok, x.y_head, e0);          // of queries
-    Values<8> v[kRopeRows], w[kRopeRows];     // the values; the other vector, or the partners
-    int row_of[kRopeRows];                    // pool rows
-    auto load = [&](const Step& of) {
-        const int left = place.left(ti, of, x.heads, an.T);
-#pragma unroll
-        for (int u = 0; u < kRopeRows; ++u) row_of[u] = -1;
-        if (!is_q) {
-            const int at = (of.tile * ti.tokens + place.of) * p.H_kv + of.part * ti.rows + place.r;   // below 2^31
-#pragma unroll
-            for (int u = 0; u < kRopeRows; ++u)
-                if (u * ti.side < left) row_of[u] = a.slots[at + u * ti.side * p.H_kv];
-        }
-        for_rows(ti, of, left, an.T, from, [&](int u, const uint16_t* row) {
-            v[u].w = *reinterpret_cast<const uint4*>(row);
-            if (TWO) {
-                w[u].w = *reinterpret_cast<const uint4*>(row + D / 2);
-            } else if (HALF && !is_v) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int e = e0 + j;
-                    w[u].h[j] = e < plan.rot_dim ? row[e < half ? j + half : j - half] : 0;
-                }
-            }
-        });
-    };
-#pragma unroll
-    for (int u = 0; u < kRopeRows; ++u) v[u].w = w[u].w = make_uint4(0u, 0u, 0u, 0u);
-    load(st);
-    pp.take(plan, an.pairs);
-    float2* table = reinterpret_cast<float2*>(smem);
     const int pool_rows = p.n_pages * p.page;          // below 2^31
-    uint8_t* rows = is_v ? pool.v : pool.k;
-    uint8_t* scales = is_v ? pool.vs : pool.ks;
-    for (int flip = 0; st.tile < ti.count; flip ^= 1) {
-        float2* angles = table + flip * (ti.tokens * an.pairs);
-        if (!is_v) {
-            const int t0 = st.tile * ti.tokens;
-            make_angles<PLACED>(an, pp, t0, min(ti.tokens, an.T - t0), angles);
-            __syncthreads();       // (and all are done with the other table, the next tile's)
-        }
-        angles += place.of * an.pairs;
-        const int deeper = ti.side * an.pairs;
-        for (int part = 0; part < ti.parts; ++part) {
-            const int left = place.left(ti, st, x.heads, an.T);
-            if (!TWO) __syncwarp();            // q_out may be q: a group's rows have been loaded before one is stored
-            for_rows(ti, st, is_v ? 0 : left, an.T, to, [&](int u, uint16_t* row) {
-                const float2* of_token = angles + u * deeper;
-                float c[P], s[P];
-                if constexpr (TWO && HALF) {
-                    take_angles<P>(of_token, unit, an.pairs, c, s);
-                    Unit<LAYOUT, 8> both{v[u], w[u]};
-                    both.turn(c, s);
-                    v[u] = both.x, w[u] = both.y;
-                } else if constexpr (TWO) {
-                    Unit<LAYOUT, 8> one{v[u], v[u]}, two{w[u], w[u]};
-                    if (e0 < plan.rot_dim) {
-                        take_angles<P>(of_token, unit, an.pairs, c, s);
-                        one.turn(c, s);
-                    }
-                    if (e0 + D / 2 < plan.rot_dim) {
-                        take_angles<P>(of_token, unit + D / 16, an.pairs, c, s);
-                        two.turn(c, s);
-                    }
-                    v[u] = one.x, w[u] = two.x;
-                } else {
+    pp.take(plan, an.pairs);
+    if (a.early) griddep_launch_dependents();
+    griddep_wait();
+    float2* table = reinterpret_cast<float2*>(smem);           // two, in turn
+    int flip = 0;
+    // Queries, keys and values, from a tensor on that differs by CTA, as one is bound by
+    // arithmetic and another by memory.
+    for (int i = 0, tensor = blockIdx.x % 3; i < 3; ++i, tensor = tensor == 2 ? 0 : tensor + 1) {
+        const bool is_q = tensor == 0, is_v = tensor == 2;
+        const RopeTensor x = is_q ? a.q : is_v ? a.v : a.k;
+        const Tiles ti = is_q ? a.q_tiles : is_v ? a.v_tiles : a.k_tiles;
+        Step st(ti);
+        if (st.tile >= ti.count) continue;
+        uint8_t* rows = is_v ? pool.v : pool.k;
+        uint8_t* scales = is_v ? pool.vs : pool.ks;
+        const Place place(ti, threadIdx.x / LPR);
+        Walk<const uint16_t> from(ti, st, place, x.x, x.x_tok, x.x_head, e0);
+        Walk<uint16_t> to(ti, st, place, x.y, x.y_tok, x.y_head, e0);          // of queries
+        Values<8> v[kRopeRows], w[kRopeRows];     // the values; the other vector, or the partners
+        int row_of[kRopeRows];                    // pool rows
+        auto load = [&](const Step& of) {
+            const int left = place.left(ti, of, x.heads, an.T);
 #pragma unroll
-                    for (int j = 0; j < P; ++j) {
-                        const int e = HALF ? e0 + j : e0 + 2 * j;
-                        const float2 cs = of_token[e >= plan.rot_dim ? 0 : !HALF ? e >> 1 : e < half ? e : e - half];
-                        c[j] = cs.x, s[j] = cs.y;
-                    }
+            for (int u = 0; u < kRopeRows; ++u) row_of[u] = -1;
+            if (!is_q) {
+                const int at = (of.tile * ti.tokens + place.of) * p.H_kv + of.part * ti.rows + place.r;   // below 2^31
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const uint32_t own = v[u].two[j];
-                        uint32_t z;
-                        if constexpr (HALF) {
-                            // y1 takes the partner's product off, y2 adds it
-                            uint32_t other = w[u].two[j];
-                            if (e0 + 2 * j < half) other ^= 0x00008000u;
-                            if (e0 + 2 * j + 1 < half) other ^= 0x80000000u;
-                            z = pack_bf16x2(fmaf(low_value(own), c[2 * j], low_value(other) * s[2 * j]),
-                                            fmaf(high_value(own), c[(2 * j + 1) % P],
-                                                 high_value(other) * s[(2 * j + 1) % P]));
-                        } else {
-                            const float x1 = low_value(own), x2 = high_value(own);
-                            z = pack_bf16x2(first_of(x1, x2, c[j % P], s[j % P]), second_of(x1, x2, c[j % P], s[j % P]));
-                        }
-                        v[u].two[j] = e0 + 2 * j < plan.rot_dim ? z : own;
+                for (int u = 0; u < kRopeRows; ++u)
+                    if (u * ti.side < left) row_of[u] = a.slots[at + u * ti.side * p.H_kv];
+            }
+            for_rows(ti, of, left, an.T, from, [&](int u, const uint16_t* row) {
+                v[u].w = *reinterpret_cast<const uint4*>(row);
+                if (TWO) {
+                    w[u].w = *reinterpret_cast<const uint4*>(row + D / 2);
+                } else if (HALF && !is_v) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int e = e0 + j;
+                        w[u].h[j] = e < plan.rot_dim ? row[e < half ? j + half : j - half] : 0;
                     }
-                }
-                if (is_q) {
-                    *reinterpret_cast<uint4*>(row) = v[u].w;
-                    if (TWO) *reinterpret_cast<uint4*>(row + D / 2) = w[u].w;
                 }
             });
-            if (!is_q) {
+        };
 #pragma unroll
-                for (int u = 0; u < kRopeRows; ++u) {
-                    if (row_of[u] >= pool_rows) {
-                        if (unit == 0) raise_status(status, TGVKV_STATUS_INDEX);
-                        row_of[u] = -1;
-                    }
-                    store_vector<D, FMT>(v[u].w, rows, scales, row_of[u], unit);
-                    if (TWO) store_vector<D, FMT>(w[u].w, rows, scales, row_of[u], unit + D / 16);
-                }
+        for (int u = 0; u < kRopeRows; ++u) v[u].w = w[u].w = make_uint4(0u, 0u, 0u, 0u);
+        load(st);
+        while (st.tile < ti.count) {
+            float2* angles = table + flip * a.table;
+            if (!is_v) {
+                flip ^= 1;
+                const int t0 = st.tile * ti.tokens;
+                make_angles<PLACED>(an, pp, t0, min(ti.tokens, an.T - t0), angles);
+                __syncthreads();   // (and all are done with the other table, the next tile's)
             }
-            from.next(ti, st);
-            to.next(ti, st);
-            st.next(ti);
-            load(st);
+            angles += place.of * an.pairs;
+            const int deeper = ti.side * an.pairs;
+            for (int part = 0; part < ti.parts; ++part) {
+                const int left = place.left(ti, st, x.heads, an.T);
+                if (!TWO) __syncwarp();            // q_out may be q: a group's rows have been loaded before one is stored
+                for_rows(ti, st, is_v ? 0 : left, an.T, to, [&](int u, uint16_t* row) {
+                    const float2* of_token = angles + u * deeper;
+                    float c[P], s[P];
+                    if constexpr (TWO && HALF) {
+                        take_angles<P>(of_token, unit, an.pairs, c, s);
+                        Unit<LAYOUT, 8> both{v[u], w[u]};
+                        both.turn(c, s);
+                        v[u] = both.x, w[u] = both.y;
+                    } else if constexpr (TWO) {
+                        Unit<LAYOUT, 8> one{v[u], v[u]}, two{w[u], w[u]};
+                        if (e0 < plan.rot_dim) {
+                            take_angles<P>(of_token, unit, an.pairs, c, s);
+                            one.turn(c, s);
+                        }
+                        if (e0 + D / 2 < plan.rot_dim) {
+                            take_angles<P>(of_token, unit + D / 16, an.pairs, c, s);
+                            two.turn(c, s);
+                        }
+                        v[u] = one.x, w[u] = two.x;
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < P; ++j) {
+                            const int e = HALF ? e0 + j : e0 + 2 * j;
+                            const float2 cs = of_token[e >= plan.rot_dim ? 0 : !HALF ? e >> 1 : e < half ? e : e - half];
+                            c[j] = cs.x, s[j] = cs.y;
+                        }
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const uint32_t own = v[u].two[j];
+                            uint32_t z;
+                            if constexpr (HALF) {
+                                // y1 takes the partner's product off, y2 adds it
+                                uint32_t other = w[u].two[j];
+                                if (e0 + 2 * j < half) other ^= 0x00008000u;
+                                if (e0 + 2 * j + 1 < half) other ^= 0x80000000u;
+                                z = pack_bf16x2(fmaf(low_value(own), c[2 * j], low_value(other) * s[2 * j]),
+                                                fmaf(high_value(own), c[(2 * j + 1) % P],
+                                                     high_value(other) * s[(2 * j + 1) % P]));
+                            } else {
+                                const float x1 = low_value(own), x2 = high_value(own);
+                                z = pack_bf16x2(first_of(x1, x2, c[j % P], s[j % P]), second_of(x1, x2, c[j % P], s[j % P]));
+                            }
+                            v[u].two[j] = e0 + 2 * j < plan.rot_dim ? z : own;
+                        }
+                    }
+                    if (is_q) {
+                        *reinterpret_cast<uint4*>(row) = v[u].w;
+                        if (TWO) *reinterpret_cast<uint4*>(row + D / 2) = w[u].w;
+                    }
+                });
+                if (!is_q) {
+#pragma unroll
+                    for (int u = 0; u < kRopeRows; ++u) {
+                        if (row_of[u] >= pool_rows) {
+                            if (unit == 0) raise_status(status, TGVKV_STATUS_INDEX);
+                            row_of[u] = -1;
+                        }
+                        store_vector<D, FMT>(v[u].w, rows, scales, row_of[u], unit);
+                        if (TWO) store_vector<D, FMT>(w[u].w, rows, scales, row_of[u], unit + D / 16);
+                    }
+                }
+                from.next(ti, st);
+                to.next(ti, st);
+                st.next(ti);
+                load(st);
+            }
         }
     }
 }
@@ -563,9 +587,16 @@ cudaError_t launch_write(const CacheProblem& p, const CachePools& pool, const tg
     a.q_tiles = make_tiles(an, a.q.heads, groups, sms);
     a.k_tiles = a.v_tiles = make_tiles(an, p.H_kv, groups, sms);
     Tiles* tiles[3] = {&a.q_tiles, &a.k_tiles, &a.v_tiles};
-    const unsigned blocks = share_blocks(tiles, {a.q.heads, p.H_kv, p.H_kv}, sms);
-    const size_t smem = 2 * sizeof(float2) * std::max(a.q_tiles.tokens, a.k_tiles.tokens) * an.pairs;
-    rope_write_kernel<D, FMT, LAYOUT, TWO><<<blocks, kRopeThreads, smem, stream>>>(plan, a, an, p, pool, status);
+    const unsigned blocks = count_blocks(tiles, an.pairs, sms, &a.table);
+    const size_t smem = 2 * sizeof(float2) * a.table;
+    const auto kernel = rope_write_kernel<D, FMT, LAYOUT, TWO>;
+    // Overlap with the calls before and after pays where the CTAs have one tile each (64 tokens
+    // 5.6 -> 2.7 us, call after call), and costs beside long ones: sixteen prompts stored and
+    // read back 282 us against 255.
+    a.early = a.q_tiles.count + a.k_tiles.count + a.v_tiles.count <= (int)blocks;
+    if (a.early)
+        return launch_early(kernel, dim3(blocks), dim3(kRopeThreads), smem, stream, plan, a, an, p, pool, status);
+    kernel<<<blocks, kRopeThreads, smem, stream>>>(plan, a, an, p, pool, status);
     return cudaGetLastError();
 }
 

@@ -110,9 +110,10 @@ def test_taking_and_giving_back_leaves_the_list_as_it_was(api):
         assert torch.equal(a, b)
 
 
-# granules of 2, 4 and 8 sets, several CTAs
-@pytest.mark.parametrize("B,H_kv,max_pages", [(9001, 1, 3), (5000, 4, 2), (65535, 1, 2)])
-def test_many_sets(api, B, H_kv, max_pages):
+# granules of 2, 4 and 8 sets, several CTAs; few new tokens a sequence, and more
+@pytest.mark.parametrize("B,H_kv,max_pages,most", [(9001, 1, 3, 3), (5000, 4, 2, 2), (65535, 1, 2, 3),
+                                                   (9001, 1, 4, 25), (2050, 5, 3, 20), (65535, 1, 3, 18)])
+def test_many_sets(api, B, H_kv, max_pages, most):
     page, rng = 16, np.random.default_rng(B)
     S = B * H_kv
     desc = api.make_cache_desc(B, H_kv, H_kv, 64, page, S * max_pages, max_pages)
@@ -128,7 +129,7 @@ def test_many_sets(api, B, H_kv, max_pages):
         table[:, j] = np.where(held > j, first + j, -1)
     assert np.array_equal(pages.page_table.cpu().numpy(), table)
     assert int(pages.n_free) == S * max_pages - held.sum()
-    news = rng.integers(0, 4, B)
+    news = rng.integers(0, most + 1, B)
     off, T = np.concatenate([[0], np.cumsum(news)]), int(news.sum())
     slots = torch.empty((T, H_kv), dtype=torch.int32, device="cuda")
     api.tgvkv_pages_append(desc, pages, ints(lens), ints(off), slots, out, ws)
