@@ -588,6 +588,13 @@ def tgvkv_chunk_attention(desc, cache: PagedCache, page_table, lens, q, tok_offs
 
 
 # ---- pages of the cache, handed out on the GPU ---------------------------------
+#
+# These calls and the rotary ones take a few microseconds on the GPU, so what the binding
+# does for a call is kept short (structures are passed as they are, ctypes takes their
+# addresses; one look at each attribute of a tensor).
+
+_I32, _U8, _BF16 = torch.int32, torch.uint8, torch.bfloat16
+
 
 @dataclass
 class PageList:
@@ -608,25 +615,28 @@ def alloc_pages(desc: CacheDesc, device=None) -> PageList:
 
 
 def _page_list(desc, pages: PageList, geo):
-    return ctypes.byref(_lib.PageListPointers(
-        _table(desc, pages.page_table, geo), _dev(pages.free, torch.int32, desc.n_pages, "pages.free"),
-        _dev(pages.n_free, torch.int32, 1, "pages.n_free")))
+    return _lib.PageListPointers(
+        _table(desc, pages.page_table, geo), _dev(pages.free, _I32, desc.n_pages, "pages.free"),
+        _dev(pages.n_free, _I32, 1, "pages.n_free"))
 
 
 def tgvkv_pages_init(desc, pages: PageList, stream=None):
     """An empty table and every page free (see include/tgvkv.h)."""
     geo = _geometry(desc, "tgvkv_pages_init")
-    _check(_lib.load().tgvkv_pages_init(ctypes.byref(desc), _page_list(desc, pages, geo),
-                                        _stream(stream)), "tgvkv_pages_init")
+    rc = _lib.load().tgvkv_pages_init(desc, _page_list(desc, pages, geo), _stream(stream))
+    if rc:
+        raise TgvkvError(rc, "tgvkv_pages_init")
 
 
 def _resize(fn, desc, pages, lens, lens_new, ws, stream):
     geo = _geometry(desc, fn)
     sets = geo[1]
-    _check(getattr(_lib.load(), fn)(
-        ctypes.byref(desc), _page_list(desc, pages, geo), _dev(lens, torch.int32, sets, "lens"),
-        _dev(lens_new, torch.int32, sets, "lens_new"), _dev(ws, torch.uint8, geo[0], "workspace"),
-        _stream(stream)), fn)
+    rc = getattr(_lib.load(), fn)(
+        desc, _page_list(desc, pages, geo), _dev(lens, _I32, sets, "lens"),
+        _dev(lens_new, _I32, sets, "lens_new"), _dev(ws, _U8, geo[0], "workspace"),
+        _stream(stream))
+    if rc:
+        raise TgvkvError(rc, fn)
 
 
 def tgvkv_pages_grow(desc, pages: PageList, lens, lens_new, ws, stream=None):
@@ -643,9 +653,10 @@ def _slot_map(desc, slots):
     """Pointer and tokens of a slot map, int32 [T, H_kv]."""
     if not isinstance(slots, torch.Tensor):
         raise TypeError("slots must be a torch.Tensor")
-    if slots.dim() != 2 or slots.shape[1] != desc.H_kv:
-        raise ValueError(f"slots has shape {tuple(slots.shape)}, expected (tokens, {desc.H_kv})")
-    return _dev(slots, torch.int32, 0, "slots"), slots.shape[0]
+    shape = slots.shape
+    if len(shape) != 2 or shape[1] != desc.H_kv:
+        raise ValueError(f"slots has shape {tuple(shape)}, expected (tokens, {desc.H_kv})")
+    return _dev(slots, _I32, 0, "slots"), shape[0]
 
 
 def tgvkv_pages_append(desc, pages: PageList, lens, tok_offsets, slots, lens_out, ws, n_tokens=None,
@@ -664,21 +675,25 @@ def tgvkv_pages_append(desc, pages: PageList, lens, tok_offsets, slots, lens_out
         if n_tokens is not None and n_tokens != n:
             raise ValueError(f"slots has {n} tokens, n_tokens is {n_tokens}")
         sp = sp or None
-    _check(_lib.load().tgvkv_pages_append(
-        ctypes.byref(desc), _page_list(desc, pages, geo), _dev(lens, torch.int32, sets, "lens"),
-        _dev(tok_offsets, torch.int32, desc.B + 1, "tok_offsets"), n, sp,
-        _dev(lens_out, torch.int32, sets, "lens_out"), _dev(ws, torch.uint8, geo[0], "workspace"),
-        _stream(stream)), "tgvkv_pages_append")
+    rc = _lib.load().tgvkv_pages_append(
+        desc, _page_list(desc, pages, geo), _dev(lens, _I32, sets, "lens"),
+        _dev(tok_offsets, _I32, desc.B + 1, "tok_offsets"), n, sp,
+        _dev(lens_out, _I32, sets, "lens_out"), _dev(ws, _U8, geo[0], "workspace"),
+        _stream(stream))
+    if rc:
+        raise TgvkvError(rc, "tgvkv_pages_append")
 
 
 def tgvkv_page_slots(desc, page_table, lens, tok_offsets, slots, ws, stream=None):
     """The slots of new tokens whose sets hold their pages already."""
     geo = _geometry(desc, "tgvkv_page_slots")
     sp, n = _slot_map(desc, slots)
-    _check(_lib.load().tgvkv_page_slots(
-        ctypes.byref(desc), _table(desc, page_table, geo), _dev(lens, torch.int32, geo[1], "lens"),
-        _dev(tok_offsets, torch.int32, desc.B + 1, "tok_offsets"), n, sp,
-        _dev(ws, torch.uint8, geo[0], "workspace"), _stream(stream)), "tgvkv_page_slots")
+    rc = _lib.load().tgvkv_page_slots(
+        desc, _table(desc, page_table, geo), _dev(lens, _I32, geo[1], "lens"),
+        _dev(tok_offsets, _I32, desc.B + 1, "tok_offsets"), n, sp,
+        _dev(ws, _U8, geo[0], "workspace"), _stream(stream))
+    if rc:
+        raise TgvkvError(rc, "tgvkv_page_slots")
 
 
 # ---- rotary positions ----------------------------------------------------------
@@ -728,24 +743,38 @@ def _positions(plan, t, n):
         raise TypeError("positions must be a torch.Tensor")
     if not t.is_cuda:
         raise ValueError("positions must be a CUDA tensor")
-    if t.dtype is not torch.int32:
+    if t.dtype is not _I32:
         raise TypeError(f"positions has dtype {t.dtype}, expected torch.int32")
-    if not (t.shape == (plan.axes, n) or (plan.axes == 1 and t.shape == (n,))):
-        raise ValueError(f"positions has shape {tuple(t.shape)}, expected ({plan.axes}, {n})")
-    if n > 1 and t.stride(-1) != 1:
+    shape, axes = t.shape, plan.axes
+    if not (shape == (axes, n) or (axes == 1 and shape == (n,))):
+        raise ValueError(f"positions has shape {tuple(shape)}, expected ({axes}, {n})")
+    if axes == 1:
+        if n > 1 and t.stride(-1) != 1:
+            raise ValueError("positions' last dimension must be contiguous")
+        return t.data_ptr(), n
+    strides = t.stride()
+    if n > 1 and strides[1] != 1:
         raise ValueError("positions' last dimension must be contiguous")
-    return t.data_ptr(), t.stride(0) if plan.axes > 1 else n
+    return t.data_ptr(), strides[0]
 
 
 def _rows(t, d, name):
-    """Pointer, (token, head) strides, heads and tokens of a tensor [T, heads, d]."""
+    """Pointer, (token, head) strides, and the shape of a tensor [T, heads, d]."""
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is _BF16:
+        shape = t.shape
+        if len(shape) == 3 and shape[2] == d:
+            n, heads = shape[0], shape[1]
+            tok, head, last = t.stride()
+            if last == 1 and n > 1 and heads > 1:
+                return t.data_ptr(), tok, head, shape
+            if n > 0 and last == 1:    # the stride of a dimension with one entry never matters
+                return t.data_ptr(), tok if n > 1 else heads * d, head if heads > 1 else d, shape
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.dim() != 3:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected (tokens, heads, {d})")
-    heads = t.shape[1]
-    p, tok, head, n = _tokens(t, heads, d, name)
-    return p, tok, head, heads, n
+    p, tok, head, _ = _tokens(t, t.shape[1], d, name)
+    return p, tok, head, t.shape
 
 
 def tgvkv_rope(plan, positions, q, q_out, k=None, k_out=None, mode="forward", stream=None):
@@ -753,22 +782,26 @@ def tgvkv_rope(plan, positions, q, q_out, k=None, k_out=None, mode="forward", st
     and head strides, turned by their tokens' positions, int32 [T] or [axes, T]; an output
     may be its input.  mode: "forward", "gradient" (q, k: the gradients of turned rows) or
     "move" (positions: differences) (see include/tgvkv.h)."""
-    qp, qt, qh, H_q, n = _rows(q, plan.d, "q")
-    op, ot, oh, H_o, n_o = _rows(q_out, plan.d, "q_out")
-    if (H_o, n_o) != (H_q, n):
-        raise ValueError(f"q_out has shape {tuple(q_out.shape)}, q {tuple(q.shape)}")
-    if (k is None) != (k_out is None):
+    d = plan.d
+    qp, qt, qh, q_shape = _rows(q, d, "q")
+    op, ot, oh, shape = _rows(q_out, d, "q_out")
+    if shape != q_shape:
+        raise ValueError(f"q_out has shape {tuple(shape)}, q {tuple(q_shape)}")
+    n, H_q, _ = q_shape
+    kp, kt, kh, H_k, lp, lt, lh = None, 0, 0, 0, None, 0, 0
+    if k is not None and k_out is not None:
+        kp, kt, kh, k_shape = _rows(k, d, "k")
+        lp, lt, lh, shape = _rows(k_out, d, "k_out")
+        if shape != k_shape or k_shape[0] != n:
+            raise ValueError(f"k has shape {tuple(k_shape)}, k_out {tuple(shape)}, q {tuple(q_shape)}")
+        H_k = k_shape[1]
+    elif k is not None or k_out is not None:
         raise TypeError("k and k_out go together")
-    ks = (None, 0, 0, 0, None, 0, 0)
-    if k is not None:
-        kp, kt, kh, H_k, n_k = _rows(k, plan.d, "k")
-        lp, lt, lh, H_l, n_l = _rows(k_out, plan.d, "k_out")
-        if n_k != n or (H_l, n_l) != (H_k, n_k):
-            raise ValueError(f"k has shape {tuple(k.shape)}, k_out {tuple(k_out.shape)}, q {tuple(q.shape)}")
-        ks = (kp, kt, kh, H_k, lp, lt, lh) if H_k else ks
     pp, ps = _positions(plan, positions, n)
-    _check(_lib.load().tgvkv_rope(ctypes.byref(plan), ROPE_MODE[mode], pp, ps, n, qp, qt, qh, H_q, op,
-                                  ot, oh, *ks, _stream(stream)), "tgvkv_rope")
+    rc = _lib.load().tgvkv_rope(plan, ROPE_MODE[mode], pp, ps, n, qp, qt, qh, H_q, op, ot, oh,
+                                kp, kt, kh, H_k, lp, lt, lh, _stream(stream))
+    if rc:
+        raise TgvkvError(rc, "tgvkv_rope")
 
 
 def tgvkv_rope_write(desc, cache: PagedCache, plan, positions, slots, q, k_new, v_new, q_out, ws,
@@ -777,22 +810,31 @@ def tgvkv_rope_write(desc, cache: PagedCache, plan, positions, slots, q, k_new, 
     and v_new stored in the cache's format at the pool rows of slots, int32 [T, H_kv] (any
     token and head strides; q and q_out None: keys and values only) (see include/tgvkv.h)."""
     geo = _geometry(desc, "tgvkv_rope_write")
-    heads, d = desc.H_kv, desc.d
-    kp, kt, kh, n = _tokens(k_new, heads, d, "k_new")
-    vp, vt, vh, nv = _tokens(v_new, heads, d, "v_new")
+    d, heads = desc.d, desc.H_kv
+    kp, kt, kh, shape = _rows(k_new, d, "k_new")
+    vp, vt, vh, v_shape = _rows(v_new, d, "v_new")
+    n = shape[0]
+    if shape[1] != heads or v_shape != shape:
+        raise ValueError(f"k_new has shape {tuple(shape)}, v_new {tuple(v_shape)}, "
+                         f"expected (tokens, {heads}, {d})")
     sp, ns = _slot_map(desc, slots)
-    if (q is None) != (q_out is None):
+    qp, qt, qh, op, ot, oh = None, 0, 0, None, 0, 0
+    if q is not None and q_out is not None:
+        qp, qt, qh, shape = _rows(q, d, "q")
+        op, ot, oh, o_shape = _rows(q_out, d, "q_out")
+        if shape[1] != desc.H_q or o_shape != shape:
+            raise ValueError(f"q has shape {tuple(shape)}, q_out {tuple(o_shape)}, "
+                             f"expected (tokens, {desc.H_q}, {d})")
+    elif q is not None or q_out is not None:
         raise TypeError("q and q_out go together")
-    qs = os = (None, 0, 0, n)
-    if q is not None:
-        qs, os = _tokens(q, desc.H_q, d, "q"), _tokens(q_out, desc.H_q, d, "q_out")
-    if not n == nv == ns == qs[3] == os[3]:
-        raise ValueError(f"tokens: k_new {n}, v_new {nv}, slots {ns}, q {qs[3]}, q_out {os[3]}")
+    if ns != n or shape[0] != n:
+        raise ValueError(f"tokens: k_new {n}, slots {ns}, q {shape[0]}")
     pp, ps = _positions(plan, positions, n)
-    _check(_lib.load().tgvkv_rope_write(
-        ctypes.byref(desc), _pools(desc, cache, geo), ctypes.byref(plan), pp, ps, sp, n, *qs[:3],
-        kp, kt, kh, vp, vt, vh, *os[:3], _dev(ws, torch.uint8, geo[0], "workspace"),
-        _stream(stream)), "tgvkv_rope_write")
+    rc = _lib.load().tgvkv_rope_write(
+        desc, _pools(desc, cache, geo), plan, pp, ps, sp, n, qp, qt, qh, kp, kt, kh, vp, vt, vh,
+        op, ot, oh, _dev(ws, _U8, geo[0], "workspace"), _stream(stream))
+    if rc:
+        raise TgvkvError(rc, "tgvkv_rope_write")
 
 
 def default_scale(d: int) -> float:
