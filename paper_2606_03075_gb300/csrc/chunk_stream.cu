@@ -259,8 +259,9 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
     using Gm = StreamGeom<D, FMT, NB>;
     constexpr int CH = Gm::CH, W = Gm::W;
     constexpr int KS = D / 16, MT = D / 16, KB = CH / 16;
-    // 4-bit floats are multiplied as K 2^-64 and, P having taken V's scales, as P V 2^-64
-    // (fp4_scale): one factor of 2^64 on S and on O in the place of one on every K and V
+    // 4-bit floats are multiplied as K 2^-64 (fp4_scale), and as V's codes 2^-126 against
+    // P 2^62 (by its exponent) with V's scale, P V 2^-64: one factor of 2^64 on S and on O, and
+    // of 2^-62 on the normaliser, in the place of one on every K and V
     constexpr float kUp = FMT == TGVKV_CACHE_FP4 ? 0x1p64f : 1.f;
     if (threadIdx.x == 0) {
         tc::tma_prefetch_desc(&mk);
@@ -550,7 +551,8 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const float ref = m[nb][e] == -INFINITY ? 0.f : m[nb][e];   // nothing seen: weights 0
+                float ref = m[nb][e] == -INFINITY ? 0.f : m[nb][e];   // nothing seen: weights 0
+                if (FMT == TGVKV_CACHE_FP4) ref -= 62.f;              // (kUp)
                 float ps = 0.f;
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb) {
@@ -620,10 +622,9 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
                         const int x = u / UPG;
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            uint32_t sc2 =
+                            const uint32_t sc2 =
                                 (__byte_perm(sw[h][0], sw[h][1], (x << 4) | ((4 + x) << 12)) >> 1) &
                                 0x7F807F80u;
-                            if (FMT == TGVKV_CACHE_FP4) sc2 = __vminu2(sc2 + 0x1F001F00u, 0x7F807F80u);
 #pragma unroll
                             for (int nb = 0; nb < NB; ++nb) pg[nb][h] = bf16x2_mul(pb[nb][h], sc2);
                         }
@@ -674,6 +675,8 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
                     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) o[t][nb][e] *= kUp;
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) l[nb][0] *= 0x1p-62f, l[nb][1] *= 0x1p-62f;
             }
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
