@@ -3,11 +3,13 @@
     python examples/follow_up.py [--config llava15] [--ratio 0.2] [--format int8]
 
 The request of a workload (synthetic inputs) is evicted after its prefill; the
-retained rows go into pages, one sequence per layer, quantised on the way.  Then a
-question arrives: its keys and values are appended and its tokens attend over the
-cache, all layers in one call.  An answer follows, one token at a time.  At the end
-the cache is read back as bf16 rows, and the decode step over those rows must agree
-with the last token's attention over the pages.
+retained rows go into pages taken for them on the GPU, one sequence per layer, quantised
+on the way.  Then a question arrives: its tokens take the pages they lack, its queries and
+keys are turned by their positions, which go on from the whole prompt's (a retained row
+keeps the position it had), its keys and values are stored, and it attends over the cache,
+all layers in one call of each.  An answer follows, one token at a time.  At the end the
+cache is read back as bf16 rows, and the decode step over those rows must agree with the
+last token's attention over the pages.
 """
 import argparse
 import os
@@ -44,37 +46,40 @@ def follow_up(wl, ratio, fmt="int8", question=48, answer=8, seed=0):
                     dev(inp["w"]), ratio, out, ws)
     status(ws)
 
-    # ---- pages for the retained rows and what is still to come: a set is a (layer, KV head)
+    # ---- pages for the retained rows: a set is a (layer, KV head), each of its own length
     L, S = wl.L, wl.L * wl.H_kv
-    kept = out.offsets.diff()
+    kept = out.offsets.diff().to(torch.int32)
     most = int(kept.max()) + question + answer
-    max_pages = -(-most // PAGE)
-    pages = (kept + question + answer + PAGE - 1) // PAGE
-    first = torch.cumsum(pages, 0) - pages
-    column = torch.arange(max_pages, device="cuda")
-    table = torch.where(column < pages[:, None], first[:, None] + column, 0).to(torch.int32)
-    cdesc = api.make_cache_desc(L, wl.H_q, wl.H_kv, wl.d, PAGE, int(pages.sum()), max_pages, fmt)
-    cache = api.alloc_cache(cdesc)
-    cws = api.new_cache_workspace(cdesc)
+    n_pages = int(((kept + question + answer + PAGE - 1) // PAGE).sum())
+    cdesc = api.make_cache_desc(L, wl.H_q, wl.H_kv, wl.d, PAGE, n_pages, -(-most // PAGE), fmt)
+    cache, pages, cws = api.alloc_cache(cdesc), api.alloc_pages(cdesc), api.new_cache_workspace(cdesc)
     lens = torch.zeros(S, dtype=torch.int32, device="cuda")
     grown = torch.empty_like(lens)
-    api.tgvkv_cache_write_rows(cdesc, cache, table, lens, out.k_out, out.v_out, out.offsets, grown, cws)
+    api.tgvkv_pages_grow(cdesc, pages, lens, kept, cws)
+    api.tgvkv_cache_write_rows(cdesc, cache, pages.page_table, lens, out.k_out, out.v_out, out.offsets,
+                               grown, cws)
     lens, grown = grown, lens
 
-    # ---- the question, then the answer's tokens: append, attend (layer l's are rows
-    # tok_offsets[l] .. tok_offsets[l + 1] of q, k and v)
+    # ---- the question, then the answer's tokens: pages, turned keys into them, attention
+    # (layer l's are rows tok_offsets[l] .. tok_offsets[l + 1] of q, k and v)
     gen = torch.Generator("cuda").manual_seed(seed)
+    rope = api.make_rope(wl.d, base=1e6)
+    position = wl.N
 
     def attend(n):
-        nonlocal lens, grown
+        nonlocal lens, grown, position
         qkv = torch.randn((L * n, wl.H_q + 2 * wl.H_kv, wl.d), generator=gen, device="cuda").bfloat16()
         q, k, v = qkv.split([wl.H_q, wl.H_kv, wl.H_kv], dim=1)       # strided views: no copies
         tok_offsets = torch.arange(0, L * n + 1, n, dtype=torch.int32, device="cuda")
-        o = torch.empty((L * n, wl.H_q, wl.d), dtype=torch.bfloat16, device="cuda")
-        api.tgvkv_cache_write(cdesc, cache, table, lens, k, v, tok_offsets, grown, cws)
+        positions = torch.arange(position, position + n, dtype=torch.int32, device="cuda").repeat(L)
+        slots = torch.empty((L * n, wl.H_kv), dtype=torch.int32, device="cuda")
+        turned, o = (torch.empty((L * n, wl.H_q, wl.d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        api.tgvkv_pages_append(cdesc, pages, lens, tok_offsets, slots, grown, cws)
         lens, grown = grown, lens
-        api.tgvkv_chunk_attention(cdesc, cache, table, lens, q, tok_offsets, n, o, cws)
-        return q, o
+        api.tgvkv_rope_write(cdesc, cache, rope, positions, slots, q, k, v, turned, cws)
+        api.tgvkv_chunk_attention(cdesc, cache, pages.page_table, lens, turned, tok_offsets, n, o, cws)
+        position += n
+        return turned, o
 
     attend(question)
     for _ in range(answer):
@@ -85,7 +90,7 @@ def follow_up(wl, ratio, fmt="int8", question=48, answer=8, seed=0):
     offsets[1:] = torch.cumsum(lens, 0)
     k_rows, v_rows = (torch.empty((int(offsets[-1]), wl.d), dtype=torch.bfloat16, device="cuda")
                       for _ in range(2))
-    api.tgvkv_cache_read(cdesc, cache, table, None, offsets, k_rows, v_rows, cws)
+    api.tgvkv_cache_read(cdesc, cache, pages.page_table, None, offsets, k_rows, v_rows, cws)
     status(cws)
     want = torch.empty((L, wl.H_q, wl.d), dtype=torch.float32, device="cuda")
     api.tgvkv_decode(desc, q.contiguous(), k_rows, v_rows, offsets, want, ws)
@@ -102,7 +107,7 @@ def main():
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     ap.add_argument("--config", default="llava15", choices=sorted(synth.WORKLOADS))
     ap.add_argument("--ratio", type=float, default=None, help="retained share (default: the workload's first)")
-    ap.add_argument("--format", default="int8", choices=("bf16", "int8", "int4"))
+    ap.add_argument("--format", default="int8", choices=("bf16", "int8", "int4", "fp4"))
     args = ap.parse_args()
     wl = synth.WORKLOADS[args.config]
     held, rows, err = follow_up(wl, args.ratio or wl.ratios[0], args.format)

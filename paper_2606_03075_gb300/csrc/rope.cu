@@ -11,8 +11,6 @@
 // flight a thread.  What a row needs beside its arithmetic counts, too (of some 60
 // instructions a 16-byte vector): a thread keeps to one tensor and to one row of its
 // tokens, so that addresses go on by constants.
-#include <numeric>
-
 #include "cache_launch.h"
 #include "launch.h"
 #include "rope.cuh"
