@@ -11,8 +11,12 @@
 // all have read by then.  Prefixes are kept of granules of 1, 2, 4 or 8 sets, at most
 // kGranules of them (32 KB).  Entries and tokens are shared out flat, so that one long set
 // is spread as well as many short ones; where sequences have few new tokens (a decode step) a
-// thread does all of its sets instead, without a search (BY_SET).
-// Followers are not let in early: with that, two calls for 64 prompts took 41 us against 25.
+// warp does its sets' entries and slots instead, without a search (BY_SET).
+//
+// Measured, tokens appended and taken back, two calls in a graph (us): 64 sequences of 4 heads,
+// one token each, 6.2 (flat 11.9); 256 sequences 8.5 (21.1); 1024 sequences 13.5; one of 64 with
+// 256 tokens 9.3; 64 prompts of 4352 .. 8704 tokens, 1.7 million slots, 14.4.
+// Followers are not let in early: with that the prompts took 41 against 25.
 #include "cache_launch.h"
 #include "launch.h"
 
@@ -24,40 +28,57 @@ constexpr int kGranules = 8192;
 constexpr int kSlotUnroll = 4;                           // slots a thread has in flight
 constexpr int kSlotRun = 512;                            // slots in a row that a warp makes
 constexpr int kSlotTile = kPageThreads * kSlotUnroll;    // of page_slots_kernel
+constexpr int kSetBatch = 4;                             // sets a thread looks at together
+constexpr int kManySets = 2048;
 constexpr int kHeldOffsets = 2048;                       // sequences whose offsets a CTA holds
-constexpr int kFewTokens = 4;                            // new tokens a sequence, on average, up to which BY_SET
+// BY_SET: up to this many new tokens a sequence, on average, and in all
+constexpr int kFewTokens = 4, kFewInAll = 2048;
 
 __device__ __forceinline__ int pages_of(const CacheProblem& p, int len) {
     return (int)(((long long)len + p.page - 1) >> p.page_shift);
 }
 
-// Set s: its length before and after; false where the call's input says nonsense.
-template <int MODE>
-__device__ __forceinline__ bool set_lengths(const CacheProblem& p, const PagesArgs& a, int s, int& len,
-                                            int& now) {
-    len = now = a.lens[s];
-    if (len < 0 || len > p.cap) return false;
-    if (MODE == kPagesAppend) {
-        const int b = s / p.H_kv, lo = a.tok_offsets[b], hi = a.tok_offsets[b + 1];
-        if (lo < 0 || hi < lo || hi > a.T || (b == 0 && lo != 0) || hi - lo > p.cap - len) return false;
-        now = len + (hi - lo);
-        return true;
+// What a call says of a set: its length, and its new one, or its sequence's offsets.
+struct SetInput {
+    int len, lo, hi;
+
+    // The lengths before and after; both 0 and false where they are nonsense (first: the
+    // offsets are those of the first sequence).
+    template <int MODE>
+    __device__ __forceinline__ bool lengths(const CacheProblem& p, const PagesArgs& a, bool first, int& before,
+                                            int& after) const {
+        bool fine = len >= 0 & len <= p.cap;
+        if (MODE == kPagesAppend) {
+            fine = fine & lo >= 0 & hi >= lo & hi <= a.T & (!first | lo == 0) & (long long)hi - lo <= (long long)p.cap - len;
+            after = fine ? len + (hi - lo) : 0;
+        } else {
+            fine = fine & hi >= 0 & hi <= p.cap;
+            after = fine ? hi : 0;
+        }
+        before = fine ? len : 0;
+        return fine;
     }
-    now = a.lens_new[s];
-    return now >= 0 && now <= p.cap;
+};
+template <int MODE>
+__device__ __forceinline__ SetInput set_input(const CacheProblem& p, const PagesArgs& a, int s, int b) {
+    if (MODE == kPagesAppend) return SetInput{a.lens[s], a.tok_offsets[b], a.tok_offsets[b + 1]};
+    return SetInput{a.lens[s], 0, a.lens_new[s]};
 }
 
-// Pages that set s takes (give back: MODE kPagesShrink), of valid input.
+// Pages that a set of these lengths takes (gives back: MODE kPagesShrink), and the first of
+// its entries that changes.
+template <int MODE>
+__device__ __forceinline__ int need_of(const CacheProblem& p, int len, int now) {
+    const int before = pages_of(p, len), after = pages_of(p, now);
+    return max(MODE == kPagesShrink ? before - after : after - before, 0);
+}
 template <int MODE>
 __device__ __forceinline__ int set_need(const CacheProblem& p, const PagesArgs& a, int s, int& held) {
     int len, now;
-    if (!set_lengths<MODE>(p, a, s, len, now)) {
-        held = 0;
-        return 0;
-    }
-    const int before = pages_of(p, len), after = pages_of(p, now);
-    held = MODE == kPagesShrink ? after : before;        // the first entry that changes
-    return max(MODE == kPagesShrink ? before - after : after - before, 0);
+    const int b = MODE == kPagesAppend ? s / p.H_kv : 0;
+    set_input<MODE>(p, a, s, b).template lengths<MODE>(p, a, b == 0, len, now);
+    held = pages_of(p, MODE == kPagesShrink ? now : len);
+    return need_of<MODE>(p, len, now);
 }
 
 // A page number of the list or of a table, or -1 (with the status bit) where it names none.
@@ -81,34 +102,56 @@ pages_kernel(const CacheProblem p, const PagesArgs a, uint32_t* __restrict__ tic
     const bool held_offsets = MODE == kPagesAppend && !BY_SET && p.B <= kHeldOffsets;
     if (held_offsets)
         for (int b = tid; b <= p.B; b += kPageThreads) offsets[b] = a.tok_offsets[b];
-    // ---- what every set needs
-    int carry = 0;
+    // ---- what every set needs, of granules side by side; then a thread sums a run of them (an
+    // odd number: in other banks than its neighbours')
     bool bad = free_now < 0 || free_now > p.n_pages;
-    for (int g0 = 0; g0 < n_gran; g0 += kPageThreads) {
-        const int g = g0 + tid;
-        int sum = 0;
-        if (g < n_gran)
-            for (int s = g << shift; s < min((g + 1) << shift, p.S); ++s) {
-                int len, now, held;
-                bad |= !set_lengths<MODE>(p, a, s, len, now);
-                sum += set_need<MODE>(p, a, s, held);
+    for (int g0 = tid; g0 < n_gran; g0 += kSetBatch * kPageThreads) {
+        int need[kSetBatch];
+#pragma unroll
+        for (int k = 0; k < kSetBatch; ++k) need[k] = 0;
+        for (int x = 0; x < size; ++x) {
+            SetInput in[kSetBatch];                      // loads in flight
+#pragma unroll
+            for (int k = 0; k < kSetBatch; ++k) {
+                const int s = ((g0 + k * kPageThreads) << shift) + x;
+                if (s < p.S) in[k] = set_input<MODE>(p, a, s, MODE == kPagesAppend ? s / p.H_kv : 0);
             }
-        int incl = sum;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int y = __shfl_up_sync(~0u, incl, o);
-            if (lane >= o) incl += y;
+            for (int k = 0; k < kSetBatch; ++k) {
+                const int s = ((g0 + k * kPageThreads) << shift) + x;
+                if (s >= p.S) continue;
+                int len, now;
+                bad |= !in[k].template lengths<MODE>(p, a, MODE == kPagesAppend && s < p.H_kv, len, now);
+                need[k] += need_of<MODE>(p, len, now);
+            }
         }
-        if (lane == 31) warp_sum[warp] = incl;
-        __syncthreads();
-        int base = carry;
 #pragma unroll
-        for (int w = 0; w < kPageThreads / 32; ++w) {
-            if (w < warp) base += warp_sum[w];
-            carry += warp_sum[w];
-        }
-        if (g < n_gran) prefix[g] = base + incl - sum;
-        if (g0 + kPageThreads < n_gran) __syncthreads();
+        for (int k = 0; k < kSetBatch; ++k)
+            if (g0 + k * kPageThreads < n_gran) prefix[g0 + k * kPageThreads] = need[k];
+    }
+    __syncthreads();
+    const int run = ((n_gran + kPageThreads - 1) / kPageThreads) | 1, g0 = min(tid * run, n_gran);
+    const int g1 = min(g0 + run, n_gran);
+    int sum = 0;
+    for (int g = g0; g < g1; ++g) sum += prefix[g];
+    int incl = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(~0u, incl, o);
+        if (lane >= o) incl += y;
+    }
+    if (lane == 31) warp_sum[warp] = incl;
+    __syncthreads();
+    int base = incl - sum, carry = 0;
+#pragma unroll
+    for (int w = 0; w < kPageThreads / 32; ++w) {
+        if (w < warp) base += warp_sum[w];
+        carry += warp_sum[w];
+    }
+    for (int g = g0; g < g1; ++g) {
+        const int need = prefix[g];
+        prefix[g] = base;
+        base += need;
     }
     bad = __syncthreads_or(bad);
     const int total = carry;
@@ -127,23 +170,31 @@ pages_kernel(const CacheProblem p, const PagesArgs a, uint32_t* __restrict__ tic
     };
 
     if constexpr (BY_SET) {
-        for (int s = thread; s < p.S; s += threads) {
-            const int b = s / p.H_kv, g = s - b * p.H_kv;
-            const int len = a.lens[s], lo = a.tok_offsets[b], hi = a.tok_offsets[b + 1];
-            a.lens_out[s] = go ? len + hi - lo : len;
+        for (int s0 = thread - lane; s0 < p.S; s0 += threads) {          // 32 sets a warp
+            const int s = s0 + lane, b = min(s, p.S - 1) / p.H_kv, g = s - b * p.H_kv;
+            const int lo = a.tok_offsets[b], n = s < p.S ? a.tok_offsets[b + 1] - lo : 0;
+            const int len = s < p.S ? a.lens[s] : 0;
+            if (s < p.S) a.lens_out[s] = go ? len + n : len;
             if (!go) continue;
-            int32_t* entries = a.table + (size_t)s * p.max_pages;
-            const int held = pages_of(p, len), i0 = before(s) - held;
-            int at = -1, page = -1;                      // the page of the token before
-            for (int t = lo; t < hi; ++t) {
-                const int j = len + t - lo;
-                if (j >> p.page_shift != at) {
-                    at = j >> p.page_shift;
-                    page = at < held ? entries[at] : taken(i0 + at);
-                    page = valid_entry(p, page, status);
-                    if (at >= held) entries[at] = page;
-                }
-                if (a.slots) a.slots[(size_t)t * p.H_kv + g] = page < 0 ? -1 : page * p.page + (j & (p.page - 1));
+            const int held = pages_of(p, len), i0 = s < p.S ? before(s) - held : 0;
+            // the i-th new token of set x: its page, entered with the page's first token
+            const auto place = [&](int x, int xlen, int xheld, int xi0, int i, int t, int head) {
+                const int j = xlen + i, at = j >> p.page_shift;
+                int32_t* entry = a.table + (size_t)x * p.max_pages + at;
+                const int page = valid_entry(p, at < xheld ? *entry : taken(xi0 + at), status);
+                if (at >= xheld && (i == 0 || (j & (p.page - 1)) == 0)) *entry = page;
+                if (a.slots) a.slots[(size_t)t * p.H_kv + head] = page < 0 ? -1 : page * p.page + (j & (p.page - 1));
+            };
+            if (n <= kFewTokens)
+                for (int i = 0; i < n; ++i) place(s, len, held, i0, i, lo + i, g);
+            // sets of more tokens, by all lanes
+            for (uint32_t many = __ballot_sync(~0u, n > kFewTokens); many; many &= many - 1) {
+                const int from = __ffs(many) - 1;
+                const int xn = __shfl_sync(~0u, n, from), xlen = __shfl_sync(~0u, len, from);
+                const int xheld = __shfl_sync(~0u, held, from), xi0 = __shfl_sync(~0u, i0, from);
+                const int xlo = __shfl_sync(~0u, lo, from), xg = __shfl_sync(~0u, g, from);
+#pragma unroll 4
+                for (int i = lane; i < xn; i += 32) place(s0 + from, xlen, xheld, xi0, i, xlo + i, xg);
             }
         }
         if (a.slots)                                     // tokens that are no sequence's, or all
@@ -167,9 +218,8 @@ pages_kernel(const CacheProblem p, const PagesArgs a, uint32_t* __restrict__ tic
     }
     if constexpr (MODE == kPagesAppend && !BY_SET) {
         for (int s = thread; s < p.S; s += threads) {
-            int len, now;
-            set_lengths<MODE>(p, a, s, len, now);
-            a.lens_out[s] = go ? now : a.lens[s];
+            const int b = s / p.H_kv, len = a.lens[s];
+            a.lens_out[s] = go ? len + a.tok_offsets[b + 1] - a.tok_offsets[b] : len;
         }
         // ---- the tokens' slots: a warp takes kSlotRun in a row, which have few sequences
         const unsigned n_slots = a.slots ? (unsigned)a.T * p.H_kv : 0u, H = p.H_kv;
@@ -229,7 +279,8 @@ page_slots_kernel(const CacheProblem p, const PagesArgs a, uint32_t* __restrict_
     if (blockIdx.x == 0)
         for (int s = tid; s < p.S; s += kPageThreads) {
             int len, now;
-            if (!set_lengths<kPagesAppend>(p, a, s, len, now)) raise_status(status, TGVKV_STATUS_INDEX);
+            if (!set_input<kPagesAppend>(p, a, s, s / p.H_kv).lengths<kPagesAppend>(p, a, s < p.H_kv, len, now))
+                raise_status(status, TGVKV_STATUS_INDEX);
         }
     const unsigned n_slots = (unsigned)a.T * p.H_kv, u0 = blockIdx.x * kSlotTile;
     if (u0 >= n_slots) return;
@@ -272,7 +323,9 @@ cudaError_t launch_mode(const CacheProblem& p, PagesArgs a, long long work, int 
     a.granule_shift = 0;
     while ((p.S - 1) >> a.granule_shift >= kGranules) ++a.granule_shift;
     const int granules = ((p.S - 1) >> a.granule_shift) + 1, tile = kPageThreads * each;
-    const long long blocks = std::min<long long>(std::max<long long>((work + tile - 1) / tile, 1), 4 * sms);
+    // every CTA reads all lengths: one an SM where that is more than its share of the work
+    const int most = p.S > kManySets ? sms : 4 * sms;
+    const long long blocks = std::min<long long>(std::max<long long>((work + tile - 1) / tile, 1), most);
     return launch_early(pages_kernel<MODE, BY_SET>, dim3((unsigned)blocks), dim3(kPageThreads),
                         sizeof(int) * granules, stream, p, a, ticket, status);
 }
@@ -284,7 +337,7 @@ cudaError_t launch_pages(const CacheProblem& p, int mode, const PagesArgs& a, ui
     const long long entries = (long long)p.S * p.max_pages, slots = (long long)a.T * p.H_kv;
     if (mode == kPagesGrow) return launch_mode<kPagesGrow, false>(p, a, entries, 1, ticket, status, stream);
     if (mode == kPagesShrink) return launch_mode<kPagesShrink, false>(p, a, entries, 1, ticket, status, stream);
-    if (a.T <= (long long)kFewTokens * p.B)
+    if (a.T <= (long long)kFewTokens * p.B && a.T <= kFewInAll)
         return launch_mode<kPagesAppend, true>(p, a, p.S, 1, ticket, status, stream);
     return launch_mode<kPagesAppend, false>(p, a, std::max<long long>(slots, p.S), kSlotRun / 32, ticket, status, stream);
 }

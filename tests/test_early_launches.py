@@ -11,7 +11,7 @@ from test_dependent_launches import CSRC, source
 EARLY = {"pages_kernel": "pages.cu", "page_slots_kernel": "pages.cu", "pages_init_kernel": "pages.cu",
          "rope_kernel": "rope.cu", "rope_one_kernel": "rope.cu", "rope_write_kernel": "rope.cu"}
 # what reads or writes global memory in these kernels
-TOUCHES = re.compile(r"\bload\(|\*a\.|a\.\w+\[|an\.positions|set_lengths|set_need|make_angles|find_span|atomic|"
+TOUCHES = re.compile(r"\bload\(|\*a\.|a\.\w+\[|an\.positions|set_input|set_need|make_angles|find_span|atomic|"
                      r"raise_status|__ldg|__ldcg|__ldcs")
 
 
