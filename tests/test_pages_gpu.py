@@ -99,6 +99,21 @@ def test_a_life_of_requests(api, B, H_kv, page, max_pages):
             rig.lens = new
 
 
+@pytest.mark.parametrize("B,H_kv,page", [(64, 4, 16), (300, 7, 32), (33, 1, 64)])
+def test_longer_sequences_beside_decode_steps(api, B, H_kv, page):
+    """A token for most, none for some, tens for a few: under 4 a sequence in all."""
+    rng = np.random.default_rng(B)
+    rig = Rig(api, B, H_kv, page, 20, B * H_kv * 20)
+    new = rng.integers(0, 5 * page, rig.S)
+    rig.grow(new)
+    rig.lens = new
+    for step in range(4):
+        news = np.where(rng.random(B) < 0.8, 1, 0)
+        news[rng.permutation(B)[:4]] = [3 * B // 2, B // 2, 5, 4]
+        assert news.sum() <= 4 * B
+        rig.append(news, pad=step % 2, slots=step != 3)
+
+
 def test_taking_and_giving_back_leaves_the_list_as_it_was(api):
     rig = Rig(api, 5, 3, 16, 8, 200)
     rig.append([3, 40, 0, 100, 16])
@@ -112,7 +127,8 @@ def test_taking_and_giving_back_leaves_the_list_as_it_was(api):
 
 # granules of 2, 4 and 8 sets, several CTAs; few new tokens a sequence, and more
 @pytest.mark.parametrize("B,H_kv,max_pages,most", [(9001, 1, 3, 3), (5000, 4, 2, 2), (65535, 1, 2, 3),
-                                                   (9001, 1, 4, 25), (2050, 5, 3, 20), (65535, 1, 3, 18)])
+                                                   (9001, 1, 4, 25), (2050, 5, 3, 20), (65535, 1, 3, 18),
+                                                   (9001, 1, 3, 0), (4500, 3, 3, 0)])
 def test_many_sets(api, B, H_kv, max_pages, most):
     page, rng = 16, np.random.default_rng(B)
     S = B * H_kv
@@ -129,7 +145,8 @@ def test_many_sets(api, B, H_kv, max_pages, most):
         table[:, j] = np.where(held > j, first + j, -1)
     assert np.array_equal(pages.page_table.cpu().numpy(), table)
     assert int(pages.n_free) == S * max_pages - held.sum()
-    news = rng.integers(0, most + 1, B)
+    # (0: a few tokens for some, less than 2048 in all)
+    news = rng.integers(0, most + 1, B) if most else np.where(rng.random(B) < 0.05, rng.integers(1, 9, B), 0)
     off, T = np.concatenate([[0], np.cumsum(news)]), int(news.sum())
     slots = torch.empty((T, H_kv), dtype=torch.int32, device="cuda")
     api.tgvkv_pages_append(desc, pages, ints(lens), ints(off), slots, out, ws)

@@ -145,6 +145,47 @@ def test_strides_in_place_and_untouched_neighbours(api):
         assert torch.equal(own[:, H_q + H_k:].view(torch.int16), fused[:, H_q + H_k:].view(torch.int16))
 
 
+def test_axes_that_share_positions_and_spread_strides(api):
+    """Positions expanded over the axes (stride 0), rows far apart."""
+    T, H, d = 21, 3, 64
+    rng = np.random.default_rng(8)
+    x = values(rng, T, H, d)
+    wide = torch.full((T, 5000, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    at = torch.tensor([0, 2400, 4800], device="cuda")
+    wide[:, at] = dev_bf16(R.bf16_bits(x)).view(T, H, d)
+    src = wide[:, ::2400]
+    pos = rng.integers(0, 5000, T)
+    shared = ints(pos).expand(3, T)
+    out = torch.full((T, 5000, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    plan = api.make_rope(d, sections=[4, 14, 14])
+    api.tgvkv_rope(plan, shared, src, out[:, ::2400])
+    got = R.bf16_values(host_bits(out[:, at]))
+    check(got, x, np.broadcast_to(pos, (3, T)), d, sections=[4, 14, 14])
+    out[:, at] = 7.0
+    assert (out == 7).all()
+
+
+@pytest.mark.parametrize("T", [1, 151, 152, 153, 609, 1217, 3650, 7301])
+@pytest.mark.parametrize("H_q,H_k", [(1, 1), (2, 1), (4, 0), (33, 5), (130, 1)])
+def test_tiles_of_every_depth(api, T, H_q, H_k):
+    """Token counts around the tiles' depths and the CTAs' rounds; in place, so that a row
+    turned twice or not at all shows."""
+    d = 64
+    gen = torch.Generator("cuda").manual_seed(T)
+    plan, pos = api.make_rope(d, rot_dim=32), torch.arange(T, dtype=torch.int32, device="cuda") - 7
+    f = torch.tensor(F.frequencies(32), dtype=torch.float64, device="cuda")
+    th = pos.double()[:, None, None] * f
+    c, s = th.cos(), th.sin()
+    xs = [torch.randn((T, h, d), generator=gen, device="cuda").bfloat16() for h in (H_q, H_k)]
+    ys = [x.clone() for x in xs]
+    api.tgvkv_rope(plan, pos, ys[0], ys[0], *((ys[1], ys[1]) if H_k else ()))
+    for x, y in zip(xs, ys):
+        x1, x2 = x[..., :16].double(), x[..., 16:32].double()
+        ref = torch.cat([x1 * c - x2 * s, x2 * c + x1 * s, x[..., 32:].double()], -1)
+        room = torch.cat([(x1.abs() + x2.abs()).repeat(1, 1, 2), torch.zeros_like(ref[..., 32:])], -1) * 2.0 ** -21
+        assert ((y.double() - ref).abs() <= 2.0 ** -8 * ref.abs() + room).all()
+
+
 def test_head_major_rows(api):
     """A prefill's layout [heads][T][d], as a view with the head stride above the token's."""
     T, H, d = 50, 4, 64

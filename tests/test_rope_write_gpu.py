@@ -144,6 +144,27 @@ def test_keys_against_the_reference(api):
     assert torch.equal(cache.v.view(-1, 64)[at], v)
 
 
+@pytest.mark.parametrize("fmt", ["bf16", "int8", "fp4"])
+@pytest.mark.parametrize("H_q,H_kv,d,rot,T", [(8, 1, 64, 64, 5000), (1, 1, 128, 128, 3001), (33, 3, 64, 20, 2500),
+                                             (28, 4, 128, 128, 9000), (130, 2, 128, 64, 700)])
+def test_long_prompts_the_same_as_turning_then_writing(api, fmt, H_q, H_kv, d, rot, T):
+    """CTAs of many tiles of every tensor, queries in place."""
+    desc, cache, ws, table, ln, off, slots, qkv = step(api, fmt, d, H_q, H_kv, [T // 3, 2 * T // 3 + 1], [100, 7], page=64)
+    q, k, v = qkv.split([H_q, H_kv, H_kv], dim=1)
+    pos, plan = torch.arange(qkv.shape[0], dtype=torch.int32, device="cuda"), api.make_rope(d, rot_dim=rot)
+    qo, ko = torch.empty_like(q.contiguous()), torch.empty_like(k.contiguous())
+    api.tgvkv_rope(plan, pos, q, qo, k, ko)
+    api.tgvkv_cache_write(desc, cache, table, ln, ko, v, off, torch.empty_like(ln), ws)
+    want = [t.clone() for t in pools_of(cache)]
+    for t in pools_of(cache):
+        t.view(torch.uint8).fill_(255)
+    api.tgvkv_rope_write(desc, cache, plan, pos, slots, q, k, v, q, ws)
+    assert api.tgvkv_status(ws) == 0
+    assert torch.equal(q.contiguous().view(torch.int16), qo.view(torch.int16))
+    for a, b in zip(pools_of(cache), want):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
 def test_no_tokens(api):
     desc, cache, ws, table, ln, off, slots, qkv = step(api, "int8", 64, 4, 2, [3], [0])
     none = qkv[:0]
