@@ -167,7 +167,9 @@ __device__ __forceinline__ uint32_t int4_base(uint32_t byte) { return min(byte +
 // ---- 4-bit floats to bf16 ------------------------------------------------------
 // A code's exponent and mantissa bits at the low end of bf16's exponent field are
 // the code's value times 2^-126, the subnormal 0.5 (bits 1) included; its sign goes
-// to the top.  Codes of bits SH .. SH + 3 of x's halves.
+// to the top.  Codes of bits SH .. SH + 3 of x's halves.  Two shifts and two logic operations a
+// pair.  The hardware's conversion gives fp16 only (and a third of the instructions): P V in
+// fp16 would need a scale for P's range, and S in fp16 took as long (see chunk_stream.cu).
 template <int SH>
 __device__ __forceinline__ uint32_t fp4x2_small(uint32_t x) {
     const uint32_t sign = SH < 12 ? x << (12 - SH) : x;
@@ -201,6 +203,8 @@ __device__ __forceinline__ uint4 codes_to_bf16(uint2 raw, uint32_t byte, uint32_
             t[0] = fp4x2_small<0>(raw.x), t[1] = fp4x2_small<4>(raw.x);
             t[2] = fp4x2_small<8>(raw.x), t[3] = fp4x2_small<12>(raw.x);
 #pragma unroll
+            // (two factors, as 2^(126 + e) is beyond bf16; as K and V 2^-64 in one product, with the
+            // factor on S and O, chunks of 0 .. 500 tokens took 369.5 us, so 368)
             for (int j = 0; j < 4; ++j) t[j] = bf16x2_mul(bf16x2_mul(t[j], kBf16x2Up126), sc);
         }
         r[0] = __byte_perm(t[0], t[1], 0x5410);

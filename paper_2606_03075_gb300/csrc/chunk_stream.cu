@@ -261,7 +261,11 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
     constexpr int KS = D / 16, MT = D / 16, KB = CH / 16;
     // 4-bit floats are multiplied as K 2^-64 (fp4_scale), and as V's codes 2^-126 against
     // P 2^62 (by its exponent) with V's scale, P V 2^-64: one factor of 2^64 on S and on O, and
-    // of 2^-62 on the normaliser, in the place of one on every K and V
+    // of 2^-62 on the normaliser, in the place of one on every K and V.  One token of 64 x 4 sets
+    // of 4353 .. 8705 slots, 7 rows: 75.8 us (int4 65, int8 87.8); two warps a scheduler in one
+    // chain of dependent steps each.  S in fp16 from the hardware's conversion of codes: a sixth
+    // fewer instructions, but a longer chain, 77.4 against 76.6 us; sixteen warps of half a chunk
+    // 76.7, ten 85; four accumulators a chain 78.
     constexpr float kUp = FMT == TGVKV_CACHE_FP4 ? 0x1p64f : 1.f;
     if (threadIdx.x == 0) {
         tc::tma_prefetch_desc(&mk);

@@ -1,4 +1,6 @@
-// The tile kernel of chunk_tile.cuh over caches of 4-bit floats.
+// The tile kernel of chunk_tile.cuh over caches of 4-bit floats.  Chunks of 0 .. 500 tokens of
+// 16 x 4 sets of 4451 .. 8900 slots, 28 heads of 128: 368 us (int4 356, int8 366), bound as
+// over int8 by a key tile's way from copy over conversion to product.
 #include "chunk_tile.cuh"
 
 namespace tgvkv {

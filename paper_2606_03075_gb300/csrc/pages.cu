@@ -323,7 +323,9 @@ cudaError_t launch_mode(const CacheProblem& p, PagesArgs a, long long work, int 
     a.granule_shift = 0;
     while ((p.S - 1) >> a.granule_shift >= kGranules) ++a.granule_shift;
     const int granules = ((p.S - 1) >> a.granule_shift) + 1, tile = kPageThreads * each;
-    // every CTA reads all lengths: one an SM where that is more than its share of the work
+    // every CTA reads all lengths: one an SM where that is more than its share of the work (a
+    // token each appended and taken back, one and four an SM, us: 4096 sets 13.5 / 15.1, 32768
+    // sets 97 / 111)
     const int most = p.S > kManySets ? sms : 4 * sms;
     const long long blocks = std::min<long long>(std::max<long long>((work + tile - 1) / tile, 1), most);
     return launch_early(pages_kernel<MODE, BY_SET>, dim3((unsigned)blocks), dim3(kPageThreads),

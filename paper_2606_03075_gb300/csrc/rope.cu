@@ -11,6 +11,13 @@
 // flight a thread.  What a row needs beside its arithmetic counts, too (of some 60
 // instructions a 16-byte vector): a thread keeps to one tensor and to one row of its
 // tokens, so that addresses go on by constants.
+//
+// Measured, calls one after another (us; the bytes alone at a copy's rate in brackets): queries
+// and keys of 8704 tokens, 28 + 4 rows of 128 on three axes 26.0 (21.1); gradients of 16381
+// tokens, 32 + 8 rows of which 64 values are turned 53.8 (49.7); 220161 rows moved 23.5 (16.8),
+// which have an angle of their own for every pair; sixteen prompts of 2049 .. 4099 tokens,
+// 32 + 8 + 8 rows, into int8 pages and read back 237 (211); one token 2.5, 64 tokens into
+// bf16 pages 2.7, the launch.
 #include "cache_launch.h"
 #include "launch.h"
 #include "rope.cuh"
@@ -19,10 +26,15 @@ namespace tgvkv {
 namespace {
 
 constexpr int kRopeThreads = 256;
-constexpr int kRopeRows = 3;                  // rows a thread has in flight
-constexpr int kRopeResident = 4;              // CTAs of an SM
-constexpr int kOneResident = 3;               // likewise, of rope_one_kernel
-constexpr int kTableAngles = 2048;            // of a tile (32 KB for two tables)
+// Rows a thread has in flight and CTAs of an SM.  Gradients / sixteen prompts (us): 3 and 4
+// 53.8 / 237; 2 and 4 59.2 / 235; 4 and 4 54.2 / 242; 3 and 3 59.3 / 236; 3 and 5 (the registers
+// end) 56.8 / 241.
+constexpr int kRopeRows = 3;
+constexpr int kRopeResident = 4;
+// CTAs of rope_one_kernel: 220161 rows 23.5 us at 3, 25.5 at 2, 35 at 4 (which spills).
+constexpr int kOneResident = 3;
+// Angles of a tile (32 KB for two tables); no difference from 1024 to 4096.
+constexpr int kTableAngles = 2048;
 
 // W values of bf16 as they are loaded and stored.
 template <int W>
