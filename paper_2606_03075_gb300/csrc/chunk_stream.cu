@@ -264,8 +264,11 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
     // of 2^-62 on the normaliser, in the place of one on every K and V.  One token of 64 x 4 sets
     // of 4353 .. 8705 slots, 7 rows: 75.8 us (int4 65, int8 87.8); two warps a scheduler in one
     // chain of dependent steps each.  S in fp16 from the hardware's conversion of codes: a sixth
-    // fewer instructions, but a longer chain, 77.4 against 76.6 us; sixteen warps of half a chunk
-    // 76.7, ten 85; four accumulators a chain 78.
+    // fewer instructions, but a longer chain, 77.4 against 76.6 us; twelve or sixteen warps of half
+    // a chunk 76.5 and 76.7 (twelve with S in fp16 73.4, for a second form of the loop and a test
+    // of every chunk's scales), ten 85; four accumulators a chain 78; codes shifted right by
+    // products or byte swaps, off the integer pipe, 83.  Shares as even as can be instead of
+    // rounded up: 75.1, but 23.0 against 19.6 for one sequence of 34000 slots (more split sets).
     constexpr float kUp = FMT == TGVKV_CACHE_FP4 ? 0x1p64f : 1.f;
     if (threadIdx.x == 0) {
         tc::tma_prefetch_desc(&mk);

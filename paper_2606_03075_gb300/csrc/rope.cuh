@@ -19,7 +19,8 @@ __device__ __forceinline__ uint32_t turn_of(int p, uint64_t f) {
 // cos and sin of t / 2^32 turns.  The nearest quarter turn is taken off, which leaves an
 // angle of at most pi / 4, x + rest with rest what fp32 loses in 2 pi / 2^32 and in the
 // product; there the Taylor series to x^9 and x^8 are within 2^-28 and 2^-25.  No library
-// call, whose reduction of large arguments is not needed here.
+// call, whose reduction of large arguments is not needed here.  (Two angles an instruction, in
+// f32x2: 28.6 us against 23.4 for 220161 moved rows, as the constants need register pairs.)
 __device__ __forceinline__ void cos_sin_of_turn(uint32_t t, float& c, float& s) {
     const uint32_t quarter = t + 0x20000000u;                // in its top two bits
     const float r = (float)(int)(t << 2);                    // the other 30, signed: 4 / 2^32 turns
