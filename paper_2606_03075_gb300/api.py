@@ -473,9 +473,11 @@ def new_cache_workspace(desc: CacheDesc, device=None) -> torch.Tensor:
 
 def _dev(t, dtype, numel, name):
     """_ptr for one dtype; these calls are short, so the checks are one expression."""
-    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.is_contiguous()
-            and t.numel() >= numel):
-        return t.data_ptr()
+    try:
+        if t.is_cuda and t.dtype is dtype and t.is_contiguous() and t.numel() >= numel:
+            return t.data_ptr()
+    except AttributeError:       # not a tensor
+        pass
     if t is None:
         raise TypeError(f"{name} must be a torch.Tensor")
     return _ptr(t, (dtype,), numel, name)
@@ -491,7 +493,16 @@ def _table(desc, t, geo):
 
 def _pools(desc, cache: PagedCache, geo):
     dtypes = _POOL[desc.format][0]
-    k, v = _ptr(cache.k, dtypes, geo[3], "cache.k"), _ptr(cache.v, dtypes, geo[3], "cache.v")
+    k, v = cache.k, cache.v
+    try:
+        fine = (k.is_cuda and v.is_cuda and k.dtype in dtypes and v.dtype in dtypes and k.is_contiguous()
+                and v.is_contiguous() and k.numel() >= geo[3] and v.numel() >= geo[3])
+    except AttributeError:       # not a tensor
+        fine = False
+    if fine:
+        k, v = k.data_ptr(), v.data_ptr()
+    else:
+        k, v = _ptr(k, dtypes, geo[3], "cache.k"), _ptr(v, dtypes, geo[3], "cache.v")
     if not geo[4]:
         return ctypes.byref(_lib.CachePools(k, v))
     if cache.k_scale is None or cache.v_scale is None:
@@ -615,9 +626,18 @@ def alloc_pages(desc: CacheDesc, device=None) -> PageList:
 
 
 def _page_list(desc, pages: PageList, geo):
-    return _lib.PageListPointers(
-        _table(desc, pages.page_table, geo), _dev(pages.free, _I32, desc.n_pages, "pages.free"),
-        _dev(pages.n_free, _I32, 1, "pages.n_free"))
+    table = pages.page_table
+    try:
+        shape = table.shape
+        if len(shape) == 2 and shape[0] * shape[1] >= geo[2] and shape[1] == desc.max_pages and \
+                table.is_cuda and table.dtype is _I32 and table.is_contiguous():
+            tp = table.data_ptr()
+        else:
+            tp = _table(desc, table, geo)
+    except AttributeError:       # not a tensor
+        tp = _table(desc, table, geo)
+    return _lib.PageListPointers(tp, _dev(pages.free, _I32, desc.n_pages, "pages.free"),
+                                 _dev(pages.n_free, _I32, 1, "pages.n_free"))
 
 
 def tgvkv_pages_init(desc, pages: PageList, stream=None):
@@ -651,9 +671,15 @@ def tgvkv_pages_shrink(desc, pages: PageList, lens, lens_new, ws, stream=None):
 
 def _slot_map(desc, slots):
     """Pointer and tokens of a slot map, int32 [T, H_kv]."""
+    try:
+        shape = slots.shape
+        if (len(shape) == 2 and shape[1] == desc.H_kv and slots.is_cuda and slots.dtype is _I32
+                and slots.is_contiguous()):
+            return slots.data_ptr(), shape[0]
+    except AttributeError:       # not a tensor
+        pass
     if not isinstance(slots, torch.Tensor):
         raise TypeError("slots must be a torch.Tensor")
-    shape = slots.shape
     if len(shape) != 2 or shape[1] != desc.H_kv:
         raise ValueError(f"slots has shape {tuple(shape)}, expected (tokens, {desc.H_kv})")
     return _dev(slots, _I32, 0, "slots"), shape[0]
@@ -739,6 +765,13 @@ def make_rope(d, rot_dim=None, base=10000.0, layout="half", sections=None, scali
 
 def _positions(plan, t, n):
     """Pointer and axis stride of positions, int32 [n] (one axis) or [axes, n]."""
+    try:
+        shape = t.shape
+        if (n and t.is_cuda and t.dtype is _I32 and 1 <= len(shape) <= 2 and shape[-1] == n
+                and t.is_contiguous() and t.numel() == n * plan.axes):
+            return t.data_ptr(), n
+    except AttributeError:       # not a tensor
+        pass
     if not isinstance(t, torch.Tensor):
         raise TypeError("positions must be a torch.Tensor")
     if not t.is_cuda:
@@ -760,15 +793,18 @@ def _positions(plan, t, n):
 
 def _rows(t, d, name):
     """Pointer, (token, head) strides, and the shape of a tensor [T, heads, d]."""
-    if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is _BF16:
-        shape = t.shape
-        if len(shape) == 3 and shape[2] == d:
-            n, heads = shape[0], shape[1]
-            tok, head, last = t.stride()
-            if last == 1 and n > 1 and heads > 1:
-                return t.data_ptr(), tok, head, shape
-            if n > 0 and last == 1:    # the stride of a dimension with one entry never matters
-                return t.data_ptr(), tok if n > 1 else heads * d, head if heads > 1 else d, shape
+    try:
+        if t.is_cuda and t.dtype is _BF16:
+            shape = t.shape
+            n, heads, last = shape
+            if last == d:
+                tok, head, last = t.stride()
+                if last == 1 and n > 1 and heads > 1:
+                    return t.data_ptr(), tok, head, shape
+                if n > 0 and last == 1:    # the stride of a dimension with one entry never matters
+                    return t.data_ptr(), tok if n > 1 else heads * d, head if heads > 1 else d, shape
+    except (AttributeError, ValueError):   # not a tensor, or not of three dimensions
+        pass
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.dim() != 3:
