@@ -35,6 +35,8 @@ constexpr int kRopeResident = 4;
 constexpr int kOneResident = 3;
 // Angles of a tile (32 KB for two tables); no difference from 1024 to 4096.
 constexpr int kTableAngles = 2048;
+// Tiles of a CTA at least where a token's rows are cut into parts for the groups' sake.
+constexpr int kTilesEach = 2;
 
 // W values of bf16 as they are loaded and stored.
 template <int W>
@@ -209,6 +211,15 @@ Tiles make_tiles(const Angles& an, int heads, int groups, int sms) {
     ti.parts = (heads + groups - 1) / groups;
     ti.rows = (heads + ti.parts - 1) / ti.parts;
     ti.side = groups / ti.rows;
+    // Smaller parts of more tokens while more than a quarter of the groups is idle and there are
+    // tiles enough.  200 MB, us: 28 rows of 64 values, 32 turned (42 groups) 77.6, so 65.5; 12 rows of
+    // 128, 64 turned (21 groups) 88.6, so 74.3; 28 rows of 96 (42 groups) 65.3, so 73.6; where an eighth
+    // is idle it costs: 28 rows of 64 (64 groups) 67.4, in parts of 4 rows 74.9.
+    for (int parts = ti.parts + 1; 4 * heads * ti.side < 3 * groups * ti.parts && parts <= std::min(heads, 16); ++parts) {
+        const int rows = (heads + parts - 1) / parts, side = groups / rows, deep = side * kRopeRows;
+        if ((long long)kTilesEach * deep * sms * kRopeResident > an.T || deep * an.pairs > kTableAngles) break;
+        if (side * ti.parts > ti.side * parts) ti.parts = parts, ti.rows = rows, ti.side = side;
+    }
     ti.deep = std::min(std::min(an.T / (ti.side * sms), kTableAngles / (ti.side * an.pairs)), kRopeRows);
     ti.deep = std::max(ti.deep, 1);
     ti.tokens = ti.side * ti.deep;
@@ -231,14 +242,61 @@ unsigned count_blocks(Tiles* (&ti)[N], int pairs, int sms, int* table) {
     return (unsigned)std::min<long long>(all, (long long)sms * kRopeResident);
 }
 
-// A unit of a row: W pairs (values i and i + half of a turned part in halves), W values (W / 2
-// neighbouring pairs), or W values that are copied.
+// How a row is cut into units, a thread each: `turned` of W pairs (halves) or W values
+// (neighbouring pairs), `narrow` of W values that are copied, up to a multiple of 8, and the rest
+// of 8 values that are copied.  (Copies as narrow as the pairs, 200 MB of 8 rows a token in halves:
+// 20 of 80 values turned 231 us, so 106; 24 of 96 130, so 97.)
+struct Cut {
+    int turned, narrow, units;
+
+    template <int LAYOUT, int W>
+    static Cut of(int d, int rot) {
+        const int wide = (rot + 7) / 8 * 8, turned = LAYOUT == TGVKV_ROPE_HALF ? rot / 2 / W : rot / W;
+        const int narrow = (wide - rot) / W;
+        return Cut{turned, narrow, turned + narrow + (d - wide) / 8};
+    }
+};
+
+// A unit of a row: what it holds between its load and its store.
 template <int LAYOUT, int W>
 struct Unit {
     using Word = typename Words<W>::type;
     static constexpr bool HALF = LAYOUT == TGVKV_ROPE_HALF;
     static constexpr int P = HALF ? W : W / 2;
     Values<W> x, y;                           // values; second halves
+    uint4 z;                                  // of a wide copy (W = 8: in x)
+
+    // a thread's kind of unit, and where it begins
+    struct Kind {
+        bool turns, wide;
+        int first;
+
+        __device__ __forceinline__ Kind(const Cut& cut, int unit, int rot) {
+            turns = unit < cut.turned;
+            wide = W < 8 && unit >= cut.turned + cut.narrow;
+            first = HALF && !turns ? rot + (unit - cut.turned) * W : unit * W;
+            if (wide) first = (rot + 7) / 8 * 8 + (unit - cut.turned - cut.narrow) * 8;
+        }
+    };
+    __device__ __forceinline__ void load(const uint16_t* row, const Kind& kind, int half) {
+        if (kind.wide) {
+            z = *reinterpret_cast<const uint4*>(row);
+        } else {
+            x.w = *reinterpret_cast<const Word*>(row);
+            if (HALF && kind.turns) y.w = *reinterpret_cast<const Word*>(row + half);
+        }
+    }
+    // (of a turned unit in halves: the first one, the second is stored where it was turned)
+    __device__ __forceinline__ void store(uint16_t* row, const Kind& kind, bool moves) const {
+        if (kind.wide) {
+            if (moves) *reinterpret_cast<uint4*>(row) = z;
+        } else if (kind.turns || moves) {
+            *reinterpret_cast<Word*>(row) = x.w;
+        }
+    }
+    __device__ __forceinline__ void store_second(uint16_t* row, int half) const {
+        if (HALF) *reinterpret_cast<Word*>(row + half) = y.w;
+    }
 
     __device__ __forceinline__ void turn(const float (&c)[P], const float (&s)[P]) {
         if constexpr (!HALF) {
@@ -269,7 +327,7 @@ struct RopeCall {
     RopeTensor q, k;
     Tiles q_tiles, k_tiles;
     int table;                                // angles of the largest tile
-    int units, turned;                        // of a row, the turned ones first
+    Cut cut;
 };
 
 template <int LAYOUT, int W>
@@ -277,14 +335,12 @@ __global__ void __launch_bounds__(kRopeThreads, kRopeResident)
 rope_kernel(const __grid_constant__ tgvkv_rope_plan plan, const __grid_constant__ RopeCall a,
             const __grid_constant__ Angles an) {
     using U = Unit<LAYOUT, W>;
-    using Word = typename U::Word;
     constexpr int P = U::P;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ PlanPairs pp;
-    const int group = threadIdx.x / a.units, unit = threadIdx.x - group * a.units;
+    const int group = threadIdx.x / a.cut.units, unit = threadIdx.x - group * a.cut.units;
     const int half = plan.rot_dim >> 1;
-    const bool turns = unit < a.turned;
-    const int first = U::HALF && !turns ? plan.rot_dim + (unit - a.turned) * W : unit * W;
+    const typename U::Kind kind(a.cut, unit, plan.rot_dim);
     pp.take(plan, an.pairs);
     griddep_launch_dependents();       // the next call's set-up may overlap this one
     griddep_wait();
@@ -297,14 +353,12 @@ rope_kernel(const __grid_constant__ tgvkv_rope_plan plan, const __grid_constant_
         if (st.tile >= ti.count) continue;
         const bool moves = x.x != x.y;
         const Place place(ti, group);
-        Walk<const uint16_t> from(ti, st, place, x.x, x.x_tok, x.x_head, first);
-        Walk<uint16_t> to(ti, st, place, x.y, x.y_tok, x.y_head, first);
+        Walk<const uint16_t> from(ti, st, place, x.x, x.x_tok, x.x_head, kind.first);
+        Walk<uint16_t> to(ti, st, place, x.y, x.y_tok, x.y_head, kind.first);
         U v[kRopeRows];
         auto load = [&](const Step& of) {
-            for_rows(ti, of, place.left(ti, of, x.heads, an.T), an.T, from, [&](int u, const uint16_t* row) {
-                v[u].x.w = *reinterpret_cast<const Word*>(row);
-                if (U::HALF && turns) v[u].y.w = *reinterpret_cast<const Word*>(row + half);
-            });
+            for_rows(ti, of, place.left(ti, of, x.heads, an.T), an.T, from,
+                     [&](int u, const uint16_t* row) { v[u].load(row, kind, half); });
         };
         load(st);
         for (; st.tile < ti.count; flip ^= 1) {
@@ -316,13 +370,13 @@ rope_kernel(const __grid_constant__ tgvkv_rope_plan plan, const __grid_constant_
             const int deeper = ti.side * an.pairs;
             for (int part = 0; part < ti.parts; ++part) {
                 for_rows(ti, st, place.left(ti, st, x.heads, an.T), an.T, to, [&](int u, uint16_t* row) {
-                    if (turns) {
+                    if (kind.turns) {
                         float c[P], s[P];
                         take_angles<P>(angles + u * deeper, unit, an.pairs, c, s);
                         v[u].turn(c, s);
-                        if (U::HALF) *reinterpret_cast<Word*>(row + half) = v[u].y.w;
+                        v[u].store_second(row, half);
                     }
-                    if (turns || moves) *reinterpret_cast<Word*>(row) = v[u].x.w;
+                    v[u].store(row, kind, moves);
                 });
                 from.next(ti, st);
                 to.next(ti, st);
@@ -336,30 +390,29 @@ rope_kernel(const __grid_constant__ tgvkv_rope_plan plan, const __grid_constant_
 // One row a token: there is nothing to share, every thread computes the angles of its rows.
 template <int LAYOUT, int W>
 __global__ void __launch_bounds__(kRopeThreads, kOneResident)
-rope_one_kernel(const __grid_constant__ tgvkv_rope_plan plan, const RopeTensor x, int units, int turned,
+rope_one_kernel(const __grid_constant__ tgvkv_rope_plan plan, const RopeTensor x, const __grid_constant__ Cut cut,
                 const __grid_constant__ Angles an) {
     using U = Unit<LAYOUT, W>;
-    using Word = typename U::Word;
     constexpr int P = U::P, N = 2;
+    const int units = cut.units;
     const int groups = kRopeThreads / units, group = threadIdx.x / units, unit = threadIdx.x - group * units;
     if (group >= groups) return;
     const int half = plan.rot_dim >> 1;
-    const bool turns = unit < turned, moves = x.x != x.y;
-    const int first = U::HALF && !turns ? plan.rot_dim + (unit - turned) * W : unit * W;
+    const bool moves = x.x != x.y;
+    const typename U::Kind kind(cut, unit, plan.rot_dim);
     uint64_t f[P];
 #pragma unroll
-    for (int i = 0; i < P; ++i) f[i] = plan.turns[turns ? unit * P + i : 0];
+    for (int i = 0; i < P; ++i) f[i] = plan.turns[kind.turns ? unit * P + i : 0];
     const long long step = (long long)gridDim.x * groups;
     long long t = (long long)blockIdx.x * groups + group, loads = t;
-    const uint16_t* from = x.x + t * x.x_tok + first;
-    uint16_t* to = x.y + t * x.y_tok + first;
+    const uint16_t* from = x.x + t * x.x_tok + kind.first;
+    uint16_t* to = x.y + t * x.y_tok + kind.first;
     const long long from_step = step * x.x_tok, to_step = step * x.y_tok;
     U v[N];
     int p[N];
     auto load = [&](int u) {
         if (loads < an.T) {
-            v[u].x.w = *reinterpret_cast<const Word*>(from);
-            if (U::HALF && turns) v[u].y.w = *reinterpret_cast<const Word*>(from + half);
+            v[u].load(from, kind, half);
             p[u] = an.positions[loads];
         }
         loads += step;
@@ -373,7 +426,7 @@ rope_one_kernel(const __grid_constant__ tgvkv_rope_plan plan, const RopeTensor x
 #pragma unroll
         for (int u = 0; u < N; ++u) {
             if (t >= an.T) break;
-            if (turns) {
+            if (kind.turns) {
                 float c[P], s[P];
 #pragma unroll
                 for (int i = 0; i < P; ++i) {
@@ -385,9 +438,9 @@ rope_one_kernel(const __grid_constant__ tgvkv_rope_plan plan, const RopeTensor x
                     for (int i = 0; i < P; ++i) c[i] = an.attention.times(c[i]), s[i] = an.attention.times(s[i]);
                 }
                 v[u].turn(c, s);
-                if (U::HALF) *reinterpret_cast<Word*>(to + half) = v[u].y.w;
+                v[u].store_second(to, half);
             }
-            if (turns || moves) *reinterpret_cast<Word*>(to) = v[u].x.w;
+            v[u].store(to, kind, moves);
             to += to_step;
             t += step;
             load(u);
@@ -397,17 +450,16 @@ rope_one_kernel(const __grid_constant__ tgvkv_rope_plan plan, const RopeTensor x
 
 template <int LAYOUT, int W>
 cudaError_t launch_rope_w(const tgvkv_rope_plan& plan, RopeCall a, const Angles& an, cudaStream_t stream) {
-    const int rot = plan.rot_dim, sms = device_sm_count();
+    const int sms = device_sm_count();
     if (sms <= 0) return cudaErrorInvalidDevice;
-    a.turned = LAYOUT == TGVKV_ROPE_HALF ? rot / 2 / W : rot / W;
-    a.units = a.turned + (plan.d - rot) / W;
-    const int groups = kRopeThreads / a.units;
+    a.cut = Cut::of<LAYOUT, W>(plan.d, plan.rot_dim);
+    const int groups = kRopeThreads / a.cut.units;
     for (RopeTensor* x : {&a.q, &a.k}) {
         if (x->heads != 1) continue;
         const unsigned blocks = (unsigned)std::min<long long>(((long long)an.T + groups - 1) / groups,
                                                               (long long)sms * kOneResident);
         const cudaError_t e = launch_early(rope_one_kernel<LAYOUT, W>, dim3(blocks), dim3(kRopeThreads), 0, stream,
-                                           plan, *x, a.units, a.turned, an);
+                                           plan, *x, a.cut, an);
         if (e != cudaSuccess) return e;
         x->heads = 0;
     }
@@ -444,17 +496,28 @@ __device__ __forceinline__ void store_vector(uint4 w, uint8_t* rows, uint8_t* sc
 }
 
 // The lanes of a group hold a row's vectors of 8 values so that a scale's 4 vectors are in 4
-// neighbouring lanes.  TWO (whole heads in halves, and neighbouring pairs): lane i has vectors
-// i and i + D / 16, which are each other's partners in halves.  Else (part of a head in halves,
-// and parts that end inside a vector) lane i has vector i and loads the partners beside it.
-template <int D, int FMT, int LAYOUT, bool TWO>
+// neighbouring lanes.
+enum Hold {
+    // lane i has vectors i and i + D / 16, which are each other's partners in halves (whole heads
+    // in halves, and neighbouring pairs)
+    kTwo,
+    // lane i has vector i, and loads beside it the vector of its partners (a part of a head in
+    // halves that is a multiple of 16)
+    kPartners,
+    // lane i has vector i, and loads the partners one by one (parts that end inside a vector.
+    // For every part of a head, 200 MB of 32 + 8 + 8 rows, 64 of 128 values turned: bf16 117 us, as
+    // partner vectors 69.5; int8 126, so 74)
+    kSingly
+};
+template <int D, int FMT, int LAYOUT, int HOLD>
 __global__ void __launch_bounds__(kRopeThreads, kRopeResident)
 rope_write_kernel(const __grid_constant__ tgvkv_rope_plan plan, const __grid_constant__ RopeWrite a,
                   const __grid_constant__ Angles an, const CacheProblem p, const CachePools pool,
                   uint32_t* __restrict__ status) {
     constexpr bool HALF = LAYOUT == TGVKV_ROPE_HALF;
+    constexpr bool TWO = HOLD == kTwo;
     constexpr int LPR = TWO ? D / 16 : D / 8, P = HALF ? 8 : 4;
-    constexpr int PLACED = TWO ? P : 1;       // how the angles lie in their table
+    constexpr int PLACED = HOLD == kSingly ? 1 : P;            // how the angles lie in their table
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ PlanPairs pp;
     const int unit = threadIdx.x % LPR, half = plan.rot_dim >> 1, e0 = 8 * unit;
@@ -493,6 +556,9 @@ rope_write_kernel(const __grid_constant__ tgvkv_rope_plan plan, const __grid_con
                 v[u].w = *reinterpret_cast<const uint4*>(row);
                 if (TWO) {
                     w[u].w = *reinterpret_cast<const uint4*>(row + D / 2);
+                } else if (HOLD == kPartners) {
+                    if (!is_v && e0 < plan.rot_dim)
+                        w[u].w = *reinterpret_cast<const uint4*>(e0 < half ? row + half : row - half);
                 } else if (HALF && !is_v) {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
@@ -537,6 +603,19 @@ rope_write_kernel(const __grid_constant__ tgvkv_rope_plan plan, const __grid_con
                             two.turn(c, s);
                         }
                         v[u] = one.x, w[u] = two.x;
+                    } else if constexpr (HOLD == kPartners) {
+                        if (e0 < plan.rot_dim) {
+                            take_angles<P>(of_token, (e0 < half ? e0 : e0 - half) >> 3, an.pairs, c, s);
+                            const uint32_t sign = e0 < half ? 0x80008000u : 0u;
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                // y1 takes the partner's product off, y2 adds it
+                                const uint32_t own = v[u].two[j], other = w[u].two[j] ^ sign;
+                                v[u].two[j] = pack_bf16x2(
+                                    fmaf(low_value(own), c[2 * j], low_value(other) * s[2 * j]),
+                                    fmaf(high_value(own), c[(2 * j + 1) % P], high_value(other) * s[(2 * j + 1) % P]));
+                            }
+                        }
                     } else {
 #pragma unroll
                         for (int j = 0; j < P; ++j) {
@@ -588,18 +667,18 @@ rope_write_kernel(const __grid_constant__ tgvkv_rope_plan plan, const __grid_con
     }
 }
 
-template <int D, int FMT, int LAYOUT, bool TWO>
+template <int D, int FMT, int LAYOUT, int HOLD>
 cudaError_t launch_write(const CacheProblem& p, const CachePools& pool, const tgvkv_rope_plan& plan,
                          RopeWrite a, const Angles& an, uint32_t* status, cudaStream_t stream) {
     const int sms = device_sm_count();
     if (sms <= 0) return cudaErrorInvalidDevice;
-    constexpr int groups = kRopeThreads / (TWO ? D / 16 : D / 8);
+    constexpr int groups = kRopeThreads / (HOLD == kTwo ? D / 16 : D / 8);
     a.q_tiles = make_tiles(an, a.q.heads, groups, sms);
     a.k_tiles = a.v_tiles = make_tiles(an, p.H_kv, groups, sms);
     Tiles* tiles[3] = {&a.q_tiles, &a.k_tiles, &a.v_tiles};
     const unsigned blocks = count_blocks(tiles, an.pairs, sms, &a.table);
     const size_t smem = 2 * sizeof(float2) * a.table;
-    const auto kernel = rope_write_kernel<D, FMT, LAYOUT, TWO>;
+    const auto kernel = rope_write_kernel<D, FMT, LAYOUT, HOLD>;
     // Overlap with the calls before and after pays where the CTAs have one tile each (64 tokens
     // 5.6 -> 2.7 us, call after call), and costs beside long ones: sixteen prompts stored and
     // read back 282 us against 255.
@@ -613,13 +692,15 @@ cudaError_t launch_write(const CacheProblem& p, const CachePools& pool, const tg
 template <int D, int FMT>
 cudaError_t launch_write_by_layout(const CacheProblem& p, const CachePools& pool, const tgvkv_rope_plan& plan,
                                    const RopeWrite& a, const Angles& an, uint32_t* status, cudaStream_t stream) {
-    if (plan.layout == TGVKV_ROPE_HALF)
-        return plan.rot_dim == D
-                   ? launch_write<D, FMT, TGVKV_ROPE_HALF, true>(p, pool, plan, a, an, status, stream)
-                   : launch_write<D, FMT, TGVKV_ROPE_HALF, false>(p, pool, plan, a, an, status, stream);
+    if (plan.layout == TGVKV_ROPE_HALF) {
+        if (plan.rot_dim == D) return launch_write<D, FMT, TGVKV_ROPE_HALF, kTwo>(p, pool, plan, a, an, status, stream);
+        return plan.rot_dim % 16 == 0
+                   ? launch_write<D, FMT, TGVKV_ROPE_HALF, kPartners>(p, pool, plan, a, an, status, stream)
+                   : launch_write<D, FMT, TGVKV_ROPE_HALF, kSingly>(p, pool, plan, a, an, status, stream);
+    }
     return plan.rot_dim % 8 == 0
-               ? launch_write<D, FMT, TGVKV_ROPE_INTERLEAVED, true>(p, pool, plan, a, an, status, stream)
-               : launch_write<D, FMT, TGVKV_ROPE_INTERLEAVED, false>(p, pool, plan, a, an, status, stream);
+               ? launch_write<D, FMT, TGVKV_ROPE_INTERLEAVED, kTwo>(p, pool, plan, a, an, status, stream)
+               : launch_write<D, FMT, TGVKV_ROPE_INTERLEAVED, kSingly>(p, pool, plan, a, an, status, stream);
 }
 
 template <int D>
