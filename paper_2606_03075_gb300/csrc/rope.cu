@@ -205,17 +205,19 @@ __device__ __forceinline__ void for_rows(const Tiles& ti, const Step& st, int le
 // Host: the tiles of the tokens' `heads` rows for CTAs of `groups` groups: kRopeRows tokens deep,
 // less where that would leave SMs without one, or where their angles would exceed
 // kTableAngles.
-Tiles make_tiles(const Angles& an, int heads, int groups, int sms) {
+Tiles make_tiles(const Angles& an, int heads, int groups, int busy, int sms) {
     Tiles ti{};
     if (heads == 0) return ti;
     ti.parts = (heads + groups - 1) / groups;
     ti.rows = (heads + ti.parts - 1) / ti.parts;
     ti.side = groups / ti.rows;
-    // Smaller parts of more tokens while more than a quarter of the groups is idle and there are
-    // tiles enough.  200 MB, us: 28 rows of 64 values, 32 turned (42 groups) 77.6, so 65.5; 12 rows of
-    // 128, 64 turned (21 groups) 88.6, so 74.3; 28 rows of 96 (42 groups) 65.3, so 73.6; where an eighth
-    // is idle it costs: 28 rows of 64 (64 groups) 67.4, in parts of 4 rows 74.9.
-    for (int parts = ti.parts + 1; 4 * heads * ti.side < 3 * groups * ti.parts && parts <= std::min(heads, 16); ++parts) {
+    // Smaller parts of more tokens while less than busy / 16 of the groups are busy and there are
+    // tiles enough.  200 MB in halves (12), us: 28 rows of 64 values, 32 turned (42 groups) 77.6, so
+    // 65.5; 12 rows of 128, 64 turned (21 groups) 88.6, so 74.3; 28 rows of 96 (42 groups) 65.3, so 73.6;
+    // at 13, 12 rows of 128 (32 groups) 67.5, so 74.7.  Neighbouring pairs, whose threads hold half as
+    // many bytes (13): 12 rows of 128 (16 groups) 77.8, so 66.8; at 15, 28 rows 65.3, so 70.
+    for (int parts = ti.parts + 1;
+         16LL * heads * ti.side < (long long)busy * groups * ti.parts && parts <= std::min(heads, 16); ++parts) {
         const int rows = (heads + parts - 1) / parts, side = groups / rows, deep = side * kRopeRows;
         if ((long long)kTilesEach * deep * sms * kRopeResident > an.T || deep * an.pairs > kTableAngles) break;
         if (side * ti.parts > ti.side * parts) ti.parts = parts, ti.rows = rows, ti.side = side;
@@ -387,7 +389,8 @@ rope_kernel(const __grid_constant__ tgvkv_rope_plan plan, const __grid_constant_
     }
 }
 
-// One row a token: there is nothing to share, every thread computes the angles of its rows.
+// One row a token, of every tensor: there is nothing to share, every thread computes the angles of
+// its rows.
 template <int LAYOUT, int W>
 __global__ void __launch_bounds__(kRopeThreads, kOneResident)
 rope_one_kernel(const __grid_constant__ tgvkv_rope_plan plan, const RopeTensor x, const __grid_constant__ Cut cut,
@@ -454,8 +457,10 @@ cudaError_t launch_rope_w(const tgvkv_rope_plan& plan, RopeCall a, const Angles&
     if (sms <= 0) return cudaErrorInvalidDevice;
     a.cut = Cut::of<LAYOUT, W>(plan.d, plan.rot_dim);
     const int groups = kRopeThreads / a.cut.units;
+    // Rows of one head go with another tensor's of more: one launch, and 200 MB of 12 + 1 rows of
+    // 96 values, 64 turned, 73.5 us, not 94 in two that overlap (of 128, all turned, 70 and 67).
     for (RopeTensor* x : {&a.q, &a.k}) {
-        if (x->heads != 1) continue;
+        if (x->heads != 1 || a.q.heads > 1 || a.k.heads > 1) continue;
         const unsigned blocks = (unsigned)std::min<long long>(((long long)an.T + groups - 1) / groups,
                                                               (long long)sms * kOneResident);
         const cudaError_t e = launch_early(rope_one_kernel<LAYOUT, W>, dim3(blocks), dim3(kRopeThreads), 0, stream,
@@ -464,8 +469,9 @@ cudaError_t launch_rope_w(const tgvkv_rope_plan& plan, RopeCall a, const Angles&
         x->heads = 0;
     }
     if (a.q.heads + a.k.heads == 0) return cudaSuccess;
-    a.q_tiles = make_tiles(an, a.q.heads, groups, sms);
-    a.k_tiles = make_tiles(an, a.k.heads, groups, sms);
+    constexpr int busy = LAYOUT == TGVKV_ROPE_HALF ? 12 : 13;
+    a.q_tiles = make_tiles(an, a.q.heads, groups, busy, sms);
+    a.k_tiles = make_tiles(an, a.k.heads, groups, busy, sms);
     Tiles* tiles[2] = {&a.q_tiles, &a.k_tiles};
     const unsigned blocks = count_blocks(tiles, an.pairs, sms, &a.table);
     const size_t smem = 2 * sizeof(float2) * a.table;
@@ -673,8 +679,8 @@ cudaError_t launch_write(const CacheProblem& p, const CachePools& pool, const tg
     const int sms = device_sm_count();
     if (sms <= 0) return cudaErrorInvalidDevice;
     constexpr int groups = kRopeThreads / (HOLD == kTwo ? D / 16 : D / 8);
-    a.q_tiles = make_tiles(an, a.q.heads, groups, sms);
-    a.k_tiles = a.v_tiles = make_tiles(an, p.H_kv, groups, sms);
+    a.q_tiles = make_tiles(an, a.q.heads, groups, 12, sms);
+    a.k_tiles = a.v_tiles = make_tiles(an, p.H_kv, groups, 12, sms);
     Tiles* tiles[3] = {&a.q_tiles, &a.k_tiles, &a.v_tiles};
     const unsigned blocks = count_blocks(tiles, an.pairs, sms, &a.table);
     const size_t smem = 2 * sizeof(float2) * a.table;
