@@ -14,10 +14,10 @@
 //
 // Measured, calls one after another (us; the bytes alone at a copy's rate in brackets): queries
 // and keys of 8704 tokens, 28 + 4 rows of 128 on three axes 26.0 (21.1); gradients of 16381
-// tokens, 32 + 8 rows of which 64 values are turned 53.8 (49.7); 220161 rows moved 23.5 (16.8),
+// tokens, 32 + 8 rows of which 64 values are turned 53.2 (49.7); 220161 rows moved 23.3 (16.8),
 // which have an angle of their own for every pair; sixteen prompts of 2049 .. 4099 tokens,
-// 32 + 8 + 8 rows, into int8 pages and read back 237 (211); one token 2.5, 64 tokens into
-// bf16 pages 2.7, the launch.
+// 32 + 8 + 8 rows, into int8 pages and read back 236 (211); one token 2.5, 64 tokens into
+// bf16 pages 3.5, the launch.
 #include "cache_launch.h"
 #include "launch.h"
 #include "rope.cuh"
@@ -686,7 +686,7 @@ cudaError_t launch_write(const CacheProblem& p, const CachePools& pool, const tg
     const size_t smem = 2 * sizeof(float2) * a.table;
     const auto kernel = rope_write_kernel<D, FMT, LAYOUT, HOLD>;
     // Overlap with the calls before and after pays where the CTAs have one tile each (64 tokens
-    // 5.6 -> 2.7 us, call after call), and costs beside long ones: sixteen prompts stored and
+    // 5.6 -> 3.5 us, call after call), and costs beside long ones: sixteen prompts stored and
     // read back 282 us against 255.
     a.early = a.q_tiles.count + a.k_tiles.count + a.v_tiles.count <= (int)blocks;
     if (a.early)
