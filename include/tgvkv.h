@@ -633,8 +633,9 @@ int tgvkv_rope_init(tgvkv_rope_plan* plan, const tgvkv_rope_desc* desc);
  * elements, multiples of 8, each tensor with its own, 16-byte aligned.  An output may
  * be its own input (the same pointer and strides); other overlaps are not allowed.
  * k and k_out may be NULL with H_k = 0.  positions: int32, of axis a and token t at
- * a * pos_stride + t (pos_stride 0: the axes share them).  mode: TGVKV_ROPE_FORWARD, GRADIENT or MOVE.  n_tokens = 0
- * launches nothing.  No workspace: nothing is reported by the device. */
+ * a * pos_stride + t (pos_stride 0: the axes share them).  mode: TGVKV_ROPE_FORWARD,
+ * GRADIENT or MOVE.  n_tokens = 0 launches nothing.  No workspace: nothing is reported by
+ * the device. */
 int tgvkv_rope(const tgvkv_rope_plan* plan, int32_t mode, const int32_t* positions,
                int64_t pos_stride, int64_t n_tokens, const uint16_t* q, int64_t q_tok_stride,
                int64_t q_head_stride, int32_t H_q, uint16_t* q_out, int64_t q_out_tok_stride,
