@@ -14,7 +14,7 @@
 //
 // Measured, calls one after another (us; the bytes alone at a copy's rate in brackets): queries
 // and keys of 8704 tokens, 28 + 4 rows of 128 on three axes 26.0 (21.1); gradients of 16381
-// tokens, 32 + 8 rows of which 64 values are turned 53.2 (49.7); 220161 rows moved 23.3 (16.8),
+// tokens, 32 + 8 rows of which 64 values are turned 53.2 (49.7); 220161 rows moved 22.6 (16.8),
 // which have an angle of their own for every pair; sixteen prompts of 2049 .. 4099 tokens,
 // 32 + 8 + 8 rows, into int8 pages and read back 236 (211); one token 2.5, 64 tokens into
 // bf16 pages 3.5, the launch.
@@ -67,8 +67,6 @@ struct Angles {
     int axes;
     int pairs;                                // of a row
     int T;                                    // tokens
-
-    __device__ __forceinline__ bool plain() const { return attention.hi == 1.f && attention.lo == 0.f; }
 };
 
 // A plan's pairs in shared memory: lanes that read different ones of a parameter wait for one
@@ -101,8 +99,8 @@ __device__ __forceinline__ void make_angles(const Angles& an, const PlanPairs& p
         const int32_t* of_token = an.positions + t0 + t;
         const int p = an.axes == 1 ? *of_token : of_token[pp.axis[i] * an.pos_stride];
         float c, s;
-        cos_sin_of_turn(turn_of(p, pp.turns[i]), c, s);
-        if (!an.plain()) c = an.attention.times(c), s = an.attention.times(s);
+        if (an.attention.one()) cos_sin_of_turn<true>(turn_of(p, pp.turns[i]), an.attention, c, s);
+        else cos_sin_of_turn<false>(turn_of(p, pp.turns[i]), an.attention, c, s);
         table[t * an.pairs + angle_place<P>(i, an.pairs)] = make_float2(c, s);
         t += dt, i += di;
         if (i >= an.pairs) i -= an.pairs, ++t;
@@ -390,8 +388,8 @@ rope_kernel(const __grid_constant__ tgvkv_rope_plan plan, const __grid_constant_
 }
 
 // One row a token, of every tensor: there is nothing to share, every thread computes the angles of
-// its rows.
-template <int LAYOUT, int W>
+// its rows.  ONE: the attention factor is 1 (220161 rows 22.6 us, with a branch 27).
+template <int LAYOUT, int W, bool ONE>
 __global__ void __launch_bounds__(kRopeThreads, kOneResident)
 rope_one_kernel(const __grid_constant__ tgvkv_rope_plan plan, const RopeTensor x, const __grid_constant__ Cut cut,
                 const __grid_constant__ Angles an) {
@@ -434,11 +432,7 @@ rope_one_kernel(const __grid_constant__ tgvkv_rope_plan plan, const RopeTensor x
 #pragma unroll
                 for (int i = 0; i < P; ++i) {
                     const int pi = an.axes == 1 ? p[u] : an.positions[plan.axis[unit * P + i] * an.pos_stride + t];
-                    cos_sin_of_turn(turn_of(pi, f[i]), c[i], s[i]);
-                }
-                if (!an.plain()) {
-#pragma unroll
-                    for (int i = 0; i < P; ++i) c[i] = an.attention.times(c[i]), s[i] = an.attention.times(s[i]);
+                    cos_sin_of_turn<ONE>(turn_of(pi, f[i]), an.attention, c[i], s[i]);
                 }
                 v[u].turn(c, s);
                 v[u].store_second(to, half);
@@ -463,8 +457,9 @@ cudaError_t launch_rope_w(const tgvkv_rope_plan& plan, RopeCall a, const Angles&
         if (x->heads != 1 || a.q.heads > 1 || a.k.heads > 1) continue;
         const unsigned blocks = (unsigned)std::min<long long>(((long long)an.T + groups - 1) / groups,
                                                               (long long)sms * kOneResident);
-        const cudaError_t e = launch_early(rope_one_kernel<LAYOUT, W>, dim3(blocks), dim3(kRopeThreads), 0, stream,
-                                           plan, *x, a.cut, an);
+        auto kernel = rope_one_kernel<LAYOUT, W, false>;
+        if (an.attention.one()) kernel = rope_one_kernel<LAYOUT, W, true>;
+        const cudaError_t e = launch_early(kernel, dim3(blocks), dim3(kRopeThreads), 0, stream, plan, *x, a.cut, an);
         if (e != cudaSuccess) return e;
         x->heads = 0;
     }
