@@ -177,6 +177,7 @@ __device__ __forceinline__ uint32_t fp4x2_small(uint32_t x) {
     return (sign & 0x80008000u) | (rest & 0x01C001C0u);
 }
 constexpr uint32_t kBf16x2Up126 = 0x7E807E80u;   // 2^126, which takes the codes to their values
+constexpr uint32_t kBf16x2Up62 = 0x5E805E80u;    // 2^62
 
 __device__ __forceinline__ uint32_t both(uint32_t half) { return half | (half << 16); }
 

@@ -260,9 +260,11 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
     constexpr int CH = Gm::CH, W = Gm::W;
     constexpr int KS = D / 16, MT = D / 16, KB = CH / 16;
     // 4-bit floats are multiplied as K 2^-64 (fp4_scale), and as V's codes 2^-126 against
-    // P 2^62 (by its exponent) with V's scale, P V 2^-64: one factor of 2^64 on S and on O, and
-    // of 2^-62 on the normaliser, in the place of one on every K and V.  One token of 64 x 4 sets
-    // of 4353 .. 8705 slots, 7 rows: 75.8 us (int4 65, int8 87.8); two warps a scheduler in one
+    // P 2^62 (kBf16x2Up62) with V's scale, P V 2^-64: one factor of 2^64 on S and on O, and one on
+    // every two weights, in the place of one on every K and V.  (The 2^62 as 62 on the exponent
+    // rounds m - 62: two warps' weights were off against each other by up to 2^4 at logits of 2^25,
+    // and small values lost from 2^30 on.)  One token of 64 x 4 sets
+    // of 4353 .. 8705 slots, 7 rows: 77.0 us (int4 65, int8 87.8); two warps a scheduler in one
     // chain of dependent steps each.  S in fp16 from the hardware's conversion of codes: a sixth
     // fewer instructions, but a longer chain, 77.4 against 76.6 us; twelve or sixteen warps of half
     // a chunk 76.5 and 76.7 (twelve with S in fp16 73.4, for a second form of the loop and a test
@@ -558,8 +560,7 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                float ref = m[nb][e] == -INFINITY ? 0.f : m[nb][e];   // nothing seen: weights 0
-                if (FMT == TGVKV_CACHE_FP4) ref -= 62.f;              // (kUp)
+                const float ref = m[nb][e] == -INFINITY ? 0.f : m[nb][e];   // nothing seen: weights 0
                 float ps = 0.f;
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb) {
@@ -590,6 +591,10 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
             for (int nb = 0; nb < NB; ++nb) {
                 pb[nb][0] = movm_trans(pack_bf16x2(sc[kb][nb][0], sc[kb][nb][1]));
                 pb[nb][1] = movm_trans(pack_bf16x2(sc[kb][nb][2], sc[kb][nb][3]));
+                if (FMT == TGVKV_CACHE_FP4) {              // (kUp)
+                    pb[nb][0] = bf16x2_mul(pb[nb][0], kBf16x2Up62);
+                    pb[nb][1] = bf16x2_mul(pb[nb][1], kBf16x2Up62);
+                }
             }
             if (FMT == TGVKV_CACHE_BF16) {
 #pragma unroll
@@ -682,8 +687,6 @@ chunk_stream_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constan
                     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) o[t][nb][e] *= kUp;
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) l[nb][0] *= 0x1p-62f, l[nb][1] *= 0x1p-62f;
             }
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
