@@ -8,6 +8,7 @@ provides device memory and streams.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import functools
 import math
@@ -134,10 +135,22 @@ def tgvkv_workspace_init(desc: Desc, ws: torch.Tensor, stream=None):
            "tgvkv_workspace_init")
 
 
+def _named(device):
+    """The device of an allocating call: the current one where none is named."""
+    return "cuda" if device is None else device
+
+
+def _on(t):
+    """The tensor's device made the current one: what a call starts runs on the current
+    device and its stream."""
+    return torch.cuda.device(t.device) if t.is_cuda else contextlib.nullcontext()
+
+
 def new_workspace(desc: Desc, device=None) -> torch.Tensor:
     """A zeroed workspace tensor (uint8) for this problem."""
-    ws = torch.empty(tgvkv_workspace_size(desc), dtype=torch.uint8, device=device or "cuda")
-    tgvkv_workspace_init(desc, ws)
+    ws = torch.empty(tgvkv_workspace_size(desc), dtype=torch.uint8, device=_named(device))
+    with _on(ws):
+        tgvkv_workspace_init(desc, ws)
     return ws
 
 
@@ -258,7 +271,7 @@ class EvictOutputs:
 
 
 def alloc_outputs(desc: Desc, ratio: float, device=None) -> EvictOutputs:
-    dev = device or "cuda"
+    dev = _named(device)
     rows = tgvkv_retained_rows(desc, ratio)
     L, Hkv = desc.L, desc.H_kv
     return EvictOutputs(
@@ -421,7 +434,7 @@ class PagedCache:
 
 def alloc_cache(desc: CacheDesc, device=None) -> PagedCache:
     """Pools of this descriptor's geometry and format (uninitialised)."""
-    dev = device or "cuda"
+    dev = _named(device)
     dtypes, row = _POOL[desc.format]
     pool = (desc.n_pages, desc.page_size, row(desc.d))
     scale = (desc.n_pages, desc.page_size, desc.d // CACHE_GROUP)
@@ -466,8 +479,9 @@ def tgvkv_cache_workspace_init(desc: CacheDesc, ws: torch.Tensor, stream=None):
 
 def new_cache_workspace(desc: CacheDesc, device=None) -> torch.Tensor:
     """A workspace tensor (uint8) for the paged-cache calls, its status clear."""
-    ws = torch.empty(tgvkv_cache_workspace_size(desc), dtype=torch.uint8, device=device or "cuda")
-    tgvkv_cache_workspace_init(desc, ws)
+    ws = torch.empty(tgvkv_cache_workspace_size(desc), dtype=torch.uint8, device=_named(device))
+    with _on(ws):
+        tgvkv_cache_workspace_init(desc, ws)
     return ws
 
 
@@ -617,11 +631,12 @@ class PageList:
 def alloc_pages(desc: CacheDesc, device=None) -> PageList:
     """A descriptor's page list: an empty table, every page of the pool free."""
     _geometry(desc, "alloc_pages")
-    new = dict(dtype=torch.int32, device=device or "cuda")
+    new = dict(dtype=torch.int32, device=_named(device))
     pages = PageList(torch.empty((desc.B * desc.H_kv, desc.max_pages), **new),
                      torch.empty(desc.n_pages, **new), torch.empty(1, **new))
     if pages.free.is_cuda:
-        tgvkv_pages_init(desc, pages)
+        with _on(pages.free):
+            tgvkv_pages_init(desc, pages)
     return pages
 
 
