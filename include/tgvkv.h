@@ -583,8 +583,9 @@ int tgvkv_page_slots(const tgvkv_cache_desc* desc, const int32_t* page_table, co
  *
  * Angles are right for every int32 position: a plan holds f_i / (2 pi), computed in
  * double, as a 64-bit fraction, so that an integer product leaves p f_i mod 1, to 2^-31
- * turns and 2^-51 of p f_i.  c, s and the products are fp32, the result is rounded to
- * bf16 once. */
+ * turns and 2^-47 of p f_i (pow and the operations around it in double, for bases up to
+ * 10^8 after scaling and, PARTS, low (factor - 1) <= 3 (high - low) and 2 low <= high).
+ * c, s and the products are fp32, the result is rounded to bf16 once. */
 #define TGVKV_ROPE_HALF        0
 #define TGVKV_ROPE_INTERLEAVED 1
 
