@@ -510,9 +510,9 @@ int tgvkv_chunk_attention(const tgvkv_cache_desc* desc, const tgvkv_cache_pools*
  * back leaves the list as it was.  A page belongs to one set; a prefix shared by hand
  * is safe as long as no call shortens a set to less than it.
  *
- * A call does all it is asked or nothing: with a length outside [0, max_pages *
- * page_size], offsets that do not start at 0, decrease or exceed n_tokens, a set that
- * would outgrow its table row, or n_free outside [0, n_pages], it sets
+ * A call on a list does all it is asked or nothing: with a length outside [0,
+ * max_pages * page_size], offsets that do not start at 0, decrease or exceed n_tokens,
+ * a set that would outgrow its table row, or n_free outside [0, n_pages], it sets
  * TGVKV_STATUS_INDEX and changes no table, no list (lens_out = lens, every slot -1);
  * likewise TGVKV_STATUS_PAGES where fewer pages are free than it would take.  An
  * entry of the stack, or of a table that gives pages back, that names no page of the
@@ -554,7 +554,9 @@ int tgvkv_pages_append(const tgvkv_cache_desc* desc, const tgvkv_page_list* page
 
 /* The slots of tgvkv_pages_append for sets that hold their pages already, of a table
  * from wherever: page_table int32 [B * H_kv][max_pages].  A slot whose page is not in
- * the pool, or past the table, is -1 (TGVKV_STATUS_INDEX). */
+ * the pool, or past the table, is -1 (TGVKV_STATUS_INDEX), and so is every slot of a set
+ * whose length is outside [0, max_pages * page_size] and of a sequence whose offsets
+ * decrease, exceed n_tokens or, the first one's, do not start at 0; the others are as ever. */
 int tgvkv_page_slots(const tgvkv_cache_desc* desc, const int32_t* page_table, const int32_t* lens,
                      const int32_t* tok_offsets, int64_t n_tokens, int32_t* slots,
                      void* workspace, void* stream);

@@ -42,17 +42,21 @@ __device__ __forceinline__ int pages_of(const CacheProblem& p, int len) {
 struct SetInput {
     int len, lo, hi;
 
-    // The lengths before and after; both 0 and false where they are nonsense (first: the
-    // offsets are those of the first sequence).
+    // A length, and (of new tokens) offsets, that may be; first: the offsets are those of the
+    // first sequence.
+    __device__ __forceinline__ bool sound(const CacheProblem& p, const PagesArgs& a, bool first) const {
+        return len >= 0 & len <= p.cap & lo >= 0 & hi >= lo & hi <= a.T & (!first | lo == 0);
+    }
+    // The lengths before and after; both 0 and false where they are nonsense.
     template <int MODE>
     __device__ __forceinline__ bool lengths(const CacheProblem& p, const PagesArgs& a, bool first, int& before,
                                             int& after) const {
-        bool fine = len >= 0 & len <= p.cap;
+        bool fine;
         if (MODE == kPagesAppend) {
-            fine = fine & lo >= 0 & hi >= lo & hi <= a.T & (!first | lo == 0) & (long long)hi - lo <= (long long)p.cap - len;
+            fine = sound(p, a, first) & (long long)hi - lo <= (long long)p.cap - len;
             after = fine ? len + (hi - lo) : 0;
         } else {
-            fine = fine & hi >= 0 & hi <= p.cap;
+            fine = len >= 0 & len <= p.cap & hi >= 0 & hi <= p.cap;
             after = fine ? hi : 0;
         }
         before = fine ? len : 0;
@@ -296,8 +300,10 @@ page_slots_kernel(const CacheProblem p, const PagesArgs a, uint32_t* __restrict_
         if (t >= a.tok_offsets[0] && t < a.tok_offsets[p.B]) {
             const int b = find_last(a.tok_offsets, span[0], span[1], t);
             const int s = b * p.H_kv + (int)(u - (unsigned)t * p.H_kv);
-            const long long j = (long long)clamp_len(a.lens[s], p.cap) + t - a.tok_offsets[b];
-            slot = pool_row(p, a.table, s, j, status);
+            const SetInput in = set_input<kPagesAppend>(p, a, s, b);
+            // (nonsense is reported by the first CTA; a set that would outgrow its row has the slots in it)
+            if (in.sound(p, a, b == 0) && t >= in.lo && t < in.hi)
+                slot = pool_row(p, a.table, s, (long long)in.len + t - in.lo, status);
         }
         a.slots[u] = slot;
     }
