@@ -64,8 +64,8 @@ constexpr int kStreamRows = 32;        // query rows a set that it takes at most
 // the registers it does without the tile kernel's 128-row tiles and the bf16 copy of
 // integer codes: 256 sets of 20 rows over 2051 .. 4101 slots, tile kernel against it
 // (us): d = 64 bf16 50 / 45, int8 62 / 45, int4 62 / 42 (32 rows 50 / 49, 62 / 54,
-// 61 / 50); d = 128 bf16 75 / 78, int8 80 / 78, int4 82 / 60; 4-bit floats: d = 64 65 / 45
-// (32 rows 64 / 54), d = 128 84 / 67.
+// 61 / 50); d = 128 bf16 75 / 78, int8 80 / 78, int4 82 / 60; 4-bit floats: d = 64 65 / 46
+// (32 rows 64 / 55), d = 128 84 / 67.
 __host__ __device__ constexpr int stream_rows(int d, int format) {
     return d == 64 ? kStreamRows : format == TGVKV_CACHE_BF16 ? 16 : 24;
 }

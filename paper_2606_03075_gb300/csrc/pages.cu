@@ -31,7 +31,11 @@ constexpr int kSlotTile = kPageThreads * kSlotUnroll;    // of page_slots_kernel
 constexpr int kSetBatch = 4;                             // sets a thread looks at together
 constexpr int kManySets = 2048;
 constexpr int kHeldOffsets = 2048;                       // sequences whose offsets a CTA holds
-// BY_SET: up to this many new tokens a sequence, on average, and in all
+// BY_SET: up to this many new tokens a sequence, on average, and in all.  Appended and taken back,
+// heads of 4, in a graph, by set / flat (us): a token each, 64 sequences 6.8 / 13.7, 1024 13.3 /
+// 27.9, 4096 30.2 / 54.5; four each, 1024 sequences 14.1 / 24.9.  But a warp has its sequence's
+// tokens to itself: all of them in one of 1024 sequences, 256 16.9 / 19.9, 1024 28.2 / 20.5, 2048
+// 43.6 / 20.3, 4096 71.8 / 19.8 (which the host cannot know: the bound in all is for that).
 constexpr int kFewTokens = 4, kFewInAll = 2048;
 
 __device__ __forceinline__ int pages_of(const CacheProblem& p, int len) {
