@@ -31,9 +31,9 @@ def turns(rot, base, scaling="none", factor=1.0, original=0, low=1.0, high=32.0)
     b = D(base)
     if scaling == "base" and rot > 2:
         b *= D(factor) ** (D(rot) / D(rot - 2))
-    out = []
+    log, out = b.ln(), []
     for i in range(rot // 2):
-        f = (b.ln() * D(-2 * i) / D(rot)).exp()
+        f = (log * D(-2 * i) / D(rot)).exp()
         if scaling == "linear":
             f /= D(factor)
         if scaling == "parts":
